@@ -328,6 +328,86 @@ int blockgtq_decode_attn_noalloc(const bgtq_config* cfg, const void* d_layout, i
                                  const int32_t* d_ctx_len, int32_t max_ctx, const bgtq_cache* cache, float* d_out,
                                  int32_t n_splits, void* stream);
 
+/* ---- Cache rows read back ---------------------------------------------------
+ * The inverse of blockgtq_quantize_append: rows of the packed cache as plain
+ * post-RoPE keys and values, dequantized and rotated back to the natural dims,
+ *   k_hat = Pi_g^T (r_g C[code] / sqrt(d_g)) per same-rate group,
+ *   v_hat = Pi_V^T (n_V C[code] / sqrt(d_h)).
+ * For handing a context to code that wants plain rows, moving it to a cache of
+ * another layout, or checking what a cache holds.  Async on `stream`; no
+ * allocation, no workspace.
+ * layer in [0, n_layers) or -1 for all layers.
+ * Rows d_read_pos[b] .. d_read_pos[b] + n_rows - 1 of sequence b go to d_k_out
+ * and d_v_out in out_dtype (BGTQ_FP32 or BGTQ_BF16, rounded once), laid out as
+ * the append's inputs: [batch][n_rows][n_kv_heads][head_dim], with a leading
+ * [n_layers] for layer == -1; 16-byte aligned (EINVAL otherwise).  Either may
+ * be NULL (not both): only the other one is read.
+ * d_read_pos: int32 [batch].  d_ctx_len: int32 [batch], or NULL.  A row at a
+ * position below 0, at or past the capacity, or at or past d_ctx_len[b] is not
+ * read and its outputs are left as they were.
+ * n_rows in [0, capacity] (ECAPACITY above). */
+int blockgtq_dequantize_rows(const bgtq_config* cfg, const void* d_layout, int32_t layer, const bgtq_cache* cache,
+                             int32_t n_rows, const int32_t* d_read_pos, const int32_t* d_ctx_len, void* d_k_out,
+                             void* d_v_out, int32_t out_dtype, void* stream);
+
+/* ---- Cross attention over the packed cache --------------------------------------
+ * n_q query rows per sequence, each attending every row [0, d_ctx_len[b]) of
+ * the sequence's packed cache (no causal mask): a decoder's queries against an
+ * encoder's states, of another length, that were packed once
+ * (blockgtq_quantize_append) and are read by every pass.  n_q runs from a
+ * single generated token to whole prompts; the key axis is split where there
+ * are few query rows.  Two launches on `stream` at most; no allocation, no
+ * state in the workspace, so the call can be captured in a HIP graph.
+ * layer in [0, n_layers) or -1 for all layers.
+ * d_q: [batch][n_q][n_kv_heads*group][128] in in_dtype, with a leading
+ *      [n_layers] for layer == -1.  d_out: the same shape in out_dtype
+ *      (BGTQ_FP32 or BGTQ_BF16, rounded once).  Both and the workspace 16-byte
+ *      aligned (EINVAL otherwise).
+ * d_ctx_len: device int32 [batch], each in [0, max_ctx]; a sequence of no rows
+ *      gets zeros, one whose length is outside [0, max_ctx] gets NaN.  What the
+ *      cache holds behind a sequence's rows (not a number or infinite radii
+ *      too) does not enter its outputs.
+ * max_ctx: host-side bound (<= capacity, ECAPACITY otherwise).
+ * n_splits: 0 = heuristic, else the splits of the key axis (1 .. 4096).
+ * d_workspace: blockgtq_cross_workspace_bytes bytes, any contents; calls that
+ *      share it must not overlap in time.
+ * EUNSUPPORTED above 2^24 query rows (layers x batch x n_q x heads) a call. */
+int blockgtq_cross_workspace_bytes(const bgtq_config* cfg, int32_t n_layers_in_call, int32_t n_q, int32_t n_splits,
+                                   int32_t max_ctx, size_t* bytes_out);
+int blockgtq_cross_attn(const bgtq_config* cfg, const void* d_layout, int32_t layer, const void* d_q, int32_t n_q,
+                        const int32_t* d_ctx_len, int32_t max_ctx, const bgtq_cache* cache, void* d_out,
+                        int32_t out_dtype, void* d_workspace, size_t ws_bytes, int32_t n_splits, void* stream);
+
+/* ---- Decode of a batch that shares a prefix ------------------------------------
+ * One decode step of sequences that share their first rows (an instruction
+ * text, a document): the prefix is packed once, in a cache of its own with one
+ * sequence, and each sequence's own rows follow in `cache`.  Every query
+ * attends rows [0, *d_prefix_len) of the prefix and then rows
+ * [0, d_ctx_len[b]) of its own, under one softmax.  The prefix's rows are read
+ * and decoded for all the sequences' queries together.  No allocation, no
+ * state in the workspace, so the call can be captured in a HIP graph.
+ * Keys are post-RoPE: sequence b's own row t was rotated at its position
+ * (*d_prefix_len + t in the usual case) by the caller.
+ * d_layout: one layout for both caches (it does not depend on batch or
+ *      capacity).
+ * prefix_cfg: cfg but for batch == 1 and the capacity (EINVAL otherwise).
+ * d_prefix_len: device int32 [1] in [0, max_prefix], max_prefix <=
+ *      prefix_cfg->capacity; outside it every output is NaN.
+ * d_ctx_len, max_ctx: as in blockgtq_cross_attn, the sequences' own rows; a
+ *      sequence without any row (prefix and own) gets zeros.
+ * d_q, d_out, out_dtype, layer: as blockgtq_cross_attn with one query row per
+ *      sequence, [batch][n_kv_heads*group][128].
+ * n_splits: splits of the prefix, 0 = heuristic.
+ * d_workspace: blockgtq_shared_workspace_bytes bytes, as in
+ *      blockgtq_cross_attn. */
+int blockgtq_shared_workspace_bytes(const bgtq_config* cfg, const bgtq_config* prefix_cfg, int32_t n_layers_in_call,
+                                    int32_t n_splits, int32_t max_prefix, int32_t max_ctx, size_t* bytes_out);
+int blockgtq_decode_attn_shared(const bgtq_config* cfg, const void* d_layout, int32_t layer, const void* d_q,
+                                const bgtq_config* prefix_cfg, const bgtq_cache* prefix, const int32_t* d_prefix_len,
+                                int32_t max_prefix, const int32_t* d_ctx_len, int32_t max_ctx, const bgtq_cache* cache,
+                                void* d_out, int32_t out_dtype, void* d_workspace, size_t ws_bytes, int32_t n_splits,
+                                void* stream);
+
 /* ---- Measurement helper (not a step of the method) ------------------------
  * Streaming read of d_src[0 .. bytes): the read-bandwidth ceiling that the
  * decode's roofline fraction is quoted against, next to the nominal 8 TB/s

@@ -27,7 +27,9 @@ EXPORTED = [
     "blockgtq_decode_attn_fp16", "blockgtq_prefill_workspace_bytes", "blockgtq_prefill_attn",
     "blockgtq_window_bytes", "blockgtq_window_append", "blockgtq_protected_workspace_bytes",
     "blockgtq_decode_attn_protected", "blockgtq_rope_step_workspace_bytes", "blockgtq_rope_decode_step",
-    "blockgtq_read_probe", "blockgtq_decode_attn_noalloc",
+    "blockgtq_read_probe", "blockgtq_decode_attn_noalloc", "blockgtq_dequantize_rows",
+    "blockgtq_cross_workspace_bytes", "blockgtq_cross_attn", "blockgtq_shared_workspace_bytes",
+    "blockgtq_decode_attn_shared",
 ]
 
 
@@ -82,6 +84,11 @@ def lib():
             "blockgtq_rope_decode_step": [P, P, ctypes.c_double, P, P, P, P, I32, P, P, P, SZ, I32, P],
             "blockgtq_read_probe": [P, SZ, P, P],
             "blockgtq_decode_attn_noalloc": [P, P, I32, P, P, I32, P, P, I32, P],
+            "blockgtq_dequantize_rows": [P, P, I32, P, I32, P, P, P, P, I32, P],
+            "blockgtq_cross_workspace_bytes": [P, I32, I32, I32, I32, PSZ],
+            "blockgtq_cross_attn": [P, P, I32, P, I32, P, I32, P, P, I32, P, SZ, I32, P],
+            "blockgtq_shared_workspace_bytes": [P, P, I32, I32, I32, I32, PSZ],
+            "blockgtq_decode_attn_shared": [P, P, I32, P, P, P, P, I32, P, I32, P, P, I32, P, SZ, I32, P],
         }
         for name, args in sig.items():
             fn = getattr(L, name)
@@ -392,6 +399,156 @@ def blockgtq_rope_decode_step(cfg: Config, layout: Layout, rope_base: float, q_p
                                            _ptr(k_pre), _ptr(v), _ptr(pos), max_ctx, ctypes.byref(cache.c()),
                                            _ptr(out), _ptr(workspace), workspace.numel(), n_splits,
                                            _stream(stream)))
+    return out
+
+
+# ---------------------------------------------------------------- packed rows read by other callers
+
+def _one_device(*tensors):
+    """The device of every tensor given (None is skipped), contiguous and on one GPU."""
+    import torch
+    on = [t for t in tensors if t is not None]
+    for t in on:
+        if not isinstance(t, torch.Tensor) or not t.is_cuda or not t.is_contiguous():
+            raise ValueError("device tensors must be contiguous CUDA tensors")
+    if len({t.device for t in on}) > 1:
+        raise ValueError("tensors on different devices: " + ", ".join(sorted({str(t.device) for t in on})))
+    return on[0].device
+
+
+def _check_shape(what, t, shape, dtype):
+    if tuple(t.shape) != tuple(shape) or t.dtype != dtype:
+        raise ValueError(f"{what}: expected {tuple(shape)} of {dtype}, got {tuple(t.shape)} of {t.dtype}")
+
+
+def _check_cache(cfg: Config, cache: Cache, what="cache"):
+    import torch
+    L, B, H, C = cfg.n_layers, cfg.batch, cfg.n_kv_heads, cfg.capacity
+    _check_shape(what + ".k_codes", cache.k_codes, (L, B, H, C, cfg.k_words), torch.int32)
+    _check_shape(what + ".k_norms", cache.k_norms, (L, B, H, C * MAX_GROUPS), torch.float16)
+    _check_shape(what + ".v_codes", cache.v_codes, (L, B, H, C // 32, HEAD_DIM, cfg.v_bits), torch.int32)
+    _check_shape(what + ".v_norms", cache.v_norms, (L, B, H, C), torch.float16)
+    return [cache.k_codes, cache.k_norms, cache.v_codes, cache.v_norms]
+
+
+def _out_type(dtype):
+    import torch
+    if dtype not in (torch.float32, torch.bfloat16):
+        raise ValueError(f"output dtype {dtype}: torch.float32 or torch.bfloat16")
+    return BGTQ_BF16 if dtype == torch.bfloat16 else BGTQ_FP32
+
+
+def _lead(cfg, layer):
+    """Leading dimensions of a call's tensors: a layer dimension for all layers."""
+    return (cfg.n_layers, cfg.batch) if layer < 0 else (cfg.batch,)
+
+
+def blockgtq_dequantize_rows(cfg: Config, layout: Layout, layer: int, cache: Cache, read_pos, n_rows: int, ctx_len=None,
+                             k_out=None, v_out=None, out_dtype=None, stream=None):
+    """Rows read_pos[b] .. + n_rows - 1 of each sequence as plain keys and values
+    [batch, n_rows, H_kv, 128] (with a leading layer dim for layer == -1).
+    Rows outside the cache or at or past ctx_len[b] are left as they were in
+    k_out / v_out.  With only one of k_out and v_out given, only that one is
+    read; with neither, both are allocated (zeros; out_dtype, fp32 by default).
+    Returns (k_out, v_out)."""
+    import torch
+    _check_shape("read_pos", read_pos, (cfg.batch,), torch.int32)
+    if ctx_len is not None:
+        _check_shape("ctx_len", ctx_len, (cfg.batch,), torch.int32)
+    shape = _lead(cfg, layer) + (max(n_rows, 0), cfg.n_kv_heads, HEAD_DIM)
+    if k_out is None and v_out is None:
+        k_out, v_out = (torch.zeros(shape, dtype=out_dtype or torch.float32, device=read_pos.device) for _ in range(2))
+    dtype = (v_out if k_out is None else k_out).dtype
+    if out_dtype is not None and dtype != out_dtype:
+        raise ValueError(f"out_dtype {out_dtype}, but the outputs are {dtype}")
+    for name, t in (("k_out", k_out), ("v_out", v_out)):
+        if t is not None:
+            _check_shape(name, t, shape, dtype)
+    kind = _out_type(dtype)
+    device = _one_device(layout.blob, read_pos, ctx_len, k_out, v_out, *_check_cache(cfg, cache))
+    with torch.cuda.device(device):
+        _check(lib().blockgtq_dequantize_rows(ctypes.byref(cfg.c()), _ptr(layout.blob), layer, ctypes.byref(cache.c()),
+                                              n_rows, _ptr(read_pos), _ptr(ctx_len), _ptr(k_out), _ptr(v_out), kind,
+                                              _stream(stream)))
+    return k_out, v_out
+
+
+def cross_workspace_bytes(cfg: Config, n_layers_in_call: int, n_q: int, n_splits: int, max_ctx: int) -> int:
+    v = ctypes.c_size_t()
+    _check(lib().blockgtq_cross_workspace_bytes(ctypes.byref(cfg.c()), n_layers_in_call, n_q, n_splits, max_ctx,
+                                                ctypes.byref(v)))
+    return v.value
+
+
+def shared_workspace_bytes(cfg: Config, prefix_cfg: Config, n_layers_in_call: int, n_splits: int, max_prefix: int,
+                           max_ctx: int) -> int:
+    v = ctypes.c_size_t()
+    _check(lib().blockgtq_shared_workspace_bytes(ctypes.byref(cfg.c()), ctypes.byref(prefix_cfg.c()), n_layers_in_call,
+                                                 n_splits, max_prefix, max_ctx, ctypes.byref(v)))
+    return v.value
+
+
+def _out_of(q, out, out_dtype):
+    import torch
+    if out is None:
+        out = torch.empty(q.shape, dtype=out_dtype or torch.float32, device=q.device)
+    elif out_dtype is not None and out.dtype != out_dtype:
+        raise ValueError(f"out_dtype {out_dtype}, but out is {out.dtype}")
+    _check_shape("out", out, q.shape, out.dtype)
+    return out, _out_type(out.dtype)
+
+
+def blockgtq_cross_attn(cfg: Config, layout: Layout, layer: int, q, ctx_len, max_ctx: int, cache: Cache, out=None,
+                        workspace=None, n_splits: int = 0, out_dtype=None, stream=None):
+    """q [batch, n_q, Hq, 128] (with a leading layer dim for layer == -1), every
+    query row attending rows [0, ctx_len[b]) of its sequence's packed cache.
+    Returns out, of q's shape in out's or out_dtype (fp32 by default)."""
+    import torch
+    n_lc = cfg.n_layers if layer < 0 else 1
+    lead = _lead(cfg, layer)
+    if q.dim() != len(lead) + 3:
+        raise ValueError(f"q: expected {lead + ('n_q', cfg.n_q_heads, HEAD_DIM)}, got {tuple(q.shape)}")
+    n_q = q.shape[len(lead)]
+    _check_shape("q", q, lead + (n_q, cfg.n_q_heads, HEAD_DIM), _in_dtype(cfg))
+    _check_shape("ctx_len", ctx_len, (cfg.batch,), torch.int32)
+    out, kind = _out_of(q, out, out_dtype)
+    if workspace is None:
+        workspace = torch.empty(max(cross_workspace_bytes(cfg, n_lc, n_q, n_splits, max_ctx), 1), dtype=torch.uint8,
+                                device=q.device)
+    device = _one_device(q, layout.blob, ctx_len, out, workspace, *_check_cache(cfg, cache))
+    with torch.cuda.device(device):
+        _check(lib().blockgtq_cross_attn(ctypes.byref(cfg.c()), _ptr(layout.blob), layer, _ptr(q), n_q, _ptr(ctx_len),
+                                         max_ctx, ctypes.byref(cache.c()), _ptr(out), kind, _ptr(workspace),
+                                         workspace.numel() * workspace.element_size(), n_splits, _stream(stream)))
+    return out
+
+
+def blockgtq_decode_attn_shared(cfg: Config, layout: Layout, layer: int, q, prefix_cfg: Config, prefix: Cache, prefix_len,
+                                max_prefix: int, ctx_len, max_ctx: int, cache: Cache, out=None, workspace=None,
+                                n_splits: int = 0, out_dtype=None, stream=None):
+    """One decode step of a batch behind one packed prefix: q [batch, Hq, 128]
+    (with a leading layer dim for layer == -1) against rows [0, prefix_len[0])
+    of `prefix` and rows [0, ctx_len[b]) of the sequence's own cache, one
+    softmax.  prefix_cfg: cfg with batch 1 and the prefix cache's capacity.
+    Returns out, of q's shape in out's or out_dtype (fp32 by default)."""
+    import torch
+    n_lc = cfg.n_layers if layer < 0 else 1
+    _check_shape("q", q, _lead(cfg, layer) + (cfg.n_q_heads, HEAD_DIM), _in_dtype(cfg))
+    _check_shape("ctx_len", ctx_len, (cfg.batch,), torch.int32)
+    _check_shape("prefix_len", prefix_len, (1,), torch.int32)
+    out, kind = _out_of(q, out, out_dtype)
+    if workspace is None:
+        workspace = torch.empty(shared_workspace_bytes(cfg, prefix_cfg, n_lc, n_splits, max_prefix, max_ctx),
+                                dtype=torch.uint8, device=q.device)
+    device = _one_device(q, layout.blob, prefix_len, ctx_len, out, workspace, *_check_cache(cfg, cache),
+                         *_check_cache(prefix_cfg, prefix, "prefix"))
+    with torch.cuda.device(device):
+        _check(lib().blockgtq_decode_attn_shared(ctypes.byref(cfg.c()), _ptr(layout.blob), layer, _ptr(q),
+                                                 ctypes.byref(prefix_cfg.c()), ctypes.byref(prefix.c()),
+                                                 _ptr(prefix_len), max_prefix, _ptr(ctx_len), max_ctx,
+                                                 ctypes.byref(cache.c()), _ptr(out), kind, _ptr(workspace),
+                                                 workspace.numel() * workspace.element_size(), n_splits,
+                                                 _stream(stream)))
     return out
 
 

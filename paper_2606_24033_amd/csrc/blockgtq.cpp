@@ -833,6 +833,198 @@ int blockgtq_prefill_attn(const bgtq_config* cfg, const void* d_layout, int32_t 
   return ok();
 }
 
+// ---------------------------------------------------------------- packed rows read by other callers
+
+static CachePtrs cache_ptrs(const bgtq_cache* cache) {
+  return {static_cast<uint32_t*>(cache->k_codes), static_cast<uint16_t*>(cache->k_norms),
+          static_cast<uint32_t*>(cache->v_codes), static_cast<uint16_t*>(cache->v_norms)};
+}
+
+static int check_cache(const bgtq_cache* c) {
+  if (!c || !c->k_codes || !c->k_norms || !c->v_codes || !c->v_norms) return fail(BGTQ_EINVAL, "NULL pointer");
+  if (!cache_aligned(c)) return fail(BGTQ_EINVAL, "cache buffers must be 16-byte aligned");
+  return BGTQ_OK;
+}
+
+static bool aligned16(const void* p) { return reinterpret_cast<uintptr_t>(p) % 16 == 0; }
+
+static int check_out_dtype(int32_t t) {
+  if (t != BGTQ_FP32 && t != BGTQ_BF16) return fail(BGTQ_EINVAL, "out_dtype %d", t);
+  return BGTQ_OK;
+}
+
+// One launch's workgroups: the grid's size in threads stays below 2^32.
+static const long kMaxItems = 1l << 22;
+
+int blockgtq_dequantize_rows(const bgtq_config* cfg, const void* d_layout, int32_t layer, const bgtq_cache* cache,
+                             int32_t n_rows, const int32_t* d_read_pos, const int32_t* d_ctx_len, void* d_k_out,
+                             void* d_v_out, int32_t out_dtype, void* stream) {
+  if (int e = check_cfg(cfg)) return e;
+  if (int e = check_out_dtype(out_dtype)) return e;
+  if (layer < -1 || layer >= cfg->n_layers) return fail(BGTQ_EINVAL, "layer %d out of range", layer);
+  if (n_rows < 0) return fail(BGTQ_EINVAL, "n_rows %d < 0", n_rows);
+  if (n_rows > cfg->capacity) return fail(BGTQ_ECAPACITY, "n_rows %d > capacity %d", n_rows, cfg->capacity);
+  if (!d_layout || !d_read_pos) return fail(BGTQ_EINVAL, "NULL pointer");
+  if (int e = check_cache(cache)) return e;
+  if (n_rows == 0) return ok();
+  if (!d_k_out && !d_v_out) return fail(BGTQ_EINVAL, "k_out and v_out are both NULL");
+  if (!aligned16(d_k_out) || !aligned16(d_v_out)) return fail(BGTQ_EINVAL, "k_out and v_out must be 16-byte aligned");
+  const long lz = static_cast<long>(layer < 0 ? cfg->n_layers : 1) * cfg->batch;
+  if (lz > 65535 || cfg->n_kv_heads > 65535 || (n_rows + 15l) / 16 * cfg->n_kv_heads * lz > kMaxItems * 4)
+    return fail(BGTQ_EUNSUPPORTED, "%d rows of %ld x %d heads in one call", n_rows, lz, cfg->n_kv_heads);
+  hipError_t e = launch_dequantize_rows(dims_of(cfg, layer), d_layout, cache_ptrs(cache), n_rows, d_read_pos,
+                                        d_ctx_len, d_k_out, d_v_out, out_dtype, static_cast<hipStream_t>(stream));
+  if (e != hipSuccess) return hip_fail(e, "dequantize_rows launch");
+  return ok();
+}
+
+// Splits of a pass of `units` workgroups per split over max_len rows: enough
+// of them for four workgroups per CU, of 256 rows at least.
+static SplitPlan cross_plan(long units, int max_len, int requested) {
+  if (max_len <= 0) return {1, 64};
+  long n = requested > 0 ? requested : std::max(1l, std::min((max_len + 255l) / 256, 1024 / std::max(units, 1l)));
+  n = std::min(n, (max_len + 63l) / 64);
+  SplitPlan p;
+  p.split_len = static_cast<int>((max_len + n - 1) / n + 63) / 64 * 64;
+  p.n_splits = (max_len + p.split_len - 1) / p.split_len;
+  return p;
+}
+
+static int check_cross_sizes(const bgtq_config* cfg, int32_t n_lc, int32_t n_q, int32_t n_splits, int32_t max_ctx) {
+  if (n_lc != 1 && n_lc != cfg->n_layers) return fail(BGTQ_EINVAL, "n_layers_in_call must be 1 or n_layers");
+  if (n_q < 0) return fail(BGTQ_EINVAL, "n_q %d < 0", n_q);
+  if (n_splits < 0 || n_splits > 4096) return fail(BGTQ_EINVAL, "n_splits %d outside 0..4096", n_splits);
+  if (max_ctx < 0 || max_ctx > cfg->capacity) return fail(BGTQ_ECAPACITY, "max_ctx %d outside [0, capacity]", max_ctx);
+  return BGTQ_OK;
+}
+
+// Query rows of a call ([n_lc][batch][n_q][Hq]), 0 where they are too many for one launch.
+static long cross_rows(const bgtq_config* cfg, int32_t n_lc, int32_t n_q) {
+  const double r = static_cast<double>(n_lc) * cfg->batch * n_q * cfg->n_kv_heads * cfg->group;
+  return r <= static_cast<double>(1l << 24) ? static_cast<long>(r) : 0;
+}
+
+static Dims cross_dims(const bgtq_config* cfg, int32_t n_lc) {
+  Dims d = dims_of(cfg, 0);
+  d.n_lc = n_lc;
+  return d;
+}
+
+static SplitPlan cross_plan_of(const Dims& d, int32_t n_q, int32_t max_len, int32_t requested) {
+  return cross_plan(cross_items(d, n_q, 1), max_len, requested);
+}
+
+int blockgtq_cross_workspace_bytes(const bgtq_config* cfg, int32_t n_layers_in_call, int32_t n_q, int32_t n_splits,
+                                   int32_t max_ctx, size_t* bytes_out) {
+  if (int e = check_cfg(cfg)) return e;
+  if (!bytes_out) return fail(BGTQ_EINVAL, "NULL pointer");
+  if (int e = check_cross_sizes(cfg, n_layers_in_call, n_q, n_splits, max_ctx)) return e;
+  *bytes_out = 0;
+  if (n_q == 0) return ok();
+  const long rows = cross_rows(cfg, n_layers_in_call, n_q);
+  if (!rows) return fail(BGTQ_EUNSUPPORTED, "more than 2^24 query rows in one call");
+  const SplitPlan p = cross_plan_of(cross_dims(cfg, n_layers_in_call), n_q, max_ctx, n_splits);
+  *bytes_out = al256(static_cast<size_t>(rows) * p.n_splits * kPartFloats * 4);
+  return ok();
+}
+
+int blockgtq_cross_attn(const bgtq_config* cfg, const void* d_layout, int32_t layer, const void* d_q, int32_t n_q,
+                        const int32_t* d_ctx_len, int32_t max_ctx, const bgtq_cache* cache, void* d_out,
+                        int32_t out_dtype, void* d_workspace, size_t ws_bytes, int32_t n_splits, void* stream) {
+  if (int e = check_cfg(cfg)) return e;
+  if (int e = check_out_dtype(out_dtype)) return e;
+  if (layer < -1 || layer >= cfg->n_layers) return fail(BGTQ_EINVAL, "layer %d out of range", layer);
+  const int n_lc = layer < 0 ? cfg->n_layers : 1;
+  if (int e = check_cross_sizes(cfg, n_lc, n_q, n_splits, max_ctx)) return e;
+  if (n_q == 0) return ok();
+  if (!d_layout || !d_q || !d_ctx_len || !d_out || !d_workspace) return fail(BGTQ_EINVAL, "NULL pointer");
+  if (int e = check_cache(cache)) return e;
+  if (!aligned16(d_q) || !aligned16(d_out) || !aligned16(d_workspace))
+    return fail(BGTQ_EINVAL, "q, out and the workspace must be 16-byte aligned");
+  size_t need = 0;
+  if (int e = blockgtq_cross_workspace_bytes(cfg, n_lc, n_q, n_splits, max_ctx, &need)) return e;
+  if (ws_bytes < need) return fail(BGTQ_EWORKSPACE, "workspace %zu bytes < %zu needed", ws_bytes, need);
+  const Dims d = dims_of(cfg, layer, max_ctx);
+  const SplitPlan p = cross_plan_of(cross_dims(cfg, n_lc), n_q, max_ctx, n_splits);
+  if (cross_items(d, n_q, p.n_splits) > kMaxItems) return fail(BGTQ_EUNSUPPORTED, "too many splits of too many query rows");
+  float* part = static_cast<float*>(d_workspace);
+  hipStream_t s = static_cast<hipStream_t>(stream);
+  hipError_t e = launch_cross_pass(d, d_layout, d_q, n_q, d_ctx_len, cache_ptrs(cache),
+                                   {part, p.n_splits, 0, p.n_splits, p.split_len, max_ctx}, s);
+  if (e != hipSuccess) return hip_fail(e, "cross_attn launch");
+  e = launch_cross_merge(d_layout, cross_rows(cfg, n_lc, n_q), part, p.n_splits, d_out, out_dtype, s);
+  if (e != hipSuccess) return hip_fail(e, "cross_attn merge launch");
+  return ok();
+}
+
+static int check_prefix_cfg(const bgtq_config* cfg, const bgtq_config* p) {
+  if (int e = check_cfg(cfg)) return e;
+  if (int e = check_cfg(p)) return e;
+  if (p->batch != 1) return fail(BGTQ_EINVAL, "the prefix cache holds %d sequences, not 1", p->batch);
+  if (p->n_layers != cfg->n_layers || p->n_kv_heads != cfg->n_kv_heads || p->group != cfg->group ||
+      p->k_budget != cfg->k_budget || p->v_bits != cfg->v_bits || p->in_dtype != cfg->in_dtype)
+    return fail(BGTQ_EINVAL, "the prefix configuration differs from the batch's in more than batch and capacity");
+  return BGTQ_OK;
+}
+
+struct SharedPlan {
+  SplitPlan prefix, own;
+};
+static SharedPlan shared_plan(const bgtq_config* cfg, const bgtq_config* pcfg, int32_t n_lc, int32_t n_splits,
+                              int32_t max_prefix, int32_t max_ctx) {
+  return {cross_plan_of(cross_dims(pcfg, n_lc), cfg->batch, max_prefix, n_splits),
+          cross_plan_of(cross_dims(cfg, n_lc), 1, max_ctx, 0)};
+}
+
+int blockgtq_shared_workspace_bytes(const bgtq_config* cfg, const bgtq_config* prefix_cfg, int32_t n_layers_in_call,
+                                    int32_t n_splits, int32_t max_prefix, int32_t max_ctx, size_t* bytes_out) {
+  if (int e = check_prefix_cfg(cfg, prefix_cfg)) return e;
+  if (!bytes_out) return fail(BGTQ_EINVAL, "NULL pointer");
+  if (int e = check_cross_sizes(cfg, n_layers_in_call, 1, n_splits, max_ctx)) return e;
+  if (int e = check_cross_sizes(prefix_cfg, n_layers_in_call, 1, n_splits, max_prefix)) return e;
+  const long rows = cross_rows(cfg, n_layers_in_call, 1);
+  if (!rows) return fail(BGTQ_EUNSUPPORTED, "more than 2^24 query rows in one call");
+  const SharedPlan p = shared_plan(cfg, prefix_cfg, n_layers_in_call, n_splits, max_prefix, max_ctx);
+  *bytes_out = al256(static_cast<size_t>(rows) * (p.prefix.n_splits + p.own.n_splits) * kPartFloats * 4);
+  return ok();
+}
+
+int blockgtq_decode_attn_shared(const bgtq_config* cfg, const void* d_layout, int32_t layer, const void* d_q,
+                                const bgtq_config* prefix_cfg, const bgtq_cache* prefix, const int32_t* d_prefix_len,
+                                int32_t max_prefix, const int32_t* d_ctx_len, int32_t max_ctx, const bgtq_cache* cache,
+                                void* d_out, int32_t out_dtype, void* d_workspace, size_t ws_bytes, int32_t n_splits,
+                                void* stream) {
+  if (int e = check_prefix_cfg(cfg, prefix_cfg)) return e;
+  if (int e = check_out_dtype(out_dtype)) return e;
+  if (layer < -1 || layer >= cfg->n_layers) return fail(BGTQ_EINVAL, "layer %d out of range", layer);
+  if (!d_layout || !d_q || !d_prefix_len || !d_ctx_len || !d_out || !d_workspace) return fail(BGTQ_EINVAL, "NULL pointer");
+  if (int e = check_cache(prefix)) return e;
+  if (int e = check_cache(cache)) return e;
+  if (!aligned16(d_q) || !aligned16(d_out) || !aligned16(d_workspace))
+    return fail(BGTQ_EINVAL, "q, out and the workspace must be 16-byte aligned");
+  const int n_lc = layer < 0 ? cfg->n_layers : 1;
+  size_t need = 0;
+  if (int e = blockgtq_shared_workspace_bytes(cfg, prefix_cfg, n_lc, n_splits, max_prefix, max_ctx, &need)) return e;
+  if (ws_bytes < need) return fail(BGTQ_EWORKSPACE, "workspace %zu bytes < %zu needed", ws_bytes, need);
+  const SharedPlan p = shared_plan(cfg, prefix_cfg, n_lc, n_splits, max_prefix, max_ctx);
+  const Dims dp = dims_of(prefix_cfg, layer, max_prefix), d = dims_of(cfg, layer, max_ctx);
+  if (cross_items(dp, cfg->batch, p.prefix.n_splits) > kMaxItems || cross_items(d, 1, p.own.n_splits) > kMaxItems)
+    return fail(BGTQ_EUNSUPPORTED, "too many splits of too many query rows");
+  float* part = static_cast<float*>(d_workspace);
+  const int slots = p.prefix.n_splits + p.own.n_splits;
+  hipStream_t s = static_cast<hipStream_t>(stream);
+  // the prefix: every sequence's query is a query row of its one sequence
+  hipError_t e = launch_cross_pass(dp, d_layout, d_q, cfg->batch, d_prefix_len, cache_ptrs(prefix),
+                                   {part, slots, 0, p.prefix.n_splits, p.prefix.split_len, max_prefix}, s);
+  if (e != hipSuccess) return hip_fail(e, "decode_attn_shared prefix launch");
+  e = launch_cross_pass(d, d_layout, d_q, 1, d_ctx_len, cache_ptrs(cache),
+                        {part, slots, p.prefix.n_splits, p.own.n_splits, p.own.split_len, max_ctx}, s);
+  if (e != hipSuccess) return hip_fail(e, "decode_attn_shared launch");
+  e = launch_cross_merge(d_layout, cross_rows(cfg, n_lc, 1), part, slots, d_out, out_dtype, s);
+  if (e != hipSuccess) return hip_fail(e, "decode_attn_shared merge launch");
+  return ok();
+}
+
 int blockgtq_read_probe(const void* d_src, size_t bytes, uint32_t* d_sink, void* stream) {
   if (!d_src || !d_sink) return fail(BGTQ_EINVAL, "NULL pointer");
   if (bytes == 0 || bytes % 16 != 0 || reinterpret_cast<uintptr_t>(d_src) % 16 != 0)

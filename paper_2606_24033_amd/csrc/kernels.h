@@ -99,6 +99,28 @@ hipError_t launch_prefill_attn(const Dims& d, const void* layout, const void* q,
                                const int32_t* q_pos0, int max_pos, const CachePtrs& c, float* qr_ws,
                                float* out, hipStream_t s);
 
+// Cache rows read back in out_dtype (rows.hip); k_out or v_out may be null.
+hipError_t launch_dequantize_rows(const Dims& d, const void* layout, const CachePtrs& c, int n_rows,
+                                  const int32_t* read_pos, const int32_t* ctx_len, void* k_out, void* v_out,
+                                  int out_dtype, hipStream_t s);
+
+// Attention passes over packed rows that every query row sees (cross.hip).  A
+// pass leaves (m, l, acc[128]) of every query row ([n_lc][batch][n_q][Hq])
+// and split in part[row][slot0 + split], n_slots partials per row.
+constexpr int kPartFloats = 130;
+struct CrossPass {
+  float* part;
+  int n_slots, slot0;
+  int n_splits, split_len;  // split_len: cache rows per split, a multiple of 64
+  int max_len;              // the host's bound on the lengths: a row of a sequence outside [0, max_len] is NaN
+};
+long cross_items(const Dims& d, int n_q, int n_splits);  // workgroups of a pass
+hipError_t launch_cross_pass(const Dims& d, const void* layout, const void* q, int n_q, const int32_t* ctx_len,
+                             const CachePtrs& c, const CrossPass& ps, hipStream_t s);
+// Joins the partials of `rows` query rows into out.
+hipError_t launch_cross_merge(const void* layout, long rows, const float* part, int n_slots, void* out, int out_dtype,
+                              hipStream_t s);
+
 // Streaming read of `bytes` (a multiple of 16, 16-byte aligned) at src;
 // writes sink[0] only in a case no real input reaches (probe.hip).
 hipError_t launch_read_probe(const void* src, size_t bytes, uint32_t* sink, hipStream_t s);
