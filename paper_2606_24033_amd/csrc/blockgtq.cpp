@@ -878,16 +878,35 @@ int blockgtq_dequantize_rows(const bgtq_config* cfg, const void* d_layout, int32
   return ok();
 }
 
-// Splits of a pass of `units` workgroups per split over max_len rows: enough
-// of them for four workgroups per CU, of 256 rows at least.
+// Splits of a pass of `units` workgroups per split over max_len rows.  One
+// 8-wave workgroup runs per CU, so units x n workgroups take ceil(units n /
+// 256) rounds, each as long as one split: a 64-row tile per wave and 512 rows,
+// plus set-up and merge worth about three of them.
 static SplitPlan cross_plan(long units, int max_len, int requested) {
   if (max_len <= 0) return {1, 64};
-  long n = requested > 0 ? requested : std::max(1l, std::min((max_len + 255l) / 256, 1024 / std::max(units, 1l)));
-  n = std::min(n, (max_len + 63l) / 64);
+  const int tiles = (max_len + 63) / 64;
+  long n = std::min(requested, tiles);
+  if (requested <= 0) {
+    double best = 0.0;
+    n = 1;
+    for (int k = 1; k <= std::min((tiles + 7) / 8, 256); ++k) {
+      const int len = (tiles + k - 1) / k;
+      const double t = static_cast<double>((units * k + 255) / 256) * ((len + 7) / 8 + 3);
+      if (k == 1 || t < best) {
+        best = t;
+        n = k;
+      }
+    }
+  }
   SplitPlan p;
-  p.split_len = static_cast<int>((max_len + n - 1) / n + 63) / 64 * 64;
+  p.split_len = static_cast<int>((tiles + n - 1) / n) * 64;
   p.n_splits = (max_len + p.split_len - 1) / p.split_len;
   return p;
+}
+
+// Bytes of the partials: at least one row's, so that a workspace is never empty.
+static size_t cross_ws_bytes(long rows, int n_slots) {
+  return al256(static_cast<size_t>(n_slots > 1 ? rows : 1) * n_slots * kPartFloats * 4);
 }
 
 static int check_cross_sizes(const bgtq_config* cfg, int32_t n_lc, int32_t n_q, int32_t n_splits, int32_t max_ctx) {
@@ -924,7 +943,7 @@ int blockgtq_cross_workspace_bytes(const bgtq_config* cfg, int32_t n_layers_in_c
   const long rows = cross_rows(cfg, n_layers_in_call, n_q);
   if (!rows) return fail(BGTQ_EUNSUPPORTED, "more than 2^24 query rows in one call");
   const SplitPlan p = cross_plan_of(cross_dims(cfg, n_layers_in_call), n_q, max_ctx, n_splits);
-  *bytes_out = al256(static_cast<size_t>(rows) * p.n_splits * kPartFloats * 4);
+  *bytes_out = cross_ws_bytes(rows, p.n_splits);
   return ok();
 }
 
@@ -946,14 +965,17 @@ int blockgtq_cross_attn(const bgtq_config* cfg, const void* d_layout, int32_t la
   if (ws_bytes < need) return fail(BGTQ_EWORKSPACE, "workspace %zu bytes < %zu needed", ws_bytes, need);
   const Dims d = dims_of(cfg, layer, max_ctx);
   const SplitPlan p = cross_plan_of(cross_dims(cfg, n_lc), n_q, max_ctx, n_splits);
-  if (cross_items(d, n_q, p.n_splits) > kMaxItems) return fail(BGTQ_EUNSUPPORTED, "too many splits of too many query rows");
-  float* part = static_cast<float*>(d_workspace);
-  hipStream_t s = static_cast<hipStream_t>(stream);
-  hipError_t e = launch_cross_pass(d, d_layout, d_q, n_q, d_ctx_len, cache_ptrs(cache),
-                                   {part, p.n_splits, 0, p.n_splits, p.split_len, max_ctx}, s);
+  const long items = cross_items(d, n_q, p.n_splits);
+  if (items > kMaxItems) return fail(BGTQ_EUNSUPPORTED, "too many splits of too many query rows");
+  CrossCall call = {};
+  call.side[0] = {cache_ptrs(cache), d_ctx_len, cfg->batch, cfg->capacity, n_q, p.n_splits, p.split_len, max_ctx, 0,
+                  static_cast<int>(items)};
+  call.part = static_cast<float*>(d_workspace);
+  call.n_slots = p.n_splits;
+  call.out = d_out;
+  call.out_dtype = out_dtype;
+  hipError_t e = launch_cross(d, d_layout, d_q, call, cross_rows(cfg, n_lc, n_q), static_cast<hipStream_t>(stream));
   if (e != hipSuccess) return hip_fail(e, "cross_attn launch");
-  e = launch_cross_merge(d_layout, cross_rows(cfg, n_lc, n_q), part, p.n_splits, d_out, out_dtype, s);
-  if (e != hipSuccess) return hip_fail(e, "cross_attn merge launch");
   return ok();
 }
 
@@ -985,7 +1007,7 @@ int blockgtq_shared_workspace_bytes(const bgtq_config* cfg, const bgtq_config* p
   const long rows = cross_rows(cfg, n_layers_in_call, 1);
   if (!rows) return fail(BGTQ_EUNSUPPORTED, "more than 2^24 query rows in one call");
   const SharedPlan p = shared_plan(cfg, prefix_cfg, n_layers_in_call, n_splits, max_prefix, max_ctx);
-  *bytes_out = al256(static_cast<size_t>(rows) * (p.prefix.n_splits + p.own.n_splits) * kPartFloats * 4);
+  *bytes_out = cross_ws_bytes(rows, p.prefix.n_splits + p.own.n_splits);
   return ok();
 }
 
@@ -1007,21 +1029,22 @@ int blockgtq_decode_attn_shared(const bgtq_config* cfg, const void* d_layout, in
   if (int e = blockgtq_shared_workspace_bytes(cfg, prefix_cfg, n_lc, n_splits, max_prefix, max_ctx, &need)) return e;
   if (ws_bytes < need) return fail(BGTQ_EWORKSPACE, "workspace %zu bytes < %zu needed", ws_bytes, need);
   const SharedPlan p = shared_plan(cfg, prefix_cfg, n_lc, n_splits, max_prefix, max_ctx);
-  const Dims dp = dims_of(prefix_cfg, layer, max_prefix), d = dims_of(cfg, layer, max_ctx);
-  if (cross_items(dp, cfg->batch, p.prefix.n_splits) > kMaxItems || cross_items(d, 1, p.own.n_splits) > kMaxItems)
-    return fail(BGTQ_EUNSUPPORTED, "too many splits of too many query rows");
-  float* part = static_cast<float*>(d_workspace);
-  const int slots = p.prefix.n_splits + p.own.n_splits;
-  hipStream_t s = static_cast<hipStream_t>(stream);
+  const Dims d = dims_of(cfg, layer, max_ctx);
+  const long items0 = cross_items(cross_dims(prefix_cfg, n_lc), cfg->batch, p.prefix.n_splits);
+  const long items1 = cross_items(d, 1, p.own.n_splits);
+  if (items0 + items1 > kMaxItems) return fail(BGTQ_EUNSUPPORTED, "too many splits of too many query rows");
+  CrossCall call = {};
   // the prefix: every sequence's query is a query row of its one sequence
-  hipError_t e = launch_cross_pass(dp, d_layout, d_q, cfg->batch, d_prefix_len, cache_ptrs(prefix),
-                                   {part, slots, 0, p.prefix.n_splits, p.prefix.split_len, max_prefix}, s);
-  if (e != hipSuccess) return hip_fail(e, "decode_attn_shared prefix launch");
-  e = launch_cross_pass(d, d_layout, d_q, 1, d_ctx_len, cache_ptrs(cache),
-                        {part, slots, p.prefix.n_splits, p.own.n_splits, p.own.split_len, max_ctx}, s);
+  call.side[0] = {cache_ptrs(prefix), d_prefix_len, 1, prefix_cfg->capacity, cfg->batch, p.prefix.n_splits,
+                  p.prefix.split_len, max_prefix, 0, static_cast<int>(items0)};
+  call.side[1] = {cache_ptrs(cache), d_ctx_len, cfg->batch, cfg->capacity, 1, p.own.n_splits, p.own.split_len, max_ctx,
+                  p.prefix.n_splits, static_cast<int>(items1)};
+  call.part = static_cast<float*>(d_workspace);
+  call.n_slots = p.prefix.n_splits + p.own.n_splits;
+  call.out = d_out;
+  call.out_dtype = out_dtype;
+  hipError_t e = launch_cross(d, d_layout, d_q, call, cross_rows(cfg, n_lc, 1), static_cast<hipStream_t>(stream));
   if (e != hipSuccess) return hip_fail(e, "decode_attn_shared launch");
-  e = launch_cross_merge(d_layout, cross_rows(cfg, n_lc, 1), part, slots, d_out, out_dtype, s);
-  if (e != hipSuccess) return hip_fail(e, "decode_attn_shared merge launch");
   return ok();
 }
 

@@ -1,0 +1,8 @@
+// Packed-row attention instantiation for value code width 1 (see cross_impl.h).
+#include "cross_impl.h"
+
+namespace bgtq {
+hipError_t launch_cross_bv1(const Dims& d, const void* layout, const void* q, const CrossCall& call, hipStream_t s) {
+  return cross_detail::launch_bv<1>(d, layout, q, call, s);
+}
+}  // namespace bgtq

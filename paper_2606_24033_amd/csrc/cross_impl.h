@@ -1,0 +1,639 @@
+// Attention of up to 32 query rows of one (layer, sequence, KV head) to a range
+// of packed rows that all of them see (cross.hip has the passes it serves).
+//
+// Work mapping.  A workgroup of 8 waves (two per SIMD; its lookup tables fill
+// the LDS) = one (unit, block of 32 query rows, split of the key axis).  A wave
+// owns 64-row tiles and decodes their codes straight into the operands of
+// 32x32x16 f16 MFMAs: the decode of a tile costs a wave the same whether 4 or
+// 32 query rows use it, nothing decoded passes through LDS and the waves meet
+// only at the end.
+//  * QK, S^T = K Q^T: lane = token decodes 16 coordinates of one group (a code
+//    width is uniform in the wave); v_permlane32_swap exchanges the halves, so
+//    that the registers of all 64 tokens become the A operands of two 32-token
+//    blocks.  B = the query rows from an image in LDS (fp16 hi and lo parts,
+//    groups padded to 16 coordinates with zeros).  The operands are the bare
+//    centroids (exact in fp16); a group's products are scaled by its radii as
+//    they are added to S, in fp32.
+//  * The accumulator's layout (lane = query row, registers = tokens 8 (i / 4) +
+//    4 hf + i % 4, hf = lane / 32) makes the softmax weights the B operand of
+//    O^T = V^T P^T as they are.  Its k runs over the tokens {4 hf + i, 8 + 4 hf
+//    + i} of a 16-token step, and a lane (dim, hf) decodes just those from the
+//    value tile, where the codes of a dim lie one after the other.
+#pragma once
+#include <hip/hip_runtime.h>
+
+#include "decode_impl.h"
+#include "kernels.h"
+#include "layout.h"
+#include "mix.h"
+
+namespace bgtq {
+namespace cross_detail {
+
+using split_detail::as_half4;
+using split_detail::decode4;
+using split_detail::field_at;
+using split_detail::half4_t;
+using split_detail::LaneRep;
+using split_detail::ld_at;
+using split_detail::swap32;
+typedef _Float16 half8_t __attribute__((ext_vector_type(8)));
+typedef _Float16 half2_t __attribute__((ext_vector_type(2)));
+typedef float float4_t __attribute__((ext_vector_type(4)));
+typedef float float16_t __attribute__((ext_vector_type(16)));
+
+constexpr int kWaves = 8, kThreads = kWaves * 64;
+constexpr int kRows = 32;      // query rows of a workgroup
+constexpr int kMaxSteps = 15;  // 16-coordinate steps of a key row: at most (128 + 8 * 14) / 16
+constexpr float kLog2e = 1.4426950408889634f;
+constexpr float kNegInf = -__builtin_huge_valf();
+constexpr float kRsqrtD = 0.08838834764831845f;  // 1 / sqrt(128)
+
+// ---- LDS map (bytes).  The lookup tables keep the decode kernel's places
+// (split_detail::kLut*), then
+constexpr int kImg = split_detail::kQimg;                // query image [step][hi, lo][lane] x 16 B
+constexpr int kRad = kImg + kMaxSteps * 2048;            // per wave: radii [8 groups, values][64 tokens] fp16
+constexpr int kRadBytes = 9 * 64 * 2;
+constexpr int kBooks = kRad + kWaves * kRadBytes;        // fp16 codebooks
+constexpr int kScale = kBooks + 1024;                    // per query row: 2^-e of its scaled image
+constexpr int kLds = kScale + kRows * 4;
+static_assert(kLds <= 160 * 1024, "LDS of one workgroup");
+// at the end: [wave][row] accumulators, then maxima and sums
+constexpr int kAccStride = kHeadDim + 4;
+constexpr int kEndM = kWaves * kRows * kAccStride * 4;
+static_assert(kEndM + 2 * kWaves * kRows * 4 <= kLds, "merge area");
+
+__device__ __forceinline__ float half_bits(uint32_t b) {
+  return static_cast<float>(__builtin_bit_cast(_Float16, static_cast<uint16_t>(b)));
+}
+
+__device__ __forceinline__ void store4(void* out, size_t i, const float4_t& y, int dtype) {  // BGTQ_BF16 = 1
+  if (dtype == 1) {
+    typedef __bf16 bf16x4_t __attribute__((ext_vector_type(4)));
+    *reinterpret_cast<bf16x4_t*>(static_cast<uint16_t*>(out) + i) = __builtin_convertvector(y, bf16x4_t);
+  } else {
+    *reinterpret_cast<float4_t*>(static_cast<float*>(out) + i) = y;
+  }
+}
+
+// x, y = 4 registers each: exchanges the upper half-wave of x with the lower
+// one of y (s_nop: the wait states around a lane swap and before an MFMA).
+__device__ __forceinline__ void swap_halves(uint2& x0, uint2& x1, uint2& y0, uint2& y1) {
+  asm("s_nop 1\n\t"
+      "v_permlane32_swap_b32 %0, %4\n\t"
+      "v_permlane32_swap_b32 %1, %5\n\t"
+      "v_permlane32_swap_b32 %2, %6\n\t"
+      "v_permlane32_swap_b32 %3, %7\n\t"
+      "s_nop 1"
+      : "+v"(x0.x), "+v"(x0.y), "+v"(x1.x), "+v"(x1.y), "+v"(y0.x), "+v"(y0.y), "+v"(y1.x), "+v"(y1.y));
+}
+
+__device__ __forceinline__ half8_t as_half8(const uint2& a, const uint2& b) {
+  return __builtin_bit_cast(half8_t, make_uint4(a.x, a.y, b.x, b.y));
+}
+
+// ---------------------------------------------------------------- QK
+// 16 coordinates (bits POS .. of aw) of all 64 tokens times the query rows:
+// hi and lo query parts into the accumulators of the two token blocks.
+template <int B, int POS, bool Z, int N>
+__device__ __forceinline__ void qk_step(const uint8_t* smem, const uint32_t (&aw)[N], const LaneRep& rep, uint32_t img,
+                                        float16_t (&part)[2]) {
+  uint2 a0 = __builtin_bit_cast(uint2, decode4<B, POS, true>(smem, aw, rep));
+  uint2 a1 = __builtin_bit_cast(uint2, decode4<B, POS + 4 * B, true>(smem, aw, rep));
+  uint2 b0 = __builtin_bit_cast(uint2, decode4<B, POS + 8 * B, true>(smem, aw, rep));
+  uint2 b1 = __builtin_bit_cast(uint2, decode4<B, POS + 12 * B, true>(smem, aw, rep));
+  const half8_t qh = *reinterpret_cast<const half8_t*>(smem + img);
+  const half8_t ql = *reinterpret_cast<const half8_t*>(smem + img + 1024);
+  swap_halves(a0, a1, b0, b1);
+  const half8_t k0 = as_half8(a0, a1), k1 = as_half8(b0, b1);
+  if constexpr (Z) {  // the group's first product starts its accumulators
+    const float16_t zero = {};
+    part[0] = __builtin_amdgcn_mfma_f32_32x32x16_f16(k0, qh, zero, 0, 0, 0);
+    part[1] = __builtin_amdgcn_mfma_f32_32x32x16_f16(k1, qh, zero, 0, 0, 0);
+  } else {
+    part[0] = __builtin_amdgcn_mfma_f32_32x32x16_f16(k0, qh, part[0], 0, 0, 0);
+    part[1] = __builtin_amdgcn_mfma_f32_32x32x16_f16(k1, qh, part[1], 0, 0, 0);
+  }
+  part[0] = __builtin_amdgcn_mfma_f32_32x32x16_f16(k0, ql, part[0], 0, 0, 0);
+  part[1] = __builtin_amdgcn_mfma_f32_32x32x16_f16(k1, ql, part[1], 0, 0, 0);
+}
+
+// The group of width B (metadata gm): S += radius * (codes x query rows).  Its
+// bits are realigned to bit 0 of a small word array, 32 coordinates at a time
+// (16 for the wide codes).
+template <int B, int KWB>
+__device__ __forceinline__ void qk_group(const uint8_t* smem, const uint32_t (&rw)[KWB + split_detail::kRowPad],
+                                         uint32_t gm, int step0, const uint8_t* radii, const LaneRep& rep, int lane,
+                                         float16_t (&s)[2]) {
+  constexpr int CH = B <= 4 ? 2 : 1;             // steps per chunk
+  constexpr int NW = (CH * 16 * B + 31) / 32;    // its words
+  const int o = split_detail::gm_off(gm), n16 = (split_detail::gm_steps(gm) + 3) >> 2;
+  float16_t part[2];
+  const auto chunk = [&](auto first, int c) {
+    const int at = o + c * 16 * B, w0 = at >> 5, sh = at & 31;
+    uint32_t aw[NW + 1];
+#pragma unroll
+    for (int i = 0; i < NW; ++i) aw[i] = __builtin_amdgcn_alignbit(rw[w0 + i + 1], rw[w0 + i], sh);
+    aw[NW] = 0;
+    const uint32_t img = kImg + (step0 + c) * 2048 + lane * 16;
+    qk_step<B, 0, decltype(first)::value>(smem, aw, rep, img, part);
+    if constexpr (CH == 2) {
+      if (c + 1 < n16) qk_step<B, 16 * B, false>(smem, aw, rep, img + 2048, part);
+    }
+  };
+  chunk(std::true_type{}, 0);
+  for (int c = CH; c < n16; c += CH) chunk(std::false_type{}, c);
+  // radii of the lane's tokens: 8 q + 4 hf .. + 3 of each block
+#pragma unroll
+  for (int n = 0; n < 2; ++n)
+#pragma unroll
+    for (int q = 0; q < 4; ++q) {
+      const half4_t r = *reinterpret_cast<const half4_t*>(radii + 2 * (32 * n + 8 * q));
+#pragma unroll
+      for (int i = 0; i < 4; ++i) s[n][4 * q + i] = fmaf(static_cast<float>(r[i]), part[n][4 * q + i], s[n][4 * q + i]);
+    }
+}
+
+template <int KWB, int... BM1>
+__device__ __forceinline__ void qk_all(std::integer_sequence<int, BM1...>, const uint8_t* smem,
+                                       const uint32_t (&rw)[KWB + split_detail::kRowPad], const uint32_t (&gm)[8],
+                                       const uint8_t* radii, const LaneRep& rep, int lane, float16_t (&s)[2]) {
+  int step0 = 0;
+  const auto one = [&](auto bm1) {
+    constexpr int b = decltype(bm1)::value;
+    if (gm[b] >> 31) {
+      qk_group<b + 1, KWB>(smem, rw, gm[b], step0, radii + split_detail::gm_plane(gm[b]) * 128, rep, lane, s);
+      step0 += (split_detail::gm_steps(gm[b]) + 3) >> 2;
+    }
+  };
+  (one(std::integral_constant<int, BM1>{}), ...);
+}
+
+// ---------------------------------------------------------------- lookup tables
+// Entries of the widths in `used` (bit b - 1), in the decode kernel's layout:
+// four codes an entry for 1, 2 and 3 bits, two for 4, one above.
+__device__ __forceinline__ void build_tables(uint8_t* smem, const uint16_t* cbs, uint32_t used, int tid) {
+  using namespace split_detail;
+  const auto quad = [](const uint16_t* cb, int i, int b) {
+    const int m = (1 << b) - 1;
+    return make_uint2(cb[i & m] | static_cast<uint32_t>(cb[(i >> b) & m]) << 16,
+                      cb[(i >> (2 * b)) & m] | static_cast<uint32_t>(cb[(i >> (3 * b)) & m]) << 16);
+  };
+  if (used & 1u) {
+    const int i = tid;  // 16 entries x 16 replicas
+    if (i < 256) *reinterpret_cast<uint2*>(smem + kLut1 + i * 8) = quad(cbs + cb_index(1), i >> 4, 1);
+  }
+  if (used & 2u) {
+    for (int e = tid >> 4; e < 256; e += cross_detail::kThreads / 16) {  // 16 lanes write an entry's 32 replicas
+      const uint2 v = quad(cbs + cb_index(2), e, 2);
+      *reinterpret_cast<uint4*>(smem + kLut2 + e * 256 + (tid & 15) * 16) = make_uint4(v.x, v.y, v.x, v.y);
+    }
+  }
+  if (used & 4u)
+    for (int i = tid; i < 4096; i += cross_detail::kThreads)
+      *reinterpret_cast<uint2*>(smem + kLut1B + i * 8) = quad(cbs + cb_index(3), i, 3);
+  if (used & 8u)
+    for (int i = tid; i < 256 * 8; i += cross_detail::kThreads) {
+      const int e = i >> 3;
+      *reinterpret_cast<uint32_t*>(smem + kLut4 + i * 4) =
+          cbs[cb_index(4) + (e & 15)] | static_cast<uint32_t>(cbs[cb_index(4) + (e >> 4)]) << 16;
+    }
+  if (used & 16u)
+    for (int i = tid; i < 32 * 32; i += cross_detail::kThreads)
+      *reinterpret_cast<uint32_t*>(smem + kLut5 + i * 4) = cbs[cb_index(5) + (i >> 5)];
+  if (used & 0xE0u) {
+    const int i = tid;
+    if (i < 256 + 128 + 64) {
+      const int b = i < 256 ? 8 : (i < 384 ? 7 : 6), k = i < 256 ? i : (i < 384 ? i - 256 : i - 384);
+      *reinterpret_cast<uint16_t*>(smem + kLutF + i * 2) = cbs[cb_index(b) + k];
+    }
+  }
+}
+
+// ---------------------------------------------------------------- kernel
+// EX: the softmax weights in two fp16 parts (22 bits) for fp32 outputs; one
+// part moves an output by at most 2^-11, half the rounding to bf16.
+template <int KWB, int BV, bool EX>
+__global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(2, 2))) void k_cross(
+    Dims d, const uint8_t* __restrict__ blob, const void* __restrict__ q, CrossCall call) {
+  __shared__ __attribute__((aligned(16))) uint8_t smem[kLds];
+  const int tid = threadIdx.x, lane = tid & 63, l32 = lane & 31, hf = lane >> 5;
+  const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int G = d.group, hq = d.n_kv * G, kw = d.k_words;
+  const int second = static_cast<int>(blockIdx.x) >= call.side[0].items;
+  const CrossSide& S = call.side[second];
+  int item = static_cast<int>(blockIdx.x) - (second ? call.side[0].items : 0);
+  const int split = item % S.n_splits;
+  item /= S.n_splits;
+  const int nr = S.n_q * G, n_blocks = (nr + kRows - 1) / kRows;
+  const int r0 = item % n_blocks * kRows;
+  item /= n_blocks;
+  const int kvh = item % d.n_kv, lz = item / d.n_kv;
+  const int seq = lz % S.batch, layer = d.layer >= 0 ? d.layer : lz / S.batch;
+  const int ri = layer * d.n_kv + kvh;
+  const RowMeta* M = reinterpret_cast<const RowMeta*>(blob + kOffRows) + ri;
+  const int ng = M->n_groups, nslot = (ng + 1) & ~1;
+  const auto row_at = [&](int r) {  // query row r of the unit, in q, out and the partials
+    return (static_cast<size_t>(lz) * S.n_q + r / G) * hq + kvh * G + r % G;
+  };
+
+  // a length outside [0, max_len] (the host's bound) makes the rows NaN
+  const int len = S.len[seq];
+  const bool ok = len >= 0 && len <= S.max_len;
+  const int t_begin = split * S.split_len;
+  const int t_end = ok ? min(len, t_begin + S.split_len) : t_begin;
+
+  // ---- set-up: codebooks; the query rows rotated into stream order,
+  //   q'[p] = log2 e / sqrt(d_g d_h) sum_d W[p][d] q[d],
+  // on fp32 MFMAs (wave = 16 positions, two blocks of 16 rows); every global
+  // read is issued before the first wait.
+  uint32_t gm[8], used = 1u << (BV - 1);
+#pragma unroll
+  for (int b = 0; b < 8; ++b) {
+    gm[b] = M->gm[b];
+    used |= (gm[b] >> 31) << b;
+  }
+  float* qs = reinterpret_cast<float*>(smem);  // [32 rows][kAccStride] rotated queries, before the tables
+  uint16_t* cbs = reinterpret_cast<uint16_t*>(smem + kBooks);
+  {
+    const uint16_t* c16 = reinterpret_cast<const uint16_t*>(blob + kOffC16);
+    const float4_t* w = reinterpret_cast<const float4_t*>(blob + layout_kdense_offset(d.n_layers * d.n_kv)) +
+                        static_cast<size_t>(ri) * (kMfmaMatFloats / 4) + wave * 8 * 64 + lane;
+    float4_t a[8];
+#pragma unroll
+    for (int s4 = 0; s4 < 8; ++s4) a[s4] = w[s4 * 64];
+    const uint16_t cv = c16[min(tid, kCodebookEntries - 1)];
+    const int p0 = 16 * wave + 4 * (lane >> 4);  // the lane's positions of the product
+    float scale[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+      scale[i] = kLog2e * kRsqrtD * rsqrtf(static_cast<float>(M->g_dim[M->grp[p0 + i]]));
+    if (tid < kCodebookEntries) cbs[tid] = cv;
+#pragma unroll
+    for (int c = 0; c < 2; ++c) {
+      const int r = r0 + 16 * c + (lane & 15);
+      const size_t at = row_at(min(r, nr - 1)) * kHeadDim + 32 * (lane >> 4);
+      float b[32];
+      if (d.in_dtype == 1) {
+        const uint4* src = reinterpret_cast<const uint4*>(static_cast<const uint16_t*>(q) + at);
+#pragma unroll
+        for (int u = 0; u < 4; ++u) {
+          const uint4 v = src[u];
+          const uint32_t x[4] = {v.x, v.y, v.z, v.w};
+#pragma unroll
+          for (int e = 0; e < 4; ++e) {
+            b[8 * u + 2 * e] = __uint_as_float(x[e] << 16);
+            b[8 * u + 2 * e + 1] = __uint_as_float(x[e] & 0xFFFF0000u);
+          }
+        }
+      } else {
+        const float4_t* src = reinterpret_cast<const float4_t*>(static_cast<const float*>(q) + at);
+#pragma unroll
+        for (int u = 0; u < 8; ++u) {
+          const float4_t v = src[u];
+#pragma unroll
+          for (int e = 0; e < 4; ++e) b[4 * u + e] = v[e];
+        }
+      }
+      float4_t acc = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+      for (int s = 0; s < 32; ++s) acc = __builtin_amdgcn_mfma_f32_16x16x4f32(a[s >> 2][s & 3], b[s], acc, 0, 0, 0);
+#pragma unroll
+      for (int i = 0; i < 4; ++i) acc[i] *= scale[i];
+      *reinterpret_cast<float4_t*>(qs + (16 * c + (lane & 15)) * kAccStride + p0) = acc;
+    }
+  }
+  __syncthreads();
+  // The image of a row is scaled by the power of two that brings its largest
+  // coordinate to [2^13, 2^14): the lo parts stay above fp16's subnormals.
+  // (thread = (row, step and half); 16 threads a row)
+  {
+    const int r = tid >> 4, sub = tid & 15;
+    const float* src = qs + r * kAccStride;
+    float mx = 0.f;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) mx = fmaxf(mx, fabsf(src[sub * 8 + i]));
+#pragma unroll
+    for (int k = 1; k < 16; k *= 2) mx = fmaxf(mx, __shfl_xor(mx, k));
+    const int e = static_cast<int>(__float_as_uint(mx) >> 23);  // biased
+    const bool plain = e == 0 || e == 255;                      // zeros; not finite
+    const int up = plain ? 127 : max(1, min(253, 127 + 13 + 127 - e));
+    const float to = __uint_as_float(static_cast<uint32_t>(up) << 23);
+    if (sub == 0) *reinterpret_cast<float*>(smem + kScale + 4 * r) = __uint_as_float(static_cast<uint32_t>(254 - up) << 23);
+    // steps numbered group after group; item = (step, half)
+    for (int it = sub; it < 2 * kMaxSteps; it += 16) {
+      int st = it >> 1, p = -1, left = 0;
+#pragma unroll
+      for (int b = 0; b < 8; ++b) {
+        const int n16 = gm[b] >> 31 ? (split_detail::gm_steps(gm[b]) + 3) >> 2 : 0;
+        if (p < 0 && st >= 0 && st < n16) {
+          const int g = split_detail::gm_plane(gm[b]);
+          p = M->g_pos[g] + 16 * st + 8 * (it & 1);
+          left = M->g_dim[g] - 16 * st - 8 * (it & 1);
+        }
+        st -= n16;
+      }
+      if (p < 0) continue;
+      half8_t hi, lo;
+#pragma unroll
+      for (int j = 0; j < 8; ++j) {
+        const float x = j < left ? src[p + j] * to : 0.f;
+        hi[j] = static_cast<_Float16>(x);
+        lo[j] = static_cast<_Float16>(x - static_cast<float>(hi[j]));
+      }
+      uint8_t* dst = smem + kImg + (it >> 1) * 2048 + ((it & 1) * 32 + r) * 16;
+      *reinterpret_cast<half8_t*>(dst) = hi;
+      *reinterpret_cast<half8_t*>(dst + 1024) = lo;
+    }
+  }
+  __syncthreads();
+  build_tables(smem, cbs, used, tid);
+  __syncthreads();
+
+  LaneRep rep{static_cast<uint32_t>(split_detail::kLut1 + (lane & 15) * 8),
+              static_cast<uint32_t>(split_detail::kLut3 + (lane & 31) * 4),
+              static_cast<uint32_t>(split_detail::kLut4 + (lane & 7) * 4),
+              static_cast<uint32_t>(split_detail::kLut5 + (lane & 31) * 4),
+              static_cast<uint32_t>(split_detail::kLut2 + (lane & 31) * 8),
+              static_cast<uint32_t>(split_detail::kLut1B), 0u};
+  asm volatile("" : "+v"(rep.r1), "+v"(rep.r3), "+v"(rep.r4), "+v"(rep.r5), "+v"(rep.r2), "+v"(rep.r1b));
+  const float sc = *reinterpret_cast<const float*>(smem + kScale + 4 * l32);
+  uint8_t* const rad = smem + kRad + wave * kRadBytes;
+  const uint8_t* const rad_l = rad + 8 * hf;  // the lane's tokens start at 4 hf
+
+  const size_t row = (static_cast<size_t>(layer) * S.batch + seq) * d.n_kv + kvh;
+  const size_t cap = S.capacity;
+  const uint32_t* kc = S.c.k_codes + row * cap * kw;
+  const uint16_t* kn = S.c.k_norms + row * kMaxGroups * cap;
+  const uint32_t* vc = S.c.v_codes + row * (cap / kTile) * kHeadDim * BV;
+  const uint16_t* vn = S.c.v_norms + row * cap;
+
+  float m_run = kNegInf, l_run = 0.f;
+  float16_t o[4];
+#pragma unroll
+  for (int cc = 0; cc < 4; ++cc)
+#pragma unroll
+    for (int i = 0; i < 16; ++i) o[cc][i] = 0.f;
+
+  uint32_t nw[KWB], knp[4], vnw, vw[2][4][BV];
+  const auto load_keys = [&](int t0) {
+    const uint32_t* src = kc + static_cast<size_t>(t0) * kw;
+    const uint32_t at = static_cast<uint32_t>(lane * kw * 4);
+    if ((kw & 3) == 0) {
+#pragma unroll
+      for (int i = 0; i < KWB; i += 4) {
+        const uint4 v = i < kw ? ld_at<uint4>(src, at + 4 * i) : make_uint4(0, 0, 0, 0);
+        nw[i] = v.x;
+        nw[i + 1] = v.y;
+        nw[i + 2] = v.z;
+        nw[i + 3] = v.w;
+      }
+    } else {
+#pragma unroll
+      for (int i = 0; i < KWB; ++i) nw[i] = i < kw ? ld_at<uint32_t>(src, at + 4 * i) : 0u;
+    }
+    // (a token's 16 bytes of radii stay inside the row's 8 slots per token)
+    const uint4 r = ld_at<uint4>(kn + static_cast<size_t>(t0) * nslot, static_cast<uint32_t>(lane * nslot * 2));
+    knp[0] = r.x;
+    knp[1] = r.y;
+    knp[2] = r.z;
+    knp[3] = r.w;
+    vnw = ld_at<uint16_t>(vn + t0, static_cast<uint32_t>(lane * 2));
+  };
+  const auto load_values = [&](int t0) {
+    const uint32_t* src = vc + static_cast<size_t>(t0 / kTile) * kHeadDim * BV;
+#pragma unroll
+    for (int n = 0; n < 2; ++n)
+#pragma unroll
+      for (int cc = 0; cc < 4; ++cc)
+#pragma unroll
+        for (int i = 0; i < BV; ++i)
+          vw[n][cc][i] = ld_at<uint32_t>(src + (n * kHeadDim + 32 * cc) * BV, static_cast<uint32_t>((l32 * BV + i) * 4));
+  };
+
+  int t0 = t_begin + wave * kKeyTile;
+  constexpr int kStride = kWaves * kKeyTile;
+  if (t0 < t_end) {
+    load_keys(t0);
+    load_values(t0);
+  }
+  for (; t0 < t_end; t0 += kStride) {
+    const bool full = t0 + kKeyTile <= t_end;
+    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");  // the last tile's reads of the radii come first
+    // this tile's radii, token-minor, for the wave's own reads (LDS operations
+    // of a wave complete in order); a token past the end has value radius 0:
+    // what lies there may be infinite or not a number
+#pragma unroll
+    for (int g = 0; g < 8; ++g)
+      if (g < ng) *reinterpret_cast<uint16_t*>(rad + 128 * g + 2 * lane) = static_cast<uint16_t>(knp[g >> 1] >> (16 * (g & 1)));
+    *reinterpret_cast<uint16_t*>(rad + 128 * 8 + 2 * lane) = static_cast<uint16_t>(t0 + lane < t_end ? vnw : 0u);
+    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+    __builtin_amdgcn_wave_barrier();
+    {
+      // the row's width table re-read every tile (scalar loads through an
+      // opaque offset): hoisted, its derived scalars exhaust the SGPRs
+      uint32_t goff = 0;
+      asm volatile("" : "+s"(goff));
+      const uint32_t* gmt = reinterpret_cast<const uint32_t*>(reinterpret_cast<const uint8_t*>(M->gm) + goff);
+#pragma unroll
+      for (int b = 0; b < 8; ++b) gm[b] = gmt[b];
+    }
+    uint32_t rw[KWB + split_detail::kRowPad];
+#pragma unroll
+    for (int i = 0; i < KWB; ++i) rw[i] = nw[i];
+#pragma unroll
+    for (int i = KWB; i < KWB + split_detail::kRowPad; ++i) rw[i] = 0u;
+    float16_t s[2];
+#pragma unroll
+    for (int n = 0; n < 2; ++n)
+#pragma unroll
+      for (int i = 0; i < 16; ++i) s[n][i] = 0.f;
+    qk_all<KWB>(std::make_integer_sequence<int, 8>{}, smem, rw, gm, rad_l, rep, lane, s);
+    if (t0 + kStride < t_end) load_keys(t0 + kStride);
+
+    // ---- online softmax, base 2
+    if (!full) {
+#pragma unroll
+      for (int n = 0; n < 2; ++n)
+#pragma unroll
+        for (int i = 0; i < 16; ++i) {
+          const int tok = t0 + 32 * n + 8 * (i >> 2) + 4 * hf + (i & 3);
+          s[n][i] = tok >= t_end ? kNegInf : s[n][i];
+        }
+    }
+    float mp[4];
+#pragma unroll
+    for (int c = 0; c < 4; ++c) {
+      mp[c] = fmaxf(s[0][4 * c], s[0][4 * c + 1]);
+      mp[c] = fmaxf(fmaxf(mp[c], s[0][4 * c + 2]), s[0][4 * c + 3]);
+      mp[c] = fmaxf(fmaxf(mp[c], s[1][4 * c]), s[1][4 * c + 1]);
+      mp[c] = fmaxf(fmaxf(mp[c], s[1][4 * c + 2]), s[1][4 * c + 3]);
+    }
+    const float mx = fmaxf(fmaxf(mp[0], mp[1]), fmaxf(mp[2], mp[3])) * sc;
+    // a tile that raises no running maximum of the wave skips the rescale
+    if (__builtin_amdgcn_ballot_w64(mx > m_run) != 0) {
+      float x, y;
+      swap32(mx, x, y);
+      const float mn = fmaxf(m_run, fmaxf(x, y));
+      const float corr = m_run == kNegInf ? 0.f : __builtin_amdgcn_exp2f(m_run - mn);
+      m_run = mn;
+      l_run *= corr;
+#pragma unroll
+      for (int cc = 0; cc < 4; ++cc) o[cc] *= corr;
+    }
+    const float mref = m_run == kNegInf ? 0.f : m_run;
+#pragma unroll
+    for (int n = 0; n < 2; ++n) {
+      uint32_t pw[8], pl[EX ? 8 : 1];
+      float ps = 0.f;
+#pragma unroll
+      for (int u = 0; u < 4; ++u) {
+        const uint2 vr = *reinterpret_cast<const uint2*>(rad_l + 128 * 8 + 2 * (32 * n + 8 * u));
+        float p[4];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) p[i] = __builtin_amdgcn_exp2f(fmaf(s[n][4 * u + i], sc, -mref));
+        ps += (p[0] + p[1]) + (p[2] + p[3]);
+        pw[2 * u] = mix_pair(p[0], p[1], vr.x);
+        pw[2 * u + 1] = mix_pair(p[2], p[3], vr.y);
+        if constexpr (EX) {
+#pragma unroll
+          for (int k = 0; k < 2; ++k) {
+            const half2_t h = __builtin_bit_cast(half2_t, pw[2 * u + k]), r = __builtin_bit_cast(half2_t, k ? vr.y : vr.x);
+            const half2_t x = {
+                static_cast<_Float16>(fmaf(p[2 * k], static_cast<float>(r[0]), -static_cast<float>(h[0]))),
+                static_cast<_Float16>(fmaf(p[2 * k + 1], static_cast<float>(r[1]), -static_cast<float>(h[1])))};
+            pl[2 * u + k] = __builtin_bit_cast(uint32_t, x);
+          }
+        }
+      }
+      l_run += ps;
+#pragma unroll
+      for (int cc = 0; cc < 4; ++cc) {
+        // the codes of tokens 8 k + 4 hf .. + 3 to bit 8 k BV
+        uint32_t w[BV + 1];
+#pragma unroll
+        for (int i = 0; i < BV; ++i) {
+          const uint32_t up = i + 1 < BV ? vw[n][cc][i + 1] : 0u;
+          if constexpr (BV == 8) w[i] = hf ? up : vw[n][cc][i];
+          else w[i] = __builtin_amdgcn_alignbit(up, vw[n][cc][i], 4 * BV * hf);
+        }
+        w[BV] = 0;
+        const half4_t v0 = decode4<BV, 0, true>(smem, w, rep), v1 = decode4<BV, 8 * BV, true>(smem, w, rep);
+        const half4_t v2 = decode4<BV, 16 * BV, true>(smem, w, rep), v3 = decode4<BV, 24 * BV, true>(smem, w, rep);
+        const half8_t a0 = {v0[0], v0[1], v0[2], v0[3], v1[0], v1[1], v1[2], v1[3]};
+        const half8_t a1 = {v2[0], v2[1], v2[2], v2[3], v3[0], v3[1], v3[2], v3[3]};
+        const half8_t b0 = __builtin_bit_cast(half8_t, make_uint4(pw[0], pw[1], pw[2], pw[3]));
+        const half8_t b1 = __builtin_bit_cast(half8_t, make_uint4(pw[4], pw[5], pw[6], pw[7]));
+        o[cc] = __builtin_amdgcn_mfma_f32_32x32x16_f16(a0, b0, o[cc], 0, 0, 0);
+        o[cc] = __builtin_amdgcn_mfma_f32_32x32x16_f16(a1, b1, o[cc], 0, 0, 0);
+        if constexpr (EX) {
+          const half8_t c0 = __builtin_bit_cast(half8_t, make_uint4(pl[0], pl[1], pl[2], pl[3]));
+          const half8_t c1 = __builtin_bit_cast(half8_t, make_uint4(pl[4], pl[5], pl[6], pl[7]));
+          o[cc] = __builtin_amdgcn_mfma_f32_32x32x16_f16(a0, c0, o[cc], 0, 0, 0);
+          o[cc] = __builtin_amdgcn_mfma_f32_32x32x16_f16(a1, c1, o[cc], 0, 0, 0);
+        }
+      }
+    }
+    if (t0 + kStride < t_end) load_values(t0 + kStride);
+  }
+  {
+    float x, y;
+    swap32(l_run, x, y);
+    l_run = x + y;
+  }
+
+  // ---- the waves' states joined in LDS (over the tables)
+  float4_t rot[8];  // this wave's 16 output dims of Pi_V^T, for the output rotation
+  if (call.n_slots == 1) {
+    const float4_t* src = reinterpret_cast<const float4_t*>(blob + kOffRotVT) +
+                          ((16 * wave + (lane & 15)) * kHeadDim + 32 * (lane >> 4)) / 4;
+#pragma unroll
+    for (int s4 = 0; s4 < 8; ++s4) rot[s4] = src[s4];
+  }
+  __syncthreads();
+  float* const acc = reinterpret_cast<float*>(smem);
+  float* const ms = reinterpret_cast<float*>(smem + kEndM);
+  float* const ls = ms + kWaves * kRows;
+#pragma unroll
+  for (int cc = 0; cc < 4; ++cc)
+#pragma unroll
+    for (int u = 0; u < 4; ++u)
+      *reinterpret_cast<float4_t*>(acc + (wave * kRows + l32) * kAccStride + 32 * cc + 8 * u + 4 * hf) =
+          float4_t{o[cc][4 * u], o[cc][4 * u + 1], o[cc][4 * u + 2], o[cc][4 * u + 3]};
+  if (hf == 0) {
+    ms[wave * kRows + l32] = m_run;
+    ls[wave * kRows + l32] = l_run;
+  }
+  __syncthreads();
+  const int r = tid >> 4, d0 = (tid & 15) * 4;  // dims d0 .. + 3 and 64 + d0 .. + 3 of row r
+  float m = kNegInf, l = 0.f;
+  float4_t a[2] = {{0.f, 0.f, 0.f, 0.f}, {0.f, 0.f, 0.f, 0.f}};
+#pragma unroll
+  for (int w = 0; w < kWaves; ++w) m = fmaxf(m, ms[w * kRows + r]);
+  const float mref = m == kNegInf ? 0.f : m;
+#pragma unroll
+  for (int w = 0; w < kWaves; ++w) {
+    const float e = __builtin_amdgcn_exp2f(ms[w * kRows + r] - mref);
+    l = fmaf(ls[w * kRows + r], e, l);
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+      const float4_t x = *reinterpret_cast<const float4_t*>(acc + (w * kRows + r) * kAccStride + 64 * h + d0);
+#pragma unroll
+      for (int i = 0; i < 4; ++i) a[h][i] = fmaf(x[i], e, a[h][i]);
+    }
+  }
+  if (!ok) l = __builtin_nanf("");
+  if (call.n_slots > 1) {
+    if (r0 + r < nr) {
+      float* P = call.part + (row_at(r0 + r) * call.n_slots + S.slot0 + split) * kPartFloats;
+      if (d0 == 0) {
+        // no row seen: -inf; logits that are all not a number leave the
+        // maximum at -inf (fmaxf passes over them) but not the sum at 0
+        P[0] = l == 0.f ? kNegInf : mref;
+        P[1] = l;
+      }
+      *reinterpret_cast<float4_t*>(P + 4 + d0) = a[0];
+      *reinterpret_cast<float4_t*>(P + 68 + d0) = a[1];
+    }
+    return;
+  }
+  // ---- the only partial: out = Pi_V^T (a / l) on fp32 MFMAs
+  __syncthreads();
+  const float inv = l == 0.f ? 0.f : kRsqrtD / l;
+  *reinterpret_cast<float4_t*>(acc + r * kAccStride + d0) = a[0] * inv;
+  *reinterpret_cast<float4_t*>(acc + r * kAccStride + 64 + d0) = a[1] * inv;
+  __syncthreads();
+#pragma unroll
+  for (int c = 0; c < 2; ++c) {
+    const int rr = 16 * c + (lane & 15);
+    const float4_t* src = reinterpret_cast<const float4_t*>(acc + rr * kAccStride + 32 * (lane >> 4));
+    float4_t y = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+    for (int s4 = 0; s4 < 8; ++s4) {
+      const float4_t b = src[s4];
+#pragma unroll
+      for (int e = 0; e < 4; ++e) y = __builtin_amdgcn_mfma_f32_16x16x4f32(rot[s4][e], b[e], y, 0, 0, 0);
+    }
+    if (r0 + rr < nr) {
+      const size_t at = row_at(r0 + rr) * kHeadDim + 16 * wave + 4 * (lane >> 4);
+      store4(call.out, at, y, call.out_dtype);
+    }
+  }
+}
+
+template <int BV>
+hipError_t launch_bv(const Dims& d, const void* layout, const void* q, const CrossCall& call, hipStream_t s) {
+  const int items = call.side[0].items + call.side[1].items;
+  const auto go = [&](auto kern) {
+    hipLaunchKernelGGL(kern, dim3(items), dim3(kThreads), 0, s, d, static_cast<const uint8_t*>(layout), q, call);
+    return hipGetLastError();
+  };
+  const bool ex = call.out_dtype == 0;  // BGTQ_FP32
+  if (d.k_words <= 8) return ex ? go(k_cross<8, BV, true>) : go(k_cross<8, BV, false>);
+  if (d.k_words <= 12) return ex ? go(k_cross<12, BV, true>) : go(k_cross<12, BV, false>);
+  if (d.k_words <= 16) return ex ? go(k_cross<16, BV, true>) : go(k_cross<16, BV, false>);
+  return ex ? go(k_cross<32, BV, true>) : go(k_cross<32, BV, false>);
+}
+
+}  // namespace cross_detail
+}  // namespace bgtq

@@ -105,21 +105,43 @@ hipError_t launch_dequantize_rows(const Dims& d, const void* layout, const Cache
                                   int out_dtype, hipStream_t s);
 
 // Attention passes over packed rows that every query row sees (cross.hip).  A
-// pass leaves (m, l, acc[128]) of every query row ([n_lc][batch][n_q][Hq])
-// and split in part[row][slot0 + split], n_slots partials per row.
-constexpr int kPartFloats = 130;
-struct CrossPass {
-  float* part;
-  int n_slots, slot0;
+// side is one pass: the query rows of each unit against rows [0, len) of one
+// cache.  With n_slots > 1 it leaves (m, l, -, -, acc[128]) of every query row
+// ([n_lc][batch][n_q][Hq]) and split in part[row][slot0 + split], and `rows`
+// rows are joined into out; with one slot out is written at once.
+constexpr int kPartFloats = 132;
+struct CrossSide {
+  CachePtrs c;
+  const int32_t* len;       // cache rows of each of the side's sequences
+  int batch, capacity;      // of the side's cache
+  int n_q;                  // query rows per sequence and query head
   int n_splits, split_len;  // split_len: cache rows per split, a multiple of 64
-  int max_len;              // the host's bound on the lengths: a row of a sequence outside [0, max_len] is NaN
+  int max_len;              // the host's bound on the lengths: rows of a sequence outside [0, max_len] are NaN
+  int slot0;
+  int items;                // workgroups
+};
+struct CrossCall {
+  CrossSide side[2];  // the second one has no items in a call of one pass
+  float* part;
+  int n_slots;
+  void* out;
+  int out_dtype;
 };
 long cross_items(const Dims& d, int n_q, int n_splits);  // workgroups of a pass
-hipError_t launch_cross_pass(const Dims& d, const void* layout, const void* q, int n_q, const int32_t* ctx_len,
-                             const CachePtrs& c, const CrossPass& ps, hipStream_t s);
-// Joins the partials of `rows` query rows into out.
-hipError_t launch_cross_merge(const void* layout, long rows, const float* part, int n_slots, void* out, int out_dtype,
-                              hipStream_t s);
+hipError_t launch_cross(const Dims& d, const void* layout, const void* q, const CrossCall& call, long rows,
+                        hipStream_t s);
+// k_cross (cross_impl.h), one entry per value code width (cross_bv1.hip .. cross_bv8.hip).
+#define BGTQ_DECL_CROSS(N) \
+  hipError_t launch_cross_bv##N(const Dims& d, const void* layout, const void* q, const CrossCall& call, hipStream_t s);
+BGTQ_DECL_CROSS(1)
+BGTQ_DECL_CROSS(2)
+BGTQ_DECL_CROSS(3)
+BGTQ_DECL_CROSS(4)
+BGTQ_DECL_CROSS(5)
+BGTQ_DECL_CROSS(6)
+BGTQ_DECL_CROSS(7)
+BGTQ_DECL_CROSS(8)
+#undef BGTQ_DECL_CROSS
 
 // Streaming read of `bytes` (a multiple of 16, 16-byte aligned) at src;
 // writes sink[0] only in a case no real input reaches (probe.hip).
