@@ -25,6 +25,10 @@ FLAGS = [
 # (finite codebooks and radii, -inf only as a mask), so skip the IEEE
 # canonicalization that would otherwise precede every max.
 DECODE_FLAGS = ["-fno-honor-nans", "-mno-amdgpu-ieee"]
+# The kernels that index a key row's words at a wave-uniform position keep them
+# in registers: beside their accumulators the default budget (bytes) puts the
+# array in scratch memory.
+INDEXED_FLAGS = ["-mllvm", "-amdgpu-promote-alloca-to-vector-limit=100000"]
 
 
 def _run(cmd):
@@ -42,7 +46,7 @@ def build(verbose: bool = False) -> str:
     for src in SOURCES:
         obj = os.path.join(BUILD_DIR, src + ".o")
         lang = ["-x", "hip"]
-        extra = DECODE_FLAGS if src.startswith("decode_") else []
+        extra = DECODE_FLAGS if src.startswith("decode_") else INDEXED_FLAGS if src == "rows.hip" else []
         cmds.append([HIPCC, *FLAGS, *extra, *lang, "-c", os.path.join(CSRC, src), "-o", obj])
         objs.append(obj)
     with ThreadPoolExecutor(max_workers=min(len(cmds), os.cpu_count() or 4, 16)) as ex:

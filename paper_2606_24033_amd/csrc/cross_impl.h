@@ -129,7 +129,7 @@ __device__ __forceinline__ void qk_group(const uint8_t* smem, const uint32_t (&r
   constexpr int NW = (CH * 16 * B + 31) / 32;    // its words
   const int o = split_detail::gm_off(gm), n16 = (split_detail::gm_steps(gm) + 3) >> 2;
   float16_t part[2];
-  const auto chunk = [&](auto first, int c) {
+  const auto chunk = [&](auto first, int c) __attribute__((always_inline)) {
     const int at = o + c * 16 * B, w0 = at >> 5, sh = at & 31;
     uint32_t aw[NW + 1];
 #pragma unroll
@@ -159,7 +159,7 @@ __device__ __forceinline__ void qk_all(std::integer_sequence<int, BM1...>, const
                                        const uint32_t (&rw)[KWB + split_detail::kRowPad], const uint32_t (&gm)[8],
                                        const uint8_t* radii, const LaneRep& rep, int lane, float16_t (&s)[2]) {
   int step0 = 0;
-  const auto one = [&](auto bm1) {
+  const auto one = [&](auto bm1) __attribute__((always_inline)) {
     constexpr int b = decltype(bm1)::value;
     if (gm[b] >> 31) {
       qk_group<b + 1, KWB>(smem, rw, gm[b], step0, radii + split_detail::gm_plane(gm[b]) * 128, rep, lane, s);

@@ -6,72 +6,451 @@
 //
 // with W the row's key rotation on the natural dims (zero outside position
 // p's group g, so its transpose is its inverse).
+//
+// Both are products with a 128 x 128 matrix on 32x32x16 f16 MFMAs,
+// D[dim][token] = A[dim][p] B[p][token], the matrix in fp16 in LDS (scaled by
+// 2^8 and 1 / sqrt(d_g)), built once per workgroup, which then walks many
+// tiles.  A workgroup does keys or values.
+//  * Keys: lane = token decodes 16 positions of one group, two codes a lookup,
+//    multiplies by the group's radius (scaled per token so that neither fp16's
+//    range nor its subnormals are reached) and v_permlane32_swap turns the 64
+//    tokens' registers into B operands of two 32-token blocks.
+//  * Values: codes lie dim after dim, so a 32-token tile is decoded lane = dim
+//    into LDS and read back lane = token.  The bare centroids are the operand;
+//    the radius scales the result.
+// bf16 outputs take one product: the matrix and r c rounded to fp16 (2^-11 each,
+// against the output's own 2^-8).  fp32 outputs take hi and lo parts of both (a
+// product of two fp16 numbers fits in them exactly), without lo x lo.
 #include <hip/hip_runtime.h>
 
+#include <algorithm>
+
+#include "decode_impl.h"
 #include "kernels.h"
 #include "layout.h"
 
 namespace bgtq {
 namespace {
 
-constexpr int kThreads = 128;  // one output dim per thread
-constexpr int kRowsPerWg = 16;
+using split_detail::field_at;
+using split_detail::ld_at;
+typedef _Float16 half8_t __attribute__((ext_vector_type(8)));
+typedef _Float16 half2_t __attribute__((ext_vector_type(2)));
+typedef float float4_t __attribute__((ext_vector_type(4)));
+typedef float float2_t __attribute__((ext_vector_type(2)));
+typedef float float16_t __attribute__((ext_vector_type(16)));
 
-__device__ __forceinline__ float half_bits(uint16_t b) { return static_cast<float>(__builtin_bit_cast(_Float16, b)); }
+constexpr int kWaves = 8, kThreads = kWaves * 64;
+constexpr int kMaxSteps = 15;       // 16-position steps of a key row, groups padded: at most (128 + 8 * 14) / 16
+constexpr float kMatScale = 256.f;  // keeps the matrix's lo parts above fp16's subnormals
+// ---- LDS map (bytes): codebooks, pair tables of the widths 1 .. 6 (entry i
+// of width b: the centroids of codes i % 2^b and i / 2^b), then the matrix
+// [part][step][dim block][lane] x 16 B, and behind it the values' tiles
+constexpr int kBooks = 0;
+constexpr int kPair = 1024;
+constexpr int kMaxPair = 6;
+__host__ __device__ constexpr int pair_offset(int b) { return kPair + 4 * (((1 << (2 * b)) - 4) / 3); }
+constexpr int kMat = (pair_offset(kMaxPair + 1) + 15) / 16 * 16;
+constexpr int kVSteps = kHeadDim / 16;
+constexpr int kTileStride = (kHeadDim + 8) * 2;  // bytes of a decoded token
+constexpr int kTileBytes = kTile * kTileStride;
+template <bool EX>
+constexpr int lds_bytes() {
+  constexpr int parts = EX ? 2 : 1;
+  constexpr int keys = parts * kMaxSteps * 4096, values = parts * kVSteps * 4096 + kWaves * kTileBytes;
+  return kMat + (keys > values ? keys : values);
+}
+static_assert(lds_bytes<true>() <= 160 * 1024, "LDS of one workgroup");
 
-__device__ __forceinline__ void store_out(void* out, size_t i, float v, int dtype) {  // BGTQ_BF16 = 1
-  if (dtype == 1) static_cast<__bf16*>(out)[i] = static_cast<__bf16>(v);
-  else static_cast<float*>(out)[i] = v;
+struct RowsCall {
+  CachePtrs c;
+  const int32_t* read_pos;
+  const int32_t* ctx_len;  // or null
+  void* out[2];            // keys, values; a null one has no workgroups
+  int n_rows;
+  int chunks[2], tiles[2];  // workgroups per unit and tiles (64 keys, 32 values) per workgroup
+  int key_items;            // workgroups of the keys
+};
+
+// Two consecutive B-bit codes at bit POS of w -> two fp16 centroids.
+template <int B, int POS, int N>
+__device__ __forceinline__ half2_t pair_at(const uint8_t* smem, const uint32_t (&w)[N]) {
+  if constexpr (B <= kMaxPair) {
+    return *reinterpret_cast<const half2_t*>(smem + pair_offset(B) + field_at<POS, 2 * B, 2>(w));
+  } else {
+    const half2_t r = {*reinterpret_cast<const _Float16*>(smem + kBooks + 2 * cb_index(B) + field_at<POS, B, 1>(w)),
+                       *reinterpret_cast<const _Float16*>(smem + kBooks + 2 * cb_index(B) + field_at<POS + B, B, 1>(w))};
+    return r;
+  }
 }
 
-// grid (ceil(n_rows / kRowsPerWg), n_kv, n_lc * batch): fp32 sums, one row at a time.
-__global__ __launch_bounds__(kThreads) void k_dequant_rows(Dims d, const uint8_t* __restrict__ blob, CachePtrs c,
-                                                           int n_rows, const int32_t* __restrict__ read_pos,
-                                                           const int32_t* __restrict__ ctx_len, void* __restrict__ k_out,
-                                                           void* __restrict__ v_out, int out_dtype) {
-  __shared__ float y[2][kHeadDim];
-  const int p = threadIdx.x, kvh = blockIdx.y, lz = blockIdx.z;
-  const int seq = lz % d.batch, layer = d.layer >= 0 ? d.layer : lz / d.batch;
-  const RowMeta* M = reinterpret_cast<const RowMeta*>(blob + kOffRows) + (layer * d.n_kv + kvh);
-  const int n_meta = d.n_layers * d.n_kv;
-  const float* w = reinterpret_cast<const float*>(blob + layout_kdense_offset(n_meta)) +
-                   static_cast<size_t>(layer * d.n_kv + kvh) * kMfmaMatFloats;
-  const float* rv = reinterpret_cast<const float*>(blob + kOffRotV);
-  const uint16_t* c16 = reinterpret_cast<const uint16_t*>(blob + kOffC16);
-  const size_t row = (static_cast<size_t>(layer) * d.batch + seq) * d.n_kv + kvh;
-  const uint32_t* kc = c.k_codes + row * d.capacity * d.k_words;
-  const uint16_t* kn = c.k_norms + row * kMaxGroups * d.capacity;
-  const uint32_t* vc = c.v_codes + row * (d.capacity / kTile) * kHeadDim * d.v_bits;
-  const uint16_t* vn = c.v_norms + row * d.capacity;
-  const int slots = (M->n_groups + 1) & ~1, width = M->width[p], off = M->bitoff[p], g = M->grp[p];
-  const float kscale = rsqrtf(static_cast<float>(M->g_dim[g]));
-  const int end = min(d.capacity, ctx_len ? ctx_len[seq] : d.capacity);
-  for (int i = blockIdx.x * kRowsPerWg; i < min(n_rows, (static_cast<int>(blockIdx.x) + 1) * kRowsPerWg); ++i) {
-    const long t = static_cast<long>(read_pos[seq]) + i;
-    if (t < 0 || t >= end) continue;  // uniform
-    const uint32_t* kr = kc + static_cast<size_t>(t) * d.k_words;
-    const int k0 = off >> 5;
-    uint64_t f = kr[k0];
-    if ((off & 31) + width > 32) f |= static_cast<uint64_t>(kr[k0 + 1]) << 32;
-    const uint32_t code = static_cast<uint32_t>(f >> (off & 31)) & ((1u << width) - 1u);
-    y[0][p] = half_bits(c16[cb_index(width) + code]) * (half_bits(kn[static_cast<size_t>(t) * slots + g]) * kscale);
-    const int vo = static_cast<int>(t % kTile) * d.v_bits, v0 = vo >> 5;
-    const uint32_t* vr = vc + (static_cast<size_t>(t / kTile) * kHeadDim + p) * d.v_bits;
-    f = vr[v0];
-    if ((vo & 31) + d.v_bits > 32) f |= static_cast<uint64_t>(vr[v0 + 1]) << 32;
-    const uint32_t vcode = static_cast<uint32_t>(f >> (vo & 31)) & ((1u << d.v_bits) - 1u);
-    y[1][p] = half_bits(c16[cb_index(d.v_bits) + vcode]) * (half_bits(vn[t]) * 0.08838834764831845f);
-    __syncthreads();
-    float k = 0.f, v = 0.f;
-    for (int j = 0; j < kHeadDim; ++j) {
-      k = fmaf(w[mfma_mat_index(j, p)], y[0][j], k);
-      v = fmaf(rv[j * kHeadDim + p], y[1][j], v);
-    }
-    const size_t o = ((static_cast<size_t>(lz) * n_rows + i) * d.n_kv + kvh) * kHeadDim + p;
-    if (k_out) store_out(k_out, o, k, out_dtype);
-    if (v_out) store_out(v_out, o, v, out_dtype);
-    __syncthreads();
+__device__ __forceinline__ void swap4(uint32_t (&x)[4], uint32_t (&y)[4]) {
+  asm("s_nop 1\n\t"
+      "v_permlane32_swap_b32 %0, %4\n\t"
+      "v_permlane32_swap_b32 %1, %5\n\t"
+      "v_permlane32_swap_b32 %2, %6\n\t"
+      "v_permlane32_swap_b32 %3, %7\n\t"
+      "s_nop 1"
+      : "+v"(x[0]), "+v"(x[1]), "+v"(x[2]), "+v"(x[3]), "+v"(y[0]), "+v"(y[1]), "+v"(y[2]), "+v"(y[3]));
+}
+__device__ __forceinline__ half8_t as_half8(const uint32_t (&x)[4]) {
+  return __builtin_bit_cast(half8_t, make_uint4(x[0], x[1], x[2], x[3]));
+}
+
+// One operand of the matrix: 8 numbers, rounded (and their residuals).
+template <bool EX>
+__device__ __forceinline__ void store_operand(uint8_t* dst, int part_bytes, float (&x)[8]) {
+  half8_t hi, lo;
+#pragma unroll
+  for (int j = 0; j < 8; ++j) {
+    // (x as fp32, opaque: a product rounded to fp16 at once in one place and by
+    // way of fp32 in the other gives two different hi parts next to a tie)
+    asm volatile("" : "+v"(x[j]));
+    hi[j] = static_cast<_Float16>(x[j]);
+    if constexpr (EX) lo[j] = static_cast<_Float16>(x[j] - static_cast<float>(hi[j]));
   }
+  *reinterpret_cast<half8_t*>(dst) = hi;
+  if constexpr (EX) *reinterpret_cast<half8_t*>(dst + part_bytes) = lo;
+}
+
+// acc (lane = token l32, registers = dims 32 cc + 8 (i / 4) + 4 hf + i % 4)
+// times scale, to the token's output row (valid lanes).
+template <bool EX>
+__device__ __forceinline__ void store_rows(const float16_t (&acc)[4], float scale, void* out, size_t at, int hf, bool valid) {
+#pragma unroll
+  for (int cc = 0; cc < 4; ++cc) {
+    float16_t y = acc[cc];
+    y *= scale;
+    if constexpr (EX) {
+      if (valid) {
+#pragma unroll
+        for (int u = 0; u < 4; ++u)
+          *reinterpret_cast<float4_t*>(static_cast<float*>(out) + at + 32 * cc + 8 * u + 4 * hf) =
+              float4_t{y[4 * u], y[4 * u + 1], y[4 * u + 2], y[4 * u + 3]};
+      }
+    } else {
+      // half-waves exchange, so that a lane has 8 consecutive dims: 16 u2 + 8 hf ..
+      typedef __bf16 bf16x4_t __attribute__((ext_vector_type(4)));
+      uint32_t a[4], b[4];
+#pragma unroll
+      for (int u = 0; u < 4; ++u) {
+        const float4_t f = {y[4 * u], y[4 * u + 1], y[4 * u + 2], y[4 * u + 3]};
+        const uint2 p = __builtin_bit_cast(uint2, __builtin_convertvector(f, bf16x4_t));
+        (u & 1 ? b : a)[u & ~1] = p.x;
+        (u & 1 ? b : a)[u | 1] = p.y;
+      }
+      swap4(a, b);
+      if (valid) {
+#pragma unroll
+        for (int u = 0; u < 2; ++u)
+          *reinterpret_cast<uint4*>(static_cast<uint16_t*>(out) + at + 32 * cc + 16 * u + 8 * hf) =
+              make_uint4(a[2 * u], a[2 * u + 1], b[2 * u], b[2 * u + 1]);
+      }
+    }
+  }
+}
+
+// ---------------------------------------------------------------- keys
+// Group of width B: its positions of the 64 tokens into the accumulators.
+template <int B, int KWB, bool EX>
+__device__ __forceinline__ void key_group(const uint8_t* smem, const uint32_t (&rw)[KWB + split_detail::kRowPad],
+                                          uint32_t gm, int step0, _Float16 radius, int lane, float16_t (&acc)[2][4]) {
+  constexpr int NW = (16 * B + 31) / 32;
+  const int o = split_detail::gm_off(gm), n16 = (split_detail::gm_steps(gm) + 3) >> 2;
+  const half2_t r = {radius, radius};
+  for (int c = 0; c < n16; ++c) {
+    const int at = o + c * 16 * B, w0 = at >> 5, sh = at & 31;
+    uint32_t aw[NW + 1];
+#pragma unroll
+    for (int i = 0; i < NW; ++i) aw[i] = __builtin_amdgcn_alignbit(rw[w0 + i + 1], rw[w0 + i], sh);
+    aw[NW] = 0;
+    const half2_t y[8] = {pair_at<B, 0>(smem, aw),      pair_at<B, 2 * B>(smem, aw),  pair_at<B, 4 * B>(smem, aw),
+                          pair_at<B, 6 * B>(smem, aw),  pair_at<B, 8 * B>(smem, aw),  pair_at<B, 10 * B>(smem, aw),
+                          pair_at<B, 12 * B>(smem, aw), pair_at<B, 14 * B>(smem, aw)};
+    uint32_t hi[2][4], lo[2][4];
+#pragma unroll
+    for (int u = 0; u < 8; ++u) {
+      const half2_t h = r * y[u];
+      hi[u >> 2][u & 3] = __builtin_bit_cast(uint32_t, h);
+      if constexpr (EX) lo[u >> 2][u & 3] = __builtin_bit_cast(uint32_t, __builtin_elementwise_fma(r, y[u], -h));
+    }
+    swap4(hi[0], hi[1]);
+    if constexpr (EX) swap4(lo[0], lo[1]);
+    const uint8_t* mat = smem + kMat + (step0 + c) * 4096 + lane * 16;
+#pragma unroll
+    for (int cc = 0; cc < 4; ++cc) {
+      const half8_t w = *reinterpret_cast<const half8_t*>(mat + cc * 1024);
+#pragma unroll
+      for (int n = 0; n < 2; ++n) acc[n][cc] = __builtin_amdgcn_mfma_f32_32x32x16_f16(w, as_half8(hi[n]), acc[n][cc], 0, 0, 0);
+      if constexpr (EX) {
+        const half8_t wl = *reinterpret_cast<const half8_t*>(mat + kMaxSteps * 4096 + cc * 1024);
+#pragma unroll
+        for (int n = 0; n < 2; ++n) acc[n][cc] = __builtin_amdgcn_mfma_f32_32x32x16_f16(w, as_half8(lo[n]), acc[n][cc], 0, 0, 0);
+#pragma unroll
+        for (int n = 0; n < 2; ++n) acc[n][cc] = __builtin_amdgcn_mfma_f32_32x32x16_f16(wl, as_half8(hi[n]), acc[n][cc], 0, 0, 0);
+      }
+    }
+  }
+}
+
+template <int KWB, bool EX, int... BM1>
+__device__ __forceinline__ void key_groups(std::integer_sequence<int, BM1...>, const uint8_t* smem,
+                                           const uint32_t (&rw)[KWB + split_detail::kRowPad], const uint32_t (&gm)[8],
+                                           const uint32_t (&radii)[4], half2_t up, int lane, float16_t (&acc)[2][4]) {
+  int step0 = 0;
+  const auto one = [&](auto bm1) __attribute__((always_inline)) {
+    constexpr int b = decltype(bm1)::value;
+    if (gm[b] >> 31) {
+      const uint32_t r = split_detail::radius_bits(radii, split_detail::gm_plane(gm[b]));
+      key_group<b + 1, KWB, EX>(smem, rw, gm[b], step0, __builtin_bit_cast(_Float16, static_cast<uint16_t>(r)) * up[0], lane, acc);
+      step0 += (split_detail::gm_steps(gm[b]) + 3) >> 2;
+    }
+  };
+  (one(std::integral_constant<int, BM1>{}), ...);
+}
+
+template <int KWB, bool EX>
+__device__ __forceinline__ void read_keys(uint8_t* smem, const Dims& d, const uint8_t* __restrict__ blob,
+                                          const RowsCall& call, int lz, int kvh, int chunk, long pos, int end) {
+  const int tid = threadIdx.x, lane = tid & 63, l32 = lane & 31, hf = lane >> 5;
+  const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int layer = d.layer >= 0 ? d.layer : lz / d.batch, seq = lz % d.batch, ri = layer * d.n_kv + kvh;
+  const RowMeta* M = reinterpret_cast<const RowMeta*>(blob + kOffRows) + ri;
+  const int ng = M->n_groups, nslot = (ng + 1) & ~1, kw = d.k_words;
+  uint32_t gm[8];
+#pragma unroll
+  for (int b = 0; b < 8; ++b) gm[b] = M->gm[b];
+
+  // ---- the matrix A[dim][p] = 2^8 / sqrt(d_g) Pi_g[p - p_g][index of dim in
+  // g], zero for dims of other groups and past a group's end; operand (step,
+  // dim block cc, lane) = dim 32 cc + lane % 32, positions 8 (lane / 32) .. + 7
+  // of the step.  The row's slot of the layout holds each Pi_g transposed.
+  {
+    const float* rot = reinterpret_cast<const float*>(blob + layout_rowrot_offset(d.n_layers * d.n_kv)) +
+                       static_cast<size_t>(ri) * kRowRotFloats;
+    uint8_t* inv = smem + kMat;  // dim -> stream position, until the matrix is built
+    if (tid < kHeadDim) inv[M->dim[tid]] = static_cast<uint8_t>(tid);
+    __syncthreads();
+    const int my = inv[tid & 127];  // (a thread always has the same dim: 512 is a multiple of 128)
+    __syncthreads();
+    // thread = (dim tid % 128, half and step parity tid / 128); the operands of
+    // steps tid / 256, + 2, ...
+    const int dim = tid & 127, h8 = (tid >> 7) & 1;
+    int st0 = 0, off = 0;
+#pragma unroll 1
+    for (int g = 0; g < ng; ++g) {
+      const int dg = M->g_dim[g], p0 = M->g_pos[g], n16 = (dg + 15) >> 4;
+      const float scale = kMatScale * rsqrtf(static_cast<float>(dg));
+      const bool mine = my >= p0 && my < p0 + dg;
+      const float* src = rot + off + (mine ? my - p0 : 0) * dg;
+      for (int st = tid >> 8; st < n16; st += 2) {
+        const int j0 = 16 * st + 8 * h8;
+        float x[8];
+#pragma unroll
+        for (int j = 0; j < 8; j += 2) {  // (group sizes are even, and so are the blocks' offsets)
+          const float2_t v = mine && j0 + j < dg ? *reinterpret_cast<const float2_t*>(src + j0 + j) : float2_t{0.f, 0.f};
+          x[j] = v[0] * scale;
+          x[j + 1] = v[1] * scale;
+        }
+        store_operand<EX>(smem + kMat + (st0 + st) * 4096 + (dim >> 5) * 1024 + (h8 * 32 + (dim & 31)) * 16, kMaxSteps * 4096, x);
+      }
+      st0 += n16;
+      off += dg * dg;
+    }
+  }
+  __syncthreads();
+
+  const size_t row = (static_cast<size_t>(layer) * d.batch + seq) * d.n_kv + kvh;
+  const size_t cap = d.capacity;
+  const uint32_t* kc = call.c.k_codes + row * cap * kw;
+  const uint16_t* kn = call.c.k_norms + row * kMaxGroups * cap;
+  const int n_tiles = (call.n_rows + 63) / 64, first = chunk * call.tiles[0];
+  for (int tile = first + wave; tile < min(n_tiles, first + call.tiles[0]); tile += kWaves) {
+    const int i = tile * 64 + lane;
+    const long t = pos + i;
+    const bool valid = i < call.n_rows && t >= 0 && t < end;
+    const size_t tr = valid ? static_cast<size_t>(t) : 0;  // (any row of the cache: its result is not stored)
+    uint32_t nw[KWB], rw[KWB + split_detail::kRowPad], radii[4];
+    const uint32_t* src = kc + tr * kw;
+    if ((kw & 3) == 0) {
+#pragma unroll
+      for (int k = 0; k < KWB; k += 4) {
+        const uint4 v = k < kw ? *reinterpret_cast<const uint4*>(src + k) : make_uint4(0, 0, 0, 0);
+        nw[k] = v.x;
+        nw[k + 1] = v.y;
+        nw[k + 2] = v.z;
+        nw[k + 3] = v.w;
+      }
+    } else {
+#pragma unroll
+      for (int k = 0; k < KWB; ++k) nw[k] = k < kw ? src[k] : 0u;
+    }
+#pragma unroll
+    for (int k = 0; k < KWB; ++k) {
+      // (one word at a time: as merged vector stores the indexed array would live in scratch memory)
+      asm volatile("" : "+v"(nw[k]));
+      rw[k] = nw[k];
+    }
+#pragma unroll
+    for (int k = KWB; k < KWB + split_detail::kRowPad; ++k) rw[k] = 0u;
+    {
+      // (a token's 16 bytes of radii stay inside the row's 8 slots per token)
+      const uint32_t* r = reinterpret_cast<const uint32_t*>(kn + tr * nslot);
+#pragma unroll
+      for (int k = 0; k < 4; ++k) radii[k] = r[k];
+    }
+    // 2^up brings the token's largest radius to [2^12, 2^13)
+    uint32_t top = 0;
+#pragma unroll
+    for (int g = 0; g < kMaxGroups; ++g)
+      if (g < ng) top = max(top, (radii[g >> 1] >> (16 * (g & 1))) & 0x7FFFu);
+    const int e = static_cast<int>(top >> 10);
+    const int up = e == 31 ? 0 : max(-3, min(15, 27 - e));
+    const _Float16 uph = __builtin_bit_cast(_Float16, static_cast<uint16_t>((up + 15) << 10));
+    float16_t acc[2][4];
+#pragma unroll
+    for (int n = 0; n < 2; ++n)
+#pragma unroll
+      for (int cc = 0; cc < 4; ++cc)
+#pragma unroll
+        for (int k = 0; k < 16; ++k) acc[n][cc][k] = 0.f;
+    key_groups<KWB, EX>(std::make_integer_sequence<int, 8>{}, smem, rw, gm, radii, half2_t{uph, uph}, lane, acc);
+    const float down = __uint_as_float(static_cast<uint32_t>(127 - up) << 23) / kMatScale;
+    const unsigned long long ok = __builtin_amdgcn_ballot_w64(valid);
+#pragma unroll
+    for (int n = 0; n < 2; ++n) {
+      // lane = token 32 n + l32 of the tile
+      const float scale = __shfl(down, 32 * n + l32);
+      const size_t at = ((static_cast<size_t>(lz) * call.n_rows + tile * 64 + 32 * n + l32) * d.n_kv + kvh) * kHeadDim;
+      store_rows<EX>(acc[n], scale, call.out[0], at, hf, (ok >> (32 * n + l32)) & 1u);
+    }
+  }
+}
+
+// ---------------------------------------------------------------- values
+template <int BV>
+__device__ __forceinline__ void decode_values(const uint8_t* smem, uint8_t* tile, const uint32_t* __restrict__ src, int lane) {
+#pragma unroll
+  for (int h = 0; h < 2; ++h) {
+    const int dim = 64 * h + lane;
+    uint32_t w[BV + 1];
+#pragma unroll
+    for (int i = 0; i < BV; ++i) w[i] = src[dim * BV + i];
+    w[BV] = 0;
+    const half2_t y[16] = {pair_at<BV, 0>(smem, w),       pair_at<BV, 2 * BV>(smem, w),  pair_at<BV, 4 * BV>(smem, w),
+                           pair_at<BV, 6 * BV>(smem, w),  pair_at<BV, 8 * BV>(smem, w),  pair_at<BV, 10 * BV>(smem, w),
+                           pair_at<BV, 12 * BV>(smem, w), pair_at<BV, 14 * BV>(smem, w), pair_at<BV, 16 * BV>(smem, w),
+                           pair_at<BV, 18 * BV>(smem, w), pair_at<BV, 20 * BV>(smem, w), pair_at<BV, 22 * BV>(smem, w),
+                           pair_at<BV, 24 * BV>(smem, w), pair_at<BV, 26 * BV>(smem, w), pair_at<BV, 28 * BV>(smem, w),
+                           pair_at<BV, 30 * BV>(smem, w)};
+#pragma unroll
+    for (int u = 0; u < 16; ++u) {
+      *reinterpret_cast<_Float16*>(tile + (2 * u) * kTileStride + 2 * dim) = y[u][0];
+      *reinterpret_cast<_Float16*>(tile + (2 * u + 1) * kTileStride + 2 * dim) = y[u][1];
+    }
+  }
+}
+
+template <bool EX>
+__device__ __forceinline__ void read_values(uint8_t* smem, const Dims& d, const uint8_t* __restrict__ blob,
+                                            const RowsCall& call, int lz, int kvh, int chunk, long pos, int end) {
+  const int tid = threadIdx.x, lane = tid & 63, l32 = lane & 31, hf = lane >> 5;
+  const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int layer = d.layer >= 0 ? d.layer : lz / d.batch, seq = lz % d.batch;
+  // A[dim][j] = 2^8 / sqrt(128) Pi_V[j][dim], read from the transposed Pi_V
+  {
+    const float* rot = reinterpret_cast<const float*>(blob + kOffRotVT);
+    for (int it = tid; it < kVSteps * 4 * 64; it += kThreads) {
+      const int l = it & 63, cc = (it >> 6) & 3, st = it >> 8;
+      const float4_t* src = reinterpret_cast<const float4_t*>(rot + (32 * cc + (l & 31)) * kHeadDim + 16 * st + 8 * (l >> 5));
+      const float4_t a = src[0] * (kMatScale * 0.08838834764831845f), b = src[1] * (kMatScale * 0.08838834764831845f);
+      float x[8] = {a[0], a[1], a[2], a[3], b[0], b[1], b[2], b[3]};
+      store_operand<EX>(smem + kMat + it * 16, kVSteps * 4096, x);
+    }
+  }
+  __syncthreads();
+  const size_t row = (static_cast<size_t>(layer) * d.batch + seq) * d.n_kv + kvh;
+  const size_t cap = d.capacity;
+  const int bv = d.v_bits;
+  const uint32_t* vc = call.c.v_codes + row * (cap / kTile) * kHeadDim * bv;
+  const uint16_t* vn = call.c.v_norms + row * cap;
+  uint8_t* const mine = smem + kMat + (EX ? 2 : 1) * kVSteps * 4096 + wave * kTileBytes;
+  // cache tiles from the one that holds the first row
+  const long tile0 = pos >> 5, tile_end = (pos + call.n_rows + kTile - 1) >> 5;
+  for (long tile = tile0 + chunk * call.tiles[1] + wave; tile < min(tile_end, tile0 + (chunk + 1l) * call.tiles[1]); tile += kWaves) {
+    if (tile < 0 || tile * kTile >= end) continue;  // uniform
+    const uint32_t* src = vc + static_cast<size_t>(tile) * kHeadDim * bv;
+    const long t = tile * kTile + l32;
+    const uint16_t radius = vn[t];
+    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");  // the last tile's reads come before this one's writes
+    switch (bv) {
+      case 1: decode_values<1>(smem, mine, src, lane); break;
+      case 2: decode_values<2>(smem, mine, src, lane); break;
+      case 3: decode_values<3>(smem, mine, src, lane); break;
+      case 4: decode_values<4>(smem, mine, src, lane); break;
+      case 5: decode_values<5>(smem, mine, src, lane); break;
+      case 6: decode_values<6>(smem, mine, src, lane); break;
+      case 7: decode_values<7>(smem, mine, src, lane); break;
+      default: decode_values<8>(smem, mine, src, lane); break;
+    }
+    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");  // a wave's LDS operations complete in order
+    __builtin_amdgcn_wave_barrier();
+    float16_t acc[4];
+#pragma unroll
+    for (int cc = 0; cc < 4; ++cc)
+#pragma unroll
+      for (int k = 0; k < 16; ++k) acc[cc][k] = 0.f;
+#pragma unroll
+    for (int st = 0; st < kVSteps; ++st) {
+      const half8_t y = *reinterpret_cast<const half8_t*>(mine + l32 * kTileStride + 32 * st + 16 * hf);
+      const uint8_t* mat = smem + kMat + st * 4096 + lane * 16;
+#pragma unroll
+      for (int cc = 0; cc < 4; ++cc)
+        acc[cc] = __builtin_amdgcn_mfma_f32_32x32x16_f16(*reinterpret_cast<const half8_t*>(mat + cc * 1024), y, acc[cc], 0, 0, 0);
+      if constexpr (EX) {
+#pragma unroll
+        for (int cc = 0; cc < 4; ++cc)
+          acc[cc] = __builtin_amdgcn_mfma_f32_32x32x16_f16(
+              *reinterpret_cast<const half8_t*>(mat + kVSteps * 4096 + cc * 1024), y, acc[cc], 0, 0, 0);
+      }
+    }
+    const float scale = static_cast<float>(__builtin_bit_cast(_Float16, radius)) / kMatScale;
+    const long i = t - pos;
+    const bool valid = i >= 0 && i < call.n_rows && t < end;
+    const size_t at = ((static_cast<size_t>(lz) * call.n_rows + (valid ? i : 0)) * d.n_kv + kvh) * kHeadDim;
+    store_rows<EX>(acc, scale, call.out[1], at, hf, valid);
+  }
+}
+
+// One-dimensional grid: the keys' (unit, chunk) items, then the values'.
+template <int KWB, bool EX>
+__global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(2, 2))) void k_read_rows(
+    Dims d, const uint8_t* __restrict__ blob, RowsCall call) {
+  __shared__ __attribute__((aligned(16))) uint8_t smem[lds_bytes<EX>()];
+  const int tid = threadIdx.x;
+  const bool keys = static_cast<int>(blockIdx.x) < call.key_items;
+  int item = static_cast<int>(blockIdx.x) - (keys ? 0 : call.key_items);
+  const int chunks = keys ? call.chunks[0] : call.chunks[1];
+  const int chunk = item % chunks;
+  item /= chunks;
+  const int kvh = item % d.n_kv, lz = item / d.n_kv, seq = lz % d.batch;
+  const long pos = call.read_pos[seq];
+  const int end = min(d.capacity, call.ctx_len ? call.ctx_len[seq] : d.capacity);
+  // codebooks and pair tables
+  {
+    const uint16_t* c16 = reinterpret_cast<const uint16_t*>(blob + kOffC16);
+    uint16_t* cbs = reinterpret_cast<uint16_t*>(smem + kBooks);
+    for (int i = tid; i < kCodebookEntries; i += kThreads) cbs[i] = c16[i];
+    __syncthreads();
+#pragma unroll
+    for (int b = 1; b <= kMaxPair; ++b)
+      if (keys || b == d.v_bits)
+        for (int i = tid; i < (1 << (2 * b)); i += kThreads)
+          *reinterpret_cast<uint32_t*>(smem + pair_offset(b) + 4 * i) =
+              cbs[cb_index(b) + (i & ((1 << b) - 1))] | (static_cast<uint32_t>(cbs[cb_index(b) + (i >> b)]) << 16);
+  }
+  if (keys) read_keys<KWB, EX>(smem, d, blob, call, lz, kvh, chunk, pos, end);
+  else read_values<EX>(smem, d, blob, call, lz, kvh, chunk, pos, end);
 }
 
 }  // namespace
@@ -79,10 +458,35 @@ __global__ __launch_bounds__(kThreads) void k_dequant_rows(Dims d, const uint8_t
 hipError_t launch_dequantize_rows(const Dims& d, const void* layout, const CachePtrs& c, int n_rows,
                                   const int32_t* read_pos, const int32_t* ctx_len, void* k_out, void* v_out,
                                   int out_dtype, hipStream_t s) {
-  hipLaunchKernelGGL(k_dequant_rows, dim3((n_rows + kRowsPerWg - 1) / kRowsPerWg, d.n_kv, d.n_lc * d.batch),
-                     dim3(kThreads), 0, s, d, static_cast<const uint8_t*>(layout), c, n_rows, read_pos, ctx_len, k_out,
-                     v_out, out_dtype);
-  return hipGetLastError();
+  RowsCall call = {};
+  call.c = c;
+  call.read_pos = read_pos;
+  call.ctx_len = ctx_len;
+  call.out[0] = k_out;
+  call.out[1] = v_out;
+  call.n_rows = n_rows;
+  // One workgroup per CU: 256 of them share the units' tiles, a multiple of 8
+  // (a tile per wave) each.
+  const long units = static_cast<long>(d.n_kv) * d.n_lc * d.batch;
+  const long sides = (k_out ? 1 : 0) + (v_out ? 1 : 0);
+  long items = 0;
+  for (int k = 0; k < 2; ++k) {
+    const long n = k == 0 ? (n_rows + 63l) / 64 : (n_rows + 2l * kTile - 2) / kTile;  // (unaligned rows reach one tile more)
+    const long want = std::max(1l, 256 / std::max(1l, units * sides));
+    call.tiles[k] = static_cast<int>(((n + want - 1) / want + kWaves - 1) / kWaves * kWaves);
+    call.chunks[k] = static_cast<int>((n + call.tiles[k] - 1) / call.tiles[k]);
+    if (call.out[k]) items += units * call.chunks[k];
+    if (k == 0) call.key_items = static_cast<int>(items);
+  }
+  const auto go = [&](auto kern) {
+    hipLaunchKernelGGL(kern, dim3(items), dim3(kThreads), 0, s, d, static_cast<const uint8_t*>(layout), call);
+    return hipGetLastError();
+  };
+  const bool ex = out_dtype == 0;  // BGTQ_FP32
+  if (d.k_words <= 8) return ex ? go(k_read_rows<8, true>) : go(k_read_rows<8, false>);
+  if (d.k_words <= 12) return ex ? go(k_read_rows<12, true>) : go(k_read_rows<12, false>);
+  if (d.k_words <= 16) return ex ? go(k_read_rows<16, true>) : go(k_read_rows<16, false>);
+  return ex ? go(k_read_rows<32, true>) : go(k_read_rows<32, false>);
 }
 
 }  // namespace bgtq

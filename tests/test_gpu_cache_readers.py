@@ -229,6 +229,22 @@ def test_dequantize_one_layer_and_allocation(rotations):
     assert bg.blockgtq_dequantize_rows(pk.cfg, pk.layout, 1, pk.cache, i32([0, 0]), 0)[0].numel() == 0
 
 
+@pytest.mark.parametrize("seed", range(6))
+def test_dequantize_fp32_rounding_errors_are_independent(seed):
+    """In the 2-norm.  An fp32 sum of 128 terms of one size: the k-th partial sum is about sqrt(k / 128) of the result,
+    and its rounding at most u of that, uniformly: u sqrt(64 / 3) = 2.8e-7 of the result together.  Operands in two
+    fp16 parts: 2^-22 / sqrt(3) each at most, two of them: 2e-7.  2^-20 = 9.5e-7 is about three times that; one matrix
+    entry of 16384 with a wrong low part (2^-11 of it) is 2^-11 / 128 = 3.8e-6 or more in a dim's column."""
+    rot = synth.rotations(seed)
+    pk = Packed(rot, 60 + seed, batch=1, kv=2, cap=192, k_budget=192, v_bits=3, kind="uniform" if seed % 2 else "mixed")
+    k, v = bg.blockgtq_dequantize_rows(pk.cfg, pk.layout, 0, pk.cache, i32([0]), 192)
+    for name, got, ref in (("k", k, pk.k), ("v", v, pk.v)):
+        off = np.moveaxis(got[0].double().cpu().numpy(), 1, 0) - ref[0, 0]
+        err = np.linalg.norm(off, axis=1) / np.linalg.norm(ref[0, 0], axis=1)  # by head and dim
+        print(f"{name}: {err.max():.3g}", flush=True)
+        assert (err <= 2.0 ** -20).all(), f"{name}: {err.max():.3g} at {np.argwhere(err > 2.0 ** -20)[:5]}"
+
+
 def test_dequantize_not_a_number_stays_in_its_row(rotations):
     pk = Packed(rotations, 8, cap=128, behind=float("nan"), lens=[70])
     k, v = bg.blockgtq_dequantize_rows(pk.cfg, pk.layout, 0, pk.cache, i32([0]), 128, out_dtype=torch.bfloat16)
