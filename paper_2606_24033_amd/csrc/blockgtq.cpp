@@ -878,35 +878,50 @@ int blockgtq_dequantize_rows(const bgtq_config* cfg, const void* d_layout, int32
   return ok();
 }
 
-// Splits of a pass of `units` workgroups per split over max_len rows.  One
-// 8-wave workgroup runs per CU, so units x n workgroups take ceil(units n /
-// 256) rounds, each as long as one split: a 64-row tile per wave and 512 rows,
-// plus set-up and merge worth about three of them.
-static SplitPlan cross_plan(long units, int max_len, int requested) {
-  if (max_len <= 0) return {1, 64};
-  const int tiles = (max_len + 63) / 64;
-  long n = std::min(requested, tiles);
-  if (requested <= 0) {
-    double best = 0.0;
-    n = 1;
-    for (int k = 1; k <= std::min((tiles + 7) / 8, 256); ++k) {
-      const int len = (tiles + k - 1) / k;
-      const double t = static_cast<double>((units * k + 255) / 256) * ((len + 7) / 8 + 3);
-      if (k == 1 || t < best) {
-        best = t;
-        n = k;
+// How one attention pass runs: the query rows of a workgroup (32: k_cross; 128
+// or 256: k_cross_tile on rotated query rows) and the splits of the key axis.
+struct CrossPlan {
+  int rows, n_splits, split_len;
+  long items;
+};
+
+// The plan with the least estimated time over the row counts and splits.  One
+// workgroup runs per CU, so `items` of them take ceil(items / 256) rounds, each
+// as long as one split.  Times in us of a workgroup, measured on long calls:
+//   32 rows (8 waves, a 64-row tile each): 6 per 8 tiles;
+//   128 rows: 2.0 a tile, 256 rows: 2.8 a tile, and a launch more for the
+//   rotation;
+// plus set-up and end, and the joining launch for more than one split.
+static CrossPlan cross_plan(const Dims& d, int n_q, int max_len, int requested, bool joined) {
+  const long units = static_cast<long>(d.n_kv) * d.n_lc * d.batch, nr = static_cast<long>(n_q) * d.group;
+  const int tiles = std::max(1, (max_len + 63) / 64);
+  CrossPlan best = {};
+  double t_best = 0.0;
+  for (const int rows : {32, 128, 256}) {
+    if (rows > 32 && (nr <= rows / 4 || static_cast<long>(d.n_lc) * d.batch > 65535)) continue;
+    const long blocks = units * ((nr + rows - 1) / rows);
+    const int k0 = requested > 0 ? std::min(requested, tiles) : 1;
+    const int k1 = requested > 0 ? k0 : std::min(rows == 32 ? (tiles + 7) / 8 : (tiles + 3) / 4, 256);
+    for (int k = k0; k <= std::max(k0, k1); ++k) {
+      const int len = (tiles + k - 1) / k, n = (tiles + len - 1) / len;
+      const double wg = rows == 32 ? 6.0 * ((len + 7) / 8) + 12.0 : (rows == 128 ? 2.0 : 2.8) * len + 12.0;
+      const double t = static_cast<double>((blocks * n + 255) / 256) * wg + (n > 1 && !joined ? 5.0 : 0.0) + (rows > 32 ? 8.0 : 0.0);
+      if (!best.rows || t < t_best) {
+        t_best = t;
+        best = {rows, n, 64 * len, blocks * n};
       }
     }
   }
-  SplitPlan p;
-  p.split_len = static_cast<int>((tiles + n - 1) / n) * 64;
-  p.n_splits = (max_len + p.split_len - 1) / p.split_len;
-  return p;
+  return best;
 }
 
-// Bytes of the partials: at least one row's, so that a workspace is never empty.
-static size_t cross_ws_bytes(long rows, int n_slots) {
+// Workspace: partials (at least one row's, so that it is never empty), then
+// the rotated query rows.
+static size_t cross_part_bytes(long rows, int n_slots) {
   return al256(static_cast<size_t>(n_slots > 1 ? rows : 1) * n_slots * kPartFloats * 4);
+}
+static size_t cross_ws_bytes(long rows, int n_slots, const CrossPlan& p) {
+  return cross_part_bytes(rows, n_slots) + (p.rows > 32 ? al256(static_cast<size_t>(rows) * kHeadDim * 4) : 0);
 }
 
 static int check_cross_sizes(const bgtq_config* cfg, int32_t n_lc, int32_t n_q, int32_t n_splits, int32_t max_ctx) {
@@ -929,8 +944,8 @@ static Dims cross_dims(const bgtq_config* cfg, int32_t n_lc) {
   return d;
 }
 
-static SplitPlan cross_plan_of(const Dims& d, int32_t n_q, int32_t max_len, int32_t requested) {
-  return cross_plan(cross_items(d, n_q, 1), max_len, requested);
+static CrossPlan cross_attn_plan(const bgtq_config* cfg, int32_t n_lc, int32_t n_q, int32_t max_ctx, int32_t n_splits) {
+  return cross_plan(cross_dims(cfg, n_lc), n_q, max_ctx, n_splits, false);
 }
 
 int blockgtq_cross_workspace_bytes(const bgtq_config* cfg, int32_t n_layers_in_call, int32_t n_q, int32_t n_splits,
@@ -942,8 +957,8 @@ int blockgtq_cross_workspace_bytes(const bgtq_config* cfg, int32_t n_layers_in_c
   if (n_q == 0) return ok();
   const long rows = cross_rows(cfg, n_layers_in_call, n_q);
   if (!rows) return fail(BGTQ_EUNSUPPORTED, "more than 2^24 query rows in one call");
-  const SplitPlan p = cross_plan_of(cross_dims(cfg, n_layers_in_call), n_q, max_ctx, n_splits);
-  *bytes_out = cross_ws_bytes(rows, p.n_splits);
+  const CrossPlan p = cross_attn_plan(cfg, n_layers_in_call, n_q, max_ctx, n_splits);
+  *bytes_out = cross_ws_bytes(rows, p.n_splits, p);
   return ok();
 }
 
@@ -964,17 +979,19 @@ int blockgtq_cross_attn(const bgtq_config* cfg, const void* d_layout, int32_t la
   if (int e = blockgtq_cross_workspace_bytes(cfg, n_lc, n_q, n_splits, max_ctx, &need)) return e;
   if (ws_bytes < need) return fail(BGTQ_EWORKSPACE, "workspace %zu bytes < %zu needed", ws_bytes, need);
   const Dims d = dims_of(cfg, layer, max_ctx);
-  const SplitPlan p = cross_plan_of(cross_dims(cfg, n_lc), n_q, max_ctx, n_splits);
-  const long items = cross_items(d, n_q, p.n_splits);
-  if (items > kMaxItems) return fail(BGTQ_EUNSUPPORTED, "too many splits of too many query rows");
+  const CrossPlan p = cross_attn_plan(cfg, n_lc, n_q, max_ctx, n_splits);
+  if (p.items > kMaxItems) return fail(BGTQ_EUNSUPPORTED, "too many splits of too many query rows");
   CrossCall call = {};
   call.side[0] = {cache_ptrs(cache), d_ctx_len, cfg->batch, cfg->capacity, n_q, p.n_splits, p.split_len, max_ctx, 0,
-                  static_cast<int>(items)};
+                  static_cast<int>(p.items)};
+  const long rows = cross_rows(cfg, n_lc, n_q);
+  call.rows0 = p.rows;
   call.part = static_cast<float*>(d_workspace);
+  call.qr = call.part + cross_part_bytes(rows, p.n_splits) / 4;
   call.n_slots = p.n_splits;
   call.out = d_out;
   call.out_dtype = out_dtype;
-  hipError_t e = launch_cross(d, d_layout, d_q, call, cross_rows(cfg, n_lc, n_q), static_cast<hipStream_t>(stream));
+  hipError_t e = launch_cross(d, d_layout, d_q, call, rows, static_cast<hipStream_t>(stream));
   if (e != hipSuccess) return hip_fail(e, "cross_attn launch");
   return ok();
 }
@@ -990,12 +1007,12 @@ static int check_prefix_cfg(const bgtq_config* cfg, const bgtq_config* p) {
 }
 
 struct SharedPlan {
-  SplitPlan prefix, own;
+  CrossPlan prefix, own;
 };
 static SharedPlan shared_plan(const bgtq_config* cfg, const bgtq_config* pcfg, int32_t n_lc, int32_t n_splits,
                               int32_t max_prefix, int32_t max_ctx) {
-  return {cross_plan_of(cross_dims(pcfg, n_lc), cfg->batch, max_prefix, n_splits),
-          cross_plan_of(cross_dims(cfg, n_lc), 1, max_ctx, 0)};
+  return {cross_plan(cross_dims(pcfg, n_lc), cfg->batch, max_prefix, n_splits, true),
+          cross_plan(cross_dims(cfg, n_lc), 1, max_ctx, 0, true)};  // (at most 8 query rows: 32-row workgroups)
 }
 
 int blockgtq_shared_workspace_bytes(const bgtq_config* cfg, const bgtq_config* prefix_cfg, int32_t n_layers_in_call,
@@ -1007,7 +1024,7 @@ int blockgtq_shared_workspace_bytes(const bgtq_config* cfg, const bgtq_config* p
   const long rows = cross_rows(cfg, n_layers_in_call, 1);
   if (!rows) return fail(BGTQ_EUNSUPPORTED, "more than 2^24 query rows in one call");
   const SharedPlan p = shared_plan(cfg, prefix_cfg, n_layers_in_call, n_splits, max_prefix, max_ctx);
-  *bytes_out = cross_ws_bytes(rows, p.prefix.n_splits + p.own.n_splits);
+  *bytes_out = cross_ws_bytes(rows, p.prefix.n_splits + p.own.n_splits, p.prefix);
   return ok();
 }
 
@@ -1030,20 +1047,21 @@ int blockgtq_decode_attn_shared(const bgtq_config* cfg, const void* d_layout, in
   if (ws_bytes < need) return fail(BGTQ_EWORKSPACE, "workspace %zu bytes < %zu needed", ws_bytes, need);
   const SharedPlan p = shared_plan(cfg, prefix_cfg, n_lc, n_splits, max_prefix, max_ctx);
   const Dims d = dims_of(cfg, layer, max_ctx);
-  const long items0 = cross_items(cross_dims(prefix_cfg, n_lc), cfg->batch, p.prefix.n_splits);
-  const long items1 = cross_items(d, 1, p.own.n_splits);
-  if (items0 + items1 > kMaxItems) return fail(BGTQ_EUNSUPPORTED, "too many splits of too many query rows");
+  if (p.prefix.items + p.own.items > kMaxItems) return fail(BGTQ_EUNSUPPORTED, "too many splits of too many query rows");
   CrossCall call = {};
   // the prefix: every sequence's query is a query row of its one sequence
   call.side[0] = {cache_ptrs(prefix), d_prefix_len, 1, prefix_cfg->capacity, cfg->batch, p.prefix.n_splits,
-                  p.prefix.split_len, max_prefix, 0, static_cast<int>(items0)};
+                  p.prefix.split_len, max_prefix, 0, static_cast<int>(p.prefix.items)};
   call.side[1] = {cache_ptrs(cache), d_ctx_len, cfg->batch, cfg->capacity, 1, p.own.n_splits, p.own.split_len, max_ctx,
-                  p.prefix.n_splits, static_cast<int>(items1)};
+                  p.prefix.n_splits, static_cast<int>(p.own.items)};
+  const long rows = cross_rows(cfg, n_lc, 1);
+  call.rows0 = p.prefix.rows;
   call.part = static_cast<float*>(d_workspace);
   call.n_slots = p.prefix.n_splits + p.own.n_splits;
+  call.qr = call.part + cross_part_bytes(rows, call.n_slots) / 4;
   call.out = d_out;
   call.out_dtype = out_dtype;
-  hipError_t e = launch_cross(d, d_layout, d_q, call, cross_rows(cfg, n_lc, 1), static_cast<hipStream_t>(stream));
+  hipError_t e = launch_cross(d, d_layout, d_q, call, rows, static_cast<hipStream_t>(stream));
   if (e != hipSuccess) return hip_fail(e, "decode_attn_shared launch");
   return ok();
 }

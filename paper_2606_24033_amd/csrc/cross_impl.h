@@ -55,8 +55,14 @@ constexpr int kImg = split_detail::kQimg;                // query image [step][h
 constexpr int kRad = kImg + kMaxSteps * 2048;            // per wave: radii [8 groups, values][64 tokens] fp16
 constexpr int kRadBytes = 9 * 64 * 2;
 constexpr int kBooks = kRad + kWaves * kRadBytes;        // fp16 codebooks
-constexpr int kScale = kBooks + 1024;                    // per query row: 2^-e of its scaled image
-constexpr int kLds = kScale + kRows * 4;
+constexpr int kTop = kBooks + 1024;                      // per query row: largest rotated magnitude, as bits,
+constexpr int kBack = kTop + kRows * 4;                  // and what its staged copy is to be multiplied with
+constexpr int kLds = kBack + kRows * 4;
+// rows staged as fp16 hi and lo parts, [part][row][128 + 8 pad]: the query rows
+// in the image's place before the rotation, the result rows at 0 after the loop
+constexpr int kHalfStride = (kHeadDim + 8) * 2;
+constexpr int kHalfPart = kRows * kHalfStride;
+static_assert(2 * kHalfPart <= kMaxSteps * 2048, "staged queries in the image's place");
 static_assert(kLds <= 160 * 1024, "LDS of one workgroup");
 // at the end: [wave][row] accumulators, then maxima and sums
 constexpr int kAccStride = kHeadDim + 4;
@@ -86,6 +92,103 @@ __device__ __forceinline__ void swap_halves(uint2& x0, uint2& x1, uint2& y0, uin
       "v_permlane32_swap_b32 %3, %7\n\t"
       "s_nop 1"
       : "+v"(x0.x), "+v"(x0.y), "+v"(x1.x), "+v"(x1.y), "+v"(y0.x), "+v"(y0.y), "+v"(y1.x), "+v"(y1.y));
+}
+
+// x = the lower half-wave's value, y = the upper one's, in both.
+__device__ __forceinline__ void spread_halves(uint32_t (&x)[4], uint32_t (&y)[4]) {
+  asm("v_mov_b32 %4, %0\n\tv_mov_b32 %5, %1\n\tv_mov_b32 %6, %2\n\tv_mov_b32 %7, %3\n\t"
+      "s_nop 1\n\t"
+      "v_permlane32_swap_b32 %0, %4\n\t"
+      "v_permlane32_swap_b32 %1, %5\n\t"
+      "v_permlane32_swap_b32 %2, %6\n\t"
+      "v_permlane32_swap_b32 %3, %7\n\t"
+      "s_nop 1"
+      : "+v"(x[0]), "+v"(x[1]), "+v"(x[2]), "+v"(x[3]), "=&v"(y[0]), "=&v"(y[1]), "=&v"(y[2]), "=&v"(y[3]));
+}
+
+// The power of two 2^up that brings a magnitude (as bits, sign cleared) to
+// [2^13, 2^14), and its inverse; 1 for zeros and what is not finite.
+__device__ __forceinline__ int up_of(uint32_t bits) {  // biased
+  const int e = static_cast<int>(bits >> 23);
+  return e == 0 || e == 255 ? 127 : max(1, min(253, 127 + 13 + 127 - e));
+}
+__device__ __forceinline__ float two_to(int biased) { return __uint_as_float(static_cast<uint32_t>(biased) << 23); }
+
+// fp16 parts of 8 floats
+__device__ __forceinline__ void split8(const float (&x)[8], half8_t& hi, half8_t& lo) {
+#pragma unroll
+  for (int j = 0; j < 8; ++j) {
+    hi[j] = static_cast<_Float16>(x[j]);
+    lo[j] = static_cast<_Float16>(x[j] - static_cast<float>(hi[j]));
+  }
+}
+
+// largest magnitude (as bits: infinities and not-a-numbers rank above every
+// number) over the 16 lanes of a row of threads
+__device__ __forceinline__ uint32_t top16(const float (&x)[8]) {
+  uint32_t mx = 0;
+#pragma unroll
+  for (int j = 0; j < 8; ++j) mx = max(mx, __float_as_uint(x[j]) & 0x7FFFFFFFu);
+#pragma unroll
+  for (int k = 1; k < 16; k *= 2) mx = max(mx, static_cast<uint32_t>(__shfl_xor(static_cast<int>(mx), k)));
+  return mx;
+}
+
+// A 16 x 128 block of a matrix (the lane's operands: row lane % 16, columns 32
+// (lane / 16) .. + 31 in m, times 2^8) times 16 NC staged rows, three fp16
+// products: acc[c] = rows 16 c + lane % 16 of the 16 results 4 (lane / 16) ..
+template <int NC>
+__device__ __forceinline__ void staged_product(const uint8_t* staged, const float4_t (&m)[8], int lane, float4_t (&acc)[NC]) {
+  const uint8_t* src = staged + (lane & 15) * kHalfStride + 64 * (lane >> 4);
+#pragma unroll
+  for (int c = 0; c < NC; ++c) acc[c] = float4_t{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+  for (int u = 0; u < 4; ++u) {
+    float x[8];
+#pragma unroll
+    for (int j = 0; j < 8; ++j) x[j] = m[2 * u + (j >> 2)][j & 3] * 256.f;
+    half8_t wh, wl;
+    split8(x, wh, wl);
+    half8_t bh[NC], bl[NC];
+#pragma unroll
+    for (int c = 0; c < NC; ++c) {
+      bh[c] = *reinterpret_cast<const half8_t*>(src + 16 * c * kHalfStride + 16 * u);
+      bl[c] = *reinterpret_cast<const half8_t*>(src + kHalfPart + 16 * c * kHalfStride + 16 * u);
+    }
+#pragma unroll
+    for (int c = 0; c < NC; ++c) acc[c] = __builtin_amdgcn_mfma_f32_16x16x32_f16(wh, bh[c], acc[c], 0, 0, 0);
+#pragma unroll
+    for (int c = 0; c < NC; ++c) acc[c] = __builtin_amdgcn_mfma_f32_16x16x32_f16(wl, bh[c], acc[c], 0, 0, 0);
+#pragma unroll
+    for (int c = 0; c < NC; ++c) acc[c] = __builtin_amdgcn_mfma_f32_16x16x32_f16(wh, bl[c], acc[c], 0, 0, 0);
+  }
+}
+
+// N consecutive words (4-byte aligned) in as few loads as they take.
+template <int N>
+__device__ __forceinline__ void load_words(const uint32_t* base, uint32_t byte_off, uint32_t (&w)[N]) {
+  typedef uint32_t u3_t __attribute__((ext_vector_type(3), aligned(4)));
+  constexpr int F = N / 4 * 4;
+#pragma unroll
+  for (int i = 0; i < F; i += 4) {
+    const uint4 v = ld_at<uint4>(base, byte_off + 4 * i);
+    w[i] = v.x;
+    w[i + 1] = v.y;
+    w[i + 2] = v.z;
+    w[i + 3] = v.w;
+  }
+  if constexpr (N % 4 == 3) {
+    const u3_t v = ld_at<u3_t>(base, byte_off + 4 * F);
+    w[F] = v[0];
+    w[F + 1] = v[1];
+    w[F + 2] = v[2];
+  } else if constexpr (N % 4 == 2) {
+    const uint2 v = ld_at<uint2>(base, byte_off + 4 * F);
+    w[F] = v.x;
+    w[F + 1] = v.y;
+  } else if constexpr (N % 4 == 1) {
+    w[F] = ld_at<uint32_t>(base, byte_off + 4 * F);
+  }
 }
 
 __device__ __forceinline__ half8_t as_half8(const uint2& a, const uint2& b) {
@@ -174,33 +277,45 @@ __device__ __forceinline__ void qk_all(std::integer_sequence<int, BM1...>, const
 // four codes an entry for 1, 2 and 3 bits, two for 4, one above.
 __device__ __forceinline__ void build_tables(uint8_t* smem, const uint16_t* cbs, uint32_t used, int tid) {
   using namespace split_detail;
-  const auto quad = [](const uint16_t* cb, int i, int b) {
+  const auto pair = [](const uint16_t* cb, int i, int b) {
     const int m = (1 << b) - 1;
-    return make_uint2(cb[i & m] | static_cast<uint32_t>(cb[(i >> b) & m]) << 16,
-                      cb[(i >> (2 * b)) & m] | static_cast<uint32_t>(cb[(i >> (3 * b)) & m]) << 16);
+    return cb[i & m] | static_cast<uint32_t>(cb[(i >> b) & m]) << 16;
   };
-  if (used & 1u) {
-    const int i = tid;  // 16 entries x 16 replicas
-    if (i < 256) *reinterpret_cast<uint2*>(smem + kLut1 + i * 8) = quad(cbs + cb_index(1), i >> 4, 1);
-  }
   if (used & 2u) {
-    for (int e = tid >> 4; e < 256; e += cross_detail::kThreads / 16) {  // 16 lanes write an entry's 32 replicas
-      const uint2 v = quad(cbs + cb_index(2), e, 2);
-      *reinterpret_cast<uint4*>(smem + kLut2 + e * 256 + (tid & 15) * 16) = make_uint4(v.x, v.y, v.x, v.y);
-    }
+    // 16 lanes write an entry's 32 replicas; a thread keeps its low code pair
+    const int e0 = tid >> 4;
+    const uint32_t lo = pair(cbs + cb_index(2), e0, 2);
+    uint32_t hi[8];
+#pragma unroll
+    for (int k = 0; k < 8; ++k) hi[k] = pair(cbs + cb_index(2), (e0 + 32 * k) >> 4, 2);
+#pragma unroll
+    for (int k = 0; k < 8; ++k)
+      *reinterpret_cast<uint4*>(smem + kLut2 + (e0 + 32 * k) * 256 + (tid & 15) * 16) = make_uint4(lo, hi[k], lo, hi[k]);
   }
-  if (used & 4u)
-    for (int i = tid; i < 4096; i += cross_detail::kThreads)
-      *reinterpret_cast<uint2*>(smem + kLut1B + i * 8) = quad(cbs + cb_index(3), i, 3);
+  if (used & 4u) {
+    const uint32_t lo = pair(cbs + cb_index(3), tid & 63, 3);
+    uint32_t hi[8];
+#pragma unroll
+    for (int k = 0; k < 8; ++k) hi[k] = pair(cbs + cb_index(3), (tid >> 6) + 8 * k, 3);
+#pragma unroll
+    for (int k = 0; k < 8; ++k) *reinterpret_cast<uint2*>(smem + kLut1B + (tid + 512 * k) * 8) = make_uint2(lo, hi[k]);
+  }
+  if (used & 1u)
+    if (tid < 256)  // 16 entries x 16 replicas
+      *reinterpret_cast<uint2*>(smem + kLut1 + tid * 8) =
+          make_uint2(pair(cbs + cb_index(1), tid >> 4, 1), pair(cbs + cb_index(1), tid >> 6, 1));
   if (used & 8u)
-    for (int i = tid; i < 256 * 8; i += cross_detail::kThreads) {
-      const int e = i >> 3;
-      *reinterpret_cast<uint32_t*>(smem + kLut4 + i * 4) =
-          cbs[cb_index(4) + (e & 15)] | static_cast<uint32_t>(cbs[cb_index(4) + (e >> 4)]) << 16;
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+      const int i = tid + 512 * k;
+      *reinterpret_cast<uint32_t*>(smem + kLut4 + i * 4) = pair(cbs + cb_index(4), i >> 3, 4);
     }
   if (used & 16u)
-    for (int i = tid; i < 32 * 32; i += cross_detail::kThreads)
+#pragma unroll
+    for (int k = 0; k < 2; ++k) {
+      const int i = tid + 512 * k;
       *reinterpret_cast<uint32_t*>(smem + kLut5 + i * 4) = cbs[cb_index(5) + (i >> 5)];
+    }
   if (used & 0xE0u) {
     const int i = tid;
     if (i < 256 + 128 + 64) {
@@ -243,139 +358,13 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(2, 2))
   const int t_begin = split * S.split_len;
   const int t_end = ok ? min(len, t_begin + S.split_len) : t_begin;
 
-  // ---- set-up: codebooks; the query rows rotated into stream order,
-  //   q'[p] = log2 e / sqrt(d_g d_h) sum_d W[p][d] q[d],
-  // on fp32 MFMAs (wave = 16 positions, two blocks of 16 rows); every global
-  // read is issued before the first wait.
-  uint32_t gm[8], used = 1u << (BV - 1);
-#pragma unroll
-  for (int b = 0; b < 8; ++b) {
-    gm[b] = M->gm[b];
-    used |= (gm[b] >> 31) << b;
-  }
-  float* qs = reinterpret_cast<float*>(smem);  // [32 rows][kAccStride] rotated queries, before the tables
-  uint16_t* cbs = reinterpret_cast<uint16_t*>(smem + kBooks);
-  {
-    const uint16_t* c16 = reinterpret_cast<const uint16_t*>(blob + kOffC16);
-    const float4_t* w = reinterpret_cast<const float4_t*>(blob + layout_kdense_offset(d.n_layers * d.n_kv)) +
-                        static_cast<size_t>(ri) * (kMfmaMatFloats / 4) + wave * 8 * 64 + lane;
-    float4_t a[8];
-#pragma unroll
-    for (int s4 = 0; s4 < 8; ++s4) a[s4] = w[s4 * 64];
-    const uint16_t cv = c16[min(tid, kCodebookEntries - 1)];
-    const int p0 = 16 * wave + 4 * (lane >> 4);  // the lane's positions of the product
-    float scale[4];
-#pragma unroll
-    for (int i = 0; i < 4; ++i)
-      scale[i] = kLog2e * kRsqrtD * rsqrtf(static_cast<float>(M->g_dim[M->grp[p0 + i]]));
-    if (tid < kCodebookEntries) cbs[tid] = cv;
-#pragma unroll
-    for (int c = 0; c < 2; ++c) {
-      const int r = r0 + 16 * c + (lane & 15);
-      const size_t at = row_at(min(r, nr - 1)) * kHeadDim + 32 * (lane >> 4);
-      float b[32];
-      if (d.in_dtype == 1) {
-        const uint4* src = reinterpret_cast<const uint4*>(static_cast<const uint16_t*>(q) + at);
-#pragma unroll
-        for (int u = 0; u < 4; ++u) {
-          const uint4 v = src[u];
-          const uint32_t x[4] = {v.x, v.y, v.z, v.w};
-#pragma unroll
-          for (int e = 0; e < 4; ++e) {
-            b[8 * u + 2 * e] = __uint_as_float(x[e] << 16);
-            b[8 * u + 2 * e + 1] = __uint_as_float(x[e] & 0xFFFF0000u);
-          }
-        }
-      } else {
-        const float4_t* src = reinterpret_cast<const float4_t*>(static_cast<const float*>(q) + at);
-#pragma unroll
-        for (int u = 0; u < 8; ++u) {
-          const float4_t v = src[u];
-#pragma unroll
-          for (int e = 0; e < 4; ++e) b[4 * u + e] = v[e];
-        }
-      }
-      float4_t acc = {0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-      for (int s = 0; s < 32; ++s) acc = __builtin_amdgcn_mfma_f32_16x16x4f32(a[s >> 2][s & 3], b[s], acc, 0, 0, 0);
-#pragma unroll
-      for (int i = 0; i < 4; ++i) acc[i] *= scale[i];
-      *reinterpret_cast<float4_t*>(qs + (16 * c + (lane & 15)) * kAccStride + p0) = acc;
-    }
-  }
-  __syncthreads();
-  // The image of a row is scaled by the power of two that brings its largest
-  // coordinate to [2^13, 2^14): the lo parts stay above fp16's subnormals.
-  // (thread = (row, step and half); 16 threads a row)
-  {
-    const int r = tid >> 4, sub = tid & 15;
-    const float* src = qs + r * kAccStride;
-    float mx = 0.f;
-#pragma unroll
-    for (int i = 0; i < 8; ++i) mx = fmaxf(mx, fabsf(src[sub * 8 + i]));
-#pragma unroll
-    for (int k = 1; k < 16; k *= 2) mx = fmaxf(mx, __shfl_xor(mx, k));
-    const int e = static_cast<int>(__float_as_uint(mx) >> 23);  // biased
-    const bool plain = e == 0 || e == 255;                      // zeros; not finite
-    const int up = plain ? 127 : max(1, min(253, 127 + 13 + 127 - e));
-    const float to = __uint_as_float(static_cast<uint32_t>(up) << 23);
-    if (sub == 0) *reinterpret_cast<float*>(smem + kScale + 4 * r) = __uint_as_float(static_cast<uint32_t>(254 - up) << 23);
-    // steps numbered group after group; item = (step, half)
-    for (int it = sub; it < 2 * kMaxSteps; it += 16) {
-      int st = it >> 1, p = -1, left = 0;
-#pragma unroll
-      for (int b = 0; b < 8; ++b) {
-        const int n16 = gm[b] >> 31 ? (split_detail::gm_steps(gm[b]) + 3) >> 2 : 0;
-        if (p < 0 && st >= 0 && st < n16) {
-          const int g = split_detail::gm_plane(gm[b]);
-          p = M->g_pos[g] + 16 * st + 8 * (it & 1);
-          left = M->g_dim[g] - 16 * st - 8 * (it & 1);
-        }
-        st -= n16;
-      }
-      if (p < 0) continue;
-      half8_t hi, lo;
-#pragma unroll
-      for (int j = 0; j < 8; ++j) {
-        const float x = j < left ? src[p + j] * to : 0.f;
-        hi[j] = static_cast<_Float16>(x);
-        lo[j] = static_cast<_Float16>(x - static_cast<float>(hi[j]));
-      }
-      uint8_t* dst = smem + kImg + (it >> 1) * 2048 + ((it & 1) * 32 + r) * 16;
-      *reinterpret_cast<half8_t*>(dst) = hi;
-      *reinterpret_cast<half8_t*>(dst + 1024) = lo;
-    }
-  }
-  __syncthreads();
-  build_tables(smem, cbs, used, tid);
-  __syncthreads();
-
-  LaneRep rep{static_cast<uint32_t>(split_detail::kLut1 + (lane & 15) * 8),
-              static_cast<uint32_t>(split_detail::kLut3 + (lane & 31) * 4),
-              static_cast<uint32_t>(split_detail::kLut4 + (lane & 7) * 4),
-              static_cast<uint32_t>(split_detail::kLut5 + (lane & 31) * 4),
-              static_cast<uint32_t>(split_detail::kLut2 + (lane & 31) * 8),
-              static_cast<uint32_t>(split_detail::kLut1B), 0u};
-  asm volatile("" : "+v"(rep.r1), "+v"(rep.r3), "+v"(rep.r4), "+v"(rep.r5), "+v"(rep.r2), "+v"(rep.r1b));
-  const float sc = *reinterpret_cast<const float*>(smem + kScale + 4 * l32);
-  uint8_t* const rad = smem + kRad + wave * kRadBytes;
-  const uint8_t* const rad_l = rad + 8 * hf;  // the lane's tokens start at 4 hf
-
   const size_t row = (static_cast<size_t>(layer) * S.batch + seq) * d.n_kv + kvh;
   const size_t cap = S.capacity;
   const uint32_t* kc = S.c.k_codes + row * cap * kw;
   const uint16_t* kn = S.c.k_norms + row * kMaxGroups * cap;
   const uint32_t* vc = S.c.v_codes + row * (cap / kTile) * kHeadDim * BV;
   const uint16_t* vn = S.c.v_norms + row * cap;
-
-  float m_run = kNegInf, l_run = 0.f;
-  float16_t o[4];
-#pragma unroll
-  for (int cc = 0; cc < 4; ++cc)
-#pragma unroll
-    for (int i = 0; i < 16; ++i) o[cc][i] = 0.f;
-
-  uint32_t nw[KWB], knp[4], vnw, vw[2][4][BV];
+  uint32_t nw[KWB], knp[4], vnw, vw[4][BV];  // (a half-wave loads the values of its own 32-row tile)
   const auto load_keys = [&](int t0) {
     const uint32_t* src = kc + static_cast<size_t>(t0) * kw;
     const uint32_t at = static_cast<uint32_t>(lane * kw * 4);
@@ -403,20 +392,158 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(2, 2))
   const auto load_values = [&](int t0) {
     const uint32_t* src = vc + static_cast<size_t>(t0 / kTile) * kHeadDim * BV;
 #pragma unroll
-    for (int n = 0; n < 2; ++n)
-#pragma unroll
-      for (int cc = 0; cc < 4; ++cc)
-#pragma unroll
-        for (int i = 0; i < BV; ++i)
-          vw[n][cc][i] = ld_at<uint32_t>(src + (n * kHeadDim + 32 * cc) * BV, static_cast<uint32_t>((l32 * BV + i) * 4));
+    for (int cc = 0; cc < 4; ++cc)
+      load_words(src + 32 * cc * BV, static_cast<uint32_t>((hf * kHeadDim + l32) * BV * 4), vw[cc]);
   };
-
   int t0 = t_begin + wave * kKeyTile;
   constexpr int kStride = kWaves * kKeyTile;
-  if (t0 < t_end) {
-    load_keys(t0);
-    load_values(t0);
+
+  // ---- set-up: the query rows rotated into stream order,
+  //   q'[p] = log2 e / sqrt(d_g d_h) sum_d W[p][d] q[d],
+  // in three fp16 products (wave = 16 positions), and written into the image,
+  // before and after scaled by the power of two that brings the row's largest
+  // coordinate to [2^13, 2^14): the lo parts stay above fp16's subnormals.
+  // Every global read of the set-up and the first tile's are issued at once
+  // (few and wide ones: the 8 waves' loads pass one by one).
+  uint32_t gm[8], used = 1u << (BV - 1);
+  int gd[8], gp[8];
+#pragma unroll
+  for (int b = 0; b < 8; ++b) {
+    gm[b] = M->gm[b];
+    used |= (gm[b] >> 31) << b;
+    gd[b] = b < ng ? M->g_dim[b] : 0;
+    gp[b] = M->g_pos[b];
   }
+  const int p0 = 16 * wave + 4 * (lane >> 4);  // the lane's 4 positions of the rotation
+  float4_t rq[2];                              // rows 16 c + lane % 16
+  {
+    const uint16_t* c16 = reinterpret_cast<const uint16_t*>(blob + kOffC16);
+    const float4_t* w = reinterpret_cast<const float4_t*>(blob + layout_kdense_offset(d.n_layers * d.n_kv)) +
+                        static_cast<size_t>(ri) * (kMfmaMatFloats / 4) + wave * 8 * 64 + lane;
+    const uint16_t cv = c16[min(tid, kCodebookEntries - 1)];
+    // thread = (row tid / 16, dims 8 (tid % 16) .. + 7)
+    const size_t at = row_at(min(r0 + (tid >> 4), nr - 1)) * kHeadDim + 8 * (tid & 15);
+    const bool bf = d.in_dtype == 1;
+    const uint4* qp = reinterpret_cast<const uint4*>(static_cast<const uint8_t*>(q) + at * (bf ? 2 : 4));
+    const uint4 x0 = qp[0], x1 = bf ? make_uint4(0, 0, 0, 0) : qp[1];
+    float4_t a[8];
+#pragma unroll
+    for (int s4 = 0; s4 < 8; ++s4) a[s4] = w[s4 * 64];
+    if (t0 < t_end) {
+      load_keys(t0);
+      load_values(t0);
+    }
+    uint16_t* cbs = reinterpret_cast<uint16_t*>(smem + kBooks);
+    if (tid < kCodebookEntries) cbs[tid] = cv;
+    if (tid < kRows) reinterpret_cast<uint32_t*>(smem + kTop)[tid] = 0;
+    {
+      const uint32_t y0[4] = {x0.x, x0.y, x0.z, x0.w}, y1[4] = {x1.x, x1.y, x1.z, x1.w};
+      float x[8];
+#pragma unroll
+      for (int e = 0; e < 8; ++e) {
+        const uint32_t half = e & 1 ? y0[e >> 1] & 0xFFFF0000u : y0[e >> 1] << 16;
+        x[e] = __uint_as_float(bf ? half : (e < 4 ? y0[e & 3] : y1[e & 3]));
+      }
+      const int up = up_of(top16(x));
+#pragma unroll
+      for (int e = 0; e < 8; ++e) x[e] *= two_to(up);
+      half8_t hi, lo;
+      split8(x, hi, lo);
+      uint8_t* dst = smem + kImg + (tid >> 4) * kHalfStride + 16 * (tid & 15);
+      *reinterpret_cast<half8_t*>(dst) = hi;
+      *reinterpret_cast<half8_t*>(dst + kHalfPart) = lo;
+      if ((tid & 15) == 0) reinterpret_cast<float*>(smem + kBack)[tid >> 4] = two_to(254 - up) * (1.f / 256.f);
+    }
+    __syncthreads();
+    build_tables(smem, cbs, used, tid);
+    staged_product<2>(smem + kImg, a, lane, rq);
+  }
+  // place of the lane's position pairs in the image (group sizes are even)
+  uint32_t img_at[2];
+#pragma unroll
+  for (int h = 0; h < 2; ++h) {
+    int st = 0, at = 0, dg = 2, base = 0;
+#pragma unroll
+    for (int g = 0; g < 8; ++g) {
+      if (g < ng && p0 + 2 * h >= gp[g]) {
+        at = p0 + 2 * h - gp[g];
+        dg = gd[g];
+        st = base;
+      }
+      base += (gd[g] + 15) >> 4;
+    }
+    img_at[h] = kImg + (st + (at >> 4)) * 2048 + ((at >> 3) & 1) * 512 + (at & 7) * 2;
+    const float scale = kLog2e * kRsqrtD * rsqrtf(static_cast<float>(dg));
+#pragma unroll
+    for (int c = 0; c < 2; ++c) {
+      rq[c][2 * h] *= scale;
+      rq[c][2 * h + 1] *= scale;
+    }
+  }
+  uint32_t* const top = reinterpret_cast<uint32_t*>(smem + kTop);
+#pragma unroll
+  for (int c = 0; c < 2; ++c) {
+    uint32_t mx = 0;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) mx = max(mx, __float_as_uint(rq[c][i]) & 0x7FFFFFFFu);
+    mx = max(mx, static_cast<uint32_t>(__shfl_xor(static_cast<int>(mx), 16)));
+    mx = max(mx, static_cast<uint32_t>(__shfl_xor(static_cast<int>(mx), 32)));
+    if (lane < 16) atomicMax(top + 16 * c + lane, mx);
+  }
+  __syncthreads();
+  // (the image takes the staged queries' place)
+#pragma unroll
+  for (int c = 0; c < 2; ++c) {
+    const int r = 16 * c + (lane & 15);
+    const float to = two_to(up_of(top[r]));
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+      half2_t hi, lo;
+#pragma unroll
+      for (int j = 0; j < 2; ++j) {
+        const float x = rq[c][2 * h + j] * to;
+        hi[j] = static_cast<_Float16>(x);
+        lo[j] = static_cast<_Float16>(x - static_cast<float>(hi[j]));
+      }
+      *reinterpret_cast<half2_t*>(smem + img_at[h] + r * 16) = hi;
+      *reinterpret_cast<half2_t*>(smem + img_at[h] + r * 16 + 1024) = lo;
+    }
+  }
+  // zeros behind the groups' ends: thread = (position pair tid / 32 from the end, row)
+  if (tid < 7 * 32) {
+    int base = 0;
+#pragma unroll
+    for (int g = 0; g < 8; ++g) {
+      const int at = gd[g] + 2 * (tid >> 5), n16 = (gd[g] + 15) >> 4;
+      if (at < 16 * n16) {
+        uint8_t* dst = smem + kImg + (base + (at >> 4)) * 2048 + ((at >> 3) & 1) * 512 + (at & 7) * 2 + (tid & 31) * 16;
+        *reinterpret_cast<uint32_t*>(dst) = 0;
+        *reinterpret_cast<uint32_t*>(dst + 1024) = 0;
+      }
+      base += n16;
+    }
+  }
+  __syncthreads();
+
+  LaneRep rep{static_cast<uint32_t>(split_detail::kLut1 + (lane & 15) * 8),
+              static_cast<uint32_t>(split_detail::kLut3 + (lane & 31) * 4),
+              static_cast<uint32_t>(split_detail::kLut4 + (lane & 7) * 4),
+              static_cast<uint32_t>(split_detail::kLut5 + (lane & 31) * 4),
+              static_cast<uint32_t>(split_detail::kLut2 + (lane & 31) * 8),
+              static_cast<uint32_t>(split_detail::kLut1B), 0u};
+  asm volatile("" : "+v"(rep.r1), "+v"(rep.r3), "+v"(rep.r4), "+v"(rep.r5), "+v"(rep.r2), "+v"(rep.r1b));
+  // the row's scales, undone on its logits
+  const float sc = two_to(254 - up_of(top[l32])) * reinterpret_cast<const float*>(smem + kBack)[l32];
+  uint8_t* const rad = smem + kRad + wave * kRadBytes;
+  const uint8_t* const rad_l = rad + 8 * hf;  // the lane's tokens start at 4 hf
+
+  float m_run = kNegInf, l_run = 0.f;
+  float16_t o[4];
+#pragma unroll
+  for (int cc = 0; cc < 4; ++cc)
+#pragma unroll
+    for (int i = 0; i < 16; ++i) o[cc][i] = 0.f;
+
   for (; t0 < t_end; t0 += kStride) {
     const bool full = t0 + kKeyTile <= t_end;
     __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");  // the last tile's reads of the radii come first
@@ -482,6 +609,18 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(2, 2))
       for (int cc = 0; cc < 4; ++cc) o[cc] *= corr;
     }
     const float mref = m_run == kNegInf ? 0.f : m_run;
+    // the values of both 32-row tiles into both half-waves
+    uint32_t v1[4 * BV];
+#pragma unroll
+    for (int i = 0; i < BV; ++i) {
+      uint32_t x[4] = {vw[0][i], vw[1][i], vw[2][i], vw[3][i]}, y[4];
+      spread_halves(x, y);
+#pragma unroll
+      for (int cc = 0; cc < 4; ++cc) {
+        vw[cc][i] = x[cc];
+        v1[cc * BV + i] = y[cc];
+      }
+    }
 #pragma unroll
     for (int n = 0; n < 2; ++n) {
       uint32_t pw[8], pl[EX ? 8 : 1];
@@ -513,9 +652,9 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(2, 2))
         uint32_t w[BV + 1];
 #pragma unroll
         for (int i = 0; i < BV; ++i) {
-          const uint32_t up = i + 1 < BV ? vw[n][cc][i + 1] : 0u;
-          if constexpr (BV == 8) w[i] = hf ? up : vw[n][cc][i];
-          else w[i] = __builtin_amdgcn_alignbit(up, vw[n][cc][i], 4 * BV * hf);
+          const uint32_t up = i + 1 < BV ? (n ? v1[cc * BV + i + 1] : vw[cc][i + 1]) : 0u;
+          if constexpr (BV == 8) w[i] = hf ? up : (n ? v1[cc * BV + i] : vw[cc][i]);
+          else w[i] = __builtin_amdgcn_alignbit(up, (n ? v1[cc * BV + i] : vw[cc][i]), 4 * BV * hf);
         }
         w[BV] = 0;
         const half4_t v0 = decode4<BV, 0, true>(smem, w, rep), v1 = decode4<BV, 8 * BV, true>(smem, w, rep);
@@ -554,6 +693,7 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(2, 2))
   float* const acc = reinterpret_cast<float*>(smem);
   float* const ms = reinterpret_cast<float*>(smem + kEndM);
   float* const ls = ms + kWaves * kRows;
+  const int n_act = min(kWaves, (t_end - t_begin + kKeyTile - 1) / kKeyTile);  // waves that had a tile
 #pragma unroll
   for (int cc = 0; cc < 4; ++cc)
 #pragma unroll
@@ -565,7 +705,7 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(2, 2))
     ls[wave * kRows + l32] = l_run;
   }
   __syncthreads();
-  const int r = tid >> 4, d0 = (tid & 15) * 4;  // dims d0 .. + 3 and 64 + d0 .. + 3 of row r
+  const int r = tid >> 4, d0 = (tid & 15) * 8;  // dims d0 .. + 7 of row r
   float m = kNegInf, l = 0.f;
   float4_t a[2] = {{0.f, 0.f, 0.f, 0.f}, {0.f, 0.f, 0.f, 0.f}};
 #pragma unroll
@@ -573,11 +713,12 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(2, 2))
   const float mref = m == kNegInf ? 0.f : m;
 #pragma unroll
   for (int w = 0; w < kWaves; ++w) {
+    if (w >= n_act) break;
     const float e = __builtin_amdgcn_exp2f(ms[w * kRows + r] - mref);
     l = fmaf(ls[w * kRows + r], e, l);
 #pragma unroll
     for (int h = 0; h < 2; ++h) {
-      const float4_t x = *reinterpret_cast<const float4_t*>(acc + (w * kRows + r) * kAccStride + 64 * h + d0);
+      const float4_t x = *reinterpret_cast<const float4_t*>(acc + (w * kRows + r) * kAccStride + 4 * h + d0);
 #pragma unroll
       for (int i = 0; i < 4; ++i) a[h][i] = fmaf(x[i], e, a[h][i]);
     }
@@ -593,31 +734,37 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(2, 2))
         P[1] = l;
       }
       *reinterpret_cast<float4_t*>(P + 4 + d0) = a[0];
-      *reinterpret_cast<float4_t*>(P + 68 + d0) = a[1];
+      *reinterpret_cast<float4_t*>(P + 8 + d0) = a[1];
     }
     return;
   }
-  // ---- the only partial: out = Pi_V^T (a / l) on fp32 MFMAs
+  // ---- the only partial: out = Pi_V^T (a / l), in three fp16 products of the
+  // rows scaled as the queries were
   __syncthreads();
-  const float inv = l == 0.f ? 0.f : kRsqrtD / l;
-  *reinterpret_cast<float4_t*>(acc + r * kAccStride + d0) = a[0] * inv;
-  *reinterpret_cast<float4_t*>(acc + r * kAccStride + 64 + d0) = a[1] * inv;
+  {
+    const float inv = l == 0.f ? 0.f : kRsqrtD / l;
+    float x[8];
+#pragma unroll
+    for (int e = 0; e < 8; ++e) x[e] = a[e >> 2][e & 3] * inv;
+    const int up = up_of(top16(x));
+#pragma unroll
+    for (int e = 0; e < 8; ++e) x[e] *= two_to(up);
+    half8_t hi, lo;
+    split8(x, hi, lo);
+    uint8_t* dst = smem + r * kHalfStride + 16 * (tid & 15);
+    *reinterpret_cast<half8_t*>(dst) = hi;
+    *reinterpret_cast<half8_t*>(dst + kHalfPart) = lo;
+    if ((tid & 15) == 0) reinterpret_cast<float*>(smem + 2 * kHalfPart)[r] = two_to(254 - up) * (1.f / 256.f);
+  }
   __syncthreads();
+  float4_t y[2];
+  staged_product<2>(smem, rot, lane, y);
 #pragma unroll
   for (int c = 0; c < 2; ++c) {
-    const int rr = 16 * c + (lane & 15);
-    const float4_t* src = reinterpret_cast<const float4_t*>(acc + rr * kAccStride + 32 * (lane >> 4));
-    float4_t y = {0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-    for (int s4 = 0; s4 < 8; ++s4) {
-      const float4_t b = src[s4];
-#pragma unroll
-      for (int e = 0; e < 4; ++e) y = __builtin_amdgcn_mfma_f32_16x16x4f32(rot[s4][e], b[e], y, 0, 0, 0);
-    }
-    if (r0 + rr < nr) {
-      const size_t at = row_at(r0 + rr) * kHeadDim + 16 * wave + 4 * (lane >> 4);
-      store4(call.out, at, y, call.out_dtype);
-    }
+    const int rl = 16 * c + (lane & 15);
+    if (r0 + rl < nr)
+      store4(call.out, row_at(r0 + rl) * kHeadDim + 16 * wave + 4 * (lane >> 4),
+             y[c] * reinterpret_cast<const float*>(smem + 2 * kHalfPart)[rl], call.out_dtype);
   }
 }
 

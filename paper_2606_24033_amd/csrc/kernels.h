@@ -93,6 +93,10 @@ hipError_t launch_decode_fp16(const Dims& d, const void* q, const int32_t* ctx_l
                               const void* k16, const void* v16, float* out,
                               const DecodeWs& ws, hipStream_t s);
 
+// Q-side rotation of every query row ([n_lc][batch][n_q][Hq]) into stream
+// order, log2 e / sqrt(d_g d_h) folded in, fp32 (prefill.hip).
+hipError_t launch_query_rotation(const Dims& d, const void* layout, const void* q, int n_q, float* qr, hipStream_t s);
+
 // Causal prefill attention over the packed cache of one layer (prefill.hip):
 // the query rotation into qr_ws, then the attention into out.
 hipError_t launch_prefill_attn(const Dims& d, const void* layout, const void* q, int n_q,
@@ -122,12 +126,13 @@ struct CrossSide {
 };
 struct CrossCall {
   CrossSide side[2];  // the second one has no items in a call of one pass
+  int rows0;          // query rows of a workgroup of side[0]: 32 (k_cross), 128 or 256 (k_cross_tile)
+  float* qr;          // the rotated query rows of side[0], for k_cross_tile
   float* part;
   int n_slots;
   void* out;
   int out_dtype;
 };
-long cross_items(const Dims& d, int n_q, int n_splits);  // workgroups of a pass
 hipError_t launch_cross(const Dims& d, const void* layout, const void* q, const CrossCall& call, long rows,
                         hipStream_t s);
 // k_cross (cross_impl.h), one entry per value code width (cross_bv1.hip .. cross_bv8.hip).
@@ -142,6 +147,11 @@ BGTQ_DECL_CROSS(6)
 BGTQ_DECL_CROSS(7)
 BGTQ_DECL_CROSS(8)
 #undef BGTQ_DECL_CROSS
+// k_cross_tile (cross_tile.h), one entry per output type; half: 128-row workgroups.
+hipError_t launch_cross_tile_bf16(const Dims& d, const void* layout, const float* qr, const CrossCall& call, bool half,
+                                  hipStream_t s);
+hipError_t launch_cross_tile_fp32(const Dims& d, const void* layout, const float* qr, const CrossCall& call, bool half,
+                                  hipStream_t s);
 
 // Streaming read of `bytes` (a multiple of 16, 16-byte aligned) at src;
 // writes sink[0] only in a case no real input reaches (probe.hip).

@@ -24,78 +24,16 @@
 //     tile.  Its epilogue: out = Pi_V^T o, with fp32 MFMAs.
 #include <hip/hip_runtime.h>
 
+#include "attn_tile.h"
 #include "kernels.h"
 #include "layout.h"
-#include "mix.h"
 #include "split.h"
 
 namespace bgtq {
 namespace prefill_detail {
 
-typedef _Float16 half8_t __attribute__((ext_vector_type(8)));
-typedef float float4_t __attribute__((ext_vector_type(4)));
-
-typedef float float16_t __attribute__((ext_vector_type(16)));
-typedef _Float16 half2_t __attribute__((ext_vector_type(2)));
-
 constexpr int kThreads = 256;      // rotation kernel: 4 waves
-constexpr int kAttnWaves = 8;      // attention kernel: 8 waves (2 per SIMD)
-constexpr int kAttnThreads = kAttnWaves * 64;
-constexpr int kWaveRows = 32;      // query rows (position x head) of a wave: one 32x32 column block
 constexpr int kQrotRows = 512;     // query rows (position x head) per rotation workgroup
-constexpr float kLog2e = 1.4426950408889634f;
-constexpr float kNegInf = -__builtin_huge_valf();
-// ---- LDS map of the attention kernel (bytes)
-constexpr int kKStride = 136;  // halves per decoded key row (128 + 8 pad)
-constexpr int kVStride = 72;   // halves per decoded value row (64 + 8 pad: 16-byte aligned, conflict-free reads)
-// decoded tile (two buffers): keys hi, lo [64 tokens][kKStride] fp16, values
-// [128 dims][kVStride] fp16, value radii [64] fp16
-constexpr int kDecKH = 0;
-constexpr int kDecKL = kDecKH + 64 * kKStride * 2;
-constexpr int kDecV = kDecKL + 64 * kKStride * 2;
-constexpr int kDecVN = kDecV + 128 * kVStride * 2;
-constexpr int kDecBytes = kDecVN + 64 * 2;
-constexpr int kOffCb = 0;                        // fp16 codebooks
-constexpr int kOffPair = kOffCb + 1024;          // pair tables of the widths 1 .. kMaxPair
-constexpr int kMaxPair = 6;
-// byte offset of the pair table of width b: 4^b entries of two fp16 centroids
-__host__ __device__ constexpr int pair_offset(int b) { return 4 * (((1 << (2 * b)) - 4) / 3); }
-// (the tables lie below 64 KB: their offsets fit the immediate of an LDS read)
-constexpr int kOffDec = (kOffPair + pair_offset(kMaxPair + 1) + 15) / 16 * 16;
-constexpr int kTileLds = kOffDec + 2 * kDecBytes;
-constexpr int kRotVLds = kHeadDim * kHeadDim * 4;  // Pi_V staged for the epilogue
-constexpr int kMergeLds = (kAttnWaves / 2) * 64 * 66 * 4;  // states of the waves that hand theirs over (KS = 2)
-constexpr int kLdsBytes = kTileLds > kRotVLds ? (kTileLds > kMergeLds ? kTileLds : kMergeLds)
-                                              : (kRotVLds > kMergeLds ? kRotVLds : kMergeLds);
-static_assert(kLdsBytes <= 160 * 1024, "LDS of one workgroup");
-static_assert(kDecBytes % 16 == 0 && kDecV % 16 == 0 && kOffDec % 16 == 0, "aligned buffers");
-static_assert(2 * kCodebookEntries <= 1024, "codebook staging");
-
-// Load of a T at a 32-bit byte offset from a wave-uniform base (the global
-// load form with a scalar base and a 32-bit vector offset).
-template <class T>
-__device__ __forceinline__ T ld_at(const void* base, uint32_t byte_off) {
-  return *reinterpret_cast<const T*>(static_cast<const char*>(base) + byte_off);
-}
-
-// r0, r1 = the values of lanes l % 32 and l % 32 + 32 (the two lanes that hold
-// the same query row of an accumulator); gfx950 lane swap
-__device__ __forceinline__ void swap32(float v, float& r0, float& r1) {
-  unsigned x = __builtin_bit_cast(unsigned, v), y = x;
-  asm volatile("s_nop 1\n\tv_permlane32_swap_b32 %0, %1\n\ts_nop 1" : "+v"(x), "+v"(y));
-  r0 = __builtin_bit_cast(float, x);
-  r1 = __builtin_bit_cast(float, y);
-}
-__device__ __forceinline__ float max2g(float v) {
-  float a, b;
-  swap32(v, a, b);
-  return fmaxf(a, b);
-}
-__device__ __forceinline__ float sum2g(float v) {
-  float a, b;
-  swap32(v, a, b);
-  return a + b;
-}
 
 __device__ __forceinline__ float ld_q(const void* q, size_t i, int in_dtype) {  // BGTQ_BF16 = 1
   if (in_dtype == 1) {
@@ -106,8 +44,8 @@ __device__ __forceinline__ float ld_q(const void* q, size_t i, int in_dtype) {  
 }
 
 // ---------------------------------------------------------------- 1. rotation
-// grid (ceil(n_q G / kQrotRows), n_kv, batch).  qr: [batch][n_q][Hq][128]
-// fp32.  The rotation of a query row is one product with a 128 x 128 matrix
+// grid (ceil(n_q G / kQrotRows), n_kv, layers in call x batch).  qr:
+// [layers in call][batch][n_q][Hq][128] fp32.  The rotation of a query row is one product with a 128 x 128 matrix
 // in stream order, W[p][k] = log2 e / sqrt(d_g d_h) Pi_g[j][k - g_pos] for
 // p = g_pos + j and k in the same group g (zero elsewhere), applied to the
 // row gathered into stream order.  W is staged in LDS once per workgroup
@@ -120,11 +58,12 @@ __global__ __launch_bounds__(kThreads) void k_prefill_qrot(Dims d, const uint8_t
   __shared__ float qs[kThreads / 64][16][kHeadDim + 4];      // per wave: 16 rows in stream order
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
   const int kvh = blockIdx.y, seq = blockIdx.z;
+  const int layer = d.layer >= 0 ? d.layer : seq / d.batch;
   const int G = d.group, hq = d.n_kv * G;
   const int n_rows_blob = d.n_layers * d.n_kv;
-  const RowMeta* M = reinterpret_cast<const RowMeta*>(blob + kOffRows) + (d.layer * d.n_kv + kvh);
+  const RowMeta* M = reinterpret_cast<const RowMeta*>(blob + kOffRows) + (layer * d.n_kv + kvh);
   const float* rowrot = reinterpret_cast<const float*>(blob + layout_rowrot_offset(n_rows_blob)) +
-                        static_cast<size_t>(d.layer * d.n_kv + kvh) * kRowRotFloats;
+                        static_cast<size_t>(layer * d.n_kv + kvh) * kRowRotFloats;
   for (int i = tid; i < kHeadDim * kHeadDim; i += kThreads) wt[i] = 0.f;
   __syncthreads();
   {
@@ -205,7 +144,7 @@ __global__ __launch_bounds__(W * 64) void k_prefill_qrot_bf16(Dims d, const uint
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, tk = lane & 15, kk = lane >> 4;
   const int kvh = blockIdx.y, seq = blockIdx.z;
   const int G = d.group, hq = d.n_kv * G, nr = n_q * G;
-  const int ri = d.layer * d.n_kv + kvh;
+  const int ri = (d.layer >= 0 ? d.layer : seq / d.batch) * d.n_kv + kvh;
   const RowMeta* M = reinterpret_cast<const RowMeta*>(blob + kOffRows) + ri;
   if (tid < kHeadDim) scale[tid] = kLog2e * rsqrtf(static_cast<float>(M->g_dim[M->grp[tid]]) * kHeadDim);
   stage_split<W>(wa, reinterpret_cast<const float4*>(blob + layout_kdense_offset(d.n_layers * d.n_kv)) +
@@ -239,166 +178,6 @@ __global__ __launch_bounds__(W * 64) void k_prefill_qrot_bf16(Dims d, const uint
 }
 
 // ---------------------------------------------------------------- 2. attention
-// Lane roles in the products (32x32x16 f16 MFMAs; l32 = lane % 32, hf =
-// lane / 32): the A operand comes from the decoded tile (token or dim l32 of
-// a 32-block, 8 consecutive k from 8 hf), the B operand is the wave's 32 query
-// rows (row l32, the same k), and an accumulator's register r holds token
-// (S^T) or dim (O^T) 8 (r / 4) + 4 hf + r % 4 of its 32-block for row l32.
-// The softmax weights of a lane are therefore, 8 registers at a time, a B
-// operand of O^T = V^T P^T whose k runs over tokens {4 hf + i, 8 + 4 hf + i}
-// of a 16-token step; the value tile stores the tokens of a step in that
-// order (0-3, 8-11, 4-7, 12-15), so that its operand is one 16-byte read.
-
-// Bits [POS, POS + LEN) of the little-endian word array w, placed at bit SH.
-template <int POS, int LEN, int SH, int N>
-__device__ __forceinline__ uint32_t field_at(const uint32_t (&w)[N]) {
-  constexpr int wi = POS / 32, sh = POS % 32;
-  static_assert(wi < N && SH + LEN <= 32, "field");
-  uint32_t v;
-  if constexpr (sh + LEN > 32) {
-    static_assert(wi + 1 < N && sh >= SH, "field word");
-    v = __builtin_amdgcn_alignbit(w[wi + 1], w[wi], sh - SH);
-  } else if constexpr (sh >= SH) {
-    v = w[wi] >> (sh - SH);
-  } else {
-    v = w[wi] << (SH - sh);
-  }
-  return v & (((1u << LEN) - 1u) << SH);
-}
-
-// Two consecutive BV-bit codes at bit POS of w -> two fp16 centroids.
-template <int BV, int POS, int N>
-__device__ __forceinline__ uint32_t value_pair(const uint8_t* smem, const uint32_t (&w)[N]) {
-  if constexpr (BV <= kMaxPair) {
-    return *reinterpret_cast<const uint32_t*>(smem + kOffPair + pair_offset(BV) + field_at<POS, 2 * BV, 2>(w));
-  } else {
-    const uint32_t c0 = *reinterpret_cast<const uint16_t*>(smem + kOffCb + 2 * cb_index(BV) + field_at<POS, BV, 1>(w));
-    const uint32_t c1 =
-        *reinterpret_cast<const uint16_t*>(smem + kOffCb + 2 * cb_index(BV) + field_at<POS + BV, BV, 1>(w));
-    return c0 | (c1 << 16);
-  }
-}
-
-// Key decode.  A key row is 32 items of 4 consecutive stream positions: two
-// pairs, each inside one group (groups have even sizes), whose codes are one
-// dense field of 2 bA + 2 bB <= 32 bits.  Lane = token; a wave decodes the
-// items wave + 8 j, so that everything that describes an item is
-// wave-uniform, and stores 8 bytes per item and token.
-constexpr int kItemsPer = kHeadDim / 4 / kAttnWaves;
-struct KeyItems {
-  uint32_t word[kItemsPer];                     // byte offset of the first of the two words that are loaded
-  uint32_t sh[kItemsPer];                       // first bit of the field in them
-  uint32_t wa[kItemsPer], wb[kItemsPer];        // 2 bA, 2 bB
-  uint32_t ta[kItemsPer], tb[kItemsPer];        // offsets of the widths' pair tables
-  uint32_t sel_lo[kItemsPer], sel_hi[kItemsPer];  // byte selectors that pick (rA, rB) from the token's 8 radii:
-                                                // groups 0-3 and 4-7, a radius in the other half selects zero
-  bool wide;                                    // some width is above kMaxPair: codes looked up one by one
-};
-// Raw words of a thread's share of one tile.
-template <int BV>
-struct Raw {
-  static constexpr int kVW = (BV + 1) / 2;  // words of 16 value codes
-  uint2 k[kItemsPer];
-  uint4 kn;
-  uint32_t v[kVW];
-  uint32_t vn;
-};
-__device__ __forceinline__ KeyItems key_items(const RowMeta* M, int wave, int kw) {
-  KeyItems k;
-  k.wide = false;
-#pragma unroll
-  for (int j = 0; j < kItemsPer; ++j) {
-    const int p = 4 * (wave + kAttnWaves * j);
-    const auto uni = [](uint32_t v) { return static_cast<uint32_t>(__builtin_amdgcn_readfirstlane(static_cast<int>(v))); };
-    const uint32_t off = uni(M->bitoff[p]), ba = uni(M->width[p]), bb = uni(M->width[p + 2]), ga = uni(M->grp[p]),
-                   gb = uni(M->grp[p + 2]);
-    const uint32_t w0 = min(off >> 5, static_cast<uint32_t>(kw - 2));  // (a row has at least 4 words)
-    const auto tab = [](uint32_t b) { return static_cast<uint32_t>(kOffPair) + 4 * (((1u << (2 * b)) - 4u) / 3u); };
-    const auto sel = [](uint32_t g) { return 2 * (g & 3u) | (2 * (g & 3u) + 1) << 8; };
-    k.word[j] = 4 * w0;
-    k.sh[j] = off - 32 * w0;
-    k.wa[j] = 2 * ba;
-    k.wb[j] = 2 * bb;
-    k.ta[j] = tab(ba);
-    k.tb[j] = tab(bb);
-    k.sel_lo[j] = (ga < 4 ? sel(ga) : 0x0C0Cu) | (gb < 4 ? sel(gb) : 0x0C0Cu) << 16;
-    k.sel_hi[j] = (ga < 4 ? 0x0C0Cu : sel(ga)) | (gb < 4 ? 0x0C0Cu : sel(gb)) << 16;
-    k.wide = k.wide || ba > kMaxPair || bb > kMaxPair;
-  }
-  return k;
-}
-// The centroids of the wave's items (c.x: pair A, c.y: pair B).
-template <bool WIDE>
-__device__ __forceinline__ void key_lookups(const uint8_t* smem, const KeyItems& it, const uint2 (&w)[kItemsPer],
-                                            uint2 (&c)[kItemsPer]) {
-#pragma unroll
-  for (int j = 0; j < kItemsPer; ++j) {
-    const uint32_t f = static_cast<uint32_t>((static_cast<uint64_t>(w[j].y) << 32 | w[j].x) >> it.sh[j]);
-    if constexpr (!WIDE) {
-      c[j].x = *reinterpret_cast<const uint32_t*>(smem + it.ta[j] + 4 * __builtin_amdgcn_ubfe(f, 0, it.wa[j]));
-      c[j].y = *reinterpret_cast<const uint32_t*>(smem + it.tb[j] + 4 * __builtin_amdgcn_ubfe(f, it.wa[j], it.wb[j]));
-    } else {
-      const uint32_t ba = it.wa[j] >> 1, bb = it.wb[j] >> 1;
-      const auto one = [&](uint32_t at, uint32_t b) {
-        return static_cast<uint32_t>(*reinterpret_cast<const uint16_t*>(
-            smem + kOffCb + 2 * ((1u << b) - 2u + __builtin_amdgcn_ubfe(f, at, b))));
-      };
-      c[j].x = one(0, ba) | one(ba, ba) << 16;
-      c[j].y = one(2 * ba, bb) | one(2 * ba + bb, bb) << 16;
-    }
-  }
-}
-// Item j: centroids times the groups' radii, as fp16 hi and lo parts.  The
-// product of two fp16 numbers has at most 22 significant bits: hi =
-// fp16(r c) and the fused residual lo = fp16(r c - hi) carry all of them above
-// fp16's subnormal step.  dst: the item's place in the token's decoded row.
-__device__ __forceinline__ void key_store(uint8_t* dst, const KeyItems& it, int j, const uint4& radii, const uint2& c) {
-  const uint32_t r =
-      __builtin_amdgcn_perm(radii.y, radii.x, it.sel_lo[j]) | __builtin_amdgcn_perm(radii.w, radii.z, it.sel_hi[j]);
-  const half2_t rr = __builtin_bit_cast(half2_t, r);
-  const half2_t ra = {rr[0], rr[0]}, rb = {rr[1], rr[1]};
-  const half2_t ca = __builtin_bit_cast(half2_t, c.x), cb = __builtin_bit_cast(half2_t, c.y);
-  const half2_t ha = ra * ca, hb = rb * cb;
-  const half2_t la = __builtin_elementwise_fma(ra, ca, -ha), lb = __builtin_elementwise_fma(rb, cb, -hb);
-  *reinterpret_cast<uint2*>(dst + kDecKH) =
-      make_uint2(__builtin_bit_cast(uint32_t, ha), __builtin_bit_cast(uint32_t, hb));
-  *reinterpret_cast<uint2*>(dst + kDecKL) =
-      make_uint2(__builtin_bit_cast(uint32_t, la), __builtin_bit_cast(uint32_t, lb));
-}
-
-// Value decode: thread = (dim tid % 128, 16-token step tid / 128); a holds
-// tokens 0-3 and 8-11 of the step, b tokens 4-7 and 12-15.
-template <int BV>
-__device__ __forceinline__ void value_lookups(const uint8_t* smem, const Raw<BV>& raw, int quarter, uint4& a, uint4& b) {
-  constexpr int NW = Raw<BV>::kVW;
-  uint32_t w[NW];
-  if constexpr (BV % 2 == 0) {
-#pragma unroll
-    for (int i = 0; i < NW; ++i) w[i] = raw.v[i];
-  } else {
-    const int sh = 16 * (quarter & 1);  // uniform
-#pragma unroll
-    for (int i = 0; i < NW; ++i) w[i] = __builtin_amdgcn_alignbit(i + 1 < NW ? raw.v[i + 1] : 0u, raw.v[i], sh);
-  }
-  a.x = value_pair<BV, 0 * BV>(smem, w);
-  a.y = value_pair<BV, 2 * BV>(smem, w);
-  b.x = value_pair<BV, 4 * BV>(smem, w);
-  b.y = value_pair<BV, 6 * BV>(smem, w);
-  a.z = value_pair<BV, 8 * BV>(smem, w);
-  a.w = value_pair<BV, 10 * BV>(smem, w);
-  b.z = value_pair<BV, 12 * BV>(smem, w);
-  b.w = value_pair<BV, 14 * BV>(smem, w);
-}
-template <int BV>
-__device__ __forceinline__ void store_values(uint8_t* dec, const Raw<BV>& raw, int tid, int quarter, const uint4& a,
-                                             const uint4& b) {
-  uint4* dst = reinterpret_cast<uint4*>(dec + kDecV + (tid & 127) * (2 * kVStride) + 32 * quarter);
-  dst[0] = a;
-  dst[1] = b;
-  // every wave stores the 64 value radii it loaded (the same ones; no branch)
-  reinterpret_cast<uint16_t*>(dec + kDecVN)[tid & 63] = static_cast<uint16_t>(raw.vn);
-}
-
 // What bounds it: per 64-token tile a SIMD's two waves issue 128 MFMAs of 32
 // cycles and 570 other VALU instructions, and meet at one barrier.  On the
 // 32K-token Llama-shaped layer (14.9 ms; 23.0 ms with 16x16x32 products and a
@@ -791,19 +570,17 @@ hipError_t launch_attn(const Dims& d, const uint8_t* blob, const float* qr, int 
 
 }  // namespace prefill_detail
 
-hipError_t launch_prefill_attn(const Dims& d, const void* layout, const void* q, int n_q,
-                               const int32_t* q_pos0, int max_pos, const CachePtrs& c, float* qr_ws,
-                               float* out, hipStream_t s) {
+hipError_t launch_query_rotation(const Dims& d, const void* layout, const void* q, int n_q, float* qr, hipStream_t s) {
   using namespace prefill_detail;
   const uint8_t* blob = static_cast<const uint8_t*>(layout);
   const int nr = n_q * d.group;
-  const bool aligned = (reinterpret_cast<uintptr_t>(q) | reinterpret_cast<uintptr_t>(qr_ws)) % 16 == 0;
+  const bool aligned = (reinterpret_cast<uintptr_t>(q) | reinterpret_cast<uintptr_t>(qr)) % 16 == 0;
   if (d.in_dtype == 1 && aligned) {
-    const long rows = static_cast<long>(nr) * d.n_kv * d.batch;
+    const long rows = static_cast<long>(nr) * d.n_kv * d.n_lc * d.batch;
     const auto go = [&](auto kern, int w, int iters) {
       const int per = w * split::kSplitRows * iters;
-      hipLaunchKernelGGL(kern, dim3((nr + per - 1) / per, d.n_kv, d.batch), dim3(w * 64), 0, s, d, blob, q, n_q, iters,
-                         qr_ws);
+      hipLaunchKernelGGL(kern, dim3((nr + per - 1) / per, d.n_kv, d.n_lc * d.batch), dim3(w * 64), 0, s, d, blob, q, n_q, iters,
+                         qr);
     };
     // 4-wave workgroups up to 64K rows, where 16-wave ones would leave CUs
     // idle; above, 16 waves share one staging of the matrix, and above 512K rows
@@ -815,10 +592,18 @@ hipError_t launch_prefill_attn(const Dims& d, const void* layout, const void* q,
     if (rows <= 256L * 256) go(k_prefill_qrot_bf16<4>, 4, 1);
     else go(k_prefill_qrot_bf16<16>, 16, rows <= 4L * 256 * 512 ? 1 : 4);
   } else {
-    const dim3 g1((nr + kQrotRows - 1) / kQrotRows, d.n_kv, d.batch);
-    hipLaunchKernelGGL(k_prefill_qrot, g1, dim3(kThreads), 0, s, d, blob, q, n_q, qr_ws);
+    const dim3 g1((nr + kQrotRows - 1) / kQrotRows, d.n_kv, d.n_lc * d.batch);
+    hipLaunchKernelGGL(k_prefill_qrot, g1, dim3(kThreads), 0, s, d, blob, q, n_q, qr);
   }
-  hipError_t e = hipGetLastError();
+  return hipGetLastError();
+}
+
+hipError_t launch_prefill_attn(const Dims& d, const void* layout, const void* q, int n_q,
+                               const int32_t* q_pos0, int max_pos, const CachePtrs& c, float* qr_ws,
+                               float* out, hipStream_t s) {
+  using namespace prefill_detail;
+  const uint8_t* blob = static_cast<const uint8_t*>(layout);
+  hipError_t e = launch_query_rotation(d, layout, q, n_q, qr_ws, s);
   if (e != hipSuccess) return e;
   switch (d.v_bits) {
     case 1: return launch_attn<1>(d, blob, qr_ws, n_q, q_pos0, max_pos, c, out, s);
