@@ -883,16 +883,21 @@ int blockgtq_dequantize_rows(const bgtq_config* cfg, const void* d_layout, int32
 struct CrossPlan {
   int rows, n_splits, split_len;
   long items;
+  double wg;  // estimated us of a workgroup
 };
 
 // The plan with the least estimated time over the row counts and splits.  One
 // workgroup runs per CU, so `items` of them take ceil(items / 256) rounds, each
-// as long as one split.  Times in us of a workgroup, measured on long calls:
-//   32 rows (8 waves, a 64-row tile each): 6 per 8 tiles;
-//   128 rows: 2.0 a tile, 256 rows: 2.8 a tile, and a launch more for the
-//   rotation;
-// plus set-up and end, and the joining launch for more than one split.
-static CrossPlan cross_plan(const Dims& d, int n_q, int max_len, int requested, bool joined) {
+// as long as one split.  In us, measured (kernel times in a graph):
+//   32 rows: 12.5 a workgroup + 5.7 (key rows of up to 8 words) or 6.6 for
+//     every 8 tiles, a tile per wave;
+//   128 rows: 14 + 1.9 a tile, 256 rows: 14 + 2.85 a tile, after a rotation
+//     launch of 9 + 1 per 5000 query rows;
+//   joining: 4, and the partials written and read at 4.5 TB/s.
+// `beside`: the sequences' own pass in the same call (prefix passes).  Its
+// workgroups fill up the last round of 32-row ones, whose launch it shares, and
+// come after wide ones.
+static CrossPlan cross_plan(const Dims& d, int n_q, int max_len, int requested, const CrossPlan* beside) {
   const long units = static_cast<long>(d.n_kv) * d.n_lc * d.batch, nr = static_cast<long>(n_q) * d.group;
   const int tiles = std::max(1, (max_len + 63) / 64);
   CrossPlan best = {};
@@ -901,14 +906,23 @@ static CrossPlan cross_plan(const Dims& d, int n_q, int max_len, int requested, 
     if (rows > 32 && (nr <= rows / 4 || static_cast<long>(d.n_lc) * d.batch > 65535)) continue;
     const long blocks = units * ((nr + rows - 1) / rows);
     const int k0 = requested > 0 ? std::min(requested, tiles) : 1;
-    const int k1 = requested > 0 ? k0 : std::min(rows == 32 ? (tiles + 7) / 8 : (tiles + 3) / 4, 256);
+    const int k1 = requested > 0 ? k0 : std::min(rows == 32 ? (tiles + 7) / 8 : tiles, 256);
     for (int k = k0; k <= std::max(k0, k1); ++k) {
       const int len = (tiles + k - 1) / k, n = (tiles + len - 1) / len;
-      const double wg = rows == 32 ? 6.0 * ((len + 7) / 8) + 12.0 : (rows == 128 ? 2.0 : 2.8) * len + 12.0;
-      const double t = static_cast<double>((blocks * n + 255) / 256) * wg + (n > 1 && !joined ? 5.0 : 0.0) + (rows > 32 ? 8.0 : 0.0);
+      const double wg = rows == 32 ? 12.5 + (d.k_words <= 8 ? 5.7 : 6.6) * ((len + 7) / 8)
+                                   : 14.0 + (rows == 128 ? 1.9 : 2.85) * len;
+      const long rounds = (blocks * n + 255) / 256;
+      double t = static_cast<double>(rounds) * wg;
+      if (rows > 32) t += 9.0 + 2e-4 * units * nr;
+      if (beside) {
+        const long left = std::max(0l, beside->items - (rows == 32 ? rounds * 256 - blocks * n : 0));
+        t += static_cast<double>((left + 255) / 256) * beside->wg + (rows > 32 ? 5.0 : 0.0);
+      }
+      if (n > 1 && !beside) t += 4.0;
+      if (n > 1 || beside) t += 2.4e-7 * kPartFloats * 4 * units * nr * n;
       if (!best.rows || t < t_best) {
         t_best = t;
-        best = {rows, n, 64 * len, blocks * n};
+        best = {rows, n, 64 * len, blocks * n, wg};
       }
     }
   }
@@ -945,7 +959,7 @@ static Dims cross_dims(const bgtq_config* cfg, int32_t n_lc) {
 }
 
 static CrossPlan cross_attn_plan(const bgtq_config* cfg, int32_t n_lc, int32_t n_q, int32_t max_ctx, int32_t n_splits) {
-  return cross_plan(cross_dims(cfg, n_lc), n_q, max_ctx, n_splits, false);
+  return cross_plan(cross_dims(cfg, n_lc), n_q, max_ctx, n_splits, nullptr);
 }
 
 int blockgtq_cross_workspace_bytes(const bgtq_config* cfg, int32_t n_layers_in_call, int32_t n_q, int32_t n_splits,
@@ -1011,8 +1025,10 @@ struct SharedPlan {
 };
 static SharedPlan shared_plan(const bgtq_config* cfg, const bgtq_config* pcfg, int32_t n_lc, int32_t n_splits,
                               int32_t max_prefix, int32_t max_ctx) {
-  return {cross_plan(cross_dims(pcfg, n_lc), cfg->batch, max_prefix, n_splits, true),
-          cross_plan(cross_dims(cfg, n_lc), 1, max_ctx, 0, true)};  // (at most 8 query rows: 32-row workgroups)
+  SharedPlan p;
+  p.own = cross_plan(cross_dims(cfg, n_lc), 1, max_ctx, 0, nullptr);  // (at most 8 query rows: 32-row workgroups)
+  p.prefix = cross_plan(cross_dims(pcfg, n_lc), cfg->batch, max_prefix, n_splits, &p.own);
+  return p;
 }
 
 int blockgtq_shared_workspace_bytes(const bgtq_config* cfg, const bgtq_config* prefix_cfg, int32_t n_layers_in_call,

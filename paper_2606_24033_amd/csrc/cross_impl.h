@@ -196,19 +196,23 @@ __device__ __forceinline__ half8_t as_half8(const uint2& a, const uint2& b) {
 }
 
 // ---------------------------------------------------------------- QK
-// 16 coordinates (bits POS .. of aw) of all 64 tokens times the query rows:
-// hi and lo query parts into the accumulators of the two token blocks.
-template <int B, int POS, bool Z, int N>
-__device__ __forceinline__ void qk_step(const uint8_t* smem, const uint32_t (&aw)[N], const LaneRep& rep, uint32_t img,
-                                        float16_t (&part)[2]) {
-  uint2 a0 = __builtin_bit_cast(uint2, decode4<B, POS, true>(smem, aw, rep));
-  uint2 a1 = __builtin_bit_cast(uint2, decode4<B, POS + 4 * B, true>(smem, aw, rep));
-  uint2 b0 = __builtin_bit_cast(uint2, decode4<B, POS + 8 * B, true>(smem, aw, rep));
-  uint2 b1 = __builtin_bit_cast(uint2, decode4<B, POS + 12 * B, true>(smem, aw, rep));
-  const half8_t qh = *reinterpret_cast<const half8_t*>(smem + img);
-  const half8_t ql = *reinterpret_cast<const half8_t*>(smem + img + 1024);
-  swap_halves(a0, a1, b0, b1);
-  const half8_t k0 = as_half8(a0, a1), k1 = as_half8(b0, b1);
+// 16 coordinates of all 64 tokens: four lookups of four codes (bits POS .. of
+// aw), or the operands of both token blocks once the half-waves have changed.
+struct Step {
+  uint2 a0, a1, b0, b1;
+};
+template <int B, int POS, int N>
+__device__ __forceinline__ Step step_lookups(const uint8_t* smem, const uint32_t (&aw)[N], const LaneRep& rep) {
+  return {__builtin_bit_cast(uint2, decode4<B, POS, true>(smem, aw, rep)),
+          __builtin_bit_cast(uint2, decode4<B, POS + 4 * B, true>(smem, aw, rep)),
+          __builtin_bit_cast(uint2, decode4<B, POS + 8 * B, true>(smem, aw, rep)),
+          __builtin_bit_cast(uint2, decode4<B, POS + 12 * B, true>(smem, aw, rep))};
+}
+// The step's products: hi and lo query parts into the accumulators of the two
+// token blocks.
+template <bool Z>
+__device__ __forceinline__ void step_products(const Step& k, const half8_t& qh, const half8_t& ql, float16_t (&part)[2]) {
+  const half8_t k0 = as_half8(k.a0, k.a1), k1 = as_half8(k.b0, k.b1);
   if constexpr (Z) {  // the group's first product starts its accumulators
     const float16_t zero = {};
     part[0] = __builtin_amdgcn_mfma_f32_32x32x16_f16(k0, qh, zero, 0, 0, 0);
@@ -221,17 +225,30 @@ __device__ __forceinline__ void qk_step(const uint8_t* smem, const uint32_t (&aw
   part[1] = __builtin_amdgcn_mfma_f32_32x32x16_f16(k1, ql, part[1], 0, 0, 0);
 }
 
-// The group of width B (metadata gm): S += radius * (codes x query rows).  Its
-// bits are realigned to bit 0 of a small word array, 32 coordinates at a time
-// (16 for the wide codes).
+// S += radius * (the products of a group)
+__device__ __forceinline__ void add_scaled(const half4_t (&r)[2][4], const float16_t (&part)[2], float16_t (&s)[2]) {
+#pragma unroll
+  for (int n = 0; n < 2; ++n)
+#pragma unroll
+    for (int q = 0; q < 4; ++q)
+#pragma unroll
+      for (int i = 0; i < 4; ++i)
+        s[n][4 * q + i] = fmaf(static_cast<float>(r[n][q][i]), part[n][4 * q + i], s[n][4 * q + i]);
+}
+
+// The group of width B (metadata gm): part = codes x query rows.  Its bits are
+// realigned to bit 0 of a small word array, 32 coordinates at a time (16 for
+// the wide codes); the lookups of both steps are in flight before the first
+// product (a step past the group's end decodes other bits of the row for
+// nobody), and the last group's products are added to S behind this one's first
+// lookups.
 template <int B, int KWB>
 __device__ __forceinline__ void qk_group(const uint8_t* smem, const uint32_t (&rw)[KWB + split_detail::kRowPad],
                                          uint32_t gm, int step0, const uint8_t* radii, const LaneRep& rep, int lane,
-                                         float16_t (&s)[2]) {
+                                         half4_t (&r)[2][4], float16_t (&part)[2], float16_t (&s)[2]) {
   constexpr int CH = B <= 4 ? 2 : 1;             // steps per chunk
   constexpr int NW = (CH * 16 * B + 31) / 32;    // its words
   const int o = split_detail::gm_off(gm), n16 = (split_detail::gm_steps(gm) + 3) >> 2;
-  float16_t part[2];
   const auto chunk = [&](auto first, int c) __attribute__((always_inline)) {
     const int at = o + c * 16 * B, w0 = at >> 5, sh = at & 31;
     uint32_t aw[NW + 1];
@@ -239,22 +256,32 @@ __device__ __forceinline__ void qk_group(const uint8_t* smem, const uint32_t (&r
     for (int i = 0; i < NW; ++i) aw[i] = __builtin_amdgcn_alignbit(rw[w0 + i + 1], rw[w0 + i], sh);
     aw[NW] = 0;
     const uint32_t img = kImg + (step0 + c) * 2048 + lane * 16;
-    qk_step<B, 0, decltype(first)::value>(smem, aw, rep, img, part);
+    Step k0 = step_lookups<B, 0>(smem, aw, rep), k1;
+    const half8_t qh = *reinterpret_cast<const half8_t*>(smem + img);
+    const half8_t ql = *reinterpret_cast<const half8_t*>(smem + img + 1024);
+    if constexpr (CH == 2) k1 = step_lookups<B, 16 * B>(smem, aw, rep);
+    __builtin_amdgcn_sched_barrier(0);  // (every read of the chunk is issued before the first wait)
+    if constexpr (decltype(first)::value) {
+      if (step0 > 0) add_scaled(r, part, s);
+      // radii of the lane's tokens: 8 q + 4 hf .. + 3 of each block
+#pragma unroll
+      for (int n = 0; n < 2; ++n)
+#pragma unroll
+        for (int q = 0; q < 4; ++q) r[n][q] = *reinterpret_cast<const half4_t*>(radii + 2 * (32 * n + 8 * q));
+    }
+    swap_halves(k0.a0, k0.a1, k0.b0, k0.b1);
+    if constexpr (CH == 2) swap_halves(k1.a0, k1.a1, k1.b0, k1.b1);
+    step_products<decltype(first)::value>(k0, qh, ql, part);
     if constexpr (CH == 2) {
-      if (c + 1 < n16) qk_step<B, 16 * B, false>(smem, aw, rep, img + 2048, part);
+      if (c + 1 < n16) {
+        const half8_t qh1 = *reinterpret_cast<const half8_t*>(smem + img + 2048);
+        const half8_t ql1 = *reinterpret_cast<const half8_t*>(smem + img + 3072);
+        step_products<false>(k1, qh1, ql1, part);
+      }
     }
   };
   chunk(std::true_type{}, 0);
   for (int c = CH; c < n16; c += CH) chunk(std::false_type{}, c);
-  // radii of the lane's tokens: 8 q + 4 hf .. + 3 of each block
-#pragma unroll
-  for (int n = 0; n < 2; ++n)
-#pragma unroll
-    for (int q = 0; q < 4; ++q) {
-      const half4_t r = *reinterpret_cast<const half4_t*>(radii + 2 * (32 * n + 8 * q));
-#pragma unroll
-      for (int i = 0; i < 4; ++i) s[n][4 * q + i] = fmaf(static_cast<float>(r[i]), part[n][4 * q + i], s[n][4 * q + i]);
-    }
 }
 
 template <int KWB, int... BM1>
@@ -262,14 +289,17 @@ __device__ __forceinline__ void qk_all(std::integer_sequence<int, BM1...>, const
                                        const uint32_t (&rw)[KWB + split_detail::kRowPad], const uint32_t (&gm)[8],
                                        const uint8_t* radii, const LaneRep& rep, int lane, float16_t (&s)[2]) {
   int step0 = 0;
+  half4_t r[2][4];
+  float16_t part[2];
   const auto one = [&](auto bm1) __attribute__((always_inline)) {
     constexpr int b = decltype(bm1)::value;
     if (gm[b] >> 31) {
-      qk_group<b + 1, KWB>(smem, rw, gm[b], step0, radii + split_detail::gm_plane(gm[b]) * 128, rep, lane, s);
+      qk_group<b + 1, KWB>(smem, rw, gm[b], step0, radii + split_detail::gm_plane(gm[b]) * 128, rep, lane, r, part, s);
       step0 += (split_detail::gm_steps(gm[b]) + 3) >> 2;
     }
   };
   (one(std::integral_constant<int, BM1>{}), ...);
+  add_scaled(r, part, s);
 }
 
 // ---------------------------------------------------------------- lookup tables
@@ -576,7 +606,9 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(2, 2))
 #pragma unroll
       for (int i = 0; i < 16; ++i) s[n][i] = 0.f;
     qk_all<KWB>(std::make_integer_sequence<int, 8>{}, smem, rw, gm, rad_l, rep, lane, s);
-    if (t0 + kStride < t_end) load_keys(t0 + kStride);
+    // (without a next tile this one again: the loads in flight stay countable)
+    const int t_next = t0 + kStride < t_end ? t0 + kStride : t0;
+    load_keys(t_next);
 
     // ---- online softmax, base 2
     if (!full) {
@@ -673,7 +705,7 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(2, 2))
         }
       }
     }
-    if (t0 + kStride < t_end) load_values(t0 + kStride);
+    load_values(t_next);
   }
   {
     float x, y;
@@ -694,12 +726,14 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(2, 2))
   float* const ms = reinterpret_cast<float*>(smem + kEndM);
   float* const ls = ms + kWaves * kRows;
   const int n_act = min(kWaves, (t_end - t_begin + kKeyTile - 1) / kKeyTile);  // waves that had a tile
+  if (wave < n_act) {
 #pragma unroll
-  for (int cc = 0; cc < 4; ++cc)
+    for (int cc = 0; cc < 4; ++cc)
 #pragma unroll
-    for (int u = 0; u < 4; ++u)
-      *reinterpret_cast<float4_t*>(acc + (wave * kRows + l32) * kAccStride + 32 * cc + 8 * u + 4 * hf) =
-          float4_t{o[cc][4 * u], o[cc][4 * u + 1], o[cc][4 * u + 2], o[cc][4 * u + 3]};
+      for (int u = 0; u < 4; ++u)
+        *reinterpret_cast<float4_t*>(acc + (wave * kRows + l32) * kAccStride + 32 * cc + 8 * u + 4 * hf) =
+            float4_t{o[cc][4 * u], o[cc][4 * u + 1], o[cc][4 * u + 2], o[cc][4 * u + 3]};
+  }
   if (hf == 0) {
     ms[wave * kRows + l32] = m_run;
     ls[wave * kRows + l32] = l_run;
