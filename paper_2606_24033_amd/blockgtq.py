@@ -6,6 +6,7 @@ if the library is missing or a call returns an error; there is no fallback.
 """
 from __future__ import annotations
 
+import contextlib
 import ctypes
 import os
 from dataclasses import dataclass
@@ -404,31 +405,40 @@ def blockgtq_rope_decode_step(cfg: Config, layout: Layout, rope_base: float, q_p
 
 # ---------------------------------------------------------------- packed rows read by other callers
 
-def _one_device(*tensors):
-    """The device of every tensor given (None is skipped), contiguous and on one GPU."""
-    import torch
-    on = [t for t in tensors if t is not None]
-    for t in on:
-        if not isinstance(t, torch.Tensor) or not t.is_cuda or not t.is_contiguous():
-            raise ValueError("device tensors must be contiguous CUDA tensors")
-    if len({t.device for t in on}) > 1:
-        raise ValueError("tensors on different devices: " + ", ".join(sorted({str(t.device) for t in on})))
-    return on[0].device
-
-
 def _check_shape(what, t, shape, dtype):
-    if tuple(t.shape) != tuple(shape) or t.dtype != dtype:
+    if t.shape != shape or t.dtype != dtype:
         raise ValueError(f"{what}: expected {tuple(shape)} of {dtype}, got {tuple(t.shape)} of {t.dtype}")
 
 
-def _check_cache(cfg: Config, cache: Cache, what="cache"):
+def _cache_tensors(cfg: Config, cache: Cache, what="cache"):
     import torch
-    L, B, H, C = cfg.n_layers, cfg.batch, cfg.n_kv_heads, cfg.capacity
-    _check_shape(what + ".k_codes", cache.k_codes, (L, B, H, C, cfg.k_words), torch.int32)
-    _check_shape(what + ".k_norms", cache.k_norms, (L, B, H, C * MAX_GROUPS), torch.float16)
-    _check_shape(what + ".v_codes", cache.v_codes, (L, B, H, C // 32, HEAD_DIM, cfg.v_bits), torch.int32)
-    _check_shape(what + ".v_norms", cache.v_norms, (L, B, H, C), torch.float16)
-    return [cache.k_codes, cache.k_norms, cache.v_codes, cache.v_norms]
+    lead = (cfg.n_layers, cfg.batch, cfg.n_kv_heads)
+    C, i32, f16 = cfg.capacity, torch.int32, torch.float16
+    _check_shape(what + ".k_codes", cache.k_codes, lead + (C, cfg.k_words), i32)
+    _check_shape(what + ".k_norms", cache.k_norms, lead + (C * MAX_GROUPS,), f16)
+    _check_shape(what + ".v_codes", cache.v_codes, lead + (C // 32, HEAD_DIM, cfg.v_bits), i32)
+    _check_shape(what + ".v_norms", cache.v_norms, lead + (C,), f16)
+    return cache.k_codes, cache.k_norms, cache.v_codes, cache.v_norms
+
+
+def _call(fn, stream, args, *tensors):
+    """fn(*args, stream) on the one GPU that holds all the tensors (None is
+    skipped), whichever is current: on `stream`, or that GPU's current one."""
+    import torch
+    tensors = [t for t in tensors if t is not None]
+    d = tensors[0].get_device()
+    for t in tensors:
+        if t.get_device() < 0 or not t.is_contiguous():
+            raise ValueError("device tensors must be contiguous CUDA tensors")
+        if t.get_device() != d:
+            raise ValueError("tensors on different devices: " + ", ".join(sorted({str(x.device) for x in tensors})))
+    with torch.cuda.device(d) if torch.cuda.current_device() != d else contextlib.nullcontext():
+        s = torch._C._cuda_getCurrentRawStream(d) if stream is None else stream.cuda_stream
+        _check(fn(*args, s))
+
+
+def _at(t):
+    return None if t is None else t.data_ptr()
 
 
 def _out_type(dtype):
@@ -464,12 +474,10 @@ def blockgtq_dequantize_rows(cfg: Config, layout: Layout, layer: int, cache: Cac
     for name, t in (("k_out", k_out), ("v_out", v_out)):
         if t is not None:
             _check_shape(name, t, shape, dtype)
-    kind = _out_type(dtype)
-    device = _one_device(layout.blob, read_pos, ctx_len, k_out, v_out, *_check_cache(cfg, cache))
-    with torch.cuda.device(device):
-        _check(lib().blockgtq_dequantize_rows(ctypes.byref(cfg.c()), _ptr(layout.blob), layer, ctypes.byref(cache.c()),
-                                              n_rows, _ptr(read_pos), _ptr(ctx_len), _ptr(k_out), _ptr(v_out), kind,
-                                              _stream(stream)))
+    _call(lib().blockgtq_dequantize_rows, stream,
+          (ctypes.byref(cfg.c()), layout.blob.data_ptr(), layer, ctypes.byref(cache.c()), n_rows, read_pos.data_ptr(),
+           _at(ctx_len), _at(k_out), _at(v_out), _out_type(dtype)),
+          read_pos, layout.blob, ctx_len, k_out, v_out, *_cache_tensors(cfg, cache))
     return k_out, v_out
 
 
@@ -515,11 +523,11 @@ def blockgtq_cross_attn(cfg: Config, layout: Layout, layer: int, q, ctx_len, max
     if workspace is None:
         workspace = torch.empty(max(cross_workspace_bytes(cfg, n_lc, n_q, n_splits, max_ctx), 1), dtype=torch.uint8,
                                 device=q.device)
-    device = _one_device(q, layout.blob, ctx_len, out, workspace, *_check_cache(cfg, cache))
-    with torch.cuda.device(device):
-        _check(lib().blockgtq_cross_attn(ctypes.byref(cfg.c()), _ptr(layout.blob), layer, _ptr(q), n_q, _ptr(ctx_len),
-                                         max_ctx, ctypes.byref(cache.c()), _ptr(out), kind, _ptr(workspace),
-                                         workspace.numel() * workspace.element_size(), n_splits, _stream(stream)))
+    _call(lib().blockgtq_cross_attn, stream,
+          (ctypes.byref(cfg.c()), layout.blob.data_ptr(), layer, q.data_ptr(), n_q, ctx_len.data_ptr(), max_ctx,
+           ctypes.byref(cache.c()), out.data_ptr(), kind, workspace.data_ptr(),
+           workspace.numel() * workspace.element_size(), n_splits),
+          q, layout.blob, ctx_len, out, workspace, *_cache_tensors(cfg, cache))
     return out
 
 
@@ -540,15 +548,13 @@ def blockgtq_decode_attn_shared(cfg: Config, layout: Layout, layer: int, q, pref
     if workspace is None:
         workspace = torch.empty(shared_workspace_bytes(cfg, prefix_cfg, n_lc, n_splits, max_prefix, max_ctx),
                                 dtype=torch.uint8, device=q.device)
-    device = _one_device(q, layout.blob, prefix_len, ctx_len, out, workspace, *_check_cache(cfg, cache),
-                         *_check_cache(prefix_cfg, prefix, "prefix"))
-    with torch.cuda.device(device):
-        _check(lib().blockgtq_decode_attn_shared(ctypes.byref(cfg.c()), _ptr(layout.blob), layer, _ptr(q),
-                                                 ctypes.byref(prefix_cfg.c()), ctypes.byref(prefix.c()),
-                                                 _ptr(prefix_len), max_prefix, _ptr(ctx_len), max_ctx,
-                                                 ctypes.byref(cache.c()), _ptr(out), kind, _ptr(workspace),
-                                                 workspace.numel() * workspace.element_size(), n_splits,
-                                                 _stream(stream)))
+    _call(lib().blockgtq_decode_attn_shared, stream,
+          (ctypes.byref(cfg.c()), layout.blob.data_ptr(), layer, q.data_ptr(), ctypes.byref(prefix_cfg.c()),
+           ctypes.byref(prefix.c()), prefix_len.data_ptr(), max_prefix, ctx_len.data_ptr(), max_ctx,
+           ctypes.byref(cache.c()), out.data_ptr(), kind, workspace.data_ptr(),
+           workspace.numel() * workspace.element_size(), n_splits),
+          q, layout.blob, prefix_len, ctx_len, out, workspace, *_cache_tensors(cfg, cache),
+          *_cache_tensors(prefix_cfg, prefix, "prefix"))
     return out
 
 

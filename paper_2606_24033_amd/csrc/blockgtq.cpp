@@ -889,14 +889,14 @@ struct CrossPlan {
 // The plan with the least estimated time over the row counts and splits.  One
 // workgroup runs per CU, so `items` of them take ceil(items / 256) rounds, each
 // as long as one split.  In us, measured (kernel times in a graph):
-//   32 rows: 12.5 a workgroup + 5.7 (key rows of up to 8 words) or 6.6 for
+//   32 rows: 12 a workgroup + 5.4 (key rows of up to 8 words) or 6.2 for
 //     every 8 tiles, a tile per wave;
 //   128 rows: 14 + 1.9 a tile, 256 rows: 14 + 2.85 a tile, after a rotation
 //     launch of 9 + 1 per 5000 query rows;
 //   joining: 4, and the partials written and read at 4.5 TB/s.
 // `beside`: the sequences' own pass in the same call (prefix passes).  Its
-// workgroups fill up the last round of 32-row ones, whose launch it shares, and
-// come after wide ones.
+// workgroups follow 32-row ones as these end, in one launch, and come after
+// wide ones.
 static CrossPlan cross_plan(const Dims& d, int n_q, int max_len, int requested, const CrossPlan* beside) {
   const long units = static_cast<long>(d.n_kv) * d.n_lc * d.batch, nr = static_cast<long>(n_q) * d.group;
   const int tiles = std::max(1, (max_len + 63) / 64);
@@ -909,15 +909,19 @@ static CrossPlan cross_plan(const Dims& d, int n_q, int max_len, int requested, 
     const int k1 = requested > 0 ? k0 : std::min(rows == 32 ? (tiles + 7) / 8 : tiles, 256);
     for (int k = k0; k <= std::max(k0, k1); ++k) {
       const int len = (tiles + k - 1) / k, n = (tiles + len - 1) / len;
-      const double wg = rows == 32 ? 12.5 + (d.k_words <= 8 ? 5.7 : 6.6) * ((len + 7) / 8)
+      const double wg = rows == 32 ? 12.0 + (d.k_words <= 8 ? 5.4 : 6.2) * ((len + 7) / 8)
                                    : 14.0 + (rows == 128 ? 1.9 : 2.85) * len;
       const long rounds = (blocks * n + 255) / 256;
       double t = static_cast<double>(rounds) * wg;
+      // Several sequences are seldom as long as the longest (the host knows only
+      // its length): half the estimate for equal lengths, half the one for
+      // lengths of 2/3 of it on average, whose workgroups follow one another
+      // without rounds.
+      if (d.batch > 1) t = std::max(wg, 0.5 * t + 0.5 * (0.65 * blocks * n / 256 * wg + 0.5 * wg));
       if (rows > 32) t += 9.0 + 2e-4 * units * nr;
-      if (beside) {
-        const long left = std::max(0l, beside->items - (rows == 32 ? rounds * 256 - blocks * n : 0));
-        t += static_cast<double>((left + 255) / 256) * beside->wg + (rows > 32 ? 5.0 : 0.0);
-      }
+      if (beside)
+        t = rows == 32 ? std::max(wg, (blocks * n * wg + beside->items * beside->wg) / 256)
+                       : t + 5.0 + static_cast<double>((beside->items + 255) / 256) * beside->wg;
       if (n > 1 && !beside) t += 4.0;
       if (n > 1 || beside) t += 2.4e-7 * kPartFloats * 4 * units * nr * n;
       if (!best.rows || t < t_best) {

@@ -388,6 +388,14 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(2, 2))
   const int t_begin = split * S.split_len;
   const int t_end = ok ? min(len, t_begin + S.split_len) : t_begin;
 
+  if (t_begin >= t_end && call.n_slots > 1) {  // no row of the sequence in this split: an empty partial
+    if (tid < kRows && r0 + tid < nr) {
+      float* P = call.part + (row_at(r0 + tid) * call.n_slots + S.slot0 + split) * kPartFloats;
+      P[0] = ok ? kNegInf : 0.f;
+      P[1] = ok ? 0.f : __builtin_nanf("");
+    }
+    return;
+  }
   const size_t row = (static_cast<size_t>(layer) * S.batch + seq) * d.n_kv + kvh;
   const size_t cap = S.capacity;
   const uint32_t* kc = S.c.k_codes + row * cap * kw;

@@ -77,6 +77,15 @@ __global__ __launch_bounds__(kAttnThreads) __attribute__((amdgpu_waves_per_eu(2,
   const int t_end = ok ? min(len, t_begin + S.split_len) : t_begin;
   const int n_kt = (max(t_end - t_begin, 0) + kKeyTile - 1) / kKeyTile;
 
+  if (t_begin >= t_end && call.n_slots > 1) {  // no row of the sequence in this split: an empty partial
+    if (r < nr && hf == 0 && (KS == 1 || wave < 4)) {
+      float* P = call.part + (row_at * call.n_slots + S.slot0 + split) * kPartFloats;
+      P[0] = ok ? kNegInf : 0.f;
+      P[1] = ok ? 0.f : __builtin_nanf("");
+    }
+    return;
+  }
+
   // query operands (B of S^T = K Q^T): dims 16 ks + 8 hf .. +7 of the row,
   // scaled, in fp16 hi and lo parts.  (The keys' radii come in at an eighth, so
   // that no product with a centroid leaves fp16's range.)
