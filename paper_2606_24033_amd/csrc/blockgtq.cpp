@@ -891,8 +891,9 @@ struct CrossPlan {
 // as long as one split.  In us, measured (kernel times in a graph):
 //   32 rows: 12 a workgroup + 5.4 (key rows of up to 8 words) or 6.2 for
 //     every 8 tiles, a tile per wave;
-//   128 rows: 14 + 1.9 a tile, 256 rows: 14 + 2.85 a tile, after a rotation
-//     launch of 9 + 1 per 5000 query rows;
+//   128 rows: 14 + 1.8 a tile, 256 rows: 14 + 2.75 a tile, up to 1.3 times as
+//     much with all CUs busy, after a rotation launch of 9 + 1 per 5000 query
+//     rows;
 //   joining: 4, and the partials written and read at 4.5 TB/s.
 // `beside`: the sequences' own pass in the same call (prefix passes).  Its
 // workgroups follow 32-row ones as these end, in one launch, and come after
@@ -909,8 +910,9 @@ static CrossPlan cross_plan(const Dims& d, int n_q, int max_len, int requested, 
     const int k1 = requested > 0 ? k0 : std::min(rows == 32 ? (tiles + 7) / 8 : tiles, 256);
     for (int k = k0; k <= std::max(k0, k1); ++k) {
       const int len = (tiles + k - 1) / k, n = (tiles + len - 1) / len;
+      const double busy = 1.0 + 0.3 * std::min(1.0, blocks * n / 256.0);
       const double wg = rows == 32 ? 12.0 + (d.k_words <= 8 ? 5.4 : 6.2) * ((len + 7) / 8)
-                                   : 14.0 + (rows == 128 ? 1.9 : 2.85) * len;
+                                   : 14.0 + (rows == 128 ? 1.8 : 2.75) * busy * len;
       const long rounds = (blocks * n + 255) / 256;
       double t = static_cast<double>(rounds) * wg;
       // Several sequences are seldom as long as the longest (the host knows only

@@ -367,13 +367,16 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(2, 2))
   const int G = d.group, hq = d.n_kv * G, kw = d.k_words;
   const int second = static_cast<int>(blockIdx.x) >= call.side[0].items;
   const CrossSide& S = call.side[second];
+  // Row blocks vary fastest and splits slowest: workgroups go to the 8 XCDs in
+  // turn, and a ragged batch's late splits, often empty, would leave some XCDs
+  // without work if the split chose the XCD.
   int item = static_cast<int>(blockIdx.x) - (second ? call.side[0].items : 0);
-  const int split = item % S.n_splits;
-  item /= S.n_splits;
   const int nr = S.n_q * G, n_blocks = (nr + kRows - 1) / kRows;
   const int r0 = item % n_blocks * kRows;
   item /= n_blocks;
-  const int kvh = item % d.n_kv, lz = item / d.n_kv;
+  const int kvh = item % d.n_kv;
+  item /= d.n_kv;
+  const int n_lz = d.n_lc * S.batch, lz = item % n_lz, split = item / n_lz;
   const int seq = lz % S.batch, layer = d.layer >= 0 ? d.layer : lz / S.batch;
   const int ri = layer * d.n_kv + kvh;
   const RowMeta* M = reinterpret_cast<const RowMeta*>(blob + kOffRows) + ri;

@@ -55,12 +55,12 @@ __global__ __launch_bounds__(kAttnThreads) __attribute__((amdgpu_waves_per_eu(2,
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int l32 = lane & 31, hf = lane >> 5;
   const int G = d.group, hq = d.n_kv * G, kw = d.k_words, nr = S.n_q * G, n_blocks = (nr + kWgRows - 1) / kWgRows;
-  int item = blockIdx.x;
-  const int split = item % S.n_splits;
-  item /= S.n_splits;
+  int item = blockIdx.x;  // (row blocks fastest, splits slowest: see k_cross)
   const int block = item % n_blocks;
   item /= n_blocks;
-  const int kvh = item % d.n_kv, lz = item / d.n_kv;
+  const int kvh = item % d.n_kv;
+  item /= d.n_kv;
+  const int n_lz = d.n_lc * S.batch, lz = item % n_lz, split = item / n_lz;
   const int seq = lz % S.batch, layer = d.layer >= 0 ? d.layer : lz / S.batch;
   const RowMeta* M = reinterpret_cast<const RowMeta*>(blob + kOffRows) + (layer * d.n_kv + kvh);
   const int nslot = (M->n_groups + 1) & ~1;

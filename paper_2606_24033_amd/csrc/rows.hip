@@ -113,23 +113,48 @@ __device__ __forceinline__ void store_operand(uint8_t* dst, int part_bytes, floa
   if constexpr (EX) *reinterpret_cast<half8_t*>(dst + part_bytes) = lo;
 }
 
+// Rows of 16 lanes: the odd ones of x change places with the even ones of y.
+__device__ __forceinline__ void swap_rows4(uint32_t (&x)[4], uint32_t (&y)[4]) {
+  asm("s_nop 1\n\t"
+      "v_permlane16_swap_b32 %0, %4\n\t"
+      "v_permlane16_swap_b32 %1, %5\n\t"
+      "v_permlane16_swap_b32 %2, %6\n\t"
+      "v_permlane16_swap_b32 %3, %7\n\t"
+      "s_nop 1"
+      : "+v"(x[0]), "+v"(x[1]), "+v"(x[2]), "+v"(x[3]), "+v"(y[0]), "+v"(y[1]), "+v"(y[2]), "+v"(y[3]));
+}
+
 // acc (lane = token l32, registers = dims 32 cc + 8 (i / 4) + 4 hf + i % 4)
-// times scale, to the token's output row (valid lanes).
+// times scale, to the output rows of the valid tokens (bit j: token j, at
+// element at0 + j stride).  A store as the registers lie has 16 bytes of a row
+// from each half-wave; lanes change places until it has 64 contiguous ones of
+// 16 rows (the memory takes 32-byte pieces at half the rate).
 template <bool EX>
-__device__ __forceinline__ void store_rows(const float16_t (&acc)[4], float scale, void* out, size_t at, int hf, bool valid) {
+__device__ __forceinline__ void store_rows(const float16_t (&acc)[4], float scale, void* out, long at0, long stride,
+                                           uint32_t valid, int lane) {
+  const int l16 = lane & 15, r1 = (lane >> 4) & 1, hf = lane >> 5;
+  const bool ok[2] = {((valid >> l16) & 1u) != 0, ((valid >> (16 + l16)) & 1u) != 0};
 #pragma unroll
   for (int cc = 0; cc < 4; ++cc) {
     float16_t y = acc[cc];
     y *= scale;
     if constexpr (EX) {
-      if (valid) {
 #pragma unroll
-        for (int u = 0; u < 4; ++u)
-          *reinterpret_cast<float4_t*>(static_cast<float*>(out) + at + 32 * cc + 8 * u + 4 * hf) =
-              float4_t{y[4 * u], y[4 * u + 1], y[4 * u + 2], y[4 * u + 3]};
+      for (int v = 0; v < 2; ++v) {  // dims 16 v .. + 15 of the block
+        uint32_t a[4], b[4];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          a[i] = __float_as_uint(y[8 * v + i]);
+          b[i] = __float_as_uint(y[8 * v + 4 + i]);
+        }
+        swap_rows4(a, b);
+        const long at = at0 + 32 * cc + 16 * v + 8 * r1 + 4 * hf;
+        if (ok[0])
+          *reinterpret_cast<uint4*>(static_cast<float*>(out) + at + l16 * stride) = make_uint4(a[0], a[1], a[2], a[3]);
+        if (ok[1])
+          *reinterpret_cast<uint4*>(static_cast<float*>(out) + at + (16 + l16) * stride) = make_uint4(b[0], b[1], b[2], b[3]);
       }
     } else {
-      // half-waves exchange, so that a lane has 8 consecutive dims: 16 u2 + 8 hf ..
       typedef __bf16 bf16x4_t __attribute__((ext_vector_type(4)));
       uint32_t a[4], b[4];
 #pragma unroll
@@ -139,13 +164,14 @@ __device__ __forceinline__ void store_rows(const float16_t (&acc)[4], float scal
         (u & 1 ? b : a)[u & ~1] = p.x;
         (u & 1 ? b : a)[u | 1] = p.y;
       }
-      swap4(a, b);
-      if (valid) {
-#pragma unroll
-        for (int u = 0; u < 2; ++u)
-          *reinterpret_cast<uint4*>(static_cast<uint16_t*>(out) + at + 32 * cc + 16 * u + 8 * hf) =
-              make_uint4(a[2 * u], a[2 * u + 1], b[2 * u], b[2 * u + 1]);
-      }
+      swap4(a, b);  // a lane has dims 8 hf .. + 7 of the block's first and second 16
+      uint32_t x[4] = {a[0], a[1], b[0], b[1]}, z[4] = {a[2], a[3], b[2], b[3]};
+      swap_rows4(x, z);
+      const long at = at0 + 32 * cc + 16 * r1 + 8 * hf;
+      if (ok[0])
+        *reinterpret_cast<uint4*>(static_cast<uint16_t*>(out) + at + l16 * stride) = make_uint4(x[0], x[1], x[2], x[3]);
+      if (ok[1])
+        *reinterpret_cast<uint4*>(static_cast<uint16_t*>(out) + at + (16 + l16) * stride) = make_uint4(z[0], z[1], z[2], z[3]);
     }
   }
 }
@@ -265,12 +291,15 @@ __device__ __forceinline__ void read_keys(uint8_t* smem, const Dims& d, const ui
   const uint32_t* kc = call.c.k_codes + row * cap * kw;
   const uint16_t* kn = call.c.k_norms + row * kMaxGroups * cap;
   const int n_tiles = (call.n_rows + 63) / 64, first = chunk * call.tiles[0];
-  for (int tile = first + wave; tile < min(n_tiles, first + call.tiles[0]); tile += kWaves) {
+  const int last = min(n_tiles, first + call.tiles[0]);
+  uint32_t nw[KWB], next_radii[4];
+  bool next_valid;
+  // a tile's words, a tile ahead (past the last one, row 0 again: in bounds, for nobody)
+  const auto load = [&](int tile) {
     const int i = tile * 64 + lane;
     const long t = pos + i;
-    const bool valid = i < call.n_rows && t >= 0 && t < end;
-    const size_t tr = valid ? static_cast<size_t>(t) : 0;  // (any row of the cache: its result is not stored)
-    uint32_t nw[KWB], rw[KWB + split_detail::kRowPad], radii[4];
+    next_valid = tile < last && i < call.n_rows && t >= 0 && t < end;
+    const size_t tr = next_valid ? static_cast<size_t>(t) : 0;  // (any row of the cache: its result is not stored)
     const uint32_t* src = kc + tr * kw;
     if ((kw & 3) == 0) {
 #pragma unroll
@@ -285,20 +314,22 @@ __device__ __forceinline__ void read_keys(uint8_t* smem, const Dims& d, const ui
 #pragma unroll
       for (int k = 0; k < KWB; ++k) nw[k] = k < kw ? src[k] : 0u;
     }
+    // (a token's 16 bytes of radii stay inside the row's 8 slots per token)
+    const uint32_t* r = reinterpret_cast<const uint32_t*>(kn + tr * nslot);
 #pragma unroll
-    for (int k = 0; k < KWB; ++k) {
-      // (one word at a time: as merged vector stores the indexed array would live in scratch memory)
-      asm volatile("" : "+v"(nw[k]));
-      rw[k] = nw[k];
-    }
+    for (int k = 0; k < 4; ++k) next_radii[k] = r[k];
+  };
+  load(first + wave);
+  for (int tile = first + wave; tile < last; tile += kWaves) {
+    uint32_t rw[KWB + split_detail::kRowPad], radii[4];
+#pragma unroll
+    for (int k = 0; k < KWB; ++k) rw[k] = nw[k];
 #pragma unroll
     for (int k = KWB; k < KWB + split_detail::kRowPad; ++k) rw[k] = 0u;
-    {
-      // (a token's 16 bytes of radii stay inside the row's 8 slots per token)
-      const uint32_t* r = reinterpret_cast<const uint32_t*>(kn + tr * nslot);
 #pragma unroll
-      for (int k = 0; k < 4; ++k) radii[k] = r[k];
-    }
+    for (int k = 0; k < 4; ++k) radii[k] = next_radii[k];
+    const bool valid = next_valid;
+    load(tile + kWaves);
     // 2^up brings the token's largest radius to [2^12, 2^13)
     uint32_t top = 0;
 #pragma unroll
@@ -321,21 +352,24 @@ __device__ __forceinline__ void read_keys(uint8_t* smem, const Dims& d, const ui
     for (int n = 0; n < 2; ++n) {
       // lane = token 32 n + l32 of the tile
       const float scale = __shfl(down, 32 * n + l32);
-      const size_t at = ((static_cast<size_t>(lz) * call.n_rows + tile * 64 + 32 * n + l32) * d.n_kv + kvh) * kHeadDim;
-      store_rows<EX>(acc[n], scale, call.out[0], at, hf, (ok >> (32 * n + l32)) & 1u);
+      const long at = ((static_cast<long>(lz) * call.n_rows + tile * 64 + 32 * n) * d.n_kv + kvh) * kHeadDim;
+      store_rows<EX>(acc[n], scale, call.out[0], at, static_cast<long>(d.n_kv) * kHeadDim,
+                     static_cast<uint32_t>(ok >> (32 * n)), lane);
     }
   }
 }
 
 // ---------------------------------------------------------------- values
+// A tile's codes (words of dims lane and 64 + lane) as fp16 centroids in LDS,
+// token after token.
 template <int BV>
-__device__ __forceinline__ void decode_values(const uint8_t* smem, uint8_t* tile, const uint32_t* __restrict__ src, int lane) {
+__device__ __forceinline__ void decode_values(const uint8_t* smem, uint8_t* tile, const uint32_t (&words)[2][BV], int lane) {
 #pragma unroll
   for (int h = 0; h < 2; ++h) {
     const int dim = 64 * h + lane;
     uint32_t w[BV + 1];
 #pragma unroll
-    for (int i = 0; i < BV; ++i) w[i] = src[dim * BV + i];
+    for (int i = 0; i < BV; ++i) w[i] = words[h][i];
     w[BV] = 0;
     const half2_t y[16] = {pair_at<BV, 0>(smem, w),       pair_at<BV, 2 * BV>(smem, w),  pair_at<BV, 4 * BV>(smem, w),
                            pair_at<BV, 6 * BV>(smem, w),  pair_at<BV, 8 * BV>(smem, w),  pair_at<BV, 10 * BV>(smem, w),
@@ -351,10 +385,67 @@ __device__ __forceinline__ void decode_values(const uint8_t* smem, uint8_t* tile
   }
 }
 
+// The wave's tiles first, first + 8, .. below last, of cache tiles that hold a
+// row below end; the next one's words are in flight.
+template <bool EX, int BV>
+__device__ __forceinline__ void value_tiles(const uint8_t* smem, uint8_t* mine, const Dims& d, const RowsCall& call,
+                                            const uint32_t* __restrict__ vc, const uint16_t* __restrict__ vn, long first,
+                                            long last, long pos, int end, int lz, int kvh, int lane) {
+  const int l32 = lane & 31, hf = lane >> 5;
+  uint32_t w[2][BV];
+  uint16_t radius;
+  const auto load = [&](long tile) {
+    const size_t t = static_cast<size_t>(tile < last && tile >= 0 && tile * kTile < end ? tile : 0);  // (else for nobody)
+    const uint32_t* src = vc + t * kHeadDim * BV;
+#pragma unroll
+    for (int h = 0; h < 2; ++h)
+#pragma unroll
+      for (int i = 0; i < BV; ++i) w[h][i] = src[(64 * h + lane) * BV + i];
+    radius = vn[t * kTile + l32];
+  };
+  load(first);
+  for (long tile = first; tile < last; tile += kWaves) {
+    if (tile < 0 || tile * kTile >= end) {  // uniform
+      load(tile + kWaves);
+      continue;
+    }
+    const long t = tile * kTile + l32;
+    const float scale = static_cast<float>(__builtin_bit_cast(_Float16, radius)) / kMatScale;
+    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");  // the last tile's reads come before this one's writes
+    decode_values<BV>(smem, mine, w, lane);
+    load(tile + kWaves);
+    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");  // a wave's LDS operations complete in order
+    __builtin_amdgcn_wave_barrier();
+    float16_t acc[4];
+#pragma unroll
+    for (int cc = 0; cc < 4; ++cc)
+#pragma unroll
+      for (int k = 0; k < 16; ++k) acc[cc][k] = 0.f;
+#pragma unroll
+    for (int st = 0; st < kVSteps; ++st) {
+      const half8_t y = *reinterpret_cast<const half8_t*>(mine + l32 * kTileStride + 32 * st + 16 * hf);
+      const uint8_t* mat = smem + kMat + st * 4096 + lane * 16;
+#pragma unroll
+      for (int cc = 0; cc < 4; ++cc)
+        acc[cc] = __builtin_amdgcn_mfma_f32_32x32x16_f16(*reinterpret_cast<const half8_t*>(mat + cc * 1024), y, acc[cc], 0, 0, 0);
+      if constexpr (EX) {
+#pragma unroll
+        for (int cc = 0; cc < 4; ++cc)
+          acc[cc] = __builtin_amdgcn_mfma_f32_32x32x16_f16(
+              *reinterpret_cast<const half8_t*>(mat + kVSteps * 4096 + cc * 1024), y, acc[cc], 0, 0, 0);
+      }
+    }
+    const long i = t - pos;
+    const unsigned long long ok = __builtin_amdgcn_ballot_w64(i >= 0 && i < call.n_rows && t < end);
+    const long at = ((static_cast<long>(lz) * call.n_rows + tile * kTile - pos) * d.n_kv + kvh) * kHeadDim;
+    store_rows<EX>(acc, scale, call.out[1], at, static_cast<long>(d.n_kv) * kHeadDim, static_cast<uint32_t>(ok), lane);
+  }
+}
+
 template <bool EX>
 __device__ __forceinline__ void read_values(uint8_t* smem, const Dims& d, const uint8_t* __restrict__ blob,
                                             const RowsCall& call, int lz, int kvh, int chunk, long pos, int end) {
-  const int tid = threadIdx.x, lane = tid & 63, l32 = lane & 31, hf = lane >> 5;
+  const int tid = threadIdx.x, lane = tid & 63;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int layer = d.layer >= 0 ? d.layer : lz / d.batch, seq = lz % d.batch;
   // A[dim][j] = 2^8 / sqrt(128) Pi_V[j][dim], read from the transposed Pi_V
@@ -377,48 +468,19 @@ __device__ __forceinline__ void read_values(uint8_t* smem, const Dims& d, const 
   uint8_t* const mine = smem + kMat + (EX ? 2 : 1) * kVSteps * 4096 + wave * kTileBytes;
   // cache tiles from the one that holds the first row
   const long tile0 = pos >> 5, tile_end = (pos + call.n_rows + kTile - 1) >> 5;
-  for (long tile = tile0 + chunk * call.tiles[1] + wave; tile < min(tile_end, tile0 + (chunk + 1l) * call.tiles[1]); tile += kWaves) {
-    if (tile < 0 || tile * kTile >= end) continue;  // uniform
-    const uint32_t* src = vc + static_cast<size_t>(tile) * kHeadDim * bv;
-    const long t = tile * kTile + l32;
-    const uint16_t radius = vn[t];
-    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");  // the last tile's reads come before this one's writes
-    switch (bv) {
-      case 1: decode_values<1>(smem, mine, src, lane); break;
-      case 2: decode_values<2>(smem, mine, src, lane); break;
-      case 3: decode_values<3>(smem, mine, src, lane); break;
-      case 4: decode_values<4>(smem, mine, src, lane); break;
-      case 5: decode_values<5>(smem, mine, src, lane); break;
-      case 6: decode_values<6>(smem, mine, src, lane); break;
-      case 7: decode_values<7>(smem, mine, src, lane); break;
-      default: decode_values<8>(smem, mine, src, lane); break;
-    }
-    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");  // a wave's LDS operations complete in order
-    __builtin_amdgcn_wave_barrier();
-    float16_t acc[4];
-#pragma unroll
-    for (int cc = 0; cc < 4; ++cc)
-#pragma unroll
-      for (int k = 0; k < 16; ++k) acc[cc][k] = 0.f;
-#pragma unroll
-    for (int st = 0; st < kVSteps; ++st) {
-      const half8_t y = *reinterpret_cast<const half8_t*>(mine + l32 * kTileStride + 32 * st + 16 * hf);
-      const uint8_t* mat = smem + kMat + st * 4096 + lane * 16;
-#pragma unroll
-      for (int cc = 0; cc < 4; ++cc)
-        acc[cc] = __builtin_amdgcn_mfma_f32_32x32x16_f16(*reinterpret_cast<const half8_t*>(mat + cc * 1024), y, acc[cc], 0, 0, 0);
-      if constexpr (EX) {
-#pragma unroll
-        for (int cc = 0; cc < 4; ++cc)
-          acc[cc] = __builtin_amdgcn_mfma_f32_32x32x16_f16(
-              *reinterpret_cast<const half8_t*>(mat + kVSteps * 4096 + cc * 1024), y, acc[cc], 0, 0, 0);
-      }
-    }
-    const float scale = static_cast<float>(__builtin_bit_cast(_Float16, radius)) / kMatScale;
-    const long i = t - pos;
-    const bool valid = i >= 0 && i < call.n_rows && t < end;
-    const size_t at = ((static_cast<size_t>(lz) * call.n_rows + (valid ? i : 0)) * d.n_kv + kvh) * kHeadDim;
-    store_rows<EX>(acc, scale, call.out[1], at, hf, valid);
+  const long at = tile0 + chunk * static_cast<long>(call.tiles[1]), last = min(tile_end, at + call.tiles[1]);
+  const auto go = [&](auto b) __attribute__((always_inline)) {
+    value_tiles<EX, decltype(b)::value>(smem, mine, d, call, vc, vn, at + wave, last, pos, end, lz, kvh, lane);
+  };
+  switch (bv) {
+    case 1: go(std::integral_constant<int, 1>{}); break;
+    case 2: go(std::integral_constant<int, 2>{}); break;
+    case 3: go(std::integral_constant<int, 3>{}); break;
+    case 4: go(std::integral_constant<int, 4>{}); break;
+    case 5: go(std::integral_constant<int, 5>{}); break;
+    case 6: go(std::integral_constant<int, 6>{}); break;
+    case 7: go(std::integral_constant<int, 7>{}); break;
+    default: go(std::integral_constant<int, 8>{}); break;
   }
 }
 
