@@ -50,7 +50,8 @@ constexpr int kBooks = 0;
 constexpr int kPair = 1024;
 constexpr int kMaxPair = 6;
 __host__ __device__ constexpr int pair_offset(int b) { return kPair + 4 * (((1 << (2 * b)) - 4) / 3); }
-constexpr int kMat = (pair_offset(kMaxPair + 1) + 15) / 16 * 16;
+constexpr int kDims = pair_offset(kMaxPair + 1);  // a key row's stream position -> dim
+constexpr int kMat = (kDims + kHeadDim + 15) / 16 * 16;
 constexpr int kVSteps = kHeadDim / 16;
 constexpr int kTileStride = (kHeadDim + 8) * 2;  // bytes of a decoded token
 constexpr int kTileBytes = kTile * kTileStride;
@@ -95,6 +96,21 @@ __device__ __forceinline__ void swap4(uint32_t (&x)[4], uint32_t (&y)[4]) {
 }
 __device__ __forceinline__ half8_t as_half8(const uint32_t (&x)[4]) {
   return __builtin_bit_cast(half8_t, make_uint4(x[0], x[1], x[2], x[3]));
+}
+
+// Pair tables of the widths in `used` (bit b - 1).
+__device__ __forceinline__ void build_pairs(uint8_t* smem, uint32_t used, int tid) {
+  const uint16_t* cbs = reinterpret_cast<const uint16_t*>(smem + kBooks);
+#pragma unroll
+  for (int b = 1; b <= kMaxPair; ++b)
+    if ((used >> (b - 1)) & 1u)
+#pragma unroll
+      for (int i0 = 0; i0 < (1 << (2 * b)); i0 += kThreads) {
+        const int i = i0 + tid;
+        if ((1 << (2 * b)) >= kThreads || i < (1 << (2 * b)))
+          *reinterpret_cast<uint32_t*>(smem + pair_offset(b) + 4 * i) =
+              cbs[cb_index(b) + (i & ((1 << b) - 1))] | (static_cast<uint32_t>(cbs[cb_index(b) + (i >> b)]) << 16);
+      }
 }
 
 // One operand of the matrix: 8 numbers, rounded (and their residuals).
@@ -193,6 +209,15 @@ __device__ __forceinline__ void key_group(const uint8_t* smem, const uint32_t (&
     const half2_t y[8] = {pair_at<B, 0>(smem, aw),      pair_at<B, 2 * B>(smem, aw),  pair_at<B, 4 * B>(smem, aw),
                           pair_at<B, 6 * B>(smem, aw),  pair_at<B, 8 * B>(smem, aw),  pair_at<B, 10 * B>(smem, aw),
                           pair_at<B, 12 * B>(smem, aw), pair_at<B, 14 * B>(smem, aw)};
+    // the step's matrix operands, in flight with the lookups
+    const uint8_t* mat = smem + kMat + (step0 + c) * 4096 + lane * 16;
+    half8_t ops[4], lows[4];
+#pragma unroll
+    for (int cc = 0; cc < 4; ++cc) {
+      ops[cc] = *reinterpret_cast<const half8_t*>(mat + cc * 1024);
+      if constexpr (EX) lows[cc] = *reinterpret_cast<const half8_t*>(mat + kMaxSteps * 4096 + cc * 1024);
+    }
+    __builtin_amdgcn_sched_barrier(0);
     uint32_t hi[2][4], lo[2][4];
 #pragma unroll
     for (int u = 0; u < 8; ++u) {
@@ -202,14 +227,13 @@ __device__ __forceinline__ void key_group(const uint8_t* smem, const uint32_t (&
     }
     swap4(hi[0], hi[1]);
     if constexpr (EX) swap4(lo[0], lo[1]);
-    const uint8_t* mat = smem + kMat + (step0 + c) * 4096 + lane * 16;
 #pragma unroll
     for (int cc = 0; cc < 4; ++cc) {
-      const half8_t w = *reinterpret_cast<const half8_t*>(mat + cc * 1024);
+      const half8_t w = ops[cc];
 #pragma unroll
       for (int n = 0; n < 2; ++n) acc[n][cc] = __builtin_amdgcn_mfma_f32_32x32x16_f16(w, as_half8(hi[n]), acc[n][cc], 0, 0, 0);
       if constexpr (EX) {
-        const half8_t wl = *reinterpret_cast<const half8_t*>(mat + kMaxSteps * 4096 + cc * 1024);
+        const half8_t wl = lows[cc];
 #pragma unroll
         for (int n = 0; n < 2; ++n) acc[n][cc] = __builtin_amdgcn_mfma_f32_32x32x16_f16(w, as_half8(lo[n]), acc[n][cc], 0, 0, 0);
 #pragma unroll
@@ -238,54 +262,20 @@ __device__ __forceinline__ void key_groups(std::integer_sequence<int, BM1...>, c
 template <int KWB, bool EX>
 __device__ __forceinline__ void read_keys(uint8_t* smem, const Dims& d, const uint8_t* __restrict__ blob,
                                           const RowsCall& call, int lz, int kvh, int chunk, long pos, int end) {
-  const int tid = threadIdx.x, lane = tid & 63, l32 = lane & 31, hf = lane >> 5;
+  const int tid = threadIdx.x, lane = tid & 63, l32 = lane & 31;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int layer = d.layer >= 0 ? d.layer : lz / d.batch, seq = lz % d.batch, ri = layer * d.n_kv + kvh;
   const RowMeta* M = reinterpret_cast<const RowMeta*>(blob + kOffRows) + ri;
   const int ng = M->n_groups, nslot = (ng + 1) & ~1, kw = d.k_words;
-  uint32_t gm[8];
+  uint32_t gm[8], used = 0;
+  int gd[8], gp[8];
 #pragma unroll
-  for (int b = 0; b < 8; ++b) gm[b] = M->gm[b];
-
-  // ---- the matrix A[dim][p] = 2^8 / sqrt(d_g) Pi_g[p - p_g][index of dim in
-  // g], zero for dims of other groups and past a group's end; operand (step,
-  // dim block cc, lane) = dim 32 cc + lane % 32, positions 8 (lane / 32) .. + 7
-  // of the step.  The row's slot of the layout holds each Pi_g transposed.
-  {
-    const float* rot = reinterpret_cast<const float*>(blob + layout_rowrot_offset(d.n_layers * d.n_kv)) +
-                       static_cast<size_t>(ri) * kRowRotFloats;
-    uint8_t* inv = smem + kMat;  // dim -> stream position, until the matrix is built
-    if (tid < kHeadDim) inv[M->dim[tid]] = static_cast<uint8_t>(tid);
-    __syncthreads();
-    const int my = inv[tid & 127];  // (a thread always has the same dim: 512 is a multiple of 128)
-    __syncthreads();
-    // thread = (dim tid % 128, half and step parity tid / 128); the operands of
-    // steps tid / 256, + 2, ...
-    const int dim = tid & 127, h8 = (tid >> 7) & 1;
-    int st0 = 0, off = 0;
-#pragma unroll 1
-    for (int g = 0; g < ng; ++g) {
-      const int dg = M->g_dim[g], p0 = M->g_pos[g], n16 = (dg + 15) >> 4;
-      const float scale = kMatScale * rsqrtf(static_cast<float>(dg));
-      const bool mine = my >= p0 && my < p0 + dg;
-      const float* src = rot + off + (mine ? my - p0 : 0) * dg;
-      for (int st = tid >> 8; st < n16; st += 2) {
-        const int j0 = 16 * st + 8 * h8;
-        float x[8];
-#pragma unroll
-        for (int j = 0; j < 8; j += 2) {  // (group sizes are even, and so are the blocks' offsets)
-          const float2_t v = mine && j0 + j < dg ? *reinterpret_cast<const float2_t*>(src + j0 + j) : float2_t{0.f, 0.f};
-          x[j] = v[0] * scale;
-          x[j + 1] = v[1] * scale;
-        }
-        store_operand<EX>(smem + kMat + (st0 + st) * 4096 + (dim >> 5) * 1024 + (h8 * 32 + (dim & 31)) * 16, kMaxSteps * 4096, x);
-      }
-      st0 += n16;
-      off += dg * dg;
-    }
+  for (int b = 0; b < 8; ++b) {
+    gm[b] = M->gm[b];
+    used |= (gm[b] >> 31) << b;
+    gd[b] = b < ng ? M->g_dim[b] : 0;
+    gp[b] = M->g_pos[b];
   }
-  __syncthreads();
-
   const size_t row = (static_cast<size_t>(layer) * d.batch + seq) * d.n_kv + kvh;
   const size_t cap = d.capacity;
   const uint32_t* kc = call.c.k_codes + row * cap * kw;
@@ -320,6 +310,66 @@ __device__ __forceinline__ void read_keys(uint8_t* smem, const Dims& d, const ui
     for (int k = 0; k < 4; ++k) next_radii[k] = r[k];
   };
   load(first + wave);
+
+  // ---- the matrix A[dim][p] = 2^8 / sqrt(d_g) Pi_g[p - p_g][index of dim in
+  // g], zero for dims of other groups and past a group's end; operand (step,
+  // dim block cc, lane) = dim 32 cc + lane % 32, positions 8 (lane / 32) .. + 7
+  // of the step.  The row's slot of the layout holds each Pi_g transposed.
+  // Item = 8 numbers of one Pi_g, in memory order (dim after dim, contiguous
+  // reads); the rest of the matrix is cleared.
+  {
+    const float* rot = reinterpret_cast<const float*>(blob + layout_rowrot_offset(d.n_layers * d.n_kv)) +
+                       static_cast<size_t>(ri) * kRowRotFloats;
+    const uint16_t* c16 = reinterpret_cast<const uint16_t*>(blob + kOffC16);
+    const uint16_t cv = c16[min(tid, kCodebookEntries - 1)];
+    const uint8_t dv = M->dim[tid & 127];
+    int n_steps = 0, n_items = 0;
+#pragma unroll
+    for (int g = 0; g < 8; ++g) {
+      n_steps += (gd[g] + 15) >> 4;
+      n_items += gd[g] * 2 * ((gd[g] + 15) >> 4);
+    }
+    if (tid < kCodebookEntries) reinterpret_cast<uint16_t*>(smem + kBooks)[tid] = cv;
+    for (int i = tid; i < n_steps * 256; i += kThreads) {
+      *reinterpret_cast<uint4*>(smem + kMat + i * 16) = make_uint4(0, 0, 0, 0);
+      if constexpr (EX) *reinterpret_cast<uint4*>(smem + kMat + kMaxSteps * 4096 + i * 16) = make_uint4(0, 0, 0, 0);
+    }
+    if (tid < kHeadDim) smem[kDims + tid] = dv;
+    __syncthreads();
+    build_pairs(smem, used, tid);
+    for (int i0 = tid; i0 < n_items; i0 += kThreads) {
+      int left = i0, dg = 2, p0 = 0, at = 0, st = 0, off = 0, base = 0;
+      bool found = false;
+#pragma unroll
+      for (int g = 0; g < 8; ++g) {
+        const int n16 = (gd[g] + 15) >> 4, n = gd[g] * 2 * n16;
+        if (!found && left < n) {
+          found = true;
+          dg = gd[g];
+          p0 = gp[g];
+          at = off;
+          st = base;
+        }
+        if (!found) left -= n;
+        off += gd[g] * gd[g];
+        base += n16;
+      }
+      const int per = 2 * ((dg + 15) >> 4), k = left / per, j0 = 8 * (left - k * per), dim = smem[kDims + p0 + k];
+      const float* src = rot + at + k * dg + j0;
+      const float scale = kMatScale * rsqrtf(static_cast<float>(dg));
+      float x[8];
+#pragma unroll
+      for (int j = 0; j < 8; j += 2) {  // (group sizes are even, and so are the blocks' offsets)
+        const float2_t v = j0 + j < dg ? *reinterpret_cast<const float2_t*>(src + j) : float2_t{0.f, 0.f};
+        x[j] = v[0] * scale;
+        x[j + 1] = v[1] * scale;
+      }
+      store_operand<EX>(smem + kMat + (st + (j0 >> 4)) * 4096 + (dim >> 5) * 1024 + (((j0 >> 3) & 1) * 32 + (dim & 31)) * 16,
+                        kMaxSteps * 4096, x);
+    }
+  }
+  __syncthreads();
+
   for (int tile = first + wave; tile < last; tile += kWaves) {
     uint32_t rw[KWB + split_detail::kRowPad], radii[4];
 #pragma unroll
@@ -450,13 +500,27 @@ __device__ __forceinline__ void read_values(uint8_t* smem, const Dims& d, const 
   const int layer = d.layer >= 0 ? d.layer : lz / d.batch, seq = lz % d.batch;
   // A[dim][j] = 2^8 / sqrt(128) Pi_V[j][dim], read from the transposed Pi_V
   {
+    const uint16_t* c16 = reinterpret_cast<const uint16_t*>(blob + kOffC16);
+    const uint16_t cv = c16[min(tid, kCodebookEntries - 1)];
     const float* rot = reinterpret_cast<const float*>(blob + kOffRotVT);
-    for (int it = tid; it < kVSteps * 4 * 64; it += kThreads) {
-      const int l = it & 63, cc = (it >> 6) & 3, st = it >> 8;
+    constexpr int kPer = kVSteps * 4 * 64 / kThreads;
+    float4_t v[kPer][2];
+#pragma unroll
+    for (int u = 0; u < kPer; ++u) {
+      const int it = tid + u * kThreads, l = it & 63, cc = (it >> 6) & 3, st = it >> 8;
       const float4_t* src = reinterpret_cast<const float4_t*>(rot + (32 * cc + (l & 31)) * kHeadDim + 16 * st + 8 * (l >> 5));
-      const float4_t a = src[0] * (kMatScale * 0.08838834764831845f), b = src[1] * (kMatScale * 0.08838834764831845f);
-      float x[8] = {a[0], a[1], a[2], a[3], b[0], b[1], b[2], b[3]};
-      store_operand<EX>(smem + kMat + it * 16, kVSteps * 4096, x);
+      v[u][0] = src[0];
+      v[u][1] = src[1];
+    }
+    if (tid < kCodebookEntries) reinterpret_cast<uint16_t*>(smem + kBooks)[tid] = cv;
+    __syncthreads();
+    build_pairs(smem, 1u << (d.v_bits - 1), tid);
+#pragma unroll
+    for (int u = 0; u < kPer; ++u) {
+      float x[8];
+#pragma unroll
+      for (int j = 0; j < 8; ++j) x[j] = v[u][j >> 2][j & 3] * (kMatScale * 0.08838834764831845f);
+      store_operand<EX>(smem + kMat + (tid + u * kThreads) * 16, kVSteps * 4096, x);
     }
   }
   __syncthreads();
@@ -489,7 +553,6 @@ template <int KWB, bool EX>
 __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(2, 2))) void k_read_rows(
     Dims d, const uint8_t* __restrict__ blob, RowsCall call) {
   __shared__ __attribute__((aligned(16))) uint8_t smem[lds_bytes<EX>()];
-  const int tid = threadIdx.x;
   const bool keys = static_cast<int>(blockIdx.x) < call.key_items;
   int item = static_cast<int>(blockIdx.x) - (keys ? 0 : call.key_items);
   const int chunks = keys ? call.chunks[0] : call.chunks[1];
@@ -498,19 +561,6 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(2, 2))
   const int kvh = item % d.n_kv, lz = item / d.n_kv, seq = lz % d.batch;
   const long pos = call.read_pos[seq];
   const int end = min(d.capacity, call.ctx_len ? call.ctx_len[seq] : d.capacity);
-  // codebooks and pair tables
-  {
-    const uint16_t* c16 = reinterpret_cast<const uint16_t*>(blob + kOffC16);
-    uint16_t* cbs = reinterpret_cast<uint16_t*>(smem + kBooks);
-    for (int i = tid; i < kCodebookEntries; i += kThreads) cbs[i] = c16[i];
-    __syncthreads();
-#pragma unroll
-    for (int b = 1; b <= kMaxPair; ++b)
-      if (keys || b == d.v_bits)
-        for (int i = tid; i < (1 << (2 * b)); i += kThreads)
-          *reinterpret_cast<uint32_t*>(smem + pair_offset(b) + 4 * i) =
-              cbs[cb_index(b) + (i & ((1 << b) - 1))] | (static_cast<uint32_t>(cbs[cb_index(b) + (i >> b)]) << 16);
-  }
   if (keys) read_keys<KWB, EX>(smem, d, blob, call, lz, kvh, chunk, pos, end);
   else read_values<EX>(smem, d, blob, call, lz, kvh, chunk, pos, end);
 }
@@ -528,13 +578,14 @@ hipError_t launch_dequantize_rows(const Dims& d, const void* layout, const Cache
   call.out[1] = v_out;
   call.n_rows = n_rows;
   // One workgroup per CU: 256 of them share the units' tiles, a multiple of 8
-  // (a tile per wave) each.
+  // (a tile per wave) each; of both sides' the keys get 9 / 16 (65536 rows x 8
+  // heads, one side alone on all CUs: keys 46 us, values 38).
   const long units = static_cast<long>(d.n_kv) * d.n_lc * d.batch;
-  const long sides = (k_out ? 1 : 0) + (v_out ? 1 : 0);
+  const bool both = k_out && v_out;
   long items = 0;
   for (int k = 0; k < 2; ++k) {
     const long n = k == 0 ? (n_rows + 63l) / 64 : (n_rows + 2l * kTile - 2) / kTile;  // (unaligned rows reach one tile more)
-    const long want = std::max(1l, 256 / std::max(1l, units * sides));
+    const long want = std::max(1l, (both ? (k == 0 ? 144 : 112) : 256) / std::max(1l, units));
     call.tiles[k] = static_cast<int>(((n + want - 1) / want + kWaves - 1) / kWaves * kWaves);
     call.chunks[k] = static_cast<int>((n + call.tiles[k] - 1) / call.tiles[k]);
     if (call.out[k]) items += units * call.chunks[k];
