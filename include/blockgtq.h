@@ -384,8 +384,9 @@ int blockgtq_cross_attn(const bgtq_config* cfg, const void* d_layout, int32_t la
  * sequence, and each sequence's own rows follow in `cache`.  Every query
  * attends rows [0, *d_prefix_len) of the prefix and then rows
  * [0, d_ctx_len[b]) of its own, under one softmax.  The prefix's rows are read
- * and decoded for all the sequences' queries together.  No allocation, no
- * state in the workspace, so the call can be captured in a HIP graph.
+ * and decoded for all the sequences' queries together.  Up to four launches on
+ * `stream`; no allocation, no state in the workspace, so the call can be
+ * captured in a HIP graph.
  * Keys are post-RoPE: sequence b's own row t was rotated at its position
  * (*d_prefix_len + t in the usual case) by the caller.
  * d_layout: one layout for both caches (it does not depend on batch or

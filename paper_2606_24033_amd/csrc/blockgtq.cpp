@@ -870,8 +870,8 @@ int blockgtq_dequantize_rows(const bgtq_config* cfg, const void* d_layout, int32
   if (!d_k_out && !d_v_out) return fail(BGTQ_EINVAL, "k_out and v_out are both NULL");
   if (!aligned16(d_k_out) || !aligned16(d_v_out)) return fail(BGTQ_EINVAL, "k_out and v_out must be 16-byte aligned");
   const long lz = static_cast<long>(layer < 0 ? cfg->n_layers : 1) * cfg->batch;
-  if (lz > 65535 || cfg->n_kv_heads > 65535 || (n_rows + 15l) / 16 * cfg->n_kv_heads * lz > kMaxItems * 4)
-    return fail(BGTQ_EUNSUPPORTED, "%d rows of %ld x %d heads in one call", n_rows, lz, cfg->n_kv_heads);
+  if (2.0 * lz * cfg->n_kv_heads > static_cast<double>(kMaxItems))  // (a workgroup for each head's keys and values at least)
+    return fail(BGTQ_EUNSUPPORTED, "%ld x %d heads in one call", lz, cfg->n_kv_heads);
   hipError_t e = launch_dequantize_rows(dims_of(cfg, layer), d_layout, cache_ptrs(cache), n_rows, d_read_pos,
                                         d_ctx_len, d_k_out, d_v_out, out_dtype, static_cast<hipStream_t>(stream));
   if (e != hipSuccess) return hip_fail(e, "dequantize_rows launch");

@@ -344,6 +344,85 @@ def test_cross_one_query_row_is_the_decode(rotations):
     assert err <= P.tol_attention(), err
 
 
+# ---------------------------------------------------------------- many query rows
+
+WIDE = [
+    # layers, batch, kv, group, k_budget, v_bits, kind, in, out, n_q, lens, cap, n_splits; sizes that take the passes with
+    # 128 or 256 query rows to a workgroup (the workspace then holds the rotated queries)
+    (1, 1, 8, 4, 128, 2, "mixed", "bf16", "bf16", 2048, [515], 576, 0),
+    (1, 1, 8, 4, 192, 3, "wide", "bf16", "fp32", 2048, [512], 512, 0),
+    (1, 1, 2, 8, 192, 3, "mixed", "bf16", "bf16", 2048, [513], 576, 0),
+    (1, 1, 2, 8, 128, 4, "wide", "fp32", "fp32", 2047, [449], 512, 0),
+    (2, 1, 2, 8, 128, 2, "mixed", "fp32", "fp32", 1500, [576], 576, 0),
+    (1, 3, 4, 8, 256, 1, "uniform", "bf16", "fp32", 1001, [600, 0, 64], 640, 0),
+    (1, 2, 8, 4, 320, 7, "wide", "bf16", "bf16", 1100, [577, 250], 640, 3),
+    (1, 2, 8, 4, 512, 8, "uniform", "fp32", "fp32", 1100, [300, 577], 640, 2),
+    (1, 1, 8, 5, 448, 6, "wide", "bf16", "bf16", 1700, [700], 704, 2),
+    (1, 1, 8, 3, 128, 5, "mixed", "bf16", "fp32", 2731, [640], 640, 2),
+    (1, 2, 2, 1, 128, 2, "wide", "fp32", "fp32", 400, [513, 70], 576, 6),
+    (1, 2, 4, 5, 192, 3, "mixed", "bf16", "bf16", 40, [513, 0], 576, 6),
+    (1, 2, 2, 4, 256, 1, "uniform", "bf16", "bf16", 100, [1, 513], 576, 6),
+    (1, 1, 4, 3, 512, 8, "uniform", "fp32", "fp32", 150, [640], 640, 6),
+]
+
+
+@pytest.mark.parametrize("layers,batch,kv,group,k_budget,v_bits,kind,tin,tout,n_q,lens,cap,n_splits", WIDE)
+def test_cross_attention_of_many_query_rows(rotations, layers, batch, kv, group, k_budget, v_bits, kind, tin, tout, n_q,
+                                            lens, cap, n_splits):
+    dt = torch.bfloat16 if tout == "bf16" else torch.float32
+    pk = Packed(rotations, 71, layers=layers, batch=batch, kv=kv, group=group, cap=cap, k_budget=k_budget, v_bits=v_bits,
+                kind=kind, dtype=tin, behind=float("nan"), lens=lens)
+    assert bg.cross_workspace_bytes(pk.cfg, layers, n_q, n_splits, max(lens)) >= layers * batch * n_q * kv * group * 512
+    q, qd = pk.queries((layers, batch, n_q))
+    # positions whose rows are compared: the ends, the edges of workgroups, and some between
+    at = sorted({0, 1, n_q - 1, *(min(n_q - 1, (r + d) // group) for r in (32, 128, 256, 512) for d in (-1, 0)),
+                 *(int(i) for i in np.random.default_rng(3).integers(0, n_q, 9))})
+    ref, bound = expect_cross(pk, q[:, :, at], lens, dt)
+    if layers > 1:
+        out = bg.blockgtq_cross_attn(pk.cfg, pk.layout, -1, qd, i32(lens), max(lens), pk.cache, n_splits=n_splits, out_dtype=dt)
+    else:
+        out = bg.blockgtq_cross_attn(pk.cfg, pk.layout, 0, qd[0], i32(lens), max(lens), pk.cache, n_splits=n_splits,
+                                     out_dtype=dt)[None]
+    check("compared rows", out[:, :, at], ref, bound)
+    if dt == torch.float32:  # every other row against the 32-row passes (a few query rows to a call)
+        few = bg.blockgtq_cross_attn(pk.cfg, pk.layout, 0, qd[0, :, :7].contiguous(), i32(lens), max(lens), pk.cache)
+        err = float((out[0, :, :7] - few).norm() / few.norm())
+        assert err <= 1e-5, err
+
+
+def test_many_query_rows_lengths_outside_the_bound_and_odd_queries(rotations):
+    pk = Packed(rotations, 72, batch=4, kv=8, group=4, cap=640, dtype="fp32")
+    lens, n_q = [600, 601, -3, 0], 600
+    assert bg.cross_workspace_bytes(pk.cfg, 1, n_q, 0, 600) >= 4 * n_q * 32 * 512
+    q, qd = pk.queries((1, 4, n_q))
+    q[0, 0, 5] *= 1e-6
+    q[0, 0, 6] *= 30.0
+    q = q.astype(np.float32).astype(np.float64)
+    qd = torch.from_numpy(q.astype(np.float32)).cuda()
+    qd[0, 0, 9] = float("nan")
+    out = bg.blockgtq_cross_attn(pk.cfg, pk.layout, 0, qd[0], i32(lens), 600, pk.cache)
+    assert torch.isnan(out[1]).all() and torch.isnan(out[2]).all() and (out[3] == 0).all() and torch.isnan(out[0, 9]).all()
+    at = [0, 5, 6, 8, 10, 599]
+    ref, bound = expect_cross(pk, q[:, :, at], [600, 0, 0, 0], torch.float32)
+    check("seq 0", out[0, at], ref[0, 0], bound[0, 0])
+
+
+def test_fp32_outputs_in_the_2_norm(rotations):
+    """The worst-case bounds above are far from what independent roundings do.  A logit of size |x| is off by about
+    2^-23 sqrt(sum of squared terms) from the operands' parts and the fp32 sums, below 2^-21 here (rotated terms of
+    about 1, logits up to about 30: 30 2^-23 at the most from the scaling and the exponential's argument), a weight by
+    as much again, so an output by less than 1e-5 of its size."""
+    for shape, n_q in ((dict(kv=2, group=4), 6), (dict(kv=8, group=4), 1100)):
+        pk = Packed(rotations, 73, cap=640, dtype="fp32", k_budget=192, v_bits=3, **shape)
+        q, qd = pk.queries((1, 1, n_q))
+        out = bg.blockgtq_cross_attn(pk.cfg, pk.layout, 0, qd[0], i32([600]), 600, pk.cache)
+        at = list(range(0, n_q, max(1, n_q // 6)))
+        ref, _ = expect_cross(pk, q[:, :, at], [600], torch.float32)
+        err = np.linalg.norm(out[:, at].double().cpu().numpy() - ref[0]) / np.linalg.norm(ref)
+        print(f"{n_q} query rows: {err:.3g}", flush=True)
+        assert err <= 1e-5, err
+
+
 # ---------------------------------------------------------------- shared prefix
 
 SHARED = [
@@ -388,6 +467,26 @@ def test_shared_prefix_decode(rotations, layers, batch, kv, group, k_budget, v_b
     check("one layer", one, ref[-1], bound[-1])
 
 
+@pytest.mark.parametrize("tout", ["bf16", "fp32"])
+def test_shared_prefix_wide_pass(rotations, tout):
+    """A batch and a prefix large enough for the passes with many query rows to a workgroup."""
+    dt = torch.bfloat16 if tout == "bf16" else torch.float32
+    batch, prefix = 384, 1000
+    lens = [(7 * b) % 41 for b in range(batch)]
+    kw = dict(kv=8, group=8, k_budget=192, v_bits=3)
+    pk = Packed(rotations, 35, batch=batch, cap=64, **kw)
+    pp = Packed(rotations, 36, cap=1024, layout_of=pk, behind=float("nan"), lens=[prefix], **kw)
+    assert bg.shared_workspace_bytes(pk.cfg, pp.cfg, 1, 0, prefix, 40) >= batch * 64 * (512 + 3 * 528)
+    q, qd = pk.queries((1, batch))
+    out = bg.blockgtq_decode_attn_shared(pk.cfg, pk.layout, 0, qd[0], pp.cfg, pp.cache, i32([prefix]), prefix, i32(lens), 40,
+                                         pk.cache, out_dtype=dt)
+    for b in (0, 1, 15, 16, 31, 32, 300, 383):
+        for h in (0, 7):
+            hs = slice(8 * h, 8 * h + 8)
+            k, v = (np.concatenate([getattr(pp, n)[0, 0, h, :prefix], getattr(pk, n)[0, b, h, :lens[b]]]) for n in "kv")
+            check(f"seq {b} head {h}", out[b, hs], *attention_and_bound(q[0, b, hs], k, v, pk.bits[0, h], pk.rot_k, pk.rot_v, dt))
+
+
 def test_shared_lengths_outside_the_bound(rotations):
     pk = Packed(rotations, 33, batch=3, cap=64)
     pp = Packed(rotations, 34, cap=128, layout_of=pk)
@@ -401,6 +500,38 @@ def test_shared_lengths_outside_the_bound(rotations):
         out = bg.blockgtq_decode_attn_shared(pk.cfg, pk.layout, 0, qd[0], pp.cfg, pp.cache, i32([bad]), 90, i32([4, 5, 6]),
                                              64, pk.cache)
         assert torch.isnan(out).all()
+
+
+# ---------------------------------------------------------------- long caches
+
+def test_rows_beyond_32_bit_offsets(rotations):
+    """Rows whose codes lie more than 2^32 bytes into the cache: read back, attended, and as a prefix.  The cache is
+    zero (radius 0: logit 0, value 0) but for its last rows, whose keys are the query's own direction with logits far
+    above ln(rows): they alone carry the output."""
+    cap = (1 << 27) + (1 << 23)
+    small = Packed(rotations, 81, cap=64, group=2, k_budget=128, v_bits=2, kind="uniform", dtype="fp32")
+    cfg = bg.Config(1, 1, 1, 2, cap, 128, 2, bg.BGTQ_FP32)
+    cache = bg.Cache(cfg)
+    n0 = cap - 64
+    assert n0 * 32 > 1 << 32
+    rng = np.random.default_rng(82)
+    d = rng.standard_normal(D)
+    x = torch.from_numpy((40.0 * d + rng.standard_normal((1, 64, 1, D))).astype(np.float32)).cuda()
+    v = torch.from_numpy(rng.standard_normal((1, 64, 1, D)).astype(np.float32)).cuda()
+    bg.blockgtq_quantize_append(cfg, small.layout, 0, x, v, i32([n0]), cache)
+    tail, head = bg.Cache(small.cfg), i32([0])
+    bg.blockgtq_quantize_append(small.cfg, small.layout, 0, x, v, head, tail)
+    near = bg.blockgtq_dequantize_rows(small.cfg, small.layout, 0, tail, head, 64)
+    far = bg.blockgtq_dequantize_rows(cfg, small.layout, 0, cache, i32([n0]), 64)
+    assert all(torch.equal(a, b) for a, b in zip(near, far))
+    q = torch.from_numpy((d + 0.1 * rng.standard_normal((1, 1, 2, D))).astype(np.float32)).cuda()
+    want = bg.blockgtq_cross_attn(small.cfg, small.layout, 0, q, i32([64]), 64, tail)
+    got = bg.blockgtq_cross_attn(cfg, small.layout, 0, q, i32([cap]), cap, cache)
+    assert float((got - want).abs().max()) <= 1e-5 * float(want.abs().max())
+    empty = bg.Cache(small.cfg)
+    got = bg.blockgtq_decode_attn_shared(small.cfg, small.layout, 0, q[:, 0].contiguous(), cfg, cache, i32([cap]), cap, i32([0]),
+                                         0, empty)
+    assert float((got - want[:, 0]).abs().max()) <= 1e-5 * float(want.abs().max())
 
 
 # ---------------------------------------------------------------- together, streams, graphs
