@@ -369,8 +369,10 @@ int blockgtq_dequantize_rows(const bgtq_config* cfg, const void* d_layout, int32
  *      too) does not enter its outputs.
  * max_ctx: host-side bound (<= capacity, ECAPACITY otherwise).
  * n_splits: 0 = heuristic, else the splits of the key axis (1 .. 4096).
- * d_workspace: blockgtq_cross_workspace_bytes bytes, any contents; calls that
- *      share it must not overlap in time.
+ * d_workspace: blockgtq_cross_workspace_bytes bytes for the same n_q, n_splits
+ *      and max_ctx (the need does not grow with each of them: a call of fewer
+ *      query rows may take more splits), any contents; calls that share it must
+ *      not overlap in time.
  * EUNSUPPORTED above 2^24 query rows (layers x batch x n_q x heads) a call. */
 int blockgtq_cross_workspace_bytes(const bgtq_config* cfg, int32_t n_layers_in_call, int32_t n_q, int32_t n_splits,
                                    int32_t max_ctx, size_t* bytes_out);
@@ -399,8 +401,8 @@ int blockgtq_cross_attn(const bgtq_config* cfg, const void* d_layout, int32_t la
  * d_q, d_out, out_dtype, layer: as blockgtq_cross_attn with one query row per
  *      sequence, [batch][n_kv_heads*group][128].
  * n_splits: splits of the prefix, 0 = heuristic.
- * d_workspace: blockgtq_shared_workspace_bytes bytes, as in
- *      blockgtq_cross_attn. */
+ * d_workspace: blockgtq_shared_workspace_bytes bytes for the same arguments, as
+ *      in blockgtq_cross_attn. */
 int blockgtq_shared_workspace_bytes(const bgtq_config* cfg, const bgtq_config* prefix_cfg, int32_t n_layers_in_call,
                                     int32_t n_splits, int32_t max_prefix, int32_t max_ctx, size_t* bytes_out);
 int blockgtq_decode_attn_shared(const bgtq_config* cfg, const void* d_layout, int32_t layer, const void* d_q,

@@ -198,6 +198,7 @@ class Layout:
         _check(lib().blockgtq_layout_init(ctypes.byref(cfg.c()), _ptr(bits), _ptr(rk), _ptr(rv),
                                           _ptr(self.blob), _stream(stream)))
         self.k_bits = bits
+        self.k_budget = cfg.k_budget
 
 
 class Cache:
@@ -421,12 +422,28 @@ def _cache_tensors(cfg: Config, cache: Cache, what="cache"):
     return cache.k_codes, cache.k_norms, cache.v_codes, cache.v_norms
 
 
+def _check_layout(cfg: Config, layout: Layout):
+    rows = cfg.n_layers * cfg.n_kv_heads
+    if layout.k_bits.shape[0] != rows or layout.k_budget != cfg.k_budget:
+        raise ValueError(f"layout of {layout.k_bits.shape[0]} (layer, head) rows with a key budget of {layout.k_budget}, "
+                         f"the configuration has {rows} with {cfg.k_budget}")
+
+
+def _on(stream):
+    """Where a call allocates: on the stream it runs on, so that what is filled
+    there is filled before, and what is freed there is reused after it."""
+    import torch
+    return contextlib.nullcontext() if stream is None else torch.cuda.stream(stream)
+
+
 def _call(fn, stream, args, *tensors):
     """fn(*args, stream) on the one GPU that holds all the tensors (None is
     skipped), whichever is current: on `stream`, or that GPU's current one."""
     import torch
     tensors = [t for t in tensors if t is not None]
     d = tensors[0].get_device()
+    if stream is not None and stream.device_index != d:
+        raise ValueError(f"a stream of device {stream.device_index} for tensors on device {d}")
     for t in tensors:
         if t.get_device() < 0 or not t.is_contiguous():
             raise ValueError("device tensors must be contiguous CUDA tensors")
@@ -462,12 +479,14 @@ def blockgtq_dequantize_rows(cfg: Config, layout: Layout, layer: int, cache: Cac
     read; with neither, both are allocated (zeros; out_dtype, fp32 by default).
     Returns (k_out, v_out)."""
     import torch
+    _check_layout(cfg, layout)
     _check_shape("read_pos", read_pos, (cfg.batch,), torch.int32)
     if ctx_len is not None:
         _check_shape("ctx_len", ctx_len, (cfg.batch,), torch.int32)
     shape = _lead(cfg, layer) + (max(n_rows, 0), cfg.n_kv_heads, HEAD_DIM)
     if k_out is None and v_out is None:
-        k_out, v_out = (torch.zeros(shape, dtype=out_dtype or torch.float32, device=read_pos.device) for _ in range(2))
+        with _on(stream):
+            k_out, v_out = (torch.zeros(shape, dtype=out_dtype or torch.float32, device=read_pos.device) for _ in range(2))
     dtype = (v_out if k_out is None else k_out).dtype
     if out_dtype is not None and dtype != out_dtype:
         raise ValueError(f"out_dtype {out_dtype}, but the outputs are {dtype}")
@@ -496,10 +515,11 @@ def shared_workspace_bytes(cfg: Config, prefix_cfg: Config, n_layers_in_call: in
     return v.value
 
 
-def _out_of(q, out, out_dtype):
+def _out_of(q, out, out_dtype, stream):
     import torch
     if out is None:
-        out = torch.empty(q.shape, dtype=out_dtype or torch.float32, device=q.device)
+        with _on(stream):
+            out = torch.empty(q.shape, dtype=out_dtype or torch.float32, device=q.device)
     elif out_dtype is not None and out.dtype != out_dtype:
         raise ValueError(f"out_dtype {out_dtype}, but out is {out.dtype}")
     _check_shape("out", out, q.shape, out.dtype)
@@ -512,6 +532,7 @@ def blockgtq_cross_attn(cfg: Config, layout: Layout, layer: int, q, ctx_len, max
     query row attending rows [0, ctx_len[b]) of its sequence's packed cache.
     Returns out, of q's shape in out's or out_dtype (fp32 by default)."""
     import torch
+    _check_layout(cfg, layout)
     n_lc = cfg.n_layers if layer < 0 else 1
     lead = _lead(cfg, layer)
     if q.dim() != len(lead) + 3:
@@ -519,10 +540,11 @@ def blockgtq_cross_attn(cfg: Config, layout: Layout, layer: int, q, ctx_len, max
     n_q = q.shape[len(lead)]
     _check_shape("q", q, lead + (n_q, cfg.n_q_heads, HEAD_DIM), _in_dtype(cfg))
     _check_shape("ctx_len", ctx_len, (cfg.batch,), torch.int32)
-    out, kind = _out_of(q, out, out_dtype)
+    out, kind = _out_of(q, out, out_dtype, stream)
     if workspace is None:
-        workspace = torch.empty(max(cross_workspace_bytes(cfg, n_lc, n_q, n_splits, max_ctx), 1), dtype=torch.uint8,
-                                device=q.device)
+        with _on(stream):
+            workspace = torch.empty(max(cross_workspace_bytes(cfg, n_lc, n_q, n_splits, max_ctx), 1), dtype=torch.uint8,
+                                    device=q.device)
     _call(lib().blockgtq_cross_attn, stream,
           (ctypes.byref(cfg.c()), layout.blob.data_ptr(), layer, q.data_ptr(), n_q, ctx_len.data_ptr(), max_ctx,
            ctypes.byref(cache.c()), out.data_ptr(), kind, workspace.data_ptr(),
@@ -540,14 +562,16 @@ def blockgtq_decode_attn_shared(cfg: Config, layout: Layout, layer: int, q, pref
     softmax.  prefix_cfg: cfg with batch 1 and the prefix cache's capacity.
     Returns out, of q's shape in out's or out_dtype (fp32 by default)."""
     import torch
+    _check_layout(cfg, layout)
     n_lc = cfg.n_layers if layer < 0 else 1
     _check_shape("q", q, _lead(cfg, layer) + (cfg.n_q_heads, HEAD_DIM), _in_dtype(cfg))
     _check_shape("ctx_len", ctx_len, (cfg.batch,), torch.int32)
     _check_shape("prefix_len", prefix_len, (1,), torch.int32)
-    out, kind = _out_of(q, out, out_dtype)
+    out, kind = _out_of(q, out, out_dtype, stream)
     if workspace is None:
-        workspace = torch.empty(shared_workspace_bytes(cfg, prefix_cfg, n_lc, n_splits, max_prefix, max_ctx),
-                                dtype=torch.uint8, device=q.device)
+        with _on(stream):
+            workspace = torch.empty(shared_workspace_bytes(cfg, prefix_cfg, n_lc, n_splits, max_prefix, max_ctx),
+                                    dtype=torch.uint8, device=q.device)
     _call(lib().blockgtq_decode_attn_shared, stream,
           (ctypes.byref(cfg.c()), layout.blob.data_ptr(), layer, q.data_ptr(), ctypes.byref(prefix_cfg.c()),
            ctypes.byref(prefix.c()), prefix_len.data_ptr(), max_prefix, ctx_len.data_ptr(), max_ctx,

@@ -3,6 +3,7 @@ sizes, and every refusal, before anything is enqueued (the pointers are never
 dereferenced)."""
 import ctypes
 
+import numpy as np
 import pytest
 
 from paper_2606_24033_amd import blockgtq as bg
@@ -130,7 +131,13 @@ def test_binding_refuses_wrong_tensors():
     cache, prefix = bg.Cache(cfg, device="cpu"), bg.Cache(one, device="cpu")
 
     class L:
-        blob = torch.zeros(8, dtype=torch.uint8)
+        blob, k_bits, k_budget = torch.zeros(8, dtype=torch.uint8), np.zeros((2, 16), dtype=np.uint8), cfg.k_budget
+
+    class Other(L):
+        k_bits = np.zeros((4, 16), dtype=np.uint8)
+
+    class Wide(L):
+        k_budget = 2 * cfg.k_budget
     i32 = lambda *a: torch.tensor(a, dtype=torch.int32)  # noqa: E731
     ctx, ws = i32(1, 2, 3), torch.zeros(1 << 20, dtype=torch.uint8)
     q = torch.zeros((3, 5, 8, 128), dtype=torch.bfloat16)
@@ -154,6 +161,15 @@ def test_binding_refuses_wrong_tensors():
                 dict(ctx=ctx[:1]), dict(out_dtype=torch.float64)):
         with pytest.raises(ValueError):
             shared(**bad)
+
+    for layout in (Other, Wide):
+        with pytest.raises(ValueError, match="layout"):
+            bg.blockgtq_dequantize_rows(cfg, layout, 0, cache, ctx, 7)
+        with pytest.raises(ValueError, match="layout"):
+            bg.blockgtq_cross_attn(cfg, layout, 0, q, ctx, 100, cache, workspace=ws)
+        with pytest.raises(ValueError, match="layout"):
+            bg.blockgtq_decode_attn_shared(cfg, layout, 0, q[:, 0].contiguous(), one, prefix, i32(4), 64, ctx, 100, cache,
+                                           workspace=ws)
 
     def rows(pos=ctx, n=7, cache=cache, **kw):
         return bg.blockgtq_dequantize_rows(cfg, L, 0, cache, pos, n, **kw)

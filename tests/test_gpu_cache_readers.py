@@ -650,6 +650,27 @@ def test_on_another_stream(rotations):
     check("rows", k[1, :, 0], *expect_rows(pk, 0, 1, 0, "k", 0, 10, torch.float32))
 
 
+def test_outputs_allocated_for_another_stream(rotations):
+    """Outputs and workspaces that a call allocates belong to the stream it runs on: a late fill or a reuse on the
+    current stream, behind slow work there, must not meet them."""
+    pk = Packed(rotations, 54, batch=2, cap=640)
+    q, qd = pk.queries((1, 2, 1))
+    lens = [600, 640]
+    ref, bound = expect_cross(pk, q, lens, torch.float32)
+    ctx, pos = i32(lens), i32([0, 0])
+    big = torch.randn(4096, 4096, device="cuda")
+    s = torch.cuda.Stream()
+    s.wait_stream(torch.cuda.current_stream())
+    for _ in range(20):
+        big = big @ big * 1e-4
+    k, v = bg.blockgtq_dequantize_rows(pk.cfg, pk.layout, 0, pk.cache, pos, 10, stream=s)
+    out = bg.blockgtq_cross_attn(pk.cfg, pk.layout, 0, qd[0], ctx, 640, pk.cache, n_splits=10, stream=s)
+    torch.cuda.synchronize()
+    check("rows", k[1, :, 0], *expect_rows(pk, 0, 1, 0, "k", 0, 10, torch.float32))
+    check("values", v[1, :, 0], *expect_rows(pk, 0, 1, 0, "v", 0, 10, torch.float32))
+    check("stream", out, ref[0], bound[0])
+
+
 def test_same_call_twice_gives_the_same_bits(rotations):
     pk = Packed(rotations, 54, batch=2, kv=2, cap=704)
     pp = Packed(rotations, 55, kv=2, cap=1088, layout_of=pk)
