@@ -365,8 +365,20 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(2, 2))
   const int tid = threadIdx.x, lane = tid & 63, l32 = lane & 31, hf = lane >> 5;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int G = d.group, hq = d.n_kv * G, kw = d.k_words;
-  const int second = static_cast<int>(blockIdx.x) >= call.side[0].items;
-  const CrossSide& S = call.side[second];
+  const bool second = static_cast<int>(blockIdx.x) >= call.side[0].items;
+  CrossSide S;  // (of both sides' arguments, read at once: no address waits for the choice)
+  {
+    const CrossSide &a = call.side[0], &b = call.side[1];
+    S.c = {second ? b.c.k_codes : a.c.k_codes, second ? b.c.k_norms : a.c.k_norms, second ? b.c.v_codes : a.c.v_codes,
+           second ? b.c.v_norms : a.c.v_norms};
+    S.len = second ? b.len : a.len;
+    S.batch = second ? b.batch : a.batch;
+    S.capacity = second ? b.capacity : a.capacity;
+    S.n_q = second ? b.n_q : a.n_q;
+    S.split_len = second ? b.split_len : a.split_len;
+    S.max_len = second ? b.max_len : a.max_len;
+    S.slot0 = second ? b.slot0 : a.slot0;
+  }
   // Row blocks vary fastest and splits slowest: workgroups go to the 8 XCDs in
   // turn, and a ragged batch's late splits, often empty, would leave some XCDs
   // without work if the split chose the XCD.
@@ -380,13 +392,51 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(2, 2))
   const int seq = lz % S.batch, layer = d.layer >= 0 ? d.layer : lz / S.batch;
   const int ri = layer * d.n_kv + kvh;
   const RowMeta* M = reinterpret_cast<const RowMeta*>(blob + kOffRows) + ri;
-  const int ng = M->n_groups, nslot = (ng + 1) & ~1;
   const auto row_at = [&](int r) {  // query row r of the unit, in q, out and the partials
     return (static_cast<size_t>(lz) * S.n_q + r / G) * hq + kvh * G + r % G;
   };
 
+  // The reads of the set-up that need no length, before the length is there (a
+  // read that misses every cache takes about 1 us): fp16 codebooks, the wave's
+  // 16 positions of the rotation, the query rows (thread = row tid / 16, dims 8
+  // (tid % 16) .. + 7).
+  const bool bf = d.in_dtype == 1;
+  const uint16_t cv = reinterpret_cast<const uint16_t*>(blob + kOffC16)[min(tid, kCodebookEntries - 1)];
+  float4_t rk[8];
+  uint4 x0, x1;
+  {
+    const float4_t* w = reinterpret_cast<const float4_t*>(blob + layout_kdense_offset(d.n_layers * d.n_kv)) +
+                        static_cast<size_t>(ri) * (kMfmaMatFloats / 4) + wave * 8 * 64 + lane;
+    const size_t at = row_at(min(r0 + (tid >> 4), nr - 1)) * kHeadDim + 8 * (tid & 15);
+    const uint4* qp = reinterpret_cast<const uint4*>(static_cast<const uint8_t*>(q) + at * (bf ? 2 : 4));
+    x0 = qp[0];
+    x1 = bf ? make_uint4(0, 0, 0, 0) : qp[1];
+#pragma unroll
+    for (int s4 = 0; s4 < 8; ++s4) rk[s4] = w[s4 * 64];
+  }
+
+  // The length and the row's groups, read together (the asm keeps the compiler
+  // from reading each group where it is used, one wait after the other).
+  int len = S.len[seq], ng = M->n_groups;
+  uint32_t gm[8], used = 1u << (BV - 1);
+  int gd[8], gp[8];
+#pragma unroll
+  for (int b = 0; b < 8; ++b) {
+    gm[b] = M->gm[b];
+    gd[b] = M->g_dim[b];
+    gp[b] = M->g_pos[b];
+  }
+  asm volatile("" : "+s"(len), "+s"(ng), "+s"(gm[0]), "+s"(gm[1]), "+s"(gm[2]), "+s"(gm[3]), "+s"(gm[4]), "+s"(gm[5]),
+               "+s"(gm[6]), "+s"(gm[7]));
+  asm volatile("" : "+s"(gd[0]), "+s"(gd[1]), "+s"(gd[2]), "+s"(gd[3]), "+s"(gd[4]), "+s"(gd[5]), "+s"(gd[6]), "+s"(gd[7]),
+               "+s"(gp[0]), "+s"(gp[1]), "+s"(gp[2]), "+s"(gp[3]), "+s"(gp[4]), "+s"(gp[5]), "+s"(gp[6]), "+s"(gp[7]));
+#pragma unroll
+  for (int b = 0; b < 8; ++b) {
+    used |= (gm[b] >> 31) << b;
+    gd[b] = b < ng ? gd[b] : 0;
+  }
+  const int nslot = (ng + 1) & ~1;
   // a length outside [0, max_len] (the host's bound) makes the rows NaN
-  const int len = S.len[seq];
   const bool ok = len >= 0 && len <= S.max_len;
   const int t_begin = split * S.split_len;
   const int t_end = ok ? min(len, t_begin + S.split_len) : t_begin;
@@ -446,30 +496,13 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(2, 2))
   // coordinate to [2^13, 2^14): the lo parts stay above fp16's subnormals.
   // Every global read of the set-up and the first tile's are issued at once
   // (few and wide ones: the 8 waves' loads pass one by one).
-  uint32_t gm[8], used = 1u << (BV - 1);
-  int gd[8], gp[8];
-#pragma unroll
-  for (int b = 0; b < 8; ++b) {
-    gm[b] = M->gm[b];
-    used |= (gm[b] >> 31) << b;
-    gd[b] = b < ng ? M->g_dim[b] : 0;
-    gp[b] = M->g_pos[b];
-  }
   const int p0 = 16 * wave + 4 * (lane >> 4);  // the lane's 4 positions of the rotation
   float4_t rq[2];                              // rows 16 c + lane % 16
   {
-    const uint16_t* c16 = reinterpret_cast<const uint16_t*>(blob + kOffC16);
-    const float4_t* w = reinterpret_cast<const float4_t*>(blob + layout_kdense_offset(d.n_layers * d.n_kv)) +
-                        static_cast<size_t>(ri) * (kMfmaMatFloats / 4) + wave * 8 * 64 + lane;
-    const uint16_t cv = c16[min(tid, kCodebookEntries - 1)];
-    // thread = (row tid / 16, dims 8 (tid % 16) .. + 7)
-    const size_t at = row_at(min(r0 + (tid >> 4), nr - 1)) * kHeadDim + 8 * (tid & 15);
-    const bool bf = d.in_dtype == 1;
-    const uint4* qp = reinterpret_cast<const uint4*>(static_cast<const uint8_t*>(q) + at * (bf ? 2 : 4));
-    const uint4 x0 = qp[0], x1 = bf ? make_uint4(0, 0, 0, 0) : qp[1];
-    float4_t a[8];
-#pragma unroll
-    for (int s4 = 0; s4 < 8; ++s4) a[s4] = w[s4 * 64];
+    // (the lane's 128 bytes of Pi_V^T for the end, brought near)
+    float near = 0.f;
+    if (call.n_slots == 1)
+      near = reinterpret_cast<const float*>(blob + kOffRotVT)[(16 * wave + (lane & 15)) * kHeadDim + 32 * (lane >> 4)];
     if (t0 < t_end) {
       load_keys(t0);
       load_values(t0);
@@ -497,7 +530,8 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(2, 2))
     }
     __syncthreads();
     build_tables(smem, cbs, used, tid);
-    staged_product<2>(smem + kImg, a, lane, rq);
+    staged_product<2>(smem + kImg, rk, lane, rq);
+    asm volatile("" ::"v"(near));
   }
   // place of the lane's position pairs in the image (group sizes are even)
   uint32_t img_at[2];
