@@ -881,7 +881,7 @@ int blockgtq_dequantize_rows(const bgtq_config* cfg, const void* d_layout, int32
 // How one attention pass runs: the query rows of a workgroup (32: k_cross; 128
 // or 256: k_cross_tile on rotated query rows) and the splits of the key axis.
 struct CrossPlan {
-  int rows, n_splits, split_len;
+  int rows, pack, n_splits, split_len;  // 2^pack sequences to a workgroup
   long items;
   double wg;  // estimated us of a workgroup
 };
@@ -890,14 +890,15 @@ struct CrossPlan {
 // workgroup runs per CU, so `items` of them take ceil(items / 256) rounds, each
 // as long as one split.  In us, measured (kernel times in a graph):
 //   32 rows: 12 a workgroup + 5.4 (key rows of up to 8 words) or 6.2 for
-//     every 8 tiles, a tile per wave;
+//     every tile that its waves take one after the other: 8 waves to a
+//     sequence, or to 2, 4 or 8 of them, whose set-up is then one;
 //   128 rows: 14 + 1.8 a tile, 256 rows: 14 + 2.75 a tile, up to 1.3 times as
 //     much with all CUs busy, after a rotation launch of 9 + 1 per 5000 query
 //     rows;
 //   joining: 4, and the partials written and read at 4.5 TB/s.
-// `beside`: the sequences' own pass in the same call (prefix passes).  Its
-// workgroups follow 32-row ones as these end, in one launch, and come after
-// wide ones.
+// `beside`: the other pass of the same call (a prefix and the sequences' own
+// rows).  The workgroups of two 32-row passes follow one another in one launch
+// as these end; the own rows' come after a prefix's wide ones.
 static CrossPlan cross_plan(const Dims& d, int n_q, int max_len, int requested, const CrossPlan* beside) {
   const long units = static_cast<long>(d.n_kv) * d.n_lc * d.batch, nr = static_cast<long>(n_q) * d.group;
   const int tiles = std::max(1, (max_len + 63) / 64);
@@ -905,30 +906,34 @@ static CrossPlan cross_plan(const Dims& d, int n_q, int max_len, int requested, 
   double t_best = 0.0;
   for (const int rows : {32, 128, 256}) {
     if (rows > 32 && (nr <= rows / 4 || static_cast<long>(d.n_lc) * d.batch > 65535)) continue;
-    const long blocks = units * ((nr + rows - 1) / rows);
-    const int k0 = requested > 0 ? std::min(requested, tiles) : 1;
-    const int k1 = requested > 0 ? k0 : std::min(rows == 32 ? (tiles + 7) / 8 : tiles, 256);
-    for (int k = k0; k <= std::max(k0, k1); ++k) {
-      const int len = (tiles + k - 1) / k, n = (tiles + len - 1) / len;
-      const double busy = 1.0 + 0.3 * std::min(1.0, blocks * n / 256.0);
-      const double wg = rows == 32 ? 12.0 + (d.k_words <= 8 ? 5.4 : 6.2) * ((len + 7) / 8)
-                                   : 14.0 + (rows == 128 ? 1.8 : 2.75) * busy * len;
-      const long rounds = (blocks * n + 255) / 256;
-      double t = static_cast<double>(rounds) * wg;
-      // Several sequences are seldom as long as the longest (the host knows only
-      // its length): half the estimate for equal lengths, half the one for
-      // lengths of 2/3 of it on average, whose workgroups follow one another
-      // without rounds.
-      if (d.batch > 1) t = std::max(wg, 0.5 * t + 0.5 * (0.65 * blocks * n / 256 * wg + 0.5 * wg));
-      if (rows > 32) t += 9.0 + 2e-4 * units * nr;
-      if (beside)
-        t = rows == 32 ? std::max(wg, (blocks * n * wg + beside->items * beside->wg) / 256)
-                       : t + 5.0 + static_cast<double>((beside->items + 255) / 256) * beside->wg;
-      if (n > 1 && !beside) t += 4.0;
-      if (n > 1 || beside) t += 2.4e-7 * kPartFloats * 4 * units * nr * n;
-      if (!best.rows || t < t_best) {
-        t_best = t;
-        best = {rows, n, 64 * len, blocks * n, wg};
+    for (int pack = 0; pack <= (rows == 32 ? 3 : 0); ++pack) {
+      if (pack && (nr << pack > 32 || d.batch < 1 << pack)) break;
+      const int wps = 8 >> pack;  // waves to a sequence (32 rows)
+      const long blocks = static_cast<long>(d.n_kv) * d.n_lc * ((d.batch + (1 << pack) - 1) >> pack) * ((nr + rows - 1) / rows);
+      const int k0 = requested > 0 ? std::min(requested, tiles) : 1;
+      const int k1 = requested > 0 ? k0 : std::min(rows == 32 ? (tiles + wps - 1) / wps : tiles, 256);
+      for (int k = k0; k <= std::max(k0, k1); ++k) {
+        const int len = (tiles + k - 1) / k, n = (tiles + len - 1) / len;
+        const double busy = 1.0 + 0.3 * std::min(1.0, blocks * n / 256.0);
+        const double wg = rows == 32 ? 12.0 + (d.k_words <= 8 ? 5.4 : 6.2) * ((len + wps - 1) / wps)
+                                     : 14.0 + (rows == 128 ? 1.8 : 2.75) * busy * len;
+        const long rounds = (blocks * n + 255) / 256;
+        double t = static_cast<double>(rounds) * wg;
+        // Several sequences are seldom as long as the longest (the host knows only
+        // its length): half the estimate for equal lengths, half the one for
+        // lengths of 2/3 of it on average (nearer to it for the longest of a
+        // workgroup), whose workgroups follow one another without rounds.
+        if (d.batch > 1) t = std::max(wg, 0.5 * t + 0.5 * ((0.65 + 0.1 * pack) * blocks * n / 256 * wg + 0.5 * wg));
+        if (rows > 32) t += 9.0 + 2e-4 * units * nr;
+        if (beside)
+          t = rows == 32 ? std::max(wg, (blocks * n * wg * (d.batch > 1 ? 0.825 + 0.05 * pack : 1.0) + beside->items * beside->wg) / 256)
+                         : t + 5.0 + static_cast<double>((beside->items + 255) / 256) * beside->wg;
+        if (n > 1 && !beside) t += 4.0;
+        if (n > 1 || beside) t += 2.4e-7 * kPartFloats * 4 * units * nr * n;
+        if (!best.rows || t < t_best) {
+          t_best = t;
+          best = {rows, pack, n, 64 * len, blocks * n, wg};
+        }
       }
     }
   }
@@ -1003,7 +1008,7 @@ int blockgtq_cross_attn(const bgtq_config* cfg, const void* d_layout, int32_t la
   if (p.items > kMaxItems) return fail(BGTQ_EUNSUPPORTED, "too many splits of too many query rows");
   CrossCall call = {};
   call.side[0] = {cache_ptrs(cache), d_ctx_len, cfg->batch, cfg->capacity, n_q, p.n_splits, p.split_len, max_ctx, 0,
-                  static_cast<int>(p.items)};
+                  static_cast<int>(p.items), p.pack};
   const long rows = cross_rows(cfg, n_lc, n_q);
   call.rows0 = p.rows;
   call.part = static_cast<float*>(d_workspace);
@@ -1032,8 +1037,10 @@ struct SharedPlan {
 static SharedPlan shared_plan(const bgtq_config* cfg, const bgtq_config* pcfg, int32_t n_lc, int32_t n_splits,
                               int32_t max_prefix, int32_t max_ctx) {
   SharedPlan p;
-  p.own = cross_plan(cross_dims(cfg, n_lc), 1, max_ctx, 0, nullptr);  // (at most 8 query rows: 32-row workgroups)
-  p.prefix = cross_plan(cross_dims(pcfg, n_lc), cfg->batch, max_prefix, n_splits, &p.own);
+  const Dims d = cross_dims(cfg, n_lc), dp = cross_dims(pcfg, n_lc);
+  p.own = cross_plan(d, 1, max_ctx, 0, nullptr);  // (at most 8 query rows: 32-row workgroups)
+  p.prefix = cross_plan(dp, cfg->batch, max_prefix, n_splits, &p.own);
+  if (p.prefix.rows == 32) p.own = cross_plan(d, 1, max_ctx, 0, &p.prefix);
   return p;
 }
 
@@ -1073,9 +1080,9 @@ int blockgtq_decode_attn_shared(const bgtq_config* cfg, const void* d_layout, in
   CrossCall call = {};
   // the prefix: every sequence's query is a query row of its one sequence
   call.side[0] = {cache_ptrs(prefix), d_prefix_len, 1, prefix_cfg->capacity, cfg->batch, p.prefix.n_splits,
-                  p.prefix.split_len, max_prefix, 0, static_cast<int>(p.prefix.items)};
+                  p.prefix.split_len, max_prefix, 0, static_cast<int>(p.prefix.items), p.prefix.pack};
   call.side[1] = {cache_ptrs(cache), d_ctx_len, cfg->batch, cfg->capacity, 1, p.own.n_splits, p.own.split_len, max_ctx,
-                  p.prefix.n_splits, static_cast<int>(p.own.items)};
+                  p.prefix.n_splits, static_cast<int>(p.own.items), p.own.pack};
   const long rows = cross_rows(cfg, n_lc, 1);
   call.rows0 = p.prefix.rows;
   call.part = static_cast<float*>(d_workspace);

@@ -67,7 +67,8 @@ static_assert(kLds <= 160 * 1024, "LDS of one workgroup");
 // at the end: [wave][row] accumulators, then maxima and sums
 constexpr int kAccStride = kHeadDim + 4;
 constexpr int kEndM = kWaves * kRows * kAccStride * 4;
-static_assert(kEndM + 2 * kWaves * kRows * 4 <= kLds, "merge area");
+constexpr int kEndTiles = kEndM + 2 * kWaves * kRows * 4;  // per wave: tiles of its sequence, -1 for a refused length
+static_assert(kEndTiles + kWaves * 4 <= kLds, "merge area");
 
 __device__ __forceinline__ float half_bits(uint32_t b) {
   return static_cast<float>(__builtin_bit_cast(_Float16, static_cast<uint16_t>(b)));
@@ -358,7 +359,9 @@ __device__ __forceinline__ void build_tables(uint8_t* smem, const uint16_t* cbs,
 // ---------------------------------------------------------------- kernel
 // EX: the softmax weights in two fp16 parts (22 bits) for fp32 outputs; one
 // part moves an output by at most 2^-11, half the rounding to bf16.
-template <int KWB, int BV, bool EX>
+// PACK: a side may have several sequences in a workgroup (what it takes to find
+// a row's sequence is 0.5 us of a call of 16 without it).
+template <int KWB, int BV, bool EX, bool PACK>
 __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(2, 2))) void k_cross(
     Dims d, const uint8_t* __restrict__ blob, const void* __restrict__ q, CrossCall call) {
   __shared__ __attribute__((aligned(16))) uint8_t smem[kLds];
@@ -378,21 +381,28 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(2, 2))
     S.split_len = second ? b.split_len : a.split_len;
     S.max_len = second ? b.max_len : a.max_len;
     S.slot0 = second ? b.slot0 : a.slot0;
+    S.pack = !PACK ? 0 : second ? b.pack : a.pack;
   }
   // Row blocks vary fastest and splits slowest: workgroups go to the 8 XCDs in
   // turn, and a ragged batch's late splits, often empty, would leave some XCDs
   // without work if the split chose the XCD.
   int item = static_cast<int>(blockIdx.x) - (second ? call.side[0].items : 0);
-  const int nr = S.n_q * G, n_blocks = (nr + kRows - 1) / kRows;
+  // 2^pack sequences of few query rows to a workgroup: their query rows lie one
+  // after the other in the 32, a wave walks the tiles of one of them, and the
+  // other sequences' columns of its products are not used.
+  const int per = 1 << S.pack, wps = kWaves >> S.pack;  // sequences; waves to a sequence
+  const int n_blocks = (S.n_q * G + kRows - 1) / kRows, n_seq = (S.batch + per - 1) >> S.pack;
   const int r0 = item % n_blocks * kRows;
   item /= n_blocks;
   const int kvh = item % d.n_kv;
   item /= d.n_kv;
-  const int n_lz = d.n_lc * S.batch, lz = item % n_lz, split = item / n_lz;
-  const int seq = lz % S.batch, layer = d.layer >= 0 ? d.layer : lz / S.batch;
+  const int n_lz = d.n_lc * n_seq, z = item % n_lz, split = item / n_lz;
+  const int seq0 = z % n_seq << S.pack, lz = z / n_seq * S.batch + seq0, layer = d.layer >= 0 ? d.layer : z / n_seq;
+  const int sub = wave >> (3 - S.pack), seq = min(seq0 + sub, S.batch - 1);  // the wave's sequence
+  const int nr = S.n_q * G * min(per, S.batch - seq0);             // query rows
   const int ri = layer * d.n_kv + kvh;
   const RowMeta* M = reinterpret_cast<const RowMeta*>(blob + kOffRows) + ri;
-  const auto row_at = [&](int r) {  // query row r of the unit, in q, out and the partials
+  const auto row_at = [&](int r) {  // query row r of the unit (or its sequences), in q, out and the partials
     return (static_cast<size_t>(lz) * S.n_q + r / G) * hq + kvh * G + r % G;
   };
 
@@ -439,9 +449,9 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(2, 2))
   // a length outside [0, max_len] (the host's bound) makes the rows NaN
   const bool ok = len >= 0 && len <= S.max_len;
   const int t_begin = split * S.split_len;
-  const int t_end = ok ? min(len, t_begin + S.split_len) : t_begin;
+  const int t_end = ok && seq0 + sub < S.batch ? min(len, t_begin + S.split_len) : t_begin;
 
-  if (t_begin >= t_end && call.n_slots > 1) {  // no row of the sequence in this split: an empty partial
+  if (t_begin >= t_end && call.n_slots > 1 && S.pack == 0) {  // no row of the sequence in this split: an empty partial
     if (tid < kRows && r0 + tid < nr) {
       float* P = call.part + (row_at(r0 + tid) * call.n_slots + S.slot0 + split) * kPartFloats;
       P[0] = ok ? kNegInf : 0.f;
@@ -486,8 +496,8 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(2, 2))
     for (int cc = 0; cc < 4; ++cc)
       load_words(src + 32 * cc * BV, static_cast<uint32_t>((hf * kHeadDim + l32) * BV * 4), vw[cc]);
   };
-  int t0 = t_begin + wave * kKeyTile;
-  constexpr int kStride = kWaves * kKeyTile;
+  int t0 = t_begin + (wave & (wps - 1)) * kKeyTile;
+  const int stride = wps * kKeyTile;
 
   // ---- set-up: the query rows rotated into stream order,
   //   q'[p] = log2 e / sqrt(d_g d_h) sum_d W[p][d] q[d],
@@ -619,7 +629,7 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(2, 2))
 #pragma unroll
     for (int i = 0; i < 16; ++i) o[cc][i] = 0.f;
 
-  for (; t0 < t_end; t0 += kStride) {
+  for (; t0 < t_end; t0 += stride) {
     const bool full = t0 + kKeyTile <= t_end;
     __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");  // the last tile's reads of the radii come first
     // this tile's radii, token-minor, for the wave's own reads (LDS operations
@@ -652,7 +662,7 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(2, 2))
       for (int i = 0; i < 16; ++i) s[n][i] = 0.f;
     qk_all<KWB>(std::make_integer_sequence<int, 8>{}, smem, rw, gm, rad_l, rep, lane, s);
     // (without a next tile this one again: the loads in flight stay countable)
-    const int t_next = t0 + kStride < t_end ? t0 + kStride : t0;
+    const int t_next = t0 + stride < t_end ? t0 + stride : t0;
     load_keys(t_next);
 
     // ---- online softmax, base 2
@@ -770,8 +780,10 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(2, 2))
   float* const acc = reinterpret_cast<float*>(smem);
   float* const ms = reinterpret_cast<float*>(smem + kEndM);
   float* const ls = ms + kWaves * kRows;
-  const int n_act = min(kWaves, (t_end - t_begin + kKeyTile - 1) / kKeyTile);  // waves that had a tile
-  if (wave < n_act) {
+  int* const tiles = reinterpret_cast<int*>(smem + kEndTiles);
+  const int n_tiles = max(t_end - t_begin + kKeyTile - 1, 0) / kKeyTile;
+  if (S.pack && lane == 0) tiles[wave] = ok ? n_tiles : -1;
+  if ((wave & (wps - 1)) < n_tiles) {
 #pragma unroll
     for (int cc = 0; cc < 4; ++cc)
 #pragma unroll
@@ -787,22 +799,26 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(2, 2))
   const int r = tid >> 4, d0 = (tid & 15) * 8;  // dims d0 .. + 7 of row r
   float m = kNegInf, l = 0.f;
   float4_t a[2] = {{0.f, 0.f, 0.f, 0.f}, {0.f, 0.f, 0.f, 0.f}};
+  // the waves of the row's sequence that had a tile
+  const int w0 = S.pack == 0 ? 0 : min(r / (S.n_q * G), per - 1) * wps;
+  const int n_row = S.pack == 0 ? (ok ? n_tiles : -1) : tiles[w0], n_act = min(wps, n_row);
 #pragma unroll
-  for (int w = 0; w < kWaves; ++w) m = fmaxf(m, ms[w * kRows + r]);
+  for (int w = 0; w < kWaves; ++w)
+    if (w < n_act) m = fmaxf(m, ms[(w0 + w) * kRows + r]);
   const float mref = m == kNegInf ? 0.f : m;
 #pragma unroll
   for (int w = 0; w < kWaves; ++w) {
     if (w >= n_act) break;
-    const float e = __builtin_amdgcn_exp2f(ms[w * kRows + r] - mref);
-    l = fmaf(ls[w * kRows + r], e, l);
+    const float e = __builtin_amdgcn_exp2f(ms[(w0 + w) * kRows + r] - mref);
+    l = fmaf(ls[(w0 + w) * kRows + r], e, l);
 #pragma unroll
     for (int h = 0; h < 2; ++h) {
-      const float4_t x = *reinterpret_cast<const float4_t*>(acc + (w * kRows + r) * kAccStride + 4 * h + d0);
+      const float4_t x = *reinterpret_cast<const float4_t*>(acc + ((w0 + w) * kRows + r) * kAccStride + 4 * h + d0);
 #pragma unroll
       for (int i = 0; i < 4; ++i) a[h][i] = fmaf(x[i], e, a[h][i]);
     }
   }
-  if (!ok) l = __builtin_nanf("");
+  if (n_row < 0) l = __builtin_nanf("");
   if (call.n_slots > 1) {
     if (r0 + r < nr) {
       float* P = call.part + (row_at(r0 + r) * call.n_slots + S.slot0 + split) * kPartFloats;
@@ -854,11 +870,17 @@ hipError_t launch_bv(const Dims& d, const void* layout, const void* q, const Cro
     hipLaunchKernelGGL(kern, dim3(items), dim3(kThreads), 0, s, d, static_cast<const uint8_t*>(layout), q, call);
     return hipGetLastError();
   };
-  const bool ex = call.out_dtype == 0;  // BGTQ_FP32
-  if (d.k_words <= 8) return ex ? go(k_cross<8, BV, true>) : go(k_cross<8, BV, false>);
-  if (d.k_words <= 12) return ex ? go(k_cross<12, BV, true>) : go(k_cross<12, BV, false>);
-  if (d.k_words <= 16) return ex ? go(k_cross<16, BV, true>) : go(k_cross<16, BV, false>);
-  return ex ? go(k_cross<32, BV, true>) : go(k_cross<32, BV, false>);
+  const auto width = [&](auto ex, auto pack) {
+    constexpr bool E = decltype(ex)::value, P = decltype(pack)::value;
+    if (d.k_words <= 8) return go(k_cross<8, BV, E, P>);
+    if (d.k_words <= 12) return go(k_cross<12, BV, E, P>);
+    if (d.k_words <= 16) return go(k_cross<16, BV, E, P>);
+    return go(k_cross<32, BV, E, P>);
+  };
+  const bool pack = call.side[0].pack || call.side[1].pack;
+  if (call.out_dtype == 0)  // BGTQ_FP32
+    return pack ? width(std::true_type{}, std::true_type{}) : width(std::true_type{}, std::false_type{});
+  return pack ? width(std::false_type{}, std::true_type{}) : width(std::false_type{}, std::false_type{});
 }
 
 }  // namespace cross_detail

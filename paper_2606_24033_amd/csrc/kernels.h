@@ -123,6 +123,7 @@ struct CrossSide {
   int max_len;              // the host's bound on the lengths: rows of a sequence outside [0, max_len] are NaN
   int slot0;
   int items;                // workgroups
+  int pack;                 // 2^pack sequences share a workgroup (32-row ones; n_q group 2^pack <= 32, pack <= 3)
 };
 struct CrossCall {
   CrossSide side[2];  // the second one has no items in a call of one pass

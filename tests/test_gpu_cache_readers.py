@@ -344,6 +344,50 @@ def test_cross_one_query_row_is_the_decode(rotations):
     assert err <= P.tol_attention(), err
 
 
+# ---------------------------------------------------------------- sequences that share a workgroup
+
+PACKED = [
+    # layers, batch, kv, group, k_budget, v_bits, kind, in, out, n_q, longest, n_splits: batches large enough that 2, 4 or 8
+    # sequences share a workgroup, some of them not full
+    (1, 65, 8, 4, 128, 2, "mixed", "bf16", "bf16", 1, 100, 0),     # 4 sequences
+    (1, 67, 8, 4, 192, 3, "wide", "fp32", "fp32", 1, 300, 0),      # 2
+    (1, 259, 4, 4, 128, 2, "uniform", "bf16", "fp32", 1, 300, 0),  # 8
+    (9, 9, 2, 4, 128, 4, "mixed", "fp32", "bf16", 1, 200, 0),
+    (1, 133, 4, 3, 320, 5, "wide", "bf16", "fp32", 3, 130, 0),     # 9 query rows a sequence: 2
+    (1, 140, 4, 1, 512, 8, "uniform", "fp32", "fp32", 4, 200, 0),
+    (1, 131, 4, 8, 256, 1, "mixed", "bf16", "bf16", 1, 500, 3),
+    (1, 131, 4, 5, 192, 7, "mixed", "bf16", "fp32", 1, 500, 2),
+]
+
+
+@pytest.mark.parametrize("layers,batch,kv,group,k_budget,v_bits,kind,tin,tout,n_q,longest,n_splits", PACKED)
+def test_cross_attention_of_many_short_sequences(rotations, layers, batch, kv, group, k_budget, v_bits, kind, tin, tout, n_q,
+                                                 longest, n_splits):
+    dt = torch.bfloat16 if tout == "bf16" else torch.float32
+    rng = np.random.default_rng(91)
+    lens = [int(x) for x in rng.integers(0, longest + 1, batch)]
+    lens[0], lens[1], lens[-1], lens[5] = longest, 0, 64, 1
+    cap = (longest + 63) // 64 * 64
+    pk = Packed(rotations, 92, layers=layers, batch=batch, kv=kv, group=group, cap=cap, k_budget=k_budget, v_bits=v_bits,
+                kind=kind, dtype=tin, behind=float("inf"), lens=lens)
+    q, qd = pk.queries((layers, batch, n_q))
+    bad = {2: -1, 6: longest + 1, batch - 2: 1 << 30}
+    dev = i32([bad.get(b, n) for b, n in enumerate(lens)])
+    qd[0, 7, 0, 0] = float("nan")
+    ref, bound = expect_cross(pk, q, lens, dt)
+    if layers > 1:
+        out = bg.blockgtq_cross_attn(pk.cfg, pk.layout, -1, qd, dev, longest, pk.cache, n_splits=n_splits, out_dtype=dt)
+    else:
+        out = bg.blockgtq_cross_attn(pk.cfg, pk.layout, 0, qd[0], dev, longest, pk.cache, n_splits=n_splits, out_dtype=dt)[None]
+    assert all(torch.isnan(out[:, b]).all() for b in bad) and (out[:, 1] == 0).all()
+    if lens[7]:
+        assert torch.isnan(out[0, 7, 0, 0]).all()
+    out[0, 7, 0, 0] = 0
+    ref[0, 7, 0, 0] = 0
+    good = [b for b in range(batch) if b not in bad]
+    check("good rows", out[:, good], ref[:, good], bound[:, good])
+
+
 # ---------------------------------------------------------------- many query rows
 
 WIDE = [
@@ -485,6 +529,33 @@ def test_shared_prefix_wide_pass(rotations, tout):
             hs = slice(8 * h, 8 * h + 8)
             k, v = (np.concatenate([getattr(pp, n)[0, 0, h, :prefix], getattr(pk, n)[0, b, h, :lens[b]]]) for n in "kv")
             check(f"seq {b} head {h}", out[b, hs], *attention_and_bound(q[0, b, hs], k, v, pk.bits[0, h], pk.rot_k, pk.rot_v, dt))
+
+
+@pytest.mark.parametrize("layers,batch,kv,group,prefix,longest", [(1, 40, 8, 4, 500, 200), (4, 17, 8, 4, 300, 130),
+                                                                  (1, 70, 4, 8, 700, 320)])
+def test_shared_prefix_of_many_short_sequences(rotations, layers, batch, kv, group, prefix, longest):
+    """The sequences' own rows in workgroups of several sequences, in one launch with the prefix's."""
+    rng = np.random.default_rng(37)
+    lens = [int(x) for x in rng.integers(0, longest + 1, batch)]
+    lens[0], lens[1], lens[-1] = longest, 0, 1
+    kw = dict(layers=layers, kv=kv, group=group)
+    pk = Packed(rotations, 38, batch=batch, cap=320, behind=float("nan"), lens=lens, **kw)
+    pp = Packed(rotations, 39, cap=704, layout_of=pk, behind=float("inf"), lens=[prefix], **kw)
+    q, qd = pk.queries((layers, batch))
+    dev = i32([longest + 1 if b == 4 else n for b, n in enumerate(lens)])
+    out = bg.blockgtq_decode_attn_shared(pk.cfg, pk.layout, -1, qd, pp.cfg, pp.cache, i32([prefix]), prefix, dev, longest,
+                                         pk.cache, out_dtype=torch.bfloat16)
+    assert torch.isnan(out[:, 4]).all()
+    for li in range(layers):
+        for b in range(batch):
+            for h in (0, kv - 1):
+                if b == 4:
+                    continue
+                hs = slice(group * h, group * h + group)
+                k, v = (np.concatenate([getattr(pp, n)[li, 0, h, :prefix], getattr(pk, n)[li, b, h, :lens[b]]]) for n in "kv")
+                ref, bound = attention_and_bound(q[li, b, hs], k, v, pk.bits[li, h], pk.rot_k, pk.rot_v, torch.bfloat16)
+                off = np.abs(out[li, b, hs].double().cpu().numpy() - ref)
+                assert (off <= bound).all(), (li, b, h, float((off / bound).max()))
 
 
 def test_shared_lengths_outside_the_bound(rotations):
