@@ -19,6 +19,18 @@
 //    O^T = V^T P^T as they are.  Its k runs over the tokens {4 hf + i, 8 + 4 hf
 //    + i} of a 16-token step, and a lane (dim, hf) decodes just those from the
 //    value tile, where the codes of a dim lie one after the other.
+//
+// What bounds it.  A small call is one chain of latencies, 16 us (38K cycles)
+// for a workgroup with a tile per wave: 15K of set-up (arguments, tables, the
+// query rotation), 9K the tile (5.3K QK, 0.8K the maximum, 1.9K PV: lookups that
+// wait on LDS with two waves a SIMD), 8K for joining the waves, the output
+// rotation and the store.  A long pass takes 5.4 to 6.2 us for every tile of
+// each wave.  32 query rows are one column block of the product; a second
+// block's accumulators and operands do not fit the 256 registers of two waves
+// a SIMD, and one wave a SIMD waits on each lookup.  Measured in a call: 8
+// sequences x 8 KV heads x 4 query rows on 150 to 1500 rows 21 us; 64 query rows
+// of 32 layers x 8 heads on 4001 rows and 4 each on 20 to 300 rows 190 us, 740
+// GB/s and 185 TFLOP/s of what the definition asks for.
 #pragma once
 #include <hip/hip_runtime.h>
 

@@ -21,6 +21,10 @@
 // bf16 outputs take one product: the matrix and r c rounded to fp16 (2^-11 each,
 // against the output's own 2^-8).  fp32 outputs take hi and lo parts of both (a
 // product of two fp16 numbers fits in them exactly), without lo x lo.
+//
+// What bounds it: writing the rows.  65536 rows x 8 heads of K2V2 to bf16: 107 us for 308
+// MB, 2.9 TB/s (72 us without the stores; keys alone 46, values alone 38).  A few
+// rows: the keys' matrix, about 10 of the 16 us of 16 rows of 32 layers x 8 heads.
 #include <hip/hip_runtime.h>
 
 #include <algorithm>
