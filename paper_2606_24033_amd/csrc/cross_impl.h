@@ -150,6 +150,29 @@ __device__ __forceinline__ uint32_t top16(const float (&x)[8]) {
 // A 16 x 128 block of a matrix (the lane's operands: row lane % 16, columns 32
 // (lane / 16) .. + 31 in m, times 2^8) times 16 NC staged rows, three fp16
 // products: acc[c] = rows 16 c + lane % 16 of the 16 results 4 (lane / 16) ..
+// Its 32 columns in four steps of 8 a lane: step u's operand parts, and products.
+__device__ __forceinline__ void matrix_parts(const float4_t (&m)[8], int u, half8_t& hi, half8_t& lo) {
+  float x[8];
+#pragma unroll
+  for (int j = 0; j < 8; ++j) x[j] = m[2 * u + (j >> 2)][j & 3] * 256.f;
+  split8(x, hi, lo);
+}
+template <int NC>
+__device__ __forceinline__ void staged_step(const uint8_t* src, int u, const half8_t& wh, const half8_t& wl,
+                                            float4_t (&acc)[NC]) {
+  half8_t bh[NC], bl[NC];
+#pragma unroll
+  for (int c = 0; c < NC; ++c) {
+    bh[c] = *reinterpret_cast<const half8_t*>(src + 16 * c * kHalfStride + 16 * u);
+    bl[c] = *reinterpret_cast<const half8_t*>(src + kHalfPart + 16 * c * kHalfStride + 16 * u);
+  }
+#pragma unroll
+  for (int c = 0; c < NC; ++c) acc[c] = __builtin_amdgcn_mfma_f32_16x16x32_f16(wh, bh[c], acc[c], 0, 0, 0);
+#pragma unroll
+  for (int c = 0; c < NC; ++c) acc[c] = __builtin_amdgcn_mfma_f32_16x16x32_f16(wl, bh[c], acc[c], 0, 0, 0);
+#pragma unroll
+  for (int c = 0; c < NC; ++c) acc[c] = __builtin_amdgcn_mfma_f32_16x16x32_f16(wh, bl[c], acc[c], 0, 0, 0);
+}
 template <int NC>
 __device__ __forceinline__ void staged_product(const uint8_t* staged, const float4_t (&m)[8], int lane, float4_t (&acc)[NC]) {
   const uint8_t* src = staged + (lane & 15) * kHalfStride + 64 * (lane >> 4);
@@ -157,23 +180,9 @@ __device__ __forceinline__ void staged_product(const uint8_t* staged, const floa
   for (int c = 0; c < NC; ++c) acc[c] = float4_t{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
   for (int u = 0; u < 4; ++u) {
-    float x[8];
-#pragma unroll
-    for (int j = 0; j < 8; ++j) x[j] = m[2 * u + (j >> 2)][j & 3] * 256.f;
     half8_t wh, wl;
-    split8(x, wh, wl);
-    half8_t bh[NC], bl[NC];
-#pragma unroll
-    for (int c = 0; c < NC; ++c) {
-      bh[c] = *reinterpret_cast<const half8_t*>(src + 16 * c * kHalfStride + 16 * u);
-      bl[c] = *reinterpret_cast<const half8_t*>(src + kHalfPart + 16 * c * kHalfStride + 16 * u);
-    }
-#pragma unroll
-    for (int c = 0; c < NC; ++c) acc[c] = __builtin_amdgcn_mfma_f32_16x16x32_f16(wh, bh[c], acc[c], 0, 0, 0);
-#pragma unroll
-    for (int c = 0; c < NC; ++c) acc[c] = __builtin_amdgcn_mfma_f32_16x16x32_f16(wl, bh[c], acc[c], 0, 0, 0);
-#pragma unroll
-    for (int c = 0; c < NC; ++c) acc[c] = __builtin_amdgcn_mfma_f32_16x16x32_f16(wh, bl[c], acc[c], 0, 0, 0);
+    matrix_parts(m, u, wh, wl);
+    staged_step<NC>(src, u, wh, wl, acc);
   }
 }
 
