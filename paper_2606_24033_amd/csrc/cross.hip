@@ -32,7 +32,7 @@ constexpr long kMergeGrid = 512;  // workgroups of a join of many rows: the two 
 // RW query rows of a workgroup; a row's partials are shared out to 16 / RW
 // groups of 32 threads (4 dims each), four slots at a time.  Bound by reading
 // the partials where there are many (32768 rows x 2 slots, 43 MB read and
-// written, 25 us: 1.7 TB/s), by its latency (5 us) otherwise.
+// written, 18 us: 2.4 TB/s), by its latency (5 us) otherwise.
 template <int RW>
 __global__ __launch_bounds__(kThreads) void k_cross_merge(const uint8_t* __restrict__ blob, const float* __restrict__ part,
                                                           int n_slots, long n_rows, void* __restrict__ out, int out_dtype) {

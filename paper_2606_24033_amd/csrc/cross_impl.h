@@ -42,9 +42,7 @@
 namespace bgtq {
 namespace cross_detail {
 
-using split_detail::as_half4;
 using split_detail::decode4;
-using split_detail::field_at;
 using split_detail::half4_t;
 using split_detail::LaneRep;
 using split_detail::ld_at;
@@ -81,10 +79,6 @@ constexpr int kAccStride = kHeadDim + 4;
 constexpr int kEndM = kWaves * kRows * kAccStride * 4;
 constexpr int kEndTiles = kEndM + 2 * kWaves * kRows * 4;  // per wave: tiles of its sequence, -1 for a refused length
 static_assert(kEndTiles + kWaves * 4 <= kLds, "merge area");
-
-__device__ __forceinline__ float half_bits(uint32_t b) {
-  return static_cast<float>(__builtin_bit_cast(_Float16, static_cast<uint16_t>(b)));
-}
 
 __device__ __forceinline__ void store4(void* out, size_t i, const float4_t& y, int dtype) {  // BGTQ_BF16 = 1
   if (dtype == 1) {

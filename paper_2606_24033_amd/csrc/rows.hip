@@ -37,7 +37,6 @@ namespace bgtq {
 namespace {
 
 using split_detail::field_at;
-using split_detail::ld_at;
 typedef _Float16 half8_t __attribute__((ext_vector_type(8)));
 typedef _Float16 half2_t __attribute__((ext_vector_type(2)));
 typedef float float4_t __attribute__((ext_vector_type(4)));
