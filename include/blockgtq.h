@@ -345,6 +345,9 @@ int blockgtq_decode_attn_noalloc(const bgtq_config* cfg, const void* d_layout, i
  * d_read_pos: int32 [batch].  d_ctx_len: int32 [batch], or NULL.  A row at a
  * position below 0, at or past the capacity, or at or past d_ctx_len[b] is not
  * read and its outputs are left as they were.
+ * Every group's dims are computed with that group's radius alone.  A radius that
+ * is not finite (a norm past fp16's range) gives numbers that are not finite: in
+ * its group's dims of the key, or in the whole value row, and nowhere else.
  * n_rows in [0, capacity] (ECAPACITY above). */
 int blockgtq_dequantize_rows(const bgtq_config* cfg, const void* d_layout, int32_t layer, const bgtq_cache* cache,
                              int32_t n_rows, const int32_t* d_read_pos, const int32_t* d_ctx_len, void* d_k_out,

@@ -12,15 +12,16 @@
 // 2^8 and 1 / sqrt(d_g)), built once per workgroup, which then walks many
 // tiles.  A workgroup does keys or values.
 //  * Keys: lane = token decodes 16 positions of one group, two codes a lookup,
-//    multiplies by the group's radius (scaled per token so that neither fp16's
-//    range nor its subnormals are reached) and v_permlane32_swap turns the 64
-//    tokens' registers into B operands of two 32-token blocks.
+//    and v_permlane32_swap turns the 64 tokens' registers into B operands of
+//    two 32-token blocks.  A dim's row of the matrix is zero outside its own
+//    group, so the group's radius scales the result, dim by dim, in fp32: a
+//    group's dims are as exact as its own radius whatever the others are, and a
+//    radius that is not finite stays in its group's dims.
 //  * Values: codes lie dim after dim, so a 32-token tile is decoded lane = dim
 //    into LDS and read back lane = token.  The bare centroids are the operand;
 //    the radius scales the result.
-// bf16 outputs take one product: the matrix and r c rounded to fp16 (2^-11 each,
-// against the output's own 2^-8).  fp32 outputs take hi and lo parts of both (a
-// product of two fp16 numbers fits in them exactly), without lo x lo.
+// Centroids are fp16 numbers, exact as operands.  fp32 outputs take hi and lo
+// parts of the matrix (two products); bf16 ones its hi part.
 //
 // What bounds it: writing the rows.  65536 rows x 8 heads of K2V2 to bf16: 107 us for 308
 // MB, 2.9 TB/s (72 us without the stores; keys alone 46, values alone 38).  A few
@@ -54,7 +55,10 @@ constexpr int kPair = 1024;
 constexpr int kMaxPair = 6;
 __host__ __device__ constexpr int pair_offset(int b) { return kPair + 4 * (((1 << (2 * b)) - 4) / 3); }
 constexpr int kDims = pair_offset(kMaxPair + 1);  // a key row's stream position -> dim
-constexpr int kMat = (kDims + kHeadDim + 15) / 16 * 16;
+// by 4 dims, 16 bytes: byte selectors that pick the dims' radii (2 bytes each)
+// from the token's 8: among groups 0-3, then 4-7 (the other half's select zero)
+constexpr int kSel = (kDims + kHeadDim + 15) / 16 * 16;
+constexpr int kMat = kSel + kHeadDim / 4 * 16;
 constexpr int kVSteps = kHeadDim / 16;
 constexpr int kTileStride = (kHeadDim + 8) * 2;  // bytes of a decoded token
 constexpr int kTileBytes = kTile * kTileStride;
@@ -96,6 +100,12 @@ __device__ __forceinline__ void swap4(uint32_t (&x)[4], uint32_t (&y)[4]) {
       "v_permlane32_swap_b32 %3, %7\n\t"
       "s_nop 1"
       : "+v"(x[0]), "+v"(x[1]), "+v"(x[2]), "+v"(x[3]), "+v"(y[0]), "+v"(y[1]), "+v"(y[2]), "+v"(y[3]));
+}
+// x = the lower half-wave's value, y = the upper one's, in both.
+__device__ __forceinline__ void spread4(uint32_t (&x)[4], uint32_t (&y)[4]) {
+#pragma unroll
+  for (int i = 0; i < 4; ++i) y[i] = x[i];
+  swap4(x, y);
 }
 __device__ __forceinline__ half8_t as_half8(const uint32_t (&x)[4]) {
   return __builtin_bit_cast(half8_t, make_uint4(x[0], x[1], x[2], x[3]));
@@ -199,10 +209,9 @@ __device__ __forceinline__ void store_rows(const float16_t (&acc)[4], float scal
 // Group of width B: its positions of the 64 tokens into the accumulators.
 template <int B, int KWB, bool EX>
 __device__ __forceinline__ void key_group(const uint8_t* smem, const uint32_t (&rw)[KWB + split_detail::kRowPad],
-                                          uint32_t gm, int step0, _Float16 radius, int lane, float16_t (&acc)[2][4]) {
+                                          uint32_t gm, int step0, int lane, float16_t (&acc)[2][4]) {
   constexpr int NW = (16 * B + 31) / 32;
   const int o = split_detail::gm_off(gm), n16 = (split_detail::gm_steps(gm) + 3) >> 2;
-  const half2_t r = {radius, radius};
   for (int c = 0; c < n16; ++c) {
     const int at = o + c * 16 * B, w0 = at >> 5, sh = at & 31;
     uint32_t aw[NW + 1];
@@ -221,26 +230,19 @@ __device__ __forceinline__ void key_group(const uint8_t* smem, const uint32_t (&
       if constexpr (EX) lows[cc] = *reinterpret_cast<const half8_t*>(mat + kMaxSteps * 4096 + cc * 1024);
     }
     __builtin_amdgcn_sched_barrier(0);
-    uint32_t hi[2][4], lo[2][4];
+    uint32_t code[2][4];
 #pragma unroll
-    for (int u = 0; u < 8; ++u) {
-      const half2_t h = r * y[u];
-      hi[u >> 2][u & 3] = __builtin_bit_cast(uint32_t, h);
-      if constexpr (EX) lo[u >> 2][u & 3] = __builtin_bit_cast(uint32_t, __builtin_elementwise_fma(r, y[u], -h));
-    }
-    swap4(hi[0], hi[1]);
-    if constexpr (EX) swap4(lo[0], lo[1]);
+    for (int u = 0; u < 8; ++u) code[u >> 2][u & 3] = __builtin_bit_cast(uint32_t, y[u]);
+    swap4(code[0], code[1]);
 #pragma unroll
     for (int cc = 0; cc < 4; ++cc) {
-      const half8_t w = ops[cc];
 #pragma unroll
-      for (int n = 0; n < 2; ++n) acc[n][cc] = __builtin_amdgcn_mfma_f32_32x32x16_f16(w, as_half8(hi[n]), acc[n][cc], 0, 0, 0);
+      for (int n = 0; n < 2; ++n)
+        acc[n][cc] = __builtin_amdgcn_mfma_f32_32x32x16_f16(ops[cc], as_half8(code[n]), acc[n][cc], 0, 0, 0);
       if constexpr (EX) {
-        const half8_t wl = lows[cc];
 #pragma unroll
-        for (int n = 0; n < 2; ++n) acc[n][cc] = __builtin_amdgcn_mfma_f32_32x32x16_f16(w, as_half8(lo[n]), acc[n][cc], 0, 0, 0);
-#pragma unroll
-        for (int n = 0; n < 2; ++n) acc[n][cc] = __builtin_amdgcn_mfma_f32_32x32x16_f16(wl, as_half8(hi[n]), acc[n][cc], 0, 0, 0);
+        for (int n = 0; n < 2; ++n)
+          acc[n][cc] = __builtin_amdgcn_mfma_f32_32x32x16_f16(lows[cc], as_half8(code[n]), acc[n][cc], 0, 0, 0);
       }
     }
   }
@@ -249,23 +251,43 @@ __device__ __forceinline__ void key_group(const uint8_t* smem, const uint32_t (&
 template <int KWB, bool EX, int... BM1>
 __device__ __forceinline__ void key_groups(std::integer_sequence<int, BM1...>, const uint8_t* smem,
                                            const uint32_t (&rw)[KWB + split_detail::kRowPad], const uint32_t (&gm)[8],
-                                           const uint32_t (&radii)[4], half2_t up, int lane, float16_t (&acc)[2][4]) {
+                                           int lane, float16_t (&acc)[2][4]) {
   int step0 = 0;
   const auto one = [&](auto bm1) __attribute__((always_inline)) {
     constexpr int b = decltype(bm1)::value;
     if (gm[b] >> 31) {
-      const uint32_t r = split_detail::radius_bits(radii, split_detail::gm_plane(gm[b]));
-      key_group<b + 1, KWB, EX>(smem, rw, gm[b], step0, __builtin_bit_cast(_Float16, static_cast<uint16_t>(r)) * up[0], lane, acc);
+      key_group<b + 1, KWB, EX>(smem, rw, gm[b], step0, lane, acc);
       step0 += (split_detail::gm_steps(gm[b]) + 3) >> 2;
     }
   };
   (one(std::integral_constant<int, BM1>{}), ...);
 }
 
+// Each dim times its group's radius: r[n] = the 8 radii of token l32 of block n.
+__device__ __forceinline__ void scale_keys(const uint8_t* smem, const uint32_t (&r)[2][4], int lane, float16_t (&acc)[2][4]) {
+#pragma unroll
+  for (int cc = 0; cc < 4; ++cc)
+#pragma unroll
+    for (int u = 0; u < 4; ++u) {  // dims 32 cc + 8 u + 4 hf .. + 3
+      const uint4 sel = *reinterpret_cast<const uint4*>(smem + kSel + (8 * cc + 2 * u + (lane >> 5)) * 16);
+#pragma unroll
+      for (int n = 0; n < 2; ++n) {
+        const half2_t x = __builtin_bit_cast(half2_t, __builtin_amdgcn_perm(r[n][1], r[n][0], sel.x) |
+                                                          __builtin_amdgcn_perm(r[n][3], r[n][2], sel.z));
+        const half2_t y = __builtin_bit_cast(half2_t, __builtin_amdgcn_perm(r[n][1], r[n][0], sel.y) |
+                                                          __builtin_amdgcn_perm(r[n][3], r[n][2], sel.w));
+        acc[n][cc][4 * u] *= static_cast<float>(x[0]);
+        acc[n][cc][4 * u + 1] *= static_cast<float>(x[1]);
+        acc[n][cc][4 * u + 2] *= static_cast<float>(y[0]);
+        acc[n][cc][4 * u + 3] *= static_cast<float>(y[1]);
+      }
+    }
+}
+
 template <int KWB, bool EX>
 __device__ __forceinline__ void read_keys(uint8_t* smem, const Dims& d, const uint8_t* __restrict__ blob,
                                           const RowsCall& call, int lz, int kvh, int chunk, long pos, int end) {
-  const int tid = threadIdx.x, lane = tid & 63, l32 = lane & 31;
+  const int tid = threadIdx.x, lane = tid & 63;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int layer = d.layer >= 0 ? d.layer : lz / d.batch, seq = lz % d.batch, ri = layer * d.n_kv + kvh;
   const RowMeta* M = reinterpret_cast<const RowMeta*>(blob + kOffRows) + ri;
@@ -325,7 +347,7 @@ __device__ __forceinline__ void read_keys(uint8_t* smem, const Dims& d, const ui
                        static_cast<size_t>(ri) * kRowRotFloats;
     const uint16_t* c16 = reinterpret_cast<const uint16_t*>(blob + kOffC16);
     const uint16_t cv = c16[min(tid, kCodebookEntries - 1)];
-    const uint8_t dv = M->dim[tid & 127];
+    const uint8_t dv = M->dim[tid & 127], gv = M->grp[tid & 127];
     int n_steps = 0, n_items = 0;
 #pragma unroll
     for (int g = 0; g < 8; ++g) {
@@ -337,7 +359,13 @@ __device__ __forceinline__ void read_keys(uint8_t* smem, const Dims& d, const ui
       *reinterpret_cast<uint4*>(smem + kMat + i * 16) = make_uint4(0, 0, 0, 0);
       if constexpr (EX) *reinterpret_cast<uint4*>(smem + kMat + kMaxSteps * 4096 + i * 16) = make_uint4(0, 0, 0, 0);
     }
-    if (tid < kHeadDim) smem[kDims + tid] = dv;
+    if (tid < kHeadDim) {
+      smem[kDims + tid] = dv;
+      const uint16_t sel = static_cast<uint16_t>(2 * (gv & 3) | (2 * (gv & 3) + 1) << 8);
+      uint8_t* at = smem + kSel + (dv >> 2) * 16 + (dv & 3) * 2;
+      *reinterpret_cast<uint16_t*>(at) = gv < 4 ? sel : 0x0C0C;
+      *reinterpret_cast<uint16_t*>(at + 8) = gv < 4 ? 0x0C0C : sel;
+    }
     __syncthreads();
     build_pairs(smem, used, tid);
     for (int i0 = tid; i0 < n_items; i0 += kThreads) {
@@ -383,14 +411,6 @@ __device__ __forceinline__ void read_keys(uint8_t* smem, const Dims& d, const ui
     for (int k = 0; k < 4; ++k) radii[k] = next_radii[k];
     const bool valid = next_valid;
     load(tile + kWaves);
-    // 2^up brings the token's largest radius to [2^12, 2^13)
-    uint32_t top = 0;
-#pragma unroll
-    for (int g = 0; g < kMaxGroups; ++g)
-      if (g < ng) top = max(top, (radii[g >> 1] >> (16 * (g & 1))) & 0x7FFFu);
-    const int e = static_cast<int>(top >> 10);
-    const int up = e == 31 ? 0 : max(-3, min(15, 27 - e));
-    const _Float16 uph = __builtin_bit_cast(_Float16, static_cast<uint16_t>((up + 15) << 10));
     float16_t acc[2][4];
 #pragma unroll
     for (int n = 0; n < 2; ++n)
@@ -398,15 +418,18 @@ __device__ __forceinline__ void read_keys(uint8_t* smem, const Dims& d, const ui
       for (int cc = 0; cc < 4; ++cc)
 #pragma unroll
         for (int k = 0; k < 16; ++k) acc[n][cc][k] = 0.f;
-    key_groups<KWB, EX>(std::make_integer_sequence<int, 8>{}, smem, rw, gm, radii, half2_t{uph, uph}, lane, acc);
-    const float down = __uint_as_float(static_cast<uint32_t>(127 - up) << 23) / kMatScale;
+    key_groups<KWB, EX>(std::make_integer_sequence<int, 8>{}, smem, rw, gm, lane, acc);
+    uint32_t r[2][4];
+#pragma unroll
+    for (int k = 0; k < 4; ++k) r[0][k] = radii[k];
+    spread4(r[0], r[1]);
+    scale_keys(smem, r, lane, acc);
     const unsigned long long ok = __builtin_amdgcn_ballot_w64(valid);
 #pragma unroll
     for (int n = 0; n < 2; ++n) {
       // lane = token 32 n + l32 of the tile
-      const float scale = __shfl(down, 32 * n + l32);
       const long at = ((static_cast<long>(lz) * call.n_rows + tile * 64 + 32 * n) * d.n_kv + kvh) * kHeadDim;
-      store_rows<EX>(acc[n], scale, call.out[0], at, static_cast<long>(d.n_kv) * kHeadDim,
+      store_rows<EX>(acc[n], 1.f / kMatScale, call.out[0], at, static_cast<long>(d.n_kv) * kHeadDim,
                      static_cast<uint32_t>(ok >> (32 * n)), lane);
     }
   }

@@ -1,0 +1,78 @@
+"""GPU tests of the operators that read the packed cache, over the ranges that
+a cache may hold: radii of every size, radii that are not finite, outputs in
+both types, long reads, and each pass over several layers.
+
+Tolerances as in test_gpu_cache_readers.py: element by element from the
+roundings, or in the 2-norm where a single low part that is lost would be
+invisible in a worst-case bound.  Radii are scaled by powers of two that keep
+them normal fp16 numbers, so that a scaled cache holds exactly the scaled rows.
+"""
+import numpy as np
+import pytest
+
+from oracle import blockgtq_oracle as o
+from paper_2606_24033_amd import blockgtq as bg
+from paper_2606_24033_amd import synth
+from tests.test_gpu_cache_readers import Packed, check, expect_rows, i32
+
+pytestmark = pytest.mark.gpu
+
+torch = pytest.importorskip("torch")
+BF16, FP32 = torch.bfloat16, torch.float32
+
+
+@pytest.fixture(scope="module", autouse=True)
+def _require_gpu():
+    if not torch.cuda.is_available():
+        pytest.skip("no GPU")
+    bg.lib()
+
+
+@pytest.fixture(scope="module")
+def rotations():
+    return synth.rotations(7)
+
+
+def key_radii(pk, layer, b, h):
+    """The key radii of a head's rows as they lie in the cache, [capacity, groups] (a view)."""
+    ng = len(o.groups(pk.bits[layer, h]))
+    slots = ng + (ng & 1)
+    return pk.cache.k_norms[layer, b, h, :pk.cfg.capacity * slots].view(pk.cfg.capacity, slots)[:, :ng]
+
+
+@pytest.mark.parametrize("out_dtype", [FP32])
+@pytest.mark.parametrize("k_budget,kind", [(192, "wide"), (128, "mixed")])
+def test_key_groups_of_very_different_radii(rotations, k_budget, kind, out_dtype):
+    """Each group's dims to the precision of its own radius, beside groups whose radii are 2^21 times as large."""
+    pk = Packed(rotations, 102, k_budget=k_budget, kind=kind)
+    groups = o.groups(pk.bits[0, 0])
+    for g, (_, dims) in enumerate(groups):
+        s = 2.0 ** (10 - round(21 * g / (len(groups) - 1)))
+        key_radii(pk, 0, 0, 0)[:, g] *= s
+        pk.k[0, 0, 0][:, dims] *= s
+    k, _ = bg.blockgtq_dequantize_rows(pk.cfg, pk.layout, 0, pk.cache, i32([0]), 192, out_dtype=out_dtype)
+    ref, bound = expect_rows(pk, 0, 0, 0, "k", 0, 192, FP32)
+    check("k", k[0, :, 0], ref, bound)
+
+
+@pytest.mark.parametrize("out_dtype", [FP32, BF16])
+@pytest.mark.parametrize("bad", [float("inf"), float("nan")])
+def test_a_radius_that_is_not_finite_reads_back_in_its_place_only(rotations, bad, out_dtype):
+    """A key group's radius: not finite in the group's dims of that row, every other number as without it.  A value
+    radius: not finite in that row."""
+    pk = Packed(rotations, 103, kv=2, k_budget=192, v_bits=3, kind="wide")
+    args = (pk.cfg, pk.layout, 0, pk.cache, i32([0]), 192)
+    k0, v0 = bg.blockgtq_dequantize_rows(*args, out_dtype=out_dtype)
+    touched = torch.zeros(k0.shape, dtype=torch.bool, device="cuda")
+    for h in range(2):
+        for g, (_, dims) in enumerate(o.groups(pk.bits[0, h])):
+            for row in (g, 40 + 3 * g, 191 - g):
+                key_radii(pk, 0, 0, h)[row, g] = bad
+                touched[0, row, h, torch.from_numpy(dims).cuda()] = True
+    rows = torch.tensor([0, 31, 32, 100, 191], device="cuda")
+    pk.cache.v_norms[0, 0, 1, rows] = bad
+    k, v = bg.blockgtq_dequantize_rows(*args, out_dtype=out_dtype)
+    assert torch.equal(k[~touched], k0[~touched]) and not torch.isfinite(k[touched]).any()
+    assert not torch.isfinite(v[0, rows, 1]).any()
+    v[0, rows, 1] = v0[0, rows, 1]
+    assert torch.equal(v, v0)
