@@ -338,7 +338,8 @@ int blockgtq_decode_attn_noalloc(const bgtq_config* cfg, const void* d_layout, i
  * allocation, no workspace.
  * layer in [0, n_layers) or -1 for all layers.
  * Rows d_read_pos[b] .. d_read_pos[b] + n_rows - 1 of sequence b go to d_k_out
- * and d_v_out in out_dtype (BGTQ_FP32 or BGTQ_BF16, rounded once), laid out as
+ * and d_v_out in out_dtype (BGTQ_FP32, or BGTQ_BF16: the fp32 result rounded
+ * once), laid out as
  * the append's inputs: [batch][n_rows][n_kv_heads][head_dim], with a leading
  * [n_layers] for layer == -1; 16-byte aligned (EINVAL otherwise).  Either may
  * be NULL (not both): only the other one is read.

@@ -20,8 +20,10 @@
 //  * Values: codes lie dim after dim, so a 32-token tile is decoded lane = dim
 //    into LDS and read back lane = token.  The bare centroids are the operand;
 //    the radius scales the result.
-// Centroids are fp16 numbers, exact as operands.  fp32 outputs take hi and lo
-// parts of the matrix (two products); bf16 ones its hi part.
+// Centroids are fp16 numbers, exact as operands; the matrix is in hi and lo
+// parts (22 bits, two products).  bf16 outputs are the fp32 result rounded: with
+// the hi part alone, 2^-11 of each term, 12 % of them would be another bf16 number
+// and elements whose terms cancel off by many of their own steps.
 //
 // What bounds it: writing the rows.  65536 rows x 8 heads of K2V2 to bf16: 107 us for 308
 // MB, 2.9 TB/s (72 us without the stores; keys alone 46, values alone 38).  A few
@@ -62,13 +64,9 @@ constexpr int kMat = kSel + kHeadDim / 4 * 16;
 constexpr int kVSteps = kHeadDim / 16;
 constexpr int kTileStride = (kHeadDim + 8) * 2;  // bytes of a decoded token
 constexpr int kTileBytes = kTile * kTileStride;
-template <bool EX>
-constexpr int lds_bytes() {
-  constexpr int parts = EX ? 2 : 1;
-  constexpr int keys = parts * kMaxSteps * 4096, values = parts * kVSteps * 4096 + kWaves * kTileBytes;
-  return kMat + (keys > values ? keys : values);
-}
-static_assert(lds_bytes<true>() <= 160 * 1024, "LDS of one workgroup");
+constexpr int kKeyBytes = 2 * kMaxSteps * 4096, kValueBytes = 2 * kVSteps * 4096 + kWaves * kTileBytes;
+constexpr int kLds = kMat + (kKeyBytes > kValueBytes ? kKeyBytes : kValueBytes);
+static_assert(kLds <= 160 * 1024, "LDS of one workgroup");
 
 struct RowsCall {
   CachePtrs c;
@@ -126,8 +124,7 @@ __device__ __forceinline__ void build_pairs(uint8_t* smem, uint32_t used, int ti
       }
 }
 
-// One operand of the matrix: 8 numbers, rounded (and their residuals).
-template <bool EX>
+// One operand of the matrix: 8 numbers, rounded, and their residuals.
 __device__ __forceinline__ void store_operand(uint8_t* dst, int part_bytes, float (&x)[8]) {
   half8_t hi, lo;
 #pragma unroll
@@ -136,10 +133,10 @@ __device__ __forceinline__ void store_operand(uint8_t* dst, int part_bytes, floa
     // way of fp32 in the other gives two different hi parts next to a tie)
     asm volatile("" : "+v"(x[j]));
     hi[j] = static_cast<_Float16>(x[j]);
-    if constexpr (EX) lo[j] = static_cast<_Float16>(x[j] - static_cast<float>(hi[j]));
+    lo[j] = static_cast<_Float16>(x[j] - static_cast<float>(hi[j]));
   }
   *reinterpret_cast<half8_t*>(dst) = hi;
-  if constexpr (EX) *reinterpret_cast<half8_t*>(dst + part_bytes) = lo;
+  *reinterpret_cast<half8_t*>(dst + part_bytes) = lo;
 }
 
 // Rows of 16 lanes: the odd ones of x change places with the even ones of y.
@@ -158,7 +155,7 @@ __device__ __forceinline__ void swap_rows4(uint32_t (&x)[4], uint32_t (&y)[4]) {
 // element at0 + j stride).  A store as the registers lie has 16 bytes of a row
 // from each half-wave; lanes change places until it has 64 contiguous ones of
 // 16 rows (the memory takes 32-byte pieces at half the rate).
-template <bool EX>
+template <bool F32>
 __device__ __forceinline__ void store_rows(const float16_t (&acc)[4], float scale, void* out, long at0, long stride,
                                            uint32_t valid, int lane) {
   const int l16 = lane & 15, r1 = (lane >> 4) & 1, hf = lane >> 5;
@@ -167,7 +164,7 @@ __device__ __forceinline__ void store_rows(const float16_t (&acc)[4], float scal
   for (int cc = 0; cc < 4; ++cc) {
     float16_t y = acc[cc];
     y *= scale;
-    if constexpr (EX) {
+    if constexpr (F32) {
 #pragma unroll
       for (int v = 0; v < 2; ++v) {  // dims 16 v .. + 15 of the block
         uint32_t a[4], b[4];
@@ -207,7 +204,7 @@ __device__ __forceinline__ void store_rows(const float16_t (&acc)[4], float scal
 
 // ---------------------------------------------------------------- keys
 // Group of width B: its positions of the 64 tokens into the accumulators.
-template <int B, int KWB, bool EX>
+template <int B, int KWB>
 __device__ __forceinline__ void key_group(const uint8_t* smem, const uint32_t (&rw)[KWB + split_detail::kRowPad],
                                           uint32_t gm, int step0, int lane, float16_t (&acc)[2][4]) {
   constexpr int NW = (16 * B + 31) / 32;
@@ -227,7 +224,7 @@ __device__ __forceinline__ void key_group(const uint8_t* smem, const uint32_t (&
 #pragma unroll
     for (int cc = 0; cc < 4; ++cc) {
       ops[cc] = *reinterpret_cast<const half8_t*>(mat + cc * 1024);
-      if constexpr (EX) lows[cc] = *reinterpret_cast<const half8_t*>(mat + kMaxSteps * 4096 + cc * 1024);
+      lows[cc] = *reinterpret_cast<const half8_t*>(mat + kMaxSteps * 4096 + cc * 1024);
     }
     __builtin_amdgcn_sched_barrier(0);
     uint32_t code[2][4];
@@ -239,16 +236,14 @@ __device__ __forceinline__ void key_group(const uint8_t* smem, const uint32_t (&
 #pragma unroll
       for (int n = 0; n < 2; ++n)
         acc[n][cc] = __builtin_amdgcn_mfma_f32_32x32x16_f16(ops[cc], as_half8(code[n]), acc[n][cc], 0, 0, 0);
-      if constexpr (EX) {
 #pragma unroll
-        for (int n = 0; n < 2; ++n)
-          acc[n][cc] = __builtin_amdgcn_mfma_f32_32x32x16_f16(lows[cc], as_half8(code[n]), acc[n][cc], 0, 0, 0);
-      }
+      for (int n = 0; n < 2; ++n)
+        acc[n][cc] = __builtin_amdgcn_mfma_f32_32x32x16_f16(lows[cc], as_half8(code[n]), acc[n][cc], 0, 0, 0);
     }
   }
 }
 
-template <int KWB, bool EX, int... BM1>
+template <int KWB, int... BM1>
 __device__ __forceinline__ void key_groups(std::integer_sequence<int, BM1...>, const uint8_t* smem,
                                            const uint32_t (&rw)[KWB + split_detail::kRowPad], const uint32_t (&gm)[8],
                                            int lane, float16_t (&acc)[2][4]) {
@@ -256,7 +251,7 @@ __device__ __forceinline__ void key_groups(std::integer_sequence<int, BM1...>, c
   const auto one = [&](auto bm1) __attribute__((always_inline)) {
     constexpr int b = decltype(bm1)::value;
     if (gm[b] >> 31) {
-      key_group<b + 1, KWB, EX>(smem, rw, gm[b], step0, lane, acc);
+      key_group<b + 1, KWB>(smem, rw, gm[b], step0, lane, acc);
       step0 += (split_detail::gm_steps(gm[b]) + 3) >> 2;
     }
   };
@@ -284,7 +279,7 @@ __device__ __forceinline__ void scale_keys(const uint8_t* smem, const uint32_t (
     }
 }
 
-template <int KWB, bool EX>
+template <int KWB, bool F32>
 __device__ __forceinline__ void read_keys(uint8_t* smem, const Dims& d, const uint8_t* __restrict__ blob,
                                           const RowsCall& call, int lz, int kvh, int chunk, long pos, int end) {
   const int tid = threadIdx.x, lane = tid & 63;
@@ -357,7 +352,7 @@ __device__ __forceinline__ void read_keys(uint8_t* smem, const Dims& d, const ui
     if (tid < kCodebookEntries) reinterpret_cast<uint16_t*>(smem + kBooks)[tid] = cv;
     for (int i = tid; i < n_steps * 256; i += kThreads) {
       *reinterpret_cast<uint4*>(smem + kMat + i * 16) = make_uint4(0, 0, 0, 0);
-      if constexpr (EX) *reinterpret_cast<uint4*>(smem + kMat + kMaxSteps * 4096 + i * 16) = make_uint4(0, 0, 0, 0);
+      *reinterpret_cast<uint4*>(smem + kMat + kMaxSteps * 4096 + i * 16) = make_uint4(0, 0, 0, 0);
     }
     if (tid < kHeadDim) {
       smem[kDims + tid] = dv;
@@ -395,7 +390,7 @@ __device__ __forceinline__ void read_keys(uint8_t* smem, const Dims& d, const ui
         x[j] = v[0] * scale;
         x[j + 1] = v[1] * scale;
       }
-      store_operand<EX>(smem + kMat + (st + (j0 >> 4)) * 4096 + (dim >> 5) * 1024 + (((j0 >> 3) & 1) * 32 + (dim & 31)) * 16,
+      store_operand(smem + kMat + (st + (j0 >> 4)) * 4096 + (dim >> 5) * 1024 + (((j0 >> 3) & 1) * 32 + (dim & 31)) * 16,
                         kMaxSteps * 4096, x);
     }
   }
@@ -418,7 +413,7 @@ __device__ __forceinline__ void read_keys(uint8_t* smem, const Dims& d, const ui
       for (int cc = 0; cc < 4; ++cc)
 #pragma unroll
         for (int k = 0; k < 16; ++k) acc[n][cc][k] = 0.f;
-    key_groups<KWB, EX>(std::make_integer_sequence<int, 8>{}, smem, rw, gm, lane, acc);
+    key_groups<KWB>(std::make_integer_sequence<int, 8>{}, smem, rw, gm, lane, acc);
     uint32_t r[2][4];
 #pragma unroll
     for (int k = 0; k < 4; ++k) r[0][k] = radii[k];
@@ -429,7 +424,7 @@ __device__ __forceinline__ void read_keys(uint8_t* smem, const Dims& d, const ui
     for (int n = 0; n < 2; ++n) {
       // lane = token 32 n + l32 of the tile
       const long at = ((static_cast<long>(lz) * call.n_rows + tile * 64 + 32 * n) * d.n_kv + kvh) * kHeadDim;
-      store_rows<EX>(acc[n], 1.f / kMatScale, call.out[0], at, static_cast<long>(d.n_kv) * kHeadDim,
+      store_rows<F32>(acc[n], 1.f / kMatScale, call.out[0], at, static_cast<long>(d.n_kv) * kHeadDim,
                      static_cast<uint32_t>(ok >> (32 * n)), lane);
     }
   }
@@ -463,7 +458,7 @@ __device__ __forceinline__ void decode_values(const uint8_t* smem, uint8_t* tile
 
 // The wave's tiles first, first + 8, .. below last, of cache tiles that hold a
 // row below end; the next one's words are in flight.
-template <bool EX, int BV>
+template <bool F32, int BV>
 __device__ __forceinline__ void value_tiles(const uint8_t* smem, uint8_t* mine, const Dims& d, const RowsCall& call,
                                             const uint32_t* __restrict__ vc, const uint16_t* __restrict__ vn, long first,
                                             long last, long pos, int end, int lz, int kvh, int lane) {
@@ -504,21 +499,19 @@ __device__ __forceinline__ void value_tiles(const uint8_t* smem, uint8_t* mine, 
 #pragma unroll
       for (int cc = 0; cc < 4; ++cc)
         acc[cc] = __builtin_amdgcn_mfma_f32_32x32x16_f16(*reinterpret_cast<const half8_t*>(mat + cc * 1024), y, acc[cc], 0, 0, 0);
-      if constexpr (EX) {
 #pragma unroll
-        for (int cc = 0; cc < 4; ++cc)
-          acc[cc] = __builtin_amdgcn_mfma_f32_32x32x16_f16(
-              *reinterpret_cast<const half8_t*>(mat + kVSteps * 4096 + cc * 1024), y, acc[cc], 0, 0, 0);
-      }
+      for (int cc = 0; cc < 4; ++cc)
+        acc[cc] = __builtin_amdgcn_mfma_f32_32x32x16_f16(
+            *reinterpret_cast<const half8_t*>(mat + kVSteps * 4096 + cc * 1024), y, acc[cc], 0, 0, 0);
     }
     const long i = t - pos;
     const unsigned long long ok = __builtin_amdgcn_ballot_w64(i >= 0 && i < call.n_rows && t < end);
     const long at = ((static_cast<long>(lz) * call.n_rows + tile * kTile - pos) * d.n_kv + kvh) * kHeadDim;
-    store_rows<EX>(acc, scale, call.out[1], at, static_cast<long>(d.n_kv) * kHeadDim, static_cast<uint32_t>(ok), lane);
+    store_rows<F32>(acc, scale, call.out[1], at, static_cast<long>(d.n_kv) * kHeadDim, static_cast<uint32_t>(ok), lane);
   }
 }
 
-template <bool EX>
+template <bool F32>
 __device__ __forceinline__ void read_values(uint8_t* smem, const Dims& d, const uint8_t* __restrict__ blob,
                                             const RowsCall& call, int lz, int kvh, int chunk, long pos, int end) {
   const int tid = threadIdx.x, lane = tid & 63;
@@ -546,7 +539,7 @@ __device__ __forceinline__ void read_values(uint8_t* smem, const Dims& d, const 
       float x[8];
 #pragma unroll
       for (int j = 0; j < 8; ++j) x[j] = v[u][j >> 2][j & 3] * (kMatScale * 0.08838834764831845f);
-      store_operand<EX>(smem + kMat + (tid + u * kThreads) * 16, kVSteps * 4096, x);
+      store_operand(smem + kMat + (tid + u * kThreads) * 16, kVSteps * 4096, x);
     }
   }
   __syncthreads();
@@ -555,12 +548,12 @@ __device__ __forceinline__ void read_values(uint8_t* smem, const Dims& d, const 
   const int bv = d.v_bits;
   const uint32_t* vc = call.c.v_codes + row * (cap / kTile) * kHeadDim * bv;
   const uint16_t* vn = call.c.v_norms + row * cap;
-  uint8_t* const mine = smem + kMat + (EX ? 2 : 1) * kVSteps * 4096 + wave * kTileBytes;
+  uint8_t* const mine = smem + kMat + 2 * kVSteps * 4096 + wave * kTileBytes;
   // cache tiles from the one that holds the first row
   const long tile0 = pos >> 5, tile_end = (pos + call.n_rows + kTile - 1) >> 5;
   const long at = tile0 + chunk * static_cast<long>(call.tiles[1]), last = min(tile_end, at + call.tiles[1]);
   const auto go = [&](auto b) __attribute__((always_inline)) {
-    value_tiles<EX, decltype(b)::value>(smem, mine, d, call, vc, vn, at + wave, last, pos, end, lz, kvh, lane);
+    value_tiles<F32, decltype(b)::value>(smem, mine, d, call, vc, vn, at + wave, last, pos, end, lz, kvh, lane);
   };
   switch (bv) {
     case 1: go(std::integral_constant<int, 1>{}); break;
@@ -575,10 +568,10 @@ __device__ __forceinline__ void read_values(uint8_t* smem, const Dims& d, const 
 }
 
 // One-dimensional grid: the keys' (unit, chunk) items, then the values'.
-template <int KWB, bool EX>
+template <int KWB, bool F32>
 __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(2, 2))) void k_read_rows(
     Dims d, const uint8_t* __restrict__ blob, RowsCall call) {
-  __shared__ __attribute__((aligned(16))) uint8_t smem[lds_bytes<EX>()];
+  __shared__ __attribute__((aligned(16))) uint8_t smem[kLds];
   const bool keys = static_cast<int>(blockIdx.x) < call.key_items;
   int item = static_cast<int>(blockIdx.x) - (keys ? 0 : call.key_items);
   const int chunks = keys ? call.chunks[0] : call.chunks[1];
@@ -587,8 +580,8 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(2, 2))
   const int kvh = item % d.n_kv, lz = item / d.n_kv, seq = lz % d.batch;
   const long pos = call.read_pos[seq];
   const int end = min(d.capacity, call.ctx_len ? call.ctx_len[seq] : d.capacity);
-  if (keys) read_keys<KWB, EX>(smem, d, blob, call, lz, kvh, chunk, pos, end);
-  else read_values<EX>(smem, d, blob, call, lz, kvh, chunk, pos, end);
+  if (keys) read_keys<KWB, F32>(smem, d, blob, call, lz, kvh, chunk, pos, end);
+  else read_values<F32>(smem, d, blob, call, lz, kvh, chunk, pos, end);
 }
 
 }  // namespace
@@ -621,11 +614,11 @@ hipError_t launch_dequantize_rows(const Dims& d, const void* layout, const Cache
     hipLaunchKernelGGL(kern, dim3(items), dim3(kThreads), 0, s, d, static_cast<const uint8_t*>(layout), call);
     return hipGetLastError();
   };
-  const bool ex = out_dtype == 0;  // BGTQ_FP32
-  if (d.k_words <= 8) return ex ? go(k_read_rows<8, true>) : go(k_read_rows<8, false>);
-  if (d.k_words <= 12) return ex ? go(k_read_rows<12, true>) : go(k_read_rows<12, false>);
-  if (d.k_words <= 16) return ex ? go(k_read_rows<16, true>) : go(k_read_rows<16, false>);
-  return ex ? go(k_read_rows<32, true>) : go(k_read_rows<32, false>);
+  const bool f32 = out_dtype == 0;  // BGTQ_FP32
+  if (d.k_words <= 8) return f32 ? go(k_read_rows<8, true>) : go(k_read_rows<8, false>);
+  if (d.k_words <= 12) return f32 ? go(k_read_rows<12, true>) : go(k_read_rows<12, false>);
+  if (d.k_words <= 16) return f32 ? go(k_read_rows<16, true>) : go(k_read_rows<16, false>);
+  return f32 ? go(k_read_rows<32, true>) : go(k_read_rows<32, false>);
 }
 
 }  // namespace bgtq

@@ -40,7 +40,51 @@ def key_radii(pk, layer, b, h):
     return pk.cache.k_norms[layer, b, h, :pk.cfg.capacity * slots].view(pk.cfg.capacity, slots)[:, :ng]
 
 
-@pytest.mark.parametrize("out_dtype", [FP32])
+def scale_rows(pk, key=1.0, value=1.0):
+    """Radii of every row times powers of two (scalars, or one per cache row)."""
+    cap = pk.cfg.capacity
+    key, value = (np.broadcast_to(np.asarray(s, dtype=np.float64), (cap,)) for s in (key, value))
+    for i in np.ndindex(pk.k.shape[:3]):
+        r = key_radii(pk, *i)
+        want = r.double() * torch.from_numpy(key.copy()).cuda()[:, None]
+        r.copy_(want.half())
+        assert torch.equal(r.double(), want)
+        r = pk.cache.v_norms[i]
+        want = r.double() * torch.from_numpy(value.copy()).cuda()
+        r.copy_(want.half())
+        assert torch.equal(r.double(), want)
+    pk.k *= key[:, None]
+    pk.v *= value[:, None]
+    return pk
+
+
+def norm_error(got, ref):
+    return float(np.linalg.norm(got.double().cpu().numpy() - ref) / np.linalg.norm(ref))
+
+
+# ---------------------------------------------------------------- rows read back
+
+ROWS = [(1, 1, 128, 2, "mixed"), (2, 1, 192, 3, "wide"), (1, 2, 256, 5, "uniform"), (1, 1, 512, 8, "uniform"),
+        (1, 1, 320, 1, "wide")]
+
+
+@pytest.mark.parametrize("batch,kv,k_budget,v_bits,kind", ROWS)
+def test_bf16_rows_are_rounded_once(rotations, batch, kv, k_budget, v_bits, kind):
+    """A bf16 output is the fp32 one rounded: half a step of bf16 from a number that is itself off by the fp32 read's
+    bound at most, also where the terms of an element cancel."""
+    pk = Packed(rotations, 101, batch=batch, kv=kv, k_budget=k_budget, v_bits=v_bits, kind=kind)
+    wide, half = (bg.blockgtq_dequantize_rows(pk.cfg, pk.layout, 0, pk.cache, i32([0] * batch), 192, out_dtype=t)
+                  for t in (FP32, BF16))
+    for n, a, b in zip("kv", wide, half):
+        assert torch.equal(a.to(BF16), b)
+        for s in range(batch):
+            for h in range(kv):
+                ref, bound = expect_rows(pk, 0, s, h, n, 0, 192, FP32)
+                check(f"{n} fp32", a[s, :, h], ref, bound)
+                check(f"{n} bf16", b[s, :, h], ref, bound + 2.0 ** -8 * (np.abs(ref) + bound))
+
+
+@pytest.mark.parametrize("out_dtype", [FP32, BF16])
 @pytest.mark.parametrize("k_budget,kind", [(192, "wide"), (128, "mixed")])
 def test_key_groups_of_very_different_radii(rotations, k_budget, kind, out_dtype):
     """Each group's dims to the precision of its own radius, beside groups whose radii are 2^21 times as large."""
@@ -52,6 +96,8 @@ def test_key_groups_of_very_different_radii(rotations, k_budget, kind, out_dtype
         pk.k[0, 0, 0][:, dims] *= s
     k, _ = bg.blockgtq_dequantize_rows(pk.cfg, pk.layout, 0, pk.cache, i32([0]), 192, out_dtype=out_dtype)
     ref, bound = expect_rows(pk, 0, 0, 0, "k", 0, 192, FP32)
+    if out_dtype == BF16:
+        bound = bound + 2.0 ** -8 * (np.abs(ref) + bound)
     check("k", k[0, :, 0], ref, bound)
 
 
