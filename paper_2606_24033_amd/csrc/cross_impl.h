@@ -78,7 +78,8 @@ static_assert(kLds <= 160 * 1024, "LDS of one workgroup");
 constexpr int kAccStride = kHeadDim + 4;
 constexpr int kEndM = kWaves * kRows * kAccStride * 4;
 constexpr int kEndTiles = kEndM + 2 * kWaves * kRows * 4;  // per wave: tiles of its sequence, -1 for a refused length
-static_assert(kEndTiles + kWaves * 4 <= kLds, "merge area");
+constexpr int kEndBack = kEndTiles + kWaves * 4;           // per wave: what undoes the scale of its value radii
+static_assert(kEndBack + kWaves * 4 <= kLds, "merge area");
 
 __device__ __forceinline__ void store4(void* out, size_t i, const float4_t& y, int dtype) {  // BGTQ_BF16 = 1
   if (dtype == 1) {
@@ -372,8 +373,9 @@ __device__ __forceinline__ void build_tables(uint8_t* smem, const uint16_t* cbs,
 }
 
 // ---------------------------------------------------------------- kernel
-// EX: the softmax weights in two fp16 parts (22 bits) for fp32 outputs; one
-// part moves an output by at most 2^-11, half the rounding to bf16.
+// EX: the softmax weights times their radii in two fp16 parts (22 bits) for fp32
+// outputs; one part is off by 2^-11 of a weight at most, an eighth of the
+// output's own rounding to bf16.
 // PACK: a side may have several sequences in a workgroup (what it takes to find
 // a row's sequence is 0.5 us of a call of 16 without it).
 template <int KWB, int BV, bool EX, bool PACK>
@@ -638,6 +640,7 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(2, 2))
   const uint8_t* const rad_l = rad + 8 * hf;  // the lane's tokens start at 4 hf
 
   float m_run = kNegInf, l_run = 0.f;
+  int v_top = 0;  // (see radius_top)
   float16_t o[4];
 #pragma unroll
   for (int cc = 0; cc < 4; ++cc)
@@ -653,7 +656,13 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(2, 2))
 #pragma unroll
     for (int g = 0; g < 8; ++g)
       if (g < ng) *reinterpret_cast<uint16_t*>(rad + 128 * g + 2 * lane) = static_cast<uint16_t>(knp[g >> 1] >> (16 * (g & 1)));
-    *reinterpret_cast<uint16_t*>(rad + 128 * 8 + 2 * lane) = static_cast<uint16_t>(t0 + lane < t_end ? vnw : 0u);
+    const uint32_t vr_now = t0 + lane < t_end ? vnw : 0u;
+    if (const int was = v_top; (v_top = radius_top(was, vr_now)) != was && was > 0) {
+      const float down = two_to(127 + was - v_top);
+#pragma unroll
+      for (int cc = 0; cc < 4; ++cc) o[cc] *= down;
+    }
+    *reinterpret_cast<uint16_t*>(rad + 128 * 8 + 2 * lane) = static_cast<uint16_t>(radius_times(vr_now, radius_up(v_top)));
     __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
     __builtin_amdgcn_wave_barrier();
     {
@@ -796,8 +805,10 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(2, 2))
   float* const ms = reinterpret_cast<float*>(smem + kEndM);
   float* const ls = ms + kWaves * kRows;
   int* const tiles = reinterpret_cast<int*>(smem + kEndTiles);
+  float* const vback = reinterpret_cast<float*>(smem + kEndBack);
   const int n_tiles = max(t_end - t_begin + kKeyTile - 1, 0) / kKeyTile;
   if (S.pack && lane == 0) tiles[wave] = ok ? n_tiles : -1;
+  if (lane == 0) vback[wave] = two_to(127 - radius_up(v_top));
   if ((wave & (wps - 1)) < n_tiles) {
 #pragma unroll
     for (int cc = 0; cc < 4; ++cc)
@@ -826,11 +837,12 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(2, 2))
     if (w >= n_act) break;
     const float e = __builtin_amdgcn_exp2f(ms[(w0 + w) * kRows + r] - mref);
     l = fmaf(ls[(w0 + w) * kRows + r], e, l);
+    const float ea = e * vback[w0 + w];
 #pragma unroll
     for (int h = 0; h < 2; ++h) {
       const float4_t x = *reinterpret_cast<const float4_t*>(acc + ((w0 + w) * kRows + r) * kAccStride + 4 * h + d0);
 #pragma unroll
-      for (int i = 0; i < 4; ++i) a[h][i] = fmaf(x[i], e, a[h][i]);
+      for (int i = 0; i < 4; ++i) a[h][i] = fmaf(x[i], ea, a[h][i]);
     }
   }
   if (n_row < 0) l = __builtin_nanf("");

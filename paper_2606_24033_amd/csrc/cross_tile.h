@@ -148,6 +148,7 @@ __global__ __launch_bounds__(kAttnThreads) __attribute__((amdgpu_waves_per_eu(2,
   const uint16_t* vnp = S.c.v_norms + row * cap;
 
   float m_run = kNegInf, l_run = 0.f;
+  int v_top = 0, v_acc = 0;  // see radius_top: of the tiles decoded so far, and of those in o
   float16_t o[4];
 #pragma unroll
   for (int cc = 0; cc < 4; ++cc)
@@ -200,6 +201,8 @@ __global__ __launch_bounds__(kAttnThreads) __attribute__((amdgpu_waves_per_eu(2,
     const uint4 radii = make_uint4(down(raw.kn.x), down(raw.kn.y), down(raw.kn.z), down(raw.kn.w));
 #pragma unroll
     for (int j = 0; j < kItemsPer; ++j) key_store(dst + 8 * kAttnWaves * j, items, j, radii, code[j]);
+    v_top = radius_top(v_top, raw.vn);  // (the same in every wave: each has the tile's 64 radii)
+    raw.vn = radius_times(raw.vn, radius_up(v_top));
     store_values<BV>(dec, raw, tt, quarter, va, vb);
   };
 
@@ -233,8 +236,16 @@ __global__ __launch_bounds__(kAttnThreads) __attribute__((amdgpu_waves_per_eu(2,
 
   // Online softmax (base 2), then O^T += V^T P^T; only a tile that reaches past
   // the end masks anything.
-  const auto softmax_pv = [&](const uint8_t* dcur, int t0) {
+  const auto softmax_pv = [&](const uint8_t* dcur, int t0, int v_cur) {
     const int tt = opaque_tid(), hf4 = (tt & 32) >> 3;  // 4 hf
+    if (v_cur != v_acc) {
+      if (v_acc > 0) {
+        const float down = __uint_as_float(static_cast<uint32_t>(127 + v_acc - v_cur) << 23);
+#pragma unroll
+        for (int cc = 0; cc < 4; ++cc) o[cc] *= down;
+      }
+      v_acc = v_cur;
+    }
     if (t0 + 32 * (blk0 + NB) > t_end) {
 #pragma unroll
       for (int n = 0; n < NB; ++n)
@@ -344,12 +355,13 @@ __global__ __launch_bounds__(kAttnThreads) __attribute__((amdgpu_waves_per_eu(2,
   for (int kt = 0; kt < n_kt; ++kt) {
     const uint8_t* const dcur = smem + kOffDec + (kt & 1) * kDecBytes;
     uint8_t* const dnxt = smem + kOffDec + (~kt & 1) * kDecBytes;
+    const int v_cur = v_top;
     if (wave < 4) {
       decode(dnxt);
       load_raw(tile_start(kt + 2));
     }
     products_qk(dcur);
-    softmax_pv(dcur, t_begin + kt * kKeyTile);
+    softmax_pv(dcur, t_begin + kt * kKeyTile, v_cur);
     if (wave >= 4) {
       decode(dnxt);
       load_raw(tile_start(kt + 2));
@@ -385,6 +397,7 @@ __global__ __launch_bounds__(kAttnThreads) __attribute__((amdgpu_waves_per_eu(2,
   }
   if (!ok) l_run = __builtin_nanf("");
   const bool mine = r < nr && (KS == 1 || wave < 4);
+  const float v_back = __uint_as_float(static_cast<uint32_t>(127 - radius_up(v_acc)) << 23);
 
   if (call.n_slots > 1) {
     if (!mine) return;
@@ -399,7 +412,7 @@ __global__ __launch_bounds__(kAttnThreads) __attribute__((amdgpu_waves_per_eu(2,
 #pragma unroll
       for (int u = 0; u < 4; ++u)
         *reinterpret_cast<float4_t*>(P + 4 + 32 * cc + 8 * u + 4 * hf) =
-            float4_t{o[cc][4 * u], o[cc][4 * u + 1], o[cc][4 * u + 2], o[cc][4 * u + 3]};
+            float4_t{o[cc][4 * u], o[cc][4 * u + 1], o[cc][4 * u + 2], o[cc][4 * u + 3]} * v_back;
     return;
   }
 
@@ -434,7 +447,7 @@ __global__ __launch_bounds__(kAttnThreads) __attribute__((amdgpu_waves_per_eu(2,
   float to, back;
   scale_of(max2g(mx), to, back);
   // (not a number in l: every output is)
-  const float scale = l_run == 0.f ? 0.f : back * (kRsqrtD / 256.f) / l_run;
+  const float scale = l_run == 0.f ? 0.f : back * (v_back * (kRsqrtD / 256.f)) / l_run;
   half8_t oh[8], ol[8];
 #pragma unroll
   for (int st = 0; st < 8; ++st)

@@ -21,4 +21,22 @@ __device__ __forceinline__ uint32_t mix_pair(float p0, float p1, uint32_t w) {
   return __builtin_bit_cast(uint32_t, r);
 }
 
+// Value radii enter a pass's products times a power of two that brings the
+// largest one so far to [2^14, 2^15): weight times radius then keeps fp16's full
+// precision for weights down to 2^-28 of the largest, whatever size the values
+// have.  `top` is the running maximum of the radii's exponent fields (0: none
+// yet); when it rises the accumulators are rescaled, as for a running maximum of
+// the logits.
+__device__ __forceinline__ int radius_top(int top, uint32_t bits) {  // bits: a lane's radius, fp16
+  const int f = static_cast<int>(bits >> 10 & 31u), e = f == 31 ? 0 : f;  // (not finite: no size)
+  for (uint64_t more; (more = __builtin_amdgcn_ballot_w64(e > top)) != 0;)  // (each turn raises top, 30 at the most)
+    top = __builtin_amdgcn_readlane(e, __builtin_ctzll(more));
+  return top;
+}
+__device__ __forceinline__ int radius_up(int top) { return 29 - max(top, 1); }
+__device__ __forceinline__ uint32_t radius_times(uint32_t bits, int up) {  // 2^up times an fp16 number, as fp16
+  const float r = static_cast<float>(__builtin_bit_cast(_Float16, static_cast<uint16_t>(bits)));
+  return __builtin_bit_cast(uint16_t, static_cast<_Float16>(__builtin_amdgcn_ldexpf(r, up)));
+}
+
 }  // namespace bgtq

@@ -13,7 +13,7 @@ import pytest
 from oracle import blockgtq_oracle as o
 from paper_2606_24033_amd import blockgtq as bg
 from paper_2606_24033_amd import synth
-from tests.test_gpu_cache_readers import Packed, check, expect_rows, i32
+from tests.test_gpu_cache_readers import Packed, check, expect_cross, expect_rows, expect_shared, i32
 
 pytestmark = pytest.mark.gpu
 
@@ -122,3 +122,47 @@ def test_a_radius_that_is_not_finite_reads_back_in_its_place_only(rotations, bad
     assert not torch.isfinite(v[0, rows, 1]).any()
     v[0, rows, 1] = v0[0, rows, 1]
     assert torch.equal(v, v0)
+
+
+# ---------------------------------------------------------------- attention: radii of every size
+
+NARROW, WIDE = (dict(kv=2, group=4), 6), (dict(kv=8, group=4), 1100)  # the second takes the passes with many query rows
+
+
+@pytest.mark.parametrize("shape,n_q", [NARROW, WIDE])
+@pytest.mark.parametrize("value", [2.0 ** -10, 2.0 ** -13, 2.0 ** -16, 2.0 ** 11, "rising", "falling"])
+def test_value_radii_of_every_size(rotations, shape, n_q, value):
+    """The bound of test_fp32_outputs_in_the_2_norm, 1e-5, holds for small, large and mixed value radii alike.  In bf16
+    the output's rounding is 2^-8 of an element at most, and a weight is off by 2^-11, together below 2^-8 + 2^-10 in the
+    2-norm (a weight's share of an output row cancels no further than the row itself: the values are independent)."""
+    pk = Packed(rotations, 111, cap=640, dtype="fp32", k_budget=192, v_bits=3, **shape)
+    t = np.arange(640)
+    scale_rows(pk, value={"rising": 2.0 ** (-16 + t // 24), "falling": 2.0 ** (10 - t // 24)}[value]
+               if isinstance(value, str) else value)
+    assert (bg.cross_workspace_bytes(pk.cfg, 1, n_q, 0, 600) >= n_q * 32 * 512) == (n_q > 100)
+    q, qd = pk.queries((1, 1, n_q))
+    at = list(range(0, n_q, max(1, n_q // 6)))
+    ref, _ = expect_cross(pk, q[:, :, at], [600], FP32)
+    for dt, tol in ((FP32, 1e-5), (BF16, 2.0 ** -8 + 2.0 ** -10)):
+        for splits in (0, 1, 3):
+            out = bg.blockgtq_cross_attn(pk.cfg, pk.layout, 0, qd[0], i32([600]), 600, pk.cache, n_splits=splits, out_dtype=dt)
+            err = norm_error(out[:, at], ref[0])
+            print(f"{n_q} query rows, {dt}, {splits} splits: {err:.3g}", flush=True)
+            assert err <= tol, err
+
+
+def test_shared_prefix_with_radii_of_another_size(rotations):
+    """Prefix and own rows whose value radii differ by 2^10 either way, in packed and plain workgroups."""
+    for batch, kv, prefix_scale, own_scale in ((3, 2, 2.0 ** -12, 2.0 ** -2), (3, 2, 2.0 ** -2, 2.0 ** -12),
+                                               (40, 8, 2.0 ** -12, 2.0 ** -2)):
+        lens = [(37 * b) % 130 for b in range(batch)]
+        kw = dict(kv=kv, group=4, k_budget=192, v_bits=3, dtype="fp32")
+        pk = scale_rows(Packed(rotations, 113, batch=batch, cap=192, **kw), value=own_scale)
+        pp = scale_rows(Packed(rotations, 114, cap=704, layout_of=pk, **kw), value=prefix_scale)
+        q, qd = pk.queries((1, batch))
+        ref, _ = expect_shared(pp, pk, q, 700, lens, FP32)
+        out = bg.blockgtq_decode_attn_shared(pk.cfg, pk.layout, 0, qd[0], pp.cfg, pp.cache, i32([700]), 700, i32(lens), 130,
+                                             pk.cache)
+        err = norm_error(out, ref[0])
+        print(f"{batch} sequences: {err:.3g}", flush=True)
+        assert err <= 1e-5, err
