@@ -6,8 +6,8 @@
 // workgroup's 8 waves decode each 64-row tile once into LDS, double-buffered,
 // for 256 query rows (128 with two waves to 32 rows, KS = 2), so that a row
 // pays 1/256 of the decode.  Here there is no causal mask, the key axis can be
-// in splits, a wave's query rows are scaled by a power of two of their own
-// (their fp16 lo parts stay above the subnormals), and the results are
+// in splits, query rows and the radii of keys and values are scaled by powers of
+// two (their fp16 lo parts stay above the subnormals), and the results are
 // partials or, with one split, outputs.
 //
 // What bounds it: the matrix cores (56 % busy) and the decode beside them; QK takes
@@ -95,8 +95,7 @@ __global__ __launch_bounds__(kAttnThreads) __attribute__((amdgpu_waves_per_eu(2,
   }
 
   // query operands (B of S^T = K Q^T): dims 16 ks + 8 hf .. +7 of the row,
-  // scaled, in fp16 hi and lo parts.  (The keys' radii come in at an eighth, so
-  // that no product with a centroid leaves fp16's range.)
+  // scaled, in fp16 hi and lo parts.
   half8_t qh[8], ql[8];
   float sc;
   {
@@ -116,7 +115,6 @@ __global__ __launch_bounds__(kAttnThreads) __attribute__((amdgpu_waves_per_eu(2,
     mx = max2g(bad ? __builtin_huge_valf() : mx);
     float to;
     scale_of(mx, to, sc);
-    sc *= 8.f;
 #pragma unroll
     for (int ks = 0; ks < 8; ++ks)
 #pragma unroll
@@ -185,8 +183,40 @@ __global__ __launch_bounds__(kAttnThreads) __attribute__((amdgpu_waves_per_eu(2,
 #pragma unroll
     for (int i = 0; i < NW; ++i) raw.v[i] = ld_at<uint32_t>(vs + 4 * i, v_lane);
     raw.vn = ld_at<uint16_t>(vnp + ta, vn_lane);
-    // what lies behind the last row may be infinite or not a number: no value radius
-    if (ta + kKeyTile > t_end) raw.vn = ta + (tt & 63) < t_end ? raw.vn : 0u;
+    // what lies behind the last row may be large, infinite or not a number: no radii
+    if (ta + kKeyTile > t_end) {
+      const uint32_t in = ta + (tt & 63) < t_end ? ~0u : 0u;
+      raw.vn &= in;
+      raw.kn = make_uint4(raw.kn.x & in, raw.kn.y & in, raw.kn.z & in, raw.kn.w & in);
+    }
+  };
+  // Key radii come in times a power of two that brings the largest one so far to
+  // [2^12, 2^13): their products with centroids (below 5) stay in fp16's range,
+  // and the lo parts of those hold 2^-37 of the largest product, whatever the
+  // size of the keys.  k_top: the running maximum of the radii's exponent fields,
+  // plus one.  A tile's logits are multiplied back by its own power.
+  int k_top = 2;
+  const auto key_up = [](int top) { return max(-3, min(26, 28 - top)); };
+  const auto scaled_keys = [&]() {
+    // (a token's 16 bytes reach into the next ones' where the row has fewer than 8 slots)
+    typedef uint16_t ushort2_t __attribute__((ext_vector_type(2)));
+    const auto fields = [](uint32_t x) {  // exponent fields plus one, 0 for what is not finite
+      return __builtin_bit_cast(ushort2_t, ((x & 0x7C007C00u) + 0x04000400u) & 0x7C007C00u);
+    };
+    const ushort2_t f = __builtin_elementwise_max(
+        __builtin_elementwise_max(fields(raw.kn.x), fields(nslot > 2 ? raw.kn.y : 0u)),
+        __builtin_elementwise_max(fields(nslot > 4 ? raw.kn.z : 0u), fields(nslot > 6 ? raw.kn.w : 0u)));
+    k_top = raise_top(k_top, max(f[0] >> 10, f[1] >> 10));
+    const int up = key_up(k_top);
+    const auto times = [&](const uint4& x, int n) {
+      const _Float16 p = __builtin_bit_cast(_Float16, static_cast<uint16_t>((n + 15) << 10));
+      const half2_t pp = {p, p};
+      const auto one = [&](uint32_t r) { return __builtin_bit_cast(uint32_t, __builtin_bit_cast(half2_t, r) * pp); };
+      return make_uint4(one(x.x), one(x.y), one(x.z), one(x.w));
+    };
+    uint4 r = times(raw.kn, min(up, 15));
+    if (up > 15) r = times(r, up - 15);
+    return r;
   };
   const auto decode = [&](uint8_t* dec) {
     const int tt = opaque_tid();
@@ -196,9 +226,7 @@ __global__ __launch_bounds__(kAttnThreads) __attribute__((amdgpu_waves_per_eu(2,
     else key_lookups<false>(smem, items, raw.k, code);
     value_lookups<BV>(smem, raw, quarter, va, vb);
     uint8_t* dst = dec + (tt & 63) * (2 * kKStride) + 8 * wave;
-    const half2_t eighth = {static_cast<_Float16>(0.125f), static_cast<_Float16>(0.125f)};
-    const auto down = [&](uint32_t x) { return __builtin_bit_cast(uint32_t, __builtin_bit_cast(half2_t, x) * eighth); };
-    const uint4 radii = make_uint4(down(raw.kn.x), down(raw.kn.y), down(raw.kn.z), down(raw.kn.w));
+    const uint4 radii = scaled_keys();
 #pragma unroll
     for (int j = 0; j < kItemsPer; ++j) key_store(dst + 8 * kAttnWaves * j, items, j, radii, code[j]);
     v_top = radius_top(v_top, raw.vn);  // (the same in every wave: each has the tile's 64 radii)
@@ -236,7 +264,7 @@ __global__ __launch_bounds__(kAttnThreads) __attribute__((amdgpu_waves_per_eu(2,
 
   // Online softmax (base 2), then O^T += V^T P^T; only a tile that reaches past
   // the end masks anything.
-  const auto softmax_pv = [&](const uint8_t* dcur, int t0, int v_cur) {
+  const auto softmax_pv = [&](const uint8_t* dcur, int t0, int k_cur, int v_cur) {
     const int tt = opaque_tid(), hf4 = (tt & 32) >> 3;  // 4 hf
     if (v_cur != v_acc) {
       if (v_acc > 0) {
@@ -246,6 +274,7 @@ __global__ __launch_bounds__(kAttnThreads) __attribute__((amdgpu_waves_per_eu(2,
       }
       v_acc = v_cur;
     }
+    const float st = sc * __uint_as_float(static_cast<uint32_t>(127 - key_up(k_cur)) << 23);
     if (t0 + 32 * (blk0 + NB) > t_end) {
 #pragma unroll
       for (int n = 0; n < NB; ++n)
@@ -271,7 +300,7 @@ __global__ __launch_bounds__(kAttnThreads) __attribute__((amdgpu_waves_per_eu(2,
         mp[c4] = fmaxf(fmaxf(mp[c4], s[1][4 * c4 + 2]), s[1][4 * c4 + 3]);
       }
     }
-    const float mx = fmaxf(fmaxf(mp[0], mp[1]), fmaxf(mp[2], mp[3])) * sc;
+    const float mx = fmaxf(fmaxf(mp[0], mp[1]), fmaxf(mp[2], mp[3])) * st;
     if (__builtin_amdgcn_ballot_w64(mx > m_run) != 0) {
       const float mn = fmaxf(m_run, max2g(mx));
       const float corr = m_run == kNegInf ? 0.f : __builtin_amdgcn_exp2f(m_run - mn);
@@ -289,7 +318,7 @@ __global__ __launch_bounds__(kAttnThreads) __attribute__((amdgpu_waves_per_eu(2,
       for (int q = 0; q < 4; ++q) {
         float p[4];
 #pragma unroll
-        for (int i = 0; i < 4; ++i) p[i] = __builtin_amdgcn_exp2f(fmaf(s[n][4 * q + i], sc, -mref));
+        for (int i = 0; i < 4; ++i) p[i] = __builtin_amdgcn_exp2f(fmaf(s[n][4 * q + i], st, -mref));
         ps += (p[0] + p[1]) + (p[2] + p[3]);
         pw[2 * q] = mix_pair(p[0], p[1], vr[q].x);
         pw[2 * q + 1] = mix_pair(p[2], p[3], vr[q].y);
@@ -355,13 +384,13 @@ __global__ __launch_bounds__(kAttnThreads) __attribute__((amdgpu_waves_per_eu(2,
   for (int kt = 0; kt < n_kt; ++kt) {
     const uint8_t* const dcur = smem + kOffDec + (kt & 1) * kDecBytes;
     uint8_t* const dnxt = smem + kOffDec + (~kt & 1) * kDecBytes;
-    const int v_cur = v_top;
+    const int k_cur = k_top, v_cur = v_top;
     if (wave < 4) {
       decode(dnxt);
       load_raw(tile_start(kt + 2));
     }
     products_qk(dcur);
-    softmax_pv(dcur, t_begin + kt * kKeyTile, v_cur);
+    softmax_pv(dcur, t_begin + kt * kKeyTile, k_cur, v_cur);
     if (wave >= 4) {
       decode(dnxt);
       load_raw(tile_start(kt + 2));

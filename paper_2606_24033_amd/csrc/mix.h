@@ -27,11 +27,14 @@ __device__ __forceinline__ uint32_t mix_pair(float p0, float p1, uint32_t w) {
 // have.  `top` is the running maximum of the radii's exponent fields (0: none
 // yet); when it rises the accumulators are rescaled, as for a running maximum of
 // the logits.
-__device__ __forceinline__ int radius_top(int top, uint32_t bits) {  // bits: a lane's radius, fp16
-  const int f = static_cast<int>(bits >> 10 & 31u), e = f == 31 ? 0 : f;  // (not finite: no size)
-  for (uint64_t more; (more = __builtin_amdgcn_ballot_w64(e > top)) != 0;)  // (each turn raises top, 30 at the most)
+__device__ __forceinline__ int raise_top(int top, int e) {  // the largest of top and the lanes' e (0 .. 31)
+  for (uint64_t more; (more = __builtin_amdgcn_ballot_w64(e > top)) != 0;)  // (each turn raises top)
     top = __builtin_amdgcn_readlane(e, __builtin_ctzll(more));
   return top;
+}
+__device__ __forceinline__ int radius_top(int top, uint32_t bits) {  // bits: a lane's radius, fp16
+  const int f = static_cast<int>(bits >> 10 & 31u);
+  return raise_top(top, f == 31 ? 0 : f);  // (not finite: no size)
 }
 __device__ __forceinline__ int radius_up(int top) { return 29 - max(top, 1); }
 __device__ __forceinline__ uint32_t radius_times(uint32_t bits, int up) {  // 2^up times an fp16 number, as fp16

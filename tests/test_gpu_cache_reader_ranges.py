@@ -151,6 +151,25 @@ def test_value_radii_of_every_size(rotations, shape, n_q, value):
             assert err <= tol, err
 
 
+@pytest.mark.parametrize("shape,n_q", [NARROW, WIDE])
+@pytest.mark.parametrize("key", [2.0 ** -7, 2.0 ** -11, 2.0 ** 9, "rising", "falling"])
+def test_key_radii_of_every_size(rotations, shape, n_q, key):
+    """Small key radii with large queries and the reverse give the logits of ordinary ones, to the same precision."""
+    pk = Packed(rotations, 112, cap=640, dtype="fp32", k_budget=192, v_bits=3, **shape)
+    t = np.arange(640)
+    # mixed: from 2^-11 to 1, with queries for the largest
+    radii = {"rising": 2.0 ** (-11 + np.minimum(t // 48, 11)), "falling": 2.0 ** -(np.minimum(t // 48, 11.0))}[key] \
+        if isinstance(key, str) else key
+    scale_rows(pk, key=radii)
+    q, qd = pk.queries((1, 1, n_q), scale=1.0 if isinstance(key, str) else 1.0 / key)
+    at = list(range(0, n_q, max(1, n_q // 6)))
+    ref, _ = expect_cross(pk, q[:, :, at], [600], FP32)
+    out = bg.blockgtq_cross_attn(pk.cfg, pk.layout, 0, qd[0], i32([600]), 600, pk.cache)
+    err = norm_error(out[:, at], ref[0])
+    print(f"{n_q} query rows: {err:.3g}", flush=True)
+    assert err <= 1e-5, err
+
+
 def test_shared_prefix_with_radii_of_another_size(rotations):
     """Prefix and own rows whose value radii differ by 2^10 either way, in packed and plain workgroups."""
     for batch, kv, prefix_scale, own_scale in ((3, 2, 2.0 ** -12, 2.0 ** -2), (3, 2, 2.0 ** -2, 2.0 ** -12),
