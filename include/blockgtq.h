@@ -370,7 +370,9 @@ int blockgtq_dequantize_rows(const bgtq_config* cfg, const void* d_layout, int32
  * d_ctx_len: device int32 [batch], each in [0, max_ctx]; a sequence of no rows
  *      gets zeros, one whose length is outside [0, max_ctx] gets NaN.  What the
  *      cache holds behind a sequence's rows (not a number or infinite radii
- *      too) does not enter its outputs.
+ *      too) does not enter its outputs.  A radius that is not finite in one of
+ *      its rows (a norm past fp16's range) makes NaN of every output that
+ *      attends the row.
  * max_ctx: host-side bound (<= capacity, ECAPACITY otherwise).
  * n_splits: 0 = heuristic, else the splits of the key axis (1 .. 4096).
  * d_workspace: blockgtq_cross_workspace_bytes bytes for the same n_q, n_splits

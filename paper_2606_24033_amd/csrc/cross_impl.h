@@ -653,6 +653,14 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(2, 2))
     // this tile's radii, token-minor, for the wave's own reads (LDS operations
     // of a wave complete in order); a token past the end has value radius 0:
     // what lies there may be infinite or not a number
+    // (an infinite key radius becomes not a number: the coordinates that it
+    // scales have both signs, so the row's logits are not numbers, where the sum
+    // of a group's products, scaled afterwards, would be infinite)
+#pragma unroll
+    for (int g = 0; g < 4; ++g) {
+      const half2_t r = __builtin_bit_cast(half2_t, knp[g]);
+      knp[g] = __builtin_bit_cast(uint32_t, r + (r - r));
+    }
 #pragma unroll
     for (int g = 0; g < 8; ++g)
       if (g < ng) *reinterpret_cast<uint16_t*>(rad + 128 * g + 2 * lane) = static_cast<uint16_t>(knp[g >> 1] >> (16 * (g & 1)));

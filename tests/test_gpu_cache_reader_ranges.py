@@ -185,3 +185,28 @@ def test_shared_prefix_with_radii_of_another_size(rotations):
         err = norm_error(out, ref[0])
         print(f"{batch} sequences: {err:.3g}", flush=True)
         assert err <= 1e-5, err
+
+
+@pytest.mark.parametrize("shape,n_q", [NARROW, WIDE])
+@pytest.mark.parametrize("which", ["key", "value"])
+def test_an_infinite_radius_reaches_every_query_that_sees_the_row(rotations, shape, n_q, which):
+    """By the definition a row with an infinite radius has coordinates that are not finite, and so has every query's
+    logit or output, whatever the query's sign: nothing is dropped silently.  Other heads and sequences are untouched."""
+    pk = Packed(rotations, 115, batch=2, cap=640, k_budget=192, v_bits=3, **shape)
+    q, qd = pk.queries((1, 2, n_q))
+    args = (pk.cfg, pk.layout, 0, qd[0], i32([600, 500]), 600, pk.cache)
+    for splits in (0, 1, 4):
+        before = bg.blockgtq_cross_attn(*args, n_splits=splits)
+        if which == "key":
+            r = key_radii(pk, 0, 1, 1)
+            keep = r[77, 0].clone()
+            r[77, 0] = float("inf")
+        else:
+            r = pk.cache.v_norms[0, 1, 1][:, None]
+            keep = r[77, 0].clone()
+            r[77, 0] = float("inf")
+        out = bg.blockgtq_cross_attn(*args, n_splits=splits)
+        r[77, 0] = keep
+        assert torch.isnan(out[1, :, 4:8]).all()
+        out[1, :, 4:8] = before[1, :, 4:8]
+        assert torch.equal(out, before)
