@@ -379,7 +379,8 @@ int blockgtq_dequantize_rows(const bgtq_config* cfg, const void* d_layout, int32
  *      and max_ctx (the need does not grow with each of them: a call of fewer
  *      query rows may take more splits), any contents; calls that share it must
  *      not overlap in time.
- * EUNSUPPORTED above 2^24 query rows (layers x batch x n_q x heads) a call. */
+ * EUNSUPPORTED above 2^24 query rows (layers x batch x n_q x heads) a call, or
+ * for a max_ctx above 2^30. */
 int blockgtq_cross_workspace_bytes(const bgtq_config* cfg, int32_t n_layers_in_call, int32_t n_q, int32_t n_splits,
                                    int32_t max_ctx, size_t* bytes_out);
 int blockgtq_cross_attn(const bgtq_config* cfg, const void* d_layout, int32_t layer, const void* d_q, int32_t n_q,
@@ -401,7 +402,7 @@ int blockgtq_cross_attn(const bgtq_config* cfg, const void* d_layout, int32_t la
  *      capacity).
  * prefix_cfg: cfg but for batch == 1 and the capacity (EINVAL otherwise).
  * d_prefix_len: device int32 [1] in [0, max_prefix], max_prefix <=
- *      prefix_cfg->capacity; outside it every output is NaN.
+ *      prefix_cfg->capacity and 2^30; outside it every output is NaN.
  * d_ctx_len, max_ctx: as in blockgtq_cross_attn, the sequences' own rows; a
  *      sequence without any row (prefix and own) gets zeros.
  * d_q, d_out, out_dtype, layer: as blockgtq_cross_attn with one query row per

@@ -949,11 +949,16 @@ static size_t cross_ws_bytes(long rows, int n_slots, const CrossPlan& p) {
   return cross_part_bytes(rows, n_slots) + (p.rows > 32 ? al256(static_cast<size_t>(rows) * kHeadDim * 4) : 0);
 }
 
+// Rows that a call may attend: a split's end and the next tile of a wave, up to
+// half as far again, are positions in 32 bits.
+static const int32_t kMaxCrossRows = 1 << 30;
+
 static int check_cross_sizes(const bgtq_config* cfg, int32_t n_lc, int32_t n_q, int32_t n_splits, int32_t max_ctx) {
   if (n_lc != 1 && n_lc != cfg->n_layers) return fail(BGTQ_EINVAL, "n_layers_in_call must be 1 or n_layers");
   if (n_q < 0) return fail(BGTQ_EINVAL, "n_q %d < 0", n_q);
   if (n_splits < 0 || n_splits > 4096) return fail(BGTQ_EINVAL, "n_splits %d outside 0..4096", n_splits);
   if (max_ctx < 0 || max_ctx > cfg->capacity) return fail(BGTQ_ECAPACITY, "max_ctx %d outside [0, capacity]", max_ctx);
+  if (max_ctx > kMaxCrossRows) return fail(BGTQ_EUNSUPPORTED, "max_ctx %d above 2^30 rows", max_ctx);
   return BGTQ_OK;
 }
 
