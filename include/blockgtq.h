@@ -339,10 +339,9 @@ int blockgtq_decode_attn_noalloc(const bgtq_config* cfg, const void* d_layout, i
  * layer in [0, n_layers) or -1 for all layers.
  * Rows d_read_pos[b] .. d_read_pos[b] + n_rows - 1 of sequence b go to d_k_out
  * and d_v_out in out_dtype (BGTQ_FP32, or BGTQ_BF16: the fp32 result rounded
- * once), laid out as
- * the append's inputs: [batch][n_rows][n_kv_heads][head_dim], with a leading
- * [n_layers] for layer == -1; 16-byte aligned (EINVAL otherwise).  Either may
- * be NULL (not both): only the other one is read.
+ * once), laid out as the append's inputs: [batch][n_rows][n_kv_heads][head_dim],
+ * with a leading [n_layers] for layer == -1; 16-byte aligned (EINVAL otherwise).
+ * Either may be NULL (not both): only the other one is read.
  * d_read_pos: int32 [batch].  d_ctx_len: int32 [batch], or NULL.  A row at a
  * position below 0, at or past the capacity, or at or past d_ctx_len[b] is not
  * read and its outputs are left as they were.
@@ -360,13 +359,17 @@ int blockgtq_dequantize_rows(const bgtq_config* cfg, const void* d_layout, int32
  * encoder's states, of another length, that were packed once
  * (blockgtq_quantize_append) and are read by every pass.  n_q runs from a
  * single generated token to whole prompts; the key axis is split where there
- * are few query rows.  Two launches on `stream` at most; no allocation, no
- * state in the workspace, so the call can be captured in a HIP graph.
+ * are few query rows.  Up to three launches on `stream` (the rotation of many
+ * query rows, the attention, the join of splits); no allocation, no state in the
+ * workspace, so the call can be captured in a HIP graph.
  * layer in [0, n_layers) or -1 for all layers.
  * d_q: [batch][n_q][n_kv_heads*group][128] in in_dtype, with a leading
  *      [n_layers] for layer == -1.  d_out: the same shape in out_dtype
- *      (BGTQ_FP32 or BGTQ_BF16, rounded once).  Both and the workspace 16-byte
- *      aligned (EINVAL otherwise).
+ *      (BGTQ_FP32 or BGTQ_BF16).  Both and the workspace 16-byte aligned (EINVAL
+ *      otherwise).  Logits, sums and accumulators are of fp32 grade for either
+ *      type; a softmax weight times its value radius is held to 22 bits for fp32
+ *      outputs and to fp16's 11 for bf16 ones (2^-11 of it, an eighth of the
+ *      output's own rounding).
  * d_ctx_len: device int32 [batch], each in [0, max_ctx]; a sequence of no rows
  *      gets zeros, one whose length is outside [0, max_ctx] gets NaN.  What the
  *      cache holds behind a sequence's rows (not a number or infinite radii
