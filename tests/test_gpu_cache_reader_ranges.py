@@ -13,7 +13,8 @@ import pytest
 from oracle import blockgtq_oracle as o
 from paper_2606_24033_amd import blockgtq as bg
 from paper_2606_24033_amd import synth
-from tests.test_gpu_cache_readers import Packed, check, expect_cross, expect_rows, expect_shared, i32
+from tests.test_gpu_cache_readers import (D, Packed, attention_and_bound, check, expect_cross, expect_rows, expect_shared, i32,
+                                          widths_of)
 
 pytestmark = pytest.mark.gpu
 
@@ -124,6 +125,39 @@ def test_a_radius_that_is_not_finite_reads_back_in_its_place_only(rotations, bad
     assert torch.equal(v, v0)
 
 
+@pytest.mark.parametrize("out_dtype,k_budget,v_bits,n_rows,pos,lens", [
+    (BF16, 128, 2, 4160, [0, 0, 0, 0, 0, 0], None),
+    (FP32, 192, 3, 4100, [60, 1, 33, 0, 64, 17], [4160, 4000, 65, 0, 3333, 2048]),
+    (BF16, 512, 8, 3001, [1159, 0, 700, 31, -5, 4100], [4160] * 6),
+])
+def test_long_reads_are_the_short_reads(rotations, out_dtype, k_budget, v_bits, n_rows, pos, lens):
+    """Reads of which a wave takes several tiles and a head several workgroups, against the same rows in short
+    reads."""
+    B, H, cap = 6, 6, 4160
+    rng = np.random.default_rng(104)
+    cfg = bg.Config(1, B, H, 1, cap, k_budget, v_bits, bg.BGTQ_BF16)
+    bits = np.stack([[widths_of("uniform" if k_budget == 512 else "mixed", k_budget, rng) for _ in range(H)]])
+    layout = bg.Layout(cfg, bits, synth.flat_rot_k(rotations[0]), rotations[1])
+    cache = bg.Cache(cfg)
+    g = torch.Generator(device="cuda")
+    g.manual_seed(5)
+    for t in (cache.k_codes, cache.v_codes):
+        t.random_(-2 ** 31, 2 ** 31 - 1, generator=g)
+    for t in (cache.k_norms, cache.v_norms):
+        t.uniform_(0.3, 3.0, generator=g)
+    ctx = None if lens is None else i32(lens)
+    shape = (B, n_rows, H, D)
+    out = [torch.full(shape, 77.0, dtype=out_dtype, device="cuda") for _ in range(2)]
+    bg.blockgtq_dequantize_rows(cfg, layout, 0, cache, i32(pos), n_rows, ctx_len=ctx, k_out=out[0], v_out=out[1])
+    for at in range(0, n_rows, 192):
+        m = min(192, n_rows - at)
+        part = [torch.full((B, m, H, D), 77.0, dtype=out_dtype, device="cuda") for _ in range(2)]
+        bg.blockgtq_dequantize_rows(cfg, layout, 0, cache, i32([p + at for p in pos]), m, ctx_len=ctx, k_out=part[0],
+                                    v_out=part[1])
+        for a, b in zip(out, part):
+            assert torch.equal(a[:, at:at + m], b), f"rows {at} .. {at + m - 1}"
+
+
 # ---------------------------------------------------------------- attention: radii of every size
 
 NARROW, WIDE = (dict(kv=2, group=4), 6), (dict(kv=8, group=4), 1100)  # the second takes the passes with many query rows
@@ -210,3 +244,81 @@ def test_an_infinite_radius_reaches_every_query_that_sees_the_row(rotations, sha
         assert torch.isnan(out[1, :, 4:8]).all()
         out[1, :, 4:8] = before[1, :, 4:8]
         assert torch.equal(out, before)
+
+
+# ---------------------------------------------------------------- passes over several layers, every row
+
+@pytest.mark.parametrize("layers,batch,kv,group,tin,tout,n_q,longest", [
+    (5, 67, 2, 4, "bf16", "bf16", 1, 200),   # 4 sequences to a workgroup
+    (9, 33, 2, 4, "fp32", "fp32", 1, 200),
+])
+def test_many_short_sequences_of_several_layers(rotations, layers, batch, kv, group, tin, tout, n_q, longest):
+    dt = BF16 if tout == "bf16" else FP32
+    rng = np.random.default_rng(121)
+    lens = [int(x) for x in rng.integers(0, longest + 1, batch)]
+    lens[0], lens[1], lens[-1] = longest, 0, 1
+    pk = Packed(rotations, 122, layers=layers, batch=batch, kv=kv, group=group, cap=256, dtype=tin, behind=float("nan"),
+                lens=lens)
+    q, qd = pk.queries((layers, batch, n_q))
+    ref, bound = expect_cross(pk, q, lens, dt)
+    out = bg.blockgtq_cross_attn(pk.cfg, pk.layout, -1, qd, i32(lens), longest, pk.cache, out_dtype=dt)
+    check("all layers", out, ref, bound)
+
+
+@pytest.mark.parametrize("layers,batch,kv,group,n_q,lens,n_splits", [
+    (2, 1, 8, 4, 1100, [577], 0),
+    (3, 2, 4, 8, 500, [449, 130], 0),
+    (2, 1, 4, 4, 301, [577], 6),
+])
+def test_many_bf16_query_rows_of_several_layers(rotations, layers, batch, kv, group, n_q, lens, n_splits):
+    pk = Packed(rotations, 123, layers=layers, batch=batch, kv=kv, group=group, cap=640, k_budget=192, v_bits=3,
+                behind=float("nan"), lens=lens)
+    assert bg.cross_workspace_bytes(pk.cfg, layers, n_q, n_splits, max(lens)) >= layers * batch * n_q * kv * group * 512
+    q, qd = pk.queries((layers, batch, n_q))
+    at = [0, 1, 31, 32, n_q // 2, n_q - 1]
+    ref, bound = expect_cross(pk, q[:, :, at], lens, FP32)
+    out = bg.blockgtq_cross_attn(pk.cfg, pk.layout, -1, qd, i32(lens), max(lens), pk.cache, n_splits=n_splits)
+    check("all layers", out[:, :, at], ref, bound)
+    one = bg.blockgtq_cross_attn(pk.cfg, pk.layout, layers - 1, qd[-1], i32(lens), max(lens), pk.cache, n_splits=n_splits)
+    check("last layer", one[:, at], ref[-1], bound[-1])
+
+
+@pytest.mark.parametrize("layers,batch,kv,group,prefix", [(2, 384, 4, 8, 1000), (3, 256, 4, 8, 700)])
+def test_shared_prefix_wide_pass_of_several_layers(rotations, layers, batch, kv, group, prefix):
+    lens = [(7 * b) % 41 for b in range(batch)]
+    kw = dict(layers=layers, kv=kv, group=group, k_budget=192, v_bits=3)
+    pk = Packed(rotations, 124, batch=batch, cap=64, **kw)
+    pp = Packed(rotations, 125, cap=1024, layout_of=pk, behind=float("inf"), lens=[prefix], **kw)
+    rows = layers * batch * kv * group
+    assert bg.shared_workspace_bytes(pk.cfg, pp.cfg, layers, 0, prefix, 40) >= rows * (512 + 2 * 528)
+    q, qd = pk.queries((layers, batch))
+    out = bg.blockgtq_decode_attn_shared(pk.cfg, pk.layout, -1, qd, pp.cfg, pp.cache, i32([prefix]), prefix, i32(lens), 40,
+                                         pk.cache, out_dtype=BF16)
+    for li in range(layers):
+        for b in (0, 1, 15, 16, 31, 32, batch - 1):
+            for h in (0, kv - 1):
+                hs = slice(group * h, group * h + group)
+                k, v = (np.concatenate([getattr(pp, n)[li, 0, h, :prefix], getattr(pk, n)[li, b, h, :lens[b]]]) for n in "kv")
+                check(f"layer {li} seq {b} head {h}", out[li, b, hs],
+                      *attention_and_bound(q[li, b, hs], k, v, pk.bits[li, h], pk.rot_k, pk.rot_v, BF16))
+
+
+@pytest.mark.parametrize("tout", ["bf16", "fp32"])
+@pytest.mark.parametrize("batch,kv,group,n_q,lens,n_splits", [
+    (1, 8, 4, 2048, [513], 0),          # 256 query rows to a workgroup
+    (2, 4, 5, 40, [513, 70], 6),        # 128
+])
+def test_every_row_of_the_wide_passes_is_that_of_the_narrow_ones(rotations, tout, batch, kv, group, n_q, lens, n_splits):
+    """Two fp32-grade results differ by 2e-5 of a row's 2-norm at most (1e-5 each); two bf16 roundings by 2^-8 each, and a
+    weight's 2^-11 each."""
+    dt = BF16 if tout == "bf16" else FP32
+    pk = Packed(rotations, 126, batch=batch, kv=kv, group=group, cap=576, k_budget=192, v_bits=3)
+    _, qd = pk.queries((batch, n_q))
+    assert bg.cross_workspace_bytes(pk.cfg, 1, n_q, n_splits, max(lens)) >= batch * n_q * kv * group * 512
+    out = bg.blockgtq_cross_attn(pk.cfg, pk.layout, 0, qd, i32(lens), max(lens), pk.cache, n_splits=n_splits, out_dtype=dt)
+    per = 32 // group
+    few = torch.cat([bg.blockgtq_cross_attn(pk.cfg, pk.layout, 0, qd[:, i:i + per].contiguous(), i32(lens), max(lens), pk.cache,
+                                            out_dtype=dt) for i in range(0, n_q, per)], 1)
+    err = float(((out.double() - few.double()).norm(dim=-1) / few.double().norm(dim=-1)).max())
+    print(f"{err:.3g}", flush=True)
+    assert err <= (2e-5 if dt == FP32 else 2.0 ** -7 + 2.0 ** -10), err
