@@ -889,9 +889,10 @@ struct CrossPlan {
 // The plan with the least estimated time over the row counts and splits.  One
 // workgroup runs per CU, so `items` of them take ceil(items / 256) rounds, each
 // as long as one split.  In us, measured (kernel times in a graph):
-//   32 rows: 12 a workgroup + 5.4 (key rows of up to 8 words) or 6.2 for
-//     every tile that its waves take one after the other: 8 waves to a
-//     sequence, or to 2, 4 or 8 of them, whose set-up is then one;
+//   32 rows: 12 a workgroup + 5.4 (key rows of up to 8 words), 6.2 (up to 16) or
+//     13 (above, where the row's words lie in scratch memory) for every tile
+//     that its waves take one after the other: 8 waves to a sequence, or to 2, 4
+//     or 8 of them, whose set-up is then one;
 //   128 rows: 14 + 1.8 a tile, 256 rows: 14 + 2.75 a tile, up to 1.3 times as
 //     much with all CUs busy, after a rotation launch of 9 + 1 per 5000 query
 //     rows;
@@ -915,7 +916,7 @@ static CrossPlan cross_plan(const Dims& d, int n_q, int max_len, int requested, 
       for (int k = k0; k <= std::max(k0, k1); ++k) {
         const int len = (tiles + k - 1) / k, n = (tiles + len - 1) / len;
         const double busy = 1.0 + 0.3 * std::min(1.0, blocks * n / 256.0);
-        const double wg = rows == 32 ? 12.0 + (d.k_words <= 8 ? 5.4 : 6.2) * ((len + wps - 1) / wps)
+        const double wg = rows == 32 ? 12.0 + (d.k_words <= 8 ? 5.4 : d.k_words <= 16 ? 6.2 : 13.0) * ((len + wps - 1) / wps)
                                      : 14.0 + (rows == 128 ? 1.8 : 2.75) * busy * len;
         const long rounds = (blocks * n + 255) / 256;
         double t = static_cast<double>(rounds) * wg;

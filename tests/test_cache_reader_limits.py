@@ -42,3 +42,12 @@ def test_shared_rows_of_a_call():
         assert bg.lib().blockgtq_decode_attn_shared(
             ctypes.byref(cfg.c()), F, 0, F, ctypes.byref(prefix.c()), ctypes.byref(cache), F, n_prefix, F, n_own,
             ctypes.byref(cache), F, 0, F, 1 << 60, 0, None) == -5
+
+
+@pytest.mark.parametrize("k_budget,wide", [(256, False), (512, True)])
+def test_wide_key_rows_go_to_the_wide_passes_sooner(k_budget, wide):
+    """A tile of a 32-word key row costs the 32-row pass twice what a 16-word one does, and the wide passes the same: 256
+    query positions on 4096 rows take 104 us there and 78 us here.  (Their workspace holds the rotated queries, 512 bytes a
+    row.)"""
+    cfg = cfg_of(4096, n_kv_heads=8, k_budget=k_budget, v_bits=4)
+    assert (bg.cross_workspace_bytes(cfg, 1, 256, 0, 4096) >= 256 * 32 * 512) == wide
