@@ -361,7 +361,9 @@ int blockgtq_dequantize_rows(const bgtq_config* cfg, const void* d_layout, int32
  * single generated token to whole prompts; the key axis is split where there
  * are few query rows.  Up to three launches on `stream` (the rotation of many
  * query rows, the attention, the join of splits); no allocation, no state in the
- * workspace, so the call can be captured in a HIP graph.
+ * workspace, so the call can be captured in a HIP graph.  (One position of a
+ * long context is faster in blockgtq_decode_attn, which has fp32 outputs only and
+ * one fp16 part of the weights.)
  * layer in [0, n_layers) or -1 for all layers.
  * d_q: [batch][n_q][n_kv_heads*group][128] in in_dtype, with a leading
  *      [n_layers] for layer == -1.  d_out: the same shape in out_dtype

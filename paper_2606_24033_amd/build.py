@@ -25,9 +25,11 @@ FLAGS = [
 # (finite codebooks and radii, -inf only as a mask), so skip the IEEE
 # canonicalization that would otherwise precede every max.
 DECODE_FLAGS = ["-fno-honor-nans", "-mno-amdgpu-ieee"]
-# The kernels that index a key row's words at a wave-uniform position keep them
-# in registers: beside their accumulators the default budget (bytes) puts the
-# array in scratch memory.
+# rows.hip indexes a key row's words at a wave-uniform position and keeps rows of
+# up to 16 words in registers (no scratch): beside its accumulators the default
+# budget (bytes) puts the array in scratch memory.  The 32-word kernels keep it
+# there all the same (176 bytes a lane), as do those of cross_impl.h without the
+# flag (0 to 164 bytes of spilled registers up to 16 words, 304 to 416 above).
 INDEXED_FLAGS = ["-mllvm", "-amdgpu-promote-alloca-to-vector-limit=100000"]
 
 

@@ -25,11 +25,12 @@
 // query rotation), 9K the tile (5.3K QK, 0.8K the maximum, 1.9K PV: lookups that
 // wait on LDS with two waves a SIMD), 8K for joining the waves, the output
 // rotation and the store.  A long pass takes 5.4 to 6.2 us for every tile of
-// each wave.  32 query rows are one column block of the product; a second
+// each wave, 13 where key rows have more than 16 words (they and some 60 other
+// registers lie in scratch memory).  32 query rows are one column block of the product; a second
 // block's accumulators and operands do not fit the 256 registers of two waves
 // a SIMD, and one wave a SIMD waits on each lookup.  Measured in a call: 8
 // sequences x 8 KV heads x 4 query rows on 150 to 1500 rows 21 us; 64 query rows
-// of 32 layers x 8 heads on 4001 rows and 4 each on 20 to 300 rows 190 us, 740
+// of 32 layers x 8 heads on 4001 rows and 4 each on 20 to 300 rows 189 us, 743
 // GB/s and 185 TFLOP/s of what the definition asks for.
 #pragma once
 #include <hip/hip_runtime.h>

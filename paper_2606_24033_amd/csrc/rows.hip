@@ -25,9 +25,10 @@
 // the hi part alone, 2^-11 of each term, 12 % of them would be another bf16 number
 // and elements whose terms cancel off by many of their own steps.
 //
-// What bounds it: writing the rows.  65536 rows x 8 heads of K2V2 to bf16: 107 us for 308
-// MB, 2.9 TB/s (72 us without the stores; keys alone 46, values alone 38).  A few
-// rows: the keys' matrix, about 10 of the 16 us of 16 rows of 32 layers x 8 heads.
+// What bounds it: writing the rows, and the decode and products that wait while a
+// wave stores.  65536 rows x 8 heads of K2V2 to bf16: 112 us for 308 MB, 2.7 TB/s.  A
+// few rows: the keys' matrix, more than half of the 20 us of 16 rows of 32 layers x
+// 8 heads, whose 512 workgroups take two rounds of the CUs.
 #include <hip/hip_runtime.h>
 
 #include <algorithm>
@@ -597,8 +598,10 @@ hipError_t launch_dequantize_rows(const Dims& d, const void* layout, const Cache
   call.out[1] = v_out;
   call.n_rows = n_rows;
   // One workgroup per CU: 256 of them share the units' tiles, a multiple of 8
-  // (a tile per wave) each; of both sides' the keys get 9 / 16 (65536 rows x 8
-  // heads, one side alone on all CUs: keys 46 us, values 38).
+  // (a tile per wave) each; of both sides' the keys get 9 / 16 (65536 random K2V2
+  // rows x 8 heads to bf16, one side alone on all CUs: keys 64 us, values 49).  In
+  // fp32 (83 and 97) 120 : 136 instead takes 175 us for 188 at 8 heads, but 55 for
+  // 42 at 2, where it rounds to one tile more a wave: the same share for both.
   const long units = static_cast<long>(d.n_kv) * d.n_lc * d.batch;
   const bool both = k_out && v_out;
   long items = 0;
