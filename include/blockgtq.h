@@ -423,6 +423,118 @@ int blockgtq_decode_attn_shared(const bgtq_config* cfg, const void* d_layout, in
                                 void* d_out, int32_t out_dtype, void* d_workspace, size_t ws_bytes, int32_t n_splits,
                                 void* stream);
 
+/* ---- Head norms and rotation of projected rows ----------------------------------
+ * What lies between a layer's projections and its cache: the root-mean-square
+ * norm of every query and key head, y = x w / sqrt(mean(x^2) + eps), and the
+ * rotation of its blocks by the token's position (Sec. 2.1; block i = dims (i,
+ * i + 64) by the angle d_pos[t][axis[i]] theta[i]) in one pass over the rows.
+ * The angle is formed and reduced in fp64; the rest is fp32, rounded once.  One
+ * launch on `stream`; no allocation.  Of cfg it takes the heads and in_dtype. */
+typedef struct {
+  int32_t n_axes;    /* positions of a token, 1..4: one for text; time, height and
+                        width for pictures and video                              */
+  uint8_t axis[64];  /* the position that each block turns with, below n_axes     */
+  double theta[64];  /* radians per position of each block, finite; text:
+                        rope_base^(-2i/128)                                       */
+} bgtq_rope;
+/* d_q: pre-RoPE queries, heads [n_kv_heads*group][128] of token t at element t *
+ *      q_stride, in in_dtype; d_k: the same for n_kv_heads and k_stride.  One of
+ *      them may be NULL (with its output).  A stride of more than the heads' own
+ *      elements reads them from a fused projection's rows.
+ * d_q_out, d_k_out: out_dtype, laid out by their own strides.  An output may be
+ *      its own input (same address, stride and type); other overlaps are the
+ *      caller's to avoid.
+ * d_pos: int32 [n_tokens][n_axes], any value.
+ * d_q_weight, d_k_weight: float [128], or NULL: that side is only rotated.
+ * eps: finite, >= 0.  (A row of zeros with eps = 0 gives not a number.)
+ * Rows, outputs and weights start 16-byte aligned, strides included (EINVAL
+ * otherwise); a stride is at least the heads' elements. */
+int blockgtq_norm_rope(const bgtq_config* cfg, const bgtq_rope* rope, int32_t n_tokens, const void* d_q,
+                       int64_t q_stride, const void* d_k, int64_t k_stride, const int32_t* d_pos,
+                       const float* d_q_weight, const float* d_k_weight, float eps, void* d_q_out,
+                       int64_t q_out_stride, void* d_k_out, int64_t k_out_stride, int32_t out_dtype, void* stream);
+
+/* ---- Packed cache in pages -------------------------------------------------------
+ * A pool of pages is a packed cache (layout above) whose "sequences" are the
+ * pages: cfg->batch pages of cfg->capacity rows (a multiple of 64).  A page
+ * table gives each sequence its pages, in any order; one table serves every
+ * layer.  A chunk is what one serving step adds to a ragged batch: each
+ * sequence's new tokens, from one (a generated token) to a prompt's, their rows
+ * one after the other.  The device arrays are read when the stream reaches the
+ * call, so that a captured graph takes new ones in the same buffers. */
+typedef struct {
+  const int32_t* d_cu_new;  /* [n_seqs + 1]: sequence s's new tokens are rows
+                               d_cu_new[s] .. d_cu_new[s + 1] - 1 of the inputs
+                               and outputs (none if equal).  Rows before the first
+                               and from the last number on belong to no sequence:
+                               they are not read into the cache, and outputs there
+                               are left as they were (a padded batch)             */
+  const int32_t* d_ctx_len; /* [n_seqs]: rows of the sequence with its new ones,
+                               which take the last of these positions            */
+  const int32_t* d_pages;   /* [n_seqs][max_pages]: row t of the sequence lies in
+                               page d_pages[s][t / capacity], at t % capacity;
+                               entries that no row needs are not read           */
+  int32_t n_seqs;           /* 0..65535                                          */
+  int32_t n_tokens;         /* rows of the inputs                                */
+  int32_t max_pages;        /* max_pages * capacity >= max_ctx (EINVAL otherwise) */
+  int32_t max_new, max_ctx; /* host-side bounds of a sequence's new tokens and rows */
+} bgtq_chunk;
+/* A sequence whose numbers leave these bounds (d_cu_new outside [0, n_tokens] or
+ * falling, more than max_new new tokens, fewer rows than new tokens, more than
+ * max_ctx rows) is appended nothing and its outputs are NaN; nothing outside the
+ * buffers is read or written. */
+
+/* Quantizes and packs the chunk's rows of one layer into the sequences' pages:
+ * blockgtq_quantize_append of a ragged batch.  Rows already in a touched page
+ * stay as they are.  d_k, d_v: post-RoPE keys and values in in_dtype, heads
+ * [n_kv_heads][128] of token t at element t * k_stride (v_stride), so that
+ * values may stay in a fused projection's rows; rows 16-byte aligned, strides
+ * included (EINVAL otherwise).  layer in [0, n_layers).  A row whose page number
+ * is outside [0, cfg->batch) is dropped (the attention over it gives NaN).  Pages
+ * that a call writes belong to one of its sequences each.  Async on `stream`, one
+ * launch, no allocation, no workspace. */
+int blockgtq_paged_append(const bgtq_config* cfg, const void* d_layout, int32_t layer, const void* d_k,
+                          int64_t k_stride, const void* d_v, int64_t v_stride, const bgtq_chunk* chunk,
+                          const bgtq_cache* cache, void* stream);
+
+/* How logits are changed and what else is seen; NULL: plain causal attention. */
+typedef struct {
+  float cap;                   /* > 0: a logit x = q k_hat / sqrt(d_h) becomes cap tanh(x / cap); 0: not */
+  const float* d_slopes;       /* [n_kv_heads*group] or NULL: head h's logits lose
+                                  d_slopes[h] |position - row| behind the cap   */
+  const int32_t* d_prefix_len; /* [n_seqs] or NULL: the sequence's first rows that
+                                  all of its new tokens see (a picture, an
+                                  instruction), also those behind a token's own
+                                  position; up to the sequence's rows            */
+} bgtq_scores;
+
+/* Attention of the chunk's new tokens over the pages: the token at position p of
+ * a sequence attends its rows 0 .. p and those of its prefix (the chunk's rows
+ * must have been appended), from single generated tokens to whole prompts and
+ * both in one call.  Up to five launches on `stream` (the rotation of many query
+ * rows; a pass each for sequences of few and of many query rows, and the join of
+ * its splits); no allocation, no state in the workspace, so the call can be
+ * captured in a HIP graph.
+ * layer in [0, n_layers).
+ * d_q: post-RoPE queries [n_tokens][n_kv_heads*group][128] in in_dtype; d_out:
+ *      the same shape in out_dtype, of the precision of blockgtq_cross_attn (the
+ *      capped logits of bf16 outputs are off by 2^-23 of the cap).  Both and
+ *      the workspace 16-byte aligned (EINVAL otherwise).
+ * A page number outside [0, cfg->batch) makes NaN of every output that attends
+ * the page's rows, and may of the sequence's other ones in this call.  What
+ * the cache holds in rows that a token does not see (not a number or infinite
+ * radii too) does not enter its outputs; a radius that is not finite in a row
+ * that it sees makes them NaN.
+ * n_splits: 0 = heuristic, else the splits of the key axis (1 .. 4096).
+ * d_workspace: blockgtq_paged_workspace_bytes bytes for the chunk's sizes, any
+ *      contents; calls that share it must not overlap in time.
+ * EUNSUPPORTED above 2^24 query rows (n_tokens x heads) or 2^30 rows. */
+int blockgtq_paged_workspace_bytes(const bgtq_config* cfg, int32_t n_seqs, int32_t n_tokens, int32_t max_new,
+                                   int32_t max_ctx, int32_t n_splits, size_t* bytes_out);
+int blockgtq_paged_attn(const bgtq_config* cfg, const void* d_layout, int32_t layer, const void* d_q,
+                        const bgtq_chunk* chunk, const bgtq_scores* scores, const bgtq_cache* cache, void* d_out,
+                        int32_t out_dtype, void* d_workspace, size_t ws_bytes, int32_t n_splits, void* stream);
+
 /* ---- Measurement helper (not a step of the method) ------------------------
  * Streaming read of d_src[0 .. bytes): the read-bandwidth ceiling that the
  * decode's roofline fraction is quoted against, next to the nominal 8 TB/s

@@ -30,7 +30,8 @@ EXPORTED = [
     "blockgtq_decode_attn_protected", "blockgtq_rope_step_workspace_bytes", "blockgtq_rope_decode_step",
     "blockgtq_read_probe", "blockgtq_decode_attn_noalloc", "blockgtq_dequantize_rows",
     "blockgtq_cross_workspace_bytes", "blockgtq_cross_attn", "blockgtq_shared_workspace_bytes",
-    "blockgtq_decode_attn_shared",
+    "blockgtq_decode_attn_shared", "blockgtq_norm_rope", "blockgtq_paged_append", "blockgtq_paged_workspace_bytes",
+    "blockgtq_paged_attn",
 ]
 
 
@@ -51,6 +52,19 @@ class _Cache(ctypes.Structure):
                 ("v_codes", ctypes.c_void_p), ("v_norms", ctypes.c_void_p)]
 
 
+class _Rope(ctypes.Structure):
+    _fields_ = [("n_axes", ctypes.c_int32), ("axis", ctypes.c_uint8 * N_BLOCKS), ("theta", ctypes.c_double * N_BLOCKS)]
+
+
+class _Chunk(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_void_p) for n in ("cu_new", "ctx_len", "pages")] + [
+        (n, ctypes.c_int32) for n in ("n_seqs", "n_tokens", "max_pages", "max_new", "max_ctx")]
+
+
+class _Scores(ctypes.Structure):
+    _fields_ = [("cap", ctypes.c_float), ("slopes", ctypes.c_void_p), ("prefix_len", ctypes.c_void_p)]
+
+
 _lib_handle = None
 
 
@@ -62,7 +76,7 @@ def lib():
             raise ImportError(f"{LIB_PATH} is missing; run __graft_entry__.build() first")
         L = ctypes.CDLL(LIB_PATH)
         L.blockgtq_last_error.restype = ctypes.c_char_p
-        P, I32, SZ = ctypes.c_void_p, ctypes.c_int32, ctypes.c_size_t
+        P, I32, I64, SZ, F32 = ctypes.c_void_p, ctypes.c_int32, ctypes.c_int64, ctypes.c_size_t, ctypes.c_float
         PSZ = ctypes.POINTER(ctypes.c_size_t)
         sig = {
             "blockgtq_energy_scores": [P, P, I32, I32, I32, P],
@@ -89,6 +103,10 @@ def lib():
             "blockgtq_cross_workspace_bytes": [P, I32, I32, I32, I32, PSZ],
             "blockgtq_cross_attn": [P, P, I32, P, I32, P, I32, P, P, I32, P, SZ, I32, P],
             "blockgtq_shared_workspace_bytes": [P, P, I32, I32, I32, I32, PSZ],
+            "blockgtq_norm_rope": [P, P, I32, P, I64, P, I64, P, P, P, F32, P, I64, P, I64, I32, P],
+            "blockgtq_paged_append": [P, P, I32, P, I64, P, I64, P, P, P],
+            "blockgtq_paged_workspace_bytes": [P, I32, I32, I32, I32, I32, PSZ],
+            "blockgtq_paged_attn": [P, P, I32, P, P, P, P, P, I32, P, SZ, I32, P],
             "blockgtq_decode_attn_shared": [P, P, I32, P, P, P, P, I32, P, I32, P, P, I32, P, SZ, I32, P],
         }
         for name, args in sig.items():
@@ -436,16 +454,20 @@ def _on(stream):
     return contextlib.nullcontext() if stream is None else torch.cuda.stream(stream)
 
 
-def _call(fn, stream, args, *tensors):
+def _call(fn, stream, args, *tensors, rows=()):
     """fn(*args, stream) on the one GPU that holds all the tensors (None is
-    skipped), whichever is current: on `stream`, or that GPU's current one."""
+    skipped), whichever is current: on `stream`, or that GPU's current one.
+    `rows`: tensors whose strides the call takes."""
     import torch
     tensors = [t for t in tensors if t is not None]
+    if not all(t.is_contiguous() for t in tensors):
+        raise ValueError("device tensors must be contiguous CUDA tensors")
+    tensors += [t for t in rows if t is not None]
     d = tensors[0].get_device()
     if stream is not None and stream.device_index != d:
         raise ValueError(f"a stream of device {stream.device_index} for tensors on device {d}")
     for t in tensors:
-        if t.get_device() < 0 or not t.is_contiguous():
+        if t.get_device() < 0:
             raise ValueError("device tensors must be contiguous CUDA tensors")
         if t.get_device() != d:
             raise ValueError("tensors on different devices: " + ", ".join(sorted({str(x.device) for x in tensors})))
@@ -579,6 +601,140 @@ def blockgtq_decode_attn_shared(cfg: Config, layout: Layout, layer: int, q, pref
            workspace.numel() * workspace.element_size(), n_splits),
           q, layout.blob, prefix_len, ctx_len, out, workspace, *_cache_tensors(cfg, cache),
           *_cache_tensors(prefix_cfg, prefix, "prefix"))
+    return out
+
+
+# ---------------------------------------------------------------- a serving step over pages
+
+class Rope:
+    """Rotation of a head's 64 blocks: radians per position of each, and the
+    position (of a token's `n_axes`) that each turns with (the only one by default)."""
+
+    def __init__(self, theta, axis=None, n_axes: int | None = None):
+        axis = [0] * N_BLOCKS if axis is None else [int(a) for a in axis]
+        theta = [float(t) for t in theta]
+        if len(theta) != N_BLOCKS or len(axis) != N_BLOCKS or not all(0 <= a < 256 for a in axis):
+            raise ValueError(f"a Rope needs {N_BLOCKS} thetas and as many axes")
+        self.n_axes = max(axis) + 1 if n_axes is None else n_axes
+        self._c = _Rope(self.n_axes, (ctypes.c_uint8 * N_BLOCKS)(*axis), (ctypes.c_double * N_BLOCKS)(*theta))
+
+    def c(self):
+        return self._c
+
+
+def _token_rows(what, t, n, heads, dtype):
+    """The token stride of [n, heads, 128] rows (a view of wider rows, too)."""
+    _check_shape(what, t, (n, heads, HEAD_DIM), dtype)
+    if t.numel() and (t.stride(2) != 1 or (heads > 1 and t.stride(1) != HEAD_DIM)):
+        raise ValueError(f"{what}: the heads of a token must lie one after the other")
+    return t.stride(0) if n > 1 else heads * HEAD_DIM
+
+
+def blockgtq_norm_rope(cfg: Config, rope: Rope, q, k, pos, q_weight=None, k_weight=None, eps: float = 1e-6, q_out=None,
+                       k_out=None, out_dtype=None, stream=None):
+    """q [n_tokens, Hq, 128] and k [n_tokens, H_kv, 128] (either may be None; the
+    token stride is free), each head normed where its weight (fp32 [128]) is given
+    and rotated at pos (int32 [n_tokens, n_axes]).  Returns (q_out, k_out), in the
+    outputs' or out_dtype (the inputs' by default); an output may be its input."""
+    import torch
+    if q is None and k is None:
+        raise ValueError("neither q nor k")
+    if (q is None and q_out is not None) or (k is None and k_out is not None):
+        raise ValueError("an output without its input")
+    n = (k if q is None else q).shape[0]
+    _check_shape("pos", pos, (n, rope.n_axes), torch.int32)
+    for name, w in (("q_weight", q_weight), ("k_weight", k_weight)):
+        if w is not None:
+            _check_shape(name, w, (HEAD_DIM,), torch.float32)
+    given = [t.dtype for t in (q_out, k_out) if t is not None]
+    dtype = given[0] if given else out_dtype or _in_dtype(cfg)
+    if any(t != dtype for t in given) or (out_dtype is not None and out_dtype != dtype):
+        raise ValueError(f"outputs of {given}, out_dtype {out_dtype}: they have one type")
+    with _on(stream):
+        if q is not None and q_out is None:
+            q_out = torch.empty(q.shape, dtype=dtype, device=q.device)
+        if k is not None and k_out is None:
+            k_out = torch.empty(k.shape, dtype=dtype, device=k.device)
+    args = [ctypes.byref(cfg.c()), ctypes.byref(rope.c()), n]
+    for name, t, heads in (("q", q, cfg.n_q_heads), ("k", k, cfg.n_kv_heads)):
+        args += [_at(t), 0 if t is None else _token_rows(name, t, n, heads, _in_dtype(cfg))]
+    args += [pos.data_ptr(), _at(q_weight), _at(k_weight), eps]
+    for name, t, heads in (("q_out", q_out, cfg.n_q_heads), ("k_out", k_out, cfg.n_kv_heads)):
+        args += [_at(t), 0 if t is None else _token_rows(name, t, n, heads, dtype)]
+    _call(lib().blockgtq_norm_rope, stream, (*args, _out_type(dtype)), pos, q_weight, k_weight, rows=(q, k, q_out, k_out))
+    return q_out, k_out
+
+
+class Chunk:
+    """What one serving step adds to a ragged batch over pages: int32 device
+    tensors cu_new [n_seqs + 1] (each sequence's new tokens among the call's
+    rows), ctx_len [n_seqs] (its rows with the new ones) and pages [n_seqs,
+    max_pages], and the host's bounds of a sequence's new tokens and rows."""
+
+    def __init__(self, cu_new, ctx_len, pages, max_new: int, max_ctx: int):
+        import torch
+        n = ctx_len.shape[0]
+        _check_shape("ctx_len", ctx_len, (n,), torch.int32)
+        _check_shape("cu_new", cu_new, (n + 1,), torch.int32)
+        if pages.dim() != 2:
+            raise ValueError(f"pages: expected [{n}, max_pages], got {tuple(pages.shape)}")
+        _check_shape("pages", pages, (n, pages.shape[1]), torch.int32)
+        self.cu_new, self.ctx_len, self.pages, self.max_new, self.max_ctx = cu_new, ctx_len, pages, max_new, max_ctx
+        self.n_seqs = n
+
+    def c(self, n_tokens: int):
+        return _Chunk(self.cu_new.data_ptr(), self.ctx_len.data_ptr(), self.pages.data_ptr(), self.n_seqs, n_tokens,
+                      self.pages.shape[1], self.max_new, self.max_ctx)
+
+    def tensors(self):
+        return self.cu_new, self.ctx_len, self.pages
+
+
+def blockgtq_paged_append(cfg: Config, layout: Layout, layer: int, k, v, chunk: Chunk, cache: Cache, stream=None):
+    """Quantizes and packs the chunk's rows k, v [n_tokens, H_kv, 128] (token
+    strides free) of one layer into the sequences' pages.  cache: the pool,
+    cfg.batch pages of cfg.capacity rows."""
+    _check_layout(cfg, layout)
+    n = k.shape[0]
+    strides = [_token_rows(name, t, n, cfg.n_kv_heads, _in_dtype(cfg)) for name, t in (("k", k), ("v", v))]
+    _call(lib().blockgtq_paged_append, stream,
+          (ctypes.byref(cfg.c()), layout.blob.data_ptr(), layer, k.data_ptr(), strides[0], v.data_ptr(), strides[1],
+           ctypes.byref(chunk.c(n)), ctypes.byref(cache.c())),
+          layout.blob, *chunk.tensors(), *_cache_tensors(cfg, cache), rows=(k, v))
+
+
+def paged_workspace_bytes(cfg: Config, chunk: Chunk, n_tokens: int, n_splits: int = 0) -> int:
+    v = ctypes.c_size_t()
+    _check(lib().blockgtq_paged_workspace_bytes(ctypes.byref(cfg.c()), chunk.n_seqs, n_tokens, chunk.max_new, chunk.max_ctx,
+                                                n_splits, ctypes.byref(v)))
+    return v.value
+
+
+def blockgtq_paged_attn(cfg: Config, layout: Layout, layer: int, q, chunk: Chunk, cache: Cache, cap: float = 0.0,
+                        slopes=None, prefix=None, out=None, workspace=None, n_splits: int = 0, out_dtype=None, stream=None):
+    """q [n_tokens, Hq, 128], the chunk's tokens, each attending the rows of its
+    sequence up to its own position and the first prefix[s] ones (int32 [n_seqs]);
+    cap: logits capped by cap tanh(x / cap); slopes (fp32 [Hq]): a bias of
+    -slopes[h] |position - row|.  Returns out, of q's shape in out's or out_dtype
+    (fp32 by default)."""
+    import torch
+    _check_layout(cfg, layout)
+    n = q.shape[0]
+    _check_shape("q", q, (n, cfg.n_q_heads, HEAD_DIM), _in_dtype(cfg))
+    if slopes is not None:
+        _check_shape("slopes", slopes, (cfg.n_q_heads,), torch.float32)
+    if prefix is not None:
+        _check_shape("prefix", prefix, (chunk.n_seqs,), torch.int32)
+    out, kind = _out_of(q, out, out_dtype, stream)
+    if workspace is None:
+        with _on(stream):
+            workspace = torch.empty(max(paged_workspace_bytes(cfg, chunk, n, n_splits), 1), dtype=torch.uint8, device=q.device)
+    scores = _Scores(cap, _at(slopes), _at(prefix))
+    _call(lib().blockgtq_paged_attn, stream,
+          (ctypes.byref(cfg.c()), layout.blob.data_ptr(), layer, q.data_ptr(), ctypes.byref(chunk.c(n)), ctypes.byref(scores),
+           ctypes.byref(cache.c()), out.data_ptr(), kind, workspace.data_ptr(),
+           workspace.numel() * workspace.element_size(), n_splits),
+          q, layout.blob, out, workspace, slopes, prefix, *chunk.tensors(), *_cache_tensors(cfg, cache))
     return out
 
 

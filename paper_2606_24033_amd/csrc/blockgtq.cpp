@@ -10,6 +10,7 @@
 #include <cstdarg>
 #include <cstdio>
 #include <cstring>
+#include <initializer_list>
 #include <string>
 #include <vector>
 
@@ -1098,6 +1099,235 @@ int blockgtq_decode_attn_shared(const bgtq_config* cfg, const void* d_layout, in
   call.out_dtype = out_dtype;
   hipError_t e = launch_cross(d, d_layout, d_q, call, rows, static_cast<hipStream_t>(stream));
   if (e != hipSuccess) return hip_fail(e, "decode_attn_shared launch");
+  return ok();
+}
+
+// ---------------------------------------------------------------- a serving step over pages
+
+static int check_rows(const char* what, const void* p, int64_t stride, long heads, int32_t dtype) {
+  const int64_t esize = dtype == BGTQ_BF16 ? 2 : 4;
+  if (stride < heads * kHeadDim) return fail(BGTQ_EINVAL, "%s: stride %lld below its heads' %ld elements", what, static_cast<long long>(stride), heads * kHeadDim);
+  if (stride > (int64_t{1} << 40)) return fail(BGTQ_EINVAL, "%s: stride %lld", what, static_cast<long long>(stride));
+  if (!aligned16(p) || stride * esize % 16 != 0) return fail(BGTQ_EINVAL, "%s: rows must be 16-byte aligned", what);
+  return BGTQ_OK;
+}
+
+int blockgtq_norm_rope(const bgtq_config* cfg, const bgtq_rope* rope, int32_t n_tokens, const void* d_q,
+                       int64_t q_stride, const void* d_k, int64_t k_stride, const int32_t* d_pos,
+                       const float* d_q_weight, const float* d_k_weight, float eps, void* d_q_out,
+                       int64_t q_out_stride, void* d_k_out, int64_t k_out_stride, int32_t out_dtype, void* stream) {
+  if (int e = check_cfg(cfg)) return e;
+  if (int e = check_out_dtype(out_dtype)) return e;
+  if (!rope) return fail(BGTQ_EINVAL, "rope is NULL");
+  if (rope->n_axes < 1 || rope->n_axes > 4) return fail(BGTQ_EINVAL, "n_axes %d outside 1..4", rope->n_axes);
+  NormRopeArgs a = {};
+  for (int i = 0; i < kRopeBlocks; ++i) {
+    if (rope->axis[i] >= rope->n_axes) return fail(BGTQ_EINVAL, "block %d turns with axis %d of %d", i, rope->axis[i], rope->n_axes);
+    if (!std::isfinite(rope->theta[i])) return fail(BGTQ_EINVAL, "theta of block %d is not finite", i);
+    a.axis[i] = rope->axis[i];
+    a.turns[i] = rope->theta[i] / (2.0 * M_PI);
+  }
+  if (!std::isfinite(eps) || eps < 0.f) return fail(BGTQ_EINVAL, "eps must be finite and >= 0");
+  if (n_tokens < 0) return fail(BGTQ_EINVAL, "n_tokens %d < 0", n_tokens);
+  if (n_tokens == 0) return ok();
+  if (!d_pos || (!d_q && !d_k)) return fail(BGTQ_EINVAL, "NULL pointer");
+  if (!d_q != !d_q_out || !d_k != !d_k_out) return fail(BGTQ_EINVAL, "an input without its output, or the other way round");
+  const long hq = static_cast<long>(cfg->n_kv_heads) * cfg->group;
+  if (hq > 1 << 20) return fail(BGTQ_EUNSUPPORTED, "%ld heads", hq);
+  if (d_q) {
+    if (int e = check_rows("q", d_q, q_stride, hq, cfg->in_dtype)) return e;
+    if (int e = check_rows("q_out", d_q_out, q_out_stride, hq, out_dtype)) return e;
+    a.q = {d_q, d_q_out, static_cast<size_t>(q_stride), static_cast<size_t>(q_out_stride), d_q_weight, static_cast<int>(hq)};
+  }
+  if (d_k) {
+    if (int e = check_rows("k", d_k, k_stride, cfg->n_kv_heads, cfg->in_dtype)) return e;
+    if (int e = check_rows("k_out", d_k_out, k_out_stride, cfg->n_kv_heads, out_dtype)) return e;
+    a.k = {d_k, d_k_out, static_cast<size_t>(k_stride), static_cast<size_t>(k_out_stride), d_k_weight, cfg->n_kv_heads};
+  }
+  if (!aligned16(d_q_weight) || !aligned16(d_k_weight)) return fail(BGTQ_EINVAL, "weights must be 16-byte aligned");
+  // (four items to a workgroup, an item at most one group of 8 heads)
+  if (static_cast<double>(n_tokens) * ((hq + 7) / 8 + (cfg->n_kv_heads + 7) / 8) > 4.0 * (1l << 24))
+    return fail(BGTQ_EUNSUPPORTED, "%d tokens of %ld heads in one call", n_tokens, hq + cfg->n_kv_heads);
+  a.pos = d_pos;
+  a.n_axes = rope->n_axes;
+  a.eps = eps;
+  hipError_t e = launch_norm_rope(a, n_tokens, cfg->in_dtype, out_dtype, static_cast<hipStream_t>(stream));
+  if (e != hipSuccess) return hip_fail(e, "norm_rope launch");
+  return ok();
+}
+
+static const long kMaxQueryRows = 1l << 24;
+
+static int check_chunk_sizes(const bgtq_config* cfg, int32_t n_seqs, int32_t n_tokens, int32_t max_new, int32_t max_ctx) {
+  if (n_seqs < 0 || n_seqs > 65535) return fail(BGTQ_EINVAL, "n_seqs %d outside 0..65535", n_seqs);
+  if (n_tokens < 0) return fail(BGTQ_EINVAL, "n_tokens %d < 0", n_tokens);
+  if (max_new < 0 || max_new > n_tokens) return fail(BGTQ_EINVAL, "max_new %d outside [0, n_tokens]", max_new);
+  if (max_ctx < max_new) return fail(BGTQ_EINVAL, "max_ctx %d below max_new %d", max_ctx, max_new);
+  if (max_ctx > kMaxCrossRows) return fail(BGTQ_EUNSUPPORTED, "max_ctx %d above 2^30 rows", max_ctx);
+  if (static_cast<double>(n_tokens) * cfg->n_kv_heads * cfg->group > static_cast<double>(kMaxQueryRows))
+    return fail(BGTQ_EUNSUPPORTED, "more than 2^24 query rows in one call");
+  return BGTQ_OK;
+}
+
+static int check_chunk(const bgtq_config* cfg, const bgtq_chunk* c) {
+  if (!c) return fail(BGTQ_EINVAL, "chunk is NULL");
+  if (int e = check_chunk_sizes(cfg, c->n_seqs, c->n_tokens, c->max_new, c->max_ctx)) return e;
+  if (c->max_pages < 0 || static_cast<int64_t>(c->max_pages) * cfg->capacity < c->max_ctx)
+    return fail(BGTQ_EINVAL, "%d pages of %d rows do not hold max_ctx %d", c->max_pages, cfg->capacity, c->max_ctx);
+  if (c->n_seqs > 0 && c->max_new > 0 && (!c->d_cu_new || !c->d_ctx_len || !c->d_pages)) return fail(BGTQ_EINVAL, "NULL pointer");
+  return BGTQ_OK;
+}
+
+static PagedBatch paged_batch(const bgtq_chunk* c) {
+  return {c->d_cu_new, c->d_ctx_len, c->d_pages, c->n_seqs, c->n_tokens, c->max_pages, c->max_new, c->max_ctx};
+}
+
+static bool chunk_empty(const bgtq_chunk* c) { return c->n_seqs == 0 || c->max_new == 0; }
+
+int blockgtq_paged_append(const bgtq_config* cfg, const void* d_layout, int32_t layer, const void* d_k,
+                          int64_t k_stride, const void* d_v, int64_t v_stride, const bgtq_chunk* chunk,
+                          const bgtq_cache* cache, void* stream) {
+  if (int e = check_cfg(cfg)) return e;
+  if (layer < 0 || layer >= cfg->n_layers) return fail(BGTQ_EINVAL, "layer %d out of range (one layer per call)", layer);
+  if (int e = check_chunk(cfg, chunk)) return e;
+  if (int e = check_cache(cache)) return e;
+  if (!d_layout) return fail(BGTQ_EINVAL, "NULL pointer");
+  if (chunk_empty(chunk)) return ok();
+  if (!d_k || !d_v) return fail(BGTQ_EINVAL, "NULL pointer");
+  if (int e = check_rows("k", d_k, k_stride, cfg->n_kv_heads, cfg->in_dtype)) return e;
+  if (int e = check_rows("v", d_v, v_stride, cfg->n_kv_heads, cfg->in_dtype)) return e;
+  if (cfg->n_kv_heads > 65535) return fail(BGTQ_EUNSUPPORTED, "%d heads", cfg->n_kv_heads);
+  const PagedRows rows = {paged_batch(chunk), static_cast<size_t>(k_stride), static_cast<size_t>(v_stride)};
+  hipError_t e = launch_paged_append(dims_of(cfg, layer), d_layout, d_k, d_v, rows, cache_ptrs(cache),
+                                     static_cast<hipStream_t>(stream));
+  if (e != hipSuccess) return hip_fail(e, "paged_append launch");
+  return ok();
+}
+
+// One pass of a call over pages (none: no rows).
+struct PagedPlan {
+  int rows, n_splits, split_len, lo, hi, unit_rows;
+  bool direct;
+  long blocks, items;
+  size_t part_bytes;
+};
+struct PagedPlans {
+  PagedPlan few, many;  // sequences of up to 32 query rows (a token or a few), and of more
+  size_t bytes;
+};
+
+// Rows of the workgroups and splits of a pass, by the estimates of cross_plan.
+// The host knows bounds only: `blocks` workgroups' rows at most, lengths of
+// max_len at most; a chunk's early rows see fewer (seen: the mean share).
+static PagedPlan paged_pass_plan(const Dims& d, std::initializer_list<int> widths, long n_seqs, long n_rows, long max_rows,
+                                 int max_len, double seen, int lo, int hi, int requested) {
+  PagedPlan best = {};
+  double t_best = 0.0;
+  const int tiles = std::max(1, (max_len + 63) / 64);
+  for (const int rows : widths) {
+    // a sequence's last block may be part empty; one block each at least
+    const long seqs = std::min(n_seqs, n_rows / (lo + 1));
+    const long blocks = max_rows <= rows ? n_seqs : std::min(seqs * ((max_rows + rows - 1) / rows), (n_rows + seqs * (rows - 1)) / rows);
+    const bool direct = max_rows <= rows;
+    const double est = d.n_kv * (direct || seqs == 1 ? static_cast<double>(blocks) : (n_rows + 0.5 * seqs * rows) / rows);
+    const int k0 = requested > 0 ? std::min(requested, tiles) : 1;
+    const int k1 = requested > 0 ? k0 : std::min(rows == 32 ? (tiles + 7) / 8 : tiles, 256);
+    for (int k = k0; k <= std::max(k0, k1); ++k) {
+      const int len = (tiles + k - 1) / k, n = (tiles + len - 1) / len;
+      const double busy = 1.0 + 0.3 * std::min(1.0, est * n / 256.0);
+      const double wg = rows == 32 ? 13.0 + (d.k_words <= 8 ? 5.4 : d.k_words <= 16 ? 6.2 : 13.0) * ((len + 7) / 8)
+                                   : 15.0 + (rows == 128 ? 1.8 : 2.75) * busy * len;
+      double t = std::ceil(est * n / 256.0) * wg;
+      // unequal workgroups follow one another without rounds
+      if (n_seqs > 1 || seen < 0.9) t = std::max(wg, 0.5 * t * seen + 0.5 * (0.65 * seen * est * n / 256 * wg + 0.5 * wg));
+      if (n > 1) t += 5.0 + 2.4e-7 * kPartFloats * 4 * n_rows * d.n_kv * n;
+      if (!best.rows || t < t_best) {
+        t_best = t;
+        best = {rows, n, 64 * len, lo, hi, direct ? static_cast<int>(std::min<long>((max_rows + 3) / 4 * 4, rows)) : rows,
+                direct, blocks, blocks * d.n_kv * n, 0};
+      }
+    }
+  }
+  best.part_bytes = best.n_splits > 1 ? al256(static_cast<size_t>(best.blocks) * d.n_kv * best.unit_rows * best.n_splits * kPartFloats * 4) : 0;
+  return best;
+}
+
+static PagedPlans paged_plans(const bgtq_config* cfg, int n_seqs, int n_tokens, int max_new, int max_ctx, int n_splits) {
+  PagedPlans p = {};
+  const Dims d = dims_of(cfg, 0);
+  const long rows = static_cast<long>(n_tokens) * d.group, max_rows = static_cast<long>(max_new) * d.group;
+  const int all = 0x7FFFFFFF;
+  if (max_rows <= 32) {
+    p.few = paged_pass_plan(d, {32}, n_seqs, rows, max_rows, max_ctx, 1.0, 0, all, n_splits);
+  } else {
+    // sequences beside the longest that have a token or a few each, on average:
+    // a pass of their own, with splits of their own
+    const bool both = n_seqs > 1 && (rows - max_rows) <= 32l * (n_seqs - 1);
+    if (both) p.few = paged_pass_plan(d, {32}, n_seqs, std::min(rows, 32l * n_seqs), 32, max_ctx, 1.0, 0, 32, n_splits);
+    const double seen = 1.0 - 0.5 * max_new / std::max(max_ctx, 1);
+    if (max_rows > 64) p.many = paged_pass_plan(d, {32, 128, 256}, n_seqs, rows, max_rows, max_ctx, seen, both ? 32 : 0, all, n_splits);
+    else p.many = paged_pass_plan(d, {32, 128}, n_seqs, rows, max_rows, max_ctx, seen, both ? 32 : 0, all, n_splits);
+  }
+  p.bytes = 256 + p.few.part_bytes + p.many.part_bytes + (p.many.rows > 32 ? al256(static_cast<size_t>(rows) * d.n_kv * kHeadDim * 4) : 0);
+  return p;
+}
+
+int blockgtq_paged_workspace_bytes(const bgtq_config* cfg, int32_t n_seqs, int32_t n_tokens, int32_t max_new,
+                                   int32_t max_ctx, int32_t n_splits, size_t* bytes_out) {
+  if (int e = check_cfg(cfg)) return e;
+  if (!bytes_out) return fail(BGTQ_EINVAL, "NULL pointer");
+  if (int e = check_chunk_sizes(cfg, n_seqs, n_tokens, max_new, max_ctx)) return e;
+  if (n_splits < 0 || n_splits > 4096) return fail(BGTQ_EINVAL, "n_splits %d outside 0..4096", n_splits);
+  *bytes_out = n_seqs == 0 || max_new == 0 ? 0 : paged_plans(cfg, n_seqs, n_tokens, max_new, max_ctx, n_splits).bytes;
+  return ok();
+}
+
+int blockgtq_paged_attn(const bgtq_config* cfg, const void* d_layout, int32_t layer, const void* d_q,
+                        const bgtq_chunk* chunk, const bgtq_scores* scores, const bgtq_cache* cache, void* d_out,
+                        int32_t out_dtype, void* d_workspace, size_t ws_bytes, int32_t n_splits, void* stream) {
+  if (int e = check_cfg(cfg)) return e;
+  if (int e = check_out_dtype(out_dtype)) return e;
+  if (layer < 0 || layer >= cfg->n_layers) return fail(BGTQ_EINVAL, "layer %d out of range (one layer per call)", layer);
+  if (int e = check_chunk(cfg, chunk)) return e;
+  if (n_splits < 0 || n_splits > 4096) return fail(BGTQ_EINVAL, "n_splits %d outside 0..4096", n_splits);
+  if (scores && (!std::isfinite(scores->cap) || scores->cap < 0.f)) return fail(BGTQ_EINVAL, "cap must be finite and >= 0");
+  if (int e = check_cache(cache)) return e;
+  if (!d_layout) return fail(BGTQ_EINVAL, "NULL pointer");
+  if (chunk_empty(chunk)) return ok();
+  if (!d_q || !d_out || !d_workspace) return fail(BGTQ_EINVAL, "NULL pointer");
+  if (!aligned16(d_q) || !aligned16(d_out) || !aligned16(d_workspace))
+    return fail(BGTQ_EINVAL, "q, out and the workspace must be 16-byte aligned");
+  const PagedPlans p = paged_plans(cfg, chunk->n_seqs, chunk->n_tokens, chunk->max_new, chunk->max_ctx, n_splits);
+  if (ws_bytes < p.bytes) return fail(BGTQ_EWORKSPACE, "workspace %zu bytes < %zu needed", ws_bytes, p.bytes);
+  for (const PagedPlan* pl : {&p.few, &p.many})  // (workgroups of a pass, and of its join of 4 rows each)
+    if (pl->items > kMaxItems || (pl->n_splits > 1 && pl->blocks * cfg->n_kv_heads * (pl->unit_rows / 4) > kMaxItems))
+      return fail(BGTQ_EUNSUPPORTED, "too many splits of too many query rows");
+  const Dims d = dims_of(cfg, layer, chunk->max_ctx);
+  hipStream_t s = static_cast<hipStream_t>(stream);
+  uint8_t* ws = static_cast<uint8_t*>(d_workspace);
+  const ScoreMods mods = scores ? ScoreMods{scores->cap, scores->d_slopes, scores->d_prefix_len} : ScoreMods{0.f, nullptr, nullptr};
+  for (const PagedPlan* pl : {&p.few, &p.many}) {
+    if (!pl->rows) continue;
+    CrossCall call = {};
+    call.side[0] = {cache_ptrs(cache), nullptr, cfg->batch, cfg->capacity, 0, pl->n_splits, pl->split_len, chunk->max_ctx, 0,
+                    static_cast<int>(pl->items), 0};
+    call.rows0 = pl->rows;
+    call.part = reinterpret_cast<float*>(ws);
+    ws += pl->part_bytes;
+    call.qr = reinterpret_cast<float*>(ws);
+    call.n_slots = pl->n_splits;
+    call.out = d_out;
+    call.out_dtype = out_dtype;
+    if (pl->rows > 32) {
+      Dims dq = d;  // (the chunk's tokens are one sequence's query rows)
+      dq.batch = 1;
+      hipError_t e = launch_query_rotation(dq, d_layout, d_q, chunk->n_tokens, call.qr, s);
+      if (e != hipSuccess) return hip_fail(e, "paged_attn rotation launch");
+    }
+    const PagedPass pass = {paged_batch(chunk), mods, static_cast<int>(pl->blocks), pl->lo, pl->hi, pl->unit_rows, pl->direct};
+    hipError_t e = launch_paged_pass(d, d_layout, d_q, call, pass, s);
+    if (e != hipSuccess) return hip_fail(e, "paged_attn launch");
+  }
   return ok();
 }
 

@@ -39,6 +39,7 @@
 #include "kernels.h"
 #include "layout.h"
 #include "mix.h"
+#include "paged_pass.h"
 
 namespace bgtq {
 namespace cross_detail {
@@ -379,9 +380,11 @@ __device__ __forceinline__ void build_tables(uint8_t* smem, const uint16_t* cbs,
 // output's own rounding to bf16.
 // PACK: a side may have several sequences in a workgroup (what it takes to find
 // a row's sequence is 0.5 us of a call of 16 without it).
-template <int KWB, int BV, bool EX, bool PACK>
+// MODE: WholeCache, or the new rows of a ragged batch over pages (paged_pass.h).
+template <int KWB, int BV, bool EX, bool PACK, class MODE>
 __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(2, 2))) void k_cross(
-    Dims d, const uint8_t* __restrict__ blob, const void* __restrict__ q, CrossCall call) {
+    Dims d, const uint8_t* __restrict__ blob, const void* __restrict__ q, CrossCall call, MODE mode) {
+  constexpr bool kPaged = MODE::kPaged, kMods = MODE::kMods;
   __shared__ __attribute__((aligned(16))) uint8_t smem[kLds];
   const int tid = threadIdx.x, lane = tid & 63, l32 = lane & 31, hf = lane >> 5;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
@@ -409,19 +412,45 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(2, 2))
   // after the other in the 32, a wave walks the tiles of one of them, and the
   // other sequences' columns of its products are not used.
   const int per = 1 << S.pack, wps = kWaves >> S.pack;  // sequences; waves to a sequence
-  const int n_blocks = (S.n_q * G + kRows - 1) / kRows, n_seq = (S.batch + per - 1) >> S.pack;
-  const int r0 = item % n_blocks * kRows;
-  item /= n_blocks;
-  const int kvh = item % d.n_kv;
-  item /= d.n_kv;
-  const int n_lz = d.n_lc * n_seq, z = item % n_lz, split = item / n_lz;
-  const int seq0 = z % n_seq << S.pack, lz = z / n_seq * S.batch + seq0, layer = d.layer >= 0 ? d.layer : z / n_seq;
-  const int sub = wave >> (3 - S.pack), seq = min(seq0 + sub, S.batch - 1);  // the wave's sequence
-  const int nr = S.n_q * G * min(per, S.batch - seq0);             // query rows
+  int r0, kvh, split, seq0 = 0, lz = 0, layer, sub = 0, seq, nr;  // nr: query rows
+  paged::Unit U = {};
+  if constexpr (kPaged) {
+    if (!paged::unit_of<kRows>(mode, d, item, U)) return;
+    r0 = U.r0;
+    kvh = U.kvh;
+    split = U.split;
+    layer = d.layer;
+    seq = U.seq;
+    nr = U.q.n * G;
+    if (!U.q.ok) {
+      if (split == 0) paged::refuse(U, d, kvh, call.out, call.out_dtype, tid, kThreads);
+      return;
+    }
+  } else {
+    const int n_blocks = (S.n_q * G + kRows - 1) / kRows, n_seq = (S.batch + per - 1) >> S.pack;
+    r0 = item % n_blocks * kRows;
+    item /= n_blocks;
+    kvh = item % d.n_kv;
+    item /= d.n_kv;
+    const int n_lz = d.n_lc * n_seq, z = item % n_lz;
+    split = item / n_lz;
+    seq0 = z % n_seq << S.pack;
+    lz = z / n_seq * S.batch + seq0;
+    layer = d.layer >= 0 ? d.layer : z / n_seq;
+    sub = wave >> (3 - S.pack);
+    seq = min(seq0 + sub, S.batch - 1);  // the wave's sequence
+    nr = S.n_q * G * min(per, S.batch - seq0);
+  }
   const int ri = layer * d.n_kv + kvh;
   const RowMeta* M = reinterpret_cast<const RowMeta*>(blob + kOffRows) + ri;
   const auto row_at = [&](int r) {  // query row r of the unit (or its sequences), in q, out and the partials
-    return (static_cast<size_t>(lz) * S.n_q + r / G) * hq + kvh * G + r % G;
+    if constexpr (kPaged) return (static_cast<size_t>(U.q.first) + r / G) * hq + kvh * G + r % G;
+    else return (static_cast<size_t>(lz) * S.n_q + r / G) * hq + kvh * G + r % G;
+  };
+  const auto part_of = [&](int r) {  // its partial
+    if constexpr (kPaged)
+      return call.part + (((static_cast<size_t>(U.block) * d.n_kv + kvh) * mode.unit_rows + (r - r0)) * call.n_slots + split) * kPartFloats;
+    else return call.part + (row_at(r) * call.n_slots + S.slot0 + split) * kPartFloats;
   };
 
   // The reads of the set-up that need no length, before the length is there (a
@@ -445,7 +474,7 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(2, 2))
 
   // The length and the row's groups, read together (the asm keeps the compiler
   // from reading each group where it is used, one wait after the other).
-  int len = S.len[seq], ng = M->n_groups;
+  int len = kPaged ? U.q.len : S.len[seq], ng = M->n_groups;
   uint32_t gm[8], used = 1u << (BV - 1);
   int gd[8], gp[8];
 #pragma unroll
@@ -465,24 +494,50 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(2, 2))
   }
   const int nslot = (ng + 1) & ~1;
   // a length outside [0, max_len] (the host's bound) makes the rows NaN
-  const bool ok = len >= 0 && len <= S.max_len;
+  const bool ok = kPaged || (len >= 0 && len <= S.max_len);
   const int t_begin = split * S.split_len;
-  const int t_end = ok && seq0 + sub < S.batch ? min(len, t_begin + S.split_len) : t_begin;
+  // the rows that the last query row sees; each row's own end (paged)
+  paged::Sight sight = {};
+  int t_end, lim = 0, lim0 = 0;
+  float slope = 0.f;
+  if constexpr (kPaged) {
+    sight = paged::sight_of(mode, U, seq);
+    t_end = min(sight.end((min(r0 + kRows, nr) - 1) / G), t_begin + S.split_len);
+    const int rl = min(r0 + l32, nr - 1);
+    lim = min(sight.end(rl / G), t_end);
+    lim0 = min(sight.end(r0 / G), t_end);
+    if (kMods && mode.m.slopes) slope = kLog2e * mode.m.slopes[kvh * G + rl % G];
+  } else {
+    t_end = ok && seq0 + sub < S.batch ? min(len, t_begin + S.split_len) : t_begin;
+  }
 
   if (t_begin >= t_end && call.n_slots > 1 && S.pack == 0) {  // no row of the sequence in this split: an empty partial
     if (tid < kRows && r0 + tid < nr) {
-      float* P = call.part + (row_at(r0 + tid) * call.n_slots + S.slot0 + split) * kPartFloats;
+      float* P = part_of(r0 + tid);
       P[0] = ok ? kNegInf : 0.f;
       P[1] = ok ? 0.f : __builtin_nanf("");
     }
     return;
   }
-  const size_t row = (static_cast<size_t>(layer) * S.batch + seq) * d.n_kv + kvh;
   const size_t cap = S.capacity;
-  const uint32_t* kc = S.c.k_codes + row * cap * kw;
-  const uint16_t* kn = S.c.k_norms + row * kMaxGroups * cap;
-  const uint32_t* vc = S.c.v_codes + row * (cap / kTile) * kHeadDim * BV;
-  const uint16_t* vn = S.c.v_norms + row * cap;
+  const uint32_t *kc, *vc;
+  const uint16_t *kn, *vn;
+  const auto rows_of = [&](size_t row) {  // (layer, sequence or page, head)
+    kc = S.c.k_codes + row * cap * kw;
+    kn = S.c.k_norms + row * kMaxGroups * cap;
+    vc = S.c.v_codes + row * (cap / kTile) * kHeadDim * BV;
+    vn = S.c.v_norms + row * cap;
+  };
+  // The wave's page numbers are read a tile ahead of the rows that need them.
+  int page_next = 0;
+  bool lost = false;  // a page outside the pool: the rows that attend it are not numbers
+  const auto turn_to = [&](int t) {  // rows [t, t + 64) of the sequence: the page whose number was read, and t there
+    lost |= static_cast<uint32_t>(page_next) >= static_cast<uint32_t>(S.batch);
+    const int page = lost ? 0 : page_next;
+    rows_of((static_cast<size_t>(layer) * S.batch + page) * d.n_kv + kvh);
+    return t % S.capacity;
+  };
+  if constexpr (!kPaged) rows_of((static_cast<size_t>(layer) * S.batch + seq) * d.n_kv + kvh);
   uint32_t nw[KWB], knp[4], vnw, vw[4][BV];  // (a half-wave loads the values of its own 32-row tile)
   const auto load_keys = [&](int t0) {
     const uint32_t* src = kc + static_cast<size_t>(t0) * kw;
@@ -516,6 +571,11 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(2, 2))
   };
   int t0 = t_begin + (wave & (wps - 1)) * kKeyTile;
   const int stride = wps * kKeyTile;
+  const auto read_page = [&](int t) {
+    if constexpr (kPaged) page_next = mode.b.pages[static_cast<size_t>(seq) * mode.b.max_pages + t / S.capacity];
+  };
+  // (without a next tile this one again: the loads in flight stay countable)
+  const auto after = [&](int t) { return t + stride < t_end ? t + stride : t; };
 
   // ---- set-up: the query rows rotated into stream order,
   //   q'[p] = log2 e / sqrt(d_g d_h) sum_d W[p][d] q[d],
@@ -532,8 +592,11 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(2, 2))
     if (call.n_slots == 1)
       near = reinterpret_cast<const float*>(blob + kOffRotVT)[(16 * wave + (lane & 15)) * kHeadDim + 32 * (lane >> 4)];
     if (t0 < t_end) {
-      load_keys(t0);
-      load_values(t0);
+      read_page(t0);
+      const int at = kPaged ? turn_to(t0) : t0;
+      load_keys(at);
+      load_values(at);
+      read_page(after(t0));
     }
     uint16_t* cbs = reinterpret_cast<uint16_t*>(smem + kBooks);
     if (tid < kCodebookEntries) cbs[tid] = cv;
@@ -649,7 +712,7 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(2, 2))
     for (int i = 0; i < 16; ++i) o[cc][i] = 0.f;
 
   for (; t0 < t_end; t0 += stride) {
-    const bool full = t0 + kKeyTile <= t_end;
+    const bool full = t0 + kKeyTile <= (kPaged ? lim0 : t_end);
     __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");  // the last tile's reads of the radii come first
     // this tile's radii, token-minor, for the wave's own reads (LDS operations
     // of a wave complete in order); a token past the end has value radius 0:
@@ -694,9 +757,23 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(2, 2))
 #pragma unroll
       for (int i = 0; i < 16; ++i) s[n][i] = 0.f;
     qk_all<KWB>(std::make_integer_sequence<int, 8>{}, smem, rw, gm, rad_l, rep, lane, s);
-    // (without a next tile this one again: the loads in flight stay countable)
-    const int t_next = t0 + stride < t_end ? t0 + stride : t0;
+    int t_next = after(t0);
+    if constexpr (kPaged) {
+      const int t = t_next;
+      t_next = turn_to(t);
+      read_page(after(t));
+    }
     load_keys(t_next);
+
+    const float sx = kMods ? 1.f : sc;  // what is left to multiply the logits with
+    if constexpr (kMods) {
+      const float at = static_cast<float>(sight.pos(min(r0 + l32, nr - 1) / G) - t0 - 4 * hf);
+#pragma unroll
+      for (int n = 0; n < 2; ++n)
+#pragma unroll
+        for (int i = 0; i < 16; ++i)
+          s[n][i] = paged::changed<EX>(mode.m.cap, slope, s[n][i] * sc, at - static_cast<float>(32 * n + 8 * (i >> 2) + (i & 3)));
+    }
 
     // ---- online softmax, base 2
     if (!full) {
@@ -705,7 +782,7 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(2, 2))
 #pragma unroll
         for (int i = 0; i < 16; ++i) {
           const int tok = t0 + 32 * n + 8 * (i >> 2) + 4 * hf + (i & 3);
-          s[n][i] = tok >= t_end ? kNegInf : s[n][i];
+          s[n][i] = tok >= (kPaged ? lim : t_end) ? kNegInf : s[n][i];
         }
     }
     float mp[4];
@@ -716,7 +793,7 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(2, 2))
       mp[c] = fmaxf(fmaxf(mp[c], s[1][4 * c]), s[1][4 * c + 1]);
       mp[c] = fmaxf(fmaxf(mp[c], s[1][4 * c + 2]), s[1][4 * c + 3]);
     }
-    const float mx = fmaxf(fmaxf(mp[0], mp[1]), fmaxf(mp[2], mp[3])) * sc;
+    const float mx = fmaxf(fmaxf(mp[0], mp[1]), fmaxf(mp[2], mp[3])) * sx;
     // a tile that raises no running maximum of the wave skips the rescale
     if (__builtin_amdgcn_ballot_w64(mx > m_run) != 0) {
       float x, y;
@@ -747,10 +824,12 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(2, 2))
       float ps = 0.f;
 #pragma unroll
       for (int u = 0; u < 4; ++u) {
-        const uint2 vr = *reinterpret_cast<const uint2*>(rad_l + 128 * 8 + 2 * (32 * n + 8 * u));
+        uint2 vr = *reinterpret_cast<const uint2*>(rad_l + 128 * 8 + 2 * (32 * n + 8 * u));
+        // (a radius that the row does not see may be infinite or not a number)
+        if (kPaged && !full) vr = paged::seen(vr, lim - (t0 + 32 * n + 8 * u + 4 * hf));
         float p[4];
 #pragma unroll
-        for (int i = 0; i < 4; ++i) p[i] = __builtin_amdgcn_exp2f(fmaf(s[n][4 * u + i], sc, -mref));
+        for (int i = 0; i < 4; ++i) p[i] = __builtin_amdgcn_exp2f(fmaf(s[n][4 * u + i], sx, -mref));
         ps += (p[0] + p[1]) + (p[2] + p[3]);
         pw[2 * u] = mix_pair(p[0], p[1], vr.x);
         pw[2 * u + 1] = mix_pair(p[2], p[3], vr.y);
@@ -800,6 +879,7 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(2, 2))
     swap32(l_run, x, y);
     l_run = x + y;
   }
+  if (kPaged && lost) l_run = __builtin_nanf("");
 
   // ---- the waves' states joined in LDS (over the tables)
   float4_t rot[8];  // this wave's 16 output dims of Pi_V^T, for the output rotation
@@ -857,7 +937,7 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(2, 2))
   if (n_row < 0) l = __builtin_nanf("");
   if (call.n_slots > 1) {
     if (r0 + r < nr) {
-      float* P = call.part + (row_at(r0 + r) * call.n_slots + S.slot0 + split) * kPartFloats;
+      float* P = part_of(r0 + r);
       if (d0 == 0) {
         // no row seen: -inf; logits that are all not a number leave the
         // maximum at -inf (fmaxf passes over them) but not the sum at 0
@@ -903,20 +983,43 @@ template <int BV>
 hipError_t launch_bv(const Dims& d, const void* layout, const void* q, const CrossCall& call, hipStream_t s) {
   const int items = call.side[0].items + call.side[1].items;
   const auto go = [&](auto kern) {
-    hipLaunchKernelGGL(kern, dim3(items), dim3(kThreads), 0, s, d, static_cast<const uint8_t*>(layout), q, call);
+    hipLaunchKernelGGL(kern, dim3(items), dim3(kThreads), 0, s, d, static_cast<const uint8_t*>(layout), q, call, paged::WholeCache{});
     return hipGetLastError();
   };
   const auto width = [&](auto ex, auto pack) {
     constexpr bool E = decltype(ex)::value, P = decltype(pack)::value;
-    if (d.k_words <= 8) return go(k_cross<8, BV, E, P>);
-    if (d.k_words <= 12) return go(k_cross<12, BV, E, P>);
-    if (d.k_words <= 16) return go(k_cross<16, BV, E, P>);
-    return go(k_cross<32, BV, E, P>);
+    using W = paged::WholeCache;
+    if (d.k_words <= 8) return go(k_cross<8, BV, E, P, W>);
+    if (d.k_words <= 12) return go(k_cross<12, BV, E, P, W>);
+    if (d.k_words <= 16) return go(k_cross<16, BV, E, P, W>);
+    return go(k_cross<32, BV, E, P, W>);
   };
   const bool pack = call.side[0].pack || call.side[1].pack;
   if (call.out_dtype == 0)  // BGTQ_FP32
     return pack ? width(std::true_type{}, std::true_type{}) : width(std::true_type{}, std::false_type{});
   return pack ? width(std::false_type{}, std::true_type{}) : width(std::false_type{}, std::false_type{});
+}
+
+template <int BV>
+hipError_t launch_paged_bv(const Dims& d, const void* layout, const void* q, const CrossCall& call, const PagedPass& pass,
+                           hipStream_t s) {
+  const auto go = [&](auto kern, auto mode) {
+    hipLaunchKernelGGL(kern, dim3(call.side[0].items), dim3(kThreads), 0, s, d, static_cast<const uint8_t*>(layout), q, call,
+                       mode);
+    return hipGetLastError();
+  };
+  const auto width = [&](auto ex, auto mode) {
+    constexpr bool E = decltype(ex)::value;
+    using M = decltype(mode);
+    if (d.k_words <= 8) return go(k_cross<8, BV, E, false, M>, mode);
+    if (d.k_words <= 12) return go(k_cross<12, BV, E, false, M>, mode);
+    if (d.k_words <= 16) return go(k_cross<16, BV, E, false, M>, mode);
+    return go(k_cross<32, BV, E, false, M>, mode);
+  };
+  const auto mods = [&](auto ex) {
+    return pass.m.cap > 0.f || pass.m.slopes ? width(ex, paged::Mode<true>{pass}) : width(ex, paged::Mode<false>{pass});
+  };
+  return call.out_dtype == 0 ? mods(std::true_type{}) : mods(std::false_type{});  // BGTQ_FP32
 }
 
 }  // namespace cross_detail

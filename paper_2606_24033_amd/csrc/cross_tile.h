@@ -24,6 +24,7 @@
 #include "kernels.h"
 #include "layout.h"
 #include "mix.h"
+#include "paged_pass.h"
 
 namespace bgtq {
 namespace cross_tile_detail {
@@ -53,41 +54,81 @@ __device__ __forceinline__ void scale_of(float mx, float& to, float& back) {
 }
 
 // EX: the softmax weights in two fp16 parts, for fp32 outputs (see cross_impl.h).
-template <int BV, int KS, bool EX>
+// MODE: WholeCache, or the new rows of a ragged batch over pages (paged_pass.h).
+template <int BV, int KS, bool EX, class MODE>
 __global__ __launch_bounds__(kAttnThreads) __attribute__((amdgpu_waves_per_eu(2, 2))) void k_cross_tile(
-    Dims d, const uint8_t* __restrict__ blob, const float* __restrict__ qr, CrossCall call) {
+    Dims d, const uint8_t* __restrict__ blob, const float* __restrict__ qr, CrossCall call, MODE mode) {
+  constexpr bool kPaged = MODE::kPaged, kMods = MODE::kMods;
   constexpr int kWgRows = kAttnWaves / KS * kWaveRows, NB = 2 / KS;  // query rows; token blocks of a wave
   __shared__ __attribute__((aligned(16))) uint8_t smem[kLdsBytes];
   const CrossSide& S = call.side[0];
   const int tid = threadIdx.x, lane = tid & 63;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int l32 = lane & 31, hf = lane >> 5;
-  const int G = d.group, hq = d.n_kv * G, kw = d.k_words, nr = S.n_q * G, n_blocks = (nr + kWgRows - 1) / kWgRows;
+  const int G = d.group, hq = d.n_kv * G, kw = d.k_words;
   int item = blockIdx.x;  // (row blocks fastest, splits slowest: see k_cross)
-  const int block = item % n_blocks;
-  item /= n_blocks;
-  const int kvh = item % d.n_kv;
-  item /= d.n_kv;
-  const int n_lz = d.n_lc * S.batch, lz = item % n_lz, split = item / n_lz;
-  const int seq = lz % S.batch, layer = d.layer >= 0 ? d.layer : lz / S.batch;
+  int nr, first, kvh, lz = 0, split, seq, layer;  // query rows of the unit, the workgroup's first one
+  paged::Unit U = {};
+  if constexpr (kPaged) {
+    if (!paged::unit_of<kWgRows>(mode, d, item, U)) return;
+    nr = U.q.n * G;
+    first = U.r0;
+    kvh = U.kvh;
+    split = U.split;
+    seq = U.seq;
+    layer = d.layer;
+    if (!U.q.ok) {
+      if (split == 0) paged::refuse(U, d, kvh, call.out, call.out_dtype, tid, kAttnThreads);
+      return;
+    }
+  } else {
+    nr = S.n_q * G;
+    const int n_blocks = (nr + kWgRows - 1) / kWgRows;
+    first = item % n_blocks * kWgRows;
+    item /= n_blocks;
+    kvh = item % d.n_kv;
+    item /= d.n_kv;
+    const int n_lz = d.n_lc * S.batch;
+    lz = item % n_lz;
+    split = item / n_lz;
+    seq = lz % S.batch;
+    layer = d.layer >= 0 ? d.layer : lz / S.batch;
+  }
   const RowMeta* M = reinterpret_cast<const RowMeta*>(blob + kOffRows) + (layer * d.n_kv + kvh);
   const int nslot = (M->n_groups + 1) & ~1;
   const int rw = KS == 1 ? wave : wave & 3;   // the wave's row block
   const int blk0 = KS == 1 ? 0 : wave >> 2;   // its first token block of a tile
-  const int r = block * kWgRows + rw * kWaveRows + l32;  // this lane's query row of the unit
+  const int r = first + rw * kWaveRows + l32;  // this lane's query row of the unit
   const int rc = min(r, nr - 1);
-  const size_t row_at = (static_cast<size_t>(lz) * S.n_q + rc / G) * hq + kvh * G + rc % G;
+  const size_t row_at = ((kPaged ? static_cast<size_t>(U.q.first) : static_cast<size_t>(lz) * S.n_q) + rc / G) * hq + kvh * G + rc % G;
+  const auto part_of = [&]() {
+    if constexpr (kPaged) return call.part + (((static_cast<size_t>(U.block) * d.n_kv + kvh) * mode.unit_rows + (rc - first)) * call.n_slots + split) * kPartFloats;
+    else return call.part + (row_at * call.n_slots + S.slot0 + split) * kPartFloats;
+  };
 
   // a length outside [0, max_len] (the host's bound) makes the rows NaN
-  const int len = S.len[seq];
-  const bool ok = len >= 0 && len <= S.max_len;
+  const int len = kPaged ? U.q.len : S.len[seq];
+  const bool ok = kPaged || (len >= 0 && len <= S.max_len);
   const int t_begin = split * S.split_len;
-  const int t_end = ok ? min(len, t_begin + S.split_len) : t_begin;
+  // the rows that the last query row sees; each row's own end, and the wave's
+  // first row's (paged)
+  paged::Sight sight = {};
+  int t_end, lim = 0, lim0 = 0;
+  float slope = 0.f;
+  if constexpr (kPaged) {
+    sight = paged::sight_of(mode, U, seq);
+    t_end = min(sight.end((min(first + kWgRows, nr) - 1) / G), t_begin + S.split_len);
+    lim = min(sight.end(rc / G), t_end);
+    lim0 = min(sight.end(min(first + rw * kWaveRows, nr - 1) / G), t_end);
+    if (kMods && mode.m.slopes) slope = kLog2e * mode.m.slopes[kvh * G + rc % G];
+  } else {
+    t_end = ok ? min(len, t_begin + S.split_len) : t_begin;
+  }
   const int n_kt = (max(t_end - t_begin, 0) + kKeyTile - 1) / kKeyTile;
 
   if (t_begin >= t_end && call.n_slots > 1) {  // no row of the sequence in this split: an empty partial
     if (r < nr && hf == 0 && (KS == 1 || wave < 4)) {
-      float* P = call.part + (row_at * call.n_slots + S.slot0 + split) * kPartFloats;
+      float* P = part_of();
       P[0] = ok ? kNegInf : 0.f;
       P[1] = ok ? 0.f : __builtin_nanf("");
     }
@@ -138,12 +179,21 @@ __global__ __launch_bounds__(kAttnThreads) __attribute__((amdgpu_waves_per_eu(2,
             cbs[cb_index(b) + (i & ((1 << b) - 1))] | (static_cast<uint32_t>(cbs[cb_index(b) + (i >> b)]) << 16);
   }
 
-  const size_t row = (static_cast<size_t>(layer) * S.batch + seq) * d.n_kv + kvh;
   const size_t cap = S.capacity;
-  const uint8_t* kc = reinterpret_cast<const uint8_t*>(S.c.k_codes + row * cap * kw);
-  const uint8_t* kn = reinterpret_cast<const uint8_t*>(S.c.k_norms + row * kMaxGroups * cap);
-  const uint8_t* vc = reinterpret_cast<const uint8_t*>(S.c.v_codes + row * (cap / kTile) * kHeadDim * BV);
-  const uint16_t* vnp = S.c.v_norms + row * cap;
+  const uint8_t *kc, *kn, *vc;
+  const uint16_t* vnp;
+  const auto rows_of = [&](size_t row) {  // (layer, sequence or page, head)
+    kc = reinterpret_cast<const uint8_t*>(S.c.k_codes + row * cap * kw);
+    kn = reinterpret_cast<const uint8_t*>(S.c.k_norms + row * kMaxGroups * cap);
+    vc = reinterpret_cast<const uint8_t*>(S.c.v_codes + row * (cap / kTile) * kHeadDim * BV);
+    vnp = S.c.v_norms + row * cap;
+  };
+  int page_next = 0;  // page number of the next tile to load, read a tile ahead of it
+  bool lost = false;  // a page outside the pool: the rows that attend it are not numbers
+  const auto read_page = [&](int t) {
+    if constexpr (kPaged) page_next = mode.b.pages[static_cast<size_t>(seq) * mode.b.max_pages + t / S.capacity];
+  };
+  if constexpr (!kPaged) rows_of((static_cast<size_t>(layer) * S.batch + seq) * d.n_kv + kvh);
 
   float m_run = kNegInf, l_run = 0.f;
   int v_top = 0, v_acc = 0;  // see radius_top: of the tiles decoded so far, and of those in o
@@ -162,8 +212,14 @@ __global__ __launch_bounds__(kAttnThreads) __attribute__((amdgpu_waves_per_eu(2,
     return t;
   };
   Raw<BV> raw;
-  const auto load_raw = [&](int ta) {
+  const auto load_raw = [&](int t) {
     const int tt = opaque_tid();
+    int ta = t;  // the tile's place in its cache row
+    if constexpr (kPaged) {
+      lost |= static_cast<uint32_t>(page_next) >= static_cast<uint32_t>(S.batch);
+      rows_of((static_cast<size_t>(layer) * S.batch + (lost ? 0 : page_next)) * d.n_kv + kvh);
+      ta = t % S.capacity;
+    }
     const uint8_t* ks = kc + static_cast<size_t>(ta) * kw * 4;
     const uint8_t* ns = kn + static_cast<size_t>(ta) * nslot * 2;
     uint32_t k_at = static_cast<uint32_t>((tt & 63) * kw * 4), n_at = static_cast<uint32_t>((tt & 63) * nslot * 2);
@@ -184,8 +240,8 @@ __global__ __launch_bounds__(kAttnThreads) __attribute__((amdgpu_waves_per_eu(2,
     for (int i = 0; i < NW; ++i) raw.v[i] = ld_at<uint32_t>(vs + 4 * i, v_lane);
     raw.vn = ld_at<uint16_t>(vnp + ta, vn_lane);
     // what lies behind the last row may be large, infinite or not a number: no radii
-    if (ta + kKeyTile > t_end) {
-      const uint32_t in = ta + (tt & 63) < t_end ? ~0u : 0u;
+    if (t + kKeyTile > t_end) {
+      const uint32_t in = t + (tt & 63) < t_end ? ~0u : 0u;
       raw.vn &= in;
       raw.kn = make_uint4(raw.kn.x & in, raw.kn.y & in, raw.kn.z & in, raw.kn.w & in);
     }
@@ -274,21 +330,35 @@ __global__ __launch_bounds__(kAttnThreads) __attribute__((amdgpu_waves_per_eu(2,
       }
       v_acc = v_cur;
     }
-    const float st = sc * __uint_as_float(static_cast<uint32_t>(127 - key_up(k_cur)) << 23);
-    if (t0 + 32 * (blk0 + NB) > t_end) {
+    float st = sc * __uint_as_float(static_cast<uint32_t>(127 - key_up(k_cur)) << 23);
+    if constexpr (kMods) {
+      const float at = static_cast<float>(sight.pos(rc / G) - t0 - hf4);
+#pragma unroll
+      for (int n = 0; n < NB; ++n)
+#pragma unroll
+        for (int i = 0; i < 16; ++i)
+          s[n][i] = paged::changed<EX>(mode.m.cap, slope, s[n][i] * st,
+                                       at - static_cast<float>(32 * (blk0 + n) + 8 * (i >> 2) + (i & 3)));
+      st = 1.f;
+    }
+    const bool cut = t0 + 32 * (blk0 + NB) > (kPaged ? lim0 : t_end);  // wave-uniform
+    if (cut) {
 #pragma unroll
       for (int n = 0; n < NB; ++n)
 #pragma unroll
         for (int i = 0; i < 16; ++i) {
           const int tok = t0 + 32 * (blk0 + n) + 8 * (i >> 2) + hf4 + (i & 3);
-          s[n][i] = tok >= t_end ? kNegInf : s[n][i];
+          s[n][i] = tok >= (kPaged ? lim : t_end) ? kNegInf : s[n][i];
         }
     }
     uint2 vr[4];
     const auto read_radii = [&](int n) {
 #pragma unroll
-      for (int q = 0; q < 4; ++q)
+      for (int q = 0; q < 4; ++q) {
         vr[q] = *reinterpret_cast<const uint2*>(dcur + kDecVN + 2 * (32 * (blk0 + n) + 8 * q + hf4));
+        // (a radius that the row does not see may be infinite or not a number)
+        if (kPaged && cut) vr[q] = paged::seen(vr[q], lim - (t0 + 32 * (blk0 + n) + 8 * q + hf4));
+      }
     };
     float mp[4];
 #pragma unroll
@@ -375,10 +445,13 @@ __global__ __launch_bounds__(kAttnThreads) __attribute__((amdgpu_waves_per_eu(2,
   // kt + 1, waves 0-3 decoding before and waves 4-7 after them, one barrier a
   // tile.  (A split without a tile loads and decodes its first one for nobody.)
   const auto tile_start = [&](int kt) { return t_begin + min(kt, max(n_kt - 1, 0)) * kKeyTile; };
+  read_page(t_begin);
   load_raw(t_begin);
+  read_page(tile_start(1));
   __syncthreads();
   decode(smem + kOffDec);
   load_raw(tile_start(1));
+  read_page(tile_start(2));
   __syncthreads();
   if (wave >= 4) __builtin_amdgcn_s_setprio(2);
   for (int kt = 0; kt < n_kt; ++kt) {
@@ -388,12 +461,14 @@ __global__ __launch_bounds__(kAttnThreads) __attribute__((amdgpu_waves_per_eu(2,
     if (wave < 4) {
       decode(dnxt);
       load_raw(tile_start(kt + 2));
+      read_page(tile_start(kt + 3));
     }
     products_qk(dcur);
     softmax_pv(dcur, t_begin + kt * kKeyTile, k_cur, v_cur);
     if (wave >= 4) {
       decode(dnxt);
       load_raw(tile_start(kt + 2));
+      read_page(tile_start(kt + 3));
     }
     __syncthreads();
   }
@@ -424,13 +499,13 @@ __global__ __launch_bounds__(kAttnThreads) __attribute__((amdgpu_waves_per_eu(2,
     }
     __syncthreads();
   }
-  if (!ok) l_run = __builtin_nanf("");
+  if (!ok || (kPaged && lost)) l_run = __builtin_nanf("");
   const bool mine = r < nr && (KS == 1 || wave < 4);
   const float v_back = __uint_as_float(static_cast<uint32_t>(127 - radius_up(v_acc)) << 23);
 
   if (call.n_slots > 1) {
     if (!mine) return;
-    float* P = call.part + (row_at * call.n_slots + S.slot0 + split) * kPartFloats;
+    float* P = part_of();
     if (hf == 0) {
       // (no row seen, or logits that are all not a number: see k_cross)
       P[0] = l_run == 0.f ? kNegInf : m_run == kNegInf ? 0.f : m_run;
@@ -509,27 +584,28 @@ __global__ __launch_bounds__(kAttnThreads) __attribute__((amdgpu_waves_per_eu(2,
   }
 }
 
-template <int BV, bool EX>
+template <int BV, bool EX, class MODE>
 hipError_t launch_tile_bv(const Dims& d, const uint8_t* blob, const float* qr, const CrossCall& call, bool half,
-                          hipStream_t s) {
+                          const MODE& mode, hipStream_t s) {
   const auto go = [&](auto kern) {
-    hipLaunchKernelGGL(kern, dim3(call.side[0].items), dim3(kAttnThreads), 0, s, d, blob, qr, call);
+    hipLaunchKernelGGL(kern, dim3(call.side[0].items), dim3(kAttnThreads), 0, s, d, blob, qr, call, mode);
     return hipGetLastError();
   };
-  return half ? go(k_cross_tile<BV, 2, EX>) : go(k_cross_tile<BV, 1, EX>);
+  return half ? go(k_cross_tile<BV, 2, EX, MODE>) : go(k_cross_tile<BV, 1, EX, MODE>);
 }
-template <bool EX>
-hipError_t launch_tile(const Dims& d, const void* layout, const float* qr, const CrossCall& call, bool half, hipStream_t s) {
+template <bool EX, class MODE>
+hipError_t launch_tile(const Dims& d, const void* layout, const float* qr, const CrossCall& call, bool half,
+                       const MODE& mode, hipStream_t s) {
   const uint8_t* blob = static_cast<const uint8_t*>(layout);
   switch (d.v_bits) {
-    case 1: return launch_tile_bv<1, EX>(d, blob, qr, call, half, s);
-    case 2: return launch_tile_bv<2, EX>(d, blob, qr, call, half, s);
-    case 3: return launch_tile_bv<3, EX>(d, blob, qr, call, half, s);
-    case 4: return launch_tile_bv<4, EX>(d, blob, qr, call, half, s);
-    case 5: return launch_tile_bv<5, EX>(d, blob, qr, call, half, s);
-    case 6: return launch_tile_bv<6, EX>(d, blob, qr, call, half, s);
-    case 7: return launch_tile_bv<7, EX>(d, blob, qr, call, half, s);
-    default: return launch_tile_bv<8, EX>(d, blob, qr, call, half, s);
+    case 1: return launch_tile_bv<1, EX>(d, blob, qr, call, half, mode, s);
+    case 2: return launch_tile_bv<2, EX>(d, blob, qr, call, half, mode, s);
+    case 3: return launch_tile_bv<3, EX>(d, blob, qr, call, half, mode, s);
+    case 4: return launch_tile_bv<4, EX>(d, blob, qr, call, half, mode, s);
+    case 5: return launch_tile_bv<5, EX>(d, blob, qr, call, half, mode, s);
+    case 6: return launch_tile_bv<6, EX>(d, blob, qr, call, half, mode, s);
+    case 7: return launch_tile_bv<7, EX>(d, blob, qr, call, half, mode, s);
+    default: return launch_tile_bv<8, EX>(d, blob, qr, call, half, mode, s);
   }
 }
 

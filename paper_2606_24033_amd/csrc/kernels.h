@@ -13,6 +13,8 @@ struct Dims {
   int max_ctx;    // decode calls: the host's bound on ctx_len (outputs of a sequence outside [0, max_ctx] are NaN)
 };
 
+constexpr int kRopeBlocks = 64;  // 2-D blocks of a head
+
 struct CachePtrs {
   uint32_t* k_codes;
   uint16_t* k_norms;
@@ -27,6 +29,25 @@ hipError_t launch_quantize_append(const Dims& d, const void* layout, const void*
 // k and v 16-byte aligned.
 hipError_t launch_quantize_prefill(const Dims& d, const void* layout, const void* k, const void* v, int n_new,
                                    const int32_t* write_pos, const CachePtrs& c, hipStream_t s);
+
+// A ragged batch over a pool of pages (paged.h).
+struct PagedBatch {
+  const int32_t* cu;     // [n_seqs + 1]
+  const int32_t* ctx;    // [n_seqs]
+  const int32_t* pages;  // [n_seqs][max_pages]
+  int n_seqs, n_tokens, max_pages;
+  int max_new, max_ctx;  // the host's bounds on a sequence's new tokens and rows
+};
+// The append of a ragged batch's rows to their pages; stride: elements from a
+// token's heads to the next one's.
+struct PagedRows {
+  PagedBatch b;
+  size_t k_stride, v_stride;
+};
+hipError_t launch_paged_append(const Dims& d, const void* layout, const void* k, const void* v, const PagedRows& rows,
+                               const CachePtrs& c, hipStream_t s);
+hipError_t launch_paged_quantize(const Dims& d, const void* layout, const void* k, const void* v, const PagedRows& rows,
+                                 const CachePtrs& c, hipStream_t s);
 
 // Workspace carve-up of one decode call.
 struct DecodeWs {
@@ -134,6 +155,41 @@ struct CrossCall {
   void* out;
   int out_dtype;
 };
+// What a query row of a pass over pages sees and how its logits are changed.
+struct ScoreMods {
+  float cap;              // 0: none
+  const float* slopes;    // [Hq] or null
+  const int32_t* prefix;  // [n_seqs] or null
+};
+// One pass over pages (paged_pass.h): blocks of the sequences with lo < query
+// rows <= hi.  Its CrossCall has one side: the pool.  Partials lie
+// [n_blocks][n_kv][unit_rows][n_slots].
+struct PagedPass {
+  PagedBatch b;
+  ScoreMods m;
+  int n_blocks, lo, hi, unit_rows;
+  bool direct;  // block = sequence
+};
+// Passes of 32-row workgroups (call.rows0) or of 128 or 256 on the rotated query rows call.qr, and
+// their join where there are splits (paged.hip).
+hipError_t launch_paged_pass(const Dims& d, const void* layout, const void* q, const CrossCall& call, const PagedPass& pass,
+                             hipStream_t s);
+#define BGTQ_DECL_PAGED(N)                                                                                          \
+  hipError_t launch_paged_bv##N(const Dims& d, const void* layout, const void* q, const CrossCall& call,            \
+                                const PagedPass& pass, hipStream_t s);
+BGTQ_DECL_PAGED(1)
+BGTQ_DECL_PAGED(2)
+BGTQ_DECL_PAGED(3)
+BGTQ_DECL_PAGED(4)
+BGTQ_DECL_PAGED(5)
+BGTQ_DECL_PAGED(6)
+BGTQ_DECL_PAGED(7)
+BGTQ_DECL_PAGED(8)
+#undef BGTQ_DECL_PAGED
+hipError_t launch_paged_tile_bf16(const Dims& d, const void* layout, const CrossCall& call, const PagedPass& pass,
+                                  hipStream_t s);
+hipError_t launch_paged_tile_fp32(const Dims& d, const void* layout, const CrossCall& call, const PagedPass& pass,
+                                  hipStream_t s);
 hipError_t launch_cross(const Dims& d, const void* layout, const void* q, const CrossCall& call, long rows,
                         hipStream_t s);
 // k_cross (cross_impl.h), one entry per value code width (cross_bv1.hip .. cross_bv8.hip).
@@ -153,6 +209,24 @@ hipError_t launch_cross_tile_bf16(const Dims& d, const void* layout, const float
                                   hipStream_t s);
 hipError_t launch_cross_tile_fp32(const Dims& d, const void* layout, const float* qr, const CrossCall& call, bool half,
                                   hipStream_t s);
+
+// Head norms and rotation of projected rows (norm_rope.hip).
+struct NormRopeSide {
+  const void* in;
+  void* out;
+  size_t in_stride, out_stride;  // elements from a token's heads to the next one's
+  const float* weight;           // [128], or null: no norm
+  int heads;                     // 0: no rows of this side
+};
+struct NormRopeArgs {
+  NormRopeSide q, k;
+  const int32_t* pos;  // [n_tokens][n_axes]
+  int n_axes;
+  float eps;
+  double turns[kRopeBlocks];  // turns (of 2 pi) per position of each block
+  uint8_t axis[kRopeBlocks];
+};
+hipError_t launch_norm_rope(const NormRopeArgs& a, long n_tokens, int in_dtype, int out_dtype, hipStream_t s);
 
 // Streaming read of `bytes` (a multiple of 16, 16-byte aligned) at src;
 // writes sink[0] only in a case no real input reaches (probe.hip).

@@ -8,8 +8,11 @@
 #include <hip/hip_fp16.h>
 #include <hip/hip_runtime.h>
 
+#include <type_traits>
+
 #include "kernels.h"
 #include "layout.h"
+#include "paged.h"
 
 namespace bgtq {
 
@@ -51,11 +54,18 @@ __device__ __forceinline__ int scalar_code(const float* thr, int b, float z) {
 // ---------------------------------------------------------------------------
 constexpr int kRowAppend = 4;
 
-template <bool BF16>
+// Rows of a cache: sequence blockIdx.y of the call, at wpos.  (PagedRows: the
+// ragged batch's sequence blockIdx.y; each row has a page of its own.)
+struct FixedRows {
+  const int32_t* wpos;
+  int n_new;
+};
+
+template <bool BF16, class ROWS>
 __global__ __launch_bounds__(1024) void k_append_rows(Dims d, const uint8_t* __restrict__ blob,
                                                       const void* __restrict__ kin,
-                                                      const void* __restrict__ vin, int n_new,
-                                                      const int32_t* __restrict__ wpos, CachePtrs c) {
+                                                      const void* __restrict__ vin, ROWS rows, CachePtrs c) {
+  constexpr bool kPaged = std::is_same_v<ROWS, PagedRows>;
   __shared__ float xk[kRowAppend][kHeadDim];
   __shared__ float xv[kRowAppend][kHeadDim];
   __shared__ float pk[kRowAppend][4][kHeadDim];  // quarter sums of the rotated key positions
@@ -71,13 +81,44 @@ __global__ __launch_bounds__(1024) void k_append_rows(Dims d, const uint8_t* __r
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
   const int head = blockIdx.x, lz = blockIdx.y;
   const int layer = d.layer >= 0 ? d.layer : lz / d.batch;
-  const int seq = lz % d.batch;
   const int cap = d.capacity;
+  // rows of the call (their first input row, where they go, how many) and the
+  // cache row (layer, sequence or page, head) of each
+  int in0, n_new, wp;
+  bool ok = true;
+  size_t row_of[kRowAppend];
+  if constexpr (kPaged) {
+    const paged::Seq q = paged::seq_of(rows.b, lz);
+    in0 = q.first;
+    wp = q.len - q.n;
+    n_new = q.n;
+    ok = q.ok && q.n <= kRowAppend;  // (the host sends sequences of more rows elsewhere)
+    if (!ok || n_new == 0) return;
+#pragma unroll
+    for (int s = 0; s < kRowAppend; ++s) {
+      const int page = s < n_new ? paged::page_of(rows.b, d.batch, cap, lz, wp + s) : -1;
+      row_of[s] = page < 0 ? ~size_t(0) : (static_cast<size_t>(layer) * d.batch + page) * d.n_kv + head;
+    }
+  } else {
+    n_new = rows.n_new;
+    in0 = lz * n_new;
+    wp = rows.wpos[lz % d.batch];
+#pragma unroll
+    for (int s = 0; s < kRowAppend; ++s)
+      row_of[s] = (static_cast<size_t>(layer) * d.batch + lz % d.batch) * d.n_kv + head;
+  }
+  const auto to = [&](int s) {  // (a select chain: s is no constant)
+    size_t r = row_of[0];
+#pragma unroll
+    for (int u = 1; u < kRowAppend; ++u) r = s == u ? row_of[u] : r;
+    return r;
+  };
+  const auto place = [&](int s) { return kPaged ? (wp + s) % cap : wp + s; };  // the row's place there
+  const auto there = [&](int s) { return !kPaged || to(s) != ~size_t(0); };
   const RowMeta* M = reinterpret_cast<const RowMeta*>(blob + kOffRows) + (layer * d.n_kv + head);
   const float* rotkt = reinterpret_cast<const float*>(blob + kOffRotKT);
   const float* rotvt = reinterpret_cast<const float*>(blob + kOffRotVT);
   const float* gthr = reinterpret_cast<const float*>(blob + kOffThr);
-  const size_t row = (static_cast<size_t>(layer) * d.batch + seq) * d.n_kv + head;
 
   // group table (wave-uniform); the group of key position p is the last one
   // that starts at or before p
@@ -114,30 +155,36 @@ __global__ __launch_bounds__(1024) void k_append_rows(Dims d, const uint8_t* __r
   for (int u = 0; u < 32; ++u) rc[u] = rsrc[min(32 * qq + u, rlast) * rstride];
   // the other reads take clamped indices (in bounds, surplus values unused)
   // so that they need no branch either
-  const size_t xoff =
-      ((static_cast<size_t>(lz) * n_new + min(tid >> 7, n_new - 1)) * d.n_kv + head) * kHeadDim + p;
+  const size_t xrow = static_cast<size_t>(in0) + min(tid >> 7, n_new - 1);
+  size_t kx, vx;
+  if constexpr (kPaged) {
+    kx = xrow * rows.k_stride + head * kHeadDim + p;
+    vx = xrow * rows.v_stride + head * kHeadDim + p;
+  } else {
+    kx = vx = (xrow * d.n_kv + head) * kHeadDim + p;
+  }
   float xkv, xvv;
   if constexpr (BF16) {
-    xkv = __uint_as_float(static_cast<uint32_t>(reinterpret_cast<const uint16_t*>(kin)[xoff]) << 16);
-    xvv = __uint_as_float(static_cast<uint32_t>(reinterpret_cast<const uint16_t*>(vin)[xoff]) << 16);
+    xkv = __uint_as_float(static_cast<uint32_t>(reinterpret_cast<const uint16_t*>(kin)[kx]) << 16);
+    xvv = __uint_as_float(static_cast<uint32_t>(reinterpret_cast<const uint16_t*>(vin)[vx]) << 16);
   } else {
-    xkv = reinterpret_cast<const float*>(kin)[xoff];
-    xvv = reinterpret_cast<const float*>(vin)[xoff];
+    xkv = reinterpret_cast<const float*>(kin)[kx];
+    xvv = reinterpret_cast<const float*>(vin)[vx];
   }
   const float tv = gthr[min(tid, kThresholdEntries - 1)];
   const uint32_t mw = reinterpret_cast<const uint32_t*>(M->dim)[tid & (kHeadDim / 4 - 1)];
   const uint32_t bw = reinterpret_cast<const uint32_t*>(M->bitoff)[tid & (kHeadDim / 2 - 1)];
   // the value words of the first row (value thread j = tid - 512 < 128), read
   // here so that its read-modify-write costs no extra round trip
-  const int wp = wpos[seq];
   const int bv = d.v_bits;
   const int vj = (tid - 512) & 127;
-  const int wp0 = min(max(wp, 0), cap - 1);
+  const int wp0 = min(max(place(0), 0), cap - 1);
   const int vbit0 = (wp0 % kTile) * bv, vw0 = vbit0 >> 5;
-  uint32_t* const vrow0 = c.v_codes + ((row * (cap / kTile) + wp0 / kTile) * kHeadDim + vj) * static_cast<size_t>(bv);
+  const size_t r0 = there(0) ? row_of[0] : 0;
+  uint32_t* const vrow0 = c.v_codes + ((r0 * (cap / kTile) + wp0 / kTile) * kHeadDim + vj) * static_cast<size_t>(bv);
   const uint32_t v0lo = vrow0[vw0], v0hi = vrow0[min(vw0 + 1, bv - 1)];
-  if (wp < 0 || wp >= cap) return;
-  const int nt = min(n_new, cap - wp);  // rows that fit (the host rejects overflow)
+  if (!kPaged && (wp < 0 || wp >= cap)) return;
+  const int nt = kPaged ? n_new : min(n_new, cap - wp);  // rows that fit (the host rejects overflow)
   if (tid < nt * kHeadDim) {
     xk[tid >> 7][p] = xkv;
     xv[tid >> 7][p] = xvv;
@@ -204,8 +251,8 @@ __global__ __launch_bounds__(1024) void k_append_rows(Dims d, const uint8_t* __r
       const int bo = boff[p], w = bo >> 5, sh = bo & 31;
       atomicOr(&kwd[s][w], code << sh);
       if (sh + bk > 32) atomicOr(&kwd[s][w + 1], code >> (32 - sh));
-      if (p == p0)
-        c.k_norms[row * kMaxGroups * cap + static_cast<size_t>(wp + s) * ((ng + 1) & ~1) + gk] =
+      if (p == p0 && there(s))
+        c.k_norms[to(s) * kMaxGroups * cap + static_cast<size_t>(place(s)) * ((ng + 1) & ~1) + gk] =
             __half_as_ushort(__float2half_rn(n));
     }
   } else if (tid < 2 * kHeadDim) {
@@ -215,7 +262,7 @@ __global__ __launch_bounds__(1024) void k_append_rows(Dims d, const uint8_t* __r
       const float n = nrm[s][kMaxGroups];
       const float scale = n > 0.f ? sqrtf(static_cast<float>(kHeadDim)) / n : 0.f;
       cv[s][p] = static_cast<uint8_t>(scalar_code(thr + thr_index(bv), bv, z * scale));
-      if (p == 0) c.v_norms[row * cap + wp + s] = __half_as_ushort(__float2half_rn(n));
+      if (p == 0 && there(s)) c.v_norms[to(s) * cap + place(s)] = __half_as_ushort(__float2half_rn(n));
     }
   }
   __syncthreads();
@@ -224,13 +271,14 @@ __global__ __launch_bounds__(1024) void k_append_rows(Dims d, const uint8_t* __r
   const int kw = d.k_words;
   if (tid < nt * kw) {
     const int s = tid / kw, w = tid - s * kw;
-    c.k_codes[(row * cap + wp + s) * kw + w] = kwd[s][w];
+    if (there(s)) c.k_codes[(to(s) * cap + place(s)) * kw + w] = kwd[s][w];
   } else if (tid >= 512 && tid < 512 + kHeadDim) {
     const int j = vj;
     const uint32_t mask = (1u << bv) - 1u;
     for (int s = 0; s < nt; ++s) {
-      const int t = wp + s, slot = t % kTile, bit = slot * bv, w = bit >> 5, sh = bit & 31;
-      uint32_t* vw = c.v_codes + ((row * (cap / kTile) + t / kTile) * kHeadDim + j) * static_cast<size_t>(bv);
+      if (!there(s)) continue;
+      const int t = place(s), slot = t % kTile, bit = slot * bv, w = bit >> 5, sh = bit & 31;
+      uint32_t* vw = c.v_codes + ((to(s) * (cap / kTile) + t / kTile) * kHeadDim + j) * static_cast<size_t>(bv);
       const uint32_t code = cv[s][j];
       // row 0 starts from the words read up front; later rows re-read (a row
       // may share a word with the previous one)
@@ -252,12 +300,21 @@ hipError_t launch_quantize_append(const Dims& d, const void* layout, const void*
                                   hipStream_t s) {
   if (n_new <= 0) return hipSuccess;
   if (n_new <= kRowAppend) {
-    const auto kern = d.in_dtype == 1 ? k_append_rows<true> : k_append_rows<false>;
+    const auto kern = d.in_dtype == 1 ? k_append_rows<true, FixedRows> : k_append_rows<false, FixedRows>;
     hipLaunchKernelGGL(kern, dim3(d.n_kv, d.batch * d.n_lc), dim3(1024), 0, s, d,
-                       static_cast<const uint8_t*>(layout), k, v, n_new, write_pos, c);
+                       static_cast<const uint8_t*>(layout), k, v, FixedRows{write_pos, n_new}, c);
     return hipGetLastError();
   }
   return launch_quantize_prefill(d, layout, k, v, n_new, write_pos, c, s);
+}
+
+hipError_t launch_paged_append(const Dims& d, const void* layout, const void* k, const void* v, const PagedRows& rows,
+                               const CachePtrs& c, hipStream_t s) {
+  if (rows.b.max_new > kRowAppend) return launch_paged_quantize(d, layout, k, v, rows, c, s);
+  const auto kern = d.in_dtype == 1 ? k_append_rows<true, PagedRows> : k_append_rows<false, PagedRows>;
+  hipLaunchKernelGGL(kern, dim3(d.n_kv, rows.b.n_seqs), dim3(1024), 0, s, d, static_cast<const uint8_t*>(layout), k, v,
+                     rows, c);
+  return hipGetLastError();
 }
 
 hipError_t launch_decode_packed(const Dims& d, const void* layout, const void* q,

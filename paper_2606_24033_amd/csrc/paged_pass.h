@@ -1,0 +1,124 @@
+// The attention passes of cross_impl.h and cross_tile.h over pages: which query
+// rows of a ragged batch a workgroup takes, which cache rows each of them sees,
+// and what happens to a logit before the softmax.
+//
+// Query row r of a sequence is head r % G of its new token r / G.  A unit is
+// (block of query rows, KV head, split of the key axis).  Blocks are numbered
+// sequence after sequence; the host knows only an upper bound of their number
+// (it has no lengths), so the last workgroups may have none.  A call may run two
+// passes, for sequences of few and of many query rows: a pass takes the
+// sequences with lo < rows <= hi.
+#pragma once
+#include <hip/hip_runtime.h>
+
+#include "kernels.h"
+#include "layout.h"
+#include "paged.h"
+
+namespace bgtq {
+namespace paged {
+
+struct WholeCache {  // not this: every query row sees rows [0, len) of a cache
+  static constexpr bool kPaged = false, kMods = false;
+};
+template <bool MODS>  // MODS: capped logits, a bias
+struct Mode : PagedPass {
+  static constexpr bool kPaged = true, kMods = MODS;
+};
+
+struct Unit {
+  int seq, block, r0, kvh, split;  // block: its number in the pass; r0: its first query row
+  Seq q;
+};
+
+// A sequence's blocks of R query rows in the pass.  (One whose numbers make no
+// sense has one in the pass of the smallest, which answers for it.)
+template <int R>
+__device__ __forceinline__ int blocks_of(const PagedPass& p, int group, const Seq& q) {
+  if (!q.ok) return p.lo == 0 && q.n > 0 ? 1 : 0;
+  const int rows = q.n * group;  // (below 2^31: the host checks)
+  return rows > p.lo && rows <= p.hi ? (rows + R - 1) / R : 0;
+}
+
+template <int R>
+__device__ __forceinline__ bool find_block(const PagedPass& p, int group, int block, Unit& u) {
+  u.block = block;
+  if (p.direct) {  // no sequence has more than one block
+    u.seq = block;
+    u.q = seq_of(p.b, block);
+    u.r0 = 0;
+    return blocks_of<R>(p, group, u.q) > 0;
+  }
+  int number;
+  u.seq = find_item(p.b, block, [&](const Seq& q) { return blocks_of<R>(p, group, q); }, number, u.q);
+  u.r0 = number * R;
+  return u.seq >= 0;
+}
+
+// Blocks vary fastest, from the last one down: a chunk's late blocks see the
+// most rows.  Then KV heads, then splits.
+template <int R>
+__device__ __forceinline__ bool unit_of(const PagedPass& p, const Dims& d, int item, Unit& u) {
+  const int block = p.n_blocks - 1 - item % p.n_blocks;
+  item /= p.n_blocks;
+  u.kvh = item % d.n_kv;
+  u.split = item / d.n_kv;
+  return find_block<R>(p, d.group, block, u);
+}
+
+// The rows of a sequence that a call cannot answer for are not numbers.
+__device__ __forceinline__ void refuse(const Unit& u, const Dims& d, int kvh, void* out, int out_dtype, int tid, int threads) {
+  const int per = d.group * kHeadDim;
+  const size_t stride = static_cast<size_t>(d.n_kv) * per;
+  for (long i = tid; i < static_cast<long>(u.q.n) * per; i += threads) {
+    const size_t at = (u.q.first + i / per) * stride + static_cast<size_t>(kvh) * per + i % per;
+    if (out_dtype == 1) static_cast<uint16_t*>(out)[at] = 0x7FC0;
+    else static_cast<float*>(out)[at] = __builtin_nanf("");
+  }
+}
+
+// What new token i of a sequence sees: rows [0, end(i)), end never falls.
+struct Sight {
+  int pos0, see;  // position of token 0; rows that all of them see
+  __device__ __forceinline__ int pos(int i) const { return pos0 + i; }
+  __device__ __forceinline__ int end(int i) const { return max(pos0 + i + 1, see); }
+};
+__device__ __forceinline__ Sight sight_of(const PagedPass& p, const Unit& u, int seq) {
+  return {u.q.len - u.q.n, p.m.prefix ? min(p.m.prefix[seq], u.q.len) : 0};
+}
+
+// Radii (fp16) of four tokens, zero from number `left` on.
+__device__ __forceinline__ uint2 seen(const uint2& r, int left) {
+  return make_uint2((left > 0 ? r.x & 0xFFFFu : 0u) | (left > 1 ? r.x & 0xFFFF0000u : 0u),
+                    (left > 2 ? r.y & 0xFFFFu : 0u) | (left > 3 ? r.y & 0xFFFF0000u : 0u));
+}
+
+// A base-2 logit x = log2 e q k / sqrt(d) after the cap, C tanh(x / C) with
+// C = cap log2 e, and the bias, -slope |distance|.  tanh(y) = (1 - t) / (1 + t),
+// t = 2^(-2 |y| log2 e); for fp32 outputs (EX) the Taylor sum below |y| = 0.36,
+// where 1 - t cancels (its first term left out is below 2^-25 of y there).
+// Without it C tanh is off by 2^-24 C for small logits: 4e-6 at a cap of 50,
+// nothing beside the rounding to bf16.
+template <bool EX>
+__device__ __forceinline__ float changed(float cap, float slope, float x, float distance) {
+  constexpr float kLog2 = 1.4426950408889634f;
+  if (cap > 0.f) {
+    const float c = cap * kLog2, y = x * (1.f / c), a = fabsf(y);
+    const float t = __builtin_amdgcn_exp2f(-2.f * kLog2 * a);
+    float h = (1.f - t) * __builtin_amdgcn_rcpf(1.f + t);
+    if constexpr (EX) {
+      const float z = a * a;
+      float s = fmaf(z, 21844.f / 6081075.f, -1382.f / 155925.f);
+      s = fmaf(z, s, 62.f / 2835.f);
+      s = fmaf(z, s, -17.f / 315.f);
+      s = fmaf(z, s, 2.f / 15.f);
+      s = fmaf(z, s, -1.f / 3.f);
+      h = a < 0.36f ? fmaf(a * z, s, a) : h;
+    }
+    x = copysignf(c * h, y);
+  }
+  return fmaf(-slope, fabsf(distance), x);
+}
+
+}  // namespace paged
+}  // namespace bgtq

@@ -27,8 +27,12 @@
 #include <hip/hip_fp16.h>
 #include <hip/hip_runtime.h>
 
+#include <algorithm>
+#include <type_traits>
+
 #include "kernels.h"
 #include "layout.h"
+#include "paged.h"
 
 namespace bgtq {
 namespace quant_detail {
@@ -56,6 +60,14 @@ struct LdsK {
   uint32_t pm[kHeadDim];                      // per stream position: bit offset | b << 10 | group << 14
   float gs[kMaxGroups];                       // sqrt(d_g)
   uint8_t gd[kHeadDim];                       // group ordinal of each input dim
+  int2 at[W][kSub];                           // pages: the page of each of a wave's rows (-1: none) and its place there
+};
+
+// Rows of the call at wpos of each sequence, n_new each.  (PagedRows: a ragged
+// batch's rows and the pages they go to.)
+struct FixedRows {
+  const int32_t* wpos;
+  int n_new;
 };
 template <int W>
 struct LdsV {
@@ -143,21 +155,80 @@ __device__ __forceinline__ float4_t mfma(float a, float b, float4_t c) {
   return __builtin_amdgcn_mfma_f32_16x16x4f32(a, b, c, 0, 0, 0);
 }
 
+// Page (-1: none) and place of input row r0 + tk of a ragged batch, r0 the same
+// in the wave, tk < 16.  The sequence of r0 by a search 64 sequences at a time,
+// the rows' own by one ballot each over the 64 sequences from there on.
+__device__ __forceinline__ int2 page_of_row(const PagedBatch& b, int n_pages, int page_rows, int r0, int tk) {
+  const int lane = threadIdx.x & 63, last = b.n_seqs - 1;
+  int s0 = last;
+  for (int base = 0; base < b.n_seqs; base += 64) {
+    const uint64_t past = __builtin_amdgcn_ballot_w64(base + lane <= last && b.cu[min(base + lane, last) + 1] > r0);
+    if (past != 0) {
+      s0 = base + __builtin_ctzll(past);
+      break;
+    }
+  }
+  const int end = s0 + lane <= last ? b.cu[min(s0 + lane, last) + 1] : 0x7FFFFFFF;
+  int s = s0;
+#pragma unroll
+  for (int j = 0; j < kSub; ++j) {
+    const int n = __builtin_popcountll(__builtin_amdgcn_ballot_w64(end <= r0 + j));
+    s = tk == j ? s0 + n : s;
+  }
+  s = min(s, last);
+  // (64 sequences behind s0 end before the row: empty ones among them)
+  while (s < last && b.cu[s + 1] <= r0 + tk) ++s;
+  const paged::Seq q = paged::seq_of(b, s);
+  const int i = r0 + tk - q.first;
+  if (!q.ok || i < 0 || i >= q.n) return make_int2(-1, 0);
+  const int t = q.len - q.n + i;
+  return make_int2(paged::page_of(b, n_pages, page_rows, s, t), t % page_rows);
+}
+
+// Value tile `want` of the new rows of a ragged batch: its page (-1: none), the
+// first row of that tile in the sequence, and the rows [lo, hi) that are new.
+struct PagedTile {
+  int page, P0, lo, hi;
+  size_t in0;  // input row of the sequence's row 0 (it may lie before the inputs)
+};
+__device__ __forceinline__ bool paged_tile(const PagedBatch& b, int n_pages, int page_rows, int want, PagedTile& t) {
+  int number;
+  paged::Seq q;
+  const int s = paged::find_item(
+      b, want, [](const paged::Seq& x) { return x.ok && x.n > 0 ? (x.len - 1) / kTile - (x.len - x.n) / kTile + 1 : 0; },
+      number, q);
+  if (s < 0) return false;
+  const int wp = q.len - q.n;
+  t.P0 = (wp / kTile + number) * kTile;
+  t.lo = max(t.P0, wp) - t.P0;
+  t.hi = min(t.P0 + kTile, q.len) - t.P0;
+  t.page = paged::page_of(b, n_pages, page_rows, s, t.P0);
+  t.in0 = static_cast<size_t>(static_cast<long>(q.first) - wp);
+  return t.page >= 0;
+}
+
 // ---------------------------------------------------------------- keys
 // Workgroup bx of the key part: rows [bx R, bx R + R) of the call, R =
 // W kSub iters.
-template <bool BF16, int W>
+template <bool BF16, int W, class ROWS>
 __device__ __forceinline__ void quant_keys(LdsK<W>& S, int bx, int iters, const Dims& d,
-                                           const uint8_t* __restrict__ blob, const void* __restrict__ kin, int n_new,
-                                           const int32_t* __restrict__ wpos, const CachePtrs& c) {
-  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+                                           const uint8_t* __restrict__ blob, const void* __restrict__ kin,
+                                           const ROWS& rows, const CachePtrs& c) {
+  constexpr bool kPaged = std::is_same_v<ROWS, PagedRows>;
+  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int head = blockIdx.y, lz = blockIdx.z;
   const int layer = d.layer >= 0 ? d.layer : lz / d.batch;
-  const int seq = lz % d.batch;
   const int cap = d.capacity;
-  const int wp = wpos[seq];
-  if (wp < 0 || wp >= cap) return;
-  const int n_fit = min(n_new, cap - wp);  // rows that fit (the host rejects overflow)
+  int wp = 0, n_fit;  // (pages: every input row is one of the call's rows, those of no sequence are passed over)
+  size_t row = 0;
+  if constexpr (kPaged) {
+    n_fit = rows.b.n_tokens;
+  } else {
+    wp = rows.wpos[lz % d.batch];
+    if (wp < 0 || wp >= cap) return;
+    n_fit = min(rows.n_new, cap - wp);  // rows that fit (the host rejects overflow)
+    row = (static_cast<size_t>(layer) * d.batch + lz % d.batch) * d.n_kv + head;
+  }
   constexpr int kThreads = W * 64;
   const int r_wg = bx * W * kSub * iters;
   if (r_wg >= n_fit) return;
@@ -196,14 +267,24 @@ __device__ __forceinline__ void quant_keys(LdsK<W>& S, int bx, int iters, const 
 
   const int tk = lane & 15, kk = lane >> 4;
   const int kw = d.k_words, nslot = (ng + 1) & ~1;
-  const size_t row = (static_cast<size_t>(layer) * d.batch + seq) * d.n_kv + head;
   for (int it = 0; it < iters; ++it) {
     const int r0 = r_wg + (it * W + wave) * kSub;
     if (r0 >= n_fit) break;  // wave-uniform
     const int r = r0 + tk;
-    const bool valid = r < n_fit;
+    bool valid = r < n_fit;
+    size_t row_r = row;  // the cache row (layer, sequence or page, head) of row r, and r's place there
+    int t_r = wp + r;
     float x[32];
-    load_slice<BF16>(kin, ((static_cast<size_t>(lz) * n_new + r) * d.n_kv + head) * kHeadDim + 32 * kk, valid, x);
+    if constexpr (kPaged) {
+      load_slice<BF16>(kin, min(r, n_fit - 1) * rows.k_stride + head * kHeadDim + 32 * kk, valid, x);
+      const int2 at = page_of_row(rows.b, d.batch, cap, r0, tk);
+      valid = valid && at.x >= 0;
+      row_r = (static_cast<size_t>(layer) * d.batch + max(at.x, 0)) * d.n_kv + head;
+      t_r = at.y;
+      S.at[wave][tk] = make_int2(valid ? at.x : -1, at.y);  // (the same from the row's four lanes)
+    } else {
+      load_slice<BF16>(kin, ((static_cast<size_t>(lz) * rows.n_new + r) * d.n_kv + head) * kHeadDim + 32 * kk, valid, x);
+    }
 
     // group radii: R2[g][row] = sum_d [group(d) = g] x[row][d]^2
     float4_t n2 = {0.f, 0.f, 0.f, 0.f};
@@ -240,7 +321,7 @@ __device__ __forceinline__ void quant_keys(LdsK<W>& S, int bx, int iters, const 
         const float nrm = sqrtf(n2[i]);
         S.sc[wave][tk][g] = nrm > 0.f ? S.gs[g] / nrm : 0.f;
         if (valid)
-          c.k_norms[row * kMaxGroups * cap + static_cast<size_t>(wp + r) * nslot + g] =
+          c.k_norms[row_r * kMaxGroups * cap + static_cast<size_t>(t_r) * nslot + g] =
               __half_as_ushort(__float2half_rn(nrm));
       }
     }
@@ -268,7 +349,14 @@ __device__ __forceinline__ void quant_keys(LdsK<W>& S, int bx, int iters, const 
     wave_sync();
     for (int idx = lane; idx < kSub * kw; idx += 64) {
       const int t2 = idx / kw, w = idx - t2 * kw;
-      if (r0 + t2 < n_fit) c.k_codes[(row * cap + wp + r0 + t2) * kw + w] = S.rw[wave][t2][w];
+      if constexpr (kPaged) {
+        const int2 at = S.at[wave][t2];
+        if (at.x >= 0)
+          c.k_codes[(((static_cast<size_t>(layer) * d.batch + at.x) * d.n_kv + head) * cap + at.y) * kw + w] =
+              S.rw[wave][t2][w];
+      } else {
+        if (r0 + t2 < n_fit) c.k_codes[(row * cap + wp + r0 + t2) * kw + w] = S.rw[wave][t2][w];
+      }
       S.rw[wave][t2][w] = 0u;
     }
     wave_sync();
@@ -276,26 +364,38 @@ __device__ __forceinline__ void quant_keys(LdsK<W>& S, int bx, int iters, const 
 }
 
 // ---------------------------------------------------------------- values
+// Where a head's value row starts among the inputs.
+__device__ __forceinline__ size_t value_row(const Dims& d, const FixedRows&, size_t r, int head) {
+  return (r * d.n_kv + head) * kHeadDim;
+}
+__device__ __forceinline__ size_t value_row(const Dims&, const PagedRows& rows, size_t r, int head) {
+  return r * rows.v_stride + head * kHeadDim;
+}
+
 // Workgroup bx of the value part: value tiles [bx T, bx T + T) of the rows
 // the call touches, T = W iters.  A wave owns whole 32-row value tiles;
 // the words of a tile partly outside [write_pos, write_pos + n_new) keep the
 // bits of the other rows.
-template <bool BF16, int W>
+template <bool BF16, int W, class ROWS>
 __device__ __forceinline__ void quant_values(LdsV<W>& S, int bx, int iters, const Dims& d,
                                              const uint8_t* __restrict__ blob, const void* __restrict__ vin,
-                                             int n_new, const int32_t* __restrict__ wpos, const CachePtrs& c) {
-  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+                                             const ROWS& rows, const CachePtrs& c) {
+  constexpr bool kPaged = std::is_same_v<ROWS, PagedRows>;
+  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int head = blockIdx.y, lz = blockIdx.z;
   const int layer = d.layer >= 0 ? d.layer : lz / d.batch;
-  const int seq = lz % d.batch;
   const int cap = d.capacity, bv = d.v_bits;
-  const int wp = wpos[seq];
-  if (wp < 0 || wp >= cap) return;
-  const int n_fit = min(n_new, cap - wp);
-  const int tile0 = wp / kTile, n_tiles = (wp + n_fit - 1) / kTile - tile0 + 1;
   constexpr int kThreads = W * 64;
   const int tw0 = bx * W * iters;
-  if (tw0 >= n_tiles) return;
+  int wp = 0, n_fit = 0, tile0 = 0, n_tiles = 0;
+  if constexpr (!kPaged) {
+    wp = rows.wpos[lz % d.batch];
+    if (wp < 0 || wp >= cap) return;
+    n_fit = min(rows.n_new, cap - wp);
+    tile0 = wp / kTile;
+    n_tiles = (wp + n_fit - 1) / kTile - tile0 + 1;
+    if (tw0 >= n_tiles) return;
+  }
   const int n_rows_blob = d.n_layers * d.n_kv;
   const float4* rsrc = reinterpret_cast<const float4*>(blob + layout_rotv_mfma_offset(n_rows_blob));
   const float* gthr = reinterpret_cast<const float*>(blob + kOffThr);
@@ -306,12 +406,29 @@ __device__ __forceinline__ void quant_values(LdsV<W>& S, int bx, int iters, cons
   const int tk = lane & 15, kk = lane >> 4;
   const float* thr = S.thr + thr_index(bv);
   const float sq = sqrtf(static_cast<float>(kHeadDim));
-  const size_t row = (static_cast<size_t>(layer) * d.batch + seq) * d.n_kv + head;
   for (int it = 0; it < iters; ++it) {
     const int tw = tw0 + it * W + wave;
-    if (tw >= n_tiles) break;  // wave-uniform
-    const int tile = tile0 + tw, P0 = tile * kTile;
-    const int s_lo = max(P0, wp) - P0, s_hi = min(P0 + kTile, wp + n_fit) - P0;  // rows [s_lo, s_hi) are new
+    // the tile's cache row, number there, and place in its sequence: rows [s_lo, s_hi) are new
+    size_t row, in_at;  // in_at: input row of slot 0
+    int tile, P0, s_lo, s_hi;
+    if constexpr (kPaged) {
+      PagedTile t;
+      if (!paged_tile(rows.b, d.batch, cap, tw, t)) continue;  // wave-uniform
+      row = (static_cast<size_t>(layer) * d.batch + t.page) * d.n_kv + head;
+      tile = t.P0 % cap / kTile;
+      P0 = t.P0 % cap;
+      s_lo = t.lo;
+      s_hi = t.hi;
+      in_at = t.in0 + t.P0;
+    } else {
+      if (tw >= n_tiles) break;  // wave-uniform
+      row = (static_cast<size_t>(layer) * d.batch + lz % d.batch) * d.n_kv + head;
+      tile = tile0 + tw;
+      P0 = tile * kTile;
+      s_lo = max(P0, wp) - P0;
+      s_hi = min(P0 + kTile, wp + n_fit) - P0;
+      in_at = static_cast<size_t>(lz) * rows.n_new + P0 - wp;
+    }
     uint32_t* gv = c.v_codes + (row * (cap / kTile) + tile) * kHeadDim * static_cast<size_t>(bv);
     const bool full = s_lo == 0 && s_hi == kTile;
     // tile words: zero, or the old words with the new rows' bits cleared
@@ -330,9 +447,7 @@ __device__ __forceinline__ void quant_values(LdsV<W>& S, int bx, int iters, cons
       const int slot = 16 * h + tk;
       const bool valid = slot >= s_lo && slot < s_hi;
       float x[32];
-      load_slice<BF16>(vin, ((static_cast<size_t>(lz) * n_new + (P0 + slot - wp)) * d.n_kv + head) * kHeadDim +
-                                32 * kk,
-                       valid, x);
+      load_slice<BF16>(vin, value_row(d, rows, in_at + slot, head) + 32 * kk, valid, x);
       float ss = 0.f;
 #pragma unroll
       for (int i = 0; i < 32; ++i) ss = fmaf(x[i], x[i], ss);
@@ -390,33 +505,49 @@ __device__ __forceinline__ void quant_values(LdsV<W>& S, int bx, int iters, cons
 // Short calls: workgroup bx encodes value tiles 2 bx and 2 bx + 1 of the
 // rows the call touches; waves 2 u and 2 u + 1 take rows 0-15 and 16-31 of
 // tile 2 bx + u and assemble its words together in LDS.
-template <bool BF16>
+template <bool BF16, class ROWS>
 __device__ __forceinline__ void quant_values_short(LdsVS& S, int bx, const Dims& d, const uint8_t* __restrict__ blob,
-                                                   const void* __restrict__ vin, int n_new,
-                                                   const int32_t* __restrict__ wpos, const CachePtrs& c) {
+                                                   const void* __restrict__ vin, const ROWS& rows, const CachePtrs& c) {
+  constexpr bool kPaged = std::is_same_v<ROWS, PagedRows>;
   constexpr int W = kWavesShort, kThreads = W * 64;
-  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int head = blockIdx.y, lz = blockIdx.z;
   const int layer = d.layer >= 0 ? d.layer : lz / d.batch;
-  const int seq = lz % d.batch;
   const int cap = d.capacity, bv = d.v_bits;
-  const int wp = wpos[seq];
-  if (wp < 0 || wp >= cap) return;  // (uniform over the workgroup: before any barrier)
-  const int n_fit = min(n_new, cap - wp);
-  const int tile0 = wp / kTile, n_tiles = (wp + n_fit - 1) / kTile - tile0 + 1;
+  const int u = wave >> 1, h = wave & 1;  // the wave's tile of the workgroup and its half
   const int tw0 = bx * (W / 2);
-  if (tw0 >= n_tiles) return;
+  bool active;  // the same for both waves of a tile
+  size_t row, in_at;  // in_at: input row of slot 0
+  int tile, P0, s_lo, s_hi;  // rows [s_lo, s_hi) are new
+  if constexpr (kPaged) {
+    PagedTile t = {0, 0, 0, 0, 0};
+    active = paged_tile(rows.b, d.batch, cap, tw0 + u, t);
+    row = (static_cast<size_t>(layer) * d.batch + max(t.page, 0)) * d.n_kv + head;
+    tile = t.P0 % cap / kTile;
+    P0 = t.P0 % cap;
+    s_lo = t.lo;
+    s_hi = t.hi;
+    in_at = t.in0 + t.P0;
+  } else {
+    const int wp = rows.wpos[lz % d.batch];
+    if (wp < 0 || wp >= cap) return;  // (uniform over the workgroup: before any barrier)
+    const int n_fit = min(rows.n_new, cap - wp);
+    const int tile0 = wp / kTile, n_tiles = (wp + n_fit - 1) / kTile - tile0 + 1;
+    if (tw0 >= n_tiles) return;
+    tile = tile0 + tw0 + u;
+    P0 = tile * kTile;
+    active = tw0 + u < n_tiles;
+    s_lo = max(P0, wp) - P0;
+    s_hi = min(P0 + kTile, wp + n_fit) - P0;
+    row = (static_cast<size_t>(layer) * d.batch + lz % d.batch) * d.n_kv + head;
+    in_at = static_cast<size_t>(lz) * rows.n_new + P0 - wp;
+  }
   const int n_rows_blob = d.n_layers * d.n_kv;
   const float4* rsrc = reinterpret_cast<const float4*>(blob + layout_rotv_mfma_offset(n_rows_blob));
   const float* gthr = reinterpret_cast<const float*>(blob + kOffThr);
   stage_matrix<W>(S.rb, rsrc, tid);
   for (int i = tid; i < kThresholdEntries; i += kThreads) S.thr[i] = gthr[i];
 
-  const int u = wave >> 1, h = wave & 1;  // the wave's tile of the workgroup and its half
-  const int tile = tile0 + tw0 + u, P0 = tile * kTile;
-  const bool active = tw0 + u < n_tiles;  // the same for both waves of a tile
-  const int s_lo = max(P0, wp) - P0, s_hi = min(P0 + kTile, wp + n_fit) - P0;  // rows [s_lo, s_hi) are new
-  const size_t row = (static_cast<size_t>(layer) * d.batch + seq) * d.n_kv + head;
   uint32_t* gv = c.v_codes + (row * (cap / kTile) + tile) * kHeadDim * static_cast<size_t>(bv);
   if (active) {
     // tile words: zero, or the old words with the new rows' bits cleared
@@ -440,8 +571,7 @@ __device__ __forceinline__ void quant_values_short(LdsVS& S, int bx, const Dims&
     const int slot = 16 * h + tk;
     const bool valid = slot >= s_lo && slot < s_hi;
     float x[32];
-    load_slice<BF16>(vin, ((static_cast<size_t>(lz) * n_new + (P0 + slot - wp)) * d.n_kv + head) * kHeadDim + 32 * kk,
-                     valid, x);
+    load_slice<BF16>(vin, value_row(d, rows, in_at + slot, head) + 32 * kk, valid, x);
     float ss = 0.f;
 #pragma unroll
     for (int i = 0; i < 32; ++i) ss = fmaf(x[i], x[i], ss);
@@ -499,11 +629,11 @@ __device__ __forceinline__ void quant_values_short(LdsVS& S, int bx, const Dims&
 // the call).  16-wave workgroups: [0, n_kwg) encode keys, the rest values.
 // 4-wave workgroups (short calls, two per CU): the value workgroups come
 // first, so that the key workgroups fill in behind.
-template <bool BF16, int W>
+template <bool BF16, int W, class ROWS>
 __global__ __launch_bounds__(W * 64) void k_quant_rows(Dims d, const uint8_t* __restrict__ blob,
                                                         const void* __restrict__ kin, const void* __restrict__ vin,
-                                                        int n_new, const int32_t* __restrict__ wpos, CachePtrs c,
-                                                        int n_kwg, int n_vwg, int k_iters, int v_iters) {
+                                                        ROWS rows, CachePtrs c, int n_kwg, int n_vwg, int k_iters,
+                                                        int v_iters) {
   constexpr size_t kVBytes = W == kWavesLong ? sizeof(LdsV<W>) : sizeof(LdsVS);
   constexpr size_t kBytes = sizeof(LdsK<W>) > kVBytes ? sizeof(LdsK<W>) : kVBytes;
   __shared__ __attribute__((aligned(16))) uint8_t smem[kBytes];
@@ -511,44 +641,58 @@ __global__ __launch_bounds__(W * 64) void k_quant_rows(Dims d, const uint8_t* __
   const bool keys = W == kWavesLong ? bx < n_kwg : bx >= n_vwg;
   if (keys)
     quant_keys<BF16, W>(*reinterpret_cast<LdsK<W>*>(smem), W == kWavesLong ? bx : bx - n_vwg, k_iters, d, blob, kin,
-                        n_new, wpos, c);
+                        rows, c);
   else if constexpr (W == kWavesLong)
-    quant_values<BF16, W>(*reinterpret_cast<LdsV<W>*>(smem), bx - n_kwg, v_iters, d, blob, vin, n_new, wpos, c);
+    quant_values<BF16, W>(*reinterpret_cast<LdsV<W>*>(smem), bx - n_kwg, v_iters, d, blob, vin, rows, c);
   else
-    quant_values_short<BF16>(*reinterpret_cast<LdsVS*>(smem), bx, d, blob, vin, n_new, wpos, c);
+    quant_values_short<BF16>(*reinterpret_cast<LdsVS*>(smem), bx, d, blob, vin, rows, c);
 }
 
 }  // namespace quant_detail
 
-hipError_t launch_quantize_prefill(const Dims& d, const void* layout, const void* k, const void* v, int n_new,
-                                   const int32_t* write_pos, const CachePtrs& c, hipStream_t s) {
+// n: rows of a sequence (of the batch, where they go to pages), z: sequences
+// times layers; tiles: value tiles at most.
+template <class ROWS>
+static hipError_t launch_rows(const Dims& d, const void* layout, const void* k, const void* v, const ROWS& rows, int n, int z,
+                              long tiles, const CachePtrs& c, hipStream_t s) {
   using namespace quant_detail;
   const uint8_t* blob = static_cast<const uint8_t*>(layout);
-  const int lz = d.batch * d.n_lc;
   // rows per workgroup: small calls spread over more workgroups (one
   // sub-tile or value tile per wave, 4-wave workgroups up to 64K rows), large
   // ones amortise the 64 KB matrix staged in LDS over more rows
-  const long rows = static_cast<long>(n_new) * d.n_kv * lz;
-  const int k_iters = rows <= 256L * 256 ? 1 : (rows <= 4L * 256 * 512 ? 2 : 4);
-  const int v_iters = rows <= 256L * 512 ? 1 : 2;
+  const long all = static_cast<long>(n) * d.n_kv * z;
+  const int k_iters = all <= 256L * 256 ? 1 : (all <= 4L * 256 * 512 ? 2 : 4);
+  const int v_iters = all <= 256L * 512 ? 1 : 2;
   const auto go = [&](auto kern, int w) {
-    const int n_kwg = (n_new + w * kSub * k_iters - 1) / (w * kSub * k_iters);
+    const int n_kwg = (n + w * kSub * k_iters - 1) / (w * kSub * k_iters);
     // value tiles per workgroup: w v_iters (a wave per tile), or 2 (short calls)
     const int vt_wg = w == kWavesLong ? w * v_iters : kWavesShort / 2;
-    const int n_vwg = (n_new / kTile + 2 + vt_wg - 1) / vt_wg;
-    const dim3 grid(n_kwg + n_vwg, d.n_kv, lz);
-    hipLaunchKernelGGL(kern, grid, dim3(w * 64), 0, s, d, blob, k, v, n_new, write_pos, c, n_kwg, n_vwg, k_iters,
-                       v_iters);
+    const int n_vwg = static_cast<int>((tiles + vt_wg - 1) / vt_wg);
+    const dim3 grid(n_kwg + n_vwg, d.n_kv, z);
+    hipLaunchKernelGGL(kern, grid, dim3(w * 64), 0, s, d, blob, k, v, rows, c, n_kwg, n_vwg, k_iters, v_iters);
   };
-  const bool bf = d.in_dtype == 1, short_call = rows <= 256L * 256;
+  const bool bf = d.in_dtype == 1, short_call = all <= 256L * 256;
   if (short_call) {
-    if (bf) go(k_quant_rows<true, kWavesShort>, kWavesShort);
-    else go(k_quant_rows<false, kWavesShort>, kWavesShort);
+    if (bf) go(k_quant_rows<true, kWavesShort, ROWS>, kWavesShort);
+    else go(k_quant_rows<false, kWavesShort, ROWS>, kWavesShort);
   } else {
-    if (bf) go(k_quant_rows<true, kWavesLong>, kWavesLong);
-    else go(k_quant_rows<false, kWavesLong>, kWavesLong);
+    if (bf) go(k_quant_rows<true, kWavesLong, ROWS>, kWavesLong);
+    else go(k_quant_rows<false, kWavesLong, ROWS>, kWavesLong);
   }
   return hipGetLastError();
+}
+
+hipError_t launch_quantize_prefill(const Dims& d, const void* layout, const void* k, const void* v, int n_new,
+                                   const int32_t* write_pos, const CachePtrs& c, hipStream_t s) {
+  return launch_rows(d, layout, k, v, quant_detail::FixedRows{write_pos, n_new}, n_new, d.batch * d.n_lc,
+                     n_new / kTile + 2, c, s);
+}
+
+hipError_t launch_paged_quantize(const Dims& d, const void* layout, const void* k, const void* v, const PagedRows& rows,
+                                 const CachePtrs& c, hipStream_t s) {
+  // n rows touch at most (n + 62) / 32 tiles, one each at most
+  const long n = rows.b.n_tokens, tiles = std::min(n, (n + 62L * rows.b.n_seqs) / kTile);
+  return launch_rows(d, layout, k, v, rows, rows.b.n_tokens, 1, tiles, c, s);
 }
 
 }  // namespace bgtq
