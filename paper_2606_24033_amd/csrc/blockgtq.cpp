@@ -1212,7 +1212,7 @@ struct PagedPlan {
   size_t part_bytes;
 };
 struct PagedPlans {
-  PagedPlan few, many;  // sequences of up to 32 query rows (a token or a few), and of more
+  PagedPlan few, many;  // sequences of a single token, and of more
   size_t bytes;
 };
 
@@ -1231,11 +1231,12 @@ static PagedPlan paged_pass_plan(const Dims& d, std::initializer_list<int> width
     const bool direct = max_rows <= rows;
     const double est = d.n_kv * (direct || seqs == 1 ? static_cast<double>(blocks) : (n_rows + 0.5 * seqs * rows) / rows);
     const int k0 = requested > 0 ? std::min(requested, tiles) : 1;
-    const int k1 = requested > 0 ? k0 : std::min(rows == 32 ? (tiles + 7) / 8 : tiles, 256);
+    const int k1 = requested > 0 ? k0 : std::min(rows <= 32 ? (tiles + 7) / 8 : tiles, 256);
     for (int k = k0; k <= std::max(k0, k1); ++k) {
       const int len = (tiles + k - 1) / k, n = (tiles + len - 1) / len;
       const double busy = 1.0 + 0.3 * std::min(1.0, est * n / 256.0);
-      const double wg = rows == 32 ? 13.0 + (d.k_words <= 8 ? 5.4 : d.k_words <= 16 ? 6.2 : 13.0) * ((len + 7) / 8)
+      const int waves = d.group <= 4 && d.k_words <= 16 ? 16 : 12;  // (8 rows)
+      const double wg = rows == 8 ? 10.0 + (d.k_words <= 16 ? 4.5 : 7.0) * ((len + waves - 1) / waves) : rows == 32 ? 13.0 + (d.k_words <= 8 ? 5.4 : d.k_words <= 16 ? 6.2 : 13.0) * ((len + 7) / 8)
                                    : 15.0 + (rows == 128 ? 1.8 : 2.75) * busy * len;
       double t = std::ceil(est * n / 256.0) * wg;
       // unequal workgroups follow one another without rounds
@@ -1257,16 +1258,23 @@ static PagedPlans paged_plans(const bgtq_config* cfg, int n_seqs, int n_tokens, 
   const Dims d = dims_of(cfg, 0);
   const long rows = static_cast<long>(n_tokens) * d.group, max_rows = static_cast<long>(max_new) * d.group;
   const int all = 0x7FFFFFFF;
-  if (max_rows <= 32) {
-    p.few = paged_pass_plan(d, {32}, n_seqs, rows, max_rows, max_ctx, 1.0, 0, all, n_splits);
+  if (max_new == 1) {
+    p.few = paged_pass_plan(d, {8}, n_seqs, rows, max_rows, max_ctx, 1.0, 0, all, n_splits);
   } else {
-    // sequences beside the longest that have a token or a few each, on average:
-    // a pass of their own, with splits of their own
-    const bool both = n_seqs > 1 && (rows - max_rows) <= 32l * (n_seqs - 1);
-    if (both) p.few = paged_pass_plan(d, {32}, n_seqs, std::min(rows, 32l * n_seqs), 32, max_ctx, 1.0, 0, 32, n_splits);
+    // sequences beside the longest that have a token or two each, on average:
+    // single tokens in a pass of their own, with splits of their own
+    const bool both = n_seqs > 1 && n_tokens - max_new <= 2l * (n_seqs - 1);
+    const int lo = both ? d.group : 0;
+    if (both)
+      p.few = paged_pass_plan(d, {8}, n_seqs, std::min(rows, static_cast<long>(d.group) * n_seqs), d.group, max_ctx, 1.0, 0,
+                              d.group, n_splits);
     const double seen = 1.0 - 0.5 * max_new / std::max(max_ctx, 1);
-    if (max_rows > 64) p.many = paged_pass_plan(d, {32, 128, 256}, n_seqs, rows, max_rows, max_ctx, seen, both ? 32 : 0, all, n_splits);
-    else p.many = paged_pass_plan(d, {32, 128}, n_seqs, rows, max_rows, max_ctx, seen, both ? 32 : 0, all, n_splits);
+    const auto many = [&](std::initializer_list<int> widths) {
+      p.many = paged_pass_plan(d, widths, n_seqs, rows, max_rows, max_ctx, seen, lo, all, n_splits);
+    };
+    if (max_rows <= 32) many({32});
+    else if (max_rows <= 64) many({32, 128});
+    else many({32, 128, 256});
   }
   p.bytes = 256 + p.few.part_bytes + p.many.part_bytes + (p.many.rows > 32 ? al256(static_cast<size_t>(rows) * d.n_kv * kHeadDim * 4) : 0);
   return p;

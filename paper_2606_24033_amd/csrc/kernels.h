@@ -170,13 +170,16 @@ struct PagedPass {
   int n_blocks, lo, hi, unit_rows;
   bool direct;  // block = sequence
 };
-// Passes of 32-row workgroups (call.rows0) or of 128 or 256 on the rotated query rows call.qr, and
-// their join where there are splits (paged.hip).
+// A pass and the join of its splits (paged.hip), by the query rows of a workgroup (call.rows0): 8, of
+// single tokens (paged_decode.h); 32 (cross_impl.h); 128 or 256, on the rotated query rows call.qr
+// (cross_tile.h).
 hipError_t launch_paged_pass(const Dims& d, const void* layout, const void* q, const CrossCall& call, const PagedPass& pass,
                              hipStream_t s);
 #define BGTQ_DECL_PAGED(N)                                                                                          \
   hipError_t launch_paged_bv##N(const Dims& d, const void* layout, const void* q, const CrossCall& call,            \
-                                const PagedPass& pass, hipStream_t s);
+                                const PagedPass& pass, hipStream_t s);                                              \
+  hipError_t launch_paged_decode_bv##N(const Dims& d, const void* layout, const void* q, const CrossCall& call,     \
+                                       const PagedPass& pass, hipStream_t s);
 BGTQ_DECL_PAGED(1)
 BGTQ_DECL_PAGED(2)
 BGTQ_DECL_PAGED(3)

@@ -51,6 +51,17 @@ hipError_t launch_paged_pass(const Dims& d, const void* layout, const void* q, c
   hipError_t e;
   if (call.rows0 > 32) {
     e = call.out_dtype == 1 ? launch_paged_tile_bf16(d, layout, call, pass, s) : launch_paged_tile_fp32(d, layout, call, pass, s);
+  } else if (call.rows0 == 8) {
+    switch (d.v_bits) {
+      case 1: e = launch_paged_decode_bv1(d, layout, q, call, pass, s); break;
+      case 2: e = launch_paged_decode_bv2(d, layout, q, call, pass, s); break;
+      case 3: e = launch_paged_decode_bv3(d, layout, q, call, pass, s); break;
+      case 4: e = launch_paged_decode_bv4(d, layout, q, call, pass, s); break;
+      case 5: e = launch_paged_decode_bv5(d, layout, q, call, pass, s); break;
+      case 6: e = launch_paged_decode_bv6(d, layout, q, call, pass, s); break;
+      case 7: e = launch_paged_decode_bv7(d, layout, q, call, pass, s); break;
+      default: e = launch_paged_decode_bv8(d, layout, q, call, pass, s); break;
+    }
   } else {
     switch (d.v_bits) {
       case 1: e = launch_paged_bv1(d, layout, q, call, pass, s); break;
@@ -64,6 +75,7 @@ hipError_t launch_paged_pass(const Dims& d, const void* layout, const void* q, c
     }
   }
   if (e != hipSuccess || call.n_slots == 1) return e;
+  if (call.rows0 == 8) return join<8>(d, layout, call, pass, s);
   return call.rows0 == 32 ? join<32>(d, layout, call, pass, s)
                           : call.rows0 == 128 ? join<128>(d, layout, call, pass, s) : join<256>(d, layout, call, pass, s);
 }

@@ -1,0 +1,9 @@
+// Single tokens over pages, instantiation for value code width 7 (see paged_decode.h).
+#include "paged_decode.h"
+
+namespace bgtq {
+hipError_t launch_paged_decode_bv7(const Dims& d, const void* layout, const void* q, const CrossCall& call,
+                                   const PagedPass& pass, hipStream_t s) {
+  return paged_decode_detail::launch_bv<7>(d, layout, q, call, pass, s);
+}
+}  // namespace bgtq
