@@ -1219,8 +1219,9 @@ struct PagedPlans {
 // Rows of the workgroups and splits of a pass, by the estimates of cross_plan.
 // The host knows bounds only: `blocks` workgroups' rows at most, lengths of
 // max_len at most; a chunk's early rows see fewer (seen: the mean share).
-static PagedPlan paged_pass_plan(const Dims& d, std::initializer_list<int> widths, long n_seqs, long n_rows, long max_rows,
-                                 int max_len, double seen, int lo, int hi, int requested) {
+// likely: sequences that the pass has rows of, for the estimate.
+static PagedPlan paged_pass_plan(const Dims& d, std::initializer_list<int> widths, long n_seqs, double likely, long n_rows,
+                                 long max_rows, int max_len, double seen, int lo, int hi, int requested) {
   PagedPlan best = {};
   double t_best = 0.0;
   const int tiles = std::max(1, (max_len + 63) / 64);
@@ -1229,7 +1230,7 @@ static PagedPlan paged_pass_plan(const Dims& d, std::initializer_list<int> width
     const long seqs = std::min(n_seqs, n_rows / (lo + 1));
     const long blocks = max_rows <= rows ? n_seqs : std::min(seqs * ((max_rows + rows - 1) / rows), (n_rows + seqs * (rows - 1)) / rows);
     const bool direct = max_rows <= rows;
-    const double est = d.n_kv * (direct || seqs == 1 ? static_cast<double>(blocks) : (n_rows + 0.5 * seqs * rows) / rows);
+    const double est = d.n_kv * (direct || seqs == 1 ? static_cast<double>(blocks) : n_rows / rows + 0.5 * likely);
     const int k0 = requested > 0 ? std::min(requested, tiles) : 1;
     const int k1 = requested > 0 ? k0 : std::min(rows <= 32 ? (tiles + 7) / 8 : tiles, 256);
     for (int k = k0; k <= std::max(k0, k1); ++k) {
@@ -1259,18 +1260,20 @@ static PagedPlans paged_plans(const bgtq_config* cfg, int n_seqs, int n_tokens, 
   const long rows = static_cast<long>(n_tokens) * d.group, max_rows = static_cast<long>(max_new) * d.group;
   const int all = 0x7FFFFFFF;
   if (max_new == 1) {
-    p.few = paged_pass_plan(d, {8}, n_seqs, rows, max_rows, max_ctx, 1.0, 0, all, n_splits);
+    p.few = paged_pass_plan(d, {8}, n_seqs, n_seqs, rows, max_rows, max_ctx, 1.0, 0, all, n_splits);
   } else {
     // sequences beside the longest that have a token or two each, on average:
     // single tokens in a pass of their own, with splits of their own
     const bool both = n_seqs > 1 && n_tokens - max_new <= 2l * (n_seqs - 1);
     const int lo = both ? d.group : 0;
     if (both)
-      p.few = paged_pass_plan(d, {8}, n_seqs, std::min(rows, static_cast<long>(d.group) * n_seqs), d.group, max_ctx, 1.0, 0,
-                              d.group, n_splits);
+      p.few = paged_pass_plan(d, {8}, n_seqs, n_seqs, std::min(rows, static_cast<long>(d.group) * n_seqs), d.group, max_ctx,
+                              1.0, 0, d.group, n_splits);
+    // (as few sequences as the rest of the tokens can be)
+    const double likely = both ? std::max(1.0, (n_tokens - n_seqs) / (max_new - 1.0)) : n_seqs;
     const double seen = 1.0 - 0.5 * max_new / std::max(max_ctx, 1);
     const auto many = [&](std::initializer_list<int> widths) {
-      p.many = paged_pass_plan(d, widths, n_seqs, rows, max_rows, max_ctx, seen, lo, all, n_splits);
+      p.many = paged_pass_plan(d, widths, n_seqs, likely, rows, max_rows, max_ctx, seen, lo, all, n_splits);
     };
     if (max_rows <= 32) many({32});
     else if (max_rows <= 64) many({32, 128});
@@ -1327,9 +1330,7 @@ int blockgtq_paged_attn(const bgtq_config* cfg, const void* d_layout, int32_t la
     call.out = d_out;
     call.out_dtype = out_dtype;
     if (pl->rows > 32) {
-      Dims dq = d;  // (the chunk's tokens are one sequence's query rows)
-      dq.batch = 1;
-      hipError_t e = launch_query_rotation(dq, d_layout, d_q, chunk->n_tokens, call.qr, s);
+      hipError_t e = launch_paged_rotation(d, d_layout, d_q, chunk->n_tokens, call.qr, s);
       if (e != hipSuccess) return hip_fail(e, "paged_attn rotation launch");
     }
     const PagedPass pass = {paged_batch(chunk), mods, static_cast<int>(pl->blocks), pl->lo, pl->hi, pl->unit_rows, pl->direct};

@@ -46,6 +46,10 @@ struct PagedRows {
 };
 hipError_t launch_paged_append(const Dims& d, const void* layout, const void* k, const void* v, const PagedRows& rows,
                                const CachePtrs& c, hipStream_t s);
+// bf16 rows of the ordinary widths (paged_quantize.hip).
+bool paged_quantize_fits(const Dims& d);
+hipError_t launch_paged_quantize_bf16(const Dims& d, const void* layout, const void* k, const void* v, const PagedRows& rows,
+                                      const CachePtrs& c, hipStream_t s);
 hipError_t launch_paged_quantize(const Dims& d, const void* layout, const void* k, const void* v, const PagedRows& rows,
                                  const CachePtrs& c, hipStream_t s);
 
@@ -173,6 +177,7 @@ struct PagedPass {
 // A pass and the join of its splits (paged.hip), by the query rows of a workgroup (call.rows0): 8, of
 // single tokens (paged_decode.h); 32 (cross_impl.h); 128 or 256, on the rotated query rows call.qr
 // (cross_tile.h).
+hipError_t launch_paged_rotation(const Dims& d, const void* layout, const void* q, int n_tokens, float* qr, hipStream_t s);
 hipError_t launch_paged_pass(const Dims& d, const void* layout, const void* q, const CrossCall& call, const PagedPass& pass,
                              hipStream_t s);
 #define BGTQ_DECL_PAGED(N)                                                                                          \

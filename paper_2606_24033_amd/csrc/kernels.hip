@@ -310,7 +310,9 @@ hipError_t launch_quantize_append(const Dims& d, const void* layout, const void*
 
 hipError_t launch_paged_append(const Dims& d, const void* layout, const void* k, const void* v, const PagedRows& rows,
                                const CachePtrs& c, hipStream_t s) {
-  if (rows.b.max_new > kRowAppend) return launch_paged_quantize(d, layout, k, v, rows, c, s);
+  if (rows.b.max_new > kRowAppend)
+    return paged_quantize_fits(d) ? launch_paged_quantize_bf16(d, layout, k, v, rows, c, s)
+                                  : launch_paged_quantize(d, layout, k, v, rows, c, s);
   const auto kern = d.in_dtype == 1 ? k_append_rows<true, PagedRows> : k_append_rows<false, PagedRows>;
   hipLaunchKernelGGL(kern, dim3(d.n_kv, rows.b.n_seqs), dim3(1024), 0, s, d, static_cast<const uint8_t*>(layout), k, v,
                      rows, c);

@@ -8,6 +8,7 @@
 #include <hip/hip_runtime.h>
 
 #include "kernels.h"
+#include "layout.h"
 
 namespace bgtq {
 namespace paged {
@@ -66,6 +67,58 @@ __device__ __forceinline__ int find_item(const PagedBatch& b, int want, const F&
   number = 0;
   seq = {0, 0, 0, false};
   return -1;
+}
+
+// Page (-1: none) and place of input row r0 + tk of a ragged batch, r0 the same
+// in the wave, tk < 16.  The sequence of r0 by a search 64 sequences at a time,
+// the rows' own by one ballot each over the 64 sequences from there on.
+__device__ __forceinline__ int2 page_of_row(const PagedBatch& b, int n_pages, int page_rows, int r0, int tk) {
+  const int lane = threadIdx.x & 63, last = b.n_seqs - 1;
+  int s0 = last;
+  for (int base = 0; base < b.n_seqs; base += 64) {
+    const uint64_t past = __builtin_amdgcn_ballot_w64(base + lane <= last && b.cu[min(base + lane, last) + 1] > r0);
+    if (past != 0) {
+      s0 = base + __builtin_ctzll(past);
+      break;
+    }
+  }
+  const int end = s0 + lane <= last ? b.cu[min(s0 + lane, last) + 1] : 0x7FFFFFFF;
+  int s = s0;
+#pragma unroll
+  for (int j = 0; j < 16; ++j) {
+    const int n = __builtin_popcountll(__builtin_amdgcn_ballot_w64(end <= r0 + j));
+    s = tk == j ? s0 + n : s;
+  }
+  s = min(s, last);
+  // (64 sequences behind s0 end before the row: empty ones among them)
+  while (s < last && b.cu[s + 1] <= r0 + tk) ++s;
+  const Seq q = seq_of(b, s);
+  const int i = r0 + tk - q.first;
+  if (!q.ok || i < 0 || i >= q.n) return make_int2(-1, 0);
+  const int t = q.len - q.n + i;
+  return make_int2(page_of(b, n_pages, page_rows, s, t), t % page_rows);
+}
+
+// Value tile `want` of the new rows of a ragged batch: its page (-1: none), the
+// first row of that tile in the sequence, and the rows [lo, hi) that are new.
+struct Tile {
+  int page, P0, lo, hi;
+  size_t in0;  // input row of the sequence's row 0 (it may lie before the inputs)
+};
+__device__ __forceinline__ bool tile_of(const PagedBatch& b, int n_pages, int page_rows, int want, Tile& t) {
+  int number;
+  Seq q;
+  const int s = find_item(
+      b, want, [](const Seq& x) { return x.ok && x.n > 0 ? (x.len - 1) / kTile - (x.len - x.n) / kTile + 1 : 0; },
+      number, q);
+  if (s < 0) return false;
+  const int wp = q.len - q.n;
+  t.P0 = (wp / kTile + number) * kTile;
+  t.lo = max(t.P0, wp) - t.P0;
+  t.hi = min(t.P0 + kTile, q.len) - t.P0;
+  t.page = page_of(b, n_pages, page_rows, s, t.P0);
+  t.in0 = static_cast<size_t>(static_cast<long>(q.first) - wp);
+  return t.page >= 0;
 }
 
 }  // namespace paged

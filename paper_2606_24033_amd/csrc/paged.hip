@@ -44,7 +44,78 @@ hipError_t join(const Dims& d, const void* layout, const CrossCall& call, const 
   return go(k_cross_merge<4, UnitRows<R>>, rows / 4);
 }
 
+// The query rotation of fp32 rows, as launch_query_rotation's but on the dense
+// key rotation over natural dims in operand order: no gather, 16 rows of a wave
+// on fp32 MFMAs, their 32 dims of a lane in 16-byte reads.  Bound by those
+// products (256 of 32 cycles a wave) and by the staging of the matrix, which
+// rows of several heads of the same KV head share.  28768 rows x 8 KV heads:
+// 112 us there, 23 here.
+constexpr int kRotWaves = 4;
+__global__ __launch_bounds__(kRotWaves * 64) void k_paged_rotate(Dims d, const uint8_t* __restrict__ blob,
+                                                                 const float* __restrict__ q, int n_tokens, int iters,
+                                                                 float* __restrict__ qr) {
+  __shared__ float4 wa[kMfmaMatFloats / 4];
+  __shared__ float scale[kHeadDim];
+  const int tid = threadIdx.x, lane = tid & 63, tk = lane & 15, kk = lane >> 4;
+  const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int kvh = blockIdx.y, ri = d.layer * d.n_kv + kvh, G = d.group, hq = d.n_kv * G, nr = n_tokens * G;
+  const RowMeta* M = reinterpret_cast<const RowMeta*>(blob + kOffRows) + ri;
+  {
+    const float4* src = reinterpret_cast<const float4*>(blob + layout_kdense_offset(d.n_layers * d.n_kv)) +
+                        static_cast<size_t>(ri) * (kMfmaMatFloats / 4);
+    constexpr int kPer = kMfmaMatFloats / 4 / (kRotWaves * 64);
+    float4 t[kPer];
+#pragma unroll
+    for (int u = 0; u < kPer; ++u) t[u] = src[tid + u * kRotWaves * 64];
+    if (tid < kHeadDim) scale[tid] = kLog2e * rsqrtf(static_cast<float>(M->g_dim[M->grp[tid]]) * kHeadDim);
+#pragma unroll
+    for (int u = 0; u < kPer; ++u) wa[tid + u * kRotWaves * 64] = t[u];
+  }
+  __syncthreads();
+  for (int it = 0; it < iters; ++it) {
+    const int r0 = ((blockIdx.x * iters + it) * kRotWaves + wave) * 16;
+    if (r0 >= nr) break;  // wave-uniform
+    const int r = r0 + tk, rc = min(r, nr - 1);
+    const size_t off = (static_cast<size_t>(rc / G) * hq + kvh * G + rc % G) * kHeadDim;
+    float4 x[8];
+#pragma unroll
+    for (int s4 = 0; s4 < 8; ++s4) x[s4] = *reinterpret_cast<const float4*>(q + off + 32 * kk + 4 * s4);
+    float4_t acc[8];
+#pragma unroll
+    for (int t = 0; t < 8; ++t) acc[t] = float4_t{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+    for (int s4 = 0; s4 < 8; ++s4)
+#pragma unroll
+      for (int t = 0; t < 8; ++t) {
+        const float4 w = wa[(t * 8 + s4) * 64 + lane];
+        acc[t] = __builtin_amdgcn_mfma_f32_16x16x4f32(w.x, x[s4].x, acc[t], 0, 0, 0);
+        acc[t] = __builtin_amdgcn_mfma_f32_16x16x4f32(w.y, x[s4].y, acc[t], 0, 0, 0);
+        acc[t] = __builtin_amdgcn_mfma_f32_16x16x4f32(w.z, x[s4].z, acc[t], 0, 0, 0);
+        acc[t] = __builtin_amdgcn_mfma_f32_16x16x4f32(w.w, x[s4].w, acc[t], 0, 0, 0);
+      }
+    if (r < nr) {
+#pragma unroll
+      for (int t = 0; t < 8; ++t)
+        *reinterpret_cast<float4_t*>(qr + off + 16 * t + 4 * kk) =
+            acc[t] * *reinterpret_cast<const float4_t*>(&scale[16 * t + 4 * kk]);
+    }
+  }
+}
+
 }  // namespace
+
+hipError_t launch_paged_rotation(const Dims& d, const void* layout, const void* q, int n_tokens, float* qr, hipStream_t s) {
+  if (d.in_dtype == 1) {
+    Dims dq = d;  // (the chunk's tokens are one sequence's query rows)
+    dq.batch = 1;
+    return launch_query_rotation(dq, layout, q, n_tokens, qr, s);
+  }
+  const long rows = static_cast<long>(n_tokens) * d.group;
+  const int iters = rows * d.n_kv <= 256L * 256 ? 1 : 4, per = kRotWaves * 16 * iters;
+  hipLaunchKernelGGL(k_paged_rotate, dim3((rows + per - 1) / per, d.n_kv), dim3(kRotWaves * 64), 0, s, d,
+                     static_cast<const uint8_t*>(layout), static_cast<const float*>(q), n_tokens, iters, qr);
+  return hipGetLastError();
+}
 
 hipError_t launch_paged_pass(const Dims& d, const void* layout, const void* q, const CrossCall& call, const PagedPass& pass,
                              hipStream_t s) {

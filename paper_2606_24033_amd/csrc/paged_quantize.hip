@@ -1,0 +1,421 @@
+// Append of a ragged batch's bf16 rows to their pages: the TQ-MSE encode of
+// quantize.hip, whose two 128 x 128 products per row run on three exact bf16
+// products (split.h): the terms are exact, the sums fp32, so codes are as right
+// as with fp32 products (a coordinate within their rounding of a threshold may
+// fall to either side of it in either).  fp32 inputs and the wider formats,
+// whose packing buffers don't fit beside 96 KB of matrix, take quantize.hip's
+// kernels; so do sequences of up to 4 rows (k_append_rows).
+//
+// A wave takes 32 rows at a time, so that each matrix operand read from LDS
+// (96 KB per workgroup, split while it is staged) serves two products, and
+// finishes the codes of one 16-wide output tile before it starts the next: 16
+// accumulator registers, so four waves fit a SIMD.  Codes by counting: up to
+// three (width <= 2) or seven (width 3) comparisons against thresholds held per
+// position, a branch-free search only for tiles that hold wider codes.  The
+// group radii stay on fp32 MFMAs (squares of bf16 numbers do not fit bf16).
+#include <hip/hip_fp16.h>
+#include <hip/hip_runtime.h>
+
+#include <algorithm>
+
+#include "kernels.h"
+#include "layout.h"
+#include "paged.h"
+#include "split.h"
+
+namespace bgtq {
+namespace {
+
+using namespace split;
+
+constexpr int kSplitKWords = 16, kSplitVBits = 4;
+
+template <int W>
+struct LdsKeys {
+  uint4_t wa[3][kMatOps];                     // W's three parts, A operand order
+  float4 ma[8 * 64];                          // group membership, fp32 A operand order
+  float4 ta[kHeadDim], tb[kHeadDim];          // first seven thresholds of each position, NaN past its last
+  uint32_t rw[W][kSplitRows * kSplitKWords];  // per wave: packed key rows, k_words apart
+  float sc[W][kSplitRows][kMaxGroups];        // per wave: sqrt(d_g) / radius
+  uint32_t pm[kHeadDim];                      // bit offset | b << 10 | group << 14
+  float thr[kThresholdEntries];
+  float gs[kMaxGroups];
+  int mw[8];                                  // largest width in each tile of 16 positions
+  uint8_t gd[kHeadDim];
+};
+template <int W>
+struct LdsValues {
+  uint4_t rb[3][kMatOps];                     // Pi_V's three parts, B operand order
+  uint32_t vt[W][kHeadDim * kSplitVBits];     // per wave: words of one value tile
+  float nv[W][kSplitRows];
+  float thr[kThresholdEntries];
+};
+constexpr int kWavesLong = 16, kWavesShort = 4;
+static_assert(sizeof(LdsKeys<kWavesLong>) <= 160 * 1024 && sizeof(LdsValues<kWavesLong>) <= 160 * 1024, "LDS");
+
+__device__ __forceinline__ void wave_sync() {  // (LDS operations of one wave complete in order)
+  __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+  __builtin_amdgcn_wave_barrier();
+}
+
+__device__ __forceinline__ float4_t mfma(float a, float b, float4_t c) {
+  return __builtin_amdgcn_mfma_f32_16x16x4f32(a, b, c, 0, 0, 0);
+}
+
+// Element i of the 32 that four operands hold.
+__device__ __forceinline__ float bf16_elem(const uint4_t (&x)[4], int i) {
+  const uint32_t w = x[i >> 3][(i & 7) >> 1];
+  return __uint_as_float(i & 1 ? w & 0xFFFF0000u : w << 16);
+}
+
+// Output tile t of the products of the wave's two sub-tiles, the rows as the
+// A operand and the matrix as the B one (split_product: the other way round).
+__device__ __forceinline__ void rows_product(const uint4_t (*mat)[kMatOps], int t, int lane, const uint4_t (&x)[2][4],
+                                             float4_t (&out)[2]) {
+  float4_t hi[2] = {{0.f, 0.f, 0.f, 0.f}, {0.f, 0.f, 0.f, 0.f}}, lo[2] = {{0.f, 0.f, 0.f, 0.f}, {0.f, 0.f, 0.f, 0.f}};
+#pragma unroll
+  for (int q = 0; q < 4; ++q) {
+    const int o = (t * 4 + q) * 64 + lane;
+    const uint4_t w0 = mat[0][o], w1 = mat[1][o], w2 = mat[2][o];
+#pragma unroll
+    for (int s = 0; s < 2; ++s) lo[s] = mfma_bf16(x[s][q], w2, lo[s]);
+#pragma unroll
+    for (int s = 0; s < 2; ++s) hi[s] = mfma_bf16(x[s][q], w0, hi[s]);
+#pragma unroll
+    for (int s = 0; s < 2; ++s) lo[s] = mfma_bf16(x[s][q], w1, lo[s]);
+  }
+#pragma unroll
+  for (int s = 0; s < 2; ++s) out[s] = hi[s] + lo[s];
+}
+
+// ---------------------------------------------------------------- keys
+template <int W>
+__device__ __forceinline__ void quant_keys(LdsKeys<W>& S, int bx, int iters, const Dims& d,
+                                           const uint8_t* __restrict__ blob, const void* __restrict__ kin,
+                                           const PagedRows& rows, const CachePtrs& c) {
+  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int head = blockIdx.y;
+  const int cap = d.capacity, n = rows.b.n_tokens;
+  constexpr int kThreads = W * 64;
+  const int r_wg = bx * W * kSplitRows * iters;
+  if (r_wg >= n) return;
+  const int n_rows_blob = d.n_layers * d.n_kv, ri = d.layer * d.n_kv + head;
+  const RowMeta* M = reinterpret_cast<const RowMeta*>(blob + kOffRows) + ri;
+  const float* gthr = reinterpret_cast<const float*>(blob + kOffThr);
+  const int ng = M->n_groups, kw = d.k_words;
+
+  for (int i = tid; i < W * kSplitRows * kSplitKWords; i += kThreads) (&S.rw[0][0])[i] = 0u;
+  for (int i = tid; i < kThresholdEntries; i += kThreads) S.thr[i] = gthr[i];
+  if (tid < kHeadDim) {
+    const int g = M->grp[tid], b = M->width[tid], nt = (1 << b) - 1;
+    S.gd[M->dim[tid]] = static_cast<uint8_t>(g);
+    S.pm[tid] = static_cast<uint32_t>(M->bitoff[tid]) | (static_cast<uint32_t>(b) << 10) | (static_cast<uint32_t>(g) << 14);
+    float th[8];
+#pragma unroll
+    for (int j = 0; j < 8; ++j) th[j] = j < nt ? gthr[thr_index(b) + j] : __builtin_nanf("");
+    S.ta[tid] = make_float4(th[0], th[1], th[2], th[3]);
+    S.tb[tid] = make_float4(th[4], th[5], th[6], th[7]);
+  }
+  if (tid < kMaxGroups) {
+    S.gs[tid] = tid < ng ? sqrtf(static_cast<float>(M->g_dim[tid])) : 0.f;
+    int w = 0;
+    for (int j = 0; j < 16; ++j) w = max(w, static_cast<int>(M->width[16 * tid + j]));
+    S.mw[tid] = w;
+  }
+  stage_split<W>(S.wa, reinterpret_cast<const float4*>(blob + layout_kdense_offset(n_rows_blob)) + static_cast<size_t>(ri) * kMatF4,
+                 tid);
+  __syncthreads();
+  for (int i = tid; i < 8 * 64; i += kThreads) {
+    // row 4 m + e of the product is group 2 m + e (e < 2): two groups to each
+    // quarter of the wave instead of four to two of them
+    const int s4 = i >> 6, l = i & 63, d0 = 32 * (l >> 4) + 4 * s4;
+    const int g = (l & 3) < 2 ? 2 * ((l >> 2) & 3) + (l & 3) : -1;
+    S.ma[i] = make_float4(S.gd[d0] == g ? 1.f : 0.f, S.gd[d0 + 1] == g ? 1.f : 0.f, S.gd[d0 + 2] == g ? 1.f : 0.f,
+                          S.gd[d0 + 3] == g ? 1.f : 0.f);
+  }
+  __syncthreads();
+
+  const int tk = lane & 15, kk = lane >> 4;
+  const float gs[2] = {S.gs[2 * kk], S.gs[2 * kk + 1]};
+  const int nslot = (ng + 1) & ~1;
+  const auto cache_row = [&](int page) { return (static_cast<size_t>(d.layer) * d.batch + page) * d.n_kv + head; };
+  for (int it = 0; it < iters; ++it) {
+    const int r0 = r_wg + (it * W + wave) * kSplitRows;
+    if (r0 >= n) break;  // wave-uniform
+    uint4_t x[2][4];
+    int2 at[2];
+#pragma unroll
+    for (int s = 0; s < 2; ++s) {
+      const int r = r0 + kSub * s + tk;
+      load_operands(kin, min(r, n - 1) * rows.k_stride + head * kHeadDim + 32 * kk, r < n, x[s]);
+    }
+#pragma unroll
+    for (int s = 0; s < 2; ++s) {
+      at[s] = paged::page_of_row(rows.b, d.batch, cap, r0 + kSub * s, tk);
+      if (r0 + kSub * s + tk >= n) at[s].x = -1;
+    }
+    // group radii: R2[g][row] = sum_d [group(d) = g] x[row][d]^2
+    float4_t n2[2] = {{0.f, 0.f, 0.f, 0.f}, {0.f, 0.f, 0.f, 0.f}};
+#pragma unroll
+    for (int s4 = 0; s4 < 8; ++s4) {
+      const float4 m = S.ma[s4 * 64 + lane];
+      const float me[4] = {m.x, m.y, m.z, m.w};
+#pragma unroll
+      for (int e = 0; e < 4; ++e)
+#pragma unroll
+        for (int s = 0; s < 2; ++s) {
+          const float v = bf16_elem(x[s], 4 * s4 + e);
+          n2[s] = mfma(me[e], v * v, n2[s]);
+        }
+      __builtin_amdgcn_sched_barrier(0);  // (eight steps' squares at once would spill)
+    }
+    // this lane holds R2 of rows tk, 16 + tk for groups 2 kk, 2 kk + 1 (zero
+    // past the last group)
+#pragma unroll
+    for (int s = 0; s < 2; ++s) {
+      float nrm[2];
+      uint16_t h[2];
+#pragma unroll
+      for (int i = 0; i < 2; ++i) {
+        nrm[i] = sqrtf(n2[s][i]);
+        S.sc[wave][kSub * s + tk][2 * kk + i] = nrm[i] > 0.f ? gs[i] / nrm[i] : 0.f;
+        h[i] = __half_as_ushort(__float2half_rn(nrm[i]));
+      }
+      if (at[s].x >= 0 && 2 * kk < ng) {
+        uint16_t* dst = c.k_norms + cache_row(at[s].x) * kMaxGroups * cap + static_cast<size_t>(at[s].y) * nslot + 2 * kk;
+        if (2 * kk + 1 < ng) *reinterpret_cast<uint32_t*>(dst) = h[0] | static_cast<uint32_t>(h[1]) << 16;
+        else *dst = h[0];
+      }
+    }
+    wave_sync();
+    // Z[p][row] = sum_d W[p][d] x[row][d]; codes of stream positions
+    // 16 t + 4 kk + i of a row: one bit field
+#pragma unroll 1
+    for (int t = 0; t < 8; ++t) {
+      const int p0 = 16 * t + 4 * kk;
+      float4_t z[2];
+      split_product(S.wa, t, lane, x, z);
+      uint32_t pm[4];
+#pragma unroll
+      for (int i = 0; i < 4; ++i) pm[i] = S.pm[p0 + i];
+#pragma unroll
+      for (int s = 0; s < 2; ++s)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) z[s][i] *= S.sc[wave][kSub * s + tk][(pm[i] >> 14) & 7];
+      const int mw = __builtin_amdgcn_readfirstlane(S.mw[t]);
+      uint32_t code[2][4];
+      if (mw <= 3) {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          const float4 th = S.ta[p0 + i];
+#pragma unroll
+          for (int s = 0; s < 2; ++s)
+            code[s][i] = (th.x <= z[s][i] ? 1u : 0u) + (th.y <= z[s][i] ? 1u : 0u) + (th.z <= z[s][i] ? 1u : 0u);
+        }
+        if (mw == 3) {
+#pragma unroll
+          for (int i = 0; i < 4; ++i) {
+            const float t3 = S.ta[p0 + i].w;
+            const float4 th = S.tb[p0 + i];
+#pragma unroll
+            for (int s = 0; s < 2; ++s)
+              code[s][i] += (t3 <= z[s][i] ? 1u : 0u) + (th.x <= z[s][i] ? 1u : 0u) + (th.y <= z[s][i] ? 1u : 0u) +
+                            (th.z <= z[s][i] ? 1u : 0u);
+          }
+        }
+      } else {
+#pragma unroll
+        for (int s = 0; s < 2; ++s)
+#pragma unroll
+          for (int i = 0; i < 4; ++i) code[s][i] = 0u;
+        // all lanes read on every step (a narrow position's index stays inside
+        // the table: thr_index(7) + 127 at most) and the eight reads of a step
+        // are in flight together
+#pragma unroll 1
+        for (uint32_t step = 1u << (mw - 1); step > 0; step >>= 1) {
+          float tv[2][4];
+#pragma unroll
+          for (int i = 0; i < 4; ++i) {
+            const int first = thr_index((pm[i] >> 10) & 15) + static_cast<int>(step) - 1;
+#pragma unroll
+            for (int s = 0; s < 2; ++s) tv[s][i] = S.thr[min(first + static_cast<int>(code[s][i]), kThresholdEntries - 1)];
+          }
+#pragma unroll
+          for (int i = 0; i < 4; ++i) {
+            const uint32_t add = (step >> ((pm[i] >> 10) & 15)) == 0 ? step : 0u;
+#pragma unroll
+            for (int s = 0; s < 2; ++s) code[s][i] += tv[s][i] <= z[s][i] ? add : 0u;
+          }
+        }
+      }
+      const int b0 = (pm[0] >> 10) & 15, b1 = b0 + ((pm[1] >> 10) & 15), b2 = b1 + ((pm[2] >> 10) & 15);
+      const int nb = b2 + ((pm[3] >> 10) & 15), bo = pm[0] & 1023, w = bo >> 5, sh = bo & 31;
+#pragma unroll
+      for (int s = 0; s < 2; ++s) {
+        const uint32_t field = code[s][0] | code[s][1] << b0 | code[s][2] << b1 | code[s][3] << b2;
+        uint32_t* dst = &S.rw[wave][(kSub * s + tk) * kw + w];
+        atomicOr(dst, field << sh);
+        if (sh + nb > 32) atomicOr(dst + 1, field >> (32 - sh));
+      }
+    }
+    wave_sync();
+    for (int idx = lane; idx < kSplitRows * kw; idx += 64) {
+      const int t2 = idx / kw, w = idx - t2 * kw;
+      // (row t2's page and place, from lane t2 % 16: lanes 0 .. 15 take part in every round)
+      const int x0 = __shfl(at[0].x, t2 & 15), y0 = __shfl(at[0].y, t2 & 15), x1 = __shfl(at[1].x, t2 & 15),
+                y1 = __shfl(at[1].y, t2 & 15);
+      const int2 a = t2 < kSub ? make_int2(x0, y0) : make_int2(x1, y1);
+      if (a.x >= 0) c.k_codes[(cache_row(a.x) * cap + a.y) * kw + w] = S.rw[wave][idx];
+      S.rw[wave][idx] = 0u;
+    }
+    wave_sync();
+  }
+}
+
+// ---------------------------------------------------------------- values
+// The BV-bit codes of one value tile, ORed into its words.
+template <int BV, int W>
+__device__ __forceinline__ void tile_codes(LdsValues<W>& S, int wave, int lane, const uint4_t (&x)[2][4], int s_lo, int s_hi) {
+  constexpr int kThr = (1 << BV) - 1;
+  const int tk = lane & 15, kk = lane >> 4;
+  const float sq = sqrtf(static_cast<float>(kHeadDim));
+  float scl[2][4], thr[kThr];
+  uint32_t keep[2] = {0u, 0u};
+#pragma unroll
+  for (int h = 0; h < 2; ++h)
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const int s = kSub * h + 4 * kk + i;
+      const float n = S.nv[wave][s];
+      scl[h][i] = n > 0.f ? sq / n : 0.f;
+      keep[h] |= (s >= s_lo && s < s_hi ? ((1u << BV) - 1u) : 0u) << (i * BV);
+    }
+#pragma unroll
+  for (int j = 0; j < kThr; ++j)
+    thr[j] = __uint_as_float(__builtin_amdgcn_readfirstlane(__float_as_uint(S.thr[thr_index(BV) + j])));
+#pragma unroll 1
+  for (int t = 0; t < 8; ++t) {
+    // Z[row][j] = sum_d x[row][d] Pi_V[j][d]; this lane: coordinate j of
+    // rows 16 h + 4 kk + i
+    float4_t z[2];
+    rows_product(S.rb, t, lane, x, z);
+    const int j = 16 * t + tk;
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+      const int bit = (kSub * h + 4 * kk) * BV, w = bit >> 5, sh = bit & 31;
+      uint32_t field = 0;
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        const float v = z[h][i] * scl[h][i];
+        uint32_t code = 0;
+#pragma unroll
+        for (int e = 0; e < kThr; ++e) code += thr[e] <= v ? 1u : 0u;
+        field |= code << (i * BV);
+      }
+      field &= keep[h];
+      atomicOr(&S.vt[wave][j * BV + w], field << sh);
+      if (sh + 4 * BV > 32) atomicOr(&S.vt[wave][j * BV + w + 1], field >> (32 - sh));
+    }
+  }
+}
+
+template <int W, int BV>
+__device__ __forceinline__ void quant_values(LdsValues<W>& S, int bx, int iters, const Dims& d,
+                                             const uint8_t* __restrict__ blob, const void* __restrict__ vin,
+                                             const PagedRows& rows, const CachePtrs& c) {
+  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int head = blockIdx.y, cap = d.capacity;
+  const float* gthr = reinterpret_cast<const float*>(blob + kOffThr);
+  for (int i = tid; i < kThresholdEntries; i += W * 64) S.thr[i] = gthr[i];
+  stage_split<W>(S.rb, reinterpret_cast<const float4*>(blob + layout_rotv_mfma_offset(d.n_layers * d.n_kv)), tid);
+  __syncthreads();
+
+  const int tk = lane & 15, kk = lane >> 4;
+  for (int it = 0; it < iters; ++it) {
+    paged::Tile t;
+    if (!paged::tile_of(rows.b, d.batch, cap, bx * W * iters + it * W + wave, t)) continue;  // wave-uniform
+    const size_t row = (static_cast<size_t>(d.layer) * d.batch + t.page) * d.n_kv + head, in_at = t.in0 + t.P0;
+    const int P0 = t.P0 % cap;
+    uint4_t x[2][4];
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+      const int slot = kSub * h + tk;
+      load_operands(vin, (in_at + slot) * rows.v_stride + head * kHeadDim + 32 * kk, slot >= t.lo && slot < t.hi, x[h]);
+    }
+    uint32_t* gv = c.v_codes + (row * (cap / kTile) + P0 / kTile) * kHeadDim * static_cast<size_t>(BV);
+    // tile words: zero, or the old words with the new rows' bits cleared
+    if (t.lo == 0 && t.hi == kTile) {
+      for (int idx = lane; idx < kHeadDim * BV; idx += 64) S.vt[wave][idx] = 0u;
+    } else {
+      for (int idx = lane; idx < kHeadDim * BV; idx += 64) {
+        const int w = idx % BV;
+        const int lo_b = max(t.lo * BV - 32 * w, 0), hi_b = min(t.hi * BV - 32 * w, 32);
+        const uint32_t mask = hi_b <= lo_b ? 0u : (hi_b - lo_b == 32 ? ~0u : ((1u << (hi_b - lo_b)) - 1u) << lo_b);
+        S.vt[wave][idx] = gv[idx] & ~mask;
+      }
+    }
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+      const int slot = kSub * h + tk;
+      float ss = 0.f;
+#pragma unroll
+      for (int i = 0; i < 32; ++i) ss = fmaf(bf16_elem(x[h], i), bf16_elem(x[h], i), ss);
+      ss += __shfl_xor(ss, 16, 64);
+      ss += __shfl_xor(ss, 32, 64);
+      const float nrm = sqrtf(ss);
+      if (kk == 0) {
+        S.nv[wave][slot] = nrm;
+        if (slot >= t.lo && slot < t.hi) c.v_norms[row * cap + P0 + slot] = __half_as_ushort(__float2half_rn(nrm));
+      }
+    }
+    wave_sync();
+    tile_codes<BV, W>(S, wave, lane, x, t.lo, t.hi);
+    wave_sync();
+    for (int idx = lane; idx < kHeadDim * BV; idx += 64) gv[idx] = S.vt[wave][idx];
+    wave_sync();
+  }
+}
+
+// The key workgroups (the longer ones) come first.
+template <int W, int BV>
+__global__ __launch_bounds__(W * 64) void k_paged_quantize(Dims d, const uint8_t* __restrict__ blob,
+                                                           const void* __restrict__ kin, const void* __restrict__ vin,
+                                                           PagedRows rows, CachePtrs c, int n_kwg, int k_iters, int v_iters) {
+  constexpr size_t kBytes = sizeof(LdsKeys<W>) > sizeof(LdsValues<W>) ? sizeof(LdsKeys<W>) : sizeof(LdsValues<W>);
+  __shared__ __attribute__((aligned(16))) uint8_t smem[kBytes];
+  const int bx = static_cast<int>(blockIdx.x);
+  if (bx < n_kwg) quant_keys<W>(*reinterpret_cast<LdsKeys<W>*>(smem), bx, k_iters, d, blob, kin, rows, c);
+  else quant_values<W, BV>(*reinterpret_cast<LdsValues<W>*>(smem), bx - n_kwg, v_iters, d, blob, vin, rows, c);
+}
+
+}  // namespace
+
+bool paged_quantize_fits(const Dims& d) { return d.in_dtype == 1 && d.k_words <= kSplitKWords && d.v_bits <= kSplitVBits; }
+
+hipError_t launch_paged_quantize_bf16(const Dims& d, const void* layout, const void* k, const void* v, const PagedRows& rows,
+                                      const CachePtrs& c, hipStream_t s) {
+  const long n = rows.b.n_tokens, all = n * d.n_kv, tiles = std::min(n, (n + 62L * rows.b.n_seqs) / kTile);
+  const auto go = [&](auto kern, int w, int k_iters, int v_iters) {
+    const int n_kwg = static_cast<int>((n + w * kSplitRows * k_iters - 1) / (w * kSplitRows * k_iters));
+    const int n_vwg = static_cast<int>((tiles + w * v_iters - 1) / (w * v_iters));
+    hipLaunchKernelGGL(kern, dim3(n_kwg + n_vwg, d.n_kv), dim3(w * 64), 0, s, d, static_cast<const uint8_t*>(layout), k, v, rows,
+                       c, n_kwg, k_iters, v_iters);
+    return hipGetLastError();
+  };
+  const auto width = [&](auto bv) {
+    constexpr int B = decltype(bv)::value;
+    // 4-wave workgroups for calls of up to 64K rows, which then spread over more
+    // CUs; 16-wave ones share the staging of a matrix, above 512K rows for four rounds
+    if (all <= 256L * 256) return go(k_paged_quantize<kWavesShort, B>, kWavesShort, 1, 1);
+    const int iters = all <= 2L * 256 * 512 ? 1 : all <= 4L * 256 * 512 ? 2 : 4;
+    return go(k_paged_quantize<kWavesLong, B>, kWavesLong, iters, iters);
+  };
+  switch (d.v_bits) {
+    case 1: return width(std::integral_constant<int, 1>{});
+    case 2: return width(std::integral_constant<int, 2>{});
+    case 3: return width(std::integral_constant<int, 3>{});
+    default: return width(std::integral_constant<int, 4>{});
+  }
+}
+
+}  // namespace bgtq

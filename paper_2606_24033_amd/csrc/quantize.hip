@@ -155,58 +155,6 @@ __device__ __forceinline__ float4_t mfma(float a, float b, float4_t c) {
   return __builtin_amdgcn_mfma_f32_16x16x4f32(a, b, c, 0, 0, 0);
 }
 
-// Page (-1: none) and place of input row r0 + tk of a ragged batch, r0 the same
-// in the wave, tk < 16.  The sequence of r0 by a search 64 sequences at a time,
-// the rows' own by one ballot each over the 64 sequences from there on.
-__device__ __forceinline__ int2 page_of_row(const PagedBatch& b, int n_pages, int page_rows, int r0, int tk) {
-  const int lane = threadIdx.x & 63, last = b.n_seqs - 1;
-  int s0 = last;
-  for (int base = 0; base < b.n_seqs; base += 64) {
-    const uint64_t past = __builtin_amdgcn_ballot_w64(base + lane <= last && b.cu[min(base + lane, last) + 1] > r0);
-    if (past != 0) {
-      s0 = base + __builtin_ctzll(past);
-      break;
-    }
-  }
-  const int end = s0 + lane <= last ? b.cu[min(s0 + lane, last) + 1] : 0x7FFFFFFF;
-  int s = s0;
-#pragma unroll
-  for (int j = 0; j < kSub; ++j) {
-    const int n = __builtin_popcountll(__builtin_amdgcn_ballot_w64(end <= r0 + j));
-    s = tk == j ? s0 + n : s;
-  }
-  s = min(s, last);
-  // (64 sequences behind s0 end before the row: empty ones among them)
-  while (s < last && b.cu[s + 1] <= r0 + tk) ++s;
-  const paged::Seq q = paged::seq_of(b, s);
-  const int i = r0 + tk - q.first;
-  if (!q.ok || i < 0 || i >= q.n) return make_int2(-1, 0);
-  const int t = q.len - q.n + i;
-  return make_int2(paged::page_of(b, n_pages, page_rows, s, t), t % page_rows);
-}
-
-// Value tile `want` of the new rows of a ragged batch: its page (-1: none), the
-// first row of that tile in the sequence, and the rows [lo, hi) that are new.
-struct PagedTile {
-  int page, P0, lo, hi;
-  size_t in0;  // input row of the sequence's row 0 (it may lie before the inputs)
-};
-__device__ __forceinline__ bool paged_tile(const PagedBatch& b, int n_pages, int page_rows, int want, PagedTile& t) {
-  int number;
-  paged::Seq q;
-  const int s = paged::find_item(
-      b, want, [](const paged::Seq& x) { return x.ok && x.n > 0 ? (x.len - 1) / kTile - (x.len - x.n) / kTile + 1 : 0; },
-      number, q);
-  if (s < 0) return false;
-  const int wp = q.len - q.n;
-  t.P0 = (wp / kTile + number) * kTile;
-  t.lo = max(t.P0, wp) - t.P0;
-  t.hi = min(t.P0 + kTile, q.len) - t.P0;
-  t.page = paged::page_of(b, n_pages, page_rows, s, t.P0);
-  t.in0 = static_cast<size_t>(static_cast<long>(q.first) - wp);
-  return t.page >= 0;
-}
-
 // ---------------------------------------------------------------- keys
 // Workgroup bx of the key part: rows [bx R, bx R + R) of the call, R =
 // W kSub iters.
@@ -277,7 +225,7 @@ __device__ __forceinline__ void quant_keys(LdsK<W>& S, int bx, int iters, const 
     float x[32];
     if constexpr (kPaged) {
       load_slice<BF16>(kin, min(r, n_fit - 1) * rows.k_stride + head * kHeadDim + 32 * kk, valid, x);
-      const int2 at = page_of_row(rows.b, d.batch, cap, r0, tk);
+      const int2 at = paged::page_of_row(rows.b, d.batch, cap, r0, tk);
       valid = valid && at.x >= 0;
       row_r = (static_cast<size_t>(layer) * d.batch + max(at.x, 0)) * d.n_kv + head;
       t_r = at.y;
@@ -412,8 +360,8 @@ __device__ __forceinline__ void quant_values(LdsV<W>& S, int bx, int iters, cons
     size_t row, in_at;  // in_at: input row of slot 0
     int tile, P0, s_lo, s_hi;
     if constexpr (kPaged) {
-      PagedTile t;
-      if (!paged_tile(rows.b, d.batch, cap, tw, t)) continue;  // wave-uniform
+      paged::Tile t;
+      if (!paged::tile_of(rows.b, d.batch, cap, tw, t)) continue;  // wave-uniform
       row = (static_cast<size_t>(layer) * d.batch + t.page) * d.n_kv + head;
       tile = t.P0 % cap / kTile;
       P0 = t.P0 % cap;
@@ -520,8 +468,8 @@ __device__ __forceinline__ void quant_values_short(LdsVS& S, int bx, const Dims&
   size_t row, in_at;  // in_at: input row of slot 0
   int tile, P0, s_lo, s_hi;  // rows [s_lo, s_hi) are new
   if constexpr (kPaged) {
-    PagedTile t = {0, 0, 0, 0, 0};
-    active = paged_tile(rows.b, d.batch, cap, tw0 + u, t);
+    paged::Tile t = {0, 0, 0, 0, 0};
+    active = paged::tile_of(rows.b, d.batch, cap, tw0 + u, t);
     row = (static_cast<size_t>(layer) * d.batch + max(t.page, 0)) * d.n_kv + head;
     tile = t.P0 % cap / kTile;
     P0 = t.P0 % cap;

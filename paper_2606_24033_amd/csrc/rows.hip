@@ -75,8 +75,22 @@ struct RowsCall {
   const int32_t* ctx_len;  // or null
   void* out[2];            // keys, values; a null one has no workgroups
   int n_rows;
-  int chunks[2], tiles[2];  // workgroups per unit and tiles (64 keys, 32 values) per workgroup
+  int of_seq[2];            // tiles (64 keys, 32 values) that a sequence's rows reach into at most
+  int chunks[2], tiles[2];  // workgroups per (layer, head), and tiles of a workgroup: those of all
+                            // sequences one after the other, so that few rows of many share a matrix
   int key_items;            // workgroups of the keys
+};
+
+// The rows of the sequence that a wave is at: read again where it changes.
+struct SeqRows {
+  int seq = -1, end = 0;
+  long pos = 0;
+  __device__ __forceinline__ void turn_to(const RowsCall& call, const Dims& d, int s) {  // (s: wave-uniform)
+    if (s == seq) return;
+    seq = s;
+    pos = call.read_pos[s];
+    end = min(d.capacity, call.ctx_len ? call.ctx_len[s] : d.capacity);
+  }
 };
 
 // Two consecutive B-bit codes at bit POS of w -> two fp16 centroids.
@@ -282,10 +296,10 @@ __device__ __forceinline__ void scale_keys(const uint8_t* smem, const uint32_t (
 
 template <int KWB, bool F32>
 __device__ __forceinline__ void read_keys(uint8_t* smem, const Dims& d, const uint8_t* __restrict__ blob,
-                                          const RowsCall& call, int lz, int kvh, int chunk, long pos, int end) {
+                                          const RowsCall& call, int lc, int kvh, int chunk) {
   const int tid = threadIdx.x, lane = tid & 63;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-  const int layer = d.layer >= 0 ? d.layer : lz / d.batch, seq = lz % d.batch, ri = layer * d.n_kv + kvh;
+  const int layer = d.layer >= 0 ? d.layer : lc, ri = layer * d.n_kv + kvh;
   const RowMeta* M = reinterpret_cast<const RowMeta*>(blob + kOffRows) + ri;
   const int ng = M->n_groups, nslot = (ng + 1) & ~1, kw = d.k_words;
   uint32_t gm[8], used = 0;
@@ -297,19 +311,20 @@ __device__ __forceinline__ void read_keys(uint8_t* smem, const Dims& d, const ui
     gd[b] = b < ng ? M->g_dim[b] : 0;
     gp[b] = M->g_pos[b];
   }
-  const size_t row = (static_cast<size_t>(layer) * d.batch + seq) * d.n_kv + kvh;
   const size_t cap = d.capacity;
-  const uint32_t* kc = call.c.k_codes + row * cap * kw;
-  const uint16_t* kn = call.c.k_norms + row * kMaxGroups * cap;
-  const int n_tiles = (call.n_rows + 63) / 64, first = chunk * call.tiles[0];
-  const int last = min(n_tiles, first + call.tiles[0]);
+  const int first = chunk * call.tiles[0], last = min(d.batch * call.of_seq[0], first + call.tiles[0]);
   uint32_t nw[KWB], next_radii[4];
   bool next_valid;
+  SeqRows sr;
   // a tile's words, a tile ahead (past the last one, row 0 again: in bounds, for nobody)
-  const auto load = [&](int tile) {
-    const int i = tile * 64 + lane;
-    const long t = pos + i;
-    next_valid = tile < last && i < call.n_rows && t >= 0 && t < end;
+  const auto load = [&](int at) {
+    if (at < last) sr.turn_to(call, d, at / call.of_seq[0]);
+    const size_t row = (static_cast<size_t>(layer) * d.batch + max(sr.seq, 0)) * d.n_kv + kvh;
+    const uint32_t* kc = call.c.k_codes + row * cap * kw;
+    const uint16_t* kn = call.c.k_norms + row * kMaxGroups * cap;
+    const int i = at % call.of_seq[0] * 64 + lane;
+    const long t = sr.pos + i;
+    next_valid = at < last && i < call.n_rows && t >= 0 && t < sr.end;
     const size_t tr = next_valid ? static_cast<size_t>(t) : 0;  // (any row of the cache: its result is not stored)
     const uint32_t* src = kc + tr * kw;
     if ((kw & 3) == 0) {
@@ -397,7 +412,13 @@ __device__ __forceinline__ void read_keys(uint8_t* smem, const Dims& d, const ui
   }
   __syncthreads();
 
-  for (int tile = first + wave; tile < last; tile += kWaves) {
+  for (int t = first + wave; t < last; t += kWaves) {
+    const int lz = lc * d.batch + t / call.of_seq[0], tile = t % call.of_seq[0];
+    const unsigned long long ok = __builtin_amdgcn_ballot_w64(next_valid);
+    if (ok == 0) {  // no row of the sequence
+      load(t + kWaves);
+      continue;
+    }
     uint32_t rw[KWB + split_detail::kRowPad], radii[4];
 #pragma unroll
     for (int k = 0; k < KWB; ++k) rw[k] = nw[k];
@@ -405,8 +426,7 @@ __device__ __forceinline__ void read_keys(uint8_t* smem, const Dims& d, const ui
     for (int k = KWB; k < KWB + split_detail::kRowPad; ++k) rw[k] = 0u;
 #pragma unroll
     for (int k = 0; k < 4; ++k) radii[k] = next_radii[k];
-    const bool valid = next_valid;
-    load(tile + kWaves);
+    load(t + kWaves);
     float16_t acc[2][4];
 #pragma unroll
     for (int n = 0; n < 2; ++n)
@@ -420,7 +440,6 @@ __device__ __forceinline__ void read_keys(uint8_t* smem, const Dims& d, const ui
     for (int k = 0; k < 4; ++k) r[0][k] = radii[k];
     spread4(r[0], r[1]);
     scale_keys(smem, r, lane, acc);
-    const unsigned long long ok = __builtin_amdgcn_ballot_w64(valid);
 #pragma unroll
     for (int n = 0; n < 2; ++n) {
       // lane = token 32 n + l32 of the tile
@@ -457,17 +476,26 @@ __device__ __forceinline__ void decode_values(const uint8_t* smem, uint8_t* tile
   }
 }
 
-// The wave's tiles first, first + 8, .. below last, of cache tiles that hold a
-// row below end; the next one's words are in flight.
+// The wave's tiles first, first + 8, .. below last (of the sequences' tiles one
+// after the other), of cache tiles that hold a row of the call; the next one's
+// words are in flight.
 template <bool F32, int BV>
 __device__ __forceinline__ void value_tiles(const uint8_t* smem, uint8_t* mine, const Dims& d, const RowsCall& call,
-                                            const uint32_t* __restrict__ vc, const uint16_t* __restrict__ vn, long first,
-                                            long last, long pos, int end, int lz, int kvh, int lane) {
+                                            int first, int last, int layer, int lc, int kvh, int lane) {
   const int l32 = lane & 31, hf = lane >> 5;
   uint32_t w[2][BV];
   uint16_t radius;
-  const auto load = [&](long tile) {
-    const size_t t = static_cast<size_t>(tile < last && tile >= 0 && tile * kTile < end ? tile : 0);  // (else for nobody)
+  SeqRows sr;
+  long next_tile = 0;  // of its sequence, whose rows are pos_n .. below end_n
+  bool next_any = false;
+  const auto load = [&](int at) {
+    if (at < last) sr.turn_to(call, d, at / call.of_seq[1]);
+    const size_t row = (static_cast<size_t>(layer) * d.batch + max(sr.seq, 0)) * d.n_kv + kvh;
+    const uint32_t* vc = call.c.v_codes + row * (d.capacity / kTile) * kHeadDim * BV;
+    const uint16_t* vn = call.c.v_norms + row * d.capacity;
+    next_tile = (sr.pos >> 5) + at % call.of_seq[1];
+    next_any = at < last && next_tile >= 0 && next_tile * kTile < min(static_cast<long>(sr.end), sr.pos + call.n_rows);
+    const size_t t = static_cast<size_t>(next_any ? next_tile : 0);  // (else for nobody)
     const uint32_t* src = vc + t * kHeadDim * BV;
 #pragma unroll
     for (int h = 0; h < 2; ++h)
@@ -476,16 +504,17 @@ __device__ __forceinline__ void value_tiles(const uint8_t* smem, uint8_t* mine, 
     radius = vn[t * kTile + l32];
   };
   load(first);
-  for (long tile = first; tile < last; tile += kWaves) {
-    if (tile < 0 || tile * kTile >= end) {  // uniform
-      load(tile + kWaves);
+  for (int f = first; f < last; f += kWaves) {
+    if (!next_any) {  // uniform
+      load(f + kWaves);
       continue;
     }
-    const long t = tile * kTile + l32;
+    const long tile = next_tile, pos = sr.pos, t = tile * kTile + l32;
+    const int end = sr.end, lz = lc * d.batch + sr.seq;
     const float scale = static_cast<float>(__builtin_bit_cast(_Float16, radius)) / kMatScale;
     __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");  // the last tile's reads come before this one's writes
     decode_values<BV>(smem, mine, w, lane);
-    load(tile + kWaves);
+    load(f + kWaves);
     __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");  // a wave's LDS operations complete in order
     __builtin_amdgcn_wave_barrier();
     float16_t acc[4];
@@ -514,10 +543,10 @@ __device__ __forceinline__ void value_tiles(const uint8_t* smem, uint8_t* mine, 
 
 template <bool F32>
 __device__ __forceinline__ void read_values(uint8_t* smem, const Dims& d, const uint8_t* __restrict__ blob,
-                                            const RowsCall& call, int lz, int kvh, int chunk, long pos, int end) {
+                                            const RowsCall& call, int lc, int kvh, int chunk) {
   const int tid = threadIdx.x, lane = tid & 63;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-  const int layer = d.layer >= 0 ? d.layer : lz / d.batch, seq = lz % d.batch;
+  const int layer = d.layer >= 0 ? d.layer : lc;
   // A[dim][j] = 2^8 / sqrt(128) Pi_V[j][dim], read from the transposed Pi_V
   {
     const uint16_t* c16 = reinterpret_cast<const uint16_t*>(blob + kOffC16);
@@ -544,17 +573,11 @@ __device__ __forceinline__ void read_values(uint8_t* smem, const Dims& d, const 
     }
   }
   __syncthreads();
-  const size_t row = (static_cast<size_t>(layer) * d.batch + seq) * d.n_kv + kvh;
-  const size_t cap = d.capacity;
   const int bv = d.v_bits;
-  const uint32_t* vc = call.c.v_codes + row * (cap / kTile) * kHeadDim * bv;
-  const uint16_t* vn = call.c.v_norms + row * cap;
   uint8_t* const mine = smem + kMat + 2 * kVSteps * 4096 + wave * kTileBytes;
-  // cache tiles from the one that holds the first row
-  const long tile0 = pos >> 5, tile_end = (pos + call.n_rows + kTile - 1) >> 5;
-  const long at = tile0 + chunk * static_cast<long>(call.tiles[1]), last = min(tile_end, at + call.tiles[1]);
+  const int at = chunk * call.tiles[1], last = min(d.batch * call.of_seq[1], at + call.tiles[1]);
   const auto go = [&](auto b) __attribute__((always_inline)) {
-    value_tiles<F32, decltype(b)::value>(smem, mine, d, call, vc, vn, at + wave, last, pos, end, lz, kvh, lane);
+    value_tiles<F32, decltype(b)::value>(smem, mine, d, call, at + wave, last, layer, lc, kvh, lane);
   };
   switch (bv) {
     case 1: go(std::integral_constant<int, 1>{}); break;
@@ -568,7 +591,7 @@ __device__ __forceinline__ void read_values(uint8_t* smem, const Dims& d, const 
   }
 }
 
-// One-dimensional grid: the keys' (unit, chunk) items, then the values'.
+// One-dimensional grid: the keys' (layer, head, chunk) items, then the values'.
 template <int KWB, bool F32>
 __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(2, 2))) void k_read_rows(
     Dims d, const uint8_t* __restrict__ blob, RowsCall call) {
@@ -578,11 +601,9 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(2, 2))
   const int chunks = keys ? call.chunks[0] : call.chunks[1];
   const int chunk = item % chunks;
   item /= chunks;
-  const int kvh = item % d.n_kv, lz = item / d.n_kv, seq = lz % d.batch;
-  const long pos = call.read_pos[seq];
-  const int end = min(d.capacity, call.ctx_len ? call.ctx_len[seq] : d.capacity);
-  if (keys) read_keys<KWB, F32>(smem, d, blob, call, lz, kvh, chunk, pos, end);
-  else read_values<F32>(smem, d, blob, call, lz, kvh, chunk, pos, end);
+  const int kvh = item % d.n_kv, lc = item / d.n_kv;
+  if (keys) read_keys<KWB, F32>(smem, d, blob, call, lc, kvh, chunk);
+  else read_values<F32>(smem, d, blob, call, lc, kvh, chunk);
 }
 
 }  // namespace
@@ -602,11 +623,12 @@ hipError_t launch_dequantize_rows(const Dims& d, const void* layout, const Cache
   // rows x 8 heads to bf16, one side alone on all CUs: keys 64 us, values 49).  In
   // fp32 (83 and 97) 120 : 136 instead takes 175 us for 188 at 8 heads, but 55 for
   // 42 at 2, where it rounds to one tile more a wave: the same share for both.
-  const long units = static_cast<long>(d.n_kv) * d.n_lc * d.batch;
+  const long units = static_cast<long>(d.n_kv) * d.n_lc;
   const bool both = k_out && v_out;
   long items = 0;
   for (int k = 0; k < 2; ++k) {
-    const long n = k == 0 ? (n_rows + 63l) / 64 : (n_rows + 2l * kTile - 2) / kTile;  // (unaligned rows reach one tile more)
+    call.of_seq[k] = k == 0 ? (n_rows + 63) / 64 : (n_rows + 2 * kTile - 2) / kTile;  // (unaligned rows reach one tile more)
+    const long n = static_cast<long>(d.batch) * call.of_seq[k];
     const long want = std::max(1l, (both ? (k == 0 ? 144 : 112) : 256) / std::max(1l, units));
     call.tiles[k] = static_cast<int>(((n + want - 1) / want + kWaves - 1) / kWaves * kWaves);
     call.chunks[k] = static_cast<int>((n + call.tiles[k] - 1) / call.tiles[k]);

@@ -14,6 +14,7 @@ import pytest
 from oracle import blockgtq_oracle as o
 from paper_2606_24033_amd import blockgtq as bg
 from paper_2606_24033_amd import synth
+from tests import _parity as P
 from tests.test_gpu_cache_readers import D, U, Packed, check, i32
 
 pytestmark = pytest.mark.gpu
@@ -193,9 +194,11 @@ def test_paged_append(rotations, layers, kv, k_budget, v_bits, kind, dtype, page
     k, v = (kvs[:, kv:2 * kv], kvs[:, 2 * kv:]) if strided else (kvs[:, :kv].contiguous(), kvs[:, kv:2 * kv].contiguous())
     bg.blockgtq_paged_append(cfg, pool.layout, layer, k, v, b.chunk, pool.cache)
     after = raw(pool.cache)
-    # each sequence by the append of a cache of its own: what the pages hold of it first, then its new rows (with some
-    # behind them, so that its kernel is the batch's: rows do not depend on one another)
+    # each sequence by the append of a cache of its own: its new rows (with some behind them, so that its kernel is the
+    # batch's: rows do not depend on one another).  Bit for bit, but for bf16 rows of the ordinary widths, whose products
+    # have another order of their sums: there a code may differ where 64 bits put the coordinate next to a threshold
     extra = 0 if small else 5
+    exact = small or dtype == "fp32" or k_budget > 256 or v_bits > 4
     cap = (max(lens) + extra + 63) // 64 * 64
     cfg1 = bg.Config(n_layers=layers, batch=1, n_kv_heads=kv, group=pool.cfg.group, capacity=cap, k_budget=k_budget,
                      v_bits=v_bits, in_dtype=cfg.in_dtype)
@@ -212,17 +215,18 @@ def test_paged_append(rotations, layers, kv, k_budget, v_bits, kind, dtype, page
             touched[b.table[s, i // page], i % page] = True
         at = torch.arange(pos, total, device="cuda")
         pg, pl = torch.from_numpy(b.table[s].astype(np.int64)).cuda()[at // page], at % page
-        assert torch.equal(after[0][layer, pg, :, pl], one.k_codes[layer, 0, :, at].transpose(0, 1)), s
-        assert torch.equal(after[3][layer, pg, :, pl], one.v_norms[layer, 0, :, at].transpose(0, 1)), s
+        for h in range(kv):
+            same_codes(key_codes(after[0][layer, pg, h, pl], pool.bits[layer, h]), key_codes(one.k_codes[layer, 0, h, at], pool.bits[layer, h]),
+                       *rotated_rows(k[rows, h], o.groups(pool.bits[layer, h]), pool.rot_k), exact)
+            same_codes(value_codes(after[2][layer], v_bits)[pg, h, pl], value_codes(one.v_codes[layer], v_bits)[0, h, at],
+                       *rotated_rows(v[rows, h], [(v_bits, list(range(D)))], {D: pool.rot_v}), exact)
+        assert near_radii(after[3][layer, pg, :, pl], one.v_norms[layer, 0, :, at].transpose(0, 1), exact), s
         for h in range(kv):
             S = slots_of(pool, layer, h)
             ng = len(o.groups(pool.bits[layer, h]))
             mine = after[1][layer, :, h, :page * S].view(pages, page, S)[pg, pl]
             other = one.k_norms[layer, 0, h, :cap * S].view(cap, S)[at]
-            assert torch.equal(mine[:, :ng], other[:, :ng]), (s, h)
-        # values: the codes of the rows, bit by bit
-        assert torch.equal(value_codes(after[2][layer], v_bits)[pg, :, pl],
-                           value_codes(one.v_codes[layer], v_bits)[0][:, at].transpose(0, 1)), s
+            assert near_radii(mine[:, :ng], other[:, :ng], exact), (s, h)
     # every other row of the touched pages, every other page and layer as before
     other = torch.from_numpy(~touched).cuda()
     for l2 in range(layers):
@@ -236,6 +240,45 @@ def test_paged_append(rotations, layers, kv, k_budget, v_bits, kind, dtype, page
             a, c = (x[1][l2, :, h, :page * S].view(pages, page, S) for x in (after, before))
             assert torch.equal(a[keep], c[keep])
             assert torch.equal(after[1][l2, :, h, page * S:], before[1][l2, :, h, page * S:])
+
+
+def key_codes(words, bits):
+    """[n, words] key rows as [n, 128] codes in stream order."""
+    w = torch.from_numpy(P.stream_widths(bits)).cuda()
+    at = torch.cumsum(w, 0) - w
+    x = torch.nn.functional.pad(words.to(torch.int64) & 0xFFFFFFFF, (0, 1))
+    return ((x[:, at // 32] | x[:, at // 32 + 1] << 32) >> (at % 32)) & ((1 << w) - 1)
+
+
+def rotated_rows(x, groups, rot):
+    """Rows in units of the codebooks, in stream order and 64 bits, how far fp32 sums may be off, and the widths."""
+    x = x.double()
+    z, off, widths = [], [], []
+    for width, dims in groups:
+        m, y = torch.from_numpy(rot[len(dims)]).double().cuda(), x[:, torch.tensor(dims, device="cuda")]
+        unit = math.sqrt(len(dims)) / y.norm(dim=1, keepdim=True).clamp_min(1e-300)
+        z.append(y @ m.T * unit)
+        # 128 terms in fp32, some in three parts; the radius and the scale 16 u more of the coordinate
+        off.append(2 * (136 * U * (y.abs() @ m.abs().T) * unit + 16 * U * z[-1].abs()))
+        widths += [width] * len(dims)
+    return torch.cat(z, 1), torch.cat(off, 1), torch.tensor(widths, device="cuda")
+
+
+def same_codes(got, ref, z, off, widths, exact):
+    if exact:
+        assert torch.equal(got, ref)
+        return
+    differ = got != ref
+    assert ((got - ref).abs() <= 1).all()
+    for i, p in differ.nonzero().tolist():
+        _, thr = bg.blockgtq_codebook(int(widths[p]))
+        near = float(np.abs(thr.astype(np.float64) - float(z[i, p])).min())
+        assert near <= float(off[i, p]), (i, p, near, float(off[i, p]))
+
+
+def near_radii(a, b, exact):
+    """Equal, or (another order of the sum of squares) neighbouring fp16 numbers."""
+    return torch.equal(a, b) if exact else bool(((a.view(torch.int16).int() - b.view(torch.int16).int()).abs() <= 1).all())
 
 
 def value_codes(words, bits):
@@ -254,7 +297,8 @@ class bare_pool:
         few = Packed(rotations, 31, layers=layers, batch=1, kv=kv, group=group, cap=64, k_budget=k_budget, v_bits=v_bits, kind=kind, dtype=dtype)
         self.cfg = bg.Config(n_layers=layers, batch=pages, n_kv_heads=kv, group=group, capacity=page, k_budget=k_budget,
                              v_bits=v_bits, in_dtype=few.cfg.in_dtype)
-        self.bits, self.layout, self.cache, self.few = few.bits, few.layout, bg.Cache(self.cfg), few
+        self.bits, self.layout, self.cache = few.bits, few.layout, bg.Cache(self.cfg)
+        self.rot_k, self.rot_v = rotations
 
 
 @pytest.mark.parametrize("small", [True, False])
