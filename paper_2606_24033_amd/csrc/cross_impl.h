@@ -415,7 +415,7 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(2, 2))
   int r0, kvh, split, seq0 = 0, lz = 0, layer, sub = 0, seq, nr;  // nr: query rows
   paged::Unit U = {};
   if constexpr (kPaged) {
-    if (!paged::unit_of<kRows>(mode, d, item, U)) return;
+    if (!paged::unit_of<kRows>(mode, d, call.n_slots, item, U)) return;
     r0 = U.r0;
     kvh = U.kvh;
     split = U.split;

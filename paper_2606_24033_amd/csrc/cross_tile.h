@@ -70,7 +70,7 @@ __global__ __launch_bounds__(kAttnThreads) __attribute__((amdgpu_waves_per_eu(2,
   int nr, first, kvh, lz = 0, split, seq, layer;  // query rows of the unit, the workgroup's first one
   paged::Unit U = {};
   if constexpr (kPaged) {
-    if (!paged::unit_of<kWgRows>(mode, d, item, U)) return;
+    if (!paged::unit_of<kWgRows>(mode, d, call.n_slots, item, U)) return;
     nr = U.q.n * G;
     first = U.r0;
     kvh = U.kvh;

@@ -22,6 +22,7 @@
 #include <type_traits>
 #include <utility>
 
+#include "cross_impl.h"
 #include "decode_impl.h"
 #include "kernels.h"
 #include "layout.h"
@@ -36,21 +37,23 @@ using namespace split_detail;
 template <int NSET, int KWB>
 constexpr int waves_of() { return NSET == 1 && KWB <= 16 ? 16 : 12; }
 
-// ---- LDS: the packed decode's tables and query image; before them, while the
-// tables are not yet built, what the query rotation needs
-constexpr int kIn = 0;                                 // [8][128] query rows in stream order
-constexpr int kSum = kIn + 8 * kHeadDim * 4;           // [4][8][128] quarter sums
-constexpr int kRot = kSum + 4 * 8 * kHeadDim * 4;      // [8][128] rotated rows
-static_assert(kRot + 8 * kHeadDim * 4 <= kQimg, "set-up below the query image");
-constexpr int kTop = split_detail::kLdsBytes;          // [8] largest magnitudes, as bits
-constexpr int kLds = kTop + 8 * 4;
-static_assert(kLds <= 160 * 1024, "LDS of one workgroup");
+using cross_detail::half8_t;
+using cross_detail::matrix_parts;
+using cross_detail::split8;
+using cross_detail::staged_product;
+using cross_detail::top16;
+using cross_detail::two_to;
+using cross_detail::up_of;
 
-__device__ __forceinline__ int up_of(uint32_t bits) {  // biased exponent of the power that brings it to [2^13, 2^14)
-  const int e = static_cast<int>(bits >> 23);
-  return e == 0 || e == 255 ? 127 : max(1, min(253, 127 + 13 + 127 - e));
-}
-__device__ __forceinline__ float two_to(int biased) { return __uint_as_float(static_cast<uint32_t>(biased) << 23); }
+// ---- LDS: the packed decode's tables and query image, then per query row its
+// largest rotated magnitude, as bits, and what its staged copy is multiplied with
+constexpr int kTop = split_detail::kLdsBytes;
+constexpr int kBack = kTop + 16 * 4;
+constexpr int kLds = kBack + 16 * 4;
+static_assert(kLds <= 160 * 1024, "LDS of one workgroup");
+// rows staged as fp16 hi and lo parts (cross_impl.h), in the image's place
+// before the rotation, behind the joined states at the end
+static_assert(cross_detail::kHalfPart + 16 * cross_detail::kHalfStride <= kQimgBytes, "staged queries in the image's place");
 
 // Tables of the widths in `used` (bit b - 1): see decode_impl.h.
 template <int THREADS, bool T12>
@@ -132,7 +135,7 @@ __attribute__((amdgpu_waves_per_eu((waves_of<NSET, KWB>() / 4)))) void k_paged_d
   const int bq = lane >> 2, jq = lane & 3;
   const int G = d.group, hq = d.n_kv * G, kw = d.k_words;
   paged::Unit U;
-  if (!paged::unit_of<8>(mode, d, static_cast<int>(blockIdx.x), U)) return;
+  if (!paged::unit_of<8>(mode, d, call.n_slots, static_cast<int>(blockIdx.x), U)) return;
   if (!U.q.ok) {
     if (U.split == 0) paged::refuse(U, d, U.kvh, call.out, call.out_dtype, tid, kThreads);
     return;
@@ -151,10 +154,20 @@ __attribute__((amdgpu_waves_per_eu((waves_of<NSET, KWB>() / 4)))) void k_paged_d
     return;
   }
 
-  // ---- set-up: the query heads in stream order, rotated as k_append_rows
-  // rotates key rows (each of 512 threads a position and a quarter of the
-  // products, its coefficients in flight together), scaled by a power of two
-  // and split into fp16 hi and lo parts; then the lookup tables.
+  // ---- set-up, in few rounds of global reads, those of the first tile among
+  // them: the query heads staged as cross_impl.h does and rotated by three fp16
+  // products (8 of the waves, 16 positions each), written into the image as hi
+  // and lo parts scaled by a power of two; the lookup tables meanwhile.
+  const int stride = kWaves * 64;
+  int t0 = t_begin + wave * 64;
+  int page_next = 0;
+  bool lost = false;  // a page outside the pool: the rows that attend it are not numbers
+  const auto read_page = [&](int t) {
+    page_next = mode.b.pages[static_cast<size_t>(U.seq) * mode.b.max_pages + t / S.capacity];
+  };
+  const auto after = [&](int t) { return t + stride < t_end ? t + stride : t; };
+  if (t0 < t_end) read_page(t0);
+  const uint16_t cv = reinterpret_cast<const uint16_t*>(blob + kOffC16)[min(tid, kCodebookEntries - 1)];
   const int ng = M->n_groups;
   int gdim[kMaxGroups], gpos[kMaxGroups];
   uint32_t used = 1u << (BV - 1);
@@ -165,125 +178,25 @@ __attribute__((amdgpu_waves_per_eu((waves_of<NSET, KWB>() / 4)))) void k_paged_d
     gpos[g] = g < ng ? b : kHeadDim;
     used |= (M->gm[g] >> 31) << g;
   }
+  const int nslot = (ng + 1) & ~1;
   uint16_t* const cbs = reinterpret_cast<uint16_t*>(smem + kCbStage);
-  float* const xin = reinterpret_cast<float*>(smem + kIn);
-  float* const sum = reinterpret_cast<float*>(smem + kSum);
-  float* const rotd = reinterpret_cast<float*>(smem + kRot);
   uint32_t* const top = reinterpret_cast<uint32_t*>(smem + kTop);
-  const int p = tid & 127, qq = (tid >> 7) & 3;
-  int dg = gdim[0], p0 = 0;
+  float* const fix = reinterpret_cast<float*>(smem + kBack);
+  float4_t rk[8];
+  uint4 x0 = make_uint4(0, 0, 0, 0), x1 = x0;
+  const bool bf = d.in_dtype == 1;
+  if (wave < 8) {
+    const float4_t* w = reinterpret_cast<const float4_t*>(blob + layout_kdense_offset(d.n_layers * d.n_kv)) +
+                        static_cast<size_t>(ri) * (kMfmaMatFloats / 4) + wave * 8 * 64 + lane;
 #pragma unroll
-  for (int h = 1; h < kMaxGroups; ++h)
-    if (p >= gpos[h]) {
-      dg = gdim[h];
-      p0 = gpos[h];
-    }
-  float rc[32];
-  {
-    const float* rsrc = reinterpret_cast<const float*>(blob + kOffRotKT) + rotk_index(dg) + (p - p0);
-#pragma unroll
-    for (int u = 0; u < 32; ++u) rc[u] = rsrc[min(32 * qq + u, dg - 1) * dg];
+    for (int s4 = 0; s4 < 8; ++s4) rk[s4] = w[s4 * 64];
   }
-  {
-    const uint16_t cv = reinterpret_cast<const uint16_t*>(blob + kOffC16)[min(tid, kCodebookEntries - 1)];
-    const int src = M->dim[p];
-    for (int i = tid; i < G * kHeadDim; i += kThreads)  // (kThreads is a multiple of 128: i % 128 = p)
-      xin[i] = ld_q(q, (out_row + (i >> 7)) * kHeadDim + src, d.in_dtype);
-    if (tid < kCodebookEntries) cbs[tid] = cv;
-    if (tid < 8) top[tid] = 0;
+  if (tid < G * 16) {  // thread = row tid / 16, dims 8 (tid % 16) .. + 7
+    const size_t at = (out_row + (tid >> 4)) * kHeadDim + 8 * (tid & 15);
+    const uint4* qp = reinterpret_cast<const uint4*>(static_cast<const uint8_t*>(q) + at * (bf ? 2 : 4));
+    x0 = qp[0];
+    if (!bf) x1 = qp[1];
   }
-  __syncthreads();
-  if (tid < 512) {
-#pragma unroll
-    for (int h = 0; h < 4 * NSET; ++h) {
-      if (h >= G) break;
-      float a = 0.f;
-#pragma unroll
-      for (int u = 0; u < 32; ++u)
-        a = 32 * qq + u < dg ? fmaf(rc[u], xin[h * kHeadDim + p0 + 32 * qq + u], a) : a;
-      sum[(qq * 8 + h) * kHeadDim + p] = a;
-    }
-  }
-  __syncthreads();
-  for (int i = tid; i < G * kHeadDim; i += kThreads) {
-    const float* s = sum + i;
-    const float v = ((s[0] + s[8 * kHeadDim]) + (s[16 * kHeadDim] + s[24 * kHeadDim])) *
-                    (kLog2e * rsqrtf(static_cast<float>(dg) * kHeadDim));
-    rotd[i] = v;
-    atomicMax(top + (i >> 7), __float_as_uint(v) & 0x7FFFFFFFu);
-  }
-  __syncthreads();
-  {
-    int sl0[kMaxGroups], nslots = 0;
-#pragma unroll
-    for (int g = 0; g < kMaxGroups; ++g) {
-      sl0[g] = nslots;
-      nslots += ((gdim[g] + 3) / 4 + 15) / 16;
-    }
-    for (int i = tid; i < nslots * NSET * 64; i += kThreads) {
-      const int l = i & 63, set = (i >> 6) % NSET, slot = (i >> 6) / NSET;
-      int gd = gdim[0], gp = 0, s0 = 0;
-#pragma unroll
-      for (int g = 1; g < kMaxGroups; ++g)
-        if (g < ng && slot >= sl0[g]) {
-          gd = gdim[g];
-          gp = gpos[g];
-          s0 = sl0[g];
-        }
-      const int coord = 4 * (16 * (slot - s0) + (l >> 2)), h = 4 * set + (l & 3);
-      const float to = two_to(up_of(top[min(h, 7)]));
-      half4_t hi, lo;
-#pragma unroll
-      for (int k = 0; k < 4; ++k) {
-        const float v = coord + k < gd && h < G ? rotd[h * kHeadDim + gp + coord + k] * to : 0.f;
-        hi[k] = static_cast<_Float16>(v);
-        lo[k] = static_cast<_Float16>(v - static_cast<float>(hi[k]));
-      }
-      uint8_t* dst = smem + kQimg + (((slot * 2 + set) * 2) * 64 + l) * 8;
-      *reinterpret_cast<half4_t*>(dst) = hi;
-      *reinterpret_cast<half4_t*>(dst + 64 * 8) = lo;
-    }
-  }
-  __syncthreads();
-  build_tables<kThreads, T12>(smem, cbs, used, tid);
-  __syncthreads();
-
-  LaneRep rep{static_cast<uint32_t>(kLut1 + (lane & 15) * 8), static_cast<uint32_t>(kLut3 + (lane & 31) * 4),
-              static_cast<uint32_t>(kLut4 + (lane & 7) * 4),   static_cast<uint32_t>(kLut5 + (lane & 31) * 4),
-              static_cast<uint32_t>(kLut2 + (lane & 31) * 8),  static_cast<uint32_t>(kLut1B + (T12 ? 0 : (lane & 7) * 16)),
-              static_cast<uint32_t>(kQimg + lane * 8)};
-  asm volatile("" : "+v"(rep.r1), "+v"(rep.r3), "+v"(rep.r4), "+v"(rep.r5), "+v"(rep.r2), "+v"(rep.r1b));
-
-  // what undoes the scales: head r of each set while lane = token (registers are
-  // heads), uniform; the slopes likewise
-  float back[NSET][4], slope[MODS ? NSET : 1][4];
-#pragma unroll
-  for (int s = 0; s < NSET; ++s)
-#pragma unroll
-    for (int r = 0; r < 4; ++r) {
-      back[s][r] = two_to(254 - up_of(__builtin_amdgcn_readfirstlane(top[4 * s + r])));
-      if constexpr (MODS) slope[s][r] = mode.m.slopes && 4 * s + r < G ? kLog2e * mode.m.slopes[kvh * G + 4 * s + r] : 0.f;
-    }
-
-  float m_run[NSET], l_run[NSET];
-  float4_t O[NSET][2];
-#pragma unroll
-  for (int s = 0; s < NSET; ++s) {
-    m_run[s] = kNegInf;
-    l_run[s] = 0.f;
-    O[s][0] = float4_t{0.f, 0.f, 0.f, 0.f};
-    O[s][1] = float4_t{0.f, 0.f, 0.f, 0.f};
-  }
-  int v_top = 0;  // (see radius_top)
-
-  const int stride = kWaves * 64, nslot = (ng + 1) & ~1;
-  int t0 = t_begin + wave * 64;
-  int page_next = 0;
-  bool lost = false;  // a page outside the pool: the rows that attend it are not numbers
-  const auto read_page = [&](int t) {
-    page_next = mode.b.pages[static_cast<size_t>(U.seq) * mode.b.max_pages + t / S.capacity];
-  };
-  const auto after = [&](int t) { return t + stride < t_end ? t + stride : t; };
   const size_t cap = S.capacity;
   const auto turn_to = [&](RowPtrs& R) {  // the page whose number was read
     lost |= static_cast<uint32_t>(page_next) >= static_cast<uint32_t>(S.batch);
@@ -299,12 +212,131 @@ __attribute__((amdgpu_waves_per_eu((waves_of<NSET, KWB>() / 4)))) void k_paged_d
 #pragma unroll
   for (int i = KWB; i < KWB + kRowPad; ++i) rw[i] = 0u;
   if (t0 < t_end) {
-    read_page(t0);
     turn_to(R2);
     load_keys<KWB>(rw2, knp2, nslot, R2, kw, t0 % S.capacity, lane);
     if constexpr (kValuesAhead) load_values<BV>(vn2, vw2, R2, t0 % S.capacity, lane);
     read_page(after(t0));
   }
+  if (tid < kCodebookEntries) cbs[tid] = cv;
+  if (tid < 16) top[tid] = 0;
+  if (tid < G * 16) {
+    const uint32_t y0[4] = {x0.x, x0.y, x0.z, x0.w}, y1[4] = {x1.x, x1.y, x1.z, x1.w};
+    float x[8];
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+      const uint32_t half = e & 1 ? y0[e >> 1] & 0xFFFF0000u : y0[e >> 1] << 16;
+      x[e] = __uint_as_float(bf ? half : (e < 4 ? y0[e & 3] : y1[e & 3]));
+    }
+    const int up = up_of(top16(x));
+#pragma unroll
+    for (int e = 0; e < 8; ++e) x[e] *= two_to(up);
+    half8_t hi, lo;
+    split8(x, hi, lo);
+    uint8_t* dst = smem + kQimg + (tid >> 4) * cross_detail::kHalfStride + 16 * (tid & 15);
+    *reinterpret_cast<half8_t*>(dst) = hi;
+    *reinterpret_cast<half8_t*>(dst + cross_detail::kHalfPart) = lo;
+    if ((tid & 15) == 0) fix[tid >> 4] = two_to(254 - up) * (1.f / 256.f);
+  }
+  __syncthreads();
+  const int hr = lane & 15, p0 = 16 * (wave & 7) + 4 * (lane >> 4);  // the lane's row and 4 positions
+  float4_t rq[1];
+  uint32_t img_at[2];
+  if (wave < 8) {
+    // (rows from G on are what LDS held: their products are not used)
+    staged_product<1>(smem + kQimg, rk, lane, rq);
+    // place of the lane's position pairs in the image (group sizes are even)
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+      int sl = 0, at = 0, dg = 2, base = 0;
+#pragma unroll
+      for (int g = 0; g < kMaxGroups; ++g) {
+        if (p0 + 2 * h >= gpos[g]) {
+          at = p0 + 2 * h - gpos[g];
+          dg = gdim[g];
+          sl = base;
+        }
+        base += ((gdim[g] + 3) / 4 + 15) / 16;
+      }
+      const int step = at >> 2;
+      img_at[h] = kQimg + ((((sl + (step >> 4)) * 2 + (hr >> 2)) * 2) * 64 + 4 * (step & 15) + (hr & 3)) * 8 + (at & 3) * 2;
+      const float scale = kLog2e * cross_detail::kRsqrtD * rsqrtf(static_cast<float>(dg));
+      rq[0][2 * h] *= scale;
+      rq[0][2 * h + 1] *= scale;
+    }
+    uint32_t mx = 0;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) mx = max(mx, __float_as_uint(rq[0][i]) & 0x7FFFFFFFu);
+    mx = max(mx, static_cast<uint32_t>(__shfl_xor(static_cast<int>(mx), 16)));
+    mx = max(mx, static_cast<uint32_t>(__shfl_xor(static_cast<int>(mx), 32)));
+    if (lane < 16) atomicMax(top + lane, mx);
+  }
+  build_tables<kThreads, T12>(smem, cbs, used, tid);
+  __syncthreads();
+  // (the image takes the staged queries' place)
+  if (wave < 8 && hr < 4 * NSET) {
+    const float to = two_to(up_of(top[hr]));
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+      _Float16 hi[2], lo[2];
+#pragma unroll
+      for (int j = 0; j < 2; ++j) {
+        const float x = hr < G ? rq[0][2 * h + j] * to : 0.f;
+        hi[j] = static_cast<_Float16>(x);
+        lo[j] = static_cast<_Float16>(x - static_cast<float>(hi[j]));
+      }
+      typedef _Float16 half2_t __attribute__((ext_vector_type(2)));
+      *reinterpret_cast<half2_t*>(smem + img_at[h]) = half2_t{hi[0], hi[1]};
+      *reinterpret_cast<half2_t*>(smem + img_at[h] + 64 * 8) = half2_t{lo[0], lo[1]};
+    }
+  } else if (wave == 8 && lane < 8 * kMaxGroups) {
+    // zeros behind a group's end: lane = (group, row)
+    int base = 0, gd = 0, sl = 0;
+#pragma unroll
+    for (int g = 0; g < kMaxGroups; ++g) {
+      if (lane >> 3 == g) {
+        gd = gdim[g];
+        sl = base;
+      }
+      base += ((gdim[g] + 3) / 4 + 15) / 16;
+    }
+    if (gd & 2) {
+      const int step = gd >> 2, r = lane & 7;
+      uint8_t* dst = smem + kQimg + ((((sl + (step >> 4)) * 2 + (r >> 2)) * 2) * 64 + 4 * (step & 15) + (r & 3)) * 8 + 4;
+      *reinterpret_cast<uint32_t*>(dst) = 0;
+      *reinterpret_cast<uint32_t*>(dst + 64 * 8) = 0;
+    }
+  }
+  __syncthreads();
+
+  LaneRep rep{static_cast<uint32_t>(kLut1 + (lane & 15) * 8), static_cast<uint32_t>(kLut3 + (lane & 31) * 4),
+              static_cast<uint32_t>(kLut4 + (lane & 7) * 4),   static_cast<uint32_t>(kLut5 + (lane & 31) * 4),
+              static_cast<uint32_t>(kLut2 + (lane & 31) * 8),  static_cast<uint32_t>(kLut1B + (T12 ? 0 : (lane & 7) * 16)),
+              static_cast<uint32_t>(kQimg + lane * 8)};
+  asm volatile("" : "+v"(rep.r1), "+v"(rep.r3), "+v"(rep.r4), "+v"(rep.r5), "+v"(rep.r2), "+v"(rep.r1b));
+
+  // what undoes the scales: head r of each set while lane = token (registers are
+  // heads), uniform; the slopes likewise
+  float back[NSET][4], slope[MODS ? NSET : 1][4];
+#pragma unroll
+  for (int s = 0; s < NSET; ++s)
+#pragma unroll
+    for (int r = 0; r < 4; ++r) {
+      back[s][r] = two_to(254 - up_of(__builtin_amdgcn_readfirstlane(top[4 * s + r]))) *
+                   (4 * s + r < G ? __uint_as_float(__builtin_amdgcn_readfirstlane(__float_as_uint(fix[4 * s + r]))) : 0.f);
+      if constexpr (MODS) slope[s][r] = mode.m.slopes && 4 * s + r < G ? kLog2e * mode.m.slopes[kvh * G + 4 * s + r] : 0.f;
+    }
+
+  float m_run[NSET], l_run[NSET];
+  float4_t O[NSET][2];
+#pragma unroll
+  for (int s = 0; s < NSET; ++s) {
+    m_run[s] = kNegInf;
+    l_run[s] = 0.f;
+    O[s][0] = float4_t{0.f, 0.f, 0.f, 0.f};
+    O[s][1] = float4_t{0.f, 0.f, 0.f, 0.f};
+  }
+  int v_top = 0;  // (see radius_top)
+
   uint32_t gmb[8];
   for (; t0 < t_end; t0 += stride) {
 #pragma unroll
@@ -445,8 +477,17 @@ __attribute__((amdgpu_waves_per_eu((waves_of<NSET, KWB>() / 4)))) void k_paged_d
   float* const fm = reinterpret_cast<float*>(smem);  // [wave][8] maxima
   float* const fl = fm + kWaves * 8;                 // [wave][8] sums
   float* const fo = fl + kWaves * 8;                 // [wave][8][128] accumulators
-  float* const os = fo + kWaves * 8 * kHeadDim;      // [8][128] the result in the rotated domain
-  static_assert((16 * 8 * 2 + 17 * 8 * kHeadDim) * 4 <= kLds, "join area");
+  constexpr int kEnd = (16 * 8 * 2 + 16 * 8 * kHeadDim) * 4;  // result rows in fp32, then staged
+  float* const os = reinterpret_cast<float*>(smem + kEnd);
+  constexpr int kStaged = kEnd + 8 * kHeadDim * 4;
+  static_assert(kStaged + cross_detail::kHalfPart + 16 * cross_detail::kHalfStride <= kTop, "join area");
+  float4_t rot[8];  // this wave's 16 output dims of Pi_V^T
+  if (call.n_slots == 1 && wave < 8) {
+    const float4_t* src = reinterpret_cast<const float4_t*>(blob + kOffRotVT) +
+                          ((16 * wave + (lane & 15)) * kHeadDim + 32 * (lane >> 4)) / 4;
+#pragma unroll
+    for (int s4 = 0; s4 < 8; ++s4) rot[s4] = src[s4];
+  }
   const float v_back = two_to(127 - radius_up(v_top));
 #pragma unroll
   for (int s = 0; s < NSET; ++s) {
@@ -485,23 +526,28 @@ __attribute__((amdgpu_waves_per_eu((waves_of<NSET, KWB>() / 4)))) void k_paged_d
   }
   if (call.n_slots > 1) return;
   __syncthreads();
-  const float* rotv = reinterpret_cast<const float*>(blob + kOffRotV);
-  for (int i = tid; i < G * kHeadDim; i += kThreads) {
-    const int dd = i & 127;
-    const float* o = os + (i & ~127);
-    float r[4] = {0.f, 0.f, 0.f, 0.f};
-#pragma unroll 4
-    for (int j = 0; j < kHeadDim; j += 4)
+  // out = Pi_V^T (a / l), in three fp16 products of the rows scaled as the queries were
+  if (tid < G * 16) {
+    const float* o = os + (tid >> 4) * kHeadDim + 8 * (tid & 15);
+    float x[8];
 #pragma unroll
-      for (int u = 0; u < 4; ++u) r[u] = fmaf(rotv[(j + u) * kHeadDim + dd], o[j + u], r[u]);
-    const float y = (r[0] + r[1]) + (r[2] + r[3]);
-    const size_t at = out_row * kHeadDim + i;
-    if (call.out_dtype == 1) {
-      const __bf16 b = static_cast<__bf16>(y);
-      static_cast<uint16_t*>(call.out)[at] = __builtin_bit_cast(uint16_t, b);
-    } else {
-      static_cast<float*>(call.out)[at] = y;
-    }
+    for (int e = 0; e < 8; ++e) x[e] = o[e];
+    const int up = up_of(top16(x));
+#pragma unroll
+    for (int e = 0; e < 8; ++e) x[e] *= two_to(up);
+    half8_t hi, lo;
+    split8(x, hi, lo);
+    uint8_t* dst = smem + kStaged + (tid >> 4) * cross_detail::kHalfStride + 16 * (tid & 15);
+    *reinterpret_cast<half8_t*>(dst) = hi;
+    *reinterpret_cast<half8_t*>(dst + cross_detail::kHalfPart) = lo;
+    if ((tid & 15) == 0) fix[tid >> 4] = two_to(254 - up) * (1.f / 256.f);
+  }
+  __syncthreads();
+  if (wave < 8) {
+    float4_t y[1];
+    staged_product<1>(smem + kStaged, rot, lane, y);
+    if (hr < G)
+      cross_detail::store4(call.out, (out_row + hr) * kHeadDim + 16 * wave + 4 * (lane >> 4), y[0] * fix[hr], call.out_dtype);
   }
 }
 

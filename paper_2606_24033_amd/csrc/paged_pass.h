@@ -55,15 +55,15 @@ __device__ __forceinline__ bool find_block(const PagedPass& p, int group, int bl
   return u.seq >= 0;
 }
 
-// Blocks vary fastest, from the last one down: a chunk's late blocks see the
-// most rows.  Then KV heads, then splits.
+// KV heads vary fastest, then splits: the workgroups of a block go to all XCDs,
+// however many blocks there turn out to be.  Blocks from the last one down: a
+// chunk's late ones see the most rows.
 template <int R>
-__device__ __forceinline__ bool unit_of(const PagedPass& p, const Dims& d, int item, Unit& u) {
-  const int block = p.n_blocks - 1 - item % p.n_blocks;
-  item /= p.n_blocks;
+__device__ __forceinline__ bool unit_of(const PagedPass& p, const Dims& d, int n_splits, int item, Unit& u) {
   u.kvh = item % d.n_kv;
-  u.split = item / d.n_kv;
-  return find_block<R>(p, d.group, block, u);
+  item /= d.n_kv;
+  u.split = item % n_splits;
+  return find_block<R>(p, d.group, p.n_blocks - 1 - item / n_splits, u);
 }
 
 // The rows of a sequence that a call cannot answer for are not numbers.

@@ -630,7 +630,9 @@ hipError_t launch_dequantize_rows(const Dims& d, const void* layout, const Cache
     call.of_seq[k] = k == 0 ? (n_rows + 63) / 64 : (n_rows + 2 * kTile - 2) / kTile;  // (unaligned rows reach one tile more)
     const long n = static_cast<long>(d.batch) * call.of_seq[k];
     const long want = std::max(1l, (both ? (k == 0 ? 144 : 112) : 256) / std::max(1l, units));
-    call.tiles[k] = static_cast<int>(((n + want - 1) / want + kWaves - 1) / kWaves * kWaves);
+    // (fewer tiles than waves where there are few: more CUs)
+    const long per = (n + want - 1) / want;
+    call.tiles[k] = static_cast<int>(per < kWaves ? per : (per + kWaves - 1) / kWaves * kWaves);
     call.chunks[k] = static_cast<int>((n + call.tiles[k] - 1) / call.tiles[k]);
     if (call.out[k]) items += units * call.chunks[k];
     if (k == 0) call.key_items = static_cast<int>(items);
