@@ -142,9 +142,24 @@ class Config:
     in_dtype: int = BGTQ_BF16
     head_dim: int = HEAD_DIM
 
+    def __setattr__(self, name, value):
+        self.__dict__.pop("_made", None)
+        object.__setattr__(self, name, value)
+
+    def _make(self):
+        """What the calls need of the fields, made again after one is set: the C struct, and the cache tensors' shapes."""
+        C, lead = self.capacity, (self.n_layers, self.batch, self.n_kv_heads)
+        made = (_Config(self.n_layers, self.batch, self.n_kv_heads, self.group, self.head_dim,
+                        self.capacity, self.k_budget, self.v_bits, self.in_dtype),
+                (lead + (C, self.k_words), lead + (C * MAX_GROUPS,), lead + (C // 32, HEAD_DIM, self.v_bits), lead + (C,)))
+        self.__dict__["_made"] = made
+        return made
+
+    def __getstate__(self):
+        return {k: v for k, v in self.__dict__.items() if k != "_made"}
+
     def c(self):
-        return _Config(self.n_layers, self.batch, self.n_kv_heads, self.group, self.head_dim,
-                       self.capacity, self.k_budget, self.v_bits, self.in_dtype)
+        return (self.__dict__.get("_made") or self._make())[0]
 
     @property
     def n_q_heads(self):
@@ -431,13 +446,14 @@ def _check_shape(what, t, shape, dtype):
 
 def _cache_tensors(cfg: Config, cache: Cache, what="cache"):
     import torch
-    lead = (cfg.n_layers, cfg.batch, cfg.n_kv_heads)
-    C, i32, f16 = cfg.capacity, torch.int32, torch.float16
-    _check_shape(what + ".k_codes", cache.k_codes, lead + (C, cfg.k_words), i32)
-    _check_shape(what + ".k_norms", cache.k_norms, lead + (C * MAX_GROUPS,), f16)
-    _check_shape(what + ".v_codes", cache.v_codes, lead + (C // 32, HEAD_DIM, cfg.v_bits), i32)
-    _check_shape(what + ".v_norms", cache.v_norms, lead + (C,), f16)
-    return cache.k_codes, cache.k_norms, cache.v_codes, cache.v_norms
+    shapes = (cfg.__dict__.get("_made") or cfg._make())[1]
+    t = (cache.k_codes, cache.k_norms, cache.v_codes, cache.v_norms)
+    i32, f16 = torch.int32, torch.float16
+    if not (t[0].shape == shapes[0] and t[1].shape == shapes[1] and t[2].shape == shapes[2] and t[3].shape == shapes[3] and
+            t[0].dtype == t[2].dtype == i32 and t[1].dtype == t[3].dtype == f16):
+        for name, x, shape, dtype in zip(("k_codes", "k_norms", "v_codes", "v_norms"), t, shapes, (i32, f16, i32, f16)):
+            _check_shape(f"{what}.{name}", x, shape, dtype)
+    return t
 
 
 def _check_layout(cfg: Config, layout: Layout):
@@ -460,20 +476,24 @@ def _call(fn, stream, args, *tensors, rows=()):
     `rows`: tensors whose strides the call takes."""
     import torch
     tensors = [t for t in tensors if t is not None]
-    if not all(t.is_contiguous() for t in tensors):
-        raise ValueError("device tensors must be contiguous CUDA tensors")
+    for t in tensors:
+        if not t.is_contiguous():
+            raise ValueError("device tensors must be contiguous CUDA tensors")
     tensors += [t for t in rows if t is not None]
     d = tensors[0].get_device()
     if stream is not None and stream.device_index != d:
         raise ValueError(f"a stream of device {stream.device_index} for tensors on device {d}")
     for t in tensors:
-        if t.get_device() < 0:
+        on = t.get_device()
+        if on < 0:
             raise ValueError("device tensors must be contiguous CUDA tensors")
-        if t.get_device() != d:
+        if on != d:
             raise ValueError("tensors on different devices: " + ", ".join(sorted({str(x.device) for x in tensors})))
-    with torch.cuda.device(d) if torch.cuda.current_device() != d else contextlib.nullcontext():
-        s = torch._C._cuda_getCurrentRawStream(d) if stream is None else stream.cuda_stream
-        _check(fn(*args, s))
+    if torch._C._cuda_getDevice() == d:
+        _check(fn(*args, torch._C._cuda_getCurrentRawStream(d) if stream is None else stream.cuda_stream))
+        return
+    with torch.cuda.device(d):
+        _check(fn(*args, torch._C._cuda_getCurrentRawStream(d) if stream is None else stream.cuda_stream))
 
 
 def _at(t):
@@ -624,10 +644,12 @@ class Rope:
 
 def _token_rows(what, t, n, heads, dtype):
     """The token stride of [n, heads, 128] rows (a view of wider rows, too)."""
-    _check_shape(what, t, (n, heads, HEAD_DIM), dtype)
-    if t.numel() and (t.stride(2) != 1 or (heads > 1 and t.stride(1) != HEAD_DIM)):
+    if t.shape != (n, heads, HEAD_DIM) or t.dtype != dtype:
+        _check_shape(what, t, (n, heads, HEAD_DIM), dtype)
+    by = t.stride()
+    if by[2] != 1 or (by[1] != HEAD_DIM and heads > 1):
         raise ValueError(f"{what}: the heads of a token must lie one after the other")
-    return t.stride(0) if n > 1 else heads * HEAD_DIM
+    return by[0] if n > 1 else heads * HEAD_DIM
 
 
 def blockgtq_norm_rope(cfg: Config, rope: Rope, q, k, pos, q_weight=None, k_weight=None, eps: float = 1e-6, q_out=None,
@@ -646,22 +668,26 @@ def blockgtq_norm_rope(cfg: Config, rope: Rope, q, k, pos, q_weight=None, k_weig
     for name, w in (("q_weight", q_weight), ("k_weight", k_weight)):
         if w is not None:
             _check_shape(name, w, (HEAD_DIM,), torch.float32)
-    given = [t.dtype for t in (q_out, k_out) if t is not None]
-    dtype = given[0] if given else out_dtype or _in_dtype(cfg)
-    if any(t != dtype for t in given) or (out_dtype is not None and out_dtype != dtype):
-        raise ValueError(f"outputs of {given}, out_dtype {out_dtype}: they have one type")
-    with _on(stream):
-        if q is not None and q_out is None:
-            q_out = torch.empty(q.shape, dtype=dtype, device=q.device)
-        if k is not None and k_out is None:
-            k_out = torch.empty(k.shape, dtype=dtype, device=k.device)
-    args = [ctypes.byref(cfg.c()), ctypes.byref(rope.c()), n]
-    for name, t, heads in (("q", q, cfg.n_q_heads), ("k", k, cfg.n_kv_heads)):
-        args += [_at(t), 0 if t is None else _token_rows(name, t, n, heads, _in_dtype(cfg))]
-    args += [pos.data_ptr(), _at(q_weight), _at(k_weight), eps]
-    for name, t, heads in (("q_out", q_out, cfg.n_q_heads), ("k_out", k_out, cfg.n_kv_heads)):
-        args += [_at(t), 0 if t is None else _token_rows(name, t, n, heads, dtype)]
-    _call(lib().blockgtq_norm_rope, stream, (*args, _out_type(dtype)), pos, q_weight, k_weight, rows=(q, k, q_out, k_out))
+    given = k_out if q_out is None else q_out
+    in_dtype = _in_dtype(cfg)
+    dtype = given.dtype if given is not None else out_dtype or in_dtype
+    if out_dtype is not None and out_dtype != dtype:
+        raise ValueError(f"out_dtype {out_dtype}, but the outputs are {dtype}")
+    if (q is not None and q_out is None) or (k is not None and k_out is None):
+        with _on(stream):
+            if q is not None and q_out is None:
+                q_out = torch.empty(q.shape, dtype=dtype, device=q.device)
+            if k is not None and k_out is None:
+                k_out = torch.empty(k.shape, dtype=dtype, device=k.device)
+    hk, qs, ks, qos, kos = cfg.n_kv_heads, 0, 0, 0, 0
+    if q is not None:
+        qs, qos = _token_rows("q", q, n, hk * cfg.group, in_dtype), _token_rows("q_out", q_out, n, hk * cfg.group, dtype)
+    if k is not None:
+        ks, kos = _token_rows("k", k, n, hk, in_dtype), _token_rows("k_out", k_out, n, hk, dtype)
+    _call(lib().blockgtq_norm_rope, stream,
+          (ctypes.byref(cfg.c()), ctypes.byref(rope.c()), n, _at(q), qs, _at(k), ks, pos.data_ptr(), _at(q_weight), _at(k_weight),
+           eps, _at(q_out), qos, _at(k_out), kos, _out_type(dtype)),
+          pos, q_weight, k_weight, rows=(q, k, q_out, k_out))
     return q_out, k_out
 
 

@@ -82,39 +82,6 @@ __global__ __launch_bounds__(1024) void k_append_rows(Dims d, const uint8_t* __r
   const int head = blockIdx.x, lz = blockIdx.y;
   const int layer = d.layer >= 0 ? d.layer : lz / d.batch;
   const int cap = d.capacity;
-  // rows of the call (their first input row, where they go, how many) and the
-  // cache row (layer, sequence or page, head) of each
-  int in0, n_new, wp;
-  bool ok = true;
-  size_t row_of[kRowAppend];
-  if constexpr (kPaged) {
-    const paged::Seq q = paged::seq_of(rows.b, lz);
-    in0 = q.first;
-    wp = q.len - q.n;
-    n_new = q.n;
-    ok = q.ok && q.n <= kRowAppend;  // (the host sends sequences of more rows elsewhere)
-    if (!ok || n_new == 0) return;
-#pragma unroll
-    for (int s = 0; s < kRowAppend; ++s) {
-      const int page = s < n_new ? paged::page_of(rows.b, d.batch, cap, lz, wp + s) : -1;
-      row_of[s] = page < 0 ? ~size_t(0) : (static_cast<size_t>(layer) * d.batch + page) * d.n_kv + head;
-    }
-  } else {
-    n_new = rows.n_new;
-    in0 = lz * n_new;
-    wp = rows.wpos[lz % d.batch];
-#pragma unroll
-    for (int s = 0; s < kRowAppend; ++s)
-      row_of[s] = (static_cast<size_t>(layer) * d.batch + lz % d.batch) * d.n_kv + head;
-  }
-  const auto to = [&](int s) {  // (a select chain: s is no constant)
-    size_t r = row_of[0];
-#pragma unroll
-    for (int u = 1; u < kRowAppend; ++u) r = s == u ? row_of[u] : r;
-    return r;
-  };
-  const auto place = [&](int s) { return kPaged ? (wp + s) % cap : wp + s; };  // the row's place there
-  const auto there = [&](int s) { return !kPaged || to(s) != ~size_t(0); };
   const RowMeta* M = reinterpret_cast<const RowMeta*>(blob + kOffRows) + (layer * d.n_kv + head);
   const float* rotkt = reinterpret_cast<const float*>(blob + kOffRotKT);
   const float* rotvt = reinterpret_cast<const float*>(blob + kOffRotVT);
@@ -130,6 +97,24 @@ __global__ __launch_bounds__(1024) void k_append_rows(Dims d, const uint8_t* __r
     gdim[g] = g < ng ? a : 0;
     gpos[g] = g < ng ? b : kHeadDim;
     gbits[g] = g < ng ? w : 1;
+  }
+
+  // rows of the call (their first input row, where they go, how many) and the
+  // cache row (layer, sequence or page, head) of each
+  int in0, n_new, wp;
+  bool ok = true;
+  size_t row_of[kRowAppend];
+  if constexpr (kPaged) {
+    const paged::Seq q = paged::seq_of(rows.b, lz);
+    in0 = q.first;
+    wp = q.len - q.n;
+    n_new = q.n;
+    ok = q.ok && q.n <= kRowAppend;  // (the host sends sequences of more rows elsewhere)
+    if (!ok || n_new == 0) return;
+  } else {
+    n_new = rows.n_new;
+    in0 = lz * n_new;
+    wp = rows.wpos[lz % d.batch];
   }
   // ---- one round of global reads
   const int p = tid & 127, qq = (tid >> 7) & 3;
@@ -153,6 +138,25 @@ __global__ __launch_bounds__(1024) void k_append_rows(Dims d, const uint8_t* __r
   float rc[32];
 #pragma unroll
   for (int u = 0; u < 32; ++u) rc[u] = rsrc[min(32 * qq + u, rlast) * rstride];
+  if constexpr (kPaged) {
+#pragma unroll
+    for (int s = 0; s < kRowAppend; ++s) {
+      const int page = s < n_new ? paged::page_of(rows.b, d.batch, cap, lz, wp + s) : -1;
+      row_of[s] = page < 0 ? ~size_t(0) : (static_cast<size_t>(layer) * d.batch + page) * d.n_kv + head;
+    }
+  } else {
+#pragma unroll
+    for (int s = 0; s < kRowAppend; ++s)
+      row_of[s] = (static_cast<size_t>(layer) * d.batch + lz % d.batch) * d.n_kv + head;
+  }
+  const auto to = [&](int s) {  // (a select chain: s is no constant)
+    size_t r = row_of[0];
+#pragma unroll
+    for (int u = 1; u < kRowAppend; ++u) r = s == u ? row_of[u] : r;
+    return r;
+  };
+  const auto place = [&](int s) { return kPaged ? (wp + s) % cap : wp + s; };  // the row's place there
+  const auto there = [&](int s) { return !kPaged || to(s) != ~size_t(0); };
   // the other reads take clamped indices (in bounds, surplus values unused)
   // so that they need no branch either
   const size_t xrow = static_cast<size_t>(in0) + min(tid >> 7, n_new - 1);

@@ -90,15 +90,13 @@ __device__ __forceinline__ void rows_product(const uint4_t (*mat)[kMatOps], int 
 
 // ---------------------------------------------------------------- keys
 template <int W>
-__device__ __forceinline__ void quant_keys(LdsKeys<W>& S, int bx, int iters, const Dims& d,
+__device__ __forceinline__ void quant_keys(LdsKeys<W>& S, int bx, int n_wg, const Dims& d,
                                            const uint8_t* __restrict__ blob, const void* __restrict__ kin,
                                            const PagedRows& rows, const CachePtrs& c) {
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int head = blockIdx.y;
   const int cap = d.capacity, n = rows.b.n_tokens;
   constexpr int kThreads = W * 64;
-  const int r_wg = bx * W * kSplitRows * iters;
-  if (r_wg >= n) return;
   const int n_rows_blob = d.n_layers * d.n_kv, ri = d.layer * d.n_kv + head;
   const RowMeta* M = reinterpret_cast<const RowMeta*>(blob + kOffRows) + ri;
   const float* gthr = reinterpret_cast<const float*>(blob + kOffThr);
@@ -139,9 +137,7 @@ __device__ __forceinline__ void quant_keys(LdsKeys<W>& S, int bx, int iters, con
   const float gs[2] = {S.gs[2 * kk], S.gs[2 * kk + 1]};
   const int nslot = (ng + 1) & ~1;
   const auto cache_row = [&](int page) { return (static_cast<size_t>(d.layer) * d.batch + page) * d.n_kv + head; };
-  for (int it = 0; it < iters; ++it) {
-    const int r0 = r_wg + (it * W + wave) * kSplitRows;
-    if (r0 >= n) break;  // wave-uniform
+  for (int r0 = (bx * W + wave) * kSplitRows; r0 < n; r0 += n_wg * W * kSplitRows) {  // (wave-uniform)
     uint4_t x[2][4];
     int2 at[2];
 #pragma unroll
@@ -320,7 +316,7 @@ __device__ __forceinline__ void tile_codes(LdsValues<W>& S, int wave, int lane, 
 }
 
 template <int W, int BV>
-__device__ __forceinline__ void quant_values(LdsValues<W>& S, int bx, int iters, const Dims& d,
+__device__ __forceinline__ void quant_values(LdsValues<W>& S, int bx, int n_wg, long n_tiles, const Dims& d,
                                              const uint8_t* __restrict__ blob, const void* __restrict__ vin,
                                              const PagedRows& rows, const CachePtrs& c) {
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
@@ -331,9 +327,9 @@ __device__ __forceinline__ void quant_values(LdsValues<W>& S, int bx, int iters,
   __syncthreads();
 
   const int tk = lane & 15, kk = lane >> 4;
-  for (int it = 0; it < iters; ++it) {
+  for (int i = bx * W + wave; i < n_tiles; i += n_wg * W) {
     paged::Tile t;
-    if (!paged::tile_of(rows.b, d.batch, cap, bx * W * iters + it * W + wave, t)) continue;  // wave-uniform
+    if (!paged::tile_of(rows.b, d.batch, cap, i, t)) continue;  // wave-uniform
     const size_t row = (static_cast<size_t>(d.layer) * d.batch + t.page) * d.n_kv + head, in_at = t.in0 + t.P0;
     const int P0 = t.P0 % cap;
     uint4_t x[2][4];
@@ -380,12 +376,12 @@ __device__ __forceinline__ void quant_values(LdsValues<W>& S, int bx, int iters,
 template <int W, int BV>
 __global__ __launch_bounds__(W * 64) void k_paged_quantize(Dims d, const uint8_t* __restrict__ blob,
                                                            const void* __restrict__ kin, const void* __restrict__ vin,
-                                                           PagedRows rows, CachePtrs c, int n_kwg, int k_iters, int v_iters) {
+                                                           PagedRows rows, CachePtrs c, int n_kwg, int n_vwg, int n_tiles) {
   constexpr size_t kBytes = sizeof(LdsKeys<W>) > sizeof(LdsValues<W>) ? sizeof(LdsKeys<W>) : sizeof(LdsValues<W>);
   __shared__ __attribute__((aligned(16))) uint8_t smem[kBytes];
   const int bx = static_cast<int>(blockIdx.x);
-  if (bx < n_kwg) quant_keys<W>(*reinterpret_cast<LdsKeys<W>*>(smem), bx, k_iters, d, blob, kin, rows, c);
-  else quant_values<W, BV>(*reinterpret_cast<LdsValues<W>*>(smem), bx - n_kwg, v_iters, d, blob, vin, rows, c);
+  if (bx < n_kwg) quant_keys<W>(*reinterpret_cast<LdsKeys<W>*>(smem), bx, n_kwg, d, blob, kin, rows, c);
+  else quant_values<W, BV>(*reinterpret_cast<LdsValues<W>*>(smem), bx - n_kwg, n_vwg, n_tiles, d, blob, vin, rows, c);
 }
 
 }  // namespace
@@ -395,20 +391,21 @@ bool paged_quantize_fits(const Dims& d) { return d.in_dtype == 1 && d.k_words <=
 hipError_t launch_paged_quantize_bf16(const Dims& d, const void* layout, const void* k, const void* v, const PagedRows& rows,
                                       const CachePtrs& c, hipStream_t s) {
   const long n = rows.b.n_tokens, all = n * d.n_kv, tiles = std::min(n, (n + 62L * rows.b.n_seqs) / kTile);
-  const auto go = [&](auto kern, int w, int k_iters, int v_iters) {
-    const int n_kwg = static_cast<int>((n + w * kSplitRows * k_iters - 1) / (w * kSplitRows * k_iters));
-    const int n_vwg = static_cast<int>((tiles + w * v_iters - 1) / (w * v_iters));
+  // One workgroup runs per CU: 256 of them, half for keys and half for values,
+  // share the rows of all heads, so that each stages its matrix once.
+  const auto go = [&](auto kern, int w) {
+    const long each = std::max(1, 128 / d.n_kv);
+    const int n_kwg = static_cast<int>(std::min(each, (n + w * kSplitRows - 1) / (w * kSplitRows)));
+    const int n_vwg = static_cast<int>(std::min(each, (tiles + w - 1) / w));
     hipLaunchKernelGGL(kern, dim3(n_kwg + n_vwg, d.n_kv), dim3(w * 64), 0, s, d, static_cast<const uint8_t*>(layout), k, v, rows,
-                       c, n_kwg, k_iters, v_iters);
+                       c, n_kwg, n_vwg, static_cast<int>(tiles));
     return hipGetLastError();
   };
   const auto width = [&](auto bv) {
     constexpr int B = decltype(bv)::value;
-    // 4-wave workgroups for calls of up to 64K rows, which then spread over more
-    // CUs; 16-wave ones share the staging of a matrix, above 512K rows for four rounds
-    if (all <= 256L * 256) return go(k_paged_quantize<kWavesShort, B>, kWavesShort, 1, 1);
-    const int iters = all <= 2L * 256 * 512 ? 1 : all <= 4L * 256 * 512 ? 2 : 4;
-    return go(k_paged_quantize<kWavesLong, B>, kWavesLong, iters, iters);
+    // 4-wave workgroups where they take one round, 16-wave ones above
+    if (all <= 128L * kWavesShort * kSplitRows) return go(k_paged_quantize<kWavesShort, B>, kWavesShort);
+    return go(k_paged_quantize<kWavesLong, B>, kWavesLong);
   };
   switch (d.v_bits) {
     case 1: return width(std::integral_constant<int, 1>{});
