@@ -1197,7 +1197,7 @@ int blockgtq_paged_append(const bgtq_config* cfg, const void* d_layout, int32_t 
   if (int e = check_rows("k", d_k, k_stride, cfg->n_kv_heads, cfg->in_dtype)) return e;
   if (int e = check_rows("v", d_v, v_stride, cfg->n_kv_heads, cfg->in_dtype)) return e;
   if (cfg->n_kv_heads > 65535) return fail(BGTQ_EUNSUPPORTED, "%d heads", cfg->n_kv_heads);
-  const PagedRows rows = {paged_batch(chunk), static_cast<size_t>(k_stride), static_cast<size_t>(v_stride)};
+  const PagedRows rows = {paged_batch(chunk), static_cast<size_t>(k_stride), static_cast<size_t>(v_stride), 1};
   hipError_t e = launch_paged_append(dims_of(cfg, layer), d_layout, d_k, d_v, rows, cache_ptrs(cache),
                                      static_cast<hipStream_t>(stream));
   if (e != hipSuccess) return hip_fail(e, "paged_append launch");

@@ -33,25 +33,26 @@ __global__ __launch_bounds__(kThreads) void k_cross_merge(const uint8_t* __restr
   // this wave's 16 output dims of Pi_V^T
   float4_t rot[8];
   half8_t wh[4], wl[4];
-  {
+  const auto matrix = [&]() {
     const float4_t* src = reinterpret_cast<const float4_t*>(blob + kOffRotVT) +
                           ((16 * wave + (lane & 15)) * kHeadDim + 32 * (lane >> 4)) / 4;
 #pragma unroll
     for (int s4 = 0; s4 < 8; ++s4) rot[s4] = src[s4];
-  }
+  };
   const auto parts = [&]() {
 #pragma unroll
     for (int u = 0; u < 4; ++u) matrix_parts(rot, u, wh[u], wl[u]);
   };
-  if (RW == 16) parts();  // (else behind the partials' reads)
-  // A workgroup of 16 rows takes every gridDim.x-th block of them: a wave's part
-  // of the matrix is read once.  (Two staging buffers: one barrier a block.)
-  long block = blockIdx.x;
+  // A workgroup takes every gridDim.x-th block of rows: a wave's part of the
+  // matrix is read once.  (Two staging buffers: one barrier a block.)
   int buf = 0;
-  do {
-    if (!map.begin(block * RW)) {
-      block += gridDim.x;
-      continue;
+  bool ready = false;
+  for (long block = blockIdx.x; block * RW < n_rows; block += RW == 16 ? static_cast<long>(gridDim.x) : n_rows) {
+    if (!map.begin(block * RW)) continue;
+    if (RW != 16 || !ready) {
+      matrix();
+      if (RW == 16) parts();  // (else behind the partials' reads)
+      ready = true;
     }
     uint8_t* const staged = staged2[buf];
     float* const back = back2[buf];
@@ -142,8 +143,7 @@ __global__ __launch_bounds__(kThreads) void k_cross_merge(const uint8_t* __restr
     if (to >= 0)
       store4(out, static_cast<size_t>(to) * kHeadDim + 16 * wave + 4 * (lane >> 4), y[0] * back[ro], out_dtype);
     buf ^= 1;
-    block += gridDim.x;
-  } while (RW == 16 && block * RW < n_rows);
+  }
 }
 
 }  // namespace cross_detail

@@ -43,6 +43,7 @@ struct PagedBatch {
 struct PagedRows {
   PagedBatch b;
   size_t k_stride, v_stride;
+  int per;  // rows of a workgroup of k_append_rows (single tokens)
 };
 hipError_t launch_paged_append(const Dims& d, const void* layout, const void* k, const void* v, const PagedRows& rows,
                                const CachePtrs& c, hipStream_t s);

@@ -8,6 +8,7 @@
 #include <hip/hip_fp16.h>
 #include <hip/hip_runtime.h>
 
+#include <algorithm>
 #include <type_traits>
 
 #include "kernels.h"
@@ -54,8 +55,9 @@ __device__ __forceinline__ int scalar_code(const float* thr, int b, float z) {
 // ---------------------------------------------------------------------------
 constexpr int kRowAppend = 4;
 
-// Rows of a cache: sequence blockIdx.y of the call, at wpos.  (PagedRows: the
-// ragged batch's sequence blockIdx.y; each row has a page of its own.)
+// Rows of a cache: sequence blockIdx.y of the call, at wpos.  (PagedRows: sequence
+// blockIdx.y of the ragged batch or, where each has a single token, input rows
+// per blockIdx.y .. + per - 1, of whatever sequences.)
 struct FixedRows {
   const int32_t* wpos;
   int n_new;
@@ -67,14 +69,14 @@ __global__ __launch_bounds__(1024) void k_append_rows(Dims d, const uint8_t* __r
                                                       const void* __restrict__ vin, ROWS rows, CachePtrs c) {
   constexpr bool kPaged = std::is_same_v<ROWS, PagedRows>;
   __shared__ float xk[kRowAppend][kHeadDim];
-  __shared__ float xv[kRowAppend][kHeadDim];
+  __shared__ __attribute__((aligned(16))) float xv[kRowAppend][kHeadDim];
   __shared__ float pk[kRowAppend][4][kHeadDim];  // quarter sums of the rotated key positions
   __shared__ float pv[kRowAppend][4][kHeadDim];  // and of the rotated value coordinates
   __shared__ float nrm[kRowAppend][kMaxGroups + 1];
   __shared__ float thr[kThresholdEntries];
   __shared__ uint32_t dimw[kHeadDim / 4];        // RowMeta::dim
   __shared__ uint16_t boff[kHeadDim];            // RowMeta::bitoff
-  __shared__ float xs[kRowAppend][kHeadDim];     // key rows in stream order: xs[s][p] = xk[s][dim(p)]
+  __shared__ __attribute__((aligned(16))) float xs[kRowAppend][kHeadDim];     // key rows in stream order: xs[s][p] = xk[s][dim(p)]
   __shared__ uint32_t kwd[kRowAppend][kMaxKWords];  // packed key rows
   __shared__ uint8_t cv[kRowAppend][kHeadDim];
 
@@ -100,18 +102,11 @@ __global__ __launch_bounds__(1024) void k_append_rows(Dims d, const uint8_t* __r
   }
 
   // rows of the call (their first input row, where they go, how many) and the
-  // cache row (layer, sequence or page, head) of each
-  int in0, n_new, wp;
-  bool ok = true;
+  // cache row (layer, sequence or page, head; all ones: none) and place of each
+  int in0, n_new, wp = 0;
   size_t row_of[kRowAppend];
-  if constexpr (kPaged) {
-    const paged::Seq q = paged::seq_of(rows.b, lz);
-    in0 = q.first;
-    wp = q.len - q.n;
-    n_new = q.n;
-    ok = q.ok && q.n <= kRowAppend;  // (the host sends sequences of more rows elsewhere)
-    if (!ok || n_new == 0) return;
-  } else {
+  int place_of[kRowAppend];
+  if constexpr (!kPaged) {
     n_new = rows.n_new;
     in0 = lz * n_new;
     wp = rows.wpos[lz % d.batch];
@@ -139,12 +134,29 @@ __global__ __launch_bounds__(1024) void k_append_rows(Dims d, const uint8_t* __r
 #pragma unroll
   for (int u = 0; u < 32; ++u) rc[u] = rsrc[min(32 * qq + u, rlast) * rstride];
   if constexpr (kPaged) {
+    int2 at;  // of the lane's row
+    if (rows.b.max_new == 1) {
+      in0 = rows.per * blockIdx.y;
+      n_new = min(rows.per, rows.b.n_tokens - in0);
+      at = paged::page_of_row(rows.b, d.batch, cap, in0, lane & 15);
+    } else {
+      // (rows of one sequence: two workgroups would write the same words of a value tile)
+      const paged::Seq q = paged::seq_of(rows.b, blockIdx.y);
+      if (!q.ok || q.n == 0) return;
+      in0 = q.first;
+      n_new = q.n;  // (max_new at most)
+      const int t = q.len - q.n + min(lane & 15, q.n - 1);
+      at = make_int2(paged::page_of(rows.b, d.batch, cap, blockIdx.y, t), t % cap);
+    }
 #pragma unroll
     for (int s = 0; s < kRowAppend; ++s) {
-      const int page = s < n_new ? paged::page_of(rows.b, d.batch, cap, lz, wp + s) : -1;
+      const int page = s < n_new ? __builtin_amdgcn_readlane(at.x, s) : -1;
+      place_of[s] = __builtin_amdgcn_readlane(at.y, s);
       row_of[s] = page < 0 ? ~size_t(0) : (static_cast<size_t>(layer) * d.batch + page) * d.n_kv + head;
     }
   } else {
+#pragma unroll
+    for (int s = 0; s < kRowAppend; ++s) place_of[s] = wp + s;
 #pragma unroll
     for (int s = 0; s < kRowAppend; ++s)
       row_of[s] = (static_cast<size_t>(layer) * d.batch + lz % d.batch) * d.n_kv + head;
@@ -155,7 +167,13 @@ __global__ __launch_bounds__(1024) void k_append_rows(Dims d, const uint8_t* __r
     for (int u = 1; u < kRowAppend; ++u) r = s == u ? row_of[u] : r;
     return r;
   };
-  const auto place = [&](int s) { return kPaged ? (wp + s) % cap : wp + s; };  // the row's place there
+  const auto place = [&](int s) {
+    if constexpr (!kPaged) return wp + s;
+    int t = place_of[0];
+#pragma unroll
+    for (int u = 1; u < kRowAppend; ++u) t = s == u ? place_of[u] : t;
+    return t;
+  };
   const auto there = [&](int s) { return !kPaged || to(s) != ~size_t(0); };
   // the other reads take clamped indices (in bounds, surplus values unused)
   // so that they need no branch either
@@ -179,14 +197,20 @@ __global__ __launch_bounds__(1024) void k_append_rows(Dims d, const uint8_t* __r
   const uint32_t mw = reinterpret_cast<const uint32_t*>(M->dim)[tid & (kHeadDim / 4 - 1)];
   const uint32_t bw = reinterpret_cast<const uint32_t*>(M->bitoff)[tid & (kHeadDim / 2 - 1)];
   // the value words of the first row (value thread j = tid - 512 < 128), read
-  // here so that its read-modify-write costs no extra round trip
+  // here so that its read-modify-write costs no extra round trip; of every row
+  // in pages of their own
   const int bv = d.v_bits;
   const int vj = (tid - 512) & 127;
-  const int wp0 = min(max(place(0), 0), cap - 1);
-  const int vbit0 = (wp0 % kTile) * bv, vw0 = vbit0 >> 5;
-  const size_t r0 = there(0) ? row_of[0] : 0;
-  uint32_t* const vrow0 = c.v_codes + ((r0 * (cap / kTile) + wp0 / kTile) * kHeadDim + vj) * static_cast<size_t>(bv);
-  const uint32_t v0lo = vrow0[vw0], v0hi = vrow0[min(vw0 + 1, bv - 1)];
+  constexpr int kEarly = kPaged ? kRowAppend : 1;
+  uint32_t vlo[kEarly], vhi[kEarly];
+#pragma unroll
+  for (int s = 0; s < kEarly; ++s) {
+    const int t = min(max(place_of[s], 0), cap - 1), w = (t % kTile) * bv >> 5;
+    const size_t r = !kPaged || row_of[s] != ~size_t(0) ? row_of[s] : 0;
+    const uint32_t* src = c.v_codes + ((r * (cap / kTile) + t / kTile) * kHeadDim + vj) * static_cast<size_t>(bv);
+    vlo[s] = src[w];
+    vhi[s] = src[min(w + 1, bv - 1)];
+  }
   if (!kPaged && (wp < 0 || wp >= cap)) return;
   const int nt = kPaged ? n_new : min(n_new, cap - wp);  // rows that fit (the host rejects overflow)
   if (tid < nt * kHeadDim) {
@@ -233,41 +257,44 @@ __global__ __launch_bounds__(1024) void k_append_rows(Dims d, const uint8_t* __r
     float a = 0.f;
     if (kside) {
 #pragma unroll
-      for (int u = 0; u < 32; ++u)
-        if (32 * qq + u < dg) a = fmaf(rc[u], xs[s][p0 + 32 * qq + u], a);
+      for (int u = 0; u < 32; u += 2) {  // (groups start at even positions and have even sizes)
+        const float2 x = *reinterpret_cast<const float2*>(&xs[s][min(p0 + 32 * qq + u, kHeadDim - 2)]);
+        if (32 * qq + u < dg) a = fmaf(rc[u + 1], x.y, fmaf(rc[u], x.x, a));
+      }
       pk[s][qq][p] = a;
     } else {
 #pragma unroll
-      for (int u = 0; u < 32; ++u) a = fmaf(rc[u], xv[s][32 * qq + u], a);
+      for (int u = 0; u < 32; u += 4) {
+        const float4 x = *reinterpret_cast<const float4*>(&xv[s][32 * qq + u]);
+        a = fmaf(rc[u + 3], x.w, fmaf(rc[u + 2], x.z, fmaf(rc[u + 1], x.y, fmaf(rc[u], x.x, a))));
+      }
       pv[s][qq][p] = a;
     }
   }
   __syncthreads();
 
-  // ---- codes (nearest centroid = count of thresholds <= z) and radii
-  if (tid < kHeadDim) {
-    for (int s = 0; s < nt; ++s) {
-      const float z = (pk[s][0][p] + pk[s][1][p]) + (pk[s][2][p] + pk[s][3][p]);
-      const float n = nrm[s][gk];
-      const float scale = n > 0.f ? sqrtf(static_cast<float>(dg)) / n : 0.f;
-      // the code's bits [boff, boff + b) go into the packed row (LDS or)
-      const uint32_t code = static_cast<uint32_t>(scalar_code(thr + thr_index(bk), bk, z * scale));
-      const int bo = boff[p], w = bo >> 5, sh = bo & 31;
-      atomicOr(&kwd[s][w], code << sh);
-      if (sh + bk > 32) atomicOr(&kwd[s][w + 1], code >> (32 - sh));
-      if (p == p0 && there(s))
-        c.k_norms[to(s) * kMaxGroups * cap + static_cast<size_t>(place(s)) * ((ng + 1) & ~1) + gk] =
-            __half_as_ushort(__float2half_rn(n));
-    }
-  } else if (tid < 2 * kHeadDim) {
-    const int bv = d.v_bits;
-    for (int s = 0; s < nt; ++s) {
-      const float z = (pv[s][0][p] + pv[s][1][p]) + (pv[s][2][p] + pv[s][3][p]);
-      const float n = nrm[s][kMaxGroups];
-      const float scale = n > 0.f ? sqrtf(static_cast<float>(kHeadDim)) / n : 0.f;
-      cv[s][p] = static_cast<uint8_t>(scalar_code(thr + thr_index(bv), bv, z * scale));
-      if (p == 0 && there(s)) c.v_norms[to(s) * cap + place(s)] = __half_as_ushort(__float2half_rn(n));
-    }
+  // ---- codes (nearest centroid = count of thresholds <= z) and radii: a thread
+  // to each row and position (keys) or coordinate (values)
+  if (tid < nt * kHeadDim) {
+    const int s = tid >> 7;
+    const float z = (pk[s][0][p] + pk[s][1][p]) + (pk[s][2][p] + pk[s][3][p]);
+    const float n = nrm[s][gk];
+    const float scale = n > 0.f ? sqrtf(static_cast<float>(dg)) / n : 0.f;
+    // the code's bits [boff, boff + b) go into the packed row (LDS or)
+    const uint32_t code = static_cast<uint32_t>(scalar_code(thr + thr_index(bk), bk, z * scale));
+    const int bo = boff[p], w = bo >> 5, sh = bo & 31;
+    atomicOr(&kwd[s][w], code << sh);
+    if (sh + bk > 32) atomicOr(&kwd[s][w + 1], code >> (32 - sh));
+    if (p == p0 && there(s))
+      c.k_norms[to(s) * kMaxGroups * cap + static_cast<size_t>(place(s)) * ((ng + 1) & ~1) + gk] =
+          __half_as_ushort(__float2half_rn(n));
+  } else if (tid >= 512 && tid < 512 + nt * kHeadDim) {
+    const int s = (tid - 512) >> 7;
+    const float z = (pv[s][0][p] + pv[s][1][p]) + (pv[s][2][p] + pv[s][3][p]);
+    const float n = nrm[s][kMaxGroups];
+    const float scale = n > 0.f ? sqrtf(static_cast<float>(kHeadDim)) / n : 0.f;
+    cv[s][p] = static_cast<uint8_t>(scalar_code(thr + thr_index(bv), bv, z * scale));
+    if (p == 0 && there(s)) c.v_norms[to(s) * cap + place(s)] = __half_as_ushort(__float2half_rn(n));
   }
   __syncthreads();
 
@@ -279,18 +306,21 @@ __global__ __launch_bounds__(1024) void k_append_rows(Dims d, const uint8_t* __r
   } else if (tid >= 512 && tid < 512 + kHeadDim) {
     const int j = vj;
     const uint32_t mask = (1u << bv) - 1u;
-    for (int s = 0; s < nt; ++s) {
-      if (!there(s)) continue;
-      const int t = place(s), slot = t % kTile, bit = slot * bv, w = bit >> 5, sh = bit & 31;
-      uint32_t* vw = c.v_codes + ((to(s) * (cap / kTile) + t / kTile) * kHeadDim + j) * static_cast<size_t>(bv);
+#pragma unroll
+    for (int s = 0; s < kRowAppend; ++s) {
+      if (s >= nt || !there(s)) continue;
+      const int t = place_of[s], slot = t % kTile, bit = slot * bv, w = bit >> 5, sh = bit & 31;
+      uint32_t* vw = c.v_codes + ((row_of[s] * (cap / kTile) + t / kTile) * kHeadDim + j) * static_cast<size_t>(bv);
       const uint32_t code = cv[s][j];
-      // row 0 starts from the words read up front; later rows re-read (a row
-      // may share a word with the previous one)
-      const uint32_t lo = s == 0 ? v0lo : vw[w];
+      // a row starts from the words read up front, or re-reads them where the
+      // previous one may have written them
+      bool fresh = s < kEarly;
+      if (kPaged && s > 0) fresh = row_of[s] != row_of[s > 0 ? s - 1 : 0] || t / kTile != place_of[s > 0 ? s - 1 : 0] / kTile;
+      const uint32_t lo = fresh ? vlo[s < kEarly ? s : 0] : vw[w];
       vw[w] = (lo & ~(mask << sh)) | (code << sh);
       if (sh + bv > 32) {
         const int hi = sh + bv - 32;  // bits of the code in the next word
-        const uint32_t up = s == 0 ? v0hi : vw[w + 1];
+        const uint32_t up = fresh ? vhi[s < kEarly ? s : 0] : vw[w + 1];
         vw[w + 1] = (up & ~((1u << hi) - 1u)) | (code >> (bv - hi));
       }
     }
@@ -318,8 +348,12 @@ hipError_t launch_paged_append(const Dims& d, const void* layout, const void* k,
     return paged_quantize_fits(d) ? launch_paged_quantize_bf16(d, layout, k, v, rows, c, s)
                                   : launch_paged_quantize(d, layout, k, v, rows, c, s);
   const auto kern = d.in_dtype == 1 ? k_append_rows<true, PagedRows> : k_append_rows<false, PagedRows>;
-  hipLaunchKernelGGL(kern, dim3(d.n_kv, rows.b.n_seqs), dim3(1024), 0, s, d, static_cast<const uint8_t*>(layout), k, v,
-                     rows, c);
+  // Each workgroup reads 128 KB of rotations, each row of one costs about 2 us:
+  // as many rows as keep the workgroups below the CUs' number.
+  PagedRows r = rows;
+  r.per = static_cast<int>(std::min<long>(kRowAppend, (static_cast<long>(rows.b.n_tokens) * d.n_kv + 159) / 160));
+  const int n = rows.b.max_new == 1 ? (rows.b.n_tokens + r.per - 1) / r.per : rows.b.n_seqs;
+  hipLaunchKernelGGL(kern, dim3(d.n_kv, n), dim3(1024), 0, s, d, static_cast<const uint8_t*>(layout), k, v, r, c);
   return hipGetLastError();
 }
 

@@ -55,50 +55,63 @@ static_assert(kLds <= 160 * 1024, "LDS of one workgroup");
 // before the rotation, behind the joined states at the end
 static_assert(cross_detail::kHalfPart + 16 * cross_detail::kHalfStride <= kQimgBytes, "staged queries in the image's place");
 
-// Tables of the widths in `used` (bit b - 1): see decode_impl.h.
+// Tables of the widths in `used` (bit b - 1): see decode_impl.h.  A thread works
+// out all its entries of a table before it writes one (the codebooks that it
+// reads and the tables lie in the same LDS: the compiler would wait for each).
+template <int THREADS, int N, class T, class F>
+__device__ __forceinline__ void fill_table(uint8_t* dst, int tid, const F& entry) {
+  constexpr int kPer = (N + THREADS - 1) / THREADS;
+  T v[kPer];
+#pragma unroll
+  for (int k = 0; k < kPer; ++k) v[k] = entry(min(tid + k * THREADS, N - 1));
+#pragma unroll
+  for (int k = 0; k < kPer; ++k)
+    if (N % THREADS == 0 || tid + k * THREADS < N) reinterpret_cast<T*>(dst)[tid + k * THREADS] = v[k];
+}
 template <int THREADS, bool T12>
 __device__ __forceinline__ void build_tables(uint8_t* smem, const uint16_t* cbs, uint32_t used, int tid) {
   const auto pair = [](const uint16_t* cb, int i, int b) {
     const int m = (1 << b) - 1;
     return cb[i & m] | static_cast<uint32_t>(cb[(i >> b) & m]) << 16;
   };
-  if (used & 1u) {
-    for (int i = tid; i < 16 * 16; i += THREADS)
-      *reinterpret_cast<uint2*>(smem + kLut1 + i * 8) =
-          make_uint2(pair(cbs + cb_index(1), i >> 4, 1), pair(cbs + cb_index(1), i >> 6, 1));
-    if constexpr (!T12)
-      for (int i = tid; i < 256 * 8; i += THREADS) {
-        const int e = i >> 3;
-        const uint16_t* cb = cbs + cb_index(1);
-        *reinterpret_cast<uint4*>(smem + kLut1B + i * 16) =
-            make_uint4(pair(cb, e, 1), pair(cb, e >> 2, 1), pair(cb, e >> 4, 1), pair(cb, e >> 6, 1));
-      }
-  }
+  // two codes of 1 or 2 bits: bytes of the codebook's words
+  const uint32_t c1 = *reinterpret_cast<const uint32_t*>(cbs + cb_index(1));
+  const uint32_t c2a = *reinterpret_cast<const uint32_t*>(cbs + cb_index(2)), c2b = *reinterpret_cast<const uint32_t*>(cbs + cb_index(2) + 2);
+  const auto pair1 = [&](int i) {
+    return __builtin_amdgcn_perm(0u, c1, 0x01000100u + 0x0202u * (i & 1) + 0x02020000u * ((i >> 1) & 1));
+  };
+  const auto pair2 = [&](int i) {
+    return __builtin_amdgcn_perm(c2b, c2a, 0x01000100u + 0x0202u * (i & 3) + 0x02020000u * ((i >> 2) & 3));
+  };
   if (used & 2u)  // 16 lanes write an entry's 32 replicas
-    for (int i = tid; i < 256 * 16; i += THREADS) {
-      const uint32_t lo = pair(cbs + cb_index(2), i >> 4, 2), hi = pair(cbs + cb_index(2), i >> 8, 2);
-      *reinterpret_cast<uint4*>(smem + kLut2 + i * 16) = make_uint4(lo, hi, lo, hi);
-    }
+    fill_table<THREADS, 256 * 16, uint4>(smem + kLut2, tid, [&](int i) {
+      const uint32_t lo = pair2(i >> 4), hi = pair2(i >> 8);
+      return make_uint4(lo, hi, lo, hi);
+    });
+  if (used & 1u) {
+    fill_table<THREADS, 16 * 16, uint2>(smem + kLut1, tid, [&](int i) { return make_uint2(pair1(i >> 4), pair1(i >> 6)); });
+    if constexpr (!T12)
+      fill_table<THREADS, 256 * 8, uint4>(smem + kLut1B, tid, [&](int i) {
+        const int e = i >> 3;
+        return make_uint4(pair1(e), pair1(e >> 2), pair1(e >> 4), pair1(e >> 6));
+      });
+  }
   if (used & 4u) {
+    const uint16_t* cb = cbs + cb_index(3);
     if constexpr (T12)
-      for (int i = tid; i < 4096; i += THREADS)
-        *reinterpret_cast<uint2*>(smem + kLut1B + i * 8) =
-            make_uint2(pair(cbs + cb_index(3), i, 3), pair(cbs + cb_index(3), i >> 6, 3));
+      fill_table<THREADS, 4096, uint2>(smem + kLut1B, tid, [&](int i) { return make_uint2(pair(cb, i, 3), pair(cb, i >> 6, 3)); });
     else
-      for (int i = tid; i < 64 * 32; i += THREADS)
-        *reinterpret_cast<uint32_t*>(smem + kLut3 + i * 4) = pair(cbs + cb_index(3), i >> 5, 3);
+      fill_table<THREADS, 64 * 32, uint32_t>(smem + kLut3, tid, [&](int i) { return pair(cb, i >> 5, 3); });
   }
   if (used & 8u)
-    for (int i = tid; i < 256 * 8; i += THREADS)
-      *reinterpret_cast<uint32_t*>(smem + kLut4 + i * 4) = pair(cbs + cb_index(4), i >> 3, 4);
+    fill_table<THREADS, 256 * 8, uint32_t>(smem + kLut4, tid, [&](int i) { return pair(cbs + cb_index(4), i >> 3, 4); });
   if (used & 16u)
-    for (int i = tid; i < 32 * 32; i += THREADS)
-      *reinterpret_cast<uint32_t*>(smem + kLut5 + i * 4) = cbs[cb_index(5) + (i >> 5)];
+    fill_table<THREADS, 32 * 32, uint32_t>(smem + kLut5, tid, [&](int i) { return static_cast<uint32_t>(cbs[cb_index(5) + (i >> 5)]); });
   if (used & 0xE0u)
-    for (int i = tid; i < 256 + 128 + 64; i += THREADS) {
+    fill_table<THREADS, 256 + 128 + 64, uint16_t>(smem + kLutF, tid, [&](int i) {
       const int b = i < 256 ? 8 : (i < 384 ? 7 : 6), k = i < 256 ? i : (i < 384 ? i - 256 : i - 384);
-      *reinterpret_cast<uint16_t*>(smem + kLutF + i * 2) = cbs[cb_index(b) + k];
-    }
+      return cbs[cb_index(b) + k];
+    });
 }
 
 // PV with weights in two parts, each decoded operand used for both.
@@ -135,14 +148,34 @@ __attribute__((amdgpu_waves_per_eu((waves_of<NSET, KWB>() / 4)))) void k_paged_d
   const int bq = lane >> 2, jq = lane & 3;
   const int G = d.group, hq = d.n_kv * G, kw = d.k_words;
   paged::Unit U;
-  if (!paged::unit_of<8>(mode, d, call.n_slots, static_cast<int>(blockIdx.x), U)) return;
+  const int block = paged::unit_at(mode, d, call.n_slots, static_cast<int>(blockIdx.x), U);
+  const RowMeta* M = reinterpret_cast<const RowMeta*>(blob + kOffRows) + (d.layer * d.n_kv + U.kvh);
+  // the reads that need no sequence, before its numbers are there
+  const uint16_t cv = reinterpret_cast<const uint16_t*>(blob + kOffC16)[min(tid, kCodebookEntries - 1)];
+  float4_t rk[8];
+  if (wave < 8) {
+    const float4_t* w = reinterpret_cast<const float4_t*>(blob + layout_kdense_offset(d.n_layers * d.n_kv)) +
+                        static_cast<size_t>(d.layer * d.n_kv + U.kvh) * (kMfmaMatFloats / 4) + wave * 8 * 64 + lane;
+#pragma unroll
+    for (int s4 = 0; s4 < 8; ++s4) rk[s4] = w[s4 * 64];
+  }
+  const int ng = M->n_groups;
+  int gdim[kMaxGroups], gpos[kMaxGroups];
+  uint32_t used = 1u << (BV - 1);
+#pragma unroll
+  for (int g = 0; g < kMaxGroups; ++g) {
+    const int a = M->g_dim[g], b = M->g_pos[g];
+    gdim[g] = g < ng ? a : 0;
+    gpos[g] = g < ng ? b : kHeadDim;
+    used |= (M->gm[g] >> 31) << g;
+  }
+  if (!paged::find_block<8>(mode, G, block, U)) return;
   if (!U.q.ok) {
     if (U.split == 0) paged::refuse(U, d, U.kvh, call.out, call.out_dtype, tid, kThreads);
     return;
   }
-  const int kvh = U.kvh, split = U.split, ri = d.layer * d.n_kv + kvh;
+  const int kvh = U.kvh, split = U.split;
   const size_t out_row = static_cast<size_t>(U.q.first) * hq + kvh * G;  // head 0's row of q and out
-  const RowMeta* M = reinterpret_cast<const RowMeta*>(blob + kOffRows) + ri;
   const int t_begin = split * S.split_len, t_end = min(U.q.len, t_begin + S.split_len), pos = U.q.len - 1;
   float* const part = call.part + ((static_cast<size_t>(U.block) * d.n_kv + kvh) * mode.unit_rows * call.n_slots + split) * kPartFloats;
   const size_t part_step = static_cast<size_t>(call.n_slots) * kPartFloats;  // from a head's partial to the next one's
@@ -167,30 +200,12 @@ __attribute__((amdgpu_waves_per_eu((waves_of<NSET, KWB>() / 4)))) void k_paged_d
   };
   const auto after = [&](int t) { return t + stride < t_end ? t + stride : t; };
   if (t0 < t_end) read_page(t0);
-  const uint16_t cv = reinterpret_cast<const uint16_t*>(blob + kOffC16)[min(tid, kCodebookEntries - 1)];
-  const int ng = M->n_groups;
-  int gdim[kMaxGroups], gpos[kMaxGroups];
-  uint32_t used = 1u << (BV - 1);
-#pragma unroll
-  for (int g = 0; g < kMaxGroups; ++g) {
-    const int a = M->g_dim[g], b = M->g_pos[g];
-    gdim[g] = g < ng ? a : 0;
-    gpos[g] = g < ng ? b : kHeadDim;
-    used |= (M->gm[g] >> 31) << g;
-  }
   const int nslot = (ng + 1) & ~1;
   uint16_t* const cbs = reinterpret_cast<uint16_t*>(smem + kCbStage);
   uint32_t* const top = reinterpret_cast<uint32_t*>(smem + kTop);
   float* const fix = reinterpret_cast<float*>(smem + kBack);
-  float4_t rk[8];
   uint4 x0 = make_uint4(0, 0, 0, 0), x1 = x0;
   const bool bf = d.in_dtype == 1;
-  if (wave < 8) {
-    const float4_t* w = reinterpret_cast<const float4_t*>(blob + layout_kdense_offset(d.n_layers * d.n_kv)) +
-                        static_cast<size_t>(ri) * (kMfmaMatFloats / 4) + wave * 8 * 64 + lane;
-#pragma unroll
-    for (int s4 = 0; s4 < 8; ++s4) rk[s4] = w[s4 * 64];
-  }
   if (tid < G * 16) {  // thread = row tid / 16, dims 8 (tid % 16) .. + 7
     const size_t at = (out_row + (tid >> 4)) * kHeadDim + 8 * (tid & 15);
     const uint4* qp = reinterpret_cast<const uint4*>(static_cast<const uint8_t*>(q) + at * (bf ? 2 : 4));

@@ -58,12 +58,15 @@ __device__ __forceinline__ bool find_block(const PagedPass& p, int group, int bl
 // KV heads vary fastest, then splits: the workgroups of a block go to all XCDs,
 // however many blocks there turn out to be.  Blocks from the last one down: a
 // chunk's late ones see the most rows.
-template <int R>
-__device__ __forceinline__ bool unit_of(const PagedPass& p, const Dims& d, int n_splits, int item, Unit& u) {
+__device__ __forceinline__ int unit_at(const PagedPass& p, const Dims& d, int n_splits, int item, Unit& u) {  // the block
   u.kvh = item % d.n_kv;
   item /= d.n_kv;
   u.split = item % n_splits;
-  return find_block<R>(p, d.group, p.n_blocks - 1 - item / n_splits, u);
+  return p.n_blocks - 1 - item / n_splits;
+}
+template <int R>
+__device__ __forceinline__ bool unit_of(const PagedPass& p, const Dims& d, int n_splits, int item, Unit& u) {
+  return find_block<R>(p, d.group, unit_at(p, d, n_splits, item, u), u);
 }
 
 // The rows of a sequence that a call cannot answer for are not numbers.

@@ -171,6 +171,8 @@ def slots_of(pool, layer, h):
     (1, 1, 128, 2, "mixed", "bf16", 64, [1], [1], 0, False),
     (2, 2, 192, 3, "wide", "fp32", 64, [1, 1, 1, 1], [65, 64, 100, 1], 0, True),     # the decode step's kernel
     (1, 2, 192, 5, "wide", "bf16", 64, [4, 1, 0, 3, 2], [66, 64, 70, 194, 130], 2, True),  # over page ends, none, padded
+    (1, 2, 192, 3, "wide", "bf16", 64, [2, 4, 3, 4, 1, 4, 2], [34, 33, 64, 68, 40, 96, 2], 1, False),  # words that neighbours share
+    (1, 2, 128, 2, "mixed", "bf16", 64, [1] * 9 + [0] * 70 + [1] * 13, None, 0, True),  # four tokens a workgroup
     (1, 2, 128, 2, "mixed", "bf16", 64, [5, 0, 1, 70, 64], [5, 10, 64, 150, 64], 0, False),
     (2, 3, 192, 3, "wide", "fp32", 128, [200, 33, 1], [301, 65, 129], 7, True),
     (1, 1, 512, 8, "uniform", "bf16", 192, [100, 31, 1, 1], [250, 31, 193, 33], 0, True),
