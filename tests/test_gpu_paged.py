@@ -362,8 +362,9 @@ def attend(q, k, v, see, pos, bits, rot_k, rot_v, out_dtype, cap=0.0, slope=None
     x = cap * np.tanh(x0 / cap) if cap else x0
     bias = np.zeros(x.shape) if slope is None else -slope[:, None] * np.abs(pos[:, None] - np.arange(len(k)))
     dcap = 0.0
-    if cap:  # t, 1 - t, 1 + t, the quotient: 8 u of 1; the product and what enters: 2 u more.  fp32: the sum for small
-        # ones, relative to them; the others are at least a third of the cap
+    if cap:  # bf16: t, 1 - t, 1 + t, the quotient: 8 u of the cap; the product and what enters: 2 u more.  fp32, relative:
+        # z 4 u (at most its own share of either polynomial), four steps of each, the quotient and two products; where
+        # the argument is cut off, 1.5e-7
         dcap = 10 * U * cap if out_dtype == torch.bfloat16 else 30 * U * np.abs(x)
     x = np.where(see, x + bias, -np.inf)
     top = x.max(1, keepdims=True)
