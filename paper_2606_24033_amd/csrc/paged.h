@@ -70,8 +70,9 @@ __device__ __forceinline__ int find_item(const PagedBatch& b, int want, const F&
 }
 
 // Page (-1: none) and place of input row r0 + tk of a ragged batch, r0 the same
-// in the wave, tk < 16.  The sequence of r0 by a search 64 sequences at a time,
+// in the wave, tk < ROWS.  The sequence of r0 by a search 64 sequences at a time,
 // the rows' own by one ballot each over the 64 sequences from there on.
+template <int ROWS = 16>
 __device__ __forceinline__ int2 page_of_row(const PagedBatch& b, int n_pages, int page_rows, int r0, int tk) {
   const int lane = threadIdx.x & 63, last = b.n_seqs - 1;
   int s0 = last;
@@ -85,7 +86,7 @@ __device__ __forceinline__ int2 page_of_row(const PagedBatch& b, int n_pages, in
   const int end = s0 + lane <= last ? b.cu[min(s0 + lane, last) + 1] : 0x7FFFFFFF;
   int s = s0;
 #pragma unroll
-  for (int j = 0; j < 16; ++j) {
+  for (int j = 0; j < ROWS; ++j) {
     const int n = __builtin_popcountll(__builtin_amdgcn_ballot_w64(end <= r0 + j));
     s = tk == j ? s0 + n : s;
   }

@@ -12,7 +12,8 @@
 // accumulator registers, so four waves fit a SIMD.  Codes by counting: up to
 // three (width <= 2) or seven (width 3) comparisons against thresholds held per
 // position, a branch-free search only for tiles that hold wider codes.  The
-// group radii stay on fp32 MFMAs (squares of bf16 numbers do not fit bf16).
+// square of a bf16 number is the sum of two: the group radii take two bf16
+// products of the rows' squares with the groups' members, exact terms as well.
 #include <hip/hip_fp16.h>
 #include <hip/hip_runtime.h>
 
@@ -29,37 +30,47 @@ namespace {
 using namespace split;
 
 constexpr int kSplitKWords = 16, kSplitVBits = 4;
+constexpr int kWaves = 16;
 
-template <int W>
 struct LdsKeys {
-  uint4_t wa[3][kMatOps];                     // W's three parts, A operand order
-  float4 ma[8 * 64];                          // group membership, fp32 A operand order
-  float4 ta[kHeadDim], tb[kHeadDim];          // first seven thresholds of each position, NaN past its last
-  uint32_t rw[W][kSplitRows * kSplitKWords];  // per wave: packed key rows, k_words apart
-  float sc[W][kSplitRows][kMaxGroups];        // per wave: sqrt(d_g) / radius
-  uint32_t pm[kHeadDim];                      // bit offset | b << 10 | group << 14
+  uint4_t wa[3][kMatOps];                          // W's three parts, A operand order
+  uint4_t ma[4 * 64];                              // group membership, A operand order
+  float4 ta[kHeadDim], tb[kHeadDim];               // first seven thresholds of each position, NaN past its last
+  uint32_t rw[kWaves][kSplitRows * kSplitKWords];  // per wave: packed key rows, k_words apart
+  float sc[kWaves][kSplitRows][kMaxGroups];        // per wave: sqrt(d_g) / radius
+  uint32_t pm[kHeadDim];                           // bit offset | b << 10 | group << 14
   float thr[kThresholdEntries];
   float gs[kMaxGroups];
-  int mw[8];                                  // largest width in each tile of 16 positions
+  int mw[8];                                       // largest width in each tile of 16 positions
   uint8_t gd[kHeadDim];
 };
-template <int W>
 struct LdsValues {
-  uint4_t rb[3][kMatOps];                     // Pi_V's three parts, B operand order
-  uint32_t vt[W][kHeadDim * kSplitVBits];     // per wave: words of one value tile
-  float nv[W][kSplitRows];
+  uint4_t rb[3][kMatOps];                       // Pi_V's three parts, B operand order
+  uint32_t vt[kWaves][kHeadDim * kSplitVBits];  // per wave: words of one value tile
+  float nv[kWaves][kSplitRows];
   float thr[kThresholdEntries];
 };
-constexpr int kWavesLong = 16, kWavesShort = 4;
-static_assert(sizeof(LdsKeys<kWavesLong>) <= 160 * 1024 && sizeof(LdsValues<kWavesLong>) <= 160 * 1024, "LDS");
+static_assert(sizeof(LdsKeys) <= 160 * 1024 && sizeof(LdsValues) <= 160 * 1024, "LDS");
 
 __device__ __forceinline__ void wave_sync() {  // (LDS operations of one wave complete in order)
   __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
   __builtin_amdgcn_wave_barrier();
 }
 
-__device__ __forceinline__ float4_t mfma(float a, float b, float4_t c) {
-  return __builtin_amdgcn_mfma_f32_16x16x4f32(a, b, c, 0, 0, 0);
+// The squares of an operand's 8 numbers, in two parts: what their upper 16 bits
+// leave of the product of two 8-bit significands has 8 bits again.
+__device__ __forceinline__ void square_parts(const uint4_t& x, uint4_t& hi, uint4_t& lo) {
+#pragma unroll
+  for (int j = 0; j < 4; ++j) {
+    float a = __uint_as_float(x[j] << 16), b = __uint_as_float(x[j] & 0xFFFF0000u);
+    a *= a;
+    b *= b;
+    const uint32_t ah = __float_as_uint(a) & 0xFFFF0000u, bh = __float_as_uint(b) & 0xFFFF0000u;
+    a -= __uint_as_float(ah);
+    b -= __uint_as_float(bh);
+    hi[j] = bh | ah >> 16;
+    lo[j] = __builtin_amdgcn_perm(__float_as_uint(b), __float_as_uint(a), 0x07060302u);
+  }
 }
 
 // Element i of the 32 that four operands hold.
@@ -89,20 +100,19 @@ __device__ __forceinline__ void rows_product(const uint4_t (*mat)[kMatOps], int 
 }
 
 // ---------------------------------------------------------------- keys
-template <int W>
-__device__ __forceinline__ void quant_keys(LdsKeys<W>& S, int bx, int n_wg, const Dims& d,
+__device__ __forceinline__ void quant_keys(LdsKeys& S, int bx, int n_wg, const Dims& d,
                                            const uint8_t* __restrict__ blob, const void* __restrict__ kin,
                                            const PagedRows& rows, const CachePtrs& c) {
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int head = blockIdx.y;
   const int cap = d.capacity, n = rows.b.n_tokens;
-  constexpr int kThreads = W * 64;
+  constexpr int kThreads = kWaves * 64;
   const int n_rows_blob = d.n_layers * d.n_kv, ri = d.layer * d.n_kv + head;
   const RowMeta* M = reinterpret_cast<const RowMeta*>(blob + kOffRows) + ri;
   const float* gthr = reinterpret_cast<const float*>(blob + kOffThr);
   const int ng = M->n_groups, kw = d.k_words;
 
-  for (int i = tid; i < W * kSplitRows * kSplitKWords; i += kThreads) (&S.rw[0][0])[i] = 0u;
+  for (int i = tid; i < kWaves * kSplitRows * kSplitKWords; i += kThreads) (&S.rw[0][0])[i] = 0u;
   for (int i = tid; i < kThresholdEntries; i += kThreads) S.thr[i] = gthr[i];
   if (tid < kHeadDim) {
     const int g = M->grp[tid], b = M->width[tid], nt = (1 << b) - 1;
@@ -120,50 +130,55 @@ __device__ __forceinline__ void quant_keys(LdsKeys<W>& S, int bx, int n_wg, cons
     for (int j = 0; j < 16; ++j) w = max(w, static_cast<int>(M->width[16 * tid + j]));
     S.mw[tid] = w;
   }
-  stage_split<W>(S.wa, reinterpret_cast<const float4*>(blob + layout_kdense_offset(n_rows_blob)) + static_cast<size_t>(ri) * kMatF4,
-                 tid);
-  __syncthreads();
-  for (int i = tid; i < 8 * 64; i += kThreads) {
-    // row 4 m + e of the product is group 2 m + e (e < 2): two groups to each
-    // quarter of the wave instead of four to two of them
-    const int s4 = i >> 6, l = i & 63, d0 = 32 * (l >> 4) + 4 * s4;
-    const int g = (l & 3) < 2 ? 2 * ((l >> 2) & 3) + (l & 3) : -1;
-    S.ma[i] = make_float4(S.gd[d0] == g ? 1.f : 0.f, S.gd[d0 + 1] == g ? 1.f : 0.f, S.gd[d0 + 2] == g ? 1.f : 0.f,
-                          S.gd[d0 + 3] == g ? 1.f : 0.f);
-  }
-  __syncthreads();
-
+  // A wave's next rows: read before the staging ends, and before the last
+  // rows' codes are written.
   const int tk = lane & 15, kk = lane >> 4;
-  const float gs[2] = {S.gs[2 * kk], S.gs[2 * kk + 1]};
-  const int nslot = (ng + 1) & ~1;
-  const auto cache_row = [&](int page) { return (static_cast<size_t>(d.layer) * d.batch + page) * d.n_kv + head; };
-  for (int r0 = (bx * W + wave) * kSplitRows; r0 < n; r0 += n_wg * W * kSplitRows) {  // (wave-uniform)
-    uint4_t x[2][4];
-    int2 at[2];
+  uint4_t x[2][4];
+  int2 at = make_int2(-1, 0);  // page and place of row lane % 32
+  const auto load_rows = [&](int r0) {
 #pragma unroll
     for (int s = 0; s < 2; ++s) {
       const int r = r0 + kSub * s + tk;
       load_operands(kin, min(r, n - 1) * rows.k_stride + head * kHeadDim + 32 * kk, r < n, x[s]);
     }
+    at = paged::page_of_row<kSplitRows>(rows.b, d.batch, cap, r0, lane & 31);
+    if (r0 + (lane & 31) >= n) at.x = -1;
+  };
+  // (the last waves of all workgroups are those that have a block less)
+  int r0 = (wave * n_wg + bx) * kSplitRows;
+  if (r0 < n) load_rows(r0);
+  stage_split<kWaves>(
+      S.wa, reinterpret_cast<const float4*>(blob + layout_kdense_offset(n_rows_blob)) + static_cast<size_t>(ri) * kMatF4, tid);
+  __syncthreads();
+  for (int i = tid; i < 4 * 64; i += kThreads) {
+    // row 4 m + e of the product is group 2 m + e (e < 2): two groups to each
+    // quarter of the wave instead of four to two of them
+    const int l = i & 63, d0 = 32 * (l >> 4) + 8 * (i >> 6);
+    const int g = (l & 3) < 2 ? 2 * ((l >> 2) & 3) + (l & 3) : -1;
+    uint4_t m;
 #pragma unroll
-    for (int s = 0; s < 2; ++s) {
-      at[s] = paged::page_of_row(rows.b, d.batch, cap, r0 + kSub * s, tk);
-      if (r0 + kSub * s + tk >= n) at[s].x = -1;
-    }
+    for (int j = 0; j < 4; ++j)
+      m[j] = (S.gd[d0 + 2 * j] == g ? 0x3F80u : 0u) | (S.gd[d0 + 2 * j + 1] == g ? 0x3F800000u : 0u);
+    S.ma[i] = m;
+  }
+  __syncthreads();
+
+  const float gs[2] = {S.gs[2 * kk], S.gs[2 * kk + 1]};
+  const int nslot = (ng + 1) & ~1;
+  const auto cache_row = [&](int page) { return (static_cast<size_t>(d.layer) * d.batch + page) * d.n_kv + head; };
+  while (r0 < n) {  // (wave-uniform)
     // group radii: R2[g][row] = sum_d [group(d) = g] x[row][d]^2
     float4_t n2[2] = {{0.f, 0.f, 0.f, 0.f}, {0.f, 0.f, 0.f, 0.f}};
 #pragma unroll
-    for (int s4 = 0; s4 < 8; ++s4) {
-      const float4 m = S.ma[s4 * 64 + lane];
-      const float me[4] = {m.x, m.y, m.z, m.w};
+    for (int q = 0; q < 4; ++q) {
+      const uint4_t m = S.ma[q * 64 + lane];
 #pragma unroll
-      for (int e = 0; e < 4; ++e)
-#pragma unroll
-        for (int s = 0; s < 2; ++s) {
-          const float v = bf16_elem(x[s], 4 * s4 + e);
-          n2[s] = mfma(me[e], v * v, n2[s]);
-        }
-      __builtin_amdgcn_sched_barrier(0);  // (eight steps' squares at once would spill)
+      for (int s = 0; s < 2; ++s) {
+        uint4_t hi, lo;
+        square_parts(x[s][q], hi, lo);
+        n2[s] = mfma_bf16(m, lo, n2[s]);
+        n2[s] = mfma_bf16(m, hi, n2[s]);
+      }
     }
     // this lane holds R2 of rows tk, 16 + tk for groups 2 kk, 2 kk + 1 (zero
     // past the last group)
@@ -177,8 +192,9 @@ __device__ __forceinline__ void quant_keys(LdsKeys<W>& S, int bx, int n_wg, cons
         S.sc[wave][kSub * s + tk][2 * kk + i] = nrm[i] > 0.f ? gs[i] / nrm[i] : 0.f;
         h[i] = __half_as_ushort(__float2half_rn(nrm[i]));
       }
-      if (at[s].x >= 0 && 2 * kk < ng) {
-        uint16_t* dst = c.k_norms + cache_row(at[s].x) * kMaxGroups * cap + static_cast<size_t>(at[s].y) * nslot + 2 * kk;
+      const int page = __shfl(at.x, kSub * s + tk), place = __shfl(at.y, kSub * s + tk);
+      if (page >= 0 && 2 * kk < ng) {
+        uint16_t* dst = c.k_norms + cache_row(page) * kMaxGroups * cap + static_cast<size_t>(place) * nslot + 2 * kk;
         if (2 * kk + 1 < ng) *reinterpret_cast<uint32_t*>(dst) = h[0] | static_cast<uint32_t>(h[1]) << 16;
         else *dst = h[0];
       }
@@ -255,12 +271,13 @@ __device__ __forceinline__ void quant_keys(LdsKeys<W>& S, int bx, int n_wg, cons
       }
     }
     wave_sync();
+    const int2 was = at;
+    r0 += n_wg * kWaves * kSplitRows;
+    if (r0 < n) load_rows(r0);
     for (int idx = lane; idx < kSplitRows * kw; idx += 64) {
       const int t2 = idx / kw, w = idx - t2 * kw;
-      // (row t2's page and place, from lane t2 % 16: lanes 0 .. 15 take part in every round)
-      const int x0 = __shfl(at[0].x, t2 & 15), y0 = __shfl(at[0].y, t2 & 15), x1 = __shfl(at[1].x, t2 & 15),
-                y1 = __shfl(at[1].y, t2 & 15);
-      const int2 a = t2 < kSub ? make_int2(x0, y0) : make_int2(x1, y1);
+      // (lanes 0 .. 31 take part in every round)
+      const int2 a = make_int2(__shfl(was.x, t2), __shfl(was.y, t2));
       if (a.x >= 0) c.k_codes[(cache_row(a.x) * cap + a.y) * kw + w] = S.rw[wave][idx];
       S.rw[wave][idx] = 0u;
     }
@@ -270,8 +287,8 @@ __device__ __forceinline__ void quant_keys(LdsKeys<W>& S, int bx, int n_wg, cons
 
 // ---------------------------------------------------------------- values
 // The BV-bit codes of one value tile, ORed into its words.
-template <int BV, int W>
-__device__ __forceinline__ void tile_codes(LdsValues<W>& S, int wave, int lane, const uint4_t (&x)[2][4], int s_lo, int s_hi) {
+template <int BV>
+__device__ __forceinline__ void tile_codes(LdsValues& S, int wave, int lane, const uint4_t (&x)[2][4], int s_lo, int s_hi) {
   constexpr int kThr = (1 << BV) - 1;
   const int tk = lane & 15, kk = lane >> 4;
   const float sq = sqrtf(static_cast<float>(kHeadDim));
@@ -315,29 +332,42 @@ __device__ __forceinline__ void tile_codes(LdsValues<W>& S, int wave, int lane, 
   }
 }
 
-template <int W, int BV>
-__device__ __forceinline__ void quant_values(LdsValues<W>& S, int bx, int n_wg, long n_tiles, const Dims& d,
+template <int BV>
+__device__ __forceinline__ void quant_values(LdsValues& S, int bx, int n_wg, long n_tiles, const Dims& d,
                                              const uint8_t* __restrict__ blob, const void* __restrict__ vin,
                                              const PagedRows& rows, const CachePtrs& c) {
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int head = blockIdx.y, cap = d.capacity;
   const float* gthr = reinterpret_cast<const float*>(blob + kOffThr);
-  for (int i = tid; i < kThresholdEntries; i += W * 64) S.thr[i] = gthr[i];
-  stage_split<W>(S.rb, reinterpret_cast<const float4*>(blob + layout_rotv_mfma_offset(d.n_layers * d.n_kv)), tid);
-  __syncthreads();
-
+  for (int i = tid; i < kThresholdEntries; i += kWaves * 64) S.thr[i] = gthr[i];
+  // as in quant_keys: a wave's next tile is read early
   const int tk = lane & 15, kk = lane >> 4;
-  for (int i = bx * W + wave; i < n_tiles; i += n_wg * W) {
-    paged::Tile t;
-    if (!paged::tile_of(rows.b, d.batch, cap, i, t)) continue;  // wave-uniform
-    const size_t row = (static_cast<size_t>(d.layer) * d.batch + t.page) * d.n_kv + head, in_at = t.in0 + t.P0;
-    const int P0 = t.P0 % cap;
-    uint4_t x[2][4];
+  uint4_t x[2][4];
+  paged::Tile next = {};
+  bool there = false;
+  const auto load_tile = [&](int i) {
+    there = paged::tile_of(rows.b, d.batch, cap, i, next);  // wave-uniform
 #pragma unroll
     for (int h = 0; h < 2; ++h) {
       const int slot = kSub * h + tk;
-      load_operands(vin, (in_at + slot) * rows.v_stride + head * kHeadDim + 32 * kk, slot >= t.lo && slot < t.hi, x[h]);
+      load_operands(vin, (next.in0 + next.P0 + slot) * rows.v_stride + head * kHeadDim + 32 * kk,
+                    there && slot >= next.lo && slot < next.hi, x[h]);
     }
+  };
+  int i = wave * n_wg + bx;
+  if (i < n_tiles) load_tile(i);
+  stage_split<kWaves>(S.rb, reinterpret_cast<const float4*>(blob + layout_rotv_mfma_offset(d.n_layers * d.n_kv)), tid);
+  __syncthreads();
+
+  while (i < n_tiles) {
+    const paged::Tile t = next;
+    i += n_wg * kWaves;
+    if (!there) {
+      if (i < n_tiles) load_tile(i);
+      continue;
+    }
+    const size_t row = (static_cast<size_t>(d.layer) * d.batch + t.page) * d.n_kv + head;
+    const int P0 = t.P0 % cap;
     uint32_t* gv = c.v_codes + (row * (cap / kTile) + P0 / kTile) * kHeadDim * static_cast<size_t>(BV);
     // tile words: zero, or the old words with the new rows' bits cleared
     if (t.lo == 0 && t.hi == kTile) {
@@ -365,53 +395,51 @@ __device__ __forceinline__ void quant_values(LdsValues<W>& S, int bx, int n_wg, 
       }
     }
     wave_sync();
-    tile_codes<BV, W>(S, wave, lane, x, t.lo, t.hi);
+    tile_codes<BV>(S, wave, lane, x, t.lo, t.hi);
     wave_sync();
+    there = false;
+    if (i < n_tiles) load_tile(i);
     for (int idx = lane; idx < kHeadDim * BV; idx += 64) gv[idx] = S.vt[wave][idx];
     wave_sync();
   }
 }
 
 // The key workgroups (the longer ones) come first.
-template <int W, int BV>
-__global__ __launch_bounds__(W * 64) void k_paged_quantize(Dims d, const uint8_t* __restrict__ blob,
+template <int BV>
+__global__ __launch_bounds__(kWaves * 64) void k_paged_quantize(Dims d, const uint8_t* __restrict__ blob,
                                                            const void* __restrict__ kin, const void* __restrict__ vin,
                                                            PagedRows rows, CachePtrs c, int n_kwg, int n_vwg, int n_tiles) {
-  constexpr size_t kBytes = sizeof(LdsKeys<W>) > sizeof(LdsValues<W>) ? sizeof(LdsKeys<W>) : sizeof(LdsValues<W>);
+  constexpr size_t kBytes = sizeof(LdsKeys) > sizeof(LdsValues) ? sizeof(LdsKeys) : sizeof(LdsValues);
   __shared__ __attribute__((aligned(16))) uint8_t smem[kBytes];
   const int bx = static_cast<int>(blockIdx.x);
-  if (bx < n_kwg) quant_keys<W>(*reinterpret_cast<LdsKeys<W>*>(smem), bx, n_kwg, d, blob, kin, rows, c);
-  else quant_values<W, BV>(*reinterpret_cast<LdsValues<W>*>(smem), bx - n_kwg, n_vwg, n_tiles, d, blob, vin, rows, c);
+  if (bx < n_kwg) quant_keys(*reinterpret_cast<LdsKeys*>(smem), bx, n_kwg, d, blob, kin, rows, c);
+  else quant_values<BV>(*reinterpret_cast<LdsValues*>(smem), bx - n_kwg, n_vwg, n_tiles, d, blob, vin, rows, c);
 }
 
 }  // namespace
 
 bool paged_quantize_fits(const Dims& d) { return d.in_dtype == 1 && d.k_words <= kSplitKWords && d.v_bits <= kSplitVBits; }
 
+// One workgroup runs per CU: 256 of them, or fewer for few rows, share the rows
+// of all heads, so that each stages its matrix once.  160 are for keys, whose
+// blocks of 32 rows take about 1.6 times as long as the values' (65536 rows x 8
+// heads: 205 us with 128, 178 with 160, 193 with 176).
 hipError_t launch_paged_quantize_bf16(const Dims& d, const void* layout, const void* k, const void* v, const PagedRows& rows,
                                       const CachePtrs& c, hipStream_t s) {
-  const long n = rows.b.n_tokens, all = n * d.n_kv, tiles = std::min(n, (n + 62L * rows.b.n_seqs) / kTile);
-  // One workgroup runs per CU: 256 of them, half for keys and half for values,
-  // share the rows of all heads, so that each stages its matrix once.
-  const auto go = [&](auto kern, int w) {
-    const long each = std::max(1, 128 / d.n_kv);
-    const int n_kwg = static_cast<int>(std::min(each, (n + w * kSplitRows - 1) / (w * kSplitRows)));
-    const int n_vwg = static_cast<int>(std::min(each, (tiles + w - 1) / w));
-    hipLaunchKernelGGL(kern, dim3(n_kwg + n_vwg, d.n_kv), dim3(w * 64), 0, s, d, static_cast<const uint8_t*>(layout), k, v, rows,
-                       c, n_kwg, n_vwg, static_cast<int>(tiles));
+  constexpr long kKeyShare = 160;
+  const long n = rows.b.n_tokens, tiles = std::min(n, (n + 62L * rows.b.n_seqs) / kTile);
+  const auto go = [&](auto kern) {
+    const int n_kwg = static_cast<int>(std::min(std::max(1l, kKeyShare / d.n_kv), (n + kSplitRows - 1) / kSplitRows));
+    const int n_vwg = static_cast<int>(std::min(std::max(1l, (256 - kKeyShare) / d.n_kv), tiles));
+    hipLaunchKernelGGL(kern, dim3(n_kwg + n_vwg, d.n_kv), dim3(kWaves * 64), 0, s, d, static_cast<const uint8_t*>(layout), k, v,
+                       rows, c, n_kwg, n_vwg, static_cast<int>(tiles));
     return hipGetLastError();
   };
-  const auto width = [&](auto bv) {
-    constexpr int B = decltype(bv)::value;
-    // 4-wave workgroups where they take one round, 16-wave ones above
-    if (all <= 128L * kWavesShort * kSplitRows) return go(k_paged_quantize<kWavesShort, B>, kWavesShort);
-    return go(k_paged_quantize<kWavesLong, B>, kWavesLong);
-  };
   switch (d.v_bits) {
-    case 1: return width(std::integral_constant<int, 1>{});
-    case 2: return width(std::integral_constant<int, 2>{});
-    case 3: return width(std::integral_constant<int, 3>{});
-    default: return width(std::integral_constant<int, 4>{});
+    case 1: return go(k_paged_quantize<1>);
+    case 2: return go(k_paged_quantize<2>);
+    case 3: return go(k_paged_quantize<3>);
+    default: return go(k_paged_quantize<4>);
   }
 }
 
