@@ -532,8 +532,9 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(2, 2))
   int page_next = 0;
   bool lost = false;  // a page outside the pool: the rows that attend it are not numbers
   const auto turn_to = [&](int t) {  // rows [t, t + 64) of the sequence: the page whose number was read, and t there
-    lost |= static_cast<uint32_t>(page_next) >= static_cast<uint32_t>(S.batch);
-    const int page = lost ? 0 : page_next;
+    const int number = __builtin_amdgcn_readfirstlane(page_next);
+    lost |= static_cast<uint32_t>(number) >= static_cast<uint32_t>(S.batch);
+    const int page = lost ? 0 : number;
     rows_of((static_cast<size_t>(layer) * S.batch + page) * d.n_kv + kvh);
     return t % S.capacity;
   };
@@ -572,7 +573,7 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(2, 2))
   int t0 = t_begin + (wave & (wps - 1)) * kKeyTile;
   const int stride = wps * kKeyTile;
   const auto read_page = [&](int t) {
-    if constexpr (kPaged) page_next = mode.b.pages[static_cast<size_t>(seq) * mode.b.max_pages + t / S.capacity];
+    if constexpr (kPaged) page_next = paged::page_ahead(mode.b, seq, t, S.capacity);
   };
   // (without a next tile this one again: the loads in flight stay countable)
   const auto after = [&](int t) { return t + stride < t_end ? t + stride : t; };

@@ -205,10 +205,11 @@ __global__ __launch_bounds__(kAttnThreads) __attribute__((amdgpu_waves_per_eu(2,
     vc = reinterpret_cast<const uint8_t*>(S.c.v_codes + row * (cap / kTile) * kHeadDim * BV);
     vnp = S.c.v_norms + row * cap;
   };
+  const uint64_t row0 = static_cast<uint64_t>(layer) * S.batch * d.n_kv + kvh;  // the layer's first page
   int page_next = 0;  // page number of the next tile to load, read a tile ahead of it
   bool lost = false;  // a page outside the pool: the rows that attend it are not numbers
   const auto read_page = [&](int t) {
-    if constexpr (kPaged) page_next = mode.b.pages[static_cast<size_t>(seq) * mode.b.max_pages + t / S.capacity];
+    if constexpr (kPaged) page_next = paged::page_ahead(mode.b, seq, t, S.capacity);
   };
   if constexpr (!kPaged) rows_of((static_cast<size_t>(layer) * S.batch + seq) * d.n_kv + kvh);
 
@@ -231,14 +232,26 @@ __global__ __launch_bounds__(kAttnThreads) __attribute__((amdgpu_waves_per_eu(2,
   Raw<BV> raw;
   const auto load_raw = [&](int t) {
     const int tt = opaque_tid();
-    int ta = t;  // the tile's place in its cache row
+    const uint8_t *ks, *ns, *vs;
+    const uint16_t* rs;
     if constexpr (kPaged) {
-      lost |= static_cast<uint32_t>(page_next) >= static_cast<uint32_t>(S.batch);
-      rows_of((static_cast<size_t>(layer) * S.batch + (lost ? 0 : page_next)) * d.n_kv + kvh);
-      ta = t % S.capacity;
+      const int page = __builtin_amdgcn_readfirstlane(page_next);
+      lost |= static_cast<uint32_t>(page) >= static_cast<uint32_t>(S.batch);
+      const int ta = t % S.capacity;  // the tile's place in its page
+      // (all rows of a cache numbered in turn: few multiplications)
+      const uint64_t x = (row0 + static_cast<uint64_t>(lost ? 0u : static_cast<uint32_t>(page)) * static_cast<uint32_t>(d.n_kv)) *
+                             static_cast<uint32_t>(S.capacity) + static_cast<uint32_t>(ta);
+      ks = reinterpret_cast<const uint8_t*>(S.c.k_codes) + x * static_cast<uint32_t>(kw) * 4;
+      ns = reinterpret_cast<const uint8_t*>(S.c.k_norms) + x * (kMaxGroups * 2) -
+           static_cast<uint64_t>(static_cast<uint32_t>(ta)) * static_cast<uint32_t>((kMaxGroups - nslot) * 2);
+      vs = reinterpret_cast<const uint8_t*>(S.c.v_codes) + x * (kHeadDim / kTile * BV * 4);
+      rs = S.c.v_norms + x;
+    } else {
+      ks = kc + static_cast<size_t>(t) * kw * 4;
+      ns = kn + static_cast<size_t>(t) * nslot * 2;
+      vs = vc + static_cast<size_t>(t / kTile) * kHeadDim * BV * 4;
+      rs = vnp + t;
     }
-    const uint8_t* ks = kc + static_cast<size_t>(ta) * kw * 4;
-    const uint8_t* ns = kn + static_cast<size_t>(ta) * nslot * 2;
     uint32_t k_at = static_cast<uint32_t>((tt & 63) * kw * 4), n_at = static_cast<uint32_t>((tt & 63) * nslot * 2);
     uint32_t v_lane = static_cast<uint32_t>((tt & 127) * BV * 4), vn_lane = static_cast<uint32_t>((tt & 63) * 2);
 #pragma unroll
@@ -251,11 +264,10 @@ __global__ __launch_bounds__(kAttnThreads) __attribute__((amdgpu_waves_per_eu(2,
     raw.kn.z = ld_at<uint32_t>(ns + 8, n_at);
     raw.kn.w = ld_at<uint32_t>(ns + 12, n_at);
     constexpr int NW = Raw<BV>::kVW;
-    const uint8_t* vs = vc + (static_cast<size_t>(ta / kTile) + (quarter >> 1)) * kHeadDim * BV * 4 +
-                        4 * (BV * (quarter & 1) / 2);
+    vs += (quarter >> 1) * kHeadDim * BV * 4 + 4 * (BV * (quarter & 1) / 2);
 #pragma unroll
     for (int i = 0; i < NW; ++i) raw.v[i] = ld_at<uint32_t>(vs + 4 * i, v_lane);
-    raw.vn = ld_at<uint16_t>(vnp + ta, vn_lane);
+    raw.vn = ld_at<uint16_t>(rs, vn_lane);
     // what lies behind the last row may be large, infinite or not a number: no radii
     if (t + kKeyTile > t_end) {
       const uint32_t in = t + (tt & 63) < t_end ? ~0u : 0u;

@@ -196,7 +196,7 @@ __attribute__((amdgpu_waves_per_eu((waves_of<NSET, KWB>() / 4)))) void k_paged_d
   int page_next = 0;
   bool lost = false;  // a page outside the pool: the rows that attend it are not numbers
   const auto read_page = [&](int t) {
-    page_next = mode.b.pages[static_cast<size_t>(U.seq) * mode.b.max_pages + t / S.capacity];
+    page_next = paged::page_ahead(mode.b, U.seq, t, S.capacity);
   };
   const auto after = [&](int t) { return t + stride < t_end ? t + stride : t; };
   if (t0 < t_end) read_page(t0);
@@ -214,8 +214,9 @@ __attribute__((amdgpu_waves_per_eu((waves_of<NSET, KWB>() / 4)))) void k_paged_d
   }
   const size_t cap = S.capacity;
   const auto turn_to = [&](RowPtrs& R) {  // the page whose number was read
-    lost |= static_cast<uint32_t>(page_next) >= static_cast<uint32_t>(S.batch);
-    const size_t row = (static_cast<size_t>(d.layer) * S.batch + (lost ? 0 : page_next)) * d.n_kv + kvh;
+    const int page = __builtin_amdgcn_readfirstlane(page_next);
+    lost |= static_cast<uint32_t>(page) >= static_cast<uint32_t>(S.batch);
+    const size_t row = (static_cast<size_t>(d.layer) * S.batch + (lost ? 0 : page)) * d.n_kv + kvh;
     R = {S.c.k_codes + row * cap * kw, S.c.k_norms + row * kMaxGroups * cap, S.c.v_codes + row * (cap / kTile) * kHeadDim * BV,
          S.c.v_norms + row * cap};
   };

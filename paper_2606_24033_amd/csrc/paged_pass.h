@@ -26,6 +26,15 @@ struct Mode : PagedPass {
   static constexpr bool kPaged = true, kMods = MODS;
 };
 
+// A page's number read ahead of its use, in a vector register: one that the
+// compiler sees to be uniform it waits for at once, and for every load before it.
+__device__ __forceinline__ int page_ahead(const PagedBatch& b, int seq, int t, int page_rows) {
+  uint32_t at = 0;
+  asm volatile("" : "+v"(at));
+  const int32_t* row = b.pages + static_cast<size_t>(seq) * b.max_pages + t / page_rows;
+  return *reinterpret_cast<const int32_t*>(reinterpret_cast<const uint8_t*>(row) + at);
+}
+
 struct Unit {
   int seq, block, r0, kvh, split;  // block: its number in the pass; r0: its first query row
   Seq q;
