@@ -344,15 +344,15 @@ hipError_t launch_quantize_append(const Dims& d, const void* layout, const void*
 
 hipError_t launch_paged_append(const Dims& d, const void* layout, const void* k, const void* v, const PagedRows& rows,
                                const CachePtrs& c, hipStream_t s) {
-  if (rows.b.max_new > kRowAppend)
-    return paged_quantize_fits(d) ? launch_paged_quantize_bf16(d, layout, k, v, rows, c, s)
-                                  : launch_paged_quantize(d, layout, k, v, rows, c, s);
   const auto kern = d.in_dtype == 1 ? k_append_rows<true, PagedRows> : k_append_rows<false, PagedRows>;
   // Each workgroup reads 128 KB of rotations, each row of one costs about 2 us:
   // as many rows as keep the workgroups below the CUs' number.
   PagedRows r = rows;
   r.per = static_cast<int>(std::min<long>(kRowAppend, (static_cast<long>(rows.b.n_tokens) * d.n_kv + 159) / 160));
   const int n = rows.b.max_new == 1 ? (rows.b.n_tokens + r.per - 1) / r.per : rows.b.n_seqs;
+  if (rows.b.max_new > kRowAppend || n > 65535)  // (a grid's second dimension; the others loop over their rows)
+    return paged_quantize_fits(d) ? launch_paged_quantize_bf16(d, layout, k, v, rows, c, s)
+                                  : launch_paged_quantize(d, layout, k, v, rows, c, s);
   hipLaunchKernelGGL(kern, dim3(d.n_kv, n), dim3(1024), 0, s, d, static_cast<const uint8_t*>(layout), k, v, r, c);
   return hipGetLastError();
 }

@@ -5,6 +5,8 @@ and a run of them together.
 Tolerances, element by element, from the arithmetic alone (u = 2^-24), as in
 the tests of the other cache readers; the cap and the bias add their own terms
 (attend below), the rotation those of its angle (rotated below).
+Where a chunk's bf16 outputs come from 6-bit operands of the small products, a
+logit could be off by 2^-12 of its terms; it is held to the same 2^-20 here.
 """
 import math
 
@@ -301,6 +303,27 @@ class bare_pool:
                              v_bits=v_bits, in_dtype=few.cfg.in_dtype)
         self.bits, self.layout, self.cache = few.bits, few.layout, bg.Cache(self.cfg)
         self.rot_k, self.rot_v = rotations
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "fp32"])
+def test_paged_append_of_single_tokens_among_many_rows(rotations, dtype):
+    """Inputs padded on both sides to more rows than a grid's dimension holds workgroups of four."""
+    pool = bare_pool(rotations, 1, 4, 1, 64, 192, 3, "wide", dtype)
+    b = Batch(pool, [1, 1, 1], [64, 3, 40], seed=2)
+    kv = torch.randn((3, 2, 1, D), generator=torch.Generator(device="cuda").manual_seed(9), device="cuda").to(typed(dtype))
+    bg.blockgtq_paged_append(pool.cfg, pool.layout, 0, kv[:, 0], kv[:, 1], b.chunk, pool.cache)
+    few = raw(pool.cache)
+    for t in (pool.cache.k_codes, pool.cache.k_norms, pool.cache.v_codes, pool.cache.v_norms):
+        t.zero_()
+    n, at = 4 * 65536 + 7, 4 * 65535 + 2
+    rows = torch.ones((n, 2, 1, D), device="cuda", dtype=typed(dtype))
+    rows[at:at + 3] = kv
+    chunk = bg.Chunk(i32(b.first + at), i32(b.lens), i32(b.table), 1, b.max_ctx)
+    bg.blockgtq_paged_append(pool.cfg, pool.layout, 0, rows[:, 0], rows[:, 1], chunk, pool.cache)
+    many = raw(pool.cache)
+    # three rows of random numbers have no coordinate next to a threshold: the kernels agree in every code
+    assert torch.equal(many[0], few[0]) and torch.equal(many[2], few[2])
+    assert near_radii(many[1], few[1], False) and near_radii(many[3], few[3], False)
 
 
 @pytest.mark.parametrize("small", [True, False])
