@@ -49,7 +49,7 @@ hipError_t join(const Dims& d, const void* layout, const CrossCall& call, const 
 // on fp32 MFMAs, their 32 dims of a lane in 16-byte reads.  Bound by those
 // products (256 of 32 cycles a wave) and by the staging of the matrix, which
 // rows of several heads of the same KV head share.  28768 rows x 8 KV heads:
-// 112 us there, 23 here.
+// 112 us there, 17 here.
 constexpr int kRotWaves = 4;
 __global__ __launch_bounds__(kRotWaves * 64) void k_paged_rotate(Dims d, const uint8_t* __restrict__ blob,
                                                                  const float* __restrict__ q, int n_tokens, int iters,
