@@ -310,7 +310,12 @@ __global__ __launch_bounds__(kAttnThreads) __attribute__((amdgpu_waves_per_eu(2,
     const auto times = [&](const uint4& x, int n) {
       const _Float16 p = __builtin_bit_cast(_Float16, static_cast<uint16_t>((n + 15) << 10));
       const half2_t pp = {p, p};
-      const auto one = [&](uint32_t r) { return __builtin_bit_cast(uint32_t, __builtin_bit_cast(half2_t, r) * pp); };
+      const auto one = [&](uint32_t r) {
+        const half2_t x = __builtin_bit_cast(half2_t, r);
+        // (kRest: an infinite radius becomes not a number, as its lo parts are where they are fp16 numbers: infinite
+        // products alone may all have one sign, and a logit of -infinity would drop the row)
+        return __builtin_bit_cast(uint32_t, kRest ? __builtin_elementwise_fma(x, pp, x - x) : x * pp);
+      };
       return make_uint4(one(x.x), one(x.y), one(x.z), one(x.w));
     };
     uint4 r = times(raw.kn, min(up, 15));

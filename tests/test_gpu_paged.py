@@ -558,6 +558,28 @@ def test_unseen_rows_do_not_matter(rotations, news, lens, out, prefix, bad):
             assert torch.isnan(got[torch.from_numpy(~clean).cuda()].float()).all()
 
 
+@pytest.mark.parametrize("new", [1, 5, 30, 300, 2500])
+@pytest.mark.parametrize("out", ["bf16", "fp32"])
+def test_infinite_radius_of_one_group(rotations, new, out):
+    """Queries against the row's own direction: all of the group's products are -infinity, and the row is not dropped."""
+    pool = Packed(rotations, 77, batch=1 + (new + 350) // 64, kv=1, cap=64, k_budget=192, v_bits=2, kind="wide")
+    b = Batch(pool, [new], [new + 350 if new < 2500 else new], seed=new)
+    groups = o.groups(pool.bits[0, 0])
+    S, t = slots_of(pool, 0, 0), 13
+    page = int(b.table[0, 0])
+    keep = pool.cache.k_norms.clone()
+    for g, (_, dims) in enumerate(groups):
+        pool.cache.k_norms.copy_(keep)
+        pool.cache.k_norms[0, page, 0, t * S + g] = math.inf
+        for scale in (-1.0, 1.0):
+            q = np.zeros((new, 4, D))
+            q[:, :, dims] = scale * pool.k[0, page, 0, t, dims]
+            got = bg.blockgtq_paged_attn(pool.cfg, pool.layout, 0, torch.from_numpy(q).cuda().to(torch.bfloat16), b.chunk,
+                                         pool.cache, out_dtype=typed(out))
+            seen = t if new == 2500 else 0  # (its first tokens come before the row)
+            assert torch.isnan(got[seen:]).all() and torch.isfinite(got[:seen]).all(), (g, scale)
+
+
 def test_refused_sequences_and_pages(rotations):
     """Numbers that make no sense give NaN, in that sequence alone; nothing behind the sequences is written."""
     page = 64
