@@ -178,7 +178,7 @@ __global__ __launch_bounds__(kAttnThreads) __attribute__((amdgpu_waves_per_eu(2,
       for (int e = 0; e < 8; ++e) {
         const float x = v[2 * ks + (e >> 2)][e & 3] * to;
         const _Float16 h = static_cast<_Float16>(x);
-        qh[ks][e] = h;
+        qh[ks][e] = kRest ? h + static_cast<_Float16>(x - x) : h;  // (infinite: not a number, see scaled_keys)
         if constexpr (!kRest) ql[ks][e] = static_cast<_Float16>(x - static_cast<float>(h));
       }
     if constexpr (kRest) {

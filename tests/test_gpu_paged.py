@@ -580,6 +580,25 @@ def test_infinite_radius_of_one_group(rotations, new, out):
             assert torch.isnan(got[seen:]).all() and torch.isfinite(got[:seen]).all(), (g, scale)
 
 
+@pytest.mark.parametrize("new", [1, 5, 300])
+@pytest.mark.parametrize("out", ["bf16", "fp32"])
+@pytest.mark.parametrize("bad", [math.inf, -math.inf, math.nan])
+def test_queries_that_are_not_finite(rotations, new, out, bad):
+    """They make their own outputs not a number and no others."""
+    pool = Packed(rotations, 5, batch=11, kv=1, cap=64, k_budget=192, v_bits=2, kind="wide")
+    b = Batch(pool, [new], [650], seed=new)
+    q, dq = pool.queries((new,))
+    ref, bound = expect(b, q, typed(out))
+    for i, dim in ((0, 0), (new // 2, 63), (new - 1, 100)):
+        x = dq.clone()
+        x[i, 2, dim] = bad
+        got = bg.blockgtq_paged_attn(pool.cfg, pool.layout, 0, x, b.chunk, pool.cache, out_dtype=typed(out))
+        assert torch.isnan(got[i, 2]).all(), (i, dim)
+        fine = torch.ones((new, 4), dtype=torch.bool, device="cuda")
+        fine[i, 2] = False
+        check(f"{i} {dim}", got[fine], ref[fine.cpu().numpy()], bound[fine.cpu().numpy()])
+
+
 def test_refused_sequences_and_pages(rotations):
     """Numbers that make no sense give NaN, in that sequence alone; nothing behind the sequences is written."""
     page = 64
