@@ -14,17 +14,20 @@ namespace bgtq {
 namespace paged {
 
 // What the arrays of a batch say is read on the device: a sequence whose
-// numbers contradict each other or the host's bounds is not `ok`.
+// numbers contradict each other or the host's bounds is not `ok`.  Its tokens
+// lie inside the inputs all the same, for any 32-bit offsets.
 struct Seq {
   int first, n, len;  // its tokens in the inputs, its rows (the new ones among them)
   bool ok;
 };
-__device__ __forceinline__ Seq make_seq(const PagedBatch& b, int c0, int c1, int len) {
+__host__ __device__ __forceinline__ Seq make_seq(const PagedBatch& b, int c0, int c1, int len) {
+  const auto inside = [&](int c) { return c < 0 ? 0 : c < b.n_tokens ? c : b.n_tokens; };
   Seq s;
-  s.first = min(max(c0, 0), b.n_tokens);
-  s.n = max(min(c1, b.n_tokens) - s.first, 0);
+  s.first = inside(c0);
+  const int last = inside(c1);  // (both in 0 .. n_tokens: the difference fits)
+  s.n = last > s.first ? last - s.first : 0;
   s.len = len;
-  s.ok = c0 == s.first && c1 - c0 == s.n && s.n <= b.max_new && len >= s.n && len <= b.max_ctx;
+  s.ok = c0 == s.first && c1 == last && c0 <= c1 && s.n <= b.max_new && len >= s.n && len <= b.max_ctx;
   return s;
 }
 __device__ __forceinline__ Seq seq_of(const PagedBatch& b, int s) {
