@@ -482,7 +482,10 @@ typedef struct {
 /* A sequence whose numbers leave these bounds (d_cu_new outside [0, n_tokens] or
  * falling, more than max_new new tokens, fewer rows than new tokens, more than
  * max_ctx rows) is appended nothing and its outputs are NaN; nothing outside the
- * buffers is read or written. */
+ * buffers is read or written.  The other sequences are appended and attended as
+ * they are, but where offsets at fault make sequences claim the same rows of the
+ * inputs: such rows' outputs are those of one of the claimants or NaN, and a
+ * sequence that claims rows of an earlier one may be refused too. */
 
 /* Quantizes and packs the chunk's rows of one layer into the sequences' pages:
  * blockgtq_quantize_append of a ragged batch.  Rows already in a touched page

@@ -138,7 +138,7 @@ __global__ __launch_bounds__(1024) void k_append_rows(Dims d, const uint8_t* __r
     if (rows.b.max_new == 1) {
       in0 = rows.per * blockIdx.y;
       n_new = min(rows.per, rows.b.n_tokens - in0);
-      at = paged::page_of_row(rows.b, d.batch, cap, in0, lane & 15);
+      at = paged::page_of_row<kRowAppend>(rows.b, d.batch, cap, in0, lane % kRowAppend);
     } else {
       // (rows of one sequence: two workgroups would write the same words of a value tile)
       const paged::Seq q = paged::seq_of(rows.b, blockIdx.y);

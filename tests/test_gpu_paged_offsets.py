@@ -82,3 +82,110 @@ def test_attention_of_a_batch_with_offsets_at_fault(rotations, news, lens):
                     assert (np.abs(got[i].double().cpu().numpy() - ref[i]) <= bound[i])[fine].all()
             assert torch.isnan(got[sorted(gone - right)]).all()
             assert (got[sorted(set(range(b.n)) - right - gone)] == 7.0).all()
+
+
+def cache_tensors(cache):
+    return cache.k_codes, cache.k_norms, cache.v_codes, cache.v_norms
+
+
+class Appends:
+    """Appends of a batch to the pages of a pool as it was."""
+
+    def __init__(self, rotations, news, lens, dtype):
+        self.pool = Packed(rotations, 8, batch=14, kv=2, cap=64, k_budget=192, v_bits=3, kind="wide", dtype=dtype)
+        self.b, self.lens, self.most = Batch(self.pool, news, lens, seed=4, pad=4), lens, max(news)
+        g = torch.Generator(device="cuda").manual_seed(1)
+        self.kv = torch.randn((self.b.n, 2, 2, D), generator=g, device="cuda").to(typed(dtype))
+        self.start = raw(self.pool.cache)
+
+    def run(self, cu, lens=None):
+        for x, y in zip(cache_tensors(self.pool.cache), self.start):
+            x.copy_(y)
+        chunk = bg.Chunk(i32(cu), i32(self.lens if lens is None else lens), i32(self.b.table), self.most, max(self.lens))
+        bg.blockgtq_paged_append(self.pool.cfg, self.pool.layout, 0, self.kv[:, 0], self.kv[:, 1], chunk, self.pool.cache)
+        return raw(self.pool.cache)
+
+    def alone(self, cu, s):
+        """Sequence s by itself: the others' lengths are none that a sequence has."""
+        return self.run(cu, [n if i == s else -1 for i, n in enumerate(self.lens)])
+
+    def pages_equal(self, x, y, pages):
+        return all(torch.equal(a[0, p], c[0, p]) for p in pages for a, c in zip(x, y))
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "fp32"])
+@pytest.mark.parametrize("news,lens", BATCHES + [([1, 1, 0, 1, 0, 1, 1], [70, 64, 3, 65, 0, 1, 2])])
+def test_append_of_a_batch_with_offsets_at_fault(rotations, news, lens, dtype):
+    """The other sequences' rows arrive, keys and values alike, and the pages of those at fault stay as they were."""
+    a = Appends(rotations, news, lens, dtype)
+    full = a.run(a.b.first)
+    for cu in faults(a.b.first, a.b.n):
+        print(f"offsets {cu.tolist()} of {a.b.n} rows", flush=True)
+        got = a.run(cu)
+        for s, (rows, fine) in enumerate(claims(cu, lens, a.b.n, max(news), max(lens))):
+            pages = a.b.table[s, :a.b.per[s]]
+            assert a.pages_equal(got, full if fine else a.start, pages), (cu, s)
+
+
+def falls(first, n):
+    """Offsets inside the inputs that fall."""
+    for i in range(1, len(first) - 1):
+        for x in (0, int(first[i - 1]) // 2, int(first[i + 1]) + 1, n):
+            cu = first.copy()
+            cu[i] = x
+            yield cu
+    yield np.array([0, first[1], 0, first[1], first[-1]][:len(first)], np.int32)  # the same rows twice
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "fp32"])
+@pytest.mark.parametrize("news,lens", BATCHES)
+def test_append_of_a_batch_whose_offsets_fall(rotations, news, lens, dtype):
+    """A sequence's rows arrive all together or not at all, and surely where it claims rows of no earlier one."""
+    a = Appends(rotations, news, lens, dtype)
+    for cu in falls(a.b.first, a.b.n):
+        print(f"offsets {cu.tolist()} of {a.b.n} rows", flush=True)
+        got = a.run(cu)
+        end = 0
+        for s, (rows, fine) in enumerate(claims(cu, lens, a.b.n, max(news), max(lens))):
+            pages = a.b.table[s, :a.b.per[s]]
+            alone = a.alone(cu, s)
+            if fine and rows.start >= end:
+                assert a.pages_equal(got, alone, pages), (cu, s)
+            else:
+                assert a.pages_equal(got, a.start, pages) or (fine and a.pages_equal(got, alone, pages)), (cu, s)
+            end = max(end, rows.stop if fine else 0)
+
+
+@pytest.mark.parametrize("news,lens", BATCHES + [([300, 300, 300], [300, 340, 300])])
+def test_attention_of_a_batch_whose_offsets_fall(rotations, news, lens):
+    """Every row that a sequence claims is not a number or one of its claimants' outputs, and surely right where the only
+    claimant starts behind the earlier ones."""
+    pool = Packed(rotations, 6, batch=18, kv=2, group=4, cap=64)
+    b = Batch(pool, news, lens, seed=3, pad=4)
+    q, dq = pool.queries((b.n,))
+    for cu in list(falls(b.first, b.n)):
+        told = claims(cu, lens, b.n, max(news), max(lens))
+        b.first, b.news = cu, [len(rows) if fine else 0 for rows, fine in told]
+        refs = [expect(b, q, torch.float32, only=[s]) for s in range(len(news))]
+        claimed, sure, end = {}, [], 0
+        for s, (rows, fine) in enumerate(told):
+            for i in rows:
+                claimed.setdefault(i, []).append(s if fine and rows.start >= end else -1 - s)
+            end = max(end, rows.stop if fine else 0)
+        for splits in (0, 1, 2):
+            print(f"offsets {cu.tolist()} of {b.n} rows, {splits} splits", flush=True)
+            chunk = bg.Chunk(i32(cu), i32(lens), i32(b.table), max(news), max(lens))
+            got = torch.full((b.n, 8, D), 7.0, device="cuda")
+            bg.blockgtq_paged_attn(pool.cfg, pool.layout, 0, dq, chunk, pool.cache, out=got, n_splits=splits)
+            x = got.double().cpu().numpy()
+            for i in range(b.n):
+                if i not in claimed:
+                    assert (x[i] == 7.0).all(), i
+                    continue
+                near = np.isnan(x[i])
+                if len(claimed[i]) == 1 and claimed[i][0] >= 0:
+                    near[:] = False
+                for s, (rows, fine) in enumerate(told):
+                    if fine and i in rows:
+                        near |= np.abs(x[i] - refs[s][0][i]) <= refs[s][1][i]
+                assert near.all(), (cu, splits, i)
