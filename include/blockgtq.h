@@ -521,15 +521,16 @@ typedef struct {
  * layer in [0, n_layers).
  * d_q: post-RoPE queries [n_tokens][n_kv_heads*group][128] in in_dtype; d_out:
  *      the same shape in out_dtype, of the precision of blockgtq_cross_attn, but
- *      for bf16 outputs: capped logits are off by 2^-23 of the cap, and those of
- *      long chunks by 2^-12 of the sum of their terms' magnitudes at most (2^-16
- *      of their spread on average).  Both and the workspace 16-byte aligned
- *      (EINVAL otherwise).
+ *      for bf16 outputs' capped logits, which are off by 2^-23 of the cap.  Both
+ *      and the workspace 16-byte aligned (EINVAL otherwise).
  * A page number outside [0, cfg->batch) makes NaN of every output that attends
  * the page's rows, and may of the sequence's other ones in this call.  What
  * the cache holds in rows that a token does not see (not a number or infinite
- * radii too) does not enter its outputs; a radius that is not finite in a row
- * that it sees makes them NaN.
+ * radii too) does not enter its outputs, but for one rounding: long chunks scale
+ * all rows' fp16 parts by a power of two that the largest finite radius so far
+ * sets, also one that only later tokens see, and hold a coordinate to 2^-37 of
+ * what that radius gives.  A radius that is not finite in a row that a token sees
+ * makes its outputs NaN.
  * n_splits: 0 = heuristic, else the splits of the key axis (1 .. 4096).
  * d_workspace: blockgtq_paged_workspace_bytes bytes for the chunk's sizes, any
  *      contents; calls that share it must not overlap in time.

@@ -16,9 +16,6 @@ typedef float float4_t __attribute__((ext_vector_type(4)));
 
 typedef float float16_t __attribute__((ext_vector_type(16)));
 typedef _Float16 half2_t __attribute__((ext_vector_type(2)));
-typedef _Float16 half32_t __attribute__((ext_vector_type(32)));
-typedef uint32_t uint6_t __attribute__((ext_vector_type(6)));
-typedef int int8_v __attribute__((ext_vector_type(8)));
 
 constexpr int kAttnWaves = 8;      // attention kernel: 8 waves (2 per SIMD)
 constexpr int kAttnThreads = kAttnWaves * 64;
@@ -35,8 +32,6 @@ constexpr int kDecKL = kDecKH + 64 * kKStride * 2;
 constexpr int kDecV = kDecKL + 64 * kKStride * 2;
 constexpr int kDecVN = kDecV + 128 * kVStride * 2;
 constexpr int kDecBytes = kDecVN + 64 * 2;
-// (or, in the lo part's place, a token's 8 waves' 32 bytes each of key_store_rest)
-constexpr float kRestKey = 2048.f, kRestQuery = 1024.f;
 constexpr int kOffCb = 0;                        // fp16 codebooks
 constexpr int kOffPair = kOffCb + 1024;          // pair tables of the widths 1 .. kMaxPair
 constexpr int kMaxPair = 6;
@@ -205,36 +200,6 @@ __device__ __forceinline__ void key_store(uint8_t* dst, const KeyItems& it, int 
       make_uint2(__builtin_bit_cast(uint32_t, ha), __builtin_bit_cast(uint32_t, hb));
   *reinterpret_cast<uint2*>(dst + kDecKL) =
       make_uint2(__builtin_bit_cast(uint32_t, la), __builtin_bit_cast(uint32_t, lb));
-}
-// The same with the lo part as what remains of the sum (cross_tile.h): a wave's
-// 16 hi and 16 lo parts of a token as 32 numbers of 6 bits (3 of exponent, 2 of
-// mantissa, up to 28), rest: their 24 bytes' place.
-__device__ __forceinline__ void key_store_rest(uint8_t* dst, uint8_t* rest, const KeyItems& it, const uint4& radii,
-                                               const uint2 (&c)[kItemsPer]) {
-  half32_t x;
-#pragma unroll
-  for (int j = 0; j < kItemsPer; ++j) {
-    const uint32_t r =
-        __builtin_amdgcn_perm(radii.y, radii.x, it.sel_lo[j]) | __builtin_amdgcn_perm(radii.w, radii.z, it.sel_hi[j]);
-    const half2_t rr = __builtin_bit_cast(half2_t, r);
-    const half2_t ra = {rr[0], rr[0]}, rb = {rr[1], rr[1]};
-    const half2_t ca = __builtin_bit_cast(half2_t, c[j].x), cb = __builtin_bit_cast(half2_t, c[j].y);
-    const half2_t ha = ra * ca, hb = rb * cb;
-    const half2_t up = {static_cast<_Float16>(kRestKey), static_cast<_Float16>(kRestKey)};
-    const half2_t la = __builtin_elementwise_fma(ra, ca, -ha) * up, lb = __builtin_elementwise_fma(rb, cb, -hb) * up;
-    *reinterpret_cast<uint2*>(dst + 8 * kAttnWaves * j + kDecKH) =
-        make_uint2(__builtin_bit_cast(uint32_t, ha), __builtin_bit_cast(uint32_t, hb));
-#pragma unroll
-    for (int e = 0; e < 2; ++e) {
-      x[4 * j + e] = ha[e];
-      x[4 * j + 2 + e] = hb[e];
-      x[16 + 4 * j + e] = la[e];
-      x[16 + 4 * j + 2 + e] = lb[e];
-    }
-  }
-  const uint6_t y = __builtin_amdgcn_cvt_scalef32_pk32_bf6_f16(x, kRestKey);
-  *reinterpret_cast<uint4*>(rest) = make_uint4(y[0], y[1], y[2], y[3]);
-  *reinterpret_cast<uint2*>(rest + 16) = make_uint2(y[4], y[5]);
 }
 
 // Value decode: thread = (dim tid % 128, 16-token step tid / 128); a holds

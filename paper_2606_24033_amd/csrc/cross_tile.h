@@ -55,26 +55,11 @@ __device__ __forceinline__ void scale_of(float mx, float& to, float& back) {
 
 // EX: the softmax weights in two fp16 parts, for fp32 outputs (see cross_impl.h).
 // MODE: WholeCache, or the new rows of a ragged batch over pages (paged_pass.h).
-//
-// kRest (pages, bf16 outputs): with q = qh + ql and k = kh + kl in fp16 parts,
-// ql kh + qh kl is 2^-11 of a logit, so its operands need few bits: 6-bit numbers
-// (3 of exponent, 2 of mantissa), 64 dims to a matrix instruction that takes the
-// time of 16 dims in fp16.  Two such operands leave a term of it off by 2^-2 of
-// itself at most (or by 2^-8 of what the largest key so far gives): 2^-12 of a
-// logit's terms, where fp16-rounded keys and queries would leave 2^-10.
-// With fp16-rounded keys instead (two products) the outputs' error rose from
-// 0.0017 of the 2-norm to 0.0025; with this it stays 0.0017.  A lane's 32 numbers
-// are the 16 hi and 16 lo parts that one wave decodes of a token, against the
-// same dims of ql and qh.  Powers of two (kRestKey, kRestQuery) bring both parts
-// to the same size and are undone by the instruction's own scale.  An
-// 8192-token prompt, 8 KV heads x 4: 1144 -> 999 us (943 with the addresses below),
-// matrix cores 44 -> 34 % busy, vector instructions 56 %.
 template <int BV, int KS, bool EX, class MODE>
 __global__ __launch_bounds__(kAttnThreads) __attribute__((amdgpu_waves_per_eu(2, 2))) void k_cross_tile(
     Dims d, const uint8_t* __restrict__ blob, const float* __restrict__ qr, CrossCall call, MODE mode) {
   constexpr bool kPaged = MODE::kPaged, kMods = MODE::kMods;
   constexpr int kWgRows = kAttnWaves / KS * kWaveRows, NB = 2 / KS;  // query rows; token blocks of a wave
-  constexpr bool kRest = kPaged && !EX;
   __shared__ __attribute__((aligned(16))) uint8_t smem[kLdsBytes];
   const CrossSide& S = call.side[0];
   const int tid = threadIdx.x, lane = tid & 63;
@@ -152,8 +137,7 @@ __global__ __launch_bounds__(kAttnThreads) __attribute__((amdgpu_waves_per_eu(2,
 
   // query operands (B of S^T = K Q^T): dims 16 ks + 8 hf .. +7 of the row,
   // scaled, in fp16 hi and lo parts.
-  half8_t qh[8], ql[kRest ? 1 : 8];
-  int8_v qx[kRest ? 4 : 1];  // (24 bytes of each)
+  half8_t qh[8], ql[8];
   float sc;
   {
     const float4_t* src = reinterpret_cast<const float4_t*>(qr + row_at * kHeadDim + 8 * hf);
@@ -178,24 +162,9 @@ __global__ __launch_bounds__(kAttnThreads) __attribute__((amdgpu_waves_per_eu(2,
       for (int e = 0; e < 8; ++e) {
         const float x = v[2 * ks + (e >> 2)][e & 3] * to;
         const _Float16 h = static_cast<_Float16>(x);
-        qh[ks][e] = kRest ? h + static_cast<_Float16>(x - x) : h;  // (infinite: not a number, see scaled_keys)
-        if constexpr (!kRest) ql[ks][e] = static_cast<_Float16>(x - static_cast<float>(h));
+        qh[ks][e] = h;
+        ql[ks][e] = static_cast<_Float16>(x - static_cast<float>(h));
       }
-    if constexpr (kRest) {
-#pragma unroll
-      for (int c = 0; c < 4; ++c) {  // against the parts of wave 4 (c / 2) + 2 hf + c % 2: its dims
-        half32_t y;
-#pragma unroll
-        for (int i = 0; i < 16; ++i) {
-          const int ks = (c >> 1) + 2 * (i >> 2), e = 4 * (c & 1) + (i & 3);
-          y[16 + i] = qh[ks][e];
-          y[i] = static_cast<_Float16>((v[2 * ks + (e >> 2)][e & 3] * to - static_cast<float>(qh[ks][e])) * kRestKey);
-        }
-        const uint6_t z = __builtin_amdgcn_cvt_scalef32_pk32_bf6_f16(y, kRestQuery);
-#pragma unroll
-        for (int i = 0; i < 8; ++i) qx[c][i] = i < 6 ? static_cast<int>(z[i < 6 ? i : 0]) : 0;
-      }
-    }
   }
   const KeyItems items = key_items(M, wave, kw);
   {
@@ -310,12 +279,7 @@ __global__ __launch_bounds__(kAttnThreads) __attribute__((amdgpu_waves_per_eu(2,
     const auto times = [&](const uint4& x, int n) {
       const _Float16 p = __builtin_bit_cast(_Float16, static_cast<uint16_t>((n + 15) << 10));
       const half2_t pp = {p, p};
-      const auto one = [&](uint32_t r) {
-        const half2_t x = __builtin_bit_cast(half2_t, r);
-        // (kRest: an infinite radius becomes not a number, as its lo parts are where they are fp16 numbers: infinite
-        // products alone may all have one sign, and a logit of -infinity would drop the row)
-        return __builtin_bit_cast(uint32_t, kRest ? __builtin_elementwise_fma(x, pp, x - x) : x * pp);
-      };
+      const auto one = [&](uint32_t r) { return __builtin_bit_cast(uint32_t, __builtin_bit_cast(half2_t, r) * pp); };
       return make_uint4(one(x.x), one(x.y), one(x.z), one(x.w));
     };
     uint4 r = times(raw.kn, min(up, 15));
@@ -331,53 +295,14 @@ __global__ __launch_bounds__(kAttnThreads) __attribute__((amdgpu_waves_per_eu(2,
     value_lookups<BV>(smem, raw, quarter, va, vb);
     uint8_t* dst = dec + (tt & 63) * (2 * kKStride) + 8 * wave;
     const uint4 radii = scaled_keys();
-    if constexpr (kRest) {
-      key_store_rest(dst, dec + kDecKL + (tt & 63) * (2 * kKStride) + 128 * ((wave >> 1) & 1) + 64 * (wave >> 2) + 32 * (wave & 1),
-                     items, radii, code);
-    } else {
 #pragma unroll
-      for (int j = 0; j < kItemsPer; ++j) key_store(dst + 8 * kAttnWaves * j, items, j, radii, code[j]);
-    }
+    for (int j = 0; j < kItemsPer; ++j) key_store(dst + 8 * kAttnWaves * j, items, j, radii, code[j]);
     v_top = radius_top(v_top, raw.vn);  // (the same in every wave: each has the tile's 64 radii)
     raw.vn = radius_times(raw.vn, radius_up(v_top));
     store_values<BV>(dec, raw, tt, quarter, va, vb);
   };
 
   float16_t s[NB];
-  // (kRest; the scale 2^10 is that of the two powers)
-  const auto products_rest = [&](const uint8_t* dcur) {
-    const int tt = opaque_tid();
-    const uint8_t* kb = dcur + (32 * blk0 + (tt & 31)) * (2 * kKStride) + ((tt & 32) >> 1);
-    const uint8_t* xb = dcur + kDecKL + (32 * blk0 + (tt & 31)) * (2 * kKStride) + 4 * (tt & 32);
-    half8_t ka[3][2];
-    int8_v kx[3];
-    const auto read_keys = [&](int u) {  // a quarter of a 32-token block's dims, and of its remaining parts
-      const uint8_t* at = kb + u % NB * 32 * 2 * kKStride + 64 * (u / NB);
-      ka[u % 3][0] = *reinterpret_cast<const half8_t*>(at + kDecKH);
-      ka[u % 3][1] = *reinterpret_cast<const half8_t*>(at + kDecKH + 32);
-      const uint8_t* rest = xb + u % NB * 32 * 2 * kKStride + 32 * (u / NB);
-      const uint4 a = *reinterpret_cast<const uint4*>(rest);
-      const uint2 b = *reinterpret_cast<const uint2*>(rest + 16);
-      kx[u % 3] = int8_v{static_cast<int>(a.x), static_cast<int>(a.y), static_cast<int>(a.z), static_cast<int>(a.w),
-                         static_cast<int>(b.x), static_cast<int>(b.y), 0, 0};
-    };
-#pragma unroll
-    for (int n = 0; n < NB; ++n)
-#pragma unroll
-      for (int i = 0; i < 16; ++i) s[n][i] = 0.f;
-    read_keys(0);
-    read_keys(1);
-#pragma unroll
-    for (int u = 0; u < 4 * NB; ++u) {
-      if (u + 2 < 4 * NB) read_keys(u + 2);
-      __builtin_amdgcn_sched_barrier(0);
-      const int n = u % NB, c = u / NB;
-      s[n] = __builtin_amdgcn_mfma_f32_32x32x16_f16(ka[u % 3][0], qh[2 * c], s[n], 0, 0, 0);
-      s[n] = __builtin_amdgcn_mfma_f32_32x32x16_f16(ka[u % 3][1], qh[2 * c + 1], s[n], 0, 0, 0);
-      s[n] = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(kx[u % 3], qx[c], s[n], 3, 3, 0, 127 + 10, 0, 127);
-      __builtin_amdgcn_sched_barrier(0);
-    }
-  };
   const auto products_qk = [&](const uint8_t* dcur) {
     const int tt = opaque_tid();
     const uint8_t* kb = dcur + (32 * blk0 + (tt & 31)) * (2 * kKStride) + ((tt & 32) >> 1);
@@ -400,7 +325,7 @@ __global__ __launch_bounds__(kAttnThreads) __attribute__((amdgpu_waves_per_eu(2,
       const int n = u % NB, ks = u / NB;
       s[n] = __builtin_amdgcn_mfma_f32_32x32x16_f16(ka[u % 3][0], qh[ks], s[n], 0, 0, 0);
       s[n] = __builtin_amdgcn_mfma_f32_32x32x16_f16(ka[u % 3][1], qh[ks], s[n], 0, 0, 0);
-      s[n] = __builtin_amdgcn_mfma_f32_32x32x16_f16(ka[u % 3][0], ql[kRest ? 0 : ks], s[n], 0, 0, 0);
+      s[n] = __builtin_amdgcn_mfma_f32_32x32x16_f16(ka[u % 3][0], ql[ks], s[n], 0, 0, 0);
       __builtin_amdgcn_sched_barrier(0);
     }
   };
@@ -550,8 +475,7 @@ __global__ __launch_bounds__(kAttnThreads) __attribute__((amdgpu_waves_per_eu(2,
       load_raw(tile_start(kt + 2));
       read_page(tile_start(kt + 3));
     }
-    if constexpr (kRest) products_rest(dcur);
-    else products_qk(dcur);
+    products_qk(dcur);
     softmax_pv(dcur, t_begin + kt * kKeyTile, k_cur, v_cur);
     if (wave >= 4) {
       decode(dnxt);
