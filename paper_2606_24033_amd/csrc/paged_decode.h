@@ -9,9 +9,9 @@
 // instructions than the decode of the tile.  What differs from the packed decode:
 //  * the rows' pages: a wave reads the page number of a tile one tile ahead of
 //    the loads that need it;
-//  * query rows and value radii are scaled by powers of two (mix.h), and fp32
-//    outputs (EX) have their weights in two fp16 parts and every query product's
-//    lo part, so that both output types have the precision of cross_impl.h;
+//  * query rows and value radii are scaled by powers of two (mix.h), every query
+//    product has its lo part and fp32 outputs (EX) have their weights in two fp16
+//    parts, so that both output types have the precision of cross_impl.h;
 //  * numbers that are not finite are kept (these files are compiled without the
 //    packed decode's no-NaN flags);
 //  * splits leave partials for a join instead of counting one another.
@@ -396,8 +396,7 @@ __attribute__((amdgpu_waves_per_eu((waves_of<NSET, KWB>() / 4)))) void k_paged_d
       const uint32_t* gmt = reinterpret_cast<const uint32_t*>(reinterpret_cast<const uint8_t*>(M->gm) + goff);
 #pragma unroll
       for (int b = 0; b < 8; ++b) {
-        gmb[b] = gmt[b];
-        if constexpr (EX) gmb[b] &= ~(1u << 23);  // every product's lo part
+        gmb[b] = gmt[b] & ~(1u << 23);  // every product's lo part
       }
     }
     float4_t L[NSET];

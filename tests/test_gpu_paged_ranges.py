@@ -119,3 +119,15 @@ def test_a_few_rows_of_a_long_context(rotations, times):
     for t in range(7, 8000, 200):
         enlarge(pool, b, 0, t, keys=times)
     near(f"{times} times", b, q, dq, "bf16")
+
+
+@pytest.mark.parametrize("times", [1, 64, 512])
+@pytest.mark.parametrize("group", [1, 4, 7])
+def test_single_tokens_and_narrow_groups_of_many_times_the_radii(rotations, group, times):
+    """A group of 1 or 2 bits beside wider ones may carry the logits as well as any other."""
+    pool, b, q, dq = paged(rotations, [1] * 6, [500, 64, 130, 700, 400, 333], kv=2, group=group, k_budget=192, v_bits=3, kind="wide")
+    for s, n in enumerate(b.lens):
+        for t in range(0, n, 7):
+            for g in (0, 1):
+                enlarge(pool, b, s, t, keys=times, group=g)
+    near(f"{times} times", b, q, dq, "bf16")
