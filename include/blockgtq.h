@@ -520,8 +520,7 @@ typedef struct {
  * captured in a HIP graph.
  * layer in [0, n_layers).
  * d_q: post-RoPE queries [n_tokens][n_kv_heads*group][128] in in_dtype; d_out:
- *      the same shape in out_dtype, of the precision of blockgtq_cross_attn, but
- *      for bf16 outputs' capped logits, which are off by 2^-23 of the cap.  Both
+ *      the same shape in out_dtype, of the precision of blockgtq_cross_attn.  Both
  *      and the workspace 16-byte aligned (EINVAL otherwise).
  * A page number outside [0, cfg->batch) makes NaN of every output that attends
  * the page's rows, and may of the sequence's other ones in this call.  What

@@ -1316,7 +1316,9 @@ int blockgtq_paged_attn(const bgtq_config* cfg, const void* d_layout, int32_t la
   const Dims d = dims_of(cfg, layer, chunk->max_ctx);
   hipStream_t s = static_cast<hipStream_t>(stream);
   uint8_t* ws = static_cast<uint8_t*>(d_workspace);
-  const ScoreMods mods = scores ? ScoreMods{scores->cap, scores->d_slopes, scores->d_prefix_len} : ScoreMods{0.f, nullptr, nullptr};
+  ScoreMods mods = scores ? ScoreMods{scores->cap, scores->d_slopes, scores->d_prefix_len} : ScoreMods{0.f, nullptr, nullptr};
+  // (a cap of 2^-100 leaves logits that are all 0 in fp32, one of 2^100 those below 2^88 as they are)
+  if (mods.cap > 0.f) mods.cap = std::min(std::max(mods.cap, 0x1p-100f), 0x1p100f);
   for (const PagedPlan* pl : {&p.few, &p.many}) {
     if (!pl->rows) continue;
     CrossCall call = {};

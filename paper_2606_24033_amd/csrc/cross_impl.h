@@ -773,7 +773,7 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(2, 2))
       for (int n = 0; n < 2; ++n)
 #pragma unroll
         for (int i = 0; i < 16; ++i)
-          s[n][i] = paged::changed<EX>(mode.m.cap, slope, s[n][i] * sc, at - static_cast<float>(32 * n + 8 * (i >> 2) + (i & 3)));
+          s[n][i] = paged::changed(mode.m.cap, slope, s[n][i] * sc, at - static_cast<float>(32 * n + 8 * (i >> 2) + (i & 3)));
     }
 
     // ---- online softmax, base 2

@@ -349,7 +349,7 @@ __global__ __launch_bounds__(kAttnThreads) __attribute__((amdgpu_waves_per_eu(2,
       for (int n = 0; n < NB; ++n)
 #pragma unroll
         for (int i = 0; i < 16; ++i)
-          s[n][i] = paged::changed<EX>(mode.m.cap, slope, s[n][i] * st,
+          s[n][i] = paged::changed(mode.m.cap, slope, s[n][i] * st,
                                        at - static_cast<float>(32 * (blk0 + n) + 8 * (i >> 2) + (i & 3)));
       st = 1.f;
     }

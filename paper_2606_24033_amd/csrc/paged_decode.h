@@ -436,7 +436,7 @@ __attribute__((amdgpu_waves_per_eu((waves_of<NSET, KWB>() / 4)))) void k_paged_d
 #pragma unroll
       for (int r = 0; r < 4; ++r) {
         x[r] *= back[s][r];
-        if constexpr (MODS) x[r] = paged::changed<EX>(mode.m.cap, slope[s][r], x[r], static_cast<float>(pos - tk));
+        if constexpr (MODS) x[r] = paged::changed(mode.m.cap, slope[s][r], x[r], static_cast<float>(pos - tk));
       }
       if (!full) {
         if (tk >= t_end) x = float4_t{kNegInf, kNegInf, kNegInf, kNegInf};

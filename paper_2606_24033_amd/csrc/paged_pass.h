@@ -106,33 +106,27 @@ __device__ __forceinline__ uint2 seen(const uint2& r, int left) {
 }
 
 // A base-2 logit x = log2 e q k / sqrt(d) after the cap, C tanh(x / C) with
-// C = cap log2 e, and the bias, -slope |distance|.
-//  * fp32 outputs (EX): x P(z) / Q(z), z = (x / C)^2, |x| up to 8.2 C, beyond
-//    which tanh is 1 to 2^-22.6.  P and Q of degree 4 are the least largest
-//    relative error of tanh(y) / y up to there (8e-9; fitted by reweighted least
-//    squares); in fp32 2^-21.7.  One transcendental instruction and 15 others.
-//  * bf16 outputs: tanh(y) = (1 - t) / (1 + t), t = 2^(-2 |y| log2 e), which is
-//    off by 2^-24 C for small logits: 4e-6 at a cap of 50, nothing beside the
-//    rounding to bf16.
-template <bool EX>
+// C = cap log2 e, and the bias, -slope |distance|.  The cap is x P(z) / Q(z),
+// z = (x / C)^2, |x| up to 8.2 C, beyond which tanh is 1 to 2^-22.6.  P and Q of
+// degree 4 are the least largest relative error of tanh(y) / y up to there (8e-9;
+// fitted by reweighted least squares); in fp32 2^-21.7, whatever the cap.  One
+// transcendental instruction and 15 others.  (1 - t) / (1 + t), t = 2^(-2 |y| log2 e),
+// has two and 7, but loses 2^-24 C of small logits: all of them at a cap of 1e7.
+// cap: 2^-100 .. 2^100 (0: none), so that C, 1 / C and 8.2 C are normal numbers; a
+// cap beyond either end changes no output that one at the end does not.
 __device__ __forceinline__ float changed(float cap, float slope, float x, float distance) {
   constexpr float kLog2 = 1.4426950408889634f;
   if (cap > 0.f) {
     const float c = cap * kLog2, inv = 1.f / c;
-    if constexpr (EX) {
-      const float xc = fminf(fmaxf(x, -8.2f * c), 8.2f * c), y = xc * inv, z = y * y;
-      float p = fmaf(z, 1.4842521e-08f, 2.1638720e-05f), q = fmaf(z, 8.3714156e-07f, 3.3865857e-04f);
-      p = fmaf(z, p, 3.5567754e-03f);
-      q = fmaf(z, q, 2.6108639e-02f);
-      p = fmaf(z, p, 0.13432199f);
-      q = fmaf(z, q, 0.46765524f);
-      p = fmaf(z, p, 1.f);
-      q = fmaf(z, q, 1.f);
-      x = x == x ? xc * p * __builtin_amdgcn_rcpf(q) : x;  // (the bounds pass over what is not a number)
-    } else {
-      const float y = x * inv, t = __builtin_amdgcn_exp2f(-2.f * kLog2 * fabsf(y));
-      x = copysignf(c * ((1.f - t) * __builtin_amdgcn_rcpf(1.f + t)), y);
-    }
+    const float xc = fminf(fmaxf(x, -8.2f * c), 8.2f * c), y = xc * inv, z = y * y;
+    float p = fmaf(z, 1.4842521e-08f, 2.1638720e-05f), q = fmaf(z, 8.3714156e-07f, 3.3865857e-04f);
+    p = fmaf(z, p, 3.5567754e-03f);
+    q = fmaf(z, q, 2.6108639e-02f);
+    p = fmaf(z, p, 0.13432199f);
+    q = fmaf(z, q, 0.46765524f);
+    p = fmaf(z, p, 1.f);
+    q = fmaf(z, q, 1.f);
+    x = x == x ? xc * p * __builtin_amdgcn_rcpf(q) : x;  // (the bounds pass over what is not a number)
   }
   return fmaf(-slope, fabsf(distance), x);
 }

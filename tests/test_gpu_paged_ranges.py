@@ -57,9 +57,9 @@ def paged(rotations, news, lens, kv=1, group=4, **kw):
     return pool, b, *pool.queries((b.n,))
 
 
-def near(what, b, q, dq, out, **kw):
-    got = bg.blockgtq_paged_attn(b.pool.cfg, b.pool.layout, 0, dq, b.chunk, b.pool.cache, out_dtype=typed(out), **kw)
-    ref, bound = expect(b, q, typed(out))
+def near(what, b, q, dq, out, cap=0.0):
+    got = bg.blockgtq_paged_attn(b.pool.cfg, b.pool.layout, 0, dq, b.chunk, b.pool.cache, out_dtype=typed(out), cap=cap)
+    ref, bound = expect(b, q, typed(out), cap=cap)
     check(what, got, ref, bound)
     size = np.linalg.norm(ref)
     off = np.linalg.norm(got.double().cpu().numpy() - ref) / size
@@ -131,3 +131,12 @@ def test_single_tokens_and_narrow_groups_of_many_times_the_radii(rotations, grou
             for g in (0, 1):
                 enlarge(pool, b, s, t, keys=times, group=g)
     near(f"{times} times", b, q, dq, "bf16")
+
+
+@pytest.mark.parametrize("news,lens", [([1, 1], [300, 64]), ([8], [300]), ([200], [500])])
+@pytest.mark.parametrize("out", ["bf16", "fp32"])
+@pytest.mark.parametrize("cap", [1e-40, 1e-20, 1e-3, 1.0, 50.0, 1e3, 1e5, 1e7, 1e20, 3.2e38])
+def test_caps_of_every_size(rotations, cap, out, news, lens):
+    """From a cap that leaves no difference between the rows to one that changes nothing, as exact as without it."""
+    pool, b, q, dq = paged(rotations, news, lens)
+    near(f"cap {cap}", b, 4 * q, 4 * dq, out, cap=cap)
