@@ -530,7 +530,10 @@ typedef struct {
  * sets, also one that only later tokens see, and hold a coordinate to 2^-37 of
  * what that radius gives.  A radius that is not finite in a row that a token sees
  * makes its outputs NaN.
- * n_splits: 0 = heuristic, else the splits of the key axis (1 .. 4096).
+ * n_splits: 0 = heuristic, else the splits of the key axis (1 .. 4096).  A pass
+ *      in splits leaves a partial of 528 bytes for each query row and split (the
+ *      pass of single tokens: n_seqs tokens' rows; the other one n_tokens');
+ *      the heuristic spends 64 MiB on a pass's at most.
  * d_workspace: blockgtq_paged_workspace_bytes bytes for the chunk's sizes, any
  *      contents; calls that share it must not overlap in time.
  * EUNSUPPORTED above 2^24 query rows (n_tokens x heads) or 2^30 rows. */

@@ -1206,7 +1206,7 @@ int blockgtq_paged_append(const bgtq_config* cfg, const void* d_layout, int32_t 
 
 // One pass of a call over pages (none: no rows).
 struct PagedPlan {
-  int rows, n_splits, split_len, lo, hi, unit_rows;
+  int rows, n_splits, split_len, lo, hi, most;
   bool direct;
   long blocks, items;
   size_t part_bytes;
@@ -1216,25 +1216,37 @@ struct PagedPlans {
   size_t bytes;
 };
 
+// What partials of a pass the heuristic spends at most: 256 workgroups of 256
+// query rows leave half of it.
+static const size_t kMaxPartBytes = size_t{64} << 20;
+
 // Rows of the workgroups and splits of a pass, by the estimates of cross_plan.
 // The host knows bounds only: `blocks` workgroups' rows at most, lengths of
 // max_len at most; a chunk's early rows see fewer (seen: the mean share).
-// likely: sequences that the pass has rows of, for the estimate.
+// likely: sequences that the pass has rows of, for the estimate.  Without a
+// requested number, only splits whose workgroups fit a launch and whose partials
+// fit kMaxPartBytes.
 static PagedPlan paged_pass_plan(const Dims& d, std::initializer_list<int> widths, long n_seqs, double likely, long n_rows,
-                                 long max_rows, int max_len, double seen, int lo, int hi, int requested) {
+                                 long max_rows, int max_len, double seen, int lo, int hi, int requested, long n_tokens) {
   PagedPlan best = {};
   double t_best = 0.0;
   const int tiles = std::max(1, (max_len + 63) / 64);
   for (const int rows : widths) {
-    // a sequence's last block may be part empty; one block each at least
-    const long seqs = std::min(n_seqs, n_rows / (lo + 1));
+    // a sequence's last block may be part empty; one block each at least (one
+    // whose numbers make no sense, too, in the pass of the smallest)
+    const long seqs = lo == 0 ? n_seqs : std::min(n_seqs, n_rows / (lo + 1));
     const long blocks = max_rows <= rows ? n_seqs : std::min(seqs * ((max_rows + rows - 1) / rows), (n_rows + seqs * (rows - 1)) / rows);
     const bool direct = max_rows <= rows;
+    const int most = static_cast<int>(max_rows / d.group);
+    const size_t part_rows = static_cast<size_t>(direct ? n_seqs * most : n_tokens) * d.n_kv * d.group;
     const double est = d.n_kv * (direct || seqs == 1 ? static_cast<double>(blocks) : n_rows / rows + 0.5 * likely);
     const int k0 = requested > 0 ? std::min(requested, tiles) : 1;
     const int k1 = requested > 0 ? k0 : std::min(rows <= 32 ? (tiles + 7) / 8 : tiles, 256);
     for (int k = k0; k <= std::max(k0, k1); ++k) {
       const int len = (tiles + k - 1) / k, n = (tiles + len - 1) / len;
+      const long items = blocks * d.n_kv * n;
+      const size_t part_bytes = n > 1 ? al256(part_rows * n * kPartFloats * 4) : 0;
+      if (requested == 0 && (items > kMaxItems || part_bytes > kMaxPartBytes) && best.rows) continue;
       const double busy = 1.0 + 0.3 * std::min(1.0, est * n / 256.0);
       const int waves = d.group <= 4 && d.k_words <= 16 ? 16 : 12;  // (8 rows)
       const double wg = rows == 8 ? 10.0 + (d.k_words <= 16 ? 4.5 : 7.0) * ((len + waves - 1) / waves) : rows == 32 ? 13.0 + (d.k_words <= 8 ? 5.4 : d.k_words <= 16 ? 6.2 : 13.0) * ((len + 7) / 8)
@@ -1243,14 +1255,12 @@ static PagedPlan paged_pass_plan(const Dims& d, std::initializer_list<int> width
       // unequal workgroups follow one another without rounds
       if (n_seqs > 1 || seen < 0.9) t = std::max(wg, 0.5 * t * seen + 0.5 * (0.65 * seen * est * n / 256 * wg + 0.5 * wg));
       if (n > 1) t += 5.0 + 2.4e-7 * kPartFloats * 4 * n_rows * d.n_kv * n;
-      if (!best.rows || t < t_best) {
+      if (!best.rows || t < t_best || (requested == 0 && best.items > kMaxItems && items <= kMaxItems)) {
         t_best = t;
-        best = {rows, n, 64 * len, lo, hi, direct ? static_cast<int>(std::min<long>((max_rows + 3) / 4 * 4, rows)) : rows,
-                direct, blocks, blocks * d.n_kv * n, 0};
+        best = {rows, n, 64 * len, lo, hi, most, direct, blocks, items, part_bytes};
       }
     }
   }
-  best.part_bytes = best.n_splits > 1 ? al256(static_cast<size_t>(best.blocks) * d.n_kv * best.unit_rows * best.n_splits * kPartFloats * 4) : 0;
   return best;
 }
 
@@ -1260,7 +1270,7 @@ static PagedPlans paged_plans(const bgtq_config* cfg, int n_seqs, int n_tokens, 
   const long rows = static_cast<long>(n_tokens) * d.group, max_rows = static_cast<long>(max_new) * d.group;
   const int all = 0x7FFFFFFF;
   if (max_new == 1) {
-    p.few = paged_pass_plan(d, {8}, n_seqs, n_seqs, rows, max_rows, max_ctx, 1.0, 0, all, n_splits);
+    p.few = paged_pass_plan(d, {8}, n_seqs, n_seqs, rows, max_rows, max_ctx, 1.0, 0, all, n_splits, n_tokens);
   } else {
     // sequences beside the longest that have a token or two each, on average:
     // single tokens in a pass of their own, with splits of their own
@@ -1268,12 +1278,12 @@ static PagedPlans paged_plans(const bgtq_config* cfg, int n_seqs, int n_tokens, 
     const int lo = both ? d.group : 0;
     if (both)
       p.few = paged_pass_plan(d, {8}, n_seqs, n_seqs, std::min(rows, static_cast<long>(d.group) * n_seqs), d.group, max_ctx,
-                              1.0, 0, d.group, n_splits);
+                              1.0, 0, d.group, n_splits, n_tokens);
     // (as few sequences as the rest of the tokens can be)
     const double likely = both ? std::max(1.0, (n_tokens - n_seqs) / (max_new - 1.0)) : n_seqs;
     const double seen = 1.0 - 0.5 * max_new / std::max(max_ctx, 1);
     const auto many = [&](std::initializer_list<int> widths) {
-      p.many = paged_pass_plan(d, widths, n_seqs, likely, rows, max_rows, max_ctx, seen, lo, all, n_splits);
+      p.many = paged_pass_plan(d, widths, n_seqs, likely, rows, max_rows, max_ctx, seen, lo, all, n_splits, n_tokens);
     };
     if (max_rows <= 32) many({32});
     else if (max_rows <= 64) many({32, 128});
@@ -1309,10 +1319,9 @@ int blockgtq_paged_attn(const bgtq_config* cfg, const void* d_layout, int32_t la
   if (!aligned16(d_q) || !aligned16(d_out) || !aligned16(d_workspace))
     return fail(BGTQ_EINVAL, "q, out and the workspace must be 16-byte aligned");
   const PagedPlans p = paged_plans(cfg, chunk->n_seqs, chunk->n_tokens, chunk->max_new, chunk->max_ctx, n_splits);
+  for (const PagedPlan* pl : {&p.few, &p.many})
+    if (pl->items > kMaxItems) return fail(BGTQ_EUNSUPPORTED, "too many splits of too many query rows");
   if (ws_bytes < p.bytes) return fail(BGTQ_EWORKSPACE, "workspace %zu bytes < %zu needed", ws_bytes, p.bytes);
-  for (const PagedPlan* pl : {&p.few, &p.many})  // (workgroups of a pass, and of its join of 4 rows each)
-    if (pl->items > kMaxItems || (pl->n_splits > 1 && pl->blocks * cfg->n_kv_heads * (pl->unit_rows / 4) > kMaxItems))
-      return fail(BGTQ_EUNSUPPORTED, "too many splits of too many query rows");
   const Dims d = dims_of(cfg, layer, chunk->max_ctx);
   hipStream_t s = static_cast<hipStream_t>(stream);
   uint8_t* ws = static_cast<uint8_t*>(d_workspace);
@@ -1335,7 +1344,7 @@ int blockgtq_paged_attn(const bgtq_config* cfg, const void* d_layout, int32_t la
       hipError_t e = launch_paged_rotation(d, d_layout, d_q, chunk->n_tokens, call.qr, s);
       if (e != hipSuccess) return hip_fail(e, "paged_attn rotation launch");
     }
-    const PagedPass pass = {paged_batch(chunk), mods, static_cast<int>(pl->blocks), pl->lo, pl->hi, pl->unit_rows, pl->direct};
+    const PagedPass pass = {paged_batch(chunk), mods, static_cast<int>(pl->blocks), pl->lo, pl->hi, pl->most, pl->direct};
     hipError_t e = launch_paged_pass(d, d_layout, d_q, call, pass, s);
     if (e != hipSuccess) return hip_fail(e, "paged_attn launch");
   }

@@ -29,6 +29,7 @@ namespace {
 using namespace cross_detail;
 
 struct RowsInOrder {  // partials of the output's rows, one after the other
+  template <int RW>
   __device__ __forceinline__ bool begin(long) { return true; }
   __device__ __forceinline__ long out_row(long r) const { return r; }
 };

@@ -449,7 +449,7 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(2, 2))
   };
   const auto part_of = [&](int r) {  // its partial
     if constexpr (kPaged)
-      return call.part + (((static_cast<size_t>(U.block) * d.n_kv + kvh) * mode.unit_rows + (r - r0)) * call.n_slots + split) * kPartFloats;
+      return call.part + (paged::part_row(mode, U, hq, r / G, kvh * G + r % G) * call.n_slots + split) * kPartFloats;
     else return call.part + (row_at(r) * call.n_slots + S.slot0 + split) * kPartFloats;
   };
 

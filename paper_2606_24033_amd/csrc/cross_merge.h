@@ -17,9 +17,9 @@ constexpr long kMergeGrid = 512;  // workgroups of a join of many rows: the two 
 // the partials where there are many (32768 rows x 2 slots, 43 MB read and
 // written, 18 us: 2.4 TB/s), by its latency (5 us) otherwise.
 //
-// MAP: where a row's partials belong.  begin(r), with the whole workgroup: the
-// first of the block's rows, false where none is to be joined; out_row(r): the
-// row of the output, -1 for none.
+// MAP: where a row's partials belong.  begin<RW>(r), with the whole workgroup: the
+// first of the block's rows, false where none is to be joined; out_row(r), in lane
+// r % 16 of each quarter of a wave: the row of the output, -1 for none.
 template <int RW, class MAP>
 __global__ __launch_bounds__(kThreads) void k_cross_merge(const uint8_t* __restrict__ blob, const float* __restrict__ part,
                                                           int n_slots, long n_rows, void* __restrict__ out, int out_dtype, MAP map) {
@@ -48,7 +48,7 @@ __global__ __launch_bounds__(kThreads) void k_cross_merge(const uint8_t* __restr
   int buf = 0;
   bool ready = false;
   for (long block = blockIdx.x; block * RW < n_rows; block += RW == 16 ? static_cast<long>(gridDim.x) : n_rows) {
-    if (!map.begin(block * RW)) continue;
+    if (!map.template begin<RW>(block * RW)) continue;
     if (RW != 16 || !ready) {
       matrix();
       if (RW == 16) parts();  // (else behind the partials' reads)

@@ -102,7 +102,8 @@ __global__ __launch_bounds__(kAttnThreads) __attribute__((amdgpu_waves_per_eu(2,
   const int rc = min(r, nr - 1);
   const size_t row_at = ((kPaged ? static_cast<size_t>(U.q.first) : static_cast<size_t>(lz) * S.n_q) + rc / G) * hq + kvh * G + rc % G;
   const auto part_of = [&]() {
-    if constexpr (kPaged) return call.part + (((static_cast<size_t>(U.block) * d.n_kv + kvh) * mode.unit_rows + (rc - first)) * call.n_slots + split) * kPartFloats;
+    if constexpr (kPaged)
+      return call.part + (paged::part_row(mode, U, hq, rc / G, kvh * G + rc % G) * call.n_slots + split) * kPartFloats;
     else return call.part + (row_at * call.n_slots + S.slot0 + split) * kPartFloats;
   };
 

@@ -167,13 +167,15 @@ struct ScoreMods {
   const int32_t* prefix;  // [n_seqs] or null
 };
 // One pass over pages (paged_pass.h): blocks of the sequences with lo < query
-// rows <= hi.  Its CrossCall has one side: the pool.  Partials lie
-// [n_blocks][n_kv][unit_rows][n_slots].
+// rows <= hi.  Its CrossCall has one side: the pool.  Partials lie in the order
+// of the output's rows, [n_tokens][Hq][n_slots], or (direct: a sequence has one
+// block, block = sequence) [n_seqs][most][Hq][n_slots].
 struct PagedPass {
   PagedBatch b;
   ScoreMods m;
-  int n_blocks, lo, hi, unit_rows;
-  bool direct;  // block = sequence
+  int n_blocks, lo, hi;
+  int most;  // new tokens of a sequence of the pass at most
+  bool direct;
 };
 // A pass and the join of its splits (paged.hip), by the query rows of a workgroup (call.rows0): 8, of
 // single tokens (paged_decode.h); 32 (cross_impl.h); 128 or 256, on the rotated query rows call.qr

@@ -100,22 +100,23 @@ __device__ __forceinline__ int find_item(const PagedBatch& b, int want, const F&
   return -1;
 }
 
-// Page (-1: none) and place of input row r0 + tk of a ragged batch, r0 the same
-// in the wave, tk < ROWS.  64 sequences at a time, one ballot where one of them
-// claims all the rows, one for each row where they claim some (16384 rows of a
-// prompt x 8 heads: 3 us less than with those alone).
-template <int ROWS = 16>
-__device__ __forceinline__ int2 page_of_row(const PagedBatch& b, int n_pages, int page_rows, int r0, int tk) {
+// The sequence that input row r0 + tk of a ragged batch belongs to (-1: none), r0
+// the same in the wave, tk < ROWS; rows from number `need` on are of no interest.
+// 64 sequences at a time, one ballot where one of them claims all the rows, one
+// for each row where they claim some (16384 rows of a prompt x 8 heads: 3 us less
+// than with those alone).
+template <int ROWS>
+__device__ __forceinline__ int seq_of_row(const PagedBatch& b, int r0, int tk, int need, Seq& seq) {
   const int lane = threadIdx.x & 63, last = b.n_seqs - 1;
-  int seq = -1, t = 0;  // of the lane's row: its sequence, its place there
+  int at = -1;
   Apart apart;
   for (int base = 0; base <= last; base += 64) {
     const int s = min(base + lane, last), c0 = b.cu[s], c1 = b.cu[s + 1];
     Seq q = make_seq(b, c0, c1, b.ctx[s]);
     apart.keep(b, c0, c1, q);
-    const bool any = base + lane <= last && q.ok && c1 > r0 && c0 - ROWS < r0;
+    const bool any = base + lane <= last && q.ok && c1 > r0 && c0 - need < r0;
     if (__builtin_amdgcn_ballot_w64(any) != 0) {
-      const uint64_t all = __builtin_amdgcn_ballot_w64(any && c0 <= r0 && c1 - ROWS >= r0);
+      const uint64_t all = __builtin_amdgcn_ballot_w64(any && c0 <= r0 && c1 - need >= r0);
       int l = -1;
       if (all != 0) {
         l = __builtin_ctzll(all);
@@ -128,14 +129,24 @@ __device__ __forceinline__ int2 page_of_row(const PagedBatch& b, int n_pages, in
       }
       const int from = max(l, 0), first = __shfl(q.first, from), n = __shfl(q.n, from), len = __shfl(q.len, from);
       if (l >= 0) {
-        seq = base + l;
-        t = len - n + r0 + tk - first;
+        at = base + l;
+        seq = {first, n, len, true};
       }
     }
-    if (__builtin_amdgcn_ballot_w64(seq < 0) == 0 || apart.high >= r0 + ROWS) break;  // (what follows starts behind `high`)
+    // (what follows starts behind `high`)
+    if (__builtin_amdgcn_ballot_w64(at < 0 && tk < need) == 0 || apart.high >= r0 + need) break;
   }
-  if (seq < 0) return make_int2(-1, 0);
-  return make_int2(page_of(b, n_pages, page_rows, seq, t), t % page_rows);
+  return at;
+}
+
+// Page (-1: none) and place of input row r0 + tk.
+template <int ROWS = 16>
+__device__ __forceinline__ int2 page_of_row(const PagedBatch& b, int n_pages, int page_rows, int r0, int tk) {
+  Seq q = {};
+  const int s = seq_of_row<ROWS>(b, r0, tk, ROWS, q);
+  if (s < 0) return make_int2(-1, 0);
+  const int t = q.len - q.n + r0 + tk - q.first;
+  return make_int2(page_of(b, n_pages, page_rows, s, t), t % page_rows);
 }
 
 // Value tile `want` of the new rows of a ragged batch: its page (-1: none), the

@@ -14,34 +14,58 @@ namespace {
 
 using namespace cross_detail;
 
-// Partials [block][KV head][row of the unit]: those of rows that a sequence has.
-template <int R>
-struct UnitRows {
+// Partials in the order of the output's rows: those of the pass's sequences.
+// (With the whole wave; a lane works out row number lane % 16 of the block.)
+struct TokenRows {
   PagedPass pass;
-  int n_kv, group;
-  paged::Unit u;
-  __device__ __forceinline__ bool begin(long r) {
-    const int unit = static_cast<int>(r / pass.unit_rows), first = static_cast<int>(r % pass.unit_rows);
-    u.kvh = unit % n_kv;
-    return paged::find_block<R>(pass, group, unit / n_kv, u) && u.q.ok && u.r0 + first < u.q.n * group;
+  int hq, group;
+  long mine;
+  template <int RW>
+  __device__ __forceinline__ bool begin(long r0) {
+    const int tk = threadIdx.x & 15, t0 = static_cast<int>(r0 / hq), need = static_cast<int>((r0 + RW - 1) / hq) - t0 + 1;
+    paged::Seq q = {};
+    const int s = paged::seq_of_row<16>(pass.b, t0, tk, need, q), rows = q.n * group;
+    const uint64_t live = __builtin_amdgcn_ballot_w64(s >= 0 && rows > pass.lo && rows <= pass.hi);
+    const long r = r0 + tk;
+    mine = tk < RW && (live >> static_cast<int>(r / hq - t0) & 1) ? r : -1;
+    return __builtin_amdgcn_ballot_w64(mine >= 0) != 0;
   }
-  __device__ __forceinline__ long out_row(long r) const {
-    const int i = u.r0 + static_cast<int>(r % pass.unit_rows);
-    return i < u.q.n * group ? (static_cast<long>(u.q.first) + i / group) * n_kv * group + u.kvh * group + i % group : -1;
+  __device__ __forceinline__ long out_row(long) const { return mine; }
+};
+// Partials [sequence][token][head].
+struct SeqRows {
+  PagedPass pass;
+  int hq, group;
+  long n_rows;
+  long mine;
+  template <int RW>
+  __device__ __forceinline__ bool begin(long r0) {
+    const int tk = threadIdx.x & 15;
+    const long r = min(r0 + tk, n_rows - 1);
+    const int t = static_cast<int>(r / hq), s = t / pass.most, i = t - s * pass.most;
+    const paged::Seq q = paged::seq_of(pass.b, s);
+    const int rows = q.n * group;
+    const bool live = tk < RW && r0 + tk < n_rows && q.ok && i < q.n && rows > pass.lo && rows <= pass.hi;
+    mine = live ? static_cast<long>(q.first + i) * hq + r % hq : -1;
+    return __builtin_amdgcn_ballot_w64(live) != 0;
   }
+  __device__ __forceinline__ long out_row(long) const { return mine; }
 };
 
-template <int R>
 hipError_t join(const Dims& d, const void* layout, const CrossCall& call, const PagedPass& pass, hipStream_t s) {
-  const long rows = static_cast<long>(pass.n_blocks) * d.n_kv * pass.unit_rows;
-  const UnitRows<R> map{pass, d.n_kv, d.group, {}};
-  const auto go = [&](auto kern, long blocks) {
+  const int hq = d.n_kv * d.group;
+  const long rows = (pass.direct ? static_cast<long>(pass.b.n_seqs) * pass.most : static_cast<long>(pass.b.n_tokens)) * hq;
+  const auto go = [&](auto kern, long blocks, auto map) {
     hipLaunchKernelGGL(kern, dim3(blocks), dim3(kThreads), 0, s, static_cast<const uint8_t*>(layout), call.part, call.n_slots,
                        rows, call.out, call.out_dtype, map);
     return hipGetLastError();
   };
-  if (rows >= 16 * 256 && pass.unit_rows % 16 == 0) return go(k_cross_merge<16, UnitRows<R>>, std::min(kMergeGrid, rows / 16));
-  return go(k_cross_merge<4, UnitRows<R>>, rows / 4);
+  const auto width = [&](auto map) {
+    using M = decltype(map);
+    if (rows >= 16 * 256) return go(k_cross_merge<16, M>, std::min(kMergeGrid, (rows + 15) / 16), map);
+    return go(k_cross_merge<4, M>, (rows + 3) / 4, map);
+  };
+  return pass.direct ? width(SeqRows{pass, hq, d.group, rows, -1}) : width(TokenRows{pass, hq, d.group, -1});
 }
 
 // The query rotation of fp32 rows, as launch_query_rotation's but on the dense
@@ -146,9 +170,7 @@ hipError_t launch_paged_pass(const Dims& d, const void* layout, const void* q, c
     }
   }
   if (e != hipSuccess || call.n_slots == 1) return e;
-  if (call.rows0 == 8) return join<8>(d, layout, call, pass, s);
-  return call.rows0 == 32 ? join<32>(d, layout, call, pass, s)
-                          : call.rows0 == 128 ? join<128>(d, layout, call, pass, s) : join<256>(d, layout, call, pass, s);
+  return join(d, layout, call, pass, s);
 }
 
 }  // namespace bgtq

@@ -183,7 +183,7 @@ __attribute__((amdgpu_waves_per_eu((waves_of<NSET, KWB>() / 4)))) void k_paged_d
   const int kvh = U.kvh, split = U.split;
   const size_t out_row = static_cast<size_t>(U.q.first) * hq + kvh * G;  // head 0's row of q and out
   const int t_begin = split * S.split_len, t_end = min(U.q.len, t_begin + S.split_len), pos = U.q.len - 1;
-  float* const part = call.part + ((static_cast<size_t>(U.block) * d.n_kv + kvh) * mode.unit_rows * call.n_slots + split) * kPartFloats;
+  float* const part = call.part + (paged::part_row(mode, U, hq, 0, kvh * G) * call.n_slots + split) * kPartFloats;
   const size_t part_step = static_cast<size_t>(call.n_slots) * kPartFloats;  // from a head's partial to the next one's
   if (t_begin >= t_end) {  // (more than one split: a sequence has a row at least)
     if (tid < G) {

@@ -36,9 +36,14 @@ __device__ __forceinline__ int page_ahead(const PagedBatch& b, int seq, int t, i
 }
 
 struct Unit {
-  int seq, block, r0, kvh, split;  // block: its number in the pass; r0: its first query row
+  int seq, r0, kvh, split;  // r0: its first query row
   Seq q;
 };
+
+// The place among the partials of new token i's head `head` (of hq).
+__device__ __forceinline__ size_t part_row(const PagedPass& p, const Unit& u, int hq, int i, int head) {
+  return (p.direct ? static_cast<size_t>(u.seq) * p.most + i : static_cast<size_t>(u.q.first + i)) * hq + head;
+}
 
 // A sequence's blocks of R query rows in the pass.  (One whose numbers make no
 // sense has one in the pass of the smallest, which answers for it.)
@@ -51,7 +56,6 @@ __device__ __forceinline__ int blocks_of(const PagedPass& p, int group, const Se
 
 template <int R>
 __device__ __forceinline__ bool find_block(const PagedPass& p, int group, int block, Unit& u) {
-  u.block = block;
   if (p.direct) {  // no sequence has more than one block
     u.seq = block;
     u.q = seq_of(p.b, block);

@@ -189,3 +189,20 @@ def test_attention_of_a_batch_whose_offsets_fall(rotations, news, lens):
                     if fine and i in rows:
                         near |= np.abs(x[i] - refs[s][0][i]) <= refs[s][1][i]
                 assert near.all(), (cu, splits, i)
+
+
+@pytest.mark.parametrize("splits", [0, 1, 3])
+@pytest.mark.parametrize("news", [[1] * 200 + [300] + [1] * 130 + [0] * 70 + [2], [3] * 90 + [0] * 200 + [250, 1, 40] + [5] * 70,
+                                  [4] * 150 + [0] * 90 + [1] * 10])
+def test_hundreds_of_sequences(rotations, news, splits):
+    """Chunks among single tokens and empty sequences, over several reads of 64: every row by the formula."""
+    lens = [n + (13 * i) % 80 for i, n in enumerate(news)]
+    pool = Packed(rotations, 9, batch=sum((t + 63) // 64 for t in lens) + 1, kv=2, group=3, cap=64)
+    b = Batch(pool, news, lens, seed=5, pad=7)
+    q, dq = pool.queries((b.n,))
+    ref, bound = expect(b, q, torch.float32)
+    got = torch.full((b.n, 6, D), 7.0, device="cuda")
+    bg.blockgtq_paged_attn(pool.cfg, pool.layout, 0, dq, b.chunk, pool.cache, out=got, n_splits=splits)
+    live = int(b.first[-1])
+    check(f"{len(news)} sequences", got[:live], ref[:live], bound[:live])
+    assert (got[live:] == 7.0).all()
