@@ -348,8 +348,8 @@ int blockgtq_decode_attn_noalloc(const bgtq_config* cfg, const void* d_layout, i
  * Every group's dims are computed with that group's radius alone.  A radius that
  * is not finite (a norm past fp16's range) gives numbers that are not finite: in
  * its group's dims of the key, or in the whole value row, and nowhere else.
- * n_rows in [0, capacity] (ECAPACITY above).  EUNSUPPORTED above 2^21 heads of the
- * call's layers, or 2^30 tiles of 32 rows over all sequences. */
+ * n_rows in [0, capacity] (ECAPACITY above).  EUNSUPPORTED from 2^21 heads of the
+ * call's layers on, or above 2^30 tiles of 32 rows over all sequences. */
 int blockgtq_dequantize_rows(const bgtq_config* cfg, const void* d_layout, int32_t layer, const bgtq_cache* cache,
                              int32_t n_rows, const int32_t* d_read_pos, const int32_t* d_ctx_len, void* d_k_out,
                              void* d_v_out, int32_t out_dtype, void* stream);

@@ -872,7 +872,7 @@ int blockgtq_dequantize_rows(const bgtq_config* cfg, const void* d_layout, int32
   if (!aligned16(d_k_out) || !aligned16(d_v_out)) return fail(BGTQ_EINVAL, "k_out and v_out must be 16-byte aligned");
   // (a workgroup for each layer's and head's keys and values at least; the sequences' tiles are numbered in 32 bits)
   const double units = static_cast<double>(layer < 0 ? cfg->n_layers : 1) * cfg->n_kv_heads;
-  if (2.0 * units > static_cast<double>(kMaxItems)) return fail(BGTQ_EUNSUPPORTED, "%.0f layers' heads in one call", units);
+  if (2.0 * units >= static_cast<double>(kMaxItems)) return fail(BGTQ_EUNSUPPORTED, "%.0f layers' heads in one call", units);
   if (static_cast<double>(cfg->batch) * (n_rows / kTile + 2) > static_cast<double>(1l << 30))
     return fail(BGTQ_EUNSUPPORTED, "%d rows of %d sequences in one call", n_rows, cfg->batch);
   hipError_t e = launch_dequantize_rows(dims_of(cfg, layer), d_layout, cache_ptrs(cache), n_rows, d_read_pos,
