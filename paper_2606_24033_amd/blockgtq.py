@@ -143,17 +143,23 @@ class Config:
     head_dim: int = HEAD_DIM
 
     def __setattr__(self, name, value):
-        self.__dict__.pop("_made", None)
         object.__setattr__(self, name, value)
+        self.__dict__.pop("_made", None)  # (behind the field: a call of another thread in between makes what it pops)
 
     def _make(self):
         """What the calls need of the fields, made again after one is set: the C struct, and the cache tensors' shapes."""
-        C, lead = self.capacity, (self.n_layers, self.batch, self.n_kv_heads)
-        made = (_Config(self.n_layers, self.batch, self.n_kv_heads, self.group, self.head_dim,
-                        self.capacity, self.k_budget, self.v_bits, self.in_dtype),
-                (lead + (C, self.k_words), lead + (C * MAX_GROUPS,), lead + (C // 32, HEAD_DIM, self.v_bits), lead + (C,)))
-        self.__dict__["_made"] = made
-        return made
+        while True:
+            layers, batch, kv, group, dim, C, budget, v_bits, dtype = was = self._fields()
+            lead = (layers, batch, kv)
+            made = (_Config(layers, batch, kv, group, dim, C, budget, v_bits, dtype),
+                    (lead + (C, self.k_words), lead + (C * MAX_GROUPS,), lead + (C // 32, HEAD_DIM, v_bits), lead + (C,)))
+            self.__dict__["_made"] = made
+            if self._fields() == was:  # (else another thread has set one meanwhile, and popped what was there before)
+                return made
+
+    def _fields(self):
+        return (self.n_layers, self.batch, self.n_kv_heads, self.group, self.head_dim, self.capacity, self.k_budget, self.v_bits,
+                self.in_dtype)
 
     def __getstate__(self):
         return {k: v for k, v in self.__dict__.items() if k != "_made"}
