@@ -19,6 +19,7 @@ namespace paged {
 struct Seq {
   int first, n, len;  // its tokens in the inputs, its rows (the new ones among them)
   bool ok;
+  bool taken;  // not ok, but only because an earlier sequence claims some of its tokens
 };
 __host__ __device__ __forceinline__ Seq make_seq(const PagedBatch& b, int c0, int c1, int len) {
   const auto inside = [&](int c) { return c < 0 ? 0 : c < b.n_tokens ? c : b.n_tokens; };
@@ -28,6 +29,7 @@ __host__ __device__ __forceinline__ Seq make_seq(const PagedBatch& b, int c0, in
   s.n = last > s.first ? last - s.first : 0;
   s.len = len;
   s.ok = c0 == s.first && c1 == last && c0 <= c1 && s.n <= b.max_new && len >= s.n && len <= b.max_ctx;
+  s.taken = false;
   return s;
 }
 __device__ __forceinline__ Seq seq_of(const PagedBatch& b, int s) {
@@ -61,7 +63,8 @@ struct Apart {
       upto = lane >= o ? max(upto, x) : upto;
     }
     const int x = __shfl_up(upto, 1), before = max(high, lane > 0 ? x : 0);
-    q.ok = q.ok && (q.n == 0 || c0 >= before);
+    q.taken = q.ok && q.n > 0 && c0 < before;
+    q.ok = q.ok && !q.taken;
     high = max(high, __builtin_amdgcn_readlane(upto, 63));
   }
 };
@@ -90,13 +93,13 @@ __device__ __forceinline__ int find_item(const PagedBatch& b, int want, const F&
       const int l = __builtin_ctzll(at);
       const auto of = [&](int v) { return __builtin_amdgcn_readlane(v, l); };
       number = want - (of(upto) - of(mine));
-      seq = {of(q.first), of(q.n), of(q.len), of(q.ok) != 0};
+      seq = {of(q.first), of(q.n), of(q.len), of(q.ok) != 0, of(q.taken) != 0};
       return base + l;
     }
     want -= __builtin_amdgcn_readlane(upto, 63);
   }
   number = 0;
-  seq = {0, 0, 0, false};
+  seq = {0, 0, 0, false, false};
   return -1;
 }
 
@@ -130,7 +133,7 @@ __device__ __forceinline__ int seq_of_row(const PagedBatch& b, int r0, int tk, i
       const int from = max(l, 0), first = __shfl(q.first, from), n = __shfl(q.n, from), len = __shfl(q.len, from);
       if (l >= 0) {
         at = base + l;
-        seq = {first, n, len, true};
+        seq = {first, n, len, true, false};
       }
     }
     // (what follows starts behind `high`)

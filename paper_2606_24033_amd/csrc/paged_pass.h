@@ -46,12 +46,13 @@ __device__ __forceinline__ size_t part_row(const PagedPass& p, const Unit& u, in
 }
 
 // A sequence's blocks of R query rows in the pass.  (One whose numbers make no
-// sense has one in the pass of the smallest, which answers for it.)
+// sense has one in the pass of the smallest, which answers for it, and one whose
+// tokens are taken has one in the pass of its rows.)
 template <int R>
 __device__ __forceinline__ int blocks_of(const PagedPass& p, int group, const Seq& q) {
-  if (!q.ok) return p.lo == 0 && q.n > 0 ? 1 : 0;
+  if (!q.ok && !q.taken) return p.lo == 0 && q.n > 0 ? 1 : 0;
   const int rows = q.n * group;  // (below 2^31: the host checks)
-  return rows > p.lo && rows <= p.hi ? (rows + R - 1) / R : 0;
+  return rows > p.lo && rows <= p.hi ? (q.ok ? (rows + R - 1) / R : 1) : 0;
 }
 
 template <int R>

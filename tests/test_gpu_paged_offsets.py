@@ -50,7 +50,8 @@ def faults(first, n):
 
 
 BATCHES = [([1, 1, 1, 1], [70, 66, 90, 64]), ([3, 2, 1, 4], [70, 66, 90, 64]), ([1, 60, 1, 2], [70, 130, 90, 64]),
-           ([60, 70, 80, 60], [70, 130, 90, 64])]
+           ([60, 70, 80, 60], [70, 130, 90, 64]),
+           ([1, 60, 1, 1, 1, 1], [70, 130, 90, 64, 70, 66])]  # (single tokens in a pass of their own)
 
 
 @pytest.mark.parametrize("news,lens", BATCHES)
@@ -134,7 +135,7 @@ def falls(first, n):
             cu = first.copy()
             cu[i] = x
             yield cu
-    yield np.array([0, first[1], 0, first[1], first[-1]][:len(first)], np.int32)  # the same rows twice
+    yield np.concatenate([[0, first[1], 0, first[1]], first[4:]]).astype(np.int32)  # the same rows twice
 
 
 @pytest.mark.parametrize("dtype", ["bf16", "fp32"])
