@@ -1234,12 +1234,13 @@ static PagedPlan paged_pass_plan(const Dims& d, std::initializer_list<int> width
   double t_best = 0.0;
   const int tiles = std::max(1, (max_len + 63) / 64);
   for (const int rows : widths) {
-    // a sequence's last block may be part empty; one block each at least, a refused one's too
-    const long blocks = max_rows <= rows ? n_seqs : std::min(n_seqs * ((max_rows + rows - 1) / rows), (n_rows + n_seqs * (rows - 1)) / rows);
+    // a sequence's last block may be part empty; one block each at least
+    const long seqs = std::min(n_seqs, n_rows / (lo + 1));
+    const long blocks = max_rows <= rows ? n_seqs : std::min(seqs * ((max_rows + rows - 1) / rows), (n_rows + seqs * (rows - 1)) / rows);
     const bool direct = max_rows <= rows;
     const int most = static_cast<int>(max_rows / d.group);
     const size_t part_rows = static_cast<size_t>(direct ? n_seqs * most : n_tokens) * d.n_kv * d.group;
-    const double est = d.n_kv * (direct || n_seqs == 1 ? static_cast<double>(blocks) : n_rows / rows + 0.5 * likely);
+    const double est = d.n_kv * (direct || seqs == 1 ? static_cast<double>(blocks) : n_rows / rows + 0.5 * likely);
     const int k0 = requested > 0 ? std::min(requested, tiles) : 1;
     const int k1 = requested > 0 ? k0 : std::min(rows <= 32 ? (tiles + 7) / 8 : tiles, 256);
     for (int k = k0; k <= std::max(k0, k1); ++k) {

@@ -415,17 +415,13 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(2, 2))
   int r0, kvh, split, seq0 = 0, lz = 0, layer, sub = 0, seq, nr;  // nr: query rows
   paged::Unit U = {};
   if constexpr (kPaged) {
-    if (!paged::unit_of<kRows>(mode, d, call.n_slots, item, U)) return;
+    if (!paged::find_unit<kRows>(mode, d, call, paged::unit_at(mode, d, call.n_slots, item, U), U, kThreads)) return;
     r0 = U.r0;
     kvh = U.kvh;
     split = U.split;
     layer = d.layer;
     seq = U.seq;
     nr = U.q.n * G;
-    if (!U.q.ok) {
-      if (split == 0) paged::refuse(U, d, kvh, call.out, call.out_dtype, tid, kThreads);
-      return;
-    }
   } else {
     const int n_blocks = (S.n_q * G + kRows - 1) / kRows, n_seq = (S.batch + per - 1) >> S.pack;
     r0 = item % n_blocks * kRows;

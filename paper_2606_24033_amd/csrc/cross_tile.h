@@ -70,17 +70,13 @@ __global__ __launch_bounds__(kAttnThreads) __attribute__((amdgpu_waves_per_eu(2,
   int nr, first, kvh, lz = 0, split, seq, layer;  // query rows of the unit, the workgroup's first one
   paged::Unit U = {};
   if constexpr (kPaged) {
-    if (!paged::unit_of<kWgRows>(mode, d, call.n_slots, item, U)) return;
+    if (!paged::find_unit<kWgRows>(mode, d, call, paged::unit_at(mode, d, call.n_slots, item, U), U, kAttnThreads)) return;
     nr = U.q.n * G;
     first = U.r0;
     kvh = U.kvh;
     split = U.split;
     seq = U.seq;
     layer = d.layer;
-    if (!U.q.ok) {
-      if (split == 0) paged::refuse(U, d, kvh, call.out, call.out_dtype, tid, kAttnThreads);
-      return;
-    }
   } else {
     nr = S.n_q * G;
     const int n_blocks = (nr + kWgRows - 1) / kWgRows;

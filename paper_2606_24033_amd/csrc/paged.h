@@ -28,7 +28,7 @@ __host__ __device__ __forceinline__ Seq make_seq(const PagedBatch& b, int c0, in
   const int last = inside(c1);  // (both in 0 .. n_tokens: the difference fits)
   s.n = last > s.first ? last - s.first : 0;
   s.len = len;
-  s.ok = c0 == s.first && c1 == last && c0 <= c1 && s.n <= b.max_new && len >= s.n && len <= b.max_ctx;
+  s.ok = c0 == s.first && c1 == s.first + s.n && s.n <= b.max_new && len >= s.n && len <= b.max_ctx;
   s.taken = false;
   return s;
 }
@@ -42,18 +42,18 @@ __device__ __forceinline__ int page_of(const PagedBatch& b, int n_pages, int pag
   return static_cast<uint32_t>(p) < static_cast<uint32_t>(n_pages) ? p : -1;
 }
 
-// Sequences of a wave's 64 lanes, the next ones after those of the call before:
-// one that claims inputs' rows of an earlier one is not ok either, so that the ok
-// ones share no row.  Offsets that never fall and stay inside the inputs keep
-// them apart by themselves; what it costs is a comparison and a ballot.
+// The sequences of a wave's 64 lanes, from `base` on in turn (the last one again
+// behind the end): one that claims inputs' rows of an earlier one is not ok
+// either, so that the ok ones share no row.  Offsets that never fall and stay
+// inside the inputs keep them apart by themselves; what that costs is a ballot.
 struct Apart {
   bool fell = false;  // an offset so far falls or lies outside
-  int high = 0;       // the end of the sequences so far
-  __device__ __forceinline__ void keep(const PagedBatch& b, int c0, int c1, Seq& q) {
-    fell = fell || __builtin_amdgcn_ballot_w64(c0 < 0 || c0 > c1 || c1 > b.n_tokens) != 0;
+  int high = 0;       // the end of the sequences so far, where one does
+  __device__ __forceinline__ void keep(int base, int c0, int c1, Seq& q) {
     if (!fell) {
-      high = __builtin_amdgcn_readlane(c1, 63);
-      return;
+      if (__builtin_amdgcn_ballot_w64(c0 != q.first || c1 != q.first + q.n) == 0) return;
+      fell = true;
+      high = base > 0 ? __builtin_amdgcn_readlane(c0, 0) : 0;
     }
     const int lane = threadIdx.x & 63;
     int upto = q.ok ? c1 : 0;
@@ -80,20 +80,20 @@ __device__ __forceinline__ int find_item(const PagedBatch& b, int want, const F&
   for (int base = 0; base < b.n_seqs; base += 64) {
     const int s = min(base + lane, b.n_seqs - 1), c0 = b.cu[s], c1 = b.cu[s + 1];
     Seq q = make_seq(b, c0, c1, b.ctx[s]);
-    apart.keep(b, c0, c1, q);
+    apart.keep(base, c0, c1, q);
     const int mine = base + lane < b.n_seqs ? count(q) : 0;
     int upto = mine;
 #pragma unroll
     for (int o = 1; o < 64; o *= 2) {
-      const int x = __shfl_up(upto, o);
-      upto += lane >= o ? x : 0;
+      const int y = __shfl_up(upto, o);
+      upto += lane >= o ? y : 0;
     }
     const uint64_t at = __builtin_amdgcn_ballot_w64(upto > want);
     if (at != 0) {
       const int l = __builtin_ctzll(at);
       const auto of = [&](int v) { return __builtin_amdgcn_readlane(v, l); };
       number = want - (of(upto) - of(mine));
-      seq = {of(q.first), of(q.n), of(q.len), of(q.ok) != 0, of(q.taken) != 0};
+      seq = {of(q.first), of(q.n), of(q.len), true, false};
       return base + l;
     }
     want -= __builtin_amdgcn_readlane(upto, 63);
@@ -104,49 +104,39 @@ __device__ __forceinline__ int find_item(const PagedBatch& b, int want, const F&
 }
 
 // The sequence that input row r0 + tk of a ragged batch belongs to (-1: none), r0
-// the same in the wave, tk < ROWS; rows from number `need` on are of no interest.
-// 64 sequences at a time, one ballot where one of them claims all the rows, one
-// for each row where they claim some (16384 rows of a prompt x 8 heads: 3 us less
-// than with those alone).
-template <int ROWS>
+// the same in the wave; rows from number `need` on are of no interest.  64
+// sequences at a time, then those of them that claim any of the rows.
 __device__ __forceinline__ int seq_of_row(const PagedBatch& b, int r0, int tk, int need, Seq& seq) {
   const int lane = threadIdx.x & 63, last = b.n_seqs - 1;
   int at = -1;
   Apart apart;
   for (int base = 0; base <= last; base += 64) {
-    const int s = min(base + lane, last), c0 = b.cu[s], c1 = b.cu[s + 1];
-    Seq q = make_seq(b, c0, c1, b.ctx[s]);
-    apart.keep(b, c0, c1, q);
-    const bool any = base + lane <= last && q.ok && c1 > r0 && c0 - need < r0;
-    if (__builtin_amdgcn_ballot_w64(any) != 0) {
-      const uint64_t all = __builtin_amdgcn_ballot_w64(any && c0 <= r0 && c1 - need >= r0);
-      int l = -1;
-      if (all != 0) {
-        l = __builtin_ctzll(all);
-      } else {
-#pragma unroll
-        for (int j = 0; j < ROWS; ++j) {
-          const uint64_t of = __builtin_amdgcn_ballot_w64(any && c0 <= r0 + j && r0 + j < c1);
-          l = tk == j && of != 0 ? __builtin_ctzll(of) : l;
-        }
-      }
-      const int from = max(l, 0), first = __shfl(q.first, from), n = __shfl(q.n, from), len = __shfl(q.len, from);
-      if (l >= 0) {
+    const int s = min(base + lane, last), c0 = b.cu[s], c1 = b.cu[s + 1], len = b.ctx[s];
+    Seq q = make_seq(b, c0, c1, len);
+    apart.keep(base, c0, c1, q);
+    const int end = apart.fell ? apart.high : __builtin_amdgcn_readlane(c1, 63);
+    if (end <= r0) continue;
+    const bool any = base + lane <= last && q.ok && c0 < c1 && c1 > r0 && c0 - need < r0;
+    for (uint64_t some = __builtin_amdgcn_ballot_w64(any); some != 0; some &= some - 1) {
+      const int l = __builtin_ctzll(some);
+      const int first = __builtin_amdgcn_readlane(c0, l), behind = __builtin_amdgcn_readlane(c1, l);
+      const int rows = __builtin_amdgcn_readlane(len, l);
+      if (first <= r0 + tk && r0 + tk < behind) {
         at = base + l;
-        seq = {first, n, len, true, false};
+        seq = {first, behind - first, rows, true, false};
       }
     }
-    // (what follows starts behind `high`)
-    if (__builtin_amdgcn_ballot_w64(at < 0 && tk < need) == 0 || apart.high >= r0 + need) break;
+    // (what follows starts behind `end`)
+    if (__builtin_amdgcn_ballot_w64(at < 0 && tk < need) == 0 || end >= r0 + need) break;
   }
   return at;
 }
 
-// Page (-1: none) and place of input row r0 + tk.
+// Page (-1: none) and place of input row r0 + tk, tk < ROWS.
 template <int ROWS = 16>
 __device__ __forceinline__ int2 page_of_row(const PagedBatch& b, int n_pages, int page_rows, int r0, int tk) {
   Seq q = {};
-  const int s = seq_of_row<ROWS>(b, r0, tk, ROWS, q);
+  const int s = seq_of_row(b, r0, tk, ROWS, q);
   if (s < 0) return make_int2(-1, 0);
   const int t = q.len - q.n + r0 + tk - q.first;
   return make_int2(page_of(b, n_pages, page_rows, s, t), t % page_rows);

@@ -24,7 +24,7 @@ struct TokenRows {
   __device__ __forceinline__ bool begin(long r0) {
     const int tk = threadIdx.x & 15, t0 = static_cast<int>(r0 / hq), need = static_cast<int>((r0 + RW - 1) / hq) - t0 + 1;
     paged::Seq q = {};
-    const int s = paged::seq_of_row<16>(pass.b, t0, tk, need, q), rows = q.n * group;
+    const int s = paged::seq_of_row(pass.b, t0, tk, need, q), rows = q.n * group;
     const uint64_t live = __builtin_amdgcn_ballot_w64(s >= 0 && rows > pass.lo && rows <= pass.hi);
     const long r = r0 + tk;
     mine = tk < RW && (live >> static_cast<int>(r / hq - t0) & 1) ? r : -1;

@@ -175,11 +175,7 @@ __attribute__((amdgpu_waves_per_eu((waves_of<NSET, KWB>() / 4)))) void k_paged_d
     gpos[g] = g < ng ? b : kHeadDim;
     used |= (M->gm[g] >> 31) << g;
   }
-  if (!paged::find_block<8>(mode, G, block, U)) return;
-  if (!U.q.ok) {
-    if (U.split == 0) paged::refuse(U, d, U.kvh, call.out, call.out_dtype, tid, kThreads);
-    return;
-  }
+  if (!paged::find_unit<8>(mode, d, call, block, U, kThreads)) return;
   const int kvh = U.kvh, split = U.split;
   const size_t out_row = static_cast<size_t>(U.q.first) * hq + kvh * G;  // head 0's row of q and out
   const int t_begin = split * S.split_len, t_end = min(U.q.len, t_begin + S.split_len), pos = U.q.len - 1;

@@ -45,28 +45,17 @@ __device__ __forceinline__ size_t part_row(const PagedPass& p, const Unit& u, in
   return (p.direct ? static_cast<size_t>(u.seq) * p.most + i : static_cast<size_t>(u.q.first + i)) * hq + head;
 }
 
-// A sequence's blocks of R query rows in the pass.  (One whose numbers make no
-// sense has one in the pass of the smallest, which answers for it, and one whose
-// tokens are taken has one in the pass of its rows.)
+// A sequence's blocks of R query rows in the pass.
 template <int R>
 __device__ __forceinline__ int blocks_of(const PagedPass& p, int group, const Seq& q) {
-  if (!q.ok && !q.taken) return p.lo == 0 && q.n > 0 ? 1 : 0;
   const int rows = q.n * group;  // (below 2^31: the host checks)
-  return rows > p.lo && rows <= p.hi ? (q.ok ? (rows + R - 1) / R : 1) : 0;
+  return q.ok && rows > p.lo && rows <= p.hi ? (rows + R - 1) / R : 0;
 }
 
-template <int R>
-__device__ __forceinline__ bool find_block(const PagedPass& p, int group, int block, Unit& u) {
-  if (p.direct) {  // no sequence has more than one block
-    u.seq = block;
-    u.q = seq_of(p.b, block);
-    u.r0 = 0;
-    return blocks_of<R>(p, group, u.q) > 0;
-  }
-  int number;
-  u.seq = find_item(p.b, block, [&](const Seq& q) { return blocks_of<R>(p, group, q); }, number, u.q);
-  u.r0 = number * R;
-  return u.seq >= 0;
+// Whether the pass answers for a refused sequence: that of the smallest, or, of
+// one whose tokens are taken, that of its rows.
+__device__ __forceinline__ bool answers(const PagedPass& p, int group, const Seq& q) {
+  return !q.ok && q.n > 0 && (q.taken ? q.n * group > p.lo && q.n * group <= p.hi : p.lo == 0);
 }
 
 // KV heads vary fastest, then splits: the workgroups of a block go to all XCDs,
@@ -78,20 +67,62 @@ __device__ __forceinline__ int unit_at(const PagedPass& p, const Dims& d, int n_
   u.split = item % n_splits;
   return p.n_blocks - 1 - item / n_splits;
 }
-template <int R>
-__device__ __forceinline__ bool unit_of(const PagedPass& p, const Dims& d, int n_splits, int item, Unit& u) {
-  return find_block<R>(p, d.group, unit_at(p, d, n_splits, item, u), u);
-}
 
 // The rows of a sequence that a call cannot answer for are not numbers.
-__device__ __forceinline__ void refuse(const Unit& u, const Dims& d, int kvh, void* out, int out_dtype, int tid, int threads) {
+__device__ __forceinline__ void refuse(const Seq& q, const Dims& d, int kvh, const CrossCall& call, int tid, int threads) {
   const int per = d.group * kHeadDim;
   const size_t stride = static_cast<size_t>(d.n_kv) * per;
-  for (long i = tid; i < static_cast<long>(u.q.n) * per; i += threads) {
-    const size_t at = (u.q.first + i / per) * stride + static_cast<size_t>(kvh) * per + i % per;
-    if (out_dtype == 1) static_cast<uint16_t*>(out)[at] = 0x7FC0;
-    else static_cast<float*>(out)[at] = __builtin_nanf("");
+  for (long i = tid; i < static_cast<long>(q.n) * per; i += threads) {
+    const size_t at = (q.first + i / per) * stride + static_cast<size_t>(kvh) * per + i % per;
+    if (call.out_dtype == 1) static_cast<uint16_t*>(call.out)[at] = 0x7FC0;
+    else static_cast<float*>(call.out)[at] = __builtin_nanf("");
   }
+}
+
+// Refused sequences of a pass whose blocks are numbered over all sequences: they
+// have none, for the list to stay within the grid whatever the offsets say.
+// Block 0's workgroups answer for them: a wave looks at every threads / 64-th 64
+// sequences, and goes through all of them where it finds one that is at fault.
+__device__ __forceinline__ void answer_refused(const PagedPass& p, const Dims& d, int kvh, const CrossCall& call, int threads) {
+  const PagedBatch& b = p.b;
+  const int lane = threadIdx.x & 63;
+  bool fault = false;
+  for (int base = threadIdx.x & ~63; base < b.n_seqs; base += threads) {
+    const int s = min(base + lane, b.n_seqs - 1), c0 = b.cu[s], c1 = b.cu[s + 1];
+    const Seq q = make_seq(b, c0, c1, b.ctx[s]);
+    fault = fault || c0 != q.first || c1 != q.first + q.n || answers(p, d.group, q);
+  }
+  if (__builtin_amdgcn_ballot_w64(fault) == 0) return;
+  Apart apart;
+  for (int base = 0; base < b.n_seqs; base += 64) {
+    const int s = min(base + lane, b.n_seqs - 1), c0 = b.cu[s], c1 = b.cu[s + 1];
+    Seq q = make_seq(b, c0, c1, b.ctx[s]);
+    apart.keep(base, c0, c1, q);
+    for (uint64_t some = __builtin_amdgcn_ballot_w64(base + lane < b.n_seqs && answers(p, d.group, q)); some != 0; some &= some - 1) {
+      const int l = __builtin_ctzll(some);
+      const Seq one = {__builtin_amdgcn_readlane(q.first, l), __builtin_amdgcn_readlane(q.n, l), 0, false, false};
+      refuse(one, d, kvh, call, lane, 64);
+    }
+  }
+}
+
+// The unit of a block (unit_at), with whole waves; false: it has no rows.  (Blocks
+// of 8 rows are single tokens', always direct.)
+template <int R>
+__device__ __forceinline__ bool find_unit(const PagedPass& p, const Dims& d, const CrossCall& call, int block, Unit& u, int threads) {
+  if (R == 8 || p.direct) {  // no sequence has more than one block
+    u.seq = block;
+    u.q = seq_of(p.b, block);
+    u.r0 = 0;
+    if (u.split == 0 && answers(p, d.group, u.q)) refuse(u.q, d, u.kvh, call, threadIdx.x, threads);
+    return blocks_of<R>(p, d.group, u.q) > 0;
+  }
+  if constexpr (R == 8) return false;
+  if (block == 0 && u.split == 0) answer_refused(p, d, u.kvh, call, threads);
+  int number;
+  u.seq = find_item(p.b, block, [&](const Seq& q) { return blocks_of<R>(p, d.group, q); }, number, u.q);
+  u.r0 = number * R;
+  return u.seq >= 0;
 }
 
 // What new token i of a sequence sees: rows [0, end(i)), end never falls.

@@ -207,3 +207,22 @@ def test_hundreds_of_sequences(rotations, news, splits):
     live = int(b.first[-1])
     check(f"{len(news)} sequences", got[:live], ref[:live], bound[:live])
     assert (got[live:] == 7.0).all()
+
+
+@pytest.mark.parametrize("splits", [0, 1, 2])
+def test_more_claims_than_blocks_of_rows(rotations, splits):
+    """The same 40 rows claimed a hundred times, then five others: the first claimant's or not numbers, and the five right."""
+    claimants = 100
+    pool = Packed(rotations, 12, batch=5, kv=1, group=8, cap=64)
+    b = Batch(pool, [40, 5], [90, 70], seed=2)
+    q, dq = pool.queries((b.n,))
+    ref, bound = expect(b, q, torch.float32)
+    cu = np.array([0, 40] * claimants + [45], np.int32)
+    lens = [90, 90] * (claimants - 1) + [90, 70]
+    table = np.concatenate([np.repeat(b.table[:1], len(lens) - 1, 0), b.table[1:]])
+    chunk = bg.Chunk(i32(cu), i32(lens), i32(table), 40, 90)
+    got = torch.full((b.n, 8, D), 7.0, device="cuda")
+    bg.blockgtq_paged_attn(pool.cfg, pool.layout, 0, dq, chunk, pool.cache, out=got, n_splits=splits)
+    check("the five", got[40:], ref[40:], bound[40:])
+    near = np.isnan(got[:40].cpu().numpy()) | (np.abs(got[:40].double().cpu().numpy() - ref[:40]) <= bound[:40])
+    assert near.all()
