@@ -449,7 +449,10 @@ typedef struct {
  * d_q_weight, d_k_weight: float [128], or NULL: that side is only rotated.
  * eps: finite, >= 0.  (A row of zeros with eps = 0 gives not a number.)
  * Rows, outputs and weights start 16-byte aligned, strides included (EINVAL
- * otherwise); a stride is at least the heads' elements. */
+ * otherwise); a stride is at least the heads' elements.
+ * EUNSUPPORTED above 2^20 query heads, or 2^26 groups of up to 8 heads (n_tokens x
+ * the groups of the query and of the key heads).  Squares are summed in fp32: a
+ * head is normed while those of its largest elements are fp32 numbers. */
 int blockgtq_norm_rope(const bgtq_config* cfg, const bgtq_rope* rope, int32_t n_tokens, const void* d_q,
                        int64_t q_stride, const void* d_k, int64_t k_stride, const int32_t* d_pos,
                        const float* d_q_weight, const float* d_k_weight, float eps, void* d_q_out,
@@ -496,7 +499,8 @@ typedef struct {
  * included (EINVAL otherwise).  layer in [0, n_layers).  A row whose page number
  * is outside [0, cfg->batch) is dropped (the attention over it gives NaN).  Pages
  * that a call writes belong to one of its sequences each.  Async on `stream`, one
- * launch, no allocation, no workspace. */
+ * launch, no allocation, no workspace.  EUNSUPPORTED as blockgtq_paged_attn of the
+ * same chunk (2^24 query rows, 2^30 rows), or above 65535 KV heads. */
 int blockgtq_paged_append(const bgtq_config* cfg, const void* d_layout, int32_t layer, const void* d_k,
                           int64_t k_stride, const void* d_v, int64_t v_stride, const bgtq_chunk* chunk,
                           const bgtq_cache* cache, void* stream);
@@ -526,10 +530,10 @@ typedef struct {
  * A page number outside [0, cfg->batch) makes NaN of every output that attends
  * the page's rows, and may of the sequence's other ones in this call.  What
  * the cache holds in rows that a token does not see (not a number or infinite
- * radii too) does not enter its outputs, but for one rounding: long chunks scale
- * all rows' fp16 parts by a power of two that the largest finite radius so far
- * sets, also one that only later tokens see, and hold a coordinate to 2^-37 of
- * what that radius gives.  A radius that is not finite in a row that a token sees
+ * radii too) does not enter its outputs, but for one rounding: the passes of
+ * several tokens scale all rows' fp16 parts by a power of two that the largest
+ * finite radius so far sets, also one that only later tokens see, and hold a
+ * coordinate to 2^-37 of what that radius gives.  A radius that is not finite in a row that a token sees
  * makes its outputs NaN.
  * n_splits: 0 = heuristic, else the splits of the key axis (1 .. 4096).  A pass
  *      in splits leaves a partial of 528 bytes for each query row and split (the

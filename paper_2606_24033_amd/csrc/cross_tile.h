@@ -14,9 +14,11 @@
 // three fp16 products and PV one (two for fp32 outputs) where fp16 attention
 // takes two in all.  A 64-row tile takes 2.75 us for 256 query rows with few CUs
 // busy, 3.65 with all.  2 x 8 heads x 2048 query positions on 16385 K3V3 rows: 521 us
-// a call, 527 TFLOP/s.  256 or 128 rows: the former pay less decode, the latter
-// give twice the workgroups (32768 rows, 8 KV heads, in us for 128 / 256: 128 query
-// rows a head 71 / 86, 512 171 / 155, 2048 614 / 497).
+// a call, 527 TFLOP/s.  An 8192-token prompt over pages, 8 KV heads x 4 query heads,
+// causal: 1092 us, matrix cores and vector instructions 51 % busy each.  256 or 128
+// rows: the former pay less decode, the latter give twice the workgroups (32768
+// rows, 8 KV heads, in us for 128 / 256: 128 query rows a head 71 / 86, 512 171 /
+// 155, 2048 614 / 497).
 #pragma once
 #include <hip/hip_runtime.h>
 

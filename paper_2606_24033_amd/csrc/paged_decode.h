@@ -16,10 +16,10 @@
 //    packed decode's no-NaN flags);
 //  * splits leave partials for a join instead of counting one another.
 //
-// What bounds it: vector instructions, 565 a 64-row tile with 16 waves, and the
+// What bounds it: vector instructions, some 560 a 64-row tile with 16 waves, and the
 // set-up (10 us: the sequence's numbers, then its first page, then rows; rotation
 // and tables meanwhile).  32 sequences of 500 to 8200 K2V2 rows x 8 KV heads x 4:
-// 46 us, decided by the longest (107 in 32-row workgroups, 55 with a set-up that
+// 47 us, decided by the longest (107 in 32-row workgroups, 55 with a set-up that
 // waits for each read in turn); one sequence of 500 rows 14.
 #pragma once
 #include <hip/hip_runtime.h>

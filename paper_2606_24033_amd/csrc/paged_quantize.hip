@@ -16,8 +16,8 @@
 // products of the rows' squares with the groups' members, exact terms as well.
 //
 // What bounds it: a wave's chain of reads, products and comparisons, four of
-// them to a SIMD (vector instructions 74 %, matrix cores 29 % of the time that a
-// CU is busy).  16384 rows x 8 heads of K2V2: 49 us (fp32 products 127; fp32 radii,
+// them to a SIMD (vector instructions 74 %, matrix cores 30 % of the time that a
+// CU is busy).  16384 rows x 8 heads of K2V2: 47 us (fp32 products 127; fp32 radii,
 // half of the workgroups for each side and a wave's rows read when it needs them
 // 61); 65536 rows 178; 4096 rows 21 (32 with all of a workgroup's waves busy
 // before the next one starts); up to 1000 rows 16.

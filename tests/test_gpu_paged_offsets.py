@@ -226,3 +226,17 @@ def test_more_claims_than_blocks_of_rows(rotations, splits):
     check("the five", got[40:], ref[40:], bound[40:])
     near = np.isnan(got[:40].cpu().numpy()) | (np.abs(got[:40].double().cpu().numpy() - ref[:40]) <= bound[:40])
     assert near.all()
+
+
+@pytest.mark.parametrize("news,lens", [([3] * 5, [70, 66, 90, 64, 66]), ([9] * 5, [70, 66, 90, 64, 66]), ([9] * 5, [70, 128, 90, 64, 66]),
+                                       ([1] * 5, [70, 65, 90, 64, 66])])
+@pytest.mark.parametrize("bad", [14, -1, HI, LO])
+def test_append_without_a_page(rotations, news, lens, bad):
+    """Rows whose page the pool does not have are dropped; those on the sequence's other page arrive, and the others'."""
+    a = Appends(rotations, news, lens, "bf16")
+    full, table = a.run(a.b.first), a.b.table.copy()
+    a.b.table[1, 1] = bad
+    got = a.run(a.b.first)
+    for s in range(len(lens)):
+        for i, p in enumerate(table[s, :a.b.per[s]]):
+            assert a.pages_equal(got, a.start if (s, i) == (1, 1) else full, [p]), (s, i)
