@@ -83,6 +83,8 @@ __device__ __forceinline__ void refuse(const Seq& q, const Dims& d, int kvh, con
 // have none, for the list to stay within the grid whatever the offsets say.
 // Block 0's workgroups answer for them: a wave looks at every threads / 64-th 64
 // sequences, and goes through all of them where it finds one that is at fault.
+// (Rows next to or among those that it has written once are not written again:
+// numbers of all sizes, as uninitialized ones, claim every row over and over.)
 __device__ __forceinline__ void answer_refused(const PagedPass& p, const Dims& d, int kvh, const CrossCall& call, int threads) {
   const PagedBatch& b = p.b;
   const int lane = threadIdx.x & 63;
@@ -94,14 +96,29 @@ __device__ __forceinline__ void answer_refused(const PagedPass& p, const Dims& d
   }
   if (__builtin_amdgcn_ballot_w64(fault) == 0) return;
   Apart apart;
+  int done0 = 0, done1 = 0;
+  const auto write = [&](int from, int to) {
+    if (from < to) refuse({from, to - from, 0, false, false}, d, kvh, call, lane, 64);
+  };
   for (int base = 0; base < b.n_seqs; base += 64) {
     const int s = min(base + lane, b.n_seqs - 1), c0 = b.cu[s], c1 = b.cu[s + 1];
     Seq q = make_seq(b, c0, c1, b.ctx[s]);
     apart.keep(base, c0, c1, q);
     for (uint64_t some = __builtin_amdgcn_ballot_w64(base + lane < b.n_seqs && answers(p, d.group, q)); some != 0; some &= some - 1) {
       const int l = __builtin_ctzll(some);
-      const Seq one = {__builtin_amdgcn_readlane(q.first, l), __builtin_amdgcn_readlane(q.n, l), 0, false, false};
-      refuse(one, d, kvh, call, lane, 64);
+      const int from = __builtin_amdgcn_readlane(q.first, l), to = from + __builtin_amdgcn_readlane(q.n, l);
+      if (done0 < done1 && from <= done1 && to >= done0) {
+        write(from, min(to, done0));
+        write(max(from, done1), to);
+        done0 = min(done0, from);
+        done1 = max(done1, to);
+      } else {
+        write(from, to);
+        if (to - from > done1 - done0) {
+          done0 = from;
+          done1 = to;
+        }
+      }
     }
   }
 }

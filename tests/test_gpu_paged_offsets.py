@@ -240,3 +240,43 @@ def test_append_without_a_page(rotations, news, lens, bad):
     for s in range(len(lens)):
         for i, p in enumerate(table[s, :a.b.per[s]]):
             assert a.pages_equal(got, a.start if (s, i) == (1, 1) else full, [p]), (s, i)
+
+
+@pytest.mark.parametrize("n_seqs", [3, 70, 700])
+@pytest.mark.parametrize("max_new", [1, 3, 90])
+@pytest.mark.parametrize("kind", ["any", "inside", "edges"])
+def test_offsets_without_any_sense(rotations, kind, max_new, n_seqs):
+    """Numbers of every size: rows that nobody claims stay as they were, rows that only refused sequences claim are not
+    numbers, the others are or are finite; the pool's pages change only where a sequence's numbers stand."""
+    rng = np.random.default_rng([n_seqs, max_new, len(kind)])
+    pool = Packed(rotations, 15, batch=4, kv=2, group=4, cap=64)
+    n, ctx, around = 90, 120, 50
+    q = torch.from_numpy(synth.cast(rng.standard_normal((n, 8, D)), "bf16")).to(torch.bfloat16).cuda()
+    for trial in range(6):
+        cu = {"any": lambda: rng.integers(LO, HI, n_seqs + 1), "inside": lambda: rng.integers(0, n + 1, n_seqs + 1),
+              "edges": lambda: rng.choice([LO, -1, 0, 1, 2, 3, 44, n - 1, n, n + 1, HI], n_seqs + 1)}[kind]().astype(np.int32)
+        lens = rng.choice([ctx, ctx, ctx, ctx + 1, -1, 2], n_seqs).astype(np.int32)
+        print(f"{kind} {n_seqs} sequences, at most {max_new} new, trial {trial}: {cu[:12].tolist()}", flush=True)
+        chunk = bg.Chunk(i32(cu), i32(lens), i32(np.tile([[1, 3]], (n_seqs, 1))), max_new, ctx)
+        told = claims(cu, lens, n, max_new, ctx)
+        right, gone = np.zeros(n, bool), np.zeros(n, bool)
+        for rows, fine in told:
+            (right if fine else gone)[rows.start:rows.stop] = True
+        for splits in (0, 2):
+            whole = torch.full((n + 2 * around, 8, D), 7.0, device="cuda")
+            bg.blockgtq_paged_attn(pool.cfg, pool.layout, 0, q, chunk, pool.cache, out=whole[around:around + n], n_splits=splits)
+            x = whole.cpu().numpy()
+            assert (x[:around] == 7.0).all() and (x[around + n:] == 7.0).all()
+            x = x[around:around + n]
+            assert (x[~right & ~gone] == 7.0).all()
+            assert np.isnan(x[gone & ~right]).all()
+            assert (x[right] != 7.0).all() and not np.isinf(x[right]).any()
+    before = raw(pool.cache)
+    kv = torch.randn((n, 2, 2, D), device="cuda").to(torch.bfloat16)
+    chunk = bg.Chunk(i32(cu), i32(np.full(n_seqs, -1)), i32(np.tile([[1, 3]], (n_seqs, 1))), max_new, ctx)
+    bg.blockgtq_paged_append(pool.cfg, pool.layout, 0, kv[:, 0], kv[:, 1], chunk, pool.cache)
+    assert all(torch.equal(a, c) for a, c in zip(raw(pool.cache), before))
+    # pages outside the pool: nothing to write, whatever the offsets
+    chunk = bg.Chunk(i32(cu), i32(np.full(n_seqs, ctx)), i32(np.tile([[4, -1]], (n_seqs, 1))), max_new, ctx)
+    bg.blockgtq_paged_append(pool.cfg, pool.layout, 0, kv[:, 0], kv[:, 1], chunk, pool.cache)
+    assert all(torch.equal(a, c) for a, c in zip(raw(pool.cache), before))
